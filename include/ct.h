@@ -481,6 +481,106 @@ ct_status ct_copy_activation(ct_model *m, int32_t slot, int32_t batch, void *dat
  * bounded wait expired).  Synchronises the model's device. */
 ct_status ct_device_error(ct_model *m, uint32_t *code);
 
+/* ---------------------------------------------------------------------------
+ * The 8-bit answer head: operators on caller-owned device tensors, without a
+ * model.  They run a network's last, wide layers in 8-bit floating point and
+ * read its answer from the logits.  They launch on the CURRENT device (the
+ * pointers' device), asynchronously on `stream`, allocate nothing and keep
+ * nothing between calls; any number of host threads may call them at once.
+ * Matrices are row-major with a row pitch (`ld...`, in elements) and unit
+ * column stride.  A dimension of 0 is valid: nothing is read, and what has
+ * no elements is not written.  Outputs must not overlap inputs unless
+ * stated.  Results do not depend on the stream, the launch or the run: the
+ * same inputs give the same bits. */
+typedef enum { CT_DT_F32 = 0, CT_DT_F16 = 1, CT_DT_BF16 = 2 } ct_dtype;
+
+/* ct_fp8_quantize -- x [m, k] (dtype: ct_dtype, pitch ldx) to 8-bit floating
+ * point (e4m3: 3 mantissa bits, largest value 448, no infinity) with one FP32
+ * scale for each block of 128 columns (the last may be shorter) by
+ * block_rows rows: block_rows = 1 for activations, 128 for weights.  The
+ * scale of a block is the least power of two 2^e, e >= -126, that brings the
+ * largest magnitude of its finite values to at most 448, or 1 if they are
+ * all 0; q = x / scale rounded to nearest, ties to even (one rounding: the
+ * division is exact).  A NaN or infinity becomes NaN.
+ *   q_dev      uint8 [m, k], pitch ldq (the products want a multiple of 16
+ *              and a 16-byte aligned base; the columns from k on are not
+ *              written).
+ *   scale_dev  FP32: row block i, column block b at i * scale_row + b * scale_blk.
+ * Errors: CT_EINVAL (dtype, block_rows, null pointer, pitch below k,
+ * misaligned pointer), CT_ERANGE (negative or too large a size), CT_ECUDA. */
+ct_status ct_fp8_quantize(const void *x_dev, int32_t dtype, int64_t m, int64_t k, int64_t ldx, int32_t block_rows,
+                          uint8_t *q_dev, int64_t ldq, float *scale_dev, int64_t scale_row, int64_t scale_blk,
+                          void *stream);
+
+/* ct_fp8_matmul -- y = act(x w^T + bias) for 8-bit operands (as
+ * ct_fp8_quantize writes them, or any e4m3 values with any finite FP32
+ * scales):
+ *   y[m, n] = act( sum_b xs[m, b] ws[n / 128, b] sum_{k in block b} xq[m, k] wq[n, k] + bias[n] )
+ * on the tcgen05 tensor cores, with the scaled block sums and the rest in FP32
+ * and one rounding to y's type.  act: ReLU that keeps NaN (relu != 0), or
+ * none.  bias_dev: FP32 [n] or NULL.
+ *   x_dev uint8 [m, k], pitch ldx; its scales at row * x_scale_row + block * x_scale_blk.
+ *   w_dev uint8 [n, k], pitch ldw; its scales at (row / 128) * w_scale_row + block * w_scale_blk.
+ * Bases must be 16-byte aligned and pitches multiples of 16 (the copy
+ * engine's rule); k, m and n are free.  k = 0 gives act(bias).
+ * A layer's input gradient is the same call with the gradient as x and the
+ * transposed weights and weight scales as w.
+ * Errors: CT_EINVAL (dtype, null or misaligned pointer, pitch), CT_ERANGE,
+ * CT_ECUDA.  A bounded wait that expires is reported by ct_ops_device_error. */
+ct_status ct_fp8_matmul(const uint8_t *x_dev, int64_t ldx, const float *x_scale_dev, int64_t x_scale_row,
+                        int64_t x_scale_blk, const uint8_t *w_dev, int64_t ldw, const float *w_scale_dev,
+                        int64_t w_scale_row, int64_t w_scale_blk, const float *bias_dev, int32_t relu, void *y_dev,
+                        int32_t y_dtype, int64_t ldy, int64_t m, int64_t n, int64_t k, void *stream);
+
+/* ct_fp8_linear -- a fully-connected layer with 8-bit weights on unquantised
+ * activations: ct_fp8_quantize of x (blocks of 1 x 128) and ct_fp8_matmul,
+ * with the same results.  workspace_dev (16-byte aligned, at least
+ * ct_fp8_linear_workspace(m, k) bytes) is scratch that must not be used by
+ * other work until this call's stream work is done.
+ * Errors: those of the two calls; CT_ENOMEM for too small a workspace. */
+ct_status ct_fp8_linear_workspace(int64_t m, int64_t k, size_t *bytes);
+ct_status ct_fp8_linear(const void *x_dev, int32_t x_dtype, int64_t ldx, const uint8_t *w_dev, int64_t ldw,
+                        const float *w_scale_dev, int64_t w_scale_row, int64_t w_scale_blk, const float *bias_dev,
+                        int32_t relu, void *y_dev, int32_t y_dtype, int64_t ldy, int64_t m, int64_t n, int64_t k,
+                        void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* ct_logprobs -- what the rows of logits [rows, vocab] (dtype, pitch ld)
+ * answer, read once, sums in FP32:
+ *   logprob_dev  FP32 [rows] or NULL: log softmax(row)[ids_dev[row]];
+ *   entropy_dev  FP32 [rows]: -sum p log p (natural logarithm);
+ *   lse_dev      FP32 [rows]: log sum e^logit;
+ *   top_id_dev, top_logprob_dev  int64 / FP32 [rows, top_k]: the most probable
+ *     tokens, the lower index first among equal logits (top_k <= CT_MAX_TOP_K).
+ * ids_dev: int64 [rows].  -1: the row has no given token, logprob 0; any
+ * other id outside [0, vocab): logprob NaN.
+ * Logits of -inf are tokens that cannot occur: probability 0, log
+ * probability -inf, never among the top; missing top slots hold id -1 and
+ * -inf.  A row with nothing left (or vocab = 0): lse -inf, entropy 0.  A row with
+ * a NaN or +inf logit: every number NaN, every top id -1.
+ * Errors: CT_EINVAL, CT_ERANGE (sizes, top_k), CT_ECUDA. */
+#define CT_MAX_TOP_K 32
+ct_status ct_logprobs(const void *logits_dev, int32_t dtype, int64_t ld, const int64_t *ids_dev, int64_t rows,
+                      int64_t vocab, int32_t top_k, float *logprob_dev, float *entropy_dev, float *lse_dev,
+                      float *top_logprob_dev, int64_t *top_id_dev, void *stream);
+
+/* ct_logprobs_grad -- gradient of sum_r g_logprob[r] logprob[r] + g_entropy[r]
+ * entropy[r] with respect to the logits:
+ *   dlogits[r, j] = g_logprob ([j = id] - p_j) - g_entropy p_j (log p_j + entropy),
+ * rounded once to the logits' type (dlogits_dev: dtype, pitch ld_d; it may
+ * be logits_dev itself with the same pitch).  lse_dev and entropy_dev are
+ * ct_logprobs' outputs.  g_logprob_dev or g_entropy_dev may be NULL (zero;
+ * ids_dev or entropy_dev then too).  0 for tokens that cannot occur; id -1:
+ * no g_logprob term; NaN where the row's lse is NaN or its id is out of range.
+ * Errors: CT_EINVAL, CT_ERANGE, CT_ECUDA. */
+ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, const int64_t *ids_dev, int64_t rows,
+                           int64_t vocab, const float *lse_dev, const float *entropy_dev, const float *g_logprob_dev,
+                           const float *g_entropy_dev, void *dlogits_dev, int64_t ld_d, void *stream);
+
+/* ct_ops_device_error -- reads and clears the current device's error word of
+ * these operators (set by a product whose bounded wait expired: its output
+ * is then invalid).  Synchronises the device. */
+ct_status ct_ops_device_error(uint32_t *code);
+
 void ct_destroy(ct_model *m);
 const char *ct_strerror(ct_status s);
 

@@ -40,9 +40,13 @@ EXPORTS = ["ct_build", "ct_set_threshold", "ct_get_threshold", "ct_infer", "ct_i
            "ct_fi_threshold",
            "ct_copy_activation", "ct_device_error", "ct_destroy", "ct_strerror",
            "ct_reexecute_noalloc", "ct_campaign_batched", "ct_resolve_roles",
-           "ct_reexecute_prepare", "ct_infer_batches", "ct_run_host_batches"]
+           "ct_reexecute_prepare", "ct_infer_batches", "ct_run_host_batches",
+           "ct_fp8_quantize", "ct_fp8_matmul", "ct_fp8_linear", "ct_fp8_linear_workspace",
+           "ct_logprobs", "ct_logprobs_grad", "ct_ops_device_error"]
 
 CT_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
+CT_DT_F32, CT_DT_F16, CT_DT_BF16 = 0, 1, 2
+CT_MAX_TOP_K = 32
 
 
 class CtError(RuntimeError):
@@ -113,6 +117,14 @@ def lib():
             "ct_reexecute_prepare": [vp, i32],
             "ct_infer_batches": [vp, i32, i32, P(vp), P(vp), P(vp), P(vp), P(i32), vp],
             "ct_run_host_batches": [vp, i32, i32, P(vp), P(vp), P(vp), P(vp), P(i32), vp],
+            "ct_fp8_quantize": [vp, i32, i64, i64, i64, i32, vp, i64, vp, i64, i64, vp],
+            "ct_fp8_matmul": [vp, i64, vp, i64, i64, vp, i64, vp, i64, i64, vp, i32, vp, i32, i64, i64, i64, i64, vp],
+            "ct_fp8_linear": [vp, i32, i64, vp, i64, vp, i64, i64, vp, i32, vp, i32, i64, i64, i64, i64, vp,
+                              ctypes.c_size_t, vp],
+            "ct_fp8_linear_workspace": [i64, i64, P(ctypes.c_size_t)],
+            "ct_logprobs": [vp, i32, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp],
+            "ct_logprobs_grad": [vp, i32, i64, vp, i64, i64, vp, vp, vp, vp, vp, i64, vp],
+            "ct_ops_device_error": [P(ctypes.c_uint32)],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -439,3 +451,237 @@ def ct_device_error(m: Model) -> int:
 
 def ct_destroy(m: Model):
     m.close()
+
+
+# ---------------------------------------------------------------------------
+# The 8-bit answer head: operators on PyTorch CUDA tensors, without a model.
+#
+# Tensors are checked here (device, type, shape, unit column stride) and
+# passed on with their row pitches; ValueError names the offending argument.
+# Outputs that are not given are allocated on the call's stream.  `stream`:
+# None (the current one), a torch stream, or a raw cudaStream_t; inputs made
+# on another stream must be ordered before it by the caller, as for any
+# PyTorch kernel.
+# ---------------------------------------------------------------------------
+_DTYPES = None
+
+
+def _dtypes():
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: CT_DT_F32, torch.float16: CT_DT_F16, torch.bfloat16: CT_DT_BF16}
+    return _DTYPES
+
+
+def _on_stream(stream):
+    """Context in which torch allocates on `stream` (None: the current one)."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream)
+    return torch.cuda.stream(stream)
+
+
+def _matrix(t, name, dtypes, shape=None, device=None):
+    """Row pitch of a 2-D CUDA tensor with unit column stride."""
+    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
+        raise ValueError("%s: a 2-D CUDA tensor of %s is wanted, got %s %s on %s"
+                         % (name, "/".join(str(d) for d in dtypes), t.dtype, tuple(t.shape), t.device))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s: shape %s is wanted, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if device is not None and t.device != device:
+        raise ValueError("%s is on %s, the other tensors on %s" % (name, t.device, device))
+    rows, cols = t.shape
+    s0, s1 = t.stride()
+    if cols > 1 and s1 != 1:
+        raise ValueError("%s: its columns must be contiguous (strides %s)" % (name, t.stride()))
+    return s0 if rows > 1 else max(s0, cols)
+
+
+def _vector(t, name, dtype, n, device):
+    if t.dim() != 1 or t.dtype != dtype or t.device != device or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError("%s: a contiguous %s tensor of %d values on %s is wanted, got %s %s on %s"
+                         % (name, dtype, n, device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _scales(t, name, shape, device):
+    import torch
+    if t.dtype != torch.float32 or t.shape != shape or t.device != device:
+        raise ValueError("%s: a float32 tensor of shape %s on %s is wanted, got %s %s on %s"
+                         % (name, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _fp8_weights(wq, ws, k, device):
+    """Pointer arguments of 8-bit weights [n, k] and their scales."""
+    import torch
+    ldw = _matrix(wq, "wq", (torch.float8_e4m3fn, torch.uint8), None, device)
+    n = wq.shape[0]
+    if wq.shape[1] != k:
+        raise ValueError("wq has %d columns, the activations %d" % (wq.shape[1], k))
+    return (wq.data_ptr(), ldw) + _scales(ws, "ws", ((n + 127) // 128, (k + 127) // 128), device)
+
+
+def _fp8_out(out, out_dtype, m, n, device, stream):
+    import torch
+    if out is None:
+        if out_dtype not in _dtypes():
+            raise ValueError("out_dtype: float32, float16 or bfloat16 is wanted, got %s" % out_dtype)
+        with _on_stream(stream):
+            out = torch.empty(m, n, dtype=out_dtype, device=device)
+        return out, n
+    if out_dtype is not None and out.dtype != out_dtype:
+        raise ValueError("out is %s, out_dtype %s" % (out.dtype, out_dtype))
+    return out, _matrix(out, "out", _dtypes(), (m, n), device)
+
+
+def ct_fp8_quantize(x, block_rows: int = 1, q=None, scale=None, stream=None):
+    """(q, scale): x [m, k] in e4m3 with one power-of-two scale for each
+    block of block_rows x 128 values (1: activations, 128: weights).  q
+    [m, k] float8_e4m3fn has a row pitch that is a multiple of 16 bytes, as the
+    products want it; scale is float32 [ceil(m / block_rows), ceil(k / 128)]."""
+    import torch
+    ldx = _matrix(x, "x", _dtypes())
+    m, k = x.shape
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows is 1 or 128, got %r" % (block_rows,))
+    rows, kb = (m + block_rows - 1) // block_rows, (k + 127) // 128
+    with _on_stream(stream):
+        if q is None:
+            pitch = (k + 15) // 16 * 16
+            q = torch.empty(m, pitch, dtype=torch.float8_e4m3fn, device=x.device)
+            if pitch != k:
+                q = q[:, :k]
+        if scale is None:
+            # activations: [block][row], the order in which the products read them
+            scale = torch.empty(kb, rows, device=x.device).t() if block_rows == 1 else \
+                torch.empty(rows, kb, device=x.device)
+    ldq = _matrix(q, "q", (torch.float8_e4m3fn, torch.uint8), (m, k), x.device)
+    sp, s0, s1 = _scales(scale, "scale", (rows, kb), x.device)
+    with _device(x):
+        _check(lib().ct_fp8_quantize(x.data_ptr(), _DTYPES[x.dtype], m, k, ldx, block_rows, q.data_ptr(), ldq, sp, s0, s1,
+                                     _stream(stream)), "ct_fp8_quantize")
+    return q, scale
+
+
+class _device:
+    """Makes a tensor's device current for a call (nothing to do where it is)."""
+
+    def __init__(self, t):
+        self.index = t.device.index
+        self.before = None
+
+    def __enter__(self):
+        import torch
+        now = torch.cuda.current_device()
+        if now != self.index:
+            self.before = now
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before is not None:
+            import torch
+            torch.cuda.set_device(self.before)
+
+
+def ct_fp8_matmul(xq, xs, wq, ws, bias=None, relu: bool = False, out_dtype=None, out=None, stream=None):
+    """y [m, n] = act(x w^T + bias) of 8-bit operands: xq [m, k] with scales xs
+    [m, ceil(k / 128)], wq [n, k] with scales ws [ceil(n / 128), ceil(k / 128)]
+    (any strides).  out_dtype: float32 unless `out` or another type is given."""
+    import torch
+    ldx = _matrix(xq, "xq", (torch.float8_e4m3fn, torch.uint8))
+    m, k = xq.shape
+    dev = xq.device
+    w = _fp8_weights(wq, ws, k, dev)
+    n = wq.shape[0]
+    xsp = _scales(xs, "xs", (m, (k + 127) // 128), dev)
+    b = None if bias is None else _vector(bias, "bias", torch.float32, n, dev)
+    y, ldy = _fp8_out(out, torch.float32 if out is None and out_dtype is None else out_dtype, m, n, dev, stream)
+    with _device(xq):
+        _check(lib().ct_fp8_matmul(xq.data_ptr(), ldx, *xsp, *w, b, int(relu), y.data_ptr(), _dtypes()[y.dtype], ldy,
+                                   m, n, k, _stream(stream)), "ct_fp8_matmul")
+    return y
+
+
+def ct_fp8_linear(x, wq, ws, bias=None, relu: bool = False, out_dtype=None, out=None, stream=None):
+    """act(x W^T + bias) with 8-bit weights on float32 / float16 / bfloat16
+    activations x [m, k], quantised on the way (1 x 128 blocks).  out_dtype: x's
+    type unless `out` or another type is given."""
+    import torch
+    ldx = _matrix(x, "x", _dtypes())
+    m, k = x.shape
+    dev = x.device
+    w = _fp8_weights(wq, ws, k, dev)
+    n = wq.shape[0]
+    b = None if bias is None else _vector(bias, "bias", torch.float32, n, dev)
+    y, ldy = _fp8_out(out, x.dtype if out is None and out_dtype is None else out_dtype, m, n, dev, stream)
+    need = ctypes.c_size_t()
+    _check(lib().ct_fp8_linear_workspace(m, k, ctypes.byref(need)), "ct_fp8_linear_workspace")
+    with _on_stream(stream):
+        work = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    with _device(x):
+        _check(lib().ct_fp8_linear(x.data_ptr(), _DTYPES[x.dtype], ldx, *w, b, int(relu), y.data_ptr(),
+                                   _DTYPES[y.dtype], ldy, m, n, k, work.data_ptr(), need.value, _stream(stream)),
+               "ct_fp8_linear")
+    return y
+
+
+def ct_logprobs(logits, ids=None, top_k: int = 0, stream=None):
+    """(logprob, entropy, lse, top_logprob, top_id) of logits [rows, vocab]:
+    the log probability of token ids[r] (int64; -1: none, 0; logprob is None
+    without ids), the entropy and log normaliser of each row (float32), and
+    its top_k most probable tokens (float32 / int64 [rows, top_k])."""
+    import torch
+    ld = _matrix(logits, "logits", _dtypes())
+    rows, vocab = logits.shape
+    dev = logits.device
+    idp = None if ids is None else _vector(ids, "ids", torch.int64, rows, dev)
+    if not 0 <= top_k <= CT_MAX_TOP_K:
+        raise ValueError("top_k is 0 to %d, got %r" % (CT_MAX_TOP_K, top_k))
+    with _on_stream(stream):
+        num = torch.empty(3, rows, device=dev)
+        top_lp = torch.empty(rows, top_k, device=dev)
+        top_id = torch.empty(rows, top_k, dtype=torch.int64, device=dev)
+    lp, entropy, lse = num.unbind(0)
+    with _device(logits):
+        _check(lib().ct_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], ld, idp, rows, vocab, top_k,
+                                 None if ids is None else lp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                                 top_lp.data_ptr(), top_id.data_ptr(), _stream(stream)), "ct_logprobs")
+    return (None if ids is None else lp), entropy, lse, top_lp, top_id
+
+
+def ct_logprobs_grad(logits, ids, lse, entropy, g_logprob=None, g_entropy=None, out=None, stream=None):
+    """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect
+    to the logits, in their type; lse and entropy are ct_logprobs' outputs.
+    `out` may be `logits`."""
+    import torch
+    ld = _matrix(logits, "logits", _dtypes())
+    rows, vocab = logits.shape
+    dev = logits.device
+    f32 = torch.float32
+    idp = None if ids is None else _vector(ids, "ids", torch.int64, rows, dev)
+    vec = [None if t is None else _vector(t, name, f32, rows, dev)
+           for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy"))]
+    if lse is None or (g_logprob is not None and ids is None) or (g_entropy is not None and entropy is None):
+        raise ValueError("lse is needed, ids for g_logprob, entropy for g_entropy")
+    if out is None:
+        with _on_stream(stream):
+            out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
+        ldd = vocab
+    else:
+        ldd = _matrix(out, "out", (logits.dtype,), (rows, vocab), dev)
+    with _device(logits):
+        _check(lib().ct_logprobs_grad(logits.data_ptr(), _DTYPES[logits.dtype], ld, idp, rows, vocab, *vec,
+                                      out.data_ptr(), ldd, _stream(stream)), "ct_logprobs_grad")
+    return out
+
+
+def ct_ops_device_error() -> int:
+    """Reads and clears the current device's error word of these operators."""
+    c = ctypes.c_uint32()
+    _check(lib().ct_ops_device_error(ctypes.byref(c)), "ct_ops_device_error")
+    return c.value
