@@ -16,15 +16,17 @@
 // holds one K block of both operands: 128-byte rows, 128-byte swizzle; rows
 // and columns past the ends are the zeros TMA fills in.
 //
-// Two orientations:
-//   rows of x on the TMEM lanes (many rows): 128 x 256 tiles, persistent
-//     CTAs; the factor of a thread's values is one product per block;
-//   rows of w on the lanes (few rows): 128 x BN tiles with BN as narrow as
-//     the rows allow, so that a few rows cost no 128-wide tile; the K range
-//     is split over a cluster of up to 8 CTAs so that the whole GPU streams
-//     the weights, and the cluster adds its partial sums through distributed
-//     shared memory, in rank order: no workspace, no atomics, one launch, the
-//     same bits each time.
+// Two kernels:
+//   wide (many rows): rows of x on the TMEM lanes, tiles of 256 rows x BN
+//     columns on CTA pairs (cta_group::2: each CTA stages half of both
+//     operands), persistent; the factor of a thread's values is one product
+//     per block;
+//   narrow (few rows): rows of w on the lanes, 128 x BN tiles with BN as
+//     narrow as the rows allow, so that a few rows cost no 128-wide tile; the
+//     K range is split over a cluster of up to 8 CTAs so that the whole GPU
+//     streams the weights, and the cluster adds its partial sums through
+//     distributed shared memory, in rank order: no workspace, no atomics, one
+//     launch, the same bits each time.
 #include <atomic>
 #include <cudaTypedefs.h>
 #include <string.h>
@@ -60,20 +62,20 @@ struct MmArgs {
     int out, relu;
     int tiles_l, tiles_c;               // tiles along the lane side and along the columns
     int splits;                         // CTAs of a cluster that share a tile's K blocks
-    int group;                          // lane tiles walked together (persistent grids)
-    int vec;                            // y rows may be written 32 bytes at a time
+    int group;                          // wide: row tiles walked together
+    int vec;                            // wide: TMA can address y's rows
     uint32_t *err;
 };
 
-template <int BN, bool SWAP> struct Shape {
+template <int BN> struct Shape {
     static constexpr int C_BYTES = BN * BK;
     static constexpr int STAGE = L_BYTES + C_BYTES;
     // two CTAs share an SM where the tiles are narrow
-    static constexpr int STAGES = BN <= 32 ? 5 : BN == 64 ? 4 : BN == 128 ? 6 : 4;
+    static constexpr int STAGES = BN <= 32 ? 5 : BN == 64 ? 4 : 6;
     static constexpr int NBUF = BN <= 64 ? 4 : 2;
     static constexpr int TMEM_COLS = NBUF * BN < 32 ? 32 : NBUF * BN;
     static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
-    static constexpr int FAC = SWAP ? N_EPI * 2 * CPW * 4 : 0;
+    static constexpr int FAC = N_EPI * 2 * CPW * 4;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16;
 };
 
@@ -127,20 +129,13 @@ __device__ __forceinline__ float finish(const MmArgs &a, float v, int n) {
     return a.relu ? relu_keep_nan(v) : v;
 }
 
-// tile -> (lane tile, column tile): `group` lane tiles are walked together,
-// so that the CTAs at work share operand tiles in L2
-__device__ __forceinline__ void tile_at(const MmArgs &a, int t, int &l, int &c) {
-    const int per = a.group * a.tiles_c;
-    const int g = t / per, r = t % per;
-    const int rows = min(a.group, a.tiles_l - g * a.group);
-    l = g * a.group + r % rows;
-    c = r / rows;
-}
-
-template <int BN, bool SWAP>
+// ---------------------------------------------------------------------------
+// narrow: few rows
+// ---------------------------------------------------------------------------
+template <int BN>
 __global__ void __launch_bounds__(THREADS, 1)
-fp8_matmul_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap, const MmArgs a) {
-    using S = Shape<BN, SWAP>;
+fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap, const MmArgs a) {
+    using S = Shape<BN>;
     constexpr int CPW = S::CPW;
     constexpr int LDN = CPW < 32 ? CPW : 32;               // columns of one TMEM load
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -153,12 +148,11 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
     uint64_t *acc_full = empty + S::STAGES;
     uint64_t *acc_empty = acc_full + S::NBUF;
     uint32_t *tmem_holder = (uint32_t *)(acc_empty + S::NBUF);
-    volatile uint32_t *abort_flag = tmem_holder + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)a.splits);
-    const int cid = (int)(blockIdx.x / (unsigned)a.splits), ncl = (int)(gridDim.x / (unsigned)a.splits);
-    const int tiles = a.tiles_l * a.tiles_c;
+    const int tile = (int)(blockIdx.x / (unsigned)a.splits);
+    const int tl = tile % a.tiles_l, tc = tile / a.tiles_l;
     const int kb0 = (int)((int64_t)a.KB * rank / a.splits), kb1 = (int)((int64_t)a.KB * (rank + 1) / a.splits);
 
     if (threadIdx.x == 0) {
@@ -170,7 +164,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
             mbar_init(smem_u32(&acc_full[b]), 1);
             mbar_init(smem_u32(&acc_empty[b]), N_EPI);
         }
-        *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -188,27 +181,21 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
     if (warp == TMA_WARP) {
         int it = 0;
         bool ok = true;
-        for (int t = cid; t < tiles && ok; t += ncl) {
-            int tl, tc;
-            tile_at(a, t, tl, tc);
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int s = it % S::STAGES;
-                if (!warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA) ||
-                    __any_sync(0xffffffffu, *abort_flag)) {
-                    ok = false;
-                    break;
-                }
-                if (elect_one()) {
-                    const uint32_t fb = smem_u32(&full[s]);
-                    mbar_arrive_expect_tx(fb, (uint32_t)S::STAGE);
-                    tma_load_2d(smem_u32(Ls + s * L_BYTES), &lmap, fb, kb * BK, tl * BL);
-                    tma_load_2d(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, kb * BK, tc * BN);
-                }
-                __syncwarp();
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            const int s = it % S::STAGES;
+            if (!warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA)) {
+                ok = false;
+                break;
             }
+            if (elect_one()) {
+                const uint32_t fb = smem_u32(&full[s]);
+                mbar_arrive_expect_tx(fb, (uint32_t)S::STAGE);
+                tma_load_2d(smem_u32(Ls + s * L_BYTES), &lmap, fb, kb * BK, tl * BL);
+                tma_load_2d(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, kb * BK, tc * BN);
+            }
+            __syncwarp();
         }
         if (!ok) {
-            if (lane == 0) *abort_flag = 1;
             // copies still in flight land before the CTA ends
             for (int j = max(0, it - S::STAGES); j < it; ++j)
                 warp_wait(smem_u32(&full[j % S::STAGES]), (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
@@ -217,151 +204,440 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
         constexpr uint32_t idesc = idesc_e4m3(BL, BN);
         int it = 0;
         bool ok = true;
-        for (int t = cid; t < tiles && ok; t += ncl) {
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int s = it % S::STAGES, b = it % S::NBUF;
-                if (!warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / S::NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
-                    !warp_wait(smem_u32(&full[s]), (uint32_t)(it / S::STAGES) & 1u, a.err, E_MMA) ||
-                    __any_sync(0xffffffffu, *abort_flag)) {
-                    ok = false;
-                    break;
-                }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (elect_one()) {
-                    const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
-                    const uint64_t cd = smem_desc_sw128(smem_u32(Cs + s * S::C_BYTES));
-#pragma unroll
-                    for (int k = 0; k < BK / 32; ++k)
-                        umma_e4m3(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
-                    umma_commit(smem_u32(&empty[s]));
-                    umma_commit(smem_u32(&acc_full[b]));
-                }
-                __syncwarp();
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            const int s = it % S::STAGES, b = it % S::NBUF;
+            if (!warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / S::NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
+                !warp_wait(smem_u32(&full[s]), (uint32_t)(it / S::STAGES) & 1u, a.err, E_MMA)) {
+                ok = false;
+                break;
             }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (elect_one()) {
+                const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
+                const uint64_t cd = smem_desc_sw128(smem_u32(Cs + s * S::C_BYTES));
+#pragma unroll
+                for (int k = 0; k < BK / 32; ++k)
+                    umma_e4m3(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
+                umma_commit(smem_u32(&empty[s]));
+                umma_commit(smem_u32(&acc_full[b]));
+            }
+            __syncwarp();
         }
-        if (!ok && lane == 0) *abort_flag = 1;
     } else {
         const int quad = warp & 3, half = warp >> 2;
         const int row = quad * 32 + lane;                  // lane row of this thread within the tile
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
+        const int l = tl * BL + row;                       // its row of w
+        const int c0 = tc * BN + half * CPW;               // first row of x of this warp
+        float acc[CPW];
+#pragma unroll
+        for (int i = 0; i < CPW; ++i) acc[i] = 0.f;
+
+        // scales of the next block, fetched one block ahead: lane j holds
+        // column j's and the warp shares the products through shared memory
+        constexpr int NF = (CPW + 31) / 32;
+        float nx[NF], nw;
+        const float *xp[NF];
+        bool xin[NF];
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            const int m = c0 + j * 32 + lane;
+            xin[j] = j * 32 + lane < CPW && m < a.M;
+            xp[j] = a.xs + (int64_t)(xin[j] ? m : 0) * a.xs_row;
+        }
+        const float *wp = a.ws + (int64_t)tl * a.ws_row;
+        const auto fetch = [&](int kb) {
+#pragma unroll
+            for (int j = 0; j < NF; ++j) nx[j] = xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
+            nw = __ldg(wp + kb * a.ws_blk);
+        };
+        if (kb0 < kb1) fetch(kb0);
+
         int it = 0;
         bool ok = true;
-        for (int t = cid; t < tiles && ok; t += ncl) {
-            int tl, tc;
-            tile_at(a, t, tl, tc);
-            const int l = tl * BL + row;                   // global index on the lane side
-            const int c0 = tc * BN + half * CPW;           // first global column of this warp
-            float acc[CPW];
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            const int b = it % S::NBUF;
+            float *fs = fac + (warp * 2 + (it & 1)) * CPW;
 #pragma unroll
-            for (int i = 0; i < CPW; ++i) acc[i] = 0.f;
-
-            // scales of the next block, fetched one block ahead
-            constexpr int NF = (CPW + 31) / 32;
-            float nx[NF], nw;
-            const float *xp[NF];
-            bool xin[NF];
-            const float *wp;
-            if constexpr (SWAP) {
-#pragma unroll
-                for (int j = 0; j < NF; ++j) {
-                    const int m = c0 + j * 32 + lane;
-                    xin[j] = j * 32 + lane < CPW && m < a.M;
-                    xp[j] = a.xs + (int64_t)(xin[j] ? m : 0) * a.xs_row;
-                }
-                wp = a.ws + (int64_t)tl * a.ws_row;
-            } else {
-                xin[0] = l < a.M;
-                xp[0] = a.xs + (int64_t)(xin[0] ? l : 0) * a.xs_row;
-                wp = a.ws + (int64_t)min(c0 / 128, (a.N - 1) / 128) * a.ws_row;
-            }
-            const auto fetch = [&](int kb) {
-#pragma unroll
-                for (int j = 0; j < NF; ++j)
-                    if (SWAP || j == 0) nx[j] = xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
-                nw = __ldg(wp + kb * a.ws_blk);
-            };
-            if (kb0 < kb1) fetch(kb0);
-
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int b = it % S::NBUF;
-                float f = nx[0] * nw;
-                const float *fs = fac + (warp * 2 + (it & 1)) * CPW;
-                if constexpr (SWAP) {
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-                        if (j * 32 + lane < CPW) const_cast<float *>(fs)[j * 32 + lane] = nx[j] * nw;
-                    __syncwarp();
-                }
-                if (kb + 1 < kb1) fetch(kb + 1);
-                ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / S::NBUF) & 1u, a.err, E_EPI) &&
-                     !__any_sync(0xffffffffu, *abort_flag);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                for (int c = 0; c < CPW; c += LDN) {
-                    uint32_t r[LDN];
-                    tmem_ld_nw<LDN>(tbase + (uint32_t)(b * BN + c), r);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < LDN; ++i) {
-                        const float p = tmem_done(r[i]);
-                        acc[c + i] = fmaf(SWAP ? fs[c + i] : f, p, acc[c + i]);
-                    }
-                }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
-            }
+            for (int j = 0; j < NF; ++j)
+                if (j * 32 + lane < CPW) fs[j * 32 + lane] = nx[j] * nw;
+            __syncwarp();
+            if (kb + 1 < kb1) fetch(kb + 1);
+            ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / S::NBUF) & 1u, a.err, E_EPI);
             if (!ok) break;
-
-            if constexpr (SWAP) {
-                if (a.splits > 1) {
-                    // partial sums [column][lane row], over the stages: every copy has
-                    // landed and every MMA has read it (the last block is complete)
-                    float *part = (float *)smem;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                    for (int i = 0; i < CPW; ++i) part[(half * CPW + i) * BL + row] = acc[i];
-                } else if (l < a.N) {
+            for (int c = 0; c < CPW; c += LDN) {
+                uint32_t r[LDN];
+                tmem_ld_nw<LDN>(tbase + (uint32_t)(b * BN + c), r);
+                tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < CPW; ++i)
-                        if (c0 + i < a.M) store_out(a, (int64_t)(c0 + i) * a.ldy + l, finish(a, acc[i], l));
-                }
-            } else if (l < a.M) {
-#pragma unroll
-                for (int i = 0; i < CPW; ++i) {
-                    const int n = c0 + i;
-                    if (n < a.N) store_out(a, (int64_t)l * a.ldy + n, finish(a, acc[i], n));
-                }
+                for (int i = 0; i < LDN; ++i) acc[c + i] = fmaf(fs[c + i], tmem_done(r[i]), acc[c + i]);
             }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
         }
-        if (!ok && lane == 0) *abort_flag = 1;
+        if (!ok) {
+            // reported; the output is invalid
+        } else if (a.splits > 1) {
+            // partial sums [column][lane row], over the stages: every copy has
+            // landed and every MMA has read it (the last block is complete)
+            float *part = (float *)smem;
+#pragma unroll
+            for (int i = 0; i < CPW; ++i) part[(half * CPW + i) * BL + row] = acc[i];
+        } else if (l < a.N) {
+#pragma unroll
+            for (int i = 0; i < CPW; ++i)
+                if (c0 + i < a.M) store_out(a, (int64_t)(c0 + i) * a.ldy + l, finish(a, acc[i], l));
+        }
     }
     __syncwarp();
-    if constexpr (SWAP) {
-        if (a.splits > 1) {
-            cluster_sync();
-            if (warp < N_EPI) {
-                // this CTA finishes every splits-th column of the cluster's tile
-                int tl, tc;
-                tile_at(a, cid, tl, tc);
-                const int row = (int)threadIdx.x & (BL - 1), l = tl * BL + row;
-                const int cols = min(BN, a.M - tc * BN);
-                for (int c = rank * 2 + ((int)threadIdx.x >> 7); c < cols; c += 2 * a.splits) {
-                    float v = 0.f;
-                    const uint32_t at = smem_u32((float *)smem + c * BL + row);
+    if (a.splits > 1) {
+        cluster_sync();
+        if (warp < N_EPI) {
+            // this CTA finishes its share of the tile's columns
+            const int row = (int)threadIdx.x & (BL - 1), l = tl * BL + row;
+            const int cols = min(BN, a.M - tc * BN);
+            for (int c = rank * 2 + ((int)threadIdx.x >> 7); c < cols; c += 2 * a.splits) {
+                float v = 0.f;
+                const uint32_t at = smem_u32((float *)smem + c * BL + row);
 #pragma unroll 4
-                    for (int s = 0; s < a.splits; ++s) v += ld_cluster_f32(mapa_shared(at, (uint32_t)s));
-                    if (l < a.N) store_out(a, (int64_t)(tc * BN + c) * a.ldy + l, finish(a, v, l));
-                }
+                for (int s = 0; s < a.splits; ++s) v += ld_cluster_f32(mapa_shared(at, (uint32_t)s));
+                if (l < a.N) store_out(a, (int64_t)(tc * BN + c) * a.ldy + l, finish(a, v, l));
             }
-            cluster_sync();
         }
+        cluster_sync();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::TMEM_COLS));
+    }
+}
+
+// ---------------------------------------------------------------------------
+// wide: CTA pairs
+// ---------------------------------------------------------------------------
+constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9 MMA, 10-11 idle
+// registers a thread after the split: 2 x 232 + 40 for three warpgroups that
+// were launched with 168 each (3 x 168 = 504)
+constexpr int W_REGS_EPI = 232, W_REGS_REST = 40;
+constexpr int W_BOX_BYTES = 32 * 128;                      // epilogue: 32 rows of 128 bytes, two for each warp
+constexpr int W_CHUNK = 16;                                // columns of one step of the unaligned store
+
+template <int BN> struct Wide {
+    static constexpr int C_BYTES = BN / 2 * BK;            // this CTA's half of the column operand
+    static constexpr int STAGES = BN == 256 ? 5 : BN == 128 ? 6 : 7;
+    static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
+    static constexpr int LDN = BN == 64 ? 16 : 32;         // columns of one TMEM load: an even number of loads
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * 2 * W_BOX_BYTES +
+                                   8 * (2 * STAGES + 5) + 16;
+};
+
+__device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc));
+}
+
+// Arrive on the even CTA's barrier.  Relaxed: what it orders is the TMEM reads
+// before it (complete at their wait, then tcgen05.fence), not memory; a
+// release would wait for the scale loads and output stores in flight.
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar_cluster) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
+}
+
+// acc += f * p on two values at once.  Volatile, like the TMEM load and the
+// wait before it: volatile asm keeps its order, so no value is read before
+// its load is complete.
+__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t f, uint32_t p0, uint32_t p1) {
+    asm volatile("{\n\t.reg .b64 p;\n\tmov.b64 p, {%2, %3};\n\tfma.rn.f32x2 %0, %1, p, %0;\n\t}"
+                 : "+l"(acc)
+                 : "l"(f), "r"(p0), "r"(p1));
+}
+__device__ __forceinline__ uint64_t dup2(float f) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(f));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"((uint64_t)map),
+                 "r"(src), "r"(x), "r"(y)
+                 : "memory");
+}
+
+// tile -> (row tile, column tile): `group` row tiles are walked together, so
+// that the pairs at work share operand tiles in L2
+__device__ __forceinline__ void tile_at(const MmArgs &a, int t, int &l, int &c) {
+    const int per = a.group * a.tiles_c;
+    const int g = t / per, r = t % per;
+    const int rows = min(a.group, a.tiles_l - g * a.group);
+    l = g * a.group + r % rows;
+    c = r / rows;
+}
+
+// 16 bytes of y from finished values: 4 FP32 or 8 of 16 bits
+template <int SIZE> __device__ __forceinline__ uint4 out16(int out, const float *v) {
+    if constexpr (SIZE == 4) return pack16<float>(v);
+    else return out == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
+}
+
+// Rows of y that TMA can address: through shared memory in boxes of 32 rows
+// by COLS columns, 128 bytes (64 where the warp's columns are fewer), swizzled
+// so that the 16-byte pieces of 8 rows hit 8 bank groups, stored by TMA, which clips what lies past the ends, while the next tile's
+// products are added.
+template <int CPW, int COLS, int SIZE>
+__device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *ymap, const uint64_t *acc, uint8_t *boxes,
+                                            uint32_t &stored, int m_warp, int c0, int lane) {
+    constexpr int PER16 = 16 / SIZE;                       // values of 16 bytes
+    constexpr int PIECES = COLS / PER16;                   // 16-byte pieces of a box row
+    static_assert((PIECES == 8 || PIECES == 4) && CPW % COLS == 0, "box rows of 128 or 64 bytes");
+    const int swz = PIECES == 8 ? lane & 7 : (lane >> 1) & 3;
+#pragma unroll
+    for (int c = 0; c < CPW; c += COLS) {
+        if (c0 + c >= a.N) break;
+        uint8_t *box = boxes + (stored++ & 1u) * W_BOX_BYTES;
+        // the store before the last has been read from this box
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            float v[PER16];
+#pragma unroll
+            for (int i = 0; i < PER16 / 2; ++i) split2(acc[(c + j * PER16) / 2 + i], v[2 * i], v[2 * i + 1]);
+            if (a.bias != nullptr) {
+#pragma unroll
+                for (int i = 0; i < PER16; ++i) v[i] += __ldg(a.bias + min(c0 + c + j * PER16 + i, a.N - 1));
+            }
+            if (a.relu) {
+#pragma unroll
+                for (int i = 0; i < PER16; ++i) v[i] = relu_keep_nan(v[i]);
+            }
+            *reinterpret_cast<uint4 *>(box + lane * (PIECES * 16) + ((j ^ swz) * 16)) = out16<SIZE>(a.out, v);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            if (m_warp < a.M) tma_store_2d(ymap, smem_u32(box), c0 + c, m_warp);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
+}
+
+template <int BN>
+__global__ void __launch_bounds__(W_THREADS, 1)
+fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap,
+                const __grid_constant__ CUtensorMap ymap, const MmArgs a) {
+    using S = Wide<BN>;
+    constexpr int CPW = S::CPW, LDN = S::LDN;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *Ls = smem;
+    uint8_t *Cs = Ls + S::STAGES * L_BYTES;
+    uint8_t *boxes = Cs + S::STAGES * S::C_BYTES;
+    uint64_t *full = (uint64_t *)(boxes + N_EPI * 2 * W_BOX_BYTES);   // even CTA's: both CTAs' copies of a stage
+    uint64_t *empty = full + S::STAGES;                    // each CTA: the pair's MMAs have read the stage
+    uint64_t *acc_full = empty + S::STAGES;                // each CTA: a block's products are in TMEM
+    uint64_t *acc_empty = acc_full + 2;                    // even CTA's: both CTAs' epilogues have read them
+    uint64_t *mma_done = acc_empty + 2;
+    uint32_t *tmem_holder = (uint32_t *)(mma_done + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t crank = cluster_ctarank();
+    const bool leader = crank == 0;
+    const int cid = (int)(blockIdx.x >> 1), ncl = (int)(gridDim.x >> 1);
+    const int tiles = a.tiles_l * a.tiles_c;
+    const int KB = a.KB;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&acc_full[b]), 1);
+            mbar_init(smem_u32(&acc_empty[b]), 2 * N_EPI);
+        }
+        mbar_init(smem_u32(mma_done), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == MMA_WARP) {
+        // one warp of each CTA of the pair allocates the same columns in both
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                     "r"((uint32_t)(2 * BN)));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();                                        // the peer's barriers exist before anything targets them
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_holder;
+    pdl_wait();
+    pdl_trigger();
+
+    if (warp >= N_EPI) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W_REGS_REST));
+        if (warp == TMA_WARP) {
+            const uint32_t full_even = mapa_shared(smem_u32(full), 0u);
+            int it = 0;
+            bool ok = true;
+            for (int t = cid; t < tiles && ok; t += ncl) {
+                int tl, tc;
+                tile_at(a, t, tl, tc);
+                const int m0 = (2 * tl + (int)crank) * BL, n0 = tc * BN + (int)crank * (BN / 2);
+                for (int kb = 0; kb < KB; ++kb, ++it) {
+                    const int s = it % S::STAGES;
+                    if (!warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA)) {
+                        ok = false;
+                        break;
+                    }
+                    if (elect_one()) {
+                        const uint32_t fb = full_even + (uint32_t)(s * 8);
+                        if (leader) mbar_arrive_expect_tx(smem_u32(&full[s]), 2u * (L_BYTES + S::C_BYTES));
+                        tma_load_2d_pair(smem_u32(Ls + s * L_BYTES), &lmap, fb, kb * BK, m0);
+                        tma_load_2d_pair(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, kb * BK, n0);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok && leader) {
+                // copies still in flight land before the CTAs end (the even CTA's barrier counts both CTAs')
+                for (int j = max(0, it - S::STAGES); j < it; ++j)
+                    warp_wait(smem_u32(&full[j % S::STAGES]), (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
+            }
+        } else if (warp == MMA_WARP && leader) {
+            constexpr uint32_t idesc = idesc_e4m3(2 * BL, BN);
+            int it = 0;
+            bool ok = true;
+            for (int t = cid; t < tiles && ok; t += ncl) {
+                for (int kb = 0; kb < KB; ++kb, ++it) {
+                    const int s = it % S::STAGES, b = it & 1;
+                    if (!warp_wait(smem_u32(&full[s]), (uint32_t)(it / S::STAGES) & 1u, a.err, E_MMA) ||
+                        !warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it >> 1) & 1u) ^ 1u, a.err, E_ACC)) {
+                        ok = false;
+                        break;
+                    }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    if (elect_one()) {
+                        const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
+                        const uint64_t cd = smem_desc_sw128(smem_u32(Cs + s * S::C_BYTES));
+#pragma unroll
+                        for (int k = 0; k < BK / 32; ++k)
+                            umma_e4m3_pair(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
+                        umma_commit_pair_mc(smem_u32(&acc_full[b]), (uint16_t)3u);
+                        umma_commit_pair_mc(smem_u32(&empty[s]), (uint16_t)3u);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (elect_one()) umma_commit_pair_mc(smem_u32(mma_done), (uint16_t)3u);
+            __syncwarp();
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W_REGS_EPI));
+        const int quad = warp & 3, half = warp >> 2;
+        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
+        const uint32_t acc_empty_even = mapa_shared(smem_u32(acc_empty), 0u);
+        uint8_t *mine = boxes + warp * 2 * W_BOX_BYTES;
+        uint32_t stored = 0;                               // boxes this warp has stored
+        int it = 0;
+        bool ok = true;
+        for (int t = cid; t < tiles && ok; t += ncl) {
+            int tl, tc;
+            tile_at(a, t, tl, tc);
+            const int m_warp = (2 * tl + (int)crank) * BL + quad * 32;
+            const int c0 = tc * BN + half * CPW;           // inside one 128-row block of w
+            uint64_t acc[CPW / 2];
+#pragma unroll
+            for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
+
+            const float *xp = a.xs + (int64_t)min(m_warp + lane, a.M - 1) * a.xs_row;
+            const float *wp = a.ws + (int64_t)(min(c0, a.N - 1) / 128) * a.ws_row;
+            float nx = __ldg(xp), nw = __ldg(wp);
+            uint32_t r[2][LDN];
+            ok = warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)(it >> 1) & 1u, a.err, E_EPI);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            tmem_ld_nw<LDN>(tbase + (uint32_t)((it & 1) * BN), r[0]);
+            for (int kb = 0; kb < KB; ++kb, ++it) {
+                const uint32_t src = tbase + (uint32_t)((it & 1) * BN);
+                const uint64_t f = dup2(nx * nw);
+                if (kb + 1 < KB) {                         // the next block's scales
+                    xp += a.xs_blk;
+                    wp += a.ws_blk;
+                    nx = __ldg(xp);
+                    nw = __ldg(wp);
+                }
+                // LDN columns are on their way while the LDN before are added,
+                // across blocks too
+#pragma unroll
+                for (int c = 0; c < CPW; c += LDN) {
+                    const int h = c / LDN & 1;
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    if (c + LDN < CPW) {
+                        tmem_ld_nw<LDN>(src + (uint32_t)(c + LDN), r[h ^ 1]);
+                    } else {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & 1) * 8));
+                        if (kb + 1 < KB) {
+                            ok = warp_wait(smem_u32(&acc_full[(it + 1) & 1]), (uint32_t)((it + 1) >> 1) & 1u, a.err, E_EPI);
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                            if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & 1) * BN), r[h ^ 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
+                }
+                if (!ok) break;
+            }
+            if (!ok) break;
+
+            if (a.vec) {
+                if (a.out == CT_DT_F32) store_boxes<CPW, 32, 4>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+                else store_boxes<CPW, CPW < 64 ? CPW : 64, 2>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+            } else {
+                // rows that start anywhere: two rows of 16 columns a step
+                float *sq = (float *)mine;
+#pragma unroll
+                for (int c = 0; c < CPW; c += W_CHUNK) {
+                    if (c0 + c < a.N) {
+#pragma unroll
+                        for (int i = 0; i < W_CHUNK / 2; ++i)
+                            split2(acc[c / 2 + i], sq[lane * (W_CHUNK + 1) + 2 * i], sq[lane * (W_CHUNK + 1) + 2 * i + 1]);
+                        __syncwarp();
+                        const int j = lane % W_CHUNK, n = c0 + c + j;
+                        if (n < a.N) {
+#pragma unroll 4
+                            for (int q = lane / W_CHUNK; q < 32; q += 32 / W_CHUNK)
+                                if (m_warp + q < a.M)
+                                    store_out(a, (int64_t)(m_warp + q) * a.ldy + n, finish(a, sq[q * (W_CHUNK + 1) + j], n));
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    __syncthreads();
+    // every MMA of the pair has completed before TMEM is freed in either CTA,
+    // and no CTA leaves while its peer may still arrive on its barriers
+    if (warp == MMA_WARP) warp_wait(smem_u32(mma_done), 0u, a.err, E_DRAIN);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_sync();
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * BN)));
     }
 }
 
@@ -389,33 +665,54 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
     return f;
 }
 
-// [rows, k] bytes, row pitch ld, in boxes of 128 bytes x box_rows, 128-byte swizzle
-bool encode(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t k, int64_t ld, int box_rows) {
+// [rows, cols] values of `size` bytes, row pitch ld bytes, in boxes of box_bytes (128 or 64) x box_rows, swizzled
+// within box_bytes
+bool encode(CUtensorMap *map, const void *p, CUtensorMapDataType type, int size, int64_t rows, int64_t cols, int64_t ld,
+            int box_bytes, int box_rows) {
     PFN_cuTensorMapEncodeTiled_v12000 f = encoder();
     if (f == nullptr) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows};
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {(cuuint32_t)BK, (cuuint32_t)box_rows};
+    const cuuint32_t box[2] = {(cuuint32_t)(box_bytes / size), (cuuint32_t)box_rows};
     const cuuint32_t es[2] = {1, 1};
-    return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(p), dims, strides, box, es,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+    return f(map, type, 2, const_cast<void *>(p), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, bool SWAP>
-cudaError_t launch(const CUtensorMap &lmap, const CUtensorMap &cmap, const MmArgs &a, int grid, cudaStream_t st) {
-    using S = Shape<BN, SWAP>;
-    static std::atomic<bool> sized[MAX_DEVICES];
+// once per kernel and device: the shared memory it may ask for
+template <typename K> cudaError_t allow_smem(K *kernel, std::atomic<bool> (&sized)[MAX_DEVICES], size_t bytes) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev >= MAX_DEVICES || !sized[dev].load(std::memory_order_relaxed)) {
-        e = cudaFuncSetAttribute(fp8_matmul_kernel<BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::SMEM);
-        if (e != cudaSuccess) return e;
-        if (dev < MAX_DEVICES) sized[dev].store(true, std::memory_order_relaxed);
-    }
-    return pdl_launch_cluster(fp8_matmul_kernel<BN, SWAP>, dim3((unsigned)grid), dim3(THREADS), S::SMEM, st, a.splits,
+    if (dev < MAX_DEVICES && sized[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && dev < MAX_DEVICES) sized[dev].store(true, std::memory_order_relaxed);
+    return e;
+}
+
+bool encode8(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t k, int64_t ld, int box_rows) {
+    return encode(map, p, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, ld, BK, box_rows);
+}
+
+template <int BN>
+cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, const MmArgs &a, int grid, cudaStream_t st) {
+    static std::atomic<bool> sized[MAX_DEVICES];
+    const cudaError_t e = allow_smem(fp8_narrow_kernel<BN>, sized, Shape<BN>::SMEM);
+    if (e != cudaSuccess) return e;
+    return pdl_launch_cluster(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Shape<BN>::SMEM, st, a.splits,
                               lmap, cmap, a);
+}
+
+template <int BN>
+cudaError_t launch_wide(const CUtensorMap &lmap, const CUtensorMap &cmap, const CUtensorMap &ymap, const MmArgs &a,
+                        int pairs, cudaStream_t st) {
+    static std::atomic<bool> sized[MAX_DEVICES];
+    const cudaError_t e = allow_smem(fp8_wide_kernel<BN>, sized, Wide<BN>::SMEM);
+    if (e != cudaSuccess) return e;
+    return pdl_launch_cluster(fp8_wide_kernel<BN>, dim3((unsigned)(2 * pairs)), dim3(W_THREADS), Wide<BN>::SMEM, st, 2,
+                              lmap, cmap, ymap, a);
 }
 
 struct Operands {
@@ -440,29 +737,46 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
     CUtensorMap lmap, cmap;
     cudaError_t e;
     if (a.M > 256) {
-        a.tiles_l = (a.M + 127) / 128;
-        a.tiles_c = (a.N + 255) / 256;
+        const int pairs = sms / 2;
+        a.tiles_l = (a.M + 2 * BL - 1) / (2 * BL);
         a.splits = 1;
         a.group = 8;
-        if (!encode(&lmap, o.xq, a.M, o.k, o.ldx, BL) || !encode(&cmap, o.wq, a.N, o.k, o.ldw, 256)) return CT_ECUDA;
+        // column width: rounds of tiles over the pairs, each as long as its width plus a fixed part
+        int64_t best = INT64_MAX;
+        int bn = 64;
+        for (int w = 64; w <= 256; w *= 2) {
+            const int64_t t = (int64_t)a.tiles_l * ((a.N + w - 1) / w);
+            const int64_t cost = (t + pairs - 1) / pairs * (w + 64);
+            if (cost <= best) { best = cost; bn = w; }
+        }
+        a.tiles_c = (a.N + bn - 1) / bn;
         const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
         if (tiles > INT32_MAX / 2) return CT_ERANGE;
-        e = launch<256, false>(lmap, cmap, a, (int)(tiles < sms ? tiles : sms), st);
+        CUtensorMap ymap = {};
+        const int es = dtype_size(a.out);
+        a.vec = aligned(a.y, 16) && a.ldy * es % 16 == 0;
+        if (!encode8(&lmap, o.xq, a.M, o.k, o.ldx, BL) || !encode8(&cmap, o.wq, a.N, o.k, o.ldw, bn / 2) ||
+            (a.vec && !encode(&ymap, a.y, a.out == CT_DT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16,
+                              es, a.M, a.N, a.ldy * es, bn == 64 && es == 2 ? 64 : 128, 32)))
+            return CT_ECUDA;
+        const int n = (int)(tiles < pairs ? tiles : pairs);
+        e = bn == 64    ? launch_wide<64>(lmap, cmap, ymap, a, n, st)
+            : bn == 128 ? launch_wide<128>(lmap, cmap, ymap, a, n, st)
+                        : launch_wide<256>(lmap, cmap, ymap, a, n, st);
     } else {
         const int bn = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
         a.tiles_l = nt;
         a.tiles_c = (a.M + bn - 1) / bn;
-        a.group = nt;
         const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
+        if (tiles > INT32_MAX / 16) return CT_ERANGE;
         a.splits = 1;
         while (a.splits < 8 && tiles * a.splits * 2 <= sms && a.splits * 2 <= a.KB) a.splits *= 2;
-        if (tiles > INT32_MAX / 16) return CT_ERANGE;
-        if (!encode(&lmap, o.wq, a.N, o.k, o.ldw, BL) || !encode(&cmap, o.xq, a.M, o.k, o.ldx, bn)) return CT_ECUDA;
+        if (!encode8(&lmap, o.wq, a.N, o.k, o.ldw, BL) || !encode8(&cmap, o.xq, a.M, o.k, o.ldx, bn)) return CT_ECUDA;
         const int grid = (int)tiles * a.splits;
-        e = bn == 16   ? launch<16, true>(lmap, cmap, a, grid, st)
-            : bn == 32 ? launch<32, true>(lmap, cmap, a, grid, st)
-            : bn == 64 ? launch<64, true>(lmap, cmap, a, grid, st)
-                       : launch<128, true>(lmap, cmap, a, grid, st);
+        e = bn == 16   ? launch_narrow<16>(lmap, cmap, a, grid, st)
+            : bn == 32 ? launch_narrow<32>(lmap, cmap, a, grid, st)
+            : bn == 64 ? launch_narrow<64>(lmap, cmap, a, grid, st)
+                       : launch_narrow<128>(lmap, cmap, a, grid, st);
     }
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
@@ -486,7 +800,6 @@ MmArgs make_args(int64_t m, int64_t n, int64_t k, const float *ws, int64_t ws_ro
     a.bias = bias; a.y = y; a.ldy = ldy;
     a.M = (int)m; a.N = (int)n; a.KB = (int)((k + BK - 1) / BK);
     a.out = out; a.relu = relu != 0;
-    a.vec = aligned(y, 32) && ldy * dtype_size(out) % 32 == 0;
     return a;
 }
 
