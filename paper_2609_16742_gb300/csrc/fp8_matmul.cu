@@ -681,17 +681,6 @@ bool encode(CUtensorMap *map, const void *p, CUtensorMapDataType type, int size,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// once per kernel and device: the shared memory it may ask for
-template <typename K> cudaError_t allow_smem(K *kernel, std::atomic<bool> (&sized)[MAX_DEVICES], size_t bytes) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < MAX_DEVICES && sized[dev].load(std::memory_order_relaxed)) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess && dev < MAX_DEVICES) sized[dev].store(true, std::memory_order_relaxed);
-    return e;
-}
-
 bool encode8(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t k, int64_t ld, int box_rows) {
     return encode(map, p, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, ld, BK, box_rows);
 }

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "ct_internal.h"
 
 namespace ct {
@@ -28,6 +30,17 @@ int sm_count();
 // ct_fp8_quantize after its checks (fp8_quantize.cu).
 ct_status quantize(const void *x, int dtype, int64_t m, int64_t k, int64_t ldx, int block_rows, uint8_t *q, int64_t ldq,
                    float *scale, int64_t srow, int64_t sblk, cudaStream_t st);
+
+// once per kernel and device: the shared memory it may ask for
+template <typename K> inline cudaError_t allow_smem(K *kernel, std::atomic<bool> (&sized)[MAX_DEVICES], size_t bytes) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < MAX_DEVICES && sized[dev].load(std::memory_order_relaxed)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && dev < MAX_DEVICES) sized[dev].store(true, std::memory_order_relaxed);
+    return e;
+}
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float to_f32(float v) { return v; }
