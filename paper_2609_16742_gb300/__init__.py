@@ -461,82 +461,122 @@ def ct_destroy(m: Model):
 # Outputs that are not given are allocated on the call's stream.  `stream`:
 # None (the current one), a torch stream, or a raw cudaStream_t; inputs made
 # on another stream must be ordered before it by the caller, as for any
-# PyTorch kernel.
+# PyTorch kernel.  The calls are short next to Python's own cost, so the
+# checks read each attribute once and build no message unless they fail.
 # ---------------------------------------------------------------------------
-_DTYPES = None
+class _TorchNames:
+    """What the operators use of torch, looked up once."""
 
-
-def _dtypes():
-    global _DTYPES
-    if _DTYPES is None:
+    def __init__(self):
         import torch
-        _DTYPES = {torch.float32: CT_DT_F32, torch.float16: CT_DT_F16, torch.bfloat16: CT_DT_BF16}
-    return _DTYPES
+        self.torch = torch
+        self.empty = torch.empty
+        self.f32, self.u8, self.i64, self.e4m3 = torch.float32, torch.uint8, torch.int64, torch.float8_e4m3fn
+        self.dtypes = {torch.float32: CT_DT_F32, torch.float16: CT_DT_F16, torch.bfloat16: CT_DT_BF16}
+        self.bytes = {self.e4m3: 0, self.u8: 0}
+        self.current_device = torch.cuda.current_device
+        # the raw handle of the current stream; torch.cuda.current_stream builds a Stream object first
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _on_stream(stream):
-    """Context in which torch allocates on `stream` (None: the current one)."""
-    import contextlib
-    import torch
-    if stream is None:
-        return contextlib.nullcontext()
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream)
-    return torch.cuda.stream(stream)
+_names = None
+
+
+def _T():
+    global _names
+    if _names is None:
+        _names = _TorchNames()
+    return _names
+
+
+class _Call:
+    """One call's stream: its raw handle, and the contexts that make it (for
+    allocations) and the tensors' device current while the call runs.  Only
+    used where the call's stream or device is not the current one."""
+
+    def __init__(self, device, stream):
+        import contextlib
+        import torch
+        self.stack = contextlib.ExitStack()
+        self.stack.enter_context(torch.cuda.device(device))
+        if stream is not None:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=device)
+            self.stack.enter_context(torch.cuda.stream(stream))
+        self.handle = torch.cuda.current_stream(device).cuda_stream
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return self.stack.__exit__(*exc)
+
+
+def _elsewhere(f, device, stream, *args):
+    """f(*args, stream=None) with the call's device and stream current."""
+    with _Call(device, stream):
+        return f(*args)
+
+
+def _bad_matrix(t, name, dtypes, shape, device):
+    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
+        return ValueError("%s: a 2-D CUDA tensor of %s is wanted, got %s %s on %s"
+                          % (name, "/".join(str(d) for d in dtypes), t.dtype, tuple(t.shape), t.device))
+    if shape is not None and tuple(t.shape) != shape:
+        return ValueError("%s: shape %s is wanted, got %s" % (name, shape, tuple(t.shape)))
+    if device is not None and t.device != device:
+        return ValueError("%s is on %s, the other tensors on %s" % (name, t.device, device))
+    return ValueError("%s: its columns must be contiguous (strides %s)" % (name, t.stride()))
 
 
 def _matrix(t, name, dtypes, shape=None, device=None):
-    """Row pitch of a 2-D CUDA tensor with unit column stride."""
-    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
-        raise ValueError("%s: a 2-D CUDA tensor of %s is wanted, got %s %s on %s"
-                         % (name, "/".join(str(d) for d in dtypes), t.dtype, tuple(t.shape), t.device))
-    if shape is not None and t.shape != shape:
-        raise ValueError("%s: shape %s is wanted, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if device is not None and t.device != device:
-        raise ValueError("%s is on %s, the other tensors on %s" % (name, t.device, device))
-    rows, cols = t.shape
+    """(rows, columns, row pitch) of a 2-D CUDA tensor with unit column stride."""
+    size = t.shape
+    if len(size) != 2 or t.dtype not in dtypes or not t.is_cuda or (shape is not None and size != shape) or \
+            (device is not None and t.device != device):
+        raise _bad_matrix(t, name, dtypes, shape, device)
+    m, n = size
     s0, s1 = t.stride()
-    if cols > 1 and s1 != 1:
-        raise ValueError("%s: its columns must be contiguous (strides %s)" % (name, t.stride()))
-    return s0 if rows > 1 else max(s0, cols)
+    if s1 != 1 and n > 1:
+        raise _bad_matrix(t, name, dtypes, shape, device)
+    return m, n, s0 if m > 1 or s0 > n else n
 
 
 def _vector(t, name, dtype, n, device):
-    if t.dim() != 1 or t.dtype != dtype or t.device != device or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.dtype != dtype or t.shape != (n,) or t.device != device or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s: a contiguous %s tensor of %d values on %s is wanted, got %s %s on %s"
                          % (name, dtype, n, device, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
 def _scales(t, name, shape, device):
-    import torch
-    if t.dtype != torch.float32 or t.shape != shape or t.device != device:
+    if t.shape != shape or t.dtype != _names.f32 or t.device != device:
         raise ValueError("%s: a float32 tensor of shape %s on %s is wanted, got %s %s on %s"
-                         % (name, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
-    return t.data_ptr(), t.stride(0), t.stride(1)
+                         % (name, shape, device, t.dtype, tuple(t.shape), t.device))
+    s0, s1 = t.stride()
+    return t.data_ptr(), s0, s1
 
 
 def _fp8_weights(wq, ws, k, device):
-    """Pointer arguments of 8-bit weights [n, k] and their scales."""
-    import torch
-    ldw = _matrix(wq, "wq", (torch.float8_e4m3fn, torch.uint8), None, device)
-    n = wq.shape[0]
-    if wq.shape[1] != k:
-        raise ValueError("wq has %d columns, the activations %d" % (wq.shape[1], k))
-    return (wq.data_ptr(), ldw) + _scales(ws, "ws", ((n + 127) // 128, (k + 127) // 128), device)
+    """(n, pointer arguments) of 8-bit weights [n, k] and their scales."""
+    n, kw, ldw = _matrix(wq, "wq", _names.bytes, None, device)
+    if kw != k:
+        raise ValueError("wq has %d columns, the activations %d" % (kw, k))
+    return n, (wq.data_ptr(), ldw) + _scales(ws, "ws", ((n + 127) // 128, (k + 127) // 128), device)
 
 
-def _fp8_out(out, out_dtype, m, n, device, stream):
-    import torch
+def _fp8_out(out, out_dtype, m, n, device):
+    """(y, its ct_dtype, its row pitch)"""
     if out is None:
-        if out_dtype not in _dtypes():
+        code = _names.dtypes.get(out_dtype)
+        if code is None:
             raise ValueError("out_dtype: float32, float16 or bfloat16 is wanted, got %s" % out_dtype)
-        with _on_stream(stream):
-            out = torch.empty(m, n, dtype=out_dtype, device=device)
-        return out, n
+        return _names.empty((m, n), dtype=out_dtype, device=device), code, n
     if out_dtype is not None and out.dtype != out_dtype:
         raise ValueError("out is %s, out_dtype %s" % (out.dtype, out_dtype))
-    return out, _matrix(out, "out", _dtypes(), (m, n), device)
+    ldy = _matrix(out, "out", _names.dtypes, (m, n), device)[2]
+    return out, _names.dtypes[out.dtype], ldy
 
 
 def ct_fp8_quantize(x, block_rows: int = 1, q=None, scale=None, stream=None):
@@ -544,66 +584,54 @@ def ct_fp8_quantize(x, block_rows: int = 1, q=None, scale=None, stream=None):
     block of block_rows x 128 values (1: activations, 128: weights).  q
     [m, k] float8_e4m3fn has a row pitch that is a multiple of 16 bytes, as the
     products want it; scale is float32 [ceil(m / block_rows), ceil(k / 128)]."""
-    import torch
-    ldx = _matrix(x, "x", _dtypes())
-    m, k = x.shape
+    T = _names or _T()
+    m, k, ldx = _matrix(x, "x", T.dtypes)
     if block_rows not in (1, 128):
         raise ValueError("block_rows is 1 or 128, got %r" % (block_rows,))
+    dev = x.device
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_fp8_quantize, dev, stream, x, block_rows, q, scale)
     rows, kb = (m + block_rows - 1) // block_rows, (k + 127) // 128
-    with _on_stream(stream):
-        if q is None:
-            pitch = (k + 15) // 16 * 16
-            q = torch.empty(m, pitch, dtype=torch.float8_e4m3fn, device=x.device)
-            if pitch != k:
-                q = q[:, :k]
-        if scale is None:
-            # activations: [block][row], the order in which the products read them
-            scale = torch.empty(kb, rows, device=x.device).t() if block_rows == 1 else \
-                torch.empty(rows, kb, device=x.device)
-    ldq = _matrix(q, "q", (torch.float8_e4m3fn, torch.uint8), (m, k), x.device)
-    sp, s0, s1 = _scales(scale, "scale", (rows, kb), x.device)
-    with _device(x):
-        _check(lib().ct_fp8_quantize(x.data_ptr(), _DTYPES[x.dtype], m, k, ldx, block_rows, q.data_ptr(), ldq, sp, s0, s1,
-                                     _stream(stream)), "ct_fp8_quantize")
+    if q is None:
+        ldq = (k + 15) // 16 * 16
+        q = T.empty((m, ldq), dtype=T.e4m3, device=dev)
+        if ldq != k:
+            q = q[:, :k]
+    else:
+        ldq = _matrix(q, "q", T.bytes, (m, k), dev)[2]
+    if scale is not None:
+        sp, s0, s1 = _scales(scale, "scale", (rows, kb), dev)
+    elif block_rows == 1:
+        # activations: [block][row], the order in which the products read them
+        scale = T.empty((kb, rows), dtype=T.f32, device=dev).t()
+        sp, s0, s1 = scale.data_ptr(), 1, rows
+    else:
+        scale = T.empty((rows, kb), dtype=T.f32, device=dev)
+        sp, s0, s1 = scale.data_ptr(), kb, 1
+    st = (_lib or lib()).ct_fp8_quantize(x.data_ptr(), T.dtypes[x.dtype], m, k, ldx, block_rows, q.data_ptr(), ldq, sp, s0, s1,
+                                         T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_fp8_quantize")
     return q, scale
-
-
-class _device:
-    """Makes a tensor's device current for a call (nothing to do where it is)."""
-
-    def __init__(self, t):
-        self.index = t.device.index
-        self.before = None
-
-    def __enter__(self):
-        import torch
-        now = torch.cuda.current_device()
-        if now != self.index:
-            self.before = now
-            torch.cuda.set_device(self.index)
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            import torch
-            torch.cuda.set_device(self.before)
 
 
 def ct_fp8_matmul(xq, xs, wq, ws, bias=None, relu: bool = False, out_dtype=None, out=None, stream=None):
     """y [m, n] = act(x w^T + bias) of 8-bit operands: xq [m, k] with scales xs
     [m, ceil(k / 128)], wq [n, k] with scales ws [ceil(n / 128), ceil(k / 128)]
     (any strides).  out_dtype: float32 unless `out` or another type is given."""
-    import torch
-    ldx = _matrix(xq, "xq", (torch.float8_e4m3fn, torch.uint8))
-    m, k = xq.shape
+    T = _names or _T()
+    m, k, ldx = _matrix(xq, "xq", T.bytes)
     dev = xq.device
-    w = _fp8_weights(wq, ws, k, dev)
-    n = wq.shape[0]
-    xsp = _scales(xs, "xs", (m, (k + 127) // 128), dev)
-    b = None if bias is None else _vector(bias, "bias", torch.float32, n, dev)
-    y, ldy = _fp8_out(out, torch.float32 if out is None and out_dtype is None else out_dtype, m, n, dev, stream)
-    with _device(xq):
-        _check(lib().ct_fp8_matmul(xq.data_ptr(), ldx, *xsp, *w, b, int(relu), y.data_ptr(), _dtypes()[y.dtype], ldy,
-                                   m, n, k, _stream(stream)), "ct_fp8_matmul")
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_fp8_matmul, dev, stream, xq, xs, wq, ws, bias, relu, out_dtype, out)
+    n, w = _fp8_weights(wq, ws, k, dev)
+    x = _scales(xs, "xs", (m, (k + 127) // 128), dev)
+    b = None if bias is None else _vector(bias, "bias", T.f32, n, dev)
+    y, code, ldy = _fp8_out(out, T.f32 if out is None and out_dtype is None else out_dtype, m, n, dev)
+    st = (_lib or lib()).ct_fp8_matmul(xq.data_ptr(), ldx, *x, *w, b, 1 if relu else 0, y.data_ptr(), code, ldy, m, n, k,
+                                       T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_fp8_matmul")
     return y
 
 
@@ -611,22 +639,23 @@ def ct_fp8_linear(x, wq, ws, bias=None, relu: bool = False, out_dtype=None, out=
     """act(x W^T + bias) with 8-bit weights on float32 / float16 / bfloat16
     activations x [m, k], quantised on the way (1 x 128 blocks).  out_dtype: x's
     type unless `out` or another type is given."""
-    import torch
-    ldx = _matrix(x, "x", _dtypes())
-    m, k = x.shape
+    T = _names or _T()
+    m, k, ldx = _matrix(x, "x", T.dtypes)
     dev = x.device
-    w = _fp8_weights(wq, ws, k, dev)
-    n = wq.shape[0]
-    b = None if bias is None else _vector(bias, "bias", torch.float32, n, dev)
-    y, ldy = _fp8_out(out, x.dtype if out is None and out_dtype is None else out_dtype, m, n, dev, stream)
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_fp8_linear, dev, stream, x, wq, ws, bias, relu, out_dtype, out)
+    n, w = _fp8_weights(wq, ws, k, dev)
+    b = None if bias is None else _vector(bias, "bias", T.f32, n, dev)
+    y, code, ldy = _fp8_out(out, x.dtype if out is None and out_dtype is None else out_dtype, m, n, dev)
+    L = _lib or lib()
     need = ctypes.c_size_t()
-    _check(lib().ct_fp8_linear_workspace(m, k, ctypes.byref(need)), "ct_fp8_linear_workspace")
-    with _on_stream(stream):
-        work = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    with _device(x):
-        _check(lib().ct_fp8_linear(x.data_ptr(), _DTYPES[x.dtype], ldx, *w, b, int(relu), y.data_ptr(),
-                                   _DTYPES[y.dtype], ldy, m, n, k, work.data_ptr(), need.value, _stream(stream)),
-               "ct_fp8_linear")
+    st = L.ct_fp8_linear_workspace(m, k, need)
+    if not st:
+        work = T.empty(need.value, dtype=T.u8, device=dev)
+        st = L.ct_fp8_linear(x.data_ptr(), T.dtypes[x.dtype], ldx, *w, b, 1 if relu else 0, y.data_ptr(), code, ldy, m, n, k,
+                             work.data_ptr(), need.value, T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_fp8_linear")
     return y
 
 
@@ -635,48 +664,52 @@ def ct_logprobs(logits, ids=None, top_k: int = 0, stream=None):
     the log probability of token ids[r] (int64; -1: none, 0; logprob is None
     without ids), the entropy and log normaliser of each row (float32), and
     its top_k most probable tokens (float32 / int64 [rows, top_k])."""
-    import torch
-    ld = _matrix(logits, "logits", _dtypes())
-    rows, vocab = logits.shape
+    T = _names or _T()
+    rows, vocab, ld = _matrix(logits, "logits", T.dtypes)
     dev = logits.device
-    idp = None if ids is None else _vector(ids, "ids", torch.int64, rows, dev)
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_logprobs, dev, stream, logits, ids, top_k)
+    idp = None if ids is None else _vector(ids, "ids", T.i64, rows, dev)
     if not 0 <= top_k <= CT_MAX_TOP_K:
         raise ValueError("top_k is 0 to %d, got %r" % (CT_MAX_TOP_K, top_k))
-    with _on_stream(stream):
-        num = torch.empty(3, rows, device=dev)
-        top_lp = torch.empty(rows, top_k, device=dev)
-        top_id = torch.empty(rows, top_k, dtype=torch.int64, device=dev)
-    lp, entropy, lse = num.unbind(0)
-    with _device(logits):
-        _check(lib().ct_logprobs(logits.data_ptr(), _DTYPES[logits.dtype], ld, idp, rows, vocab, top_k,
-                                 None if ids is None else lp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
-                                 top_lp.data_ptr(), top_id.data_ptr(), _stream(stream)), "ct_logprobs")
-    return (None if ids is None else lp), entropy, lse, top_lp, top_id
+    lp = None if ids is None else T.empty(rows, dtype=T.f32, device=dev)
+    entropy = T.empty(rows, dtype=T.f32, device=dev)
+    lse = T.empty(rows, dtype=T.f32, device=dev)
+    top_lp = T.empty((rows, top_k), dtype=T.f32, device=dev)
+    top_id = T.empty((rows, top_k), dtype=T.i64, device=dev)
+    st = (_lib or lib()).ct_logprobs(logits.data_ptr(), T.dtypes[logits.dtype], ld, idp, rows, vocab, top_k,
+                                     None if lp is None else lp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                                     top_lp.data_ptr(), top_id.data_ptr(), T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_logprobs")
+    return lp, entropy, lse, top_lp, top_id
 
 
 def ct_logprobs_grad(logits, ids, lse, entropy, g_logprob=None, g_entropy=None, out=None, stream=None):
     """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect
     to the logits, in their type; lse and entropy are ct_logprobs' outputs.
     `out` may be `logits`."""
-    import torch
-    ld = _matrix(logits, "logits", _dtypes())
-    rows, vocab = logits.shape
+    T = _names or _T()
+    rows, vocab, ld = _matrix(logits, "logits", T.dtypes)
     dev = logits.device
-    f32 = torch.float32
-    idp = None if ids is None else _vector(ids, "ids", torch.int64, rows, dev)
-    vec = [None if t is None else _vector(t, name, f32, rows, dev)
-           for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy"))]
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_logprobs_grad, dev, stream, logits, ids, lse, entropy, g_logprob, g_entropy, out)
     if lse is None or (g_logprob is not None and ids is None) or (g_entropy is not None and entropy is None):
         raise ValueError("lse is needed, ids for g_logprob, entropy for g_entropy")
+    f32 = T.f32
+    idp = None if ids is None else _vector(ids, "ids", T.i64, rows, dev)
+    lsep = _vector(lse, "lse", f32, rows, dev)
+    hp = None if entropy is None else _vector(entropy, "entropy", f32, rows, dev)
+    gp = None if g_logprob is None else _vector(g_logprob, "g_logprob", f32, rows, dev)
+    ghp = None if g_entropy is None else _vector(g_entropy, "g_entropy", f32, rows, dev)
     if out is None:
-        with _on_stream(stream):
-            out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
-        ldd = vocab
+        out, ldd = T.empty((rows, vocab), dtype=logits.dtype, device=dev), vocab
     else:
-        ldd = _matrix(out, "out", (logits.dtype,), (rows, vocab), dev)
-    with _device(logits):
-        _check(lib().ct_logprobs_grad(logits.data_ptr(), _DTYPES[logits.dtype], ld, idp, rows, vocab, *vec,
-                                      out.data_ptr(), ldd, _stream(stream)), "ct_logprobs_grad")
+        ldd = _matrix(out, "out", (logits.dtype,), (rows, vocab), dev)[2]
+    st = (_lib or lib()).ct_logprobs_grad(logits.data_ptr(), T.dtypes[logits.dtype], ld, idp, rows, vocab, lsep, hp, gp, ghp,
+                                          out.data_ptr(), ldd, T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_logprobs_grad")
     return out
 
 

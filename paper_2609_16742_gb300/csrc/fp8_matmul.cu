@@ -690,6 +690,8 @@ cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, cons
     static std::atomic<bool> sized[MAX_DEVICES];
     const cudaError_t e = allow_smem(fp8_narrow_kernel<BN>, sized, Shape<BN>::SMEM);
     if (e != cudaSuccess) return e;
+    if (a.splits == 1)
+        return pdl_launch(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Shape<BN>::SMEM, st, lmap, cmap, a);
     return pdl_launch_cluster(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Shape<BN>::SMEM, st, a.splits,
                               lmap, cmap, a);
 }

@@ -28,8 +28,6 @@ struct QuantArgs {
     int xvec, qvec;            // rows of x / q may be read 16 / written 8 (4 for FP32) bytes at a time
 };
 
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
-
 // magnitude bits of a finite value, 0 for a non-finite one: ordered like the magnitudes
 __device__ __forceinline__ uint32_t mag_bits(float v) {
     const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
@@ -44,33 +42,43 @@ __device__ __forceinline__ void block_scale(uint32_t amax, float &scale, float &
     inv = amax == 0u ? 1.f : __uint_as_float((uint32_t)(254 - f) << 23);
 }
 
-// two e4m3 values, `lo` in the low byte; NaN for a non-finite input
+// two e4m3 values, `lo` in the low byte; NaN for a non-finite input (x * 0 is
+// NaN there and 0 elsewhere; the conversion alone would make 448 of infinity)
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi, float inv) {
-    lo = finite(lo) ? lo * inv : __uint_as_float(0x7FC00000u);
-    hi = finite(hi) ? hi * inv : __uint_as_float(0x7FC00000u);
     uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(fmaf(hi, 0.f, hi * inv)), "f"(fmaf(lo, 0.f, lo * inv)));
     return r;
 }
 
+// the V values of row `row` from column c0 on: 16 bytes at once (vec), or one
+// by one with zeros past the end
 template <typename T, int V>
-__device__ __forceinline__ uint32_t load_values(const QuantArgs &a, int64_t row, int64_t c0, bool vec, float *v) {
+__device__ __forceinline__ void load_values(const QuantArgs &a, int64_t row, int64_t c0, bool vec, uint4 &u) {
     const T *p = static_cast<const T *>(a.x) + row * a.ldx + c0;
     if (vec) {
-        unpack16<T>(__ldg(reinterpret_cast<const uint4 *>(p)), v);
+        u = __ldg(reinterpret_cast<const uint4 *>(p));
     } else {
+        float v[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = c0 + i < a.k ? to_f32(p[i]) : 0.f;
+        u = pack16<T>(v);
     }
+}
+
+template <typename T, int V> __device__ __forceinline__ uint32_t largest(const uint4 &u) {
+    float v[V];
+    unpack16<T>(u, v);
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) amax = max(amax, mag_bits(v[i]));
     return amax;
 }
 
-template <int V>
-__device__ __forceinline__ void store_values(const QuantArgs &a, int64_t row, int64_t c0, bool vec, const float *v,
+template <typename T, int V>
+__device__ __forceinline__ void store_values(const QuantArgs &a, int64_t row, int64_t c0, bool vec, const uint4 &u,
                                              float inv) {
+    float v[V];
+    unpack16<T>(u, v);
     uint32_t w[V / 4];
 #pragma unroll
     for (int i = 0; i < V / 4; ++i)
@@ -86,80 +94,103 @@ __device__ __forceinline__ void store_values(const QuantArgs &a, int64_t row, in
     }
 }
 
-constexpr int THREADS = 256;
+constexpr int ROW_THREADS = 256;
+constexpr int ROW_STEPS = 4;                 // blocks of a group: their loads are in flight together
 
-// One block of 128 values of a row for each group of 128 / V lanes.
+// One block of 128 values of a row for each group of 128 / V lanes, ROW_STEPS
+// of them.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) quantize_rows_kernel(const QuantArgs a) {
+__global__ void __launch_bounds__(ROW_THREADS) quantize_rows_kernel(const QuantArgs a) {
     constexpr int V = Vec16<T>::N;
     constexpr int G = 128 / V;               // lanes of a block: 32 (FP32) or 16
+    constexpr int GROUPS = ROW_THREADS / G;
     pdl_wait();
     pdl_trigger();
     const int64_t blocks = a.m * a.kb;
     const int g = threadIdx.x / G, l = threadIdx.x % G;
-    const int64_t at = (int64_t)blockIdx.x * (THREADS / G) + g;
-    const bool live = at < blocks;
-    const int64_t row = live ? at / a.kb : 0, b = live ? at % a.kb : 0;
-    const int64_t c0 = b * 128 + l * V;
-    const bool whole = c0 + V <= a.k;
-    float v[V] = {};
-    uint32_t amax = live ? load_values<T, V>(a, row, c0, a.xvec && whole, v) : 0u;
+    uint4 u[ROW_STEPS];
+    int64_t row[ROW_STEPS], b[ROW_STEPS];
 #pragma unroll
-    for (int d = G / 2; d > 0; d >>= 1) amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
-    if (!live) return;
-    float s, inv;
-    block_scale(amax, s, inv);
-    store_values<V>(a, row, c0, a.qvec && whole, v, inv);
-    if (l == 0) a.scale[row * a.srow + b * a.sblk] = s;
+    for (int i = 0; i < ROW_STEPS; ++i) {
+        const int64_t at = ((int64_t)blockIdx.x * ROW_STEPS + i) * GROUPS + g;
+        row[i] = -1;
+        b[i] = 0;
+        u[i] = make_uint4(0, 0, 0, 0);
+        if (at < blocks) {
+            if (blocks <= UINT32_MAX) {      // one 32-bit division where it is enough
+                row[i] = (uint32_t)at / (uint32_t)a.kb;
+                b[i] = (uint32_t)at % (uint32_t)a.kb;
+            } else {
+                row[i] = at / a.kb;
+                b[i] = at % a.kb;
+            }
+            const int64_t c0 = b[i] * 128 + l * V;
+            load_values<T, V>(a, row[i], c0, a.xvec && c0 + V <= a.k, u[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ROW_STEPS; ++i) {
+        uint32_t amax = largest<T, V>(u[i]);
+#pragma unroll
+        for (int d = G / 2; d > 0; d >>= 1) amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
+        if (row[i] >= 0) {
+            float s, inv;
+            block_scale(amax, s, inv);
+            const int64_t c0 = b[i] * 128 + l * V;
+            store_values<T, V>(a, row[i], c0, a.qvec && c0 + V <= a.k, u[i], inv);
+            if (l == 0) a.scale[row[i] * a.srow + b[i] * a.sblk] = s;
+        }
+    }
 }
+
+constexpr int BLOCK_THREADS = 512;
 
 // One CTA per 128 x 128 block: its values stay in registers between the
 // maximum and the rounding.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) quantize_blocks_kernel(const QuantArgs a) {
+__global__ void __launch_bounds__(BLOCK_THREADS, 2) quantize_blocks_kernel(const QuantArgs a) {
     constexpr int V = Vec16<T>::N;
     constexpr int G = 128 / V;
-    constexpr int ROWS = THREADS / G;        // rows of one step
+    constexpr int ROWS = BLOCK_THREADS / G;  // rows of one step
     constexpr int STEPS = 128 / ROWS;
-    __shared__ uint32_t part[THREADS / 32];
+    __shared__ uint32_t part[BLOCK_THREADS / 32];
     pdl_wait();
     pdl_trigger();
     const int64_t br = blockIdx.x / a.kb, b = blockIdx.x % a.kb;
     const int g = threadIdx.x / G, l = threadIdx.x % G;
-    const int64_t c0 = b * 128 + l * V;
-    const bool whole = c0 + V <= a.k;
-    float v[STEPS][V];
-    uint32_t amax = 0;
+    const int64_t c0 = b * 128 + l * V, r0 = br * 128 + g;
+    const bool inside = b * 128 + 128 <= a.k && br * 128 + 128 <= a.m;
+    uint4 u[STEPS];
+    if (inside && a.xvec) {                  // all loads in flight at once
+        const T *p = static_cast<const T *>(a.x) + r0 * a.ldx + c0;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int64_t row = br * 128 + i * ROWS + g;
-        if (row < a.m) {
-            amax = max(amax, load_values<T, V>(a, row, c0, a.xvec && whole, v[i]));
-        } else {
+        for (int i = 0; i < STEPS; ++i) u[i] = __ldg(reinterpret_cast<const uint4 *>(p + i * ROWS * a.ldx));
+    } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = 0.f;
+        for (int i = 0; i < STEPS; ++i) {
+            u[i] = make_uint4(0, 0, 0, 0);
+            if (r0 + i * ROWS < a.m) load_values<T, V>(a, r0 + i * ROWS, c0, a.xvec && c0 + V <= a.k, u[i]);
         }
     }
+    uint32_t amax = 0;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
+    for (int i = 0; i < STEPS; ++i) amax = max(amax, largest<T, V>(u[i]));
+    amax = __reduce_max_sync(0xFFFFFFFFu, amax);
     if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = amax;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < THREADS / 32; ++i) amax = max(amax, part[i]);
+    amax = __reduce_max_sync(0xFFFFFFFFu, part[threadIdx.x % (BLOCK_THREADS / 32)]);
     float s, inv;
     block_scale(amax, s, inv);
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        const int64_t row = br * 128 + i * ROWS + g;
-        if (row < a.m) store_values<V>(a, row, c0, a.qvec && whole, v[i], inv);
-    }
+    for (int i = 0; i < STEPS; ++i)
+        if (r0 + i * ROWS < a.m) store_values<T, V>(a, r0 + i * ROWS, c0, a.qvec && c0 + V <= a.k, u[i], inv);
     if (threadIdx.x == 0) a.scale[br * a.srow + b * a.sblk] = s;
 }
 
 template <typename T>
 cudaError_t launch(const QuantArgs &a, int block_rows, int64_t grid, cudaStream_t st) {
-    return block_rows == 1 ? pdl_launch(quantize_rows_kernel<T>, dim3((unsigned)grid), dim3(THREADS), 0, st, a)
-                           : pdl_launch(quantize_blocks_kernel<T>, dim3((unsigned)grid), dim3(THREADS), 0, st, a);
+    return block_rows == 1 ? pdl_launch(quantize_rows_kernel<T>, dim3((unsigned)grid), dim3(ROW_THREADS), 0, st, a)
+                           : pdl_launch(quantize_blocks_kernel<T>, dim3((unsigned)grid), dim3(BLOCK_THREADS), 0, st, a);
 }
 
 }  // namespace
@@ -173,7 +204,8 @@ ct_status quantize(const void *x, int dtype, int64_t m, int64_t k, int64_t ldx, 
     const int64_t rows = (m + block_rows - 1) / block_rows;
     if (a.kb > INT64_MAX / 2 / rows) return CT_ERANGE;
     int64_t grid = rows * a.kb;
-    if (block_rows == 1) grid = (grid + THREADS / (128 / per16) - 1) / (THREADS / (128 / per16));
+    const int64_t per_cta = ROW_THREADS / (128 / per16) * ROW_STEPS;
+    if (block_rows == 1) grid = (grid + per_cta - 1) / per_cta;
     if (grid > INT32_MAX) return CT_ERANGE;
     cudaError_t e = dtype == CT_DT_F32   ? launch<float>(a, block_rows, grid, st)
                     : dtype == CT_DT_F16 ? launch<__half>(a, block_rows, grid, st)

@@ -602,7 +602,11 @@ __global__ void __launch_bounds__(NT, Long<NT>::CTAS) logprobs_long_kernel(const
     }
 }
 
-constexpr int THREADS = 256;
+// ---------------------------------------------------------------------------
+// Gradient: each CTA a piece of one row, GRAD_VECS 16-byte vectors a thread.
+// ---------------------------------------------------------------------------
+constexpr int GRAD_THREADS = 256;
+constexpr int GRAD_VECS = 4;
 
 struct GradArgs {
     const void *x;
@@ -612,30 +616,88 @@ struct GradArgs {
     void *dx;
     int64_t lddx;
     int64_t rows, vocab;
-    int vec;
 };
 
+// what a row's gradient needs
+struct GradRow {
+    float lse, g, gh, h;
+    int64_t id;
+    bool bad;
+};
+
+// d = -p (g + gh (log p + h)), without the given token's own g
+__device__ __forceinline__ float grad_value(const GradRow &q, float x) {
+    const float lp = x - q.lse;
+    const float p = ex2(lp * LOG2E);
+    const float d = -p * fmaf(q.gh, lp + q.h, q.g);
+    return p == 0.f ? 0.f : d;                             // also where lp is -inf
+}
+
 template <typename T>
-__global__ void __launch_bounds__(THREADS) logprobs_grad_kernel(const GradArgs a, int chunks, int64_t chunk) {
+__device__ __forceinline__ void grad_one(const GradRow &q, const T *x, T *dx, int64_t j) {
+    float d = grad_value(q, to_f32(x[j]));
+    if (j == q.id) d += q.g;
+    dx[j] = from_f32<T>(q.bad ? nan_f() : d);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradArgs a, int pieces) {
+    constexpr int E = Vec16<T>::N;
     pdl_wait();
     pdl_trigger();
-    const int64_t r = blockIdx.x / chunks;
-    const int64_t j0 = blockIdx.x % chunks * chunk, j1 = min(j0 + chunk, a.vocab);
+    const int64_t r = blockIdx.x / (unsigned)pieces;
+    const int piece = (int)(blockIdx.x % (unsigned)pieces);
     const T *x = static_cast<const T *>(a.x) + r * a.ldx;
     T *dx = static_cast<T *>(a.dx) + r * a.lddx;
-    const float lse = a.lse[r];
-    const int64_t id = a.g_lp != nullptr ? a.ids[r] : -1;
-    const float g = id == -1 ? 0.f : id >= 0 && id < a.vocab ? a.g_lp[r] : nan_f();
-    const float gh = a.g_h != nullptr ? a.g_h[r] : 0.f;
-    const float h = a.g_h != nullptr ? a.entropy[r] : 0.f;
-    for (int64_t j = j0 + threadIdx.x; j < j1; j += THREADS) {
-        const float v = to_f32(x[j]);
-        const float lp = v - lse;
-        float p = v == -INF ? 0.f : expf(lp);
-        float d = p == 0.f ? 0.f : -p * (g + gh * (lp + h));
-        if (j == id) d += g;
-        if (lse != lse || g != g) d = nan_f();
-        dx[j] = from_f32<T>(d);
+    GradRow q;
+    q.lse = a.lse[r];
+    q.id = a.g_lp != nullptr ? a.ids[r] : -1;
+    q.g = q.id == -1 ? 0.f : q.id >= 0 && q.id < a.vocab ? a.g_lp[r] : nan_f();
+    q.gh = a.g_h != nullptr ? a.g_h[r] : 0.f;
+    q.h = a.g_h != nullptr ? a.entropy[r] : 0.f;
+    q.bad = q.lse != q.lse || q.g != q.g;
+    if (q.lse == -INF) q.lse = 0.f;                        // nothing can occur: every p is 0
+    // values before the first 16-byte boundary, and the vectors after it
+    const int64_t head = min((int64_t)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T), a.vocab);
+    const bool same = (((uintptr_t)x ^ (uintptr_t)dx) & 15) == 0;
+    const int64_t vecs = (a.vocab - head) / E, per = GRAD_THREADS * GRAD_VECS;
+    const int64_t v0 = piece * per + threadIdx.x;
+    uint4 u[GRAD_VECS];
+#pragma unroll
+    for (int i = 0; i < GRAD_VECS; ++i) {
+        const int64_t v = v0 + i * GRAD_THREADS;
+        if (v < vecs) u[i] = __ldcs(reinterpret_cast<const uint4 *>(x + head + v * E));
+    }
+    // the ends of the row: its first piece's threads
+    if (piece == 0) {
+        const int64_t tail = head + vecs * E;
+        if ((int64_t)threadIdx.x < head) grad_one(q, x, dx, (int64_t)threadIdx.x);
+        if (tail + (int64_t)threadIdx.x < a.vocab) grad_one(q, x, dx, tail + (int64_t)threadIdx.x);
+    }
+#pragma unroll
+    for (int i = 0; i < GRAD_VECS; ++i) {
+        const int64_t v = v0 + i * GRAD_THREADS;
+        if (v >= vecs) break;
+        const int64_t j = head + v * E;
+        float d[E];
+        unpack16<T>(u[i], d);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] = grad_value(q, d[e]);
+        if (q.id >= j && q.id < j + E) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (q.id == j + e) d[e] += q.g;
+        }
+        if (q.bad) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = nan_f();
+        }
+        if (same) {
+            __stcs(reinterpret_cast<uint4 *>(dx + j), pack16<T>(d));
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) dx[j + e] = from_f32<T>(d[e]);
+        }
     }
 }
 
@@ -650,6 +712,8 @@ template <typename T, int NT> cudaError_t launch_long(const LpArgs &a, cudaStrea
     int splits = 1;
     while (splits < 8 && a.rows * splits * 2 <= slots && splits * 2 <= chunks) splits *= 2;
     const int64_t clusters = a.rows < slots / splits ? a.rows : slots / splits;
+    if (splits == 1)
+        return pdl_launch(logprobs_long_kernel<T, NT>, dim3((unsigned)clusters), dim3(NT), L::SMEM, st, a, splits);
     return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(clusters * splits)), dim3(NT), L::SMEM, st,
                               splits, a, splits);
 }
@@ -710,15 +774,14 @@ extern "C" ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int
         !ct::ops::aligned(g_entropy_dev, 4))
         return CT_EINVAL;
     const GradArgs a = {logits_dev, ld, ids_dev, lse_dev, entropy_dev, g_logprob_dev, g_entropy_dev, dlogits_dev, ld_d,
-                        rows, vocab, 0};
+                        rows, vocab};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int64_t chunk = 8192, chunks = (vocab + chunk - 1) / chunk;
-    if (rows > INT32_MAX / chunks) return CT_ERANGE;
-    const dim3 grid((unsigned)(rows * chunks)), block(THREADS);
+    const int64_t per = (int64_t)GRAD_THREADS * GRAD_VECS * (16 / es), pieces = (vocab + per - 1) / per;
+    if (rows > INT32_MAX / pieces) return CT_ERANGE;
+    const dim3 grid((unsigned)(rows * pieces)), block(GRAD_THREADS);
     const cudaError_t e =
-        dtype == CT_DT_F32   ? ct::pdl_launch(logprobs_grad_kernel<float>, grid, block, 0, st, a, (int)chunks, chunk)
-        : dtype == CT_DT_F16 ? ct::pdl_launch(logprobs_grad_kernel<__half>, grid, block, 0, st, a, (int)chunks, chunk)
-                             : ct::pdl_launch(logprobs_grad_kernel<__nv_bfloat16>, grid, block, 0, st, a, (int)chunks,
-                                              chunk);
+        dtype == CT_DT_F32   ? ct::pdl_launch(logprobs_grad_kernel<float>, grid, block, 0, st, a, (int)pieces)
+        : dtype == CT_DT_F16 ? ct::pdl_launch(logprobs_grad_kernel<__half>, grid, block, 0, st, a, (int)pieces)
+                             : ct::pdl_launch(logprobs_grad_kernel<__nv_bfloat16>, grid, block, 0, st, a, (int)pieces);
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
