@@ -470,7 +470,7 @@ class _TorchNames:
     def __init__(self):
         import torch
         self.torch = torch
-        self.empty = torch.empty
+        self.empty, self.empty_strided = torch.empty, torch.empty_strided
         self.f32, self.u8, self.i64, self.e4m3 = torch.float32, torch.uint8, torch.int64, torch.float8_e4m3fn
         self.dtypes = {torch.float32: CT_DT_F32, torch.float16: CT_DT_F16, torch.bfloat16: CT_DT_BF16}
         self.bytes = {self.e4m3: 0, self.u8: 0}
@@ -603,7 +603,7 @@ def ct_fp8_quantize(x, block_rows: int = 1, q=None, scale=None, stream=None):
         sp, s0, s1 = _scales(scale, "scale", (rows, kb), dev)
     elif block_rows == 1:
         # activations: [block][row], the order in which the products read them
-        scale = T.empty((kb, rows), dtype=T.f32, device=dev).t()
+        scale = T.empty_strided((rows, kb), (1, rows), dtype=T.f32, device=dev)
         sp, s0, s1 = scale.data_ptr(), 1, rows
     else:
         scale = T.empty((rows, kb), dtype=T.f32, device=dev)

@@ -19,6 +19,8 @@ namespace {
 constexpr float INF = __builtin_huge_valf();
 __device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); }
 
+constexpr uint32_t E_LOGPROBS = 0x2000;      // error code of the bounded waits
+
 struct LpArgs {
     const void *x;
     int64_t ldx;
@@ -118,30 +120,54 @@ template <> struct Words<__nv_bfloat16> {
     }
 };
 
+// two FP32 values at once
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // x - m kept away from -inf (a forbidden token, or a mask of the type's lowest
 // value below a large m), where e^(x - m) (x - m) would be NaN instead of 0;
 // keeps NaN
-__device__ __forceinline__ float below(float x, float m) {
+__device__ __forceinline__ float above_inf(float d) {
     float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x - m), "f"(-1e30f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(d), "f"(-1e30f));
     return r;
 }
 
 // Sums of one thread.  A logit more than 8 above the reference moves it.
 template <typename T> struct Sums {
     float m, lim;              // reference; the largest logit it stands for (-inf: none yet)
-    float z0, z1, t0, t1;
+    uint64_t z, t;             // even and odd values'
 
     __device__ __forceinline__ void start() {
         m = 0.f; lim = -INF;
-        z0 = z1 = t0 = t1 = 0.f;
+        z = t = 0;
     }
     __device__ __forceinline__ void raise(float top) {     // top > lim: the largest logit so far
         if (lim > -INF) {
             const float d = m - top, f = ex2(d * LOG2E);
-            t0 = f == 0.f ? 0.f : f * (t0 + d * z0);
-            t1 = f == 0.f ? 0.f : f * (t1 + d * z1);
-            z0 *= f; z1 *= f;
+            t = f == 0.f ? 0 : mul2(pair(f, f), fma2(pair(d, d), z, t));
+            z = mul2(pair(f, f), z);
         }
         m = top;
         lim = top + 8.f;
@@ -149,26 +175,40 @@ template <typename T> struct Sums {
     // N words; `top`: their largest value
     template <int N> __device__ __forceinline__ void add(const uint32_t (&w)[N], float top) {
         if (top > lim) raise(top);
+        const uint64_t minus_m = pair(-m, -m), log2e = pair(LOG2E, LOG2E);
 #pragma unroll
         for (int i = 0; i < N; i += sizeof(T) == 4 ? 2 : 1) {
             const float a = Words<T>::value(w[i], 0);
             const float b = sizeof(T) == 4 ? Words<T>::value(w[sizeof(T) == 4 ? i + 1 : i], 0) : Words<T>::value(w[i], 1);
-            const float d0 = below(a, m), d1 = below(b, m);
-            const float e0 = ex2(d0 * LOG2E), e1 = ex2(d1 * LOG2E);
-            z0 += e0; z1 += e1;
-            t0 = fmaf(e0, d0, t0); t1 = fmaf(e1, d1, t1);
+            float d0, d1, u0, u1;
+            unpair(add2(pair(a, b), minus_m), d0, d1);
+            const uint64_t d = pair(above_inf(d0), above_inf(d1));
+            unpair(mul2(d, log2e), u0, u1);
+            const uint64_t e = pair(ex2(u0), ex2(u1));
+            z = add2(z, e);
+            t = fma2(e, d, t);
         }
     }
     __device__ __forceinline__ Stat stat() const {
+        float z0, z1, t0, t1;
+        unpair(z, z0, z1);
+        unpair(t, t0, t1);
         // the reference of a thread that saw only -inf is -inf; a NaN among them stays in z
         return Stat{lim > -INF ? m : -INF, z0 + z1, t0 + t1};
     }
 };
 
+// over the warp: the largest reference first, then plain sums relative to it
 __device__ __forceinline__ Stat warp_merge(Stat s) {
+    float m = s.m;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
-        s = merge(s, Stat{__shfl_xor_sync(~0u, s.m, d), __shfl_xor_sync(~0u, s.z, d), __shfl_xor_sync(~0u, s.t, d)});
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    s = merge(s, Stat{m, 0.f, 0.f});
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        s.z += __shfl_xor_sync(~0u, s.z, d);
+        s.t += __shfl_xor_sync(~0u, s.t, d);
+    }
     return s;
 }
 
@@ -210,11 +250,14 @@ template <typename T> __device__ __forceinline__ float given_logit(const LpArgs 
 }
 
 // ---------------------------------------------------------------------------
-// Short rows: one warp each, the whole row in registers.  The next top token
-// is the warp's largest key below the last one.
+// Short rows: one warp each, the whole row in registers.  Top tokens: at least
+// top_k logits reach the top_k-th largest of the lanes' maxima; those that do
+// are listed in shared memory and sorted by counting.  Where ties overflow
+// the list, the next token is the warp's largest key below the last one.
 // ---------------------------------------------------------------------------
 constexpr int SHORT = 1024;
 constexpr int SHORT_WARPS = 4;
+constexpr int SHORT_CAP = 192;                             // candidates of a warp
 
 template <typename T>
 __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const LpArgs a, int vec) {
@@ -250,213 +293,335 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
     }
     Sums<T> sums;
     sums.start();
+    float mx = -INF;                                       // this lane's largest logit
 #pragma unroll
     for (int i = 0; i < NW; i += 4) {
         if (i / 4 * 32 * E >= vocab) break;
         uint32_t part[4] = {w[i], w[i + 1], w[i + 2], w[i + 3]};
-        sums.add(part, Words<T>::largest(Words<T>::max2(Words<T>::max2(w[i], w[i + 1]), Words<T>::max2(w[i + 2], w[i + 3]))));
+        const float top =
+            Words<T>::largest(Words<T>::max2(Words<T>::max2(w[i], w[i + 1]), Words<T>::max2(w[i + 2], w[i + 3])));
+        sums.add(part, top);
+        mx = fmaxf(mx, top);
     }
     const RowResult q = row_result(warp_merge(sums.stat()));
     if (lane == 0) write_row(a, r, q, id, given);
-    uint64_t last = ~0ull, mine = ~0ull;                   // mine: this lane's largest key below `last`
-    uint64_t out = 0;                                      // lane i keeps the i-th token
-    for (int k = 0; k < a.top_k && !q.bad; ++k) {
-        if (mine >= last) {
-            mine = 0;
+    if (a.top_k == 0) return;
+    __shared__ uint64_t lists[SHORT_WARPS][SHORT_CAP];
+    uint64_t *list = lists[threadIdx.x / 32];
+    const int k = a.top_k;
+    // the k-th largest of the lanes' maxima
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const float o = __shfl_sync(~0u, mx, i);
+        rank += o > mx || (o == mx && i < lane);
+    }
+    const float thr = __shfl_sync(~0u, mx, __ffs(__ballot_sync(~0u, rank == k - 1)) - 1);
+    // how many of this lane's logits reach it, and where they go in the list
+    int have = 0;
+    if (mx >= thr && mx > -INF) {
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            if (i / 4 * 32 * E >= vocab) break;
+#pragma unroll
+            for (int e = 0; e < W2; ++e) {
+                const float v = Words<T>::value(w[i], e);
+                have += v >= thr && v > -INF;
+            }
+        }
+    }
+    int at = have;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(~0u, at, d);
+        if (lane >= d) at += o;
+    }
+    const int n = __shfl_sync(~0u, at, 31);
+    at -= have;
+    uint64_t out = 0;                                      // lane i: the i-th token
+    if (n <= SHORT_CAP) {
+        if (have > 0) {
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
                 if (i / 4 * 32 * E >= vocab) break;
 #pragma unroll
                 for (int e = 0; e < W2; ++e) {
-                    const uint32_t j = (uint32_t)((i / 4 * 32 + lane) * E + i % 4 * W2 + e);
-                    const uint64_t key = order_key(Words<T>::value(w[i], e), j);
-                    if (key < last && key > mine) mine = key;
+                    const float v = Words<T>::value(w[i], e);
+                    if (v >= thr && v > -INF)
+                        list[at++] = order_key(v, (uint32_t)((i / 4 * 32 + lane) * E + i % 4 * W2 + e));
                 }
             }
         }
-        uint64_t b = mine;
+        __syncwarp();
+        uint64_t keys[SHORT_CAP / 32];
+        int ranks[SHORT_CAP / 32];
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(~0u, b, d));
-        if (lane == k) out = b;
-        last = b;
-        if (b == 0) break;
+        for (int q = 0; q < SHORT_CAP / 32; ++q) {
+            ranks[q] = 0;
+            keys[q] = q * 32 + lane < n ? list[q * 32 + lane] : 0;
+        }
+        for (int j = 0; j < n; ++j) {
+            const uint64_t o = list[j];
+#pragma unroll
+            for (int q = 0; q < SHORT_CAP / 32; ++q)
+                if (q * 32 < n) ranks[q] += o > keys[q];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < SHORT_CAP / 32; ++q)
+            if (q * 32 + lane < n && ranks[q] < k) list[ranks[q]] = keys[q];
+        __syncwarp();
+        if (lane < min(n, k)) out = list[lane];
+    } else {
+        uint64_t last = ~0ull, mine = ~0ull;               // mine: this lane's largest key below `last`
+        for (int t = 0; t < k; ++t) {
+            if (mine >= last) {
+                mine = 0;
+#pragma unroll
+                for (int i = 0; i < NW; ++i) {
+                    if (i / 4 * 32 * E >= vocab) break;
+#pragma unroll
+                    for (int e = 0; e < W2; ++e) {
+                        const uint32_t j = (uint32_t)((i / 4 * 32 + lane) * E + i % 4 * W2 + e);
+                        const uint64_t key = order_key(Words<T>::value(w[i], e), j);
+                        if (key < last && key > mine) mine = key;
+                    }
+                }
+            }
+            uint64_t b = mine;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(~0u, b, d));
+            if (lane == t) out = b;
+            last = b;
+            if (b == 0) break;
+        }
     }
-    if (lane < a.top_k) write_top(a, r, lane, out, q);
+    if (lane < k) write_top(a, r, lane, out, q);
 }
 
 // ---------------------------------------------------------------------------
 // Long rows: a row, or a share of it, streams through shared memory in chunks
-// of 128 bytes a thread, copied by the bulk engine STAGES ahead (of the next
-// row too, while this one is finished).
+// of 128 bytes a thread.  A producer warp has the bulk engine copy STAGES
+// chunks ahead (of the next row too, while this one is finished); the other
+// warps take each chunk at their own pace.
 //
-// Top tokens: `thr` is a logit that at least top_k of the row's tokens reach.
-// A thread that meets a logit >= thr writes its key to a candidate list; the
-// list's best top_k are the answer.  The first chunk (every chunk, until one
-// has enough tokens) sets thr to the top_k-th largest of 64 group maxima and is
-// looked over again by the threads whose maximum reaches it: some 1.1 top_k
-// candidates, and about as many from each later chunk.  A chunk that overflows
-// the list is looked over again with a threshold of its own, and if that fails
-// too (its best tokens all in a few threads' hands) its best are picked one by
-// one.  The list's order varies, the set and its sorted best do not.
+// Top tokens: each thread keeps its largest logit, and that of each of up to 8
+// segments of the row.  thr, the top_k-th largest of 64 group maxima, is reached
+// by at least top_k tokens, and by few threads in few segments (some 1.1 top_k):
+// all threads together look over those threads' logits of those segments
+// again, list the keys that reach thr, and sort the list by counting.  Where ties overflow the list (a row of equal logits), the maxima
+// are taken again as keys, which have no ties; if that overflows too (the best
+// tokens all in a few threads' hands) the best are picked one by one.  The
+// list's order varies, the set and its sorted best do not.
 // ---------------------------------------------------------------------------
 constexpr int STAGES = 3;
 constexpr int THREAD_VECS = 8;                             // 16-byte vectors of a thread in a chunk
 constexpr int BATCH = 4;                                   // ... examined together
+constexpr int SEGMENTS = 8;                                // of a row, for a thread's maxima
 constexpr int GROUPS = 64;                                 // of threads, for the threshold; > CT_MAX_TOP_K
 
+// NT consumer threads and a producer warp
 template <int NT> struct Long {
     static constexpr int CHUNK = NT * THREAD_VECS * 16;    // bytes
     static constexpr int STAGE = CHUNK + 128;              // a row may start anywhere in its first 16 bytes
     static constexpr int CTAS = NT == 256 ? 2 : 7;         // on an SM: what its shared memory holds
-    static constexpr int CAP = NT == 256 ? 2048 : 512;     // candidates
+    static constexpr int CAP = NT == 256 ? 384 : 256;      // candidates; at least NT, and 8 CTAs' top_k
     struct Shared {
-        uint64_t full[STAGES];
+        uint64_t full[STAGES], empty[STAGES];
         uint64_t cand[CAP];
         uint64_t best[CT_MAX_TOP_K];
+        uint64_t group[GROUPS];
+        uint64_t thr;
         uint64_t pick[NT / 32];
         Stat part[NT / 32];
         Stat total;
-        float group[GROUPS];
-        float thr;
-        int count;
+        int count, hits;
+        float seg[SEGMENTS][NT];
+        uint16_t hit[SEGMENTS * NT];                       // thread * SEGMENTS + segment
     };
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + sizeof(Shared) + 16;
+    static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory of an SM");
 };
 
 template <typename T, int NT> struct LongRow {
     using L = Long<NT>;
+    using Shared = typename L::Shared;
     static constexpr int E = Vec16<T>::N;
     static constexpr int W2 = 4 / (int)sizeof(T);
     static constexpr int CE = L::CHUNK / (int)sizeof(T);   // values of a chunk
 
-    // the 4 words of 16-byte vector v of a chunk whose first value lies `shift` bytes into the stage
-    static __device__ __forceinline__ void load(const uint8_t *stage, int v, int shift, uint32_t *w) {
+    // barrier of the consumer threads
+    static __device__ __forceinline__ void sync() { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); }
+
+    // The 4 words of 16-byte vector v of a chunk whose first value lies WS words and `bits` bits into the stage
+    // (WS = -1: at its start).  Which values a thread takes does not depend on where the row starts, so neither do
+    // the sums.
+    template <int WS> static __device__ __forceinline__ void load(const uint8_t *stage, int v, uint32_t bits, uint32_t *w) {
         const uint4 p = *reinterpret_cast<const uint4 *>(stage + v * 16);
-        if (shift == 0) {
+        if constexpr (WS < 0) {
             w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
-            return;
-        }
-        const uint4 n = *reinterpret_cast<const uint4 *>(stage + v * 16 + 16);
-        const uint32_t bits = (uint32_t)(shift & 3) * 8;
-        uint32_t s[5];
-        switch (shift >> 2) {
-            case 0: s[0] = p.x; s[1] = p.y; s[2] = p.z; s[3] = p.w; s[4] = n.x; break;
-            case 1: s[0] = p.y; s[1] = p.z; s[2] = p.w; s[3] = n.x; s[4] = n.y; break;
-            case 2: s[0] = p.z; s[1] = p.w; s[2] = n.x; s[3] = n.y; s[4] = n.z; break;
-            default: s[0] = p.w; s[1] = n.x; s[2] = n.y; s[3] = n.z; s[4] = n.w; break;
-        }
+        } else {
+            const uint4 n = *reinterpret_cast<const uint4 *>(stage + v * 16 + 16);
+            const uint32_t s[8] = {p.x, p.y, p.z, p.w, n.x, n.y, n.z, n.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(s[i], s[i + 1], bits);
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
+        }
     }
-    // ... with the values from n_valid on replaced by -inf
-    static __device__ __forceinline__ void load_masked(const uint8_t *stage, int v, int shift, int n_valid, uint32_t *w) {
-        load(stage, v, shift, w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = Words<T>::mask(w[i], n_valid - v * E - i * W2);
-    }
-    // writes the keys of a thread's values in vectors [i0, i1) that reach thr
-    static __device__ __noinline__ void push(const uint8_t *stage, int shift, int n_valid, int i0, int i1, float thr,
-                                             uint32_t j0, uint64_t *cand, int *count) {
+    // adds a chunk's first n_valid values to the thread's sums; the thread's largest
+    template <int WS>
+    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t bits, int n_valid, Sums<T> &sums) {
+        float mx = -INF;
 #pragma unroll 1
-        for (int i = i0; i < i1; ++i) {
+        for (int i = 0; i < THREAD_VECS; i += BATCH) {
             const int v = i * NT + (int)threadIdx.x;
-            if (v * E >= n_valid) break;
-            uint32_t w[4];
-            load_masked(stage, v, shift, n_valid, w);
+            if ((v & ~31) * E >= n_valid) break;
+            uint32_t w[4 * BATCH];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int b = 0; b < BATCH; ++b) load<WS>(stage, v + b * NT, bits, w + 4 * b);
+            if (n_valid < CE) {
 #pragma unroll
-                for (int e = 0; e < W2; ++e) {
-                    const float x = Words<T>::value(w[q], e);
-                    if (x >= thr && x > -INF) {
-                        const int at = atomicAdd(count, 1);
-                        if (at < L::CAP) cand[at] = order_key(x, j0 + (uint32_t)(v * E + q * W2 + e));
-                    }
-                }
+                for (int b = 0; b < 4 * BATCH; ++b)
+                    w[b] = Words<T>::mask(w[b], n_valid - (v + b / 4 * NT) * E - b % 4 * W2);
+            }
+            uint32_t m2 = w[0];
+#pragma unroll
+            for (int b = 1; b < 4 * BATCH; ++b) m2 = Words<T>::max2(m2, w[b]);
+            const float top = Words<T>::largest(m2);
+            sums.add(w, top);
+            mx = fmaxf(mx, top);
+        }
+        return mx;
+    }
+    // a share of a row in global memory: n values from x on, whose first has index j0 in the row
+    struct Share {
+        const T *x;
+        int64_t n;
+        uint32_t j0;
+        bool vec;                                          // x is 16-byte aligned
+        int seg_vecs;                                      // vectors of a thread in a segment
+        int segs;
+    };
+    // calls f(value, index in the row) for the values of vector v
+    template <typename F> static __device__ __forceinline__ void each(const Share &q, int64_t v, F f) {
+        const int64_t j = v * E;
+        if (q.vec && j + E <= q.n) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(q.x + j));
+            float x[E];
+            unpack16<T>(u, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(x[e], q.j0 + (uint32_t)j + (uint32_t)e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (j + e < q.n) f(to_f32(q.x[j + e]), q.j0 + (uint32_t)j + (uint32_t)e);
         }
     }
-    // the top_k-th largest of the groups' maxima (all threads)
-    static __device__ __forceinline__ float threshold(typename L::Shared &sh, float mx, int k) {
+    // the top_k-th largest of the groups' largest keys (a thread's key: of its largest logit, or its best token)
+    static __device__ __forceinline__ uint64_t threshold(Shared &sh, uint64_t key, int k) {
         constexpr int LANES = NT / GROUPS;
 #pragma unroll
-        for (int d = LANES / 2; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, d));
-        if (threadIdx.x % LANES == 0) sh.group[threadIdx.x / LANES] = mx;
-        __syncthreads();
+        for (int d = LANES / 2; d > 0; d >>= 1) key = max(key, __shfl_xor_sync(~0u, key, d));
+        if (threadIdx.x % LANES == 0) sh.group[threadIdx.x / LANES] = key;
+        sync();
         if (threadIdx.x < GROUPS) {
-            const float g = sh.group[threadIdx.x];
+            const uint64_t g = sh.group[threadIdx.x];
             int rank = 0;
+#pragma unroll 16
             for (int i = 0; i < GROUPS; ++i) {
-                const float o = sh.group[i];
+                const uint64_t o = sh.group[i];
                 rank += o > g || (o == g && i < (int)threadIdx.x);
             }
             if (rank == k - 1) sh.thr = g;
         }
-        __syncthreads();
+        if (threadIdx.x == 0) sh.count = sh.hits = 0;
+        sync();
         return sh.thr;
     }
-    // sorts the list's best top_k into sh.best (all threads)
-    static __device__ __forceinline__ void select(typename L::Shared &sh, int n, int k) {
+    // lists the keys >= thr (not 0) among the logits of the threads' segments whose maxima reach it; the list's
+    // length.  key: this thread's own
+    static __device__ __forceinline__ int collect(Shared &sh, const Share &q, uint64_t key, uint64_t thr) {
+        if (key >= thr && key != 0)
+            for (int g = 0; g < q.segs; ++g)
+                if (order_key(sh.seg[g][threadIdx.x], 0) >= thr)
+                    sh.hit[atomicAdd(&sh.hits, 1)] = (uint16_t)(threadIdx.x * SEGMENTS + g);
+        sync();
+        const int all = sh.hits * q.seg_vecs;
+        const auto list = [&](float x, uint32_t j) {
+            const uint64_t o = order_key(x, j);
+            if (o >= thr && o != 0) {
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < L::CAP) sh.cand[at] = o;
+            }
+        };
+        for (int i = threadIdx.x; i < all; i += NT) {
+            const int h = sh.hit[i / q.seg_vecs];
+            each(q, (int64_t)(h % SEGMENTS * q.seg_vecs + i % q.seg_vecs) * NT + h / SEGMENTS, list);
+        }
+        sync();
+        return sh.count;
+    }
+    // sorts the list's best top_k into sh.best
+    static __device__ __forceinline__ void select(Shared &sh, int n, int k) {
         if ((int)threadIdx.x < k) sh.best[threadIdx.x] = 0;
-        __syncthreads();
+        sync();
         for (int i = threadIdx.x; i < n; i += NT) {
             const uint64_t key = sh.cand[i];
             int rank = 0;
-            for (int j = 0; j < n && rank < k; ++j) rank += sh.cand[j] > key;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) rank += sh.cand[j] > key;
             if (rank < k) sh.best[rank] = key;
         }
-        __syncthreads();
+        sync();
     }
-    // keeps only the list's best top_k; the new threshold
-    static __device__ __noinline__ float compact(typename L::Shared &sh, int n, int k, float thr) {
-        select(sh, n, k);
-        if ((int)threadIdx.x < k) sh.cand[threadIdx.x] = sh.best[threadIdx.x];
-        if (threadIdx.x == 0) sh.count = min(n, k);
-        __syncthreads();
-        return n >= k ? fmaxf(thr, key_value(sh.best[k - 1])) : thr;
+    // the share's best top_k into sh.best; mx: this thread's largest logit
+    static __device__ __forceinline__ void top(Shared &sh, const Share &q, float mx, int k) {
+        // the highest index: the least of the keys with this logit
+        uint64_t key = order_key(mx, 0xFFFFFFFFu);
+        int n = collect(sh, q, key, threshold(sh, key, k));
+        if (n > L::CAP) n = top_ties(sh, q, k);
+        if (n >= 0) select(sh, n, k);
     }
-    // the best top_k of the list's first n and the whole chunk, one by one
-    static __device__ __noinline__ float pick(typename L::Shared &sh, int n, int k, float thr, const uint8_t *stage,
-                                              int shift, int n_valid, uint32_t j0) {
+    // the same where too many logits reach the threshold; -1: sh.best is written
+    static __device__ __noinline__ int top_ties(Shared &sh, const Share &q, int k) {
+        const int64_t vecs = (q.n + E - 1) / E;
+        uint64_t key = 0;
+        for (int64_t v = threadIdx.x; v < vecs; v += NT)
+            each(q, v, [&](float x, uint32_t j) { key = max(key, order_key(x, j)); });
+        // (a segment's maximum says too little here: all segments of the threads that reach it)
+        for (int g = 0; g < q.segs; ++g) sh.seg[g][threadIdx.x] = key_value(key);
+        sh.cand[threadIdx.x] = key;
+        sync();
+        int rank = 0;
+        for (int i = 0; i < NT; ++i) rank += sh.cand[i] > key || (sh.cand[i] == key && i < (int)threadIdx.x);
+        if (rank == k - 1) sh.thr = key;
+        if (threadIdx.x == 0) sh.count = sh.hits = 0;
+        sync();
+        const int n = collect(sh, q, key, sh.thr);
+        if (n <= L::CAP) return n;
+        if ((int)threadIdx.x < k) sh.best[threadIdx.x] = 0;
         uint64_t last = ~0ull;
-        int found = 0;
-        for (; found < k && last != 0; ++found) {
+        for (int i = 0; i < k && last != 0; ++i) {
             uint64_t b = 0;
-            for (int i = threadIdx.x; i < n; i += NT) {
-                const uint64_t key = sh.cand[i];
-                if (key < last && key > b) b = key;
-            }
-#pragma unroll 1
-            for (int i = 0; i < THREAD_VECS; ++i) {
-                const int v = i * NT + (int)threadIdx.x;
-                if (v * E >= n_valid) break;
-                uint32_t w[4];
-                load_masked(stage, v, shift, n_valid, w);
+            for (int64_t v = threadIdx.x; v < vecs; v += NT)
+                each(q, v, [&](float x, uint32_t j) {
+                    const uint64_t o = order_key(x, j);
+                    if (o < last && o > b) b = o;
+                });
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int e = 0; e < W2; ++e) {
-                        const uint64_t key = order_key(Words<T>::value(w[q], e), j0 + (uint32_t)(v * E + q * W2 + e));
-                        if (key < last && key > b) b = key;
-                    }
-            }
             for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(~0u, b, d));
             if (threadIdx.x % 32 == 0) sh.pick[threadIdx.x / 32] = b;
-            __syncthreads();
-            for (int i = 0; i < NT / 32; ++i) b = max(b, sh.pick[i]);
-            if (threadIdx.x == 0) sh.best[found] = b;
+            sync();
+            for (int w = 0; w < NT / 32; ++w) b = max(b, sh.pick[w]);
+            if (threadIdx.x == 0) sh.best[i] = b;
             last = b;
-            __syncthreads();
+            sync();
         }
-        if (last == 0) --found;
-        if ((int)threadIdx.x < found) sh.cand[threadIdx.x] = sh.best[threadIdx.x];
-        if (threadIdx.x == 0) sh.count = found;
-        __syncthreads();
-        return found == k ? fmaxf(thr, key_value(last)) : thr;
+        return -1;
     }
 };
 
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT, Long<NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
+__global__ void __launch_bounds__(NT + 32, Long<NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
     using L = Long<NT>;
     using R = LongRow<T, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -466,110 +631,95 @@ __global__ void __launch_bounds__(NT, Long<NT>::CTAS) logprobs_long_kernel(const
     const int64_t cid = blockIdx.x / (unsigned)splits, ncl = gridDim.x / (unsigned)splits;
     const int chunks = (int)((a.vocab + R::CE - 1) / R::CE);
     const int ch0 = (int)((int64_t)chunks * rank / splits), ch1 = (int)((int64_t)chunks * (rank + 1) / splits);
+    const int seg_chunks = (ch1 - ch0 + SEGMENTS - 1) / SEGMENTS;
     const int k = a.top_k;
 
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) tc::mbar_init(tc::smem_u32(&sh.full[s]), 1);
+        for (int s = 0; s < STAGES; ++s) {
+            tc::mbar_init(tc::smem_u32(&sh.full[s]), 1);
+            tc::mbar_init(tc::smem_u32(&sh.empty[s]), NT / 32);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
     pdl_wait();
     pdl_trigger();
 
-    // thread 0: the next chunk to copy
-    int64_t next_row = cid;
-    int next_ch = ch0;
-    const auto copy_next = [&](int s) {
-        if (next_row >= a.rows) return;
-        const uint8_t *row = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.x) + next_row * a.ldx);
-        const int64_t end = min((int64_t)(next_ch + 1) * L::CHUNK, a.vocab * (int64_t)sizeof(T));
-        // whole 16-byte units that hold a value of the chunk
-        const uintptr_t from = (uintptr_t)(row + (int64_t)next_ch * L::CHUNK) & ~(uintptr_t)15;
-        const uintptr_t to = ((uintptr_t)(row + end) + 15) & ~(uintptr_t)15;
-        const uint32_t bar = tc::smem_u32(&sh.full[s]);
-        tc::mbar_arrive_expect_tx(bar, (uint32_t)(to - from));
-        tc::bulk_load(tc::smem_u32(smem + s * L::STAGE), reinterpret_cast<const void *>(from), (uint32_t)(to - from), bar);
-        if (++next_ch == ch1) { next_ch = ch0; next_row += ncl; }
-    };
-    if (tid == 0)
-        for (int s = 0; s < STAGES; ++s) copy_next(s);
+    if (warp == NT / 32) {
+        if (lane == 0) {
+            int it = 0;
+            for (int64_t r = cid; r < a.rows; r += ncl) {
+                const uint8_t *row = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.x) + r * a.ldx);
+                const int64_t row_bytes = a.vocab * (int64_t)sizeof(T);
+                for (int ch = ch0; ch < ch1; ++ch, ++it) {
+                    const int s = it % STAGES;
+                    // a wait that runs out leaves the results invalid; it is reported
+                    tc::mbar_wait(tc::smem_u32(&sh.empty[s]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_LOGPROBS);
+                    // whole 16-byte units that hold a value of the chunk
+                    const int64_t end = min((int64_t)(ch + 1) * L::CHUNK, row_bytes);
+                    const uintptr_t from = (uintptr_t)(row + (int64_t)ch * L::CHUNK) & ~(uintptr_t)15;
+                    const uintptr_t to = ((uintptr_t)(row + end) + 15) & ~(uintptr_t)15;
+                    const uint32_t bar = tc::smem_u32(&sh.full[s]);
+                    tc::mbar_arrive_expect_tx(bar, (uint32_t)(to - from));
+                    tc::bulk_load(tc::smem_u32(smem + s * L::STAGE), reinterpret_cast<const void *>(from),
+                                  (uint32_t)(to - from), bar);
+                }
+            }
+        }
+        if (splits > 1) {
+            __syncwarp();
+            for (int64_t r = cid; r < a.rows; r += ncl) {
+                tc::cluster_sync();
+                tc::cluster_sync();
+            }
+        }
+        return;
+    }
 
     int it = 0;
     for (int64_t r = cid; r < a.rows; r += ncl) {
-        const int shift = (int)((uintptr_t)(static_cast<const T *>(a.x) + r * a.ldx) & 15);
+        const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+        const int shift = (int)((uintptr_t)row & 15);
         int64_t id = -1;
         const float given = tid == 0 && rank == 0 ? given_logit<T>(a, r, id) : 0.f;
         Sums<T> sums;
         sums.start();
-        float thr = k > 0 ? -INF : INF;
-        if (tid == 0) sh.count = 0;
-        __syncthreads();
+        float mx = -INF, seg_mx = -INF;
         for (int ch = ch0; ch < ch1; ++ch, ++it) {
             const int s = it % STAGES;
             const uint8_t *stage = smem + s * L::STAGE;
-            const uint32_t j0 = (uint32_t)ch * R::CE;
             const int n_valid = (int)min((int64_t)R::CE, a.vocab - (int64_t)ch * R::CE);
-            const int before = k > 0 ? sh.count : 0;       // the same for all threads: between two barriers
-            const bool first = thr == -INF;                // no threshold yet
-            const float limit = first ? INF : thr;
-            // a wait that runs out leaves the results invalid; it is reported
-            tc::mbar_wait(tc::smem_u32(&sh.full[s]), (uint32_t)(it / STAGES) & 1u, a.err, 0x2000u);
-            __syncthreads();
-            float mx = -INF;
-#pragma unroll 1
-            for (int i = 0; i < THREAD_VECS; i += BATCH) {
-                if ((i * NT + (tid & ~31)) * R::E >= n_valid) break;
-                uint32_t w[4 * BATCH];
-                if (n_valid == R::CE) {
-#pragma unroll
-                    for (int b = 0; b < BATCH; ++b) R::load(stage, (i + b) * NT + tid, shift, w + 4 * b);
-                } else {
-#pragma unroll
-                    for (int b = 0; b < BATCH; ++b) R::load_masked(stage, (i + b) * NT + tid, shift, n_valid, w + 4 * b);
-                }
-                uint32_t m2 = w[0];
-#pragma unroll
-                for (int b = 1; b < 4 * BATCH; ++b) m2 = Words<T>::max2(m2, w[b]);
-                const float top = Words<T>::largest(m2);
-                sums.add(w, top);
-                mx = fmaxf(mx, top);
-                if (top >= limit) R::push(stage, shift, n_valid, i, i + BATCH, thr, j0, sh.cand, &sh.count);
+            tc::mbar_wait(tc::smem_u32(&sh.full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_LOGPROBS);
+            __syncwarp();
+            const uint32_t bits = (uint32_t)(shift & 3) * 8;
+            float top;
+            switch (shift == 0 ? -1 : shift >> 2) {
+                case -1: top = R::template chunk<-1>(stage, 0, n_valid, sums); break;
+                case 0: top = R::template chunk<0>(stage, bits, n_valid, sums); break;
+                case 1: top = R::template chunk<1>(stage, bits, n_valid, sums); break;
+                case 2: top = R::template chunk<2>(stage, bits, n_valid, sums); break;
+                default: top = R::template chunk<3>(stage, bits, n_valid, sums); break;
             }
-            if (k > 0) {
-                if (first) {
-                    thr = R::threshold(sh, mx, k);
-                    if (mx >= thr && mx > -INF) R::push(stage, shift, n_valid, 0, THREAD_VECS, thr, j0, sh.cand, &sh.count);
-                }
-                __syncthreads();
-                int n = sh.count;
-                if (n > L::CAP) {
-                    __syncthreads();
-                    if (tid == 0) sh.count = before;
-                    const float own = fmaxf(thr, R::threshold(sh, mx, k));
-                    if (mx >= own && mx > -INF) R::push(stage, shift, n_valid, 0, THREAD_VECS, own, j0, sh.cand, &sh.count);
-                    __syncthreads();
-                    n = sh.count;
-                    if (n > L::CAP) {
-                        __syncthreads();
-                        thr = R::pick(sh, before, k, thr, stage, shift, n_valid, j0);
-                        n = 0;
-                    } else {
-                        thr = own;
-                    }
-                }
-                if (n > L::CAP / 2) {
-                    __syncthreads();
-                    thr = R::compact(sh, n, k, thr);
-                }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.empty[s]));
+            mx = fmaxf(mx, top);
+            seg_mx = fmaxf(seg_mx, top);
+            if ((ch - ch0 + 1) % seg_chunks == 0 || ch + 1 == ch1) {
+                sh.seg[(ch - ch0) / seg_chunks][tid] = seg_mx;
+                seg_mx = -INF;
             }
-            __syncthreads();                               // the chunk has been read
-            if (tid == 0) copy_next(s);
         }
-        // the row
+        // the row, or this CTA's share of it
         Stat st = warp_merge(sums.stat());
         if (lane == 0) sh.part[warp] = st;
-        if (k > 0) R::select(sh, sh.count, k);
-        else __syncthreads();
+        if (k > 0) {
+            const int64_t v0 = (int64_t)ch0 * R::CE;
+            const typename R::Share q = {row + v0, min((int64_t)ch1 * R::CE, a.vocab) - v0, (uint32_t)v0, shift == 0,
+                                        seg_chunks * THREAD_VECS, (ch1 - ch0 + seg_chunks - 1) / seg_chunks};
+            R::top(sh, q, mx, k);
+        } else {
+            R::sync();
+        }
         st = sh.part[0];
 #pragma unroll
         for (int i = 1; i < NT / 32; ++i) st = merge(st, sh.part[i]);
@@ -591,14 +741,14 @@ __global__ void __launch_bounds__(NT, Long<NT>::CTAS) logprobs_long_kernel(const
                 if (k > 0) {
                     for (int i = tid; i < splits * k; i += NT)
                         sh.cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.best[i % k]), (uint32_t)(i / k)));
-                    __syncthreads();
+                    R::sync();
                     R::select(sh, splits * k, k);
                     if (tid < k) write_top(a, r, tid, sh.best[tid], q);
                 }
             }
             tc::cluster_sync();
         }
-        __syncthreads();
+        R::sync();
     }
 }
 
@@ -713,8 +863,8 @@ template <typename T, int NT> cudaError_t launch_long(const LpArgs &a, cudaStrea
     while (splits < 8 && a.rows * splits * 2 <= slots && splits * 2 <= chunks) splits *= 2;
     const int64_t clusters = a.rows < slots / splits ? a.rows : slots / splits;
     if (splits == 1)
-        return pdl_launch(logprobs_long_kernel<T, NT>, dim3((unsigned)clusters), dim3(NT), L::SMEM, st, a, splits);
-    return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(clusters * splits)), dim3(NT), L::SMEM, st,
+        return pdl_launch(logprobs_long_kernel<T, NT>, dim3((unsigned)clusters), dim3(NT + 32), L::SMEM, st, a, splits);
+    return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(clusters * splits)), dim3(NT + 32), L::SMEM, st,
                               splits, a, splits);
 }
 
