@@ -35,6 +35,7 @@ struct LpArgs {
 };
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
     float v;
@@ -54,8 +55,8 @@ __device__ __forceinline__ float ex2(float v) {
 }
 
 // Running sums of a set of logits relative to m, one of its logits near the
-// largest: z = sum e^(x - m), t = sum e^(x - m) (x - m).  m = -inf: nothing but
-// -inf so far.
+// largest, in units of log 2: z = sum 2^u, t = sum 2^u u, u = (x - m) log2(e).
+// m = -inf: nothing but -inf so far.
 struct Stat {
     float m, z, t;
 };
@@ -63,8 +64,8 @@ struct Stat {
 __device__ __forceinline__ Stat merge(const Stat &a, const Stat &b) {
     Stat r;
     r.m = fmaxf(a.m, b.m);
-    const float da = a.m - r.m, db = b.m - r.m;
-    const float fa = a.m == -INF ? 0.f : ex2(da * LOG2E), fb = b.m == -INF ? 0.f : ex2(db * LOG2E);
+    const float da = (a.m - r.m) * LOG2E, db = (b.m - r.m) * LOG2E;
+    const float fa = a.m == -INF ? 0.f : ex2(da), fb = b.m == -INF ? 0.f : ex2(db);
     r.z = fa * a.z + fb * b.z;                 // a NaN or +inf stays one
     r.t = (fa == 0.f ? 0.f : fa * (a.t + da * a.z)) + (fb == 0.f ? 0.f : fb * (b.t + db * b.z));
     return r;
@@ -90,6 +91,13 @@ template <> struct Words<float> {
         return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
     }
     static __device__ __forceinline__ float largest(uint32_t a) { return __uint_as_float(a); }
+    static __device__ __forceinline__ uint32_t dup(float v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static constexpr float MODERATE = 1e6f;
     static __device__ __forceinline__ float value(uint32_t w, int) { return __uint_as_float(w); }
     static __device__ __forceinline__ uint32_t mask(uint32_t w, int valid) { return valid > 0 ? w : 0xFF800000u; }
 };
@@ -99,6 +107,13 @@ template <> struct Words<__half> {
         asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
     }
+    static __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t dup(float v) { return pack2<__half>(v, v); }
+    static constexpr float MODERATE = 6e4f;
     static __device__ __forceinline__ float value(uint32_t w, int i) {
         return __half2float(__ushort_as_half((unsigned short)(i ? w >> 16 : w & 0xFFFFu)));
     }
@@ -113,6 +128,13 @@ template <> struct Words<__nv_bfloat16> {
         asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
     }
+    static __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t dup(float v) { return pack2<__nv_bfloat16>(v, v); }
+    static constexpr float MODERATE = 1e6f;
     static __device__ __forceinline__ float value(uint32_t w, int i) { return __uint_as_float(i ? w & 0xFFFF0000u : w << 16); }
     static __device__ __forceinline__ float largest(uint32_t a) { return fmaxf(value(a, 0), value(a, 1)); }
     static __device__ __forceinline__ uint32_t mask(uint32_t w, int valid) {
@@ -145,56 +167,85 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
-// x - m kept away from -inf (a forbidden token, or a mask of the type's lowest
-// value below a large m), where e^(x - m) (x - m) would be NaN instead of 0;
-// keeps NaN
-__device__ __forceinline__ float above_inf(float d) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(d), "f"(-1e30f));
-    return r;
+// (2^u, 2^u u) with u kept above -inf
+__device__ __noinline__ float2 one_term(float x, float m) {
+    const float u = fmaxf((x - m) * LOG2E, -1e30f), e = x != x ? x : ex2(u);
+    return make_float2(e, e * u);
 }
 
-// Sums of one thread.  A logit more than 8 above the reference moves it.
+// Sums of one thread, relative to one of its logits, m; one more than 8 above it
+// takes its place.
+//
+// The sums are taken with v = x log2(e) - c, c = m log2(e) rounded: one
+// instruction.  v differs from u by what c was rounded by, the same for every
+// x, and stat() takes that out.  Logits that vanish next to m are raised to
+// `low`, a value some 160 or more below it, so that -inf (a forbidden token)
+// and masks of the type's lowest value add 2^v v = 0 * finite and not 0 * inf.
+// Where |m| > MODERATE the rounding of c would matter or the type has no such
+// value; there c is 0 and the terms are taken one by one from x - m.
 template <typename T> struct Sums {
     float m, lim;              // reference; the largest logit it stands for (-inf: none yet)
+    float c;
+    uint32_t low;
     uint64_t z, t;             // even and odd values'
 
     __device__ __forceinline__ void start() {
-        m = 0.f; lim = -INF;
+        m = c = 0.f;
+        lim = -INF;
+        low = Words<T>::dup(-160.f);
         z = t = 0;
     }
+    static __device__ __forceinline__ bool moderate(float m) { return fabsf(m) <= Words<T>::MODERATE; }
+    // v - u
+    __device__ __forceinline__ float rounded() const { return moderate(m) ? fmaf(m, LOG2E, -c) : 0.f; }
     __device__ __forceinline__ void raise(float top) {     // top > lim: the largest logit so far
+        const float cn = moderate(top) ? top * LOG2E : 0.f;
         if (lim > -INF) {
-            const float d = m - top, f = ex2(d * LOG2E);
+            const float d = (m - top) * LOG2E - rounded() + (moderate(top) ? fmaf(top, LOG2E, -cn) : 0.f), f = ex2(d);
             t = f == 0.f ? 0 : mul2(pair(f, f), fma2(pair(d, d), z, t));
             z = mul2(pair(f, f), z);
         }
         m = top;
+        c = cn;
         lim = top + 8.f;
+        low = Words<T>::dup(top - fmaxf(160.f, fabsf(top) * 0.03125f));
     }
     // N words; `top`: their largest value
     template <int N> __device__ __forceinline__ void add(const uint32_t (&w)[N], float top) {
         if (top > lim) raise(top);
-        const uint64_t minus_m = pair(-m, -m), log2e = pair(LOG2E, LOG2E);
+        if (!moderate(m)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < 4 / (int)sizeof(T); ++e) {
+                    const float2 q = one_term(Words<T>::value(w[i], e), m);
+                    z = add2(z, pair(q.x, 0.f));
+                    t = add2(t, pair(q.y, 0.f));
+                }
+            return;
+        }
+        const uint64_t minus_c = pair(-c, -c), log2e = pair(LOG2E, LOG2E);
 #pragma unroll
         for (int i = 0; i < N; i += sizeof(T) == 4 ? 2 : 1) {
-            const float a = Words<T>::value(w[i], 0);
-            const float b = sizeof(T) == 4 ? Words<T>::value(w[sizeof(T) == 4 ? i + 1 : i], 0) : Words<T>::value(w[i], 1);
-            float d0, d1, u0, u1;
-            unpair(add2(pair(a, b), minus_m), d0, d1);
-            const uint64_t d = pair(above_inf(d0), above_inf(d1));
-            unpair(mul2(d, log2e), u0, u1);
-            const uint64_t e = pair(ex2(u0), ex2(u1));
+            const uint32_t x = Words<T>::max2_nan(w[i], low);
+            const float a = Words<T>::value(x, 0);
+            const float b = sizeof(T) == 4 ? Words<T>::value(Words<T>::max2_nan(w[sizeof(T) == 4 ? i + 1 : i], low), 0)
+                                           : Words<T>::value(x, 1);
+            const uint64_t v = fma2(pair(a, b), log2e, minus_c);
+            float v0, v1;
+            unpair(v, v0, v1);
+            const uint64_t e = pair(ex2(v0), ex2(v1));
             z = add2(z, e);
-            t = fma2(e, d, t);
+            t = fma2(e, v, t);
         }
     }
     __device__ __forceinline__ Stat stat() const {
         float z0, z1, t0, t1;
         unpair(z, z0, z1);
         unpair(t, t0, t1);
+        const float d = -rounded(), f = ex2(d), zs = z0 + z1, ts = t0 + t1;
         // the reference of a thread that saw only -inf is -inf; a NaN among them stays in z
-        return Stat{lim > -INF ? m : -INF, z0 + z1, t0 + t1};
+        return Stat{lim > -INF ? m : -INF, f * zs, f * fmaf(d, zs, ts)};
     }
 };
 
@@ -221,9 +272,9 @@ __device__ __forceinline__ RowResult row_result(const Stat &s) {
     RowResult r;
     r.bad = !(s.z < INF);
     r.none = s.m == -INF;
-    const float lz = logf(s.z);
-    r.lse = r.bad ? nan_f() : r.none ? -INF : s.m + lz;
-    r.entropy = r.bad ? nan_f() : r.none ? 0.f : lz - s.t / s.z;
+    const float lz = log2f(s.z);
+    r.lse = r.bad ? nan_f() : r.none ? -INF : fmaf(lz, LN2, s.m);
+    r.entropy = r.bad ? nan_f() : r.none ? 0.f : (lz - s.t / s.z) * LN2;
     return r;
 }
 
@@ -400,58 +451,54 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
 }
 
 // ---------------------------------------------------------------------------
-// Long rows: a row, or a share of it, streams through shared memory in chunks
-// of 128 bytes a thread.  A producer warp has the bulk engine copy STAGES
-// chunks ahead (of the next row too, while this one is finished); the other
-// warps take each chunk at their own pace.
+// Long rows.  A row, or a share of it, streams through shared memory in chunks
+// of 64 bytes a thread.  A producer warp has the bulk engine copy STAGES chunks
+// ahead, the consumer warps take each chunk at their own pace and go on with
+// the next row, and a finisher warp turns what they leave of a row (two
+// buffers) into its results meanwhile.
 //
-// Top tokens: each thread keeps its largest logit, and that of each of up to 8
-// segments of the row.  thr, the top_k-th largest of 64 group maxima, is reached
-// by at least top_k tokens, and by few threads in few segments (some 1.1 top_k):
-// all threads together look over those threads' logits of those segments
-// again, list the keys that reach thr, and sort the list by counting.  Where ties overflow the list (a row of equal logits), the maxima
-// are taken again as keys, which have no ties; if that overflows too (the best
-// tokens all in a few threads' hands) the best are picked one by one.  The
-// list's order varies, the set and its sorted best do not.
+// Top tokens: each consumer thread leaves its largest logit of the row and of
+// each of up to 8 segments of it.  thr, the top_k-th largest of 64 group
+// maxima, is reached by at least top_k tokens, but by few threads in few
+// segments (little more than top_k): the finisher looks over those threads'
+// logits of those segments again, lists the keys that reach thr, and sorts the
+// list by counting.  Where ties overflow the list it lists what exceeds thr and
+// then the first tokens of the row that equal it; where that overflows too
+// (the best tokens all in a few threads' hands) it picks the best one by one.
+// The list's order varies, the set and its sorted best do not.
 // ---------------------------------------------------------------------------
 constexpr int STAGES = 3;
-constexpr int THREAD_VECS = 8;                             // 16-byte vectors of a thread in a chunk
-constexpr int BATCH = 4;                                   // ... examined together
+constexpr int VECS = 4;                                    // 16-byte vectors of a thread in a chunk
 constexpr int SEGMENTS = 8;                                // of a row, for a thread's maxima
-constexpr int GROUPS = 64;                                 // of threads, for the threshold; > CT_MAX_TOP_K
 
-// NT consumer threads and a producer warp
-template <int NT> struct Long {
-    static constexpr int CHUNK = NT * THREAD_VECS * 16;    // bytes
+// NT consumer threads, a producer warp and a finisher warp
+template <typename T, int NT> struct Long {
+    static constexpr int E = Vec16<T>::N;                  // values of a vector
+    static constexpr int W2 = 4 / (int)sizeof(T);          // values of a word
+    static constexpr int CHUNK = NT * VECS * 16;           // bytes
+    static constexpr int CE = CHUNK / (int)sizeof(T);      // values
     static constexpr int STAGE = CHUNK + 128;              // a row may start anywhere in its first 16 bytes
-    static constexpr int CTAS = NT == 256 ? 2 : 7;         // on an SM: what its shared memory holds
-    static constexpr int CAP = NT == 256 ? 384 : 256;      // candidates; at least NT, and 8 CTAs' top_k
+    static constexpr int CTAS = NT == 256 ? 3 : 8;         // on an SM
+    static constexpr int CAP = 8 * CT_MAX_TOP_K;           // candidates; also 8 CTAs' best
+    static constexpr int HITS = 512;                       // thread segments looked over again
+    struct Left {                                          // what the consumers leave of a row
+        Stat part[NT / 32];
+        float mx[NT];
+        T seg[SEGMENTS][NT];
+    };
     struct Shared {
         uint64_t full[STAGES], empty[STAGES];
+        uint64_t left_full[2], left_free[2];
         uint64_t cand[CAP];
         uint64_t best[CT_MAX_TOP_K];
-        uint64_t group[GROUPS];
-        uint64_t thr;
-        uint64_t pick[NT / 32];
-        Stat part[NT / 32];
+        Left left[2];
         Stat total;
-        int count, hits;
-        float seg[SEGMENTS][NT];
-        uint16_t hit[SEGMENTS * NT];                       // thread * SEGMENTS + segment
+        int count;
+        uint8_t thread[NT];                                // threads, and
+        uint16_t hit[HITS];                                // thread segments (thread * SEGMENTS + segment) with top tokens
     };
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + sizeof(Shared) + 16;
     static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory of an SM");
-};
-
-template <typename T, int NT> struct LongRow {
-    using L = Long<NT>;
-    using Shared = typename L::Shared;
-    static constexpr int E = Vec16<T>::N;
-    static constexpr int W2 = 4 / (int)sizeof(T);
-    static constexpr int CE = L::CHUNK / (int)sizeof(T);   // values of a chunk
-
-    // barrier of the consumer threads
-    static __device__ __forceinline__ void sync() { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); }
 
     // The 4 words of 16-byte vector v of a chunk whose first value lies WS words and `bits` bits into the stage
     // (WS = -1: at its start).  Which values a thread takes does not depend on where the row starts, so neither do
@@ -467,32 +514,31 @@ template <typename T, int NT> struct LongRow {
             for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
         }
     }
-    // adds a chunk's first n_valid values to the thread's sums; the thread's largest
+    // adds a chunk's first n_valid values to the thread's sums, releases the stage as soon as it is read; the
+    // thread's largest
     template <int WS>
-    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t bits, int n_valid, Sums<T> &sums) {
-        float mx = -INF;
-#pragma unroll 1
-        for (int i = 0; i < THREAD_VECS; i += BATCH) {
-            const int v = i * NT + (int)threadIdx.x;
-            if ((v & ~31) * E >= n_valid) break;
-            uint32_t w[4 * BATCH];
+    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t bits, int n_valid, uint64_t *empty,
+                                                  Sums<T> &sums) {
+        uint32_t w[4 * VECS];
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) load<WS>(stage, v + b * NT, bits, w + 4 * b);
-            if (n_valid < CE) {
+        for (int b = 0; b < VECS; ++b) load<WS>(stage, b * NT + (int)threadIdx.x, bits, w + 4 * b);
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) tc::mbar_arrive(tc::smem_u32(empty));
+        if (n_valid < CE) {
 #pragma unroll
-                for (int b = 0; b < 4 * BATCH; ++b)
-                    w[b] = Words<T>::mask(w[b], n_valid - (v + b / 4 * NT) * E - b % 4 * W2);
-            }
-            uint32_t m2 = w[0];
-#pragma unroll
-            for (int b = 1; b < 4 * BATCH; ++b) m2 = Words<T>::max2(m2, w[b]);
-            const float top = Words<T>::largest(m2);
-            sums.add(w, top);
-            mx = fmaxf(mx, top);
+            for (int b = 0; b < 4 * VECS; ++b)
+                w[b] = Words<T>::mask(w[b], n_valid - (b / 4 * NT + (int)threadIdx.x) * E - b % 4 * W2);
         }
-        return mx;
+        uint32_t m2 = w[0];
+#pragma unroll
+        for (int b = 1; b < 4 * VECS; ++b) m2 = Words<T>::max2(m2, w[b]);
+        const float top = Words<T>::largest(m2);
+        sums.add(w, top);
+        return top;
     }
-    // a share of a row in global memory: n values from x on, whose first has index j0 in the row
+
+    // ---- the finisher warp ----
+    // a row's share in global memory: n values from x on, whose first has index j0 in the row
     struct Share {
         const T *x;
         int64_t n;
@@ -501,135 +547,189 @@ template <typename T, int NT> struct LongRow {
         int seg_vecs;                                      // vectors of a thread in a segment
         int segs;
     };
-    // calls f(value, index in the row) for the values of vector v
-    template <typename F> static __device__ __forceinline__ void each(const Share &q, int64_t v, F f) {
+    // the words of vector v; -inf past the end
+    static __device__ __forceinline__ uint4 vec(const Share &q, int64_t v) {
         const int64_t j = v * E;
-        if (q.vec && j + E <= q.n) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(q.x + j));
-            float x[E];
-            unpack16<T>(u, x);
+        if (q.vec && j + E <= q.n) return __ldg(reinterpret_cast<const uint4 *>(q.x + j));
+        float x[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(x[e], q.j0 + (uint32_t)j + (uint32_t)e);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (j + e < q.n) f(to_f32(q.x[j + e]), q.j0 + (uint32_t)j + (uint32_t)e);
-        }
+        for (int e = 0; e < E; ++e) x[e] = j + e < q.n ? to_f32(q.x[j + e]) : -INF;
+        return pack16<T>(x);
     }
-    // the top_k-th largest of the groups' largest keys (a thread's key: of its largest logit, or its best token)
-    static __device__ __forceinline__ uint64_t threshold(Shared &sh, uint64_t key, int k) {
-        constexpr int LANES = NT / GROUPS;
+    // 32 bits ordered like the logits, 0 for none
+    static __device__ __forceinline__ uint32_t order(float x) { return (uint32_t)(order_key(x, 0) >> 32); }
+
+    // lists the keys of the logits whose order is at least `from` (> 0), looking at the thread segments that have
+    // any; the list's length, or CAP + 1 where something overflowed
+    static __device__ __forceinline__ int collect(Shared &sh, const Left &left, const Share &q, uint32_t from) {
+        const int lane = threadIdx.x % 32;
+        const uint32_t below = (1u << lane) - 1u;
+        // threads
+        int threads = 0;
+        for (int t = lane; t < NT; t += 32) {
+            const bool hit = order(left.mx[t]) >= from;
+            const uint32_t b = __ballot_sync(~0u, hit);
+            if (hit) sh.thread[threads + __popc(b & below)] = (uint8_t)t;
+            threads += __popc(b);
+        }
+        __syncwarp();
+        // their segments: 4 threads at a time
+        int hits = 0;
+        for (int i = 0; i < threads; i += 4) {
+            const int t = i + lane / SEGMENTS < threads ? sh.thread[i + lane / SEGMENTS] : -1, g = lane % SEGMENTS;
+            const bool hit = t >= 0 && g < q.segs && order(to_f32(left.seg[g][t < 0 ? 0 : t])) >= from;
+            const uint32_t b = __ballot_sync(~0u, hit);
+            if (hits + __popc(b) > HITS) return CAP + 1;
+            if (hit) sh.hit[hits + __popc(b & below)] = (uint16_t)(t * SEGMENTS + g);
+            hits += __popc(b);
+        }
+        if (lane == 0) sh.count = 0;
+        __syncwarp();
+        // their vectors
+        const int all = hits * q.seg_vecs;
+        constexpr int AHEAD = 4;                           // loads in flight together
+        for (int i = lane; i < all; i += 32 * AHEAD) {
+            uint4 x[AHEAD];
+            uint32_t v[AHEAD];
 #pragma unroll
-        for (int d = LANES / 2; d > 0; d >>= 1) key = max(key, __shfl_xor_sync(~0u, key, d));
-        if (threadIdx.x % LANES == 0) sh.group[threadIdx.x / LANES] = key;
-        sync();
-        if (threadIdx.x < GROUPS) {
-            const uint64_t g = sh.group[threadIdx.x];
-            int rank = 0;
-#pragma unroll 16
-            for (int i = 0; i < GROUPS; ++i) {
-                const uint64_t o = sh.group[i];
-                rank += o > g || (o == g && i < (int)threadIdx.x);
+            for (int u = 0; u < AHEAD; ++u) {
+                const int j = i + 32 * u;
+                x[u] = make_uint4(0, 0, 0, 0);
+                v[u] = 0;
+                if (j < all) {
+                    const int h = sh.hit[j / q.seg_vecs], o = j % q.seg_vecs;
+                    v[u] = (uint32_t)(h % SEGMENTS * q.seg_vecs + o) * NT + h / SEGMENTS;
+                    x[u] = vec(q, v[u]);
+                }
             }
-            if (rank == k - 1) sh.thr = g;
-        }
-        if (threadIdx.x == 0) sh.count = sh.hits = 0;
-        sync();
-        return sh.thr;
-    }
-    // lists the keys >= thr (not 0) among the logits of the threads' segments whose maxima reach it; the list's
-    // length.  key: this thread's own
-    static __device__ __forceinline__ int collect(Shared &sh, const Share &q, uint64_t key, uint64_t thr) {
-        if (key >= thr && key != 0)
-            for (int g = 0; g < q.segs; ++g)
-                if (order_key(sh.seg[g][threadIdx.x], 0) >= thr)
-                    sh.hit[atomicAdd(&sh.hits, 1)] = (uint16_t)(threadIdx.x * SEGMENTS + g);
-        sync();
-        const int all = sh.hits * q.seg_vecs;
-        const auto list = [&](float x, uint32_t j) {
-            const uint64_t o = order_key(x, j);
-            if (o >= thr && o != 0) {
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < L::CAP) sh.cand[at] = o;
+#pragma unroll 1
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint4 y = u == 0 ? x[0] : u == 1 ? x[1] : u == 2 ? x[2] : x[3];
+                const uint32_t vu = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
+                const float top = Words<T>::largest(Words<T>::max2(Words<T>::max2(y.x, y.y), Words<T>::max2(y.z, y.w)));
+                if (i + 32 * u < all && order(top) >= from) {
+                    float f[E];
+                    unpack16<T>(y, f);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const uint64_t key = order_key(f[e], q.j0 + vu * E + (uint32_t)e);
+                        if ((uint32_t)(key >> 32) >= from) {
+                            const int at = atomicAdd(&sh.count, 1);
+                            if (at < CAP) sh.cand[at] = key;
+                        }
+                    }
+                }
             }
-        };
-        for (int i = threadIdx.x; i < all; i += NT) {
-            const int h = sh.hit[i / q.seg_vecs];
-            each(q, (int64_t)(h % SEGMENTS * q.seg_vecs + i % q.seg_vecs) * NT + h / SEGMENTS, list);
         }
-        sync();
-        return sh.count;
+        __syncwarp();
+        return min(sh.count, CAP + 1);
     }
-    // sorts the list's best top_k into sh.best
+    // sorts the list's best k into sh.best
     static __device__ __forceinline__ void select(Shared &sh, int n, int k) {
-        if ((int)threadIdx.x < k) sh.best[threadIdx.x] = 0;
-        sync();
-        for (int i = threadIdx.x; i < n; i += NT) {
+        const int lane = threadIdx.x % 32;
+        if (lane < k) sh.best[lane] = 0;
+        __syncwarp();
+        for (int i = lane; i < n; i += 32) {
             const uint64_t key = sh.cand[i];
             int rank = 0;
-#pragma unroll 8
+#pragma unroll 4
             for (int j = 0; j < n; ++j) rank += sh.cand[j] > key;
             if (rank < k) sh.best[rank] = key;
         }
-        sync();
+        __syncwarp();
     }
-    // the share's best top_k into sh.best; mx: this thread's largest logit
-    static __device__ __forceinline__ void top(Shared &sh, const Share &q, float mx, int k) {
-        // the highest index: the least of the keys with this logit
-        uint64_t key = order_key(mx, 0xFFFFFFFFu);
-        int n = collect(sh, q, key, threshold(sh, key, k));
-        if (n > L::CAP) n = top_ties(sh, q, k);
-        if (n >= 0) select(sh, n, k);
+    // the share's best k into sh.best
+    static __device__ __forceinline__ void top(Shared &sh, const Left &left, const Share &q, int k) {
+        const int lane = threadIdx.x % 32;
+        // 64 groups of threads, two for each lane
+        uint32_t g0 = 0, g1 = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 32; i += 2) {
+            g0 = max(g0, order(left.mx[i * 32 + lane]));
+            g1 = max(g1, order(left.mx[i * 32 + 32 + lane]));
+        }
+        int r0 = 0, r1 = g0 >= g1;                         // ranks among them; of equals the lower lane, then g0, comes first
+#pragma unroll 8
+        for (int i = 0; i < 32; ++i) {
+            const uint32_t o0 = __shfl_sync(~0u, g0, i), o1 = __shfl_sync(~0u, g1, i);
+            const uint32_t tie = i < lane ? 1u : 0u;       // a lower lane's equal comes first
+            r0 += i != lane && (o0 > g0 || (o0 == g0 && tie));
+            r0 += i != lane && (o1 > g0 || (o1 == g0 && tie));
+            r1 += i != lane && (o0 > g1 || (o0 == g1 && tie));
+            r1 += i != lane && (o1 > g1 || (o1 == g1 && tie));
+        }
+        r0 += g1 > g0;
+        const uint32_t thr = __reduce_max_sync(~0u, r0 == k - 1 ? g0 : r1 == k - 1 ? g1 : 0u);
+        const int n = thr == 0 ? collect(sh, left, q, 1u) : collect(sh, left, q, thr);
+        if (n <= CAP) select(sh, n, k);
+        else top_ties(sh, q, left, k, thr);
     }
-    // the same where too many logits reach the threshold; -1: sh.best is written
-    static __device__ __noinline__ int top_ties(Shared &sh, const Share &q, int k) {
+    // the same where more logits reach thr than the list holds
+    static __device__ __noinline__ void top_ties(Shared &sh, const Share &q, const Left &left, int k, uint32_t thr) {
+        const int lane = threadIdx.x % 32;
         const int64_t vecs = (q.n + E - 1) / E;
-        uint64_t key = 0;
-        for (int64_t v = threadIdx.x; v < vecs; v += NT)
-            each(q, v, [&](float x, uint32_t j) { key = max(key, order_key(x, j)); });
-        // (a segment's maximum says too little here: all segments of the threads that reach it)
-        for (int g = 0; g < q.segs; ++g) sh.seg[g][threadIdx.x] = key_value(key);
-        sh.cand[threadIdx.x] = key;
-        sync();
-        int rank = 0;
-        for (int i = 0; i < NT; ++i) rank += sh.cand[i] > key || (sh.cand[i] == key && i < (int)threadIdx.x);
-        if (rank == k - 1) sh.thr = key;
-        if (threadIdx.x == 0) sh.count = sh.hits = 0;
-        sync();
-        const int n = collect(sh, q, key, sh.thr);
-        if (n <= L::CAP) return n;
-        if ((int)threadIdx.x < k) sh.best[threadIdx.x] = 0;
+        int n = thr == 0 ? CAP + 1 : collect(sh, left, q, thr + 1);
+        if (n <= CAP) {
+            select(sh, n, k);
+            // ... and the first that equal it, in the row's order
+            for (int64_t v0 = 0; n < k && v0 < vecs; v0 += 32) {
+                float x[E];
+                unpack16<T>(vec(q, v0 + lane), x);
+                int have = 0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) have += order(x[e]) == thr;
+                int at = have;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int u = __shfl_up_sync(~0u, at, d);
+                    if (lane >= d) at += u;
+                }
+                const int found = __shfl_sync(~0u, at, 31);
+                at += n - have;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (order(x[e]) == thr) {
+                        if (at < k) sh.best[at] = order_key(x[e], q.j0 + (uint32_t)((v0 + lane) * E + e));
+                        ++at;
+                    }
+                n += found;
+            }
+            __syncwarp();
+            return;
+        }
+        if (lane < k) sh.best[lane] = 0;
+        __syncwarp();
         uint64_t last = ~0ull;
         for (int i = 0; i < k && last != 0; ++i) {
             uint64_t b = 0;
-            for (int64_t v = threadIdx.x; v < vecs; v += NT)
-                each(q, v, [&](float x, uint32_t j) {
-                    const uint64_t o = order_key(x, j);
-                    if (o < last && o > b) b = o;
-                });
+#pragma unroll 2
+            for (int64_t v = lane; v < vecs; v += 32) {
+                float x[E];
+                unpack16<T>(vec(q, v), x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const uint64_t key = order_key(x[e], q.j0 + (uint32_t)(v * E + e));
+                    if (key < last && key > b) b = key;
+                }
+            }
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) b = max(b, __shfl_xor_sync(~0u, b, d));
-            if (threadIdx.x % 32 == 0) sh.pick[threadIdx.x / 32] = b;
-            sync();
-            for (int w = 0; w < NT / 32; ++w) b = max(b, sh.pick[w]);
-            if (threadIdx.x == 0) sh.best[i] = b;
+            if (lane == 0) sh.best[i] = b;
             last = b;
-            sync();
         }
-        return -1;
+        __syncwarp();
     }
 };
 
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT + 32, Long<NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
-    using L = Long<NT>;
-    using R = LongRow<T, NT>;
+__global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
+    using L = Long<T, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
     typename L::Shared &sh = *reinterpret_cast<typename L::Shared *>(smem + STAGES * L::STAGE);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     const int rank = (int)(blockIdx.x % (unsigned)splits);
     const int64_t cid = blockIdx.x / (unsigned)splits, ncl = gridDim.x / (unsigned)splits;
-    const int chunks = (int)((a.vocab + R::CE - 1) / R::CE);
+    const int chunks = (int)((a.vocab + L::CE - 1) / L::CE);
     const int ch0 = (int)((int64_t)chunks * rank / splits), ch1 = (int)((int64_t)chunks * (rank + 1) / splits);
     const int seg_chunks = (ch1 - ch0 + SEGMENTS - 1) / SEGMENTS;
     const int k = a.top_k;
@@ -639,12 +739,17 @@ __global__ void __launch_bounds__(NT + 32, Long<NT>::CTAS) logprobs_long_kernel(
             tc::mbar_init(tc::smem_u32(&sh.full[s]), 1);
             tc::mbar_init(tc::smem_u32(&sh.empty[s]), NT / 32);
         }
+        for (int b = 0; b < 2; ++b) {
+            tc::mbar_init(tc::smem_u32(&sh.left_full[b]), NT / 32);
+            tc::mbar_init(tc::smem_u32(&sh.left_free[b]), 1);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
     pdl_wait();
     pdl_trigger();
 
+    // a wait that runs out leaves the results invalid; it is reported
     if (warp == NT / 32) {
         if (lane == 0) {
             int it = 0;
@@ -653,7 +758,6 @@ __global__ void __launch_bounds__(NT + 32, Long<NT>::CTAS) logprobs_long_kernel(
                 const int64_t row_bytes = a.vocab * (int64_t)sizeof(T);
                 for (int ch = ch0; ch < ch1; ++ch, ++it) {
                     const int s = it % STAGES;
-                    // a wait that runs out leaves the results invalid; it is reported
                     tc::mbar_wait(tc::smem_u32(&sh.empty[s]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_LOGPROBS);
                     // whole 16-byte units that hold a value of the chunk
                     const int64_t end = min((int64_t)(ch + 1) * L::CHUNK, row_bytes);
@@ -666,89 +770,99 @@ __global__ void __launch_bounds__(NT + 32, Long<NT>::CTAS) logprobs_long_kernel(
                 }
             }
         }
-        if (splits > 1) {
-            __syncwarp();
-            for (int64_t r = cid; r < a.rows; r += ncl) {
-                tc::cluster_sync();
-                tc::cluster_sync();
-            }
-        }
-        return;
-    }
-
-    int it = 0;
-    for (int64_t r = cid; r < a.rows; r += ncl) {
-        const T *row = static_cast<const T *>(a.x) + r * a.ldx;
-        const int shift = (int)((uintptr_t)row & 15);
-        int64_t id = -1;
-        const float given = tid == 0 && rank == 0 ? given_logit<T>(a, r, id) : 0.f;
-        Sums<T> sums;
-        sums.start();
-        float mx = -INF, seg_mx = -INF;
-        for (int ch = ch0; ch < ch1; ++ch, ++it) {
-            const int s = it % STAGES;
-            const uint8_t *stage = smem + s * L::STAGE;
-            const int n_valid = (int)min((int64_t)R::CE, a.vocab - (int64_t)ch * R::CE);
-            tc::mbar_wait(tc::smem_u32(&sh.full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_LOGPROBS);
-            __syncwarp();
-            const uint32_t bits = (uint32_t)(shift & 3) * 8;
-            float top;
-            switch (shift == 0 ? -1 : shift >> 2) {
-                case -1: top = R::template chunk<-1>(stage, 0, n_valid, sums); break;
-                case 0: top = R::template chunk<0>(stage, bits, n_valid, sums); break;
-                case 1: top = R::template chunk<1>(stage, bits, n_valid, sums); break;
-                case 2: top = R::template chunk<2>(stage, bits, n_valid, sums); break;
-                default: top = R::template chunk<3>(stage, bits, n_valid, sums); break;
+        __syncwarp();
+    } else if (warp == NT / 32 + 1) {
+        int n = 0;
+        for (int64_t r = cid; r < a.rows; r += ncl, ++n) {
+            const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+            int64_t id = -1;
+            const float given = lane == 0 && splits == 1 ? given_logit<T>(a, r, id) : 0.f;
+            const typename L::Left &left = sh.left[n & 1];
+            tc::warp_wait(tc::smem_u32(&sh.left_full[n & 1]), (uint32_t)(n >> 1) & 1u, a.err, E_LOGPROBS);
+            const Stat st = warp_merge(lane < NT / 32 ? left.part[lane] : Stat{-INF, 0.f, 0.f});
+            if (k > 0) {
+                const int64_t v0 = (int64_t)ch0 * L::CE;
+                const typename L::Share q = {row + v0, min((int64_t)ch1 * L::CE, a.vocab) - v0, (uint32_t)v0,
+                                             ((uintptr_t)row & 15) == 0, seg_chunks * VECS,
+                                             (ch1 - ch0 + seg_chunks - 1) / seg_chunks};
+                L::top(sh, left, q, k);
             }
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.empty[s]));
-            mx = fmaxf(mx, top);
-            seg_mx = fmaxf(seg_mx, top);
-            if ((ch - ch0 + 1) % seg_chunks == 0 || ch + 1 == ch1) {
-                sh.seg[(ch - ch0) / seg_chunks][tid] = seg_mx;
-                seg_mx = -INF;
-            }
-        }
-        // the row, or this CTA's share of it
-        Stat st = warp_merge(sums.stat());
-        if (lane == 0) sh.part[warp] = st;
-        if (k > 0) {
-            const int64_t v0 = (int64_t)ch0 * R::CE;
-            const typename R::Share q = {row + v0, min((int64_t)ch1 * R::CE, a.vocab) - v0, (uint32_t)v0, shift == 0,
-                                        seg_chunks * THREAD_VECS, (ch1 - ch0 + seg_chunks - 1) / seg_chunks};
-            R::top(sh, q, mx, k);
-        } else {
-            R::sync();
-        }
-        st = sh.part[0];
-#pragma unroll
-        for (int i = 1; i < NT / 32; ++i) st = merge(st, sh.part[i]);
-        if (splits == 1) {
-            const RowResult q = row_result(st);
-            if (tid == 0) write_row(a, r, q, id, given);
-            if (tid < k) write_top(a, r, tid, sh.best[tid], q);
-        } else {
-            // rank 0 joins the shares, in rank order
-            if (tid == 0) sh.total = st;
-            tc::cluster_sync();
-            if (rank == 0) {
-                for (int p = 1; p < splits; ++p) {
-                    const uint32_t at = tc::mapa_shared(tc::smem_u32(&sh.total), (uint32_t)p);
-                    st = merge(st, Stat{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)});
-                }
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_free[n & 1]));
+            if (splits == 1) {
                 const RowResult q = row_result(st);
-                if (tid == 0) write_row(a, r, q, id, given);
-                if (k > 0) {
-                    for (int i = tid; i < splits * k; i += NT)
-                        sh.cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.best[i % k]), (uint32_t)(i / k)));
-                    R::sync();
-                    R::select(sh, splits * k, k);
-                    if (tid < k) write_top(a, r, tid, sh.best[tid], q);
+                if (lane == 0) write_row(a, r, q, id, given);
+                if (lane < k) write_top(a, r, lane, sh.best[lane], q);
+            } else if (lane == 0) {
+                sh.total = st;
+            }
+            __syncwarp();
+        }
+    } else {
+        int it = 0, n = 0;
+        for (int64_t r = cid; r < a.rows; r += ncl, ++n) {
+            const uint32_t shift = (uint32_t)((uintptr_t)(static_cast<const T *>(a.x) + r * a.ldx) & 15);
+            typename L::Left &left = sh.left[n & 1];
+            Sums<T> sums;
+            sums.start();
+            float mx = -INF, seg_mx = -INF;
+            int seg = 0, seg_left = seg_chunks;
+            for (int ch = ch0; ch < ch1; ++ch, ++it) {
+                const int s = it % STAGES;
+                const uint8_t *stage = smem + s * L::STAGE;
+                const int n_valid = (int)min((int64_t)L::CE, a.vocab - (int64_t)ch * L::CE);
+                tc::mbar_wait(tc::smem_u32(&sh.full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_LOGPROBS);
+                const uint32_t bits = (shift & 3u) * 8u;
+                float top;
+                switch (shift == 0 ? -1 : (int)(shift >> 2)) {
+                    case -1: top = L::template chunk<-1>(stage, 0, n_valid, &sh.empty[s], sums); break;
+                    case 0: top = L::template chunk<0>(stage, bits, n_valid, &sh.empty[s], sums); break;
+                    case 1: top = L::template chunk<1>(stage, bits, n_valid, &sh.empty[s], sums); break;
+                    case 2: top = L::template chunk<2>(stage, bits, n_valid, &sh.empty[s], sums); break;
+                    default: top = L::template chunk<3>(stage, bits, n_valid, &sh.empty[s], sums); break;
+                }
+                seg_mx = fmaxf(seg_mx, top);
+                if (--seg_left == 0 || ch + 1 == ch1) {
+                    if (seg == 0)                          // the row before the last is finished
+                        tc::mbar_wait(tc::smem_u32(&sh.left_free[n & 1]), ((uint32_t)(n >> 1) & 1u) ^ 1u, a.err, E_LOGPROBS);
+                    left.seg[seg++][tid] = from_f32<T>(seg_mx);        // exact: a value of this type
+                    mx = fmaxf(mx, seg_mx);
+                    seg_mx = -INF;
+                    seg_left = seg_chunks;
                 }
             }
-            tc::cluster_sync();
+            left.mx[tid] = mx;
+            const Stat st = warp_merge(sums.stat());
+            if (lane == 0) left.part[warp] = st;
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_full[n & 1]));
         }
-        R::sync();
+    }
+    __syncwarp();
+    if (splits > 1) {
+        // one row for each cluster: rank 0's finisher joins the shares, in rank order
+        tc::cluster_sync();
+        if (rank == 0 && warp == NT / 32 + 1) {
+            Stat st = sh.total;
+            for (int p = 1; p < splits; ++p) {
+                const uint32_t at = tc::mapa_shared(tc::smem_u32(&sh.total), (uint32_t)p);
+                st = merge(st, Stat{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)});
+            }
+            const RowResult q = row_result(st);
+            int64_t id = -1;
+            if (lane == 0) {
+                const float given = given_logit<T>(a, cid, id);
+                write_row(a, cid, q, id, given);
+            }
+            if (k > 0) {
+                for (int i = lane; i < splits * k; i += 32)
+                    sh.cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.best[i % k]), (uint32_t)(i / k)));
+                __syncwarp();
+                L::select(sh, splits * k, k);
+                if (lane < k) write_top(a, cid, lane, sh.best[lane], q);
+            }
+        }
+        tc::cluster_sync();
     }
 }
 
@@ -852,20 +966,21 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradA
 }
 
 template <typename T, int NT> cudaError_t launch_long(const LpArgs &a, cudaStream_t st) {
-    using L = Long<NT>;
+    using L = Long<T, NT>;
     static std::atomic<bool> sized[MAX_DEVICES];
     cudaError_t e = allow_smem(logprobs_long_kernel<T, NT>, sized, L::SMEM);
     if (e != cudaSuccess) return e;
     const int64_t slots = (int64_t)sm_count() * L::CTAS;
-    const int64_t chunks = (a.vocab * (int64_t)sizeof(T) + L::CHUNK - 1) / L::CHUNK;
-    // few rows: each is shared by a cluster, so that the whole GPU reads
+    const int64_t chunks = (a.vocab + L::CE - 1) / L::CE;
+    // few rows: each is shared by a cluster (one row each), so that the whole GPU reads
     int splits = 1;
     while (splits < 8 && a.rows * splits * 2 <= slots && splits * 2 <= chunks) splits *= 2;
-    const int64_t clusters = a.rows < slots / splits ? a.rows : slots / splits;
-    if (splits == 1)
-        return pdl_launch(logprobs_long_kernel<T, NT>, dim3((unsigned)clusters), dim3(NT + 32), L::SMEM, st, a, splits);
-    return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(clusters * splits)), dim3(NT + 32), L::SMEM, st,
-                              splits, a, splits);
+    const dim3 block(NT + 64);
+    if (splits > 1)
+        return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(a.rows * splits)), block, L::SMEM, st,
+                                  splits, a, splits);
+    return pdl_launch(logprobs_long_kernel<T, NT>, dim3((unsigned)(a.rows < slots ? a.rows : slots)), block, L::SMEM, st,
+                      a, splits);
 }
 
 template <typename T> cudaError_t launch_logprobs(const LpArgs &a, cudaStream_t st) {
@@ -874,7 +989,7 @@ template <typename T> cudaError_t launch_logprobs(const LpArgs &a, cudaStream_t 
         return pdl_launch(logprobs_short_kernel<T>, dim3((unsigned)((a.rows + SHORT_WARPS - 1) / SHORT_WARPS)),
                           dim3(32 * SHORT_WARPS), 0, st, a, vec);
     }
-    return a.vocab * (int64_t)sizeof(T) <= 4 * Long<64>::CHUNK ? launch_long<T, 64>(a, st) : launch_long<T, 256>(a, st);
+    return a.vocab * (int64_t)sizeof(T) <= 32768 ? launch_long<T, 64>(a, st) : launch_long<T, 256>(a, st);
 }
 
 }  // namespace
