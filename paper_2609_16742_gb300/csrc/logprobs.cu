@@ -454,8 +454,8 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
 // Long rows.  A row, or a share of it, streams through shared memory in chunks
 // of 64 bytes a thread.  A producer warp has the bulk engine copy STAGES chunks
 // ahead, the consumer warps take each chunk at their own pace and go on with
-// the next row, and a finisher warp turns what they leave of a row (two
-// buffers) into its results meanwhile.
+// the next row, and finisher warps, in turn, make a row's results of what they
+// leave of it meanwhile.
 //
 // Top tokens: each consumer thread leaves its largest logit of the row and of
 // each of up to 8 segments of it.  thr, the top_k-th largest of 64 group
@@ -467,20 +467,29 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
 // (the best tokens all in a few threads' hands) it picks the best one by one.
 // The list's order varies, the set and its sorted best do not.
 // ---------------------------------------------------------------------------
-constexpr int STAGES = 3;
 constexpr int VECS = 4;                                    // 16-byte vectors of a thread in a chunk
 constexpr int SEGMENTS = 8;                                // of a row, for a thread's maxima
 
-// NT consumer threads, a producer warp and a finisher warp
+// NT consumer threads, a producer warp and FIN finisher warps
 template <typename T, int NT> struct Long {
     static constexpr int E = Vec16<T>::N;                  // values of a vector
     static constexpr int W2 = 4 / (int)sizeof(T);          // values of a word
     static constexpr int CHUNK = NT * VECS * 16;           // bytes
     static constexpr int CE = CHUNK / (int)sizeof(T);      // values
     static constexpr int STAGE = CHUNK + 128;              // a row may start anywhere in its first 16 bytes
-    static constexpr int CTAS = NT == 256 ? 3 : 8;         // on an SM
+    static constexpr int FIN = NT == 256 ? 2 : 4;
+    static constexpr int THREADS = NT + 32 + 32 * FIN;
+    static constexpr int CTAS = NT == 256 ? 2 : 4;         // on an SM
+    static constexpr int STAGES = 3;
     static constexpr int CAP = 8 * CT_MAX_TOP_K;           // candidates; also 8 CTAs' best
     static constexpr int HITS = 512;                       // thread segments looked over again
+    struct Scratch {                                       // a finisher's
+        uint64_t cand[CAP];
+        uint64_t best[CT_MAX_TOP_K];
+        int count;
+        uint8_t thread[NT];                                // threads, and
+        uint16_t hit[HITS];                                // thread segments (thread * SEGMENTS + segment) with top tokens
+    };
     struct Left {                                          // what the consumers leave of a row
         Stat part[NT / 32];
         float mx[NT];
@@ -488,14 +497,10 @@ template <typename T, int NT> struct Long {
     };
     struct Shared {
         uint64_t full[STAGES], empty[STAGES];
-        uint64_t left_full[2], left_free[2];
-        uint64_t cand[CAP];
-        uint64_t best[CT_MAX_TOP_K];
-        Left left[2];
+        uint64_t left_full[FIN], left_free[FIN];
+        Scratch scratch[FIN];
+        Left left[FIN];
         Stat total;
-        int count;
-        uint8_t thread[NT];                                // threads, and
-        uint16_t hit[HITS];                                // thread segments (thread * SEGMENTS + segment) with top tokens
     };
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + sizeof(Shared) + 16;
     static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory of an SM");
@@ -537,7 +542,7 @@ template <typename T, int NT> struct Long {
         return top;
     }
 
-    // ---- the finisher warp ----
+    // ---- the finisher warps ----
     // a row's share in global memory: n values from x on, whose first has index j0 in the row
     struct Share {
         const T *x;
@@ -556,12 +561,16 @@ template <typename T, int NT> struct Long {
         for (int e = 0; e < E; ++e) x[e] = j + e < q.n ? to_f32(q.x[j + e]) : -INF;
         return pack16<T>(x);
     }
-    // 32 bits ordered like the logits, 0 for none
+    // 32 bits ordered like the logits, 0 for none; and the least logit of that order
     static __device__ __forceinline__ uint32_t order(float x) { return (uint32_t)(order_key(x, 0) >> 32); }
+    static __device__ __forceinline__ float order_value(uint32_t o) {
+        // below every order: the lowest finite number's is the least that a token has
+        return o <= order(-3.402823466e+38f) ? -3.402823466e+38f : key_value((uint64_t)o << 32);
+    }
 
     // lists the keys of the logits whose order is at least `from` (> 0), looking at the thread segments that have
     // any; the list's length, or CAP + 1 where something overflowed
-    static __device__ __forceinline__ int collect(Shared &sh, const Left &left, const Share &q, uint32_t from) {
+    static __device__ __forceinline__ int collect(Scratch &sh, const Left &left, const Share &q, uint32_t from) {
         const int lane = threadIdx.x % 32;
         const uint32_t below = (1u << lane) - 1u;
         // threads
@@ -585,38 +594,32 @@ template <typename T, int NT> struct Long {
         }
         if (lane == 0) sh.count = 0;
         __syncwarp();
-        // their vectors
-        const int all = hits * q.seg_vecs;
-        constexpr int AHEAD = 4;                           // loads in flight together
-        for (int i = lane; i < all; i += 32 * AHEAD) {
-            uint4 x[AHEAD];
-            uint32_t v[AHEAD];
+        // their vectors: 8 lanes take those of one segment
+        const float least = order_value(from);
+        constexpr int AHEAD = 2;                           // loads in flight together
+        for (int i = lane / 8; i < hits; i += 4 * AHEAD) {
+            for (int o = lane % 8; o < q.seg_vecs; o += 8) {
+                uint4 x[AHEAD];
+                uint32_t v[AHEAD];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int j = i + 32 * u;
-                x[u] = make_uint4(0, 0, 0, 0);
-                v[u] = 0;
-                if (j < all) {
-                    const int h = sh.hit[j / q.seg_vecs], o = j % q.seg_vecs;
-                    v[u] = (uint32_t)(h % SEGMENTS * q.seg_vecs + o) * NT + h / SEGMENTS;
-                    x[u] = vec(q, v[u]);
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int h = i + 4 * u < hits ? sh.hit[i + 4 * u] : -1;
+                    v[u] = (uint32_t)((h & (SEGMENTS - 1)) * q.seg_vecs + o) * NT + (uint32_t)(h / SEGMENTS);
+                    if (h >= 0) x[u] = vec(q, v[u]);
+                    else x[u].x = x[u].y = x[u].z = x[u].w = Words<T>::dup(-INF);
                 }
-            }
-#pragma unroll 1
-            for (int u = 0; u < AHEAD; ++u) {
-                const uint4 y = u == 0 ? x[0] : u == 1 ? x[1] : u == 2 ? x[2] : x[3];
-                const uint32_t vu = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
-                const float top = Words<T>::largest(Words<T>::max2(Words<T>::max2(y.x, y.y), Words<T>::max2(y.z, y.w)));
-                if (i + 32 * u < all && order(top) >= from) {
-                    float f[E];
-                    unpack16<T>(y, f);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const uint64_t key = order_key(f[e], q.j0 + vu * E + (uint32_t)e);
-                        if ((uint32_t)(key >> 32) >= from) {
-                            const int at = atomicAdd(&sh.count, 1);
-                            if (at < CAP) sh.cand[at] = key;
-                        }
+                for (int u = 0; u < AHEAD; ++u) {
+                    const uint32_t m2 = Words<T>::max2(Words<T>::max2(x[u].x, x[u].y), Words<T>::max2(x[u].z, x[u].w));
+                    if (Words<T>::largest(m2) >= least) {
+                        float f[E];
+                        unpack16<T>(x[u], f);
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (f[e] >= least) {
+                                const int at = atomicAdd(&sh.count, 1);
+                                if (at < CAP) sh.cand[at] = order_key(f[e], q.j0 + v[u] * E + (uint32_t)e);
+                            }
                     }
                 }
             }
@@ -625,7 +628,7 @@ template <typename T, int NT> struct Long {
         return min(sh.count, CAP + 1);
     }
     // sorts the list's best k into sh.best
-    static __device__ __forceinline__ void select(Shared &sh, int n, int k) {
+    static __device__ __forceinline__ void select(Scratch &sh, int n, int k) {
         const int lane = threadIdx.x % 32;
         if (lane < k) sh.best[lane] = 0;
         __syncwarp();
@@ -639,7 +642,7 @@ template <typename T, int NT> struct Long {
         __syncwarp();
     }
     // the share's best k into sh.best
-    static __device__ __forceinline__ void top(Shared &sh, const Left &left, const Share &q, int k) {
+    static __device__ __forceinline__ void top(Scratch &sh, const Left &left, const Share &q, int k) {
         const int lane = threadIdx.x % 32;
         // 64 groups of threads, two for each lane
         uint32_t g0 = 0, g1 = 0;
@@ -648,24 +651,31 @@ template <typename T, int NT> struct Long {
             g0 = max(g0, order(left.mx[i * 32 + lane]));
             g1 = max(g1, order(left.mx[i * 32 + 32 + lane]));
         }
-        int r0 = 0, r1 = g0 >= g1;                         // ranks among them; of equals the lower lane, then g0, comes first
-#pragma unroll 8
-        for (int i = 0; i < 32; ++i) {
-            const uint32_t o0 = __shfl_sync(~0u, g0, i), o1 = __shfl_sync(~0u, g1, i);
-            const uint32_t tie = i < lane ? 1u : 0u;       // a lower lane's equal comes first
-            r0 += i != lane && (o0 > g0 || (o0 == g0 && tie));
-            r0 += i != lane && (o1 > g0 || (o1 == g0 && tie));
-            r1 += i != lane && (o0 > g1 || (o0 == g1 && tie));
-            r1 += i != lane && (o1 > g1 || (o1 == g1 && tie));
+        // sorted by a bitonic network, descending: position lane in g0, 32 + lane in g1
+#pragma unroll
+        for (int size = 2; size <= 64; size *= 2) {
+#pragma unroll
+            for (int d = size / 2; d > 0; d /= 2) {
+                if (d == 32) {
+                    const uint32_t hi = max(g0, g1);
+                    g1 = min(g0, g1);
+                    g0 = hi;
+                } else {
+                    const uint32_t o0 = __shfl_xor_sync(~0u, g0, d), o1 = __shfl_xor_sync(~0u, g1, d);
+                    const bool first = (lane & d) == 0;
+                    const bool down0 = (lane & size) == 0 || size == 64, down1 = ((32 + lane) & size) == 0 || size == 64;
+                    g0 = first == down0 ? max(g0, o0) : min(g0, o0);
+                    g1 = first == down1 ? max(g1, o1) : min(g1, o1);
+                }
+            }
         }
-        r0 += g1 > g0;
-        const uint32_t thr = __reduce_max_sync(~0u, r0 == k - 1 ? g0 : r1 == k - 1 ? g1 : 0u);
+        const uint32_t thr = __shfl_sync(~0u, g0, k - 1);  // k <= 32
         const int n = thr == 0 ? collect(sh, left, q, 1u) : collect(sh, left, q, thr);
         if (n <= CAP) select(sh, n, k);
         else top_ties(sh, q, left, k, thr);
     }
     // the same where more logits reach thr than the list holds
-    static __device__ __noinline__ void top_ties(Shared &sh, const Share &q, const Left &left, int k, uint32_t thr) {
+    static __device__ __noinline__ void top_ties(Scratch &sh, const Share &q, const Left &left, int k, uint32_t thr) {
         const int lane = threadIdx.x % 32;
         const int64_t vecs = (q.n + E - 1) / E;
         int n = thr == 0 ? CAP + 1 : collect(sh, left, q, thr + 1);
@@ -722,8 +732,9 @@ template <typename T, int NT> struct Long {
 };
 
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
+__global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
     using L = Long<T, NT>;
+    constexpr int STAGES = L::STAGES, FIN = L::FIN;
     extern __shared__ __align__(128) uint8_t smem[];
     typename L::Shared &sh = *reinterpret_cast<typename L::Shared *>(smem + STAGES * L::STAGE);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -739,7 +750,7 @@ __global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kern
             tc::mbar_init(tc::smem_u32(&sh.full[s]), 1);
             tc::mbar_init(tc::smem_u32(&sh.empty[s]), NT / 32);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < FIN; ++b) {
             tc::mbar_init(tc::smem_u32(&sh.left_full[b]), NT / 32);
             tc::mbar_init(tc::smem_u32(&sh.left_free[b]), 1);
         }
@@ -771,38 +782,41 @@ __global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kern
             }
         }
         __syncwarp();
-    } else if (warp == NT / 32 + 1) {
-        int n = 0;
-        for (int64_t r = cid; r < a.rows; r += ncl, ++n) {
+    } else if (warp > NT / 32) {
+        const int f = warp - NT / 32 - 1;                  // rows f, f + FIN, ... of this CTA's
+        typename L::Scratch &scratch = sh.scratch[f];
+        const typename L::Left &left = sh.left[f];
+        uint32_t phase = 0;
+        for (int64_t r = cid + f * ncl; r < a.rows; r += FIN * ncl, phase ^= 1u) {
             const T *row = static_cast<const T *>(a.x) + r * a.ldx;
             int64_t id = -1;
             const float given = lane == 0 && splits == 1 ? given_logit<T>(a, r, id) : 0.f;
-            const typename L::Left &left = sh.left[n & 1];
-            tc::warp_wait(tc::smem_u32(&sh.left_full[n & 1]), (uint32_t)(n >> 1) & 1u, a.err, E_LOGPROBS);
+            tc::warp_wait(tc::smem_u32(&sh.left_full[f]), phase, a.err, E_LOGPROBS);
             const Stat st = warp_merge(lane < NT / 32 ? left.part[lane] : Stat{-INF, 0.f, 0.f});
             if (k > 0) {
                 const int64_t v0 = (int64_t)ch0 * L::CE;
                 const typename L::Share q = {row + v0, min((int64_t)ch1 * L::CE, a.vocab) - v0, (uint32_t)v0,
                                              ((uintptr_t)row & 15) == 0, seg_chunks * VECS,
                                              (ch1 - ch0 + seg_chunks - 1) / seg_chunks};
-                L::top(sh, left, q, k);
+                L::top(scratch, left, q, k);
             }
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_free[n & 1]));
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_free[f]));
             if (splits == 1) {
                 const RowResult q = row_result(st);
                 if (lane == 0) write_row(a, r, q, id, given);
-                if (lane < k) write_top(a, r, lane, sh.best[lane], q);
+                if (lane < k) write_top(a, r, lane, scratch.best[lane], q);
             } else if (lane == 0) {
                 sh.total = st;
             }
             __syncwarp();
         }
     } else {
-        int it = 0, n = 0;
-        for (int64_t r = cid; r < a.rows; r += ncl, ++n) {
+        int it = 0, f = 0;                                 // f: whose turn it is to finish the row
+        uint32_t phase = 0;
+        for (int64_t r = cid; r < a.rows; r += ncl) {
             const uint32_t shift = (uint32_t)((uintptr_t)(static_cast<const T *>(a.x) + r * a.ldx) & 15);
-            typename L::Left &left = sh.left[n & 1];
+            typename L::Left &left = sh.left[f];
             Sums<T> sums;
             sums.start();
             float mx = -INF, seg_mx = -INF;
@@ -823,8 +837,8 @@ __global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kern
                 }
                 seg_mx = fmaxf(seg_mx, top);
                 if (--seg_left == 0 || ch + 1 == ch1) {
-                    if (seg == 0)                          // the row before the last is finished
-                        tc::mbar_wait(tc::smem_u32(&sh.left_free[n & 1]), ((uint32_t)(n >> 1) & 1u) ^ 1u, a.err, E_LOGPROBS);
+                    if (seg == 0)                          // the row FIN before is finished
+                        tc::mbar_wait(tc::smem_u32(&sh.left_free[f]), phase ^ 1u, a.err, E_LOGPROBS);
                     left.seg[seg++][tid] = from_f32<T>(seg_mx);        // exact: a value of this type
                     mx = fmaxf(mx, seg_mx);
                     seg_mx = -INF;
@@ -835,12 +849,16 @@ __global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kern
             const Stat st = warp_merge(sums.stat());
             if (lane == 0) left.part[warp] = st;
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_full[n & 1]));
+            if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_full[f]));
+            if (++f == FIN) {
+                f = 0;
+                phase ^= 1u;
+            }
         }
     }
     __syncwarp();
     if (splits > 1) {
-        // one row for each cluster: rank 0's finisher joins the shares, in rank order
+        // one row for each cluster: rank 0's first finisher joins the shares, in rank order
         tc::cluster_sync();
         if (rank == 0 && warp == NT / 32 + 1) {
             Stat st = sh.total;
@@ -856,10 +874,10 @@ __global__ void __launch_bounds__(NT + 64, Long<T, NT>::CTAS) logprobs_long_kern
             }
             if (k > 0) {
                 for (int i = lane; i < splits * k; i += 32)
-                    sh.cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.best[i % k]), (uint32_t)(i / k)));
+                    sh.scratch[0].cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[i % k]), (uint32_t)(i / k)));
                 __syncwarp();
-                L::select(sh, splits * k, k);
-                if (lane < k) write_top(a, cid, lane, sh.best[lane], q);
+                L::select(sh.scratch[0], splits * k, k);
+                if (lane < k) write_top(a, cid, lane, sh.scratch[0].best[lane], q);
             }
         }
         tc::cluster_sync();
@@ -975,7 +993,7 @@ template <typename T, int NT> cudaError_t launch_long(const LpArgs &a, cudaStrea
     // few rows: each is shared by a cluster (one row each), so that the whole GPU reads
     int splits = 1;
     while (splits < 8 && a.rows * splits * 2 <= slots && splits * 2 <= chunks) splits *= 2;
-    const dim3 block(NT + 64);
+    const dim3 block(L::THREADS);
     if (splits > 1)
         return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(a.rows * splits)), block, L::SMEM, st,
                                   splits, a, splits);
