@@ -450,112 +450,73 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
     if (lane < k) write_top(a, r, lane, out, q);
 }
 
+// 16 bytes from `shift` bytes on of the 32 in p, n
+__device__ __forceinline__ uint4 shifted(const uint4 &p, const uint4 &n, uint32_t shift) {
+    const uint32_t bits = (shift & 3u) * 8u;
+    switch (shift >> 2) {
+        case 0:
+            return make_uint4(__funnelshift_r(p.x, p.y, bits), __funnelshift_r(p.y, p.z, bits),
+                              __funnelshift_r(p.z, p.w, bits), __funnelshift_r(p.w, n.x, bits));
+        case 1:
+            return make_uint4(__funnelshift_r(p.y, p.z, bits), __funnelshift_r(p.z, p.w, bits),
+                              __funnelshift_r(p.w, n.x, bits), __funnelshift_r(n.x, n.y, bits));
+        case 2:
+            return make_uint4(__funnelshift_r(p.z, p.w, bits), __funnelshift_r(p.w, n.x, bits),
+                              __funnelshift_r(n.x, n.y, bits), __funnelshift_r(n.y, n.z, bits));
+        default:
+            return make_uint4(__funnelshift_r(p.w, n.x, bits), __funnelshift_r(n.x, n.y, bits),
+                              __funnelshift_r(n.y, n.z, bits), __funnelshift_r(n.z, n.w, bits));
+    }
+}
+
 // ---------------------------------------------------------------------------
-// Long rows.  A row, or a share of it, streams through shared memory in chunks
-// of 64 bytes a thread.  A producer warp has the bulk engine copy STAGES chunks
-// ahead, the consumer warps take each chunk at their own pace and go on with
-// the next row, and finisher warps, in turn, make a row's results of what they
-// leave of it meanwhile.
-//
-// Top tokens: each consumer thread leaves its largest logit of the row and of
-// each of up to 8 segments of it.  thr, the top_k-th largest of 64 group
-// maxima, is reached by at least top_k tokens, but by few threads in few
-// segments (little more than top_k): the finisher looks over those threads'
-// logits of those segments again, lists the keys that reach thr, and sorts the
-// list by counting.  Where ties overflow the list it lists what exceeds thr and
-// then the first tokens of the row that equal it; where that overflows too
-// (the best tokens all in a few threads' hands) it picks the best one by one.
-// The list's order varies, the set and its sorted best do not.
+// Top tokens of a row, or of a share of it, that NT threads read in vectors of
+// 16 bytes, thread t vectors t, t + NT, ...  Each thread leaves its largest logit of
+// the row and of each of up to 8 segments of it.  thr, the top_k-th largest of
+// (up to) 64 group maxima, is reached by at least top_k tokens, but by few
+// threads in few segments (little more than top_k): one warp looks over those
+// threads' logits of those segments again, lists the keys that reach thr, and
+// sorts the list by counting.  Where ties overflow the list it lists what
+// exceeds thr and then the first tokens of the row that equal it; where that
+// overflows too (the best tokens all in a few threads' hands) it picks the
+// best one by one.  The list's order varies, the set and its sorted best do not.
 // ---------------------------------------------------------------------------
-constexpr int VECS = 4;                                    // 16-byte vectors of a thread in a chunk
+constexpr int VECS = 4;                                    // 16-byte vectors that a thread examines together
 constexpr int SEGMENTS = 8;                                // of a row, for a thread's maxima
 
-// NT consumer threads, a producer warp and FIN finisher warps
-template <typename T, int NT> struct Long {
+template <typename T, int NT> struct Top {
     static constexpr int E = Vec16<T>::N;                  // values of a vector
     static constexpr int W2 = 4 / (int)sizeof(T);          // values of a word
-    static constexpr int CHUNK = NT * VECS * 16;           // bytes
-    static constexpr int CE = CHUNK / (int)sizeof(T);      // values
-    static constexpr int STAGE = CHUNK + 128;              // a row may start anywhere in its first 16 bytes
-    static constexpr int FIN = NT == 256 ? 2 : 4;
-    static constexpr int THREADS = NT + 32 + 32 * FIN;
-    static constexpr int CTAS = NT == 256 ? 2 : 4;         // on an SM
-    static constexpr int STAGES = 3;
     static constexpr int CAP = 8 * CT_MAX_TOP_K;           // candidates; also 8 CTAs' best
-    static constexpr int HITS = 512;                       // thread segments looked over again
-    struct Scratch {                                       // a finisher's
+    static constexpr int HITS = 8 * (NT < 64 ? NT : 64);   // thread segments looked over again
+    struct Scratch {                                       // a finishing warp's
         uint64_t cand[CAP];
         uint64_t best[CT_MAX_TOP_K];
         int count;
         uint8_t thread[NT];                                // threads, and
         uint16_t hit[HITS];                                // thread segments (thread * SEGMENTS + segment) with top tokens
     };
-    struct Left {                                          // what the consumers leave of a row
-        Stat part[NT / 32];
+    struct Left {                                          // what the threads leave of a row
         float mx[NT];
         T seg[SEGMENTS][NT];
     };
-    struct Shared {
-        uint64_t full[STAGES], empty[STAGES];
-        uint64_t left_full[FIN], left_free[FIN];
-        Scratch scratch[FIN];
-        Left left[FIN];
-        Stat total;
-    };
-    static constexpr size_t SMEM = (size_t)STAGES * STAGE + sizeof(Shared) + 16;
-    static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory of an SM");
-
-    // The 4 words of 16-byte vector v of a chunk whose first value lies WS words and `bits` bits into the stage
-    // (WS = -1: at its start).  Which values a thread takes does not depend on where the row starts, so neither do
-    // the sums.
-    template <int WS> static __device__ __forceinline__ void load(const uint8_t *stage, int v, uint32_t bits, uint32_t *w) {
-        const uint4 p = *reinterpret_cast<const uint4 *>(stage + v * 16);
-        if constexpr (WS < 0) {
-            w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
-        } else {
-            const uint4 n = *reinterpret_cast<const uint4 *>(stage + v * 16 + 16);
-            const uint32_t s[8] = {p.x, p.y, p.z, p.w, n.x, n.y, n.z, n.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
-        }
-    }
-    // adds a chunk's first n_valid values to the thread's sums, releases the stage as soon as it is read; the
-    // thread's largest
-    template <int WS>
-    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t bits, int n_valid, uint64_t *empty,
-                                                  Sums<T> &sums) {
-        uint32_t w[4 * VECS];
-#pragma unroll
-        for (int b = 0; b < VECS; ++b) load<WS>(stage, b * NT + (int)threadIdx.x, bits, w + 4 * b);
-        __syncwarp();
-        if (threadIdx.x % 32 == 0) tc::mbar_arrive(tc::smem_u32(empty));
-        if (n_valid < CE) {
-#pragma unroll
-            for (int b = 0; b < 4 * VECS; ++b)
-                w[b] = Words<T>::mask(w[b], n_valid - (b / 4 * NT + (int)threadIdx.x) * E - b % 4 * W2);
-        }
-        uint32_t m2 = w[0];
-#pragma unroll
-        for (int b = 1; b < 4 * VECS; ++b) m2 = Words<T>::max2(m2, w[b]);
-        const float top = Words<T>::largest(m2);
-        sums.add(w, top);
-        return top;
-    }
-
-    // ---- the finisher warps ----
     // a row's share in global memory: n values from x on, whose first has index j0 in the row
     struct Share {
         const T *x;
         int64_t n;
         uint32_t j0;
-        bool vec;                                          // x is 16-byte aligned
+        uint32_t shift;                                    // bytes by which x misses a 16-byte boundary
         int seg_vecs;                                      // vectors of a thread in a segment
         int segs;
     };
-    // the words of vector v; -inf past the end
+    // the words of vector v, wherever it starts; -inf past the end
     static __device__ __forceinline__ uint4 vec(const Share &q, int64_t v) {
         const int64_t j = v * E;
-        if (q.vec && j + E <= q.n) return __ldg(reinterpret_cast<const uint4 *>(q.x + j));
+        if (j + E <= q.n) {
+            if (q.shift == 0) return __ldg(reinterpret_cast<const uint4 *>(q.x + j));
+            const uint4 *at = reinterpret_cast<const uint4 *>((uintptr_t)(q.x + j) & ~(uintptr_t)15);
+            return shifted(__ldg(at), __ldg(at + 1), q.shift);
+        }
         float x[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = j + e < q.n ? to_f32(q.x[j + e]) : -INF;
@@ -644,12 +605,12 @@ template <typename T, int NT> struct Long {
     // the share's best k into sh.best
     static __device__ __forceinline__ void top(Scratch &sh, const Left &left, const Share &q, int k) {
         const int lane = threadIdx.x % 32;
-        // 64 groups of threads, two for each lane
+        // up to 64 groups of threads, two for each lane
         uint32_t g0 = 0, g1 = 0;
 #pragma unroll
         for (int i = 0; i < NT / 32; i += 2) {
             g0 = max(g0, order(left.mx[i * 32 + lane]));
-            g1 = max(g1, order(left.mx[i * 32 + 32 + lane]));
+            if (NT > 32) g1 = max(g1, order(left.mx[i * 32 + (NT > 32 ? 32 : 0) + lane]));
         }
         // sorted by a bitonic network, descending: position lane in g0, 32 + lane in g1
 #pragma unroll
@@ -731,6 +692,142 @@ template <typename T, int NT> struct Long {
     }
 };
 
+// ---------------------------------------------------------------------------
+// Many rows of moderate length: one warp each, straight from global memory,
+// VECS vectors a lane on their way while VECS are added.
+// ---------------------------------------------------------------------------
+constexpr int ROW_WARPS = 4;
+
+template <typename T>
+__global__ void __launch_bounds__(32 * ROW_WARPS) logprobs_warp_kernel(const LpArgs a) {
+    using P = Top<T, 32>;
+    __shared__ typename P::Scratch scratch[ROW_WARPS];
+    __shared__ typename P::Left lefts[ROW_WARPS];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int64_t r = (int64_t)blockIdx.x * ROW_WARPS + warp;
+    if (r >= a.rows) return;
+    const T *row = static_cast<const T *>(a.x) + r * a.ldx;
+    int64_t id = -1;
+    const float given = lane == 0 ? given_logit<T>(a, r, id) : 0.f;
+    const int batches = (int)((a.vocab + 32 * VECS * P::E - 1) / (32 * VECS * P::E));
+    const int seg_batches = (batches + SEGMENTS - 1) / SEGMENTS;
+    const typename P::Share q = {row, a.vocab, 0u, (uint32_t)((uintptr_t)row & 15), seg_batches * VECS,
+                                 (batches + seg_batches - 1) / seg_batches};
+    typename P::Left &left = lefts[warp];
+    Sums<T> sums;
+    sums.start();
+    float mx = -INF, seg_mx = -INF;
+    uint4 x[VECS];
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) x[u] = P::vec(q, u * 32 + lane);
+    int seg = 0, seg_left = seg_batches;
+    for (int b = 0; b < batches; ++b) {
+        uint32_t w[4 * VECS];
+#pragma unroll
+        for (int u = 0; u < VECS; ++u) {
+            w[4 * u] = x[u].x; w[4 * u + 1] = x[u].y; w[4 * u + 2] = x[u].z; w[4 * u + 3] = x[u].w;
+        }
+        if (b + 1 < batches) {
+#pragma unroll
+            for (int u = 0; u < VECS; ++u) x[u] = P::vec(q, ((b + 1) * VECS + u) * 32 + lane);
+        }
+        uint32_t m2 = w[0];
+#pragma unroll
+        for (int i = 1; i < 4 * VECS; ++i) m2 = Words<T>::max2(m2, w[i]);
+        const float top = Words<T>::largest(m2);
+        sums.add(w, top);
+        seg_mx = fmaxf(seg_mx, top);
+        if (--seg_left == 0 || b + 1 == batches) {
+            left.seg[seg++][lane] = from_f32<T>(seg_mx);   // exact: a value of this type
+            mx = fmaxf(mx, seg_mx);
+            seg_mx = -INF;
+            seg_left = seg_batches;
+        }
+    }
+    left.mx[lane] = mx;
+    const RowResult res = row_result(warp_merge(sums.stat()));
+    if (lane == 0) write_row(a, r, res, id, given);
+    if (a.top_k > 0) {
+        __syncwarp();
+        P::top(scratch[warp], left, q, a.top_k);
+        if (lane < a.top_k) write_top(a, r, lane, scratch[warp].best[lane], res);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Long rows.  A row, or a share of it, streams through shared memory in chunks
+// of 64 bytes a thread.  A producer warp has the bulk engine copy STAGES chunks
+// ahead, the consumer warps take each chunk at their own pace and go on with
+// the next row, and finisher warps, in turn, make a row's results of what they
+// leave of it meanwhile.
+// ---------------------------------------------------------------------------
+
+// NT consumer threads, a producer warp and FIN finisher warps
+template <typename T, int NT> struct Long : Top<T, NT> {
+    using P = Top<T, NT>;
+    using P::E;
+    using P::W2;
+    static constexpr int CHUNK = NT * VECS * 16;           // bytes
+    static constexpr int CE = CHUNK / (int)sizeof(T);      // values
+    static constexpr int STAGE = CHUNK + 128;              // a row may start anywhere in its first 16 bytes
+    static constexpr int FIN = NT == 256 ? 2 : 4;
+    static constexpr int THREADS = NT + 32 + 32 * FIN;
+    static constexpr int CTAS = NT == 256 ? 2 : 3;         // on an SM
+    static constexpr int STAGES = 3;
+    struct Left : P::Left {
+        Stat part[NT / 32];
+    };
+    struct Shared {
+        uint64_t full[STAGES], empty[STAGES];
+        uint64_t left_full[FIN], left_free[FIN];
+        typename P::Scratch scratch[FIN];
+        Left left[FIN];
+        Stat total;
+    };
+    static constexpr size_t SMEM = (size_t)STAGES * STAGE + sizeof(Shared) + 16;
+    static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory of an SM");
+
+    // The 4 words of 16-byte vector v of a chunk whose first value lies WS words and `bits` bits into the stage
+    // (WS = -1: at its start).  Which values a thread takes does not depend on where the row starts, so neither do
+    // the sums.
+    template <int WS> static __device__ __forceinline__ void load(const uint8_t *stage, int v, uint32_t bits, uint32_t *w) {
+        const uint4 p = *reinterpret_cast<const uint4 *>(stage + v * 16);
+        if constexpr (WS < 0) {
+            w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w;
+        } else {
+            const uint4 n = *reinterpret_cast<const uint4 *>(stage + v * 16 + 16);
+            const uint32_t s[8] = {p.x, p.y, p.z, p.w, n.x, n.y, n.z, n.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
+        }
+    }
+    // adds a chunk's first n_valid values to the thread's sums, releases the stage as soon as it is read; the
+    // thread's largest
+    template <int WS>
+    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t bits, int n_valid, uint64_t *empty,
+                                                  Sums<T> &sums) {
+        uint32_t w[4 * VECS];
+#pragma unroll
+        for (int b = 0; b < VECS; ++b) load<WS>(stage, b * NT + (int)threadIdx.x, bits, w + 4 * b);
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) tc::mbar_arrive(tc::smem_u32(empty));
+        if (n_valid < CE) {
+#pragma unroll
+            for (int b = 0; b < 4 * VECS; ++b)
+                w[b] = Words<T>::mask(w[b], n_valid - (b / 4 * NT + (int)threadIdx.x) * E - b % 4 * W2);
+        }
+        uint32_t m2 = w[0];
+#pragma unroll
+        for (int b = 1; b < 4 * VECS; ++b) m2 = Words<T>::max2(m2, w[b]);
+        const float top = Words<T>::largest(m2);
+        sums.add(w, top);
+        return top;
+    }
+
+};
+
 template <typename T, int NT>
 __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logprobs_long_kernel(const LpArgs a, int splits) {
     using L = Long<T, NT>;
@@ -796,7 +893,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
             if (k > 0) {
                 const int64_t v0 = (int64_t)ch0 * L::CE;
                 const typename L::Share q = {row + v0, min((int64_t)ch1 * L::CE, a.vocab) - v0, (uint32_t)v0,
-                                             ((uintptr_t)row & 15) == 0, seg_chunks * VECS,
+                                             (uint32_t)((uintptr_t)(row + v0) & 15), seg_chunks * VECS,
                                              (ch1 - ch0 + seg_chunks - 1) / seg_chunks};
                 L::top(scratch, left, q, k);
             }
@@ -1007,7 +1104,11 @@ template <typename T> cudaError_t launch_logprobs(const LpArgs &a, cudaStream_t 
         return pdl_launch(logprobs_short_kernel<T>, dim3((unsigned)((a.rows + SHORT_WARPS - 1) / SHORT_WARPS)),
                           dim3(32 * SHORT_WARPS), 0, st, a, vec);
     }
-    return a.vocab * (int64_t)sizeof(T) <= 32768 ? launch_long<T, 64>(a, st) : launch_long<T, 256>(a, st);
+    const int64_t row_bytes = a.vocab * (int64_t)sizeof(T);
+    if (row_bytes <= 32768 && a.rows >= 8 * (int64_t)sm_count())
+        return pdl_launch(logprobs_warp_kernel<T>, dim3((unsigned)((a.rows + ROW_WARPS - 1) / ROW_WARPS)),
+                          dim3(32 * ROW_WARPS), 0, st, a);
+    return row_bytes < 98304 ? launch_long<T, 128>(a, st) : launch_long<T, 256>(a, st);
 }
 
 }  // namespace

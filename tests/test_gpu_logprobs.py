@@ -102,6 +102,32 @@ def test_masks_infinities_and_empty_rows(dtype, vocab):
     check_forward(torch.from_numpy(x).to(getattr(torch, dtype)).cuda(), ids, 6)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab,k", [(1025, 5), (2047, 32), (4096, 8), (8001, 20)])
+def test_many_rows(dtype, vocab, k):
+    """More rows than the GPU has warps for at first, of moderate length: as
+    few rows do, with odd starts, masks, ties, poisoned and empty rows."""
+    torch = torch_()
+    rng = np.random.default_rng(vocab)
+    rows = 1300
+    low = float(torch.finfo(getattr(torch, dtype)).min)
+    x = rng.standard_normal((rows, vocab + 3)) * rng.uniform(0.3, 6, (rows, 1))
+    x[0] = -math.inf
+    x[1] = 1.5
+    x[2] = low
+    x[3, ::3] = math.nan
+    x[4, 700] = math.inf
+    x[5] = rng.integers(0, 3, vocab + 3)
+    x[6] = np.sort(x[6])
+    x[7] = np.sort(x[7])[::-1]
+    x[8, rng.random(vocab + 3) < 0.99] = -math.inf
+    x[9] = -math.inf; x[9, 100:140] = 1.0
+    ids = rng.integers(-1, vocab, rows)
+    xt = torch.from_numpy(x).to(getattr(torch, dtype)).cuda()
+    check_forward(xt[:, 1:vocab + 1], ids, k)
+    check_forward(xt[:, :vocab].contiguous(), ids, k)
+
+
 def test_few_values_many_ties():
     """Logits of three values: every choice among the top is a tie."""
     torch = torch_()
