@@ -167,10 +167,17 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
-// (2^u, 2^u u) with u kept above -inf
-__device__ __noinline__ float2 one_term(float x, float m) {
-    const float u = fmaxf((x - m) * LOG2E, -1e30f), e = x != x ? x : ex2(u);
-    return make_float2(e, e * u);
+// sums of (2^u, 2^u u) over 4 words, with u kept above -inf
+template <typename T> __device__ __noinline__ float2 slow_terms(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, float m) {
+    float2 r = make_float2(0.f, 0.f);
+    for (int i = 0; i < 4; ++i)
+        for (int h = 0; h < 4 / (int)sizeof(T); ++h) {
+            const float x = Words<T>::value(i == 0 ? w0 : i == 1 ? w1 : i == 2 ? w2 : w3, h);
+            const float u = fmaxf((x - m) * LOG2E, -1e30f), e = x != x ? x : ex2(u);
+            r.x += e;
+            r.y += e * u;
+        }
+    return r;
 }
 
 // Sums of one thread, relative to one of its logits, m; one more than 8 above it
@@ -215,13 +222,11 @@ template <typename T> struct Sums {
         if (top > lim) raise(top);
         if (!moderate(m)) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int e = 0; e < 4 / (int)sizeof(T); ++e) {
-                    const float2 q = one_term(Words<T>::value(w[i], e), m);
-                    z = add2(z, pair(q.x, 0.f));
-                    t = add2(t, pair(q.y, 0.f));
-                }
+            for (int i = 0; i < N; i += 4) {
+                const float2 q = slow_terms<T>(w[i], w[i + 1], w[i + 2], w[i + 3], m);
+                z = add2(z, pair(q.x, 0.f));
+                t = add2(t, pair(q.y, 0.f));
+            }
             return;
         }
         const uint64_t minus_c = pair(-c, -c), log2e = pair(LOG2E, LOG2E);
@@ -631,7 +636,7 @@ template <typename T, int NT> struct Top {
             }
         }
         const uint32_t thr = __shfl_sync(~0u, g0, k - 1);  // k <= 32
-        const int n = thr == 0 ? collect(sh, left, q, 1u) : collect(sh, left, q, thr);
+        const int n = collect(sh, left, q, max(thr, 1u));
         if (n <= CAP) select(sh, n, k);
         else top_ties(sh, q, left, k, thr);
     }
@@ -803,14 +808,21 @@ template <typename T, int NT> struct Long : Top<T, NT> {
             for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
         }
     }
-    // adds a chunk's first n_valid values to the thread's sums, releases the stage as soon as it is read; the
-    // thread's largest
-    template <int WS>
-    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t bits, int n_valid, uint64_t *empty,
-                                                  Sums<T> &sums) {
-        uint32_t w[4 * VECS];
+    template <int WS> static __device__ __forceinline__ void load_all(const uint8_t *stage, uint32_t bits, uint32_t *w) {
 #pragma unroll
         for (int b = 0; b < VECS; ++b) load<WS>(stage, b * NT + (int)threadIdx.x, bits, w + 4 * b);
+    }
+    // adds a chunk's first n_valid values to the thread's sums, releases the stage as soon as it is read; the
+    // thread's largest
+    static __device__ __forceinline__ float chunk(const uint8_t *stage, uint32_t shift, int n_valid, uint64_t *empty,
+                                                  Sums<T> &sums) {
+        uint32_t w[4 * VECS];
+        const uint32_t bits = (shift & 3u) * 8u;
+        if (shift == 0) load_all<-1>(stage, 0, w);
+        else if (shift < 4) load_all<0>(stage, bits, w);
+        else if (shift < 8) load_all<1>(stage, bits, w);
+        else if (shift < 12) load_all<2>(stage, bits, w);
+        else load_all<3>(stage, bits, w);
         __syncwarp();
         if (threadIdx.x % 32 == 0) tc::mbar_arrive(tc::smem_u32(empty));
         if (n_valid < CE) {
@@ -825,7 +837,6 @@ template <typename T, int NT> struct Long : Top<T, NT> {
         sums.add(w, top);
         return top;
     }
-
 };
 
 template <typename T, int NT>
@@ -923,15 +934,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
                 const uint8_t *stage = smem + s * L::STAGE;
                 const int n_valid = (int)min((int64_t)L::CE, a.vocab - (int64_t)ch * L::CE);
                 tc::mbar_wait(tc::smem_u32(&sh.full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_LOGPROBS);
-                const uint32_t bits = (shift & 3u) * 8u;
-                float top;
-                switch (shift == 0 ? -1 : (int)(shift >> 2)) {
-                    case -1: top = L::template chunk<-1>(stage, 0, n_valid, &sh.empty[s], sums); break;
-                    case 0: top = L::template chunk<0>(stage, bits, n_valid, &sh.empty[s], sums); break;
-                    case 1: top = L::template chunk<1>(stage, bits, n_valid, &sh.empty[s], sums); break;
-                    case 2: top = L::template chunk<2>(stage, bits, n_valid, &sh.empty[s], sums); break;
-                    default: top = L::template chunk<3>(stage, bits, n_valid, &sh.empty[s], sums); break;
-                }
+                const float top = L::chunk(stage, shift, n_valid, &sh.empty[s], sums);
                 seg_mx = fmaxf(seg_mx, top);
                 if (--seg_left == 0 || ch + 1 == ch1) {
                     if (seg == 0)                          // the row FIN before is finished
