@@ -64,17 +64,23 @@ struct MmArgs {
     int splits;                         // CTAs of a cluster that share a tile's K blocks
     int group;                          // wide: row tiles walked together
     int vec;                            // wide: TMA can address y's rows
+    int early;                          // narrow: the kernel before does not write w
     uint32_t *err;
 };
 
-template <int BN> struct Shape {
+template <int BN> struct Narrow {
     static constexpr int C_BYTES = BN * BK;
     static constexpr int STAGE = L_BYTES + C_BYTES;
     // two CTAs share an SM where the tiles are narrow
     static constexpr int STAGES = BN <= 32 ? 5 : BN == 64 ? 4 : 6;
     static constexpr int NBUF = BN <= 64 ? 4 : 2;
-    static constexpr int TMEM_COLS = NBUF * BN < 32 ? 32 : NBUF * BN;
-    static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
+    static constexpr int TMEM_COLS = NBUF * BN;
+    // up to 64 columns: the two halves of the epilogue warps take K blocks in
+    // turn, all columns each (what a block costs them is latency); 128
+    // columns: every block, half the columns each
+    static constexpr int GROUPS = BN <= 64 ? 2 : 1;
+    static constexpr int CPW = BN / (2 / GROUPS);          // columns of an epilogue warp
+    static constexpr int LDN = CPW < 32 ? CPW : 32;        // columns of one TMEM load
     static constexpr int FAC = N_EPI * 2 * CPW * 4;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16;
 };
@@ -129,40 +135,57 @@ __device__ __forceinline__ float finish(const MmArgs &a, float v, int n) {
     return a.relu ? relu_keep_nan(v) : v;
 }
 
+// acc += f * p on two values at once.  Volatile, like the TMEM load and the
+// wait before it: volatile asm keeps its order, so no value is read before
+// its load is complete.
+__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t f, uint32_t p0, uint32_t p1) {
+    asm volatile("{\n\t.reg .b64 p;\n\tmov.b64 p, {%2, %3};\n\tfma.rn.f32x2 %0, %1, p, %0;\n\t}"
+                 : "+l"(acc)
+                 : "l"(f), "r"(p0), "r"(p1));
+}
+__device__ __forceinline__ uint64_t dup2(float f) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(f));
+    return r;
+}
+__device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+
 // ---------------------------------------------------------------------------
 // narrow: few rows
 // ---------------------------------------------------------------------------
 template <int BN>
 __global__ void __launch_bounds__(THREADS, 1)
 fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap, const MmArgs a) {
-    using S = Shape<BN>;
-    constexpr int CPW = S::CPW;
-    constexpr int LDN = CPW < 32 ? CPW : 32;               // columns of one TMEM load
+    using S = Narrow<BN>;
+    constexpr int CPW = S::CPW, LDN = S::LDN, STAGES = S::STAGES, NBUF = S::NBUF, GROUPS = S::GROUPS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *Ls = smem;
-    uint8_t *Cs = Ls + S::STAGES * L_BYTES;
-    float *fac = (float *)(Cs + S::STAGES * S::C_BYTES);
+    uint8_t *Cs = Ls + STAGES * L_BYTES;
+    float *fac = (float *)(Cs + STAGES * S::C_BYTES);
     uint64_t *full = (uint64_t *)((uint8_t *)fac + S::FAC);
-    uint64_t *empty = full + S::STAGES;
-    uint64_t *acc_full = empty + S::STAGES;
-    uint64_t *acc_empty = acc_full + S::NBUF;
-    uint32_t *tmem_holder = (uint32_t *)(acc_empty + S::NBUF);
+    uint64_t *empty = full + STAGES;
+    uint64_t *acc_full = empty + STAGES;
+    uint64_t *acc_empty = acc_full + NBUF;
+    uint32_t *tmem_holder = (uint32_t *)(acc_empty + NBUF);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)a.splits);
     const int tile = (int)(blockIdx.x / (unsigned)a.splits);
     const int tl = tile % a.tiles_l, tc = tile / a.tiles_l;
     const int kb0 = (int)((int64_t)a.KB * rank / a.splits), kb1 = (int)((int64_t)a.KB * (rank + 1) / a.splits);
+    const int nkb = kb1 - kb0;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::STAGES; ++s) {
+        for (int s = 0; s < STAGES; ++s) {
             mbar_init(smem_u32(&full[s]), 1);
             mbar_init(smem_u32(&empty[s]), 1);
         }
-        for (int b = 0; b < S::NBUF; ++b) {
+        for (int b = 0; b < NBUF; ++b) {
             mbar_init(smem_u32(&acc_full[b]), 1);
-            mbar_init(smem_u32(&acc_empty[b]), N_EPI);
+            mbar_init(smem_u32(&acc_empty[b]), N_EPI / GROUPS);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -175,42 +198,50 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *tmem_holder;
-    pdl_wait();
     pdl_trigger();
 
     if (warp == TMA_WARP) {
-        int it = 0;
+        const auto load_l = [&](int i) {
+            const int s = i % STAGES;
+            mbar_arrive_expect_tx(smem_u32(&full[s]), (uint32_t)S::STAGE);
+            tma_load_2d(smem_u32(Ls + s * L_BYTES), &lmap, smem_u32(&full[s]), (kb0 + i) * BK, tl * BL);
+        };
+        const auto load_c = [&](int i) {
+            const int s = i % STAGES;
+            tma_load_2d(smem_u32(Cs + s * S::C_BYTES), &cmap, smem_u32(&full[s]), (kb0 + i) * BK, tc * BN);
+        };
+        // the weights of the first stages may be on their way while the kernel before still quantises x
+        const int ahead = a.early ? min(STAGES, nkb) : 0;
+        if (elect_one())
+            for (int i = 0; i < ahead; ++i) load_l(i);
+        __syncwarp();
+        pdl_wait();
+        if (elect_one())
+            for (int i = 0; i < ahead; ++i) load_c(i);
+        __syncwarp();
         bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-            const int s = it % S::STAGES;
-            if (!warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA)) {
-                ok = false;
-                break;
-            }
+        int it = ahead;
+        for (; it < nkb; ++it) {
+            ok = warp_wait(smem_u32(&empty[it % STAGES]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_TMA);
+            if (!ok) break;
             if (elect_one()) {
-                const uint32_t fb = smem_u32(&full[s]);
-                mbar_arrive_expect_tx(fb, (uint32_t)S::STAGE);
-                tma_load_2d(smem_u32(Ls + s * L_BYTES), &lmap, fb, kb * BK, tl * BL);
-                tma_load_2d(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, kb * BK, tc * BN);
+                load_l(it);
+                load_c(it);
             }
             __syncwarp();
         }
         if (!ok) {
             // copies still in flight land before the CTA ends
-            for (int j = max(0, it - S::STAGES); j < it; ++j)
-                warp_wait(smem_u32(&full[j % S::STAGES]), (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
+            for (int j = max(0, it - STAGES); j < it; ++j)
+                warp_wait(smem_u32(&full[j % STAGES]), (uint32_t)(j / STAGES) & 1u, a.err, E_DRAIN);
         }
     } else if (warp == MMA_WARP) {
         constexpr uint32_t idesc = idesc_e4m3(BL, BN);
-        int it = 0;
-        bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-            const int s = it % S::STAGES, b = it % S::NBUF;
-            if (!warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / S::NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
-                !warp_wait(smem_u32(&full[s]), (uint32_t)(it / S::STAGES) & 1u, a.err, E_MMA)) {
-                ok = false;
+        for (int it = 0; it < nkb; ++it) {
+            const int s = it % STAGES, b = it % NBUF;
+            if (!warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
+                !warp_wait(smem_u32(&full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_MMA))
                 break;
-            }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (elect_one()) {
                 const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
@@ -218,25 +249,27 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
 #pragma unroll
                 for (int k = 0; k < BK / 32; ++k)
                     umma_e4m3(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
-                umma_commit(smem_u32(&empty[s]));
                 umma_commit(smem_u32(&acc_full[b]));
+                umma_commit(smem_u32(&empty[s]));
             }
             __syncwarp();
         }
     } else {
+        pdl_wait();
         const int quad = warp & 3, half = warp >> 2;
         const int row = quad * 32 + lane;                  // lane row of this thread within the tile
-        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
-        const int l = tl * BL + row;                       // its row of w
-        const int c0 = tc * BN + half * CPW;               // first row of x of this warp
-        float acc[CPW];
+        const int cw = GROUPS == 1 ? half * CPW : 0;       // first of this warp's columns in the tile
+        const int c0 = tc * BN + cw;                       // ... its row of x
+        const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)cw;
+        uint64_t acc[CPW / 2];
 #pragma unroll
-        for (int i = 0; i < CPW; ++i) acc[i] = 0.f;
+        for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
 
-        // scales of the next block, fetched one block ahead: lane j holds
-        // column j's and the warp shares the products through shared memory
+        // scales of this warp's next block, fetched ahead: lane j holds
+        // column j's; the warp shares the products through shared memory
         constexpr int NF = (CPW + 31) / 32;
-        float nx[NF], nw;
+        const int first = GROUPS == 1 ? 0 : half;
+        float nx[NF], nw = 0.f;
         const float *xp[NF];
         bool xin[NF];
 #pragma unroll
@@ -244,26 +277,27 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
             const int m = c0 + j * 32 + lane;
             xin[j] = j * 32 + lane < CPW && m < a.M;
             xp[j] = a.xs + (int64_t)(xin[j] ? m : 0) * a.xs_row;
+            nx[j] = 0.f;
         }
         const float *wp = a.ws + (int64_t)tl * a.ws_row;
-        const auto fetch = [&](int kb) {
+        const auto fetch = [&](int i) {
+            const int64_t kb = kb0 + i;
 #pragma unroll
             for (int j = 0; j < NF; ++j) nx[j] = xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
             nw = __ldg(wp + kb * a.ws_blk);
         };
-        if (kb0 < kb1) fetch(kb0);
+        if (first < nkb) fetch(first);
 
-        int it = 0;
         bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
-            const int b = it % S::NBUF;
-            float *fs = fac + (warp * 2 + (it & 1)) * CPW;
+        for (int it = first; it < nkb; it += GROUPS) {
+            const int b = it % NBUF;
+            float *fs = fac + (warp * 2 + (it / GROUPS & 1)) * CPW;
 #pragma unroll
             for (int j = 0; j < NF; ++j)
                 if (j * 32 + lane < CPW) fs[j * 32 + lane] = nx[j] * nw;
             __syncwarp();
-            if (kb + 1 < kb1) fetch(kb + 1);
-            ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / S::NBUF) & 1u, a.err, E_EPI);
+            if (it + GROUPS < nkb) fetch(it + GROUPS);
+            ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -272,43 +306,58 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
                 tmem_ld_nw<LDN>(tbase + (uint32_t)(b * BN + c), r);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < LDN; ++i) acc[c + i] = fmaf(fs[c + i], tmem_done(r[i]), acc[c + i]);
+                for (int i = 0; i < LDN; i += 4) {
+                    const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(fs + c + i);
+                    fma2(acc[(c + i) / 2], f.x, r[i], r[i + 1]);
+                    fma2(acc[(c + i) / 2 + 1], f.y, r[i + 2], r[i + 3]);
+                }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
         }
-        if (!ok) {
-            // reported; the output is invalid
-        } else if (a.splits > 1) {
-            // partial sums [column][lane row], over the stages: every copy has
-            // landed and every MMA has read it (the last block is complete)
-            float *part = (float *)smem;
+        // Partial sums [column][lane row], over the stages: once both halves
+        // are here every copy has landed and every MMA has read it.  (After a
+        // wait that ran out, which is reported, the output is invalid.)
+        float *part = (float *)smem;
+        const auto put = [&](bool add) {
 #pragma unroll
-            for (int i = 0; i < CPW; ++i) part[(half * CPW + i) * BL + row] = acc[i];
-        } else if (l < a.N) {
-#pragma unroll
-            for (int i = 0; i < CPW; ++i)
-                if (c0 + i < a.M) store_out(a, (int64_t)(c0 + i) * a.ldy + l, finish(a, acc[i], l));
+            for (int i = 0; i < CPW / 2; ++i) {
+                float u, v;
+                split2(acc[i], u, v);
+                float *p = part + (cw + 2 * i) * BL + row;
+                p[0] = add ? p[0] + u : u;
+                p[BL] = add ? p[BL] + v : v;
+            }
+        };
+        asm volatile("bar.sync 1, %0;" ::"n"(N_EPI * 32) : "memory");
+        if (GROUPS == 1 || half == 1) put(false);
+        if (GROUPS == 2) {
+            asm volatile("bar.sync 1, %0;" ::"n"(N_EPI * 32) : "memory");
+            if (half == 0) put(true);
         }
     }
     __syncwarp();
-    if (a.splits > 1) {
-        cluster_sync();
-        if (warp < N_EPI) {
-            // this CTA finishes its share of the tile's columns
-            const int row = (int)threadIdx.x & (BL - 1), l = tl * BL + row;
-            const int cols = min(BN, a.M - tc * BN);
-            for (int c = rank * 2 + ((int)threadIdx.x >> 7); c < cols; c += 2 * a.splits) {
-                float v = 0.f;
-                const uint32_t at = smem_u32((float *)smem + c * BL + row);
+    if (a.splits > 1) cluster_sync();
+    else __syncthreads();
+    if (warp < N_EPI) {
+        // this CTA finishes its share of the tile's columns
+        const int row = (int)threadIdx.x & (BL - 1), l = tl * BL + row;
+        const int cols = min(BN, a.M - tc * BN);
+        for (int c = rank * 2 + ((int)threadIdx.x >> 7); c < cols; c += 2 * a.splits) {
+            const float *p = (const float *)smem + c * BL + row;
+            float v = 0.f;
+            if (a.splits > 1) {
+                const uint32_t at = smem_u32(p);
 #pragma unroll 4
                 for (int s = 0; s < a.splits; ++s) v += ld_cluster_f32(mapa_shared(at, (uint32_t)s));
-                if (l < a.N) store_out(a, (int64_t)(tc * BN + c) * a.ldy + l, finish(a, v, l));
+            } else {
+                v = *p;
             }
+            if (l < a.N) store_out(a, (int64_t)(tc * BN + c) * a.ldy + l, finish(a, v, l));
         }
-        cluster_sync();
     }
+    if (a.splits > 1) cluster_sync();                      // no CTA leaves while its sums may still be read
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == MMA_WARP) {
@@ -349,23 +398,6 @@ __device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t a, uint
 // release would wait for the scale loads and output stores in flight.
 __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar_cluster) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
-}
-
-// acc += f * p on two values at once.  Volatile, like the TMEM load and the
-// wait before it: volatile asm keeps its order, so no value is read before
-// its load is complete.
-__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t f, uint32_t p0, uint32_t p1) {
-    asm volatile("{\n\t.reg .b64 p;\n\tmov.b64 p, {%2, %3};\n\tfma.rn.f32x2 %0, %1, p, %0;\n\t}"
-                 : "+l"(acc)
-                 : "l"(f), "r"(p0), "r"(p1));
-}
-__device__ __forceinline__ uint64_t dup2(float f) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(f));
-    return r;
-}
-__device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
 }
 
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y) {
@@ -688,11 +720,11 @@ bool encode8(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t k, int64_
 template <int BN>
 cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, const MmArgs &a, int grid, cudaStream_t st) {
     static std::atomic<bool> sized[MAX_DEVICES];
-    const cudaError_t e = allow_smem(fp8_narrow_kernel<BN>, sized, Shape<BN>::SMEM);
+    const cudaError_t e = allow_smem(fp8_narrow_kernel<BN>, sized, Narrow<BN>::SMEM);
     if (e != cudaSuccess) return e;
     if (a.splits == 1)
-        return pdl_launch(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Shape<BN>::SMEM, st, lmap, cmap, a);
-    return pdl_launch_cluster(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Shape<BN>::SMEM, st, a.splits,
+        return pdl_launch(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Narrow<BN>::SMEM, st, lmap, cmap, a);
+    return pdl_launch_cluster(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Narrow<BN>::SMEM, st, a.splits,
                               lmap, cmap, a);
 }
 
@@ -848,5 +880,8 @@ extern "C" ct_status ct_fp8_linear(const void *x_dev, int32_t x_dtype, int64_t l
     const ct_status r = quantize(x_dev, x_dtype, m, k, ldx, 1, q, q_pitch(k), xs, 1, m, static_cast<cudaStream_t>(stream));
     if (r != CT_OK) return r;
     a.xs = xs; a.xs_row = 1; a.xs_blk = m;
+    // the quantisation lets this kernel start only after all work before itself
+    // is complete, and does not write w
+    a.early = 1;
     return matmul(a, Operands{q, q_pitch(k), w_dev, ldw, k}, static_cast<cudaStream_t>(stream));
 }
