@@ -11,8 +11,10 @@
 // epilogue warps add factor * P_b to FP32 registers while the next block's
 // MMAs run into another accumulator.
 //
-// Warp roles: 8 epilogue warps (warp w reads TMEM lanes 32 (w % 4) .. and the
-// column half w / 4), one TMA warp, one MMA warp.  A stage of shared memory
+// Warp roles: 8 epilogue warps (warp w reads TMEM lanes 32 (w % 4) ..), one TMA
+// warp, two MMA warps that take K blocks in turn (testing two barriers and
+// issuing four MMAs and two commits takes one thread 600 cycles, as long as
+// the MMAs of a 256 x 256 tile).  A stage of shared memory
 // holds one K block of both operands: 128-byte rows, 128-byte swizzle; rows
 // and columns past the ends are the zeros TMA fills in.
 //
@@ -44,8 +46,8 @@ constexpr int BL = 128;                 // lane side of a tile
 constexpr int BK = 128;                 // K block: one scale, one 128-byte row
 constexpr int L_BYTES = BL * BK;
 constexpr int N_EPI = 8;
-constexpr int TMA_WARP = 8, MMA_WARP = 9;
-constexpr int THREADS = 320;
+constexpr int TMA_WARP = 8, MMA_WARP = 9, N_MMA = 2;
+constexpr int THREADS = 32 * (MMA_WARP + N_MMA);
 
 // error codes of the bounded waits
 constexpr uint32_t E_TMA = 0x100, E_MMA = 0x200, E_ACC = 0x400, E_EPI = 0x800, E_DRAIN = 0x1000;
@@ -72,7 +74,7 @@ template <int BN> struct Narrow {
     static constexpr int C_BYTES = BN * BK;
     static constexpr int STAGE = L_BYTES + C_BYTES;
     // two CTAs share an SM where the tiles are narrow
-    static constexpr int STAGES = BN <= 32 ? 5 : BN == 64 ? 4 : 6;
+    static constexpr int STAGES = BN == 16 ? 6 : BN <= 64 ? 4 : 6;
     static constexpr int NBUF = BN <= 64 ? 4 : 2;
     static constexpr int TMEM_COLS = NBUF * BN;
     // up to 64 columns: the two halves of the epilogue warps take K blocks in
@@ -83,6 +85,9 @@ template <int BN> struct Narrow {
     static constexpr int LDN = CPW < 32 ? CPW : 32;        // columns of one TMEM load
     static constexpr int FAC = N_EPI * 2 * CPW * 4;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16;
+    // each stage and each accumulator is one MMA warp's: a barrier's phases are
+    // told apart by parity, so no warp may be a phase ahead of another's wait
+    static_assert(STAGES % N_MMA == 0 && NBUF % N_MMA == 0, "stages and accumulators of one MMA warp");
 };
 
 template <int N> __device__ __forceinline__ void tmem_ld_nw(uint32_t taddr, uint32_t (&r)[N]) {
@@ -212,38 +217,33 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
         };
         // the weights of the first stages may be on their way while the kernel before still quantises x
         const int ahead = a.early ? min(STAGES, nkb) : 0;
-        if (elect_one())
+        if (elect_one()) {
             for (int i = 0; i < ahead; ++i) load_l(i);
-        __syncwarp();
-        pdl_wait();
-        if (elect_one())
+            pdl_wait();
             for (int i = 0; i < ahead; ++i) load_c(i);
-        __syncwarp();
-        bool ok = true;
-        int it = ahead;
-        for (; it < nkb; ++it) {
-            ok = warp_wait(smem_u32(&empty[it % STAGES]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_TMA);
-            if (!ok) break;
-            if (elect_one()) {
+            int it = ahead;
+            for (; it < nkb; ++it) {
+                if (!mbar_wait(smem_u32(&empty[it % STAGES]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_TMA)) break;
                 load_l(it);
                 load_c(it);
             }
-            __syncwarp();
-        }
-        if (!ok) {
-            // copies still in flight land before the CTA ends
+            // No copy and no commit is under way when the CTA ends: the last
+            // use of each stage has been released (or, after a wait that ran
+            // out, its copies have landed).
             for (int j = max(0, it - STAGES); j < it; ++j)
-                warp_wait(smem_u32(&full[j % STAGES]), (uint32_t)(j / STAGES) & 1u, a.err, E_DRAIN);
+                mbar_wait(smem_u32(it < nkb ? &full[j % STAGES] : &empty[j % STAGES]), (uint32_t)(j / STAGES) & 1u, a.err,
+                          E_DRAIN);
         }
-    } else if (warp == MMA_WARP) {
+        __syncwarp();
+    } else if (warp >= MMA_WARP) {
         constexpr uint32_t idesc = idesc_e4m3(BL, BN);
-        for (int it = 0; it < nkb; ++it) {
-            const int s = it % STAGES, b = it % NBUF;
-            if (!warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
-                !warp_wait(smem_u32(&full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_MMA))
-                break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if (elect_one()) {
+        if (elect_one()) {
+            for (int it = warp - MMA_WARP; it < nkb; it += N_MMA) {
+                const int s = it % STAGES, b = it % NBUF;
+                if (!mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
+                    !mbar_wait(smem_u32(&full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_MMA))
+                    break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
                 const uint64_t cd = smem_desc_sw128(smem_u32(Cs + s * S::C_BYTES));
 #pragma unroll
@@ -252,8 +252,8 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
                 umma_commit(smem_u32(&acc_full[b]));
                 umma_commit(smem_u32(&empty[s]));
             }
-            __syncwarp();
         }
+        __syncwarp();
     } else {
         pdl_wait();
         const int quad = warp & 3, half = warp >> 2;
@@ -369,20 +369,22 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
 // ---------------------------------------------------------------------------
 // wide: CTA pairs
 // ---------------------------------------------------------------------------
-constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9 MMA, 10-11 idle
+constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9-10 MMA, 11 idle
 // registers a thread after the split: 2 x 232 + 40 for three warpgroups that
 // were launched with 168 each (3 x 168 = 504)
 constexpr int W_REGS_EPI = 232, W_REGS_REST = 40;
-constexpr int W_BOX_BYTES = 32 * 128;                      // epilogue: 32 rows of 128 bytes, two for each warp
+constexpr int W_BOX_BYTES = 32 * 128;
 constexpr int W_CHUNK = 16;                                // columns of one step of the unaligned store
 
 template <int BN> struct Wide {
     static constexpr int C_BYTES = BN / 2 * BK;            // this CTA's half of the column operand
-    static constexpr int STAGES = BN == 256 ? 5 : BN == 128 ? 6 : 7;
+    static constexpr int STAGES = BN == 64 ? 8 : 6;
+    static constexpr int BOXES = BN == 256 ? 1 : 2;        // epilogue: 32 rows of 128 bytes on their way to y, for each warp
     static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
     static constexpr int LDN = BN == 64 ? 16 : 32;         // columns of one TMEM load: an even number of loads
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * 2 * W_BOX_BYTES +
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES +
                                    8 * (2 * STAGES + 5) + 16;
+    static_assert(STAGES % N_MMA == 0, "a stage is one MMA warp's, see Narrow");
 };
 
 __device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
@@ -426,7 +428,7 @@ template <int SIZE> __device__ __forceinline__ uint4 out16(int out, const float 
 // by COLS columns, 128 bytes (64 where the warp's columns are fewer), swizzled
 // so that the 16-byte pieces of 8 rows hit 8 bank groups, stored by TMA, which clips what lies past the ends, while the next tile's
 // products are added.
-template <int CPW, int COLS, int SIZE>
+template <int CPW, int COLS, int SIZE, int BOXES>
 __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *ymap, const uint64_t *acc, uint8_t *boxes,
                                             uint32_t &stored, int m_warp, int c0, int lane) {
     constexpr int PER16 = 16 / SIZE;                       // values of 16 bytes
@@ -436,9 +438,9 @@ __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *
 #pragma unroll
     for (int c = 0; c < CPW; c += COLS) {
         if (c0 + c >= a.N) break;
-        uint8_t *box = boxes + (stored++ & 1u) * W_BOX_BYTES;
-        // the store before the last has been read from this box
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        uint8_t *box = boxes + stored++ % BOXES * W_BOX_BYTES;
+        // the store before from this box has been read
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(BOXES - 1) : "memory");
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
@@ -475,7 +477,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     uint8_t *Ls = smem;
     uint8_t *Cs = Ls + S::STAGES * L_BYTES;
     uint8_t *boxes = Cs + S::STAGES * S::C_BYTES;
-    uint64_t *full = (uint64_t *)(boxes + N_EPI * 2 * W_BOX_BYTES);   // even CTA's: both CTAs' copies of a stage
+    uint64_t *full = (uint64_t *)(boxes + N_EPI * S::BOXES * W_BOX_BYTES);   // even CTA's: both CTAs' copies of a stage
     uint64_t *empty = full + S::STAGES;                    // each CTA: the pair's MMAs have read the stage
     uint64_t *acc_full = empty + S::STAGES;                // each CTA: a block's products are in TMEM
     uint64_t *acc_empty = acc_full + 2;                    // even CTA's: both CTAs' epilogues have read them
@@ -498,7 +500,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             mbar_init(smem_u32(&acc_full[b]), 1);
             mbar_init(smem_u32(&acc_empty[b]), 2 * N_EPI);
         }
-        mbar_init(smem_u32(mma_done), 1);
+        mbar_init(smem_u32(mma_done), N_MMA);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -519,66 +521,62 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W_REGS_REST));
         if (warp == TMA_WARP) {
             const uint32_t full_even = mapa_shared(smem_u32(full), 0u);
-            int it = 0;
-            bool ok = true;
-            for (int t = cid; t < tiles && ok; t += ncl) {
-                int tl, tc;
-                tile_at(a, t, tl, tc);
-                const int m0 = (2 * tl + (int)crank) * BL, n0 = tc * BN + (int)crank * (BN / 2);
-                for (int kb = 0; kb < KB; ++kb, ++it) {
-                    const int s = it % S::STAGES;
-                    if (!warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA)) {
-                        ok = false;
-                        break;
-                    }
-                    if (elect_one()) {
+            if (elect_one()) {
+                int it = 0;
+                bool ok = true;
+                for (int t = cid; t < tiles && ok; t += ncl) {
+                    int tl, tc;
+                    tile_at(a, t, tl, tc);
+                    const int m0 = (2 * tl + (int)crank) * BL, n0 = tc * BN + (int)crank * (BN / 2);
+                    for (int kb = 0; kb < KB; ++kb, ++it) {
+                        const int s = it % S::STAGES;
+                        ok = mbar_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA);
+                        if (!ok) break;
                         const uint32_t fb = full_even + (uint32_t)(s * 8);
                         if (leader) mbar_arrive_expect_tx(smem_u32(&full[s]), 2u * (L_BYTES + S::C_BYTES));
                         tma_load_2d_pair(smem_u32(Ls + s * L_BYTES), &lmap, fb, kb * BK, m0);
                         tma_load_2d_pair(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, kb * BK, n0);
                     }
-                    __syncwarp();
                 }
+                // no copy and no commit is under way when the CTA ends, see the narrow kernel (the even CTA's
+                // barriers count both CTAs' copies)
+                if (ok || leader)
+                    for (int j = max(0, it - S::STAGES); j < it; ++j)
+                        mbar_wait(smem_u32(ok ? &empty[j % S::STAGES] : &full[j % S::STAGES]),
+                                  (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
             }
-            if (!ok && leader) {
-                // copies still in flight land before the CTAs end (the even CTA's barrier counts both CTAs')
-                for (int j = max(0, it - S::STAGES); j < it; ++j)
-                    warp_wait(smem_u32(&full[j % S::STAGES]), (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
-            }
-        } else if (warp == MMA_WARP && leader) {
+        } else if (warp < MMA_WARP + N_MMA && leader) {
             constexpr uint32_t idesc = idesc_e4m3(2 * BL, BN);
-            int it = 0;
-            bool ok = true;
-            for (int t = cid; t < tiles && ok; t += ncl) {
-                for (int kb = 0; kb < KB; ++kb, ++it) {
-                    const int s = it % S::STAGES, b = it & 1;
-                    if (!warp_wait(smem_u32(&full[s]), (uint32_t)(it / S::STAGES) & 1u, a.err, E_MMA) ||
-                        !warp_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it >> 1) & 1u) ^ 1u, a.err, E_ACC)) {
-                        ok = false;
+            if (elect_one()) {
+                // this pair's blocks, all tiles in a row
+                const int64_t all = (int64_t)((tiles - cid + ncl - 1) / ncl) * KB;
+                int s = warp - MMA_WARP, round = 0;        // stage, times it was used before
+                for (int64_t it = warp - MMA_WARP; it < all; it += N_MMA) {
+                    const int b = (int)(it & 1);
+                    if (!mbar_wait(smem_u32(&full[s]), (uint32_t)round & 1u, a.err, E_MMA) ||
+                        !mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it >> 1) & 1u) ^ 1u, a.err, E_ACC))
                         break;
-                    }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    if (elect_one()) {
-                        const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
-                        const uint64_t cd = smem_desc_sw128(smem_u32(Cs + s * S::C_BYTES));
+                    const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
+                    const uint64_t cd = smem_desc_sw128(smem_u32(Cs + s * S::C_BYTES));
 #pragma unroll
-                        for (int k = 0; k < BK / 32; ++k)
-                            umma_e4m3_pair(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
-                        umma_commit_pair_mc(smem_u32(&acc_full[b]), (uint16_t)3u);
-                        umma_commit_pair_mc(smem_u32(&empty[s]), (uint16_t)3u);
-                    }
-                    __syncwarp();
+                    for (int k = 0; k < BK / 32; ++k)
+                        umma_e4m3_pair(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
+                    umma_commit_pair_mc(smem_u32(&acc_full[b]), (uint16_t)3u);
+                    umma_commit_pair_mc(smem_u32(&empty[s]), (uint16_t)3u);
+                    s += N_MMA;
+                    if (s >= S::STAGES) { s -= S::STAGES; ++round; }
                 }
+                umma_commit_pair_mc(smem_u32(mma_done), (uint16_t)3u);
             }
-            if (elect_one()) umma_commit_pair_mc(smem_u32(mma_done), (uint16_t)3u);
-            __syncwarp();
         }
+        __syncwarp();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W_REGS_EPI));
         const int quad = warp & 3, half = warp >> 2;
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
         const uint32_t acc_empty_even = mapa_shared(smem_u32(acc_empty), 0u);
-        uint8_t *mine = boxes + warp * 2 * W_BOX_BYTES;
+        uint8_t *mine = boxes + warp * S::BOXES * W_BOX_BYTES;
         uint32_t stored = 0;                               // boxes this warp has stored
         int it = 0;
         bool ok = true;
@@ -634,8 +632,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             if (!ok) break;
 
             if (a.vec) {
-                if (a.out == CT_DT_F32) store_boxes<CPW, 32, 4>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
-                else store_boxes<CPW, CPW < 64 ? CPW : 64, 2>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+                if (a.out == CT_DT_F32) store_boxes<CPW, 32, 4, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+                else store_boxes<CPW, CPW < 64 ? CPW : 64, 2, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
             } else {
                 // rows that start anywhere: two rows of 16 columns a step
                 float *sq = (float *)mine;

@@ -117,6 +117,25 @@ def test_matmul_sizes(m, n, k):
                   bias.astype(np.float64), relu, kb)
 
 
+@pytest.mark.parametrize("m", [1, 20, 50, 100, 256, 300, 700])
+def test_matmul_long_k(m):
+    """K long enough that every stage of the pipeline is used many times, on
+    few tiles and on many, called back to back."""
+    torch = torch_()
+    rng = np.random.default_rng(m)
+    for n, k in [(130, 30000), (4400, 9000)]:
+        xq, xv = rand_fp8(rng, m, k)
+        wq, wv = rand_fp8(rng, n, k)
+        kb = (k + 127) // 128
+        xs = torch.rand(m, kb, device="cuda")
+        ws = torch.rand((n + 127) // 128, kb, device="cuda")
+        ys = [ct().ct_fp8_matmul(xq, xs, wq, ws) for _ in range(20)]
+        assert ct().ct_ops_device_error() == 0
+        check_product(ys[0], "float32", xv * _ops.widen(xs.double().cpu().numpy(), 1, m, k),
+                      wv * _ops.widen(ws.double().cpu().numpy(), 128, n, k), None, False, kb)
+        assert all(torch.equal(y, ys[0]) for y in ys)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 4096, 2048), (8, 520, 4096), (200, 1000, 1152), (300, 516, 640), (1300, 770, 400)])
 def test_matmul_exact_on_integers(m, n, k):
     """Small integers and power-of-two scales: every sum is exact, so all
