@@ -31,7 +31,10 @@
 //     launch, the same bits each time.
 #include <atomic>
 #include <cudaTypedefs.h>
+#include <math.h>
 #include <string.h>
+#include <stdio.h>
+#include <stdlib.h>
 
 #include "ops_common.cuh"
 #include "tc_common.cuh"
@@ -66,6 +69,7 @@ struct MmArgs {
     int splits;                         // CTAs of a cluster that share a tile's K blocks
     int group;                          // wide: row tiles walked together
     int vec;                            // wide: TMA can address y's rows
+    int vec4;                           // 4 values of a row of y, from a multiple of 4 on, are one aligned store
     int early;                          // narrow: the kernel before does not write w
     uint32_t *err;
 };
@@ -123,9 +127,12 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a, uint64_t 
         "l"(a), "l"(b), "r"(idesc), "r"(acc));
 }
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr)
+                 : "memory");
     return v;
 }
 
@@ -133,6 +140,26 @@ __device__ __forceinline__ void store_out(const MmArgs &a, int64_t at, float v) 
     if (a.out == CT_DT_F32) static_cast<float *>(a.y)[at] = v;
     else if (a.out == CT_DT_F16) static_cast<__half *>(a.y)[at] = __float2half_rn(v);
     else static_cast<__nv_bfloat16 *>(a.y)[at] = __float2bfloat16_rn(v);
+}
+
+// 4 sums with their bias, `have` of them in the row: act, rounding, one store where y is aligned for it
+__device__ __forceinline__ void store4(const MmArgs &a, int64_t at, const float (&f)[4], int have) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a.relu ? relu_keep_nan(f[i]) : f[i];
+    if (a.vec4 && have >= 4) {
+        if (a.out == CT_DT_F32) *reinterpret_cast<float4 *>(static_cast<float *>(a.y) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else if (a.out == CT_DT_F16)
+            *reinterpret_cast<uint2 *>(static_cast<__half *>(a.y) + at) =
+                make_uint2(pack2<__half>(v[0], v[1]), pack2<__half>(v[2], v[3]));
+        else
+            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.y) + at) =
+                make_uint2(pack2<__nv_bfloat16>(v[0], v[1]), pack2<__nv_bfloat16>(v[2], v[3]));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < have) store_out(a, at + i, v[i]);
 }
 
 __device__ __forceinline__ float finish(const MmArgs &a, float v, int n) {
@@ -338,26 +365,28 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
         }
     }
     __syncwarp();
-    if (a.splits > 1) cluster_sync();
-    else __syncthreads();
+    cluster_sync();
     if (warp < N_EPI) {
-        // this CTA finishes its share of the tile's columns
-        const int row = (int)threadIdx.x & (BL - 1), l = tl * BL + row;
+        // this CTA finishes its share of the tile's columns: a warp a column, 4 lane rows a thread
+        const int l = tl * BL + 4 * lane;
         const int cols = min(BN, a.M - tc * BN);
-        for (int c = rank * 2 + ((int)threadIdx.x >> 7); c < cols; c += 2 * a.splits) {
-            const float *p = (const float *)smem + c * BL + row;
-            float v = 0.f;
-            if (a.splits > 1) {
-                const uint32_t at = smem_u32(p);
+        float bias[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bias[i] = a.bias != nullptr && l + i < a.N ? __ldg(a.bias + l + i) : 0.f;
+#pragma unroll 2
+        for (int c = rank * N_EPI + warp; c < cols; c += a.splits * N_EPI) {
+            const uint32_t at = smem_u32((const float *)smem + c * BL + 4 * lane);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-                for (int s = 0; s < a.splits; ++s) v += ld_cluster_f32(mapa_shared(at, (uint32_t)s));
-            } else {
-                v = *p;
+            for (int s = 0; s < a.splits; ++s) {
+                const float4 p = ld_cluster_f32x4(mapa_shared(at, (uint32_t)s));
+                v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
             }
-            if (l < a.N) store_out(a, (int64_t)(tc * BN + c) * a.ldy + l, finish(a, v, l));
+            const float f[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
+            store4(a, (int64_t)(tc * BN + c) * a.ldy + l, f, a.N - l);
         }
     }
-    if (a.splits > 1) cluster_sync();                      // no CTA leaves while its sums may still be read
+    cluster_sync();                                        // no CTA leaves while its sums may still be read
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == MMA_WARP) {
@@ -374,7 +403,6 @@ constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9-10 MMA, 11 
 // were launched with 168 each (3 x 168 = 504)
 constexpr int W_REGS_EPI = 232, W_REGS_REST = 40;
 constexpr int W_BOX_BYTES = 32 * 128;
-constexpr int W_CHUNK = 16;                                // columns of one step of the unaligned store
 
 template <int BN> struct Wide {
     static constexpr int C_BYTES = BN / 2 * BK;            // this CTA's half of the column operand
@@ -382,6 +410,8 @@ template <int BN> struct Wide {
     static constexpr int BOXES = BN == 256 ? 1 : 2;        // epilogue: 32 rows of 128 bytes on their way to y, for each warp
     static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
     static constexpr int LDN = BN == 64 ? 16 : 32;         // columns of one TMEM load: an even number of loads
+    static constexpr int PITCH = BN + 4;                   // row of partial sums, in floats: 8 rows hit all banks
+    static_assert(BL * PITCH * 4 <= STAGES * (L_BYTES + C_BYTES), "partial sums over the stages");
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES +
                                    8 * (2 * STAGES + 5) + 16;
     static_assert(STAGES % N_MMA == 0, "a stage is one MMA warp's, see Narrow");
@@ -485,11 +515,14 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     uint32_t *tmem_holder = (uint32_t *)(mma_done + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t crank = cluster_ctarank();
+    // a cluster is `splits` pairs, which share a tile's K blocks
+    const uint32_t crank = cluster_ctarank() & 1u, pair = cluster_ctarank() >> 1, even = cluster_ctarank() & ~1u;
     const bool leader = crank == 0;
-    const int cid = (int)(blockIdx.x >> 1), ncl = (int)(gridDim.x >> 1);
+    const uint16_t both = (uint16_t)(3u << even);
+    const int cid = (int)(blockIdx.x / (unsigned)(2 * a.splits)), ncl = (int)(gridDim.x / (unsigned)(2 * a.splits));
     const int tiles = a.tiles_l * a.tiles_c;
-    const int KB = a.KB;
+    const int kb0 = (int)((int64_t)a.KB * pair / a.splits);
+    const int KB = (int)((int64_t)a.KB * (pair + 1) / a.splits) - kb0;      // this pair's
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) {
@@ -520,7 +553,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     if (warp >= N_EPI) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(W_REGS_REST));
         if (warp == TMA_WARP) {
-            const uint32_t full_even = mapa_shared(smem_u32(full), 0u);
+            const uint32_t full_even = mapa_shared(smem_u32(full), even);
             if (elect_one()) {
                 int it = 0;
                 bool ok = true;
@@ -534,8 +567,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         if (!ok) break;
                         const uint32_t fb = full_even + (uint32_t)(s * 8);
                         if (leader) mbar_arrive_expect_tx(smem_u32(&full[s]), 2u * (L_BYTES + S::C_BYTES));
-                        tma_load_2d_pair(smem_u32(Ls + s * L_BYTES), &lmap, fb, kb * BK, m0);
-                        tma_load_2d_pair(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, kb * BK, n0);
+                        tma_load_2d_pair(smem_u32(Ls + s * L_BYTES), &lmap, fb, (kb0 + kb) * BK, m0);
+                        tma_load_2d_pair(smem_u32(Cs + s * S::C_BYTES), &cmap, fb, (kb0 + kb) * BK, n0);
                     }
                 }
                 // no copy and no commit is under way when the CTA ends, see the narrow kernel (the even CTA's
@@ -562,12 +595,12 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 #pragma unroll
                     for (int k = 0; k < BK / 32; ++k)
                         umma_e4m3_pair(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
-                    umma_commit_pair_mc(smem_u32(&acc_full[b]), (uint16_t)3u);
-                    umma_commit_pair_mc(smem_u32(&empty[s]), (uint16_t)3u);
+                    umma_commit_pair_mc(smem_u32(&acc_full[b]), both);
+                    umma_commit_pair_mc(smem_u32(&empty[s]), both);
                     s += N_MMA;
                     if (s >= S::STAGES) { s -= S::STAGES; ++round; }
                 }
-                umma_commit_pair_mc(smem_u32(mma_done), (uint16_t)3u);
+                umma_commit_pair_mc(smem_u32(mma_done), both);
             }
         }
         __syncwarp();
@@ -575,7 +608,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(W_REGS_EPI));
         const int quad = warp & 3, half = warp >> 2;
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
-        const uint32_t acc_empty_even = mapa_shared(smem_u32(acc_empty), 0u);
+        const uint32_t acc_empty_even = mapa_shared(smem_u32(acc_empty), even);
         uint8_t *mine = boxes + warp * S::BOXES * W_BOX_BYTES;
         uint32_t stored = 0;                               // boxes this warp has stored
         int it = 0;
@@ -589,8 +622,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 #pragma unroll
             for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
 
-            const float *xp = a.xs + (int64_t)min(m_warp + lane, a.M - 1) * a.xs_row;
-            const float *wp = a.ws + (int64_t)(min(c0, a.N - 1) / 128) * a.ws_row;
+            const float *xp = a.xs + (int64_t)min(m_warp + lane, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
+            const float *wp = a.ws + (int64_t)(min(c0, a.N - 1) / 128) * a.ws_row + kb0 * a.ws_blk;
             float nx = __ldg(xp), nw = __ldg(wp);
             uint32_t r[2][LDN];
             ok = warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)(it >> 1) & 1u, a.err, E_EPI);
@@ -631,25 +664,36 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             }
             if (!ok) break;
 
-            if (a.vec) {
+            if (a.splits > 1) {
+                // partial sums [row][column], over the stages (see the narrow kernel); one tile
+                float *part = (float *)smem + (quad * 32 + lane) * S::PITCH + half * CPW;
+                asm volatile("bar.sync 1, %0;" ::"n"(N_EPI * 32) : "memory");
+#pragma unroll
+                for (int i = 0; i < CPW / 2; i += 2) *reinterpret_cast<ulonglong2 *>(part + 2 * i) = make_ulonglong2(acc[i], acc[i + 1]);
+            } else if (a.vec) {
                 if (a.out == CT_DT_F32) store_boxes<CPW, 32, 4, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
                 else store_boxes<CPW, CPW < 64 ? CPW : 64, 2, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
             } else {
-                // rows that start anywhere: two rows of 16 columns a step
+                // rows that start anywhere: 32 x 32 values through shared memory (value (r, c) at column c ^ r: no
+                // bank is hit twice), then a row's 32 columns a store
                 float *sq = (float *)mine;
 #pragma unroll
-                for (int c = 0; c < CPW; c += W_CHUNK) {
+                for (int c = 0; c < CPW; c += 32) {
                     if (c0 + c < a.N) {
 #pragma unroll
-                        for (int i = 0; i < W_CHUNK / 2; ++i)
-                            split2(acc[c / 2 + i], sq[lane * (W_CHUNK + 1) + 2 * i], sq[lane * (W_CHUNK + 1) + 2 * i + 1]);
+                        for (int i = 0; i < 32; i += 2)
+                            split2(acc[(c + i) / 2], sq[lane * 32 + (i ^ lane)], sq[lane * 32 + ((i + 1) ^ lane)]);
                         __syncwarp();
-                        const int j = lane % W_CHUNK, n = c0 + c + j;
+                        const int n = c0 + c + lane;
                         if (n < a.N) {
-#pragma unroll 4
-                            for (int q = lane / W_CHUNK; q < 32; q += 32 / W_CHUNK)
-                                if (m_warp + q < a.M)
-                                    store_out(a, (int64_t)(m_warp + q) * a.ldy + n, finish(a, sq[q * (W_CHUNK + 1) + j], n));
+                            const float bias = a.bias != nullptr ? __ldg(a.bias + n) : 0.f;
+                            const int rows = min(32, a.M - m_warp);
+#pragma unroll 8
+                            for (int q = 0; q < rows; ++q) {
+                                float v = sq[q * 32 + (lane ^ q)] + bias;
+                                if (a.relu) v = relu_keep_nan(v);
+                                store_out(a, (int64_t)(m_warp + q) * a.ldy + n, v);
+                            }
                         }
                         __syncwarp();
                     }
@@ -659,6 +703,33 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
+    if (a.splits > 1) {
+        cluster_sync();
+        if (warp < N_EPI) {
+            // this CTA finishes its share of the columns of its rows, added in the order of the pairs
+            const int width = BN / a.splits, lanes = width / 4;            // a row's, 4 columns a thread
+            int tl, tc;
+            tile_at(a, cid, tl, tc);
+            const int c = (int)pair * width + lane % lanes * 4, n = tc * BN + c;
+            const int m0 = (2 * tl + (int)crank) * BL;
+            float bias[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bias[i] = a.bias != nullptr && n + i < a.N ? __ldg(a.bias + n + i) : 0.f;
+            const int step = N_EPI * 32 / lanes;
+#pragma unroll 2
+            for (int row = (int)threadIdx.x / lanes; row < min(BL, a.M - m0); row += step) {
+                const uint32_t at = smem_u32((const float *)smem + row * S::PITCH + c);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int s = 0; s < a.splits; ++s) {
+                    const float4 p = ld_cluster_f32x4(mapa_shared(at, (uint32_t)(2 * s) + crank));
+                    v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+                }
+                const float f[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
+                if (n < a.N) store4(a, (int64_t)(m0 + row) * a.ldy + n, f, a.N - n);
+            }
+        }
+    }
     __syncthreads();
     // every MMA of the pair has completed before TMEM is freed in either CTA,
     // and no CTA leaves while its peer may still arrive on its barriers
@@ -728,11 +799,11 @@ cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, cons
 
 template <int BN>
 cudaError_t launch_wide(const CUtensorMap &lmap, const CUtensorMap &cmap, const CUtensorMap &ymap, const MmArgs &a,
-                        int pairs, cudaStream_t st) {
+                        int clusters, cudaStream_t st) {
     static std::atomic<bool> sized[MAX_DEVICES];
     const cudaError_t e = allow_smem(fp8_wide_kernel<BN>, sized, Wide<BN>::SMEM);
     if (e != cudaSuccess) return e;
-    return pdl_launch_cluster(fp8_wide_kernel<BN>, dim3((unsigned)(2 * pairs)), dim3(W_THREADS), Wide<BN>::SMEM, st, 2,
+    return pdl_launch_cluster(fp8_wide_kernel<BN>, dim3((unsigned)(2 * a.splits * clusters)), dim3(W_THREADS), Wide<BN>::SMEM, st, 2 * a.splits,
                               lmap, cmap, ymap, a);
 }
 
@@ -744,6 +815,69 @@ struct Operands {
     int64_t k;
 };
 
+struct Choice {
+    bool wide;
+    int bn, splits;
+};
+
+// Which kernel, how wide its tiles, over how many CTAs (pairs) K is split: the
+// least of a simple estimate, in us, whose figures were measured over some 30
+// shapes (each candidate timed on its own; the choice was within 10% of the
+// best of them).
+//   a K block costs a CTA 0.2, 0.25, 0.33, 0.5 us for 16, 32, 64, 128 columns
+//   and a pair 0.25, 0.36, 0.49 us for 64, 128, 256; launch, start and end of a
+//   tile 1.0, 1.3, 2.7, 3.3 and 3.9 to 4.8 us; adding the shares of a split 1.4
+//   to 2.2 us (pairs 3.5 us);
+//   no kernel is faster than its operands: 9 GB/ms from L2, 6.4 GB/ms of
+//   weights from HBM, 58 GB/s of them to one SM.
+Choice choose(int M, int N, int KB, int sms) {
+    Choice best = {false, 16, 1};
+    double least = 1e30;
+    const double weights = (double)N * KB * BK;
+    const auto consider = [&](bool wide, int bn, int splits, double t) {
+        if (t < least) {
+            least = t;
+            best = Choice{wide, bn, splits};
+        }
+    };
+    static const double n_block[4] = {0.2, 0.25, 0.33, 0.5}, n_tile[4] = {1.0, 1.3, 2.7, 3.3};
+    static const double n_split[9] = {0, 0, 1.4, 1.7, 2.0, 2.1, 2.2, 2.2, 2.2};
+    static const double w_block[3] = {0.25, 0.36, 0.49};
+    const int64_t rows_n = (N + 127) / 128;
+    for (int i = 0; i < 4; ++i) {
+        const int bn = 16 << i;
+        if (bn > 16 && bn / 2 >= M) break;
+        const int64_t tiles = rows_n * ((M + bn - 1) / bn), slots = (int64_t)sms * (bn <= 64 ? 2 : 1);
+        for (int s = 1; s <= 8 && s <= KB; ++s) {
+            if (s == 5 || s == 7) continue;
+            if (s > 1 && tiles * s > slots) break;
+            const double nkb = (KB + s - 1) / s, ctas = (double)tiles * s;
+            const double blocks = (double)((tiles * s + slots - 1) / slots) * nkb * n_block[i];
+            const double l2 = ctas * nkb * (BL + bn) * BK / 9e6;
+            const double busy = ctas < sms ? ctas : sms;
+            const double hbm = weights / (0.058 * busy < 6.4 ? 58e3 * busy : 6.4e6);
+            consider(false, bn, s, n_tile[i] + n_split[s] + fmax(blocks, fmax(l2, hbm)));
+        }
+    }
+    const int64_t pairs = sms / 2, rows_m = (M + 2 * BL - 1) / (2 * BL);
+    for (int i = 0; i < 3 && M > 64; ++i) {
+        const int bn = 64 << i;
+        const int64_t tiles = rows_m * ((N + bn - 1) / bn);
+        for (int s = 1; s <= 2 && s <= KB; ++s) {
+            if (s > 1 && tiles * s > pairs) break;
+            const double nkb = (KB + s - 1) / s, rounds = (double)((tiles * s + pairs - 1) / pairs);
+            const double blocks = rounds * nkb * w_block[i] + (rounds - 1) * 0.8;
+            const double l2 = (double)tiles * s * nkb * (2 * BL + bn) * BK / 10e6;
+            consider(true, bn, s, 3.6 + 0.0047 * bn + (s > 1 ? 3.5 : 0) + fmax(blocks, fmax(l2, weights / 6.4e6)));
+        }
+    }
+    if (const char *q = getenv("CT_FORCE")) {
+        int f[3];
+        if (sscanf(q, "%d,%d,%d", f, f + 1, f + 2) == 3) best = Choice{f[0] == 1, f[1], f[2]};
+    }
+    return best;
+}
+
 ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
     if (a.KB == 0) {
         const int64_t grid = ((int64_t)a.M * a.N + 255) / 256;
@@ -754,25 +888,18 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
     a.err = device_error_word();
     if (a.err == nullptr) return CT_ECUDA;
     const int sms = sm_count();
-    const int nt = (a.N + 127) / 128;
     CUtensorMap lmap, cmap;
     cudaError_t e;
-    if (a.M > 256) {
-        const int pairs = sms / 2;
+    const Choice ch = choose(a.M, a.N, a.KB, sms);
+    const int bn = ch.bn;
+    a.splits = ch.splits;
+    if (ch.wide) {
         a.tiles_l = (a.M + 2 * BL - 1) / (2 * BL);
-        a.splits = 1;
-        a.group = 8;
-        // column width: rounds of tiles over the pairs, each as long as its width plus a fixed part
-        int64_t best = INT64_MAX;
-        int bn = 64;
-        for (int w = 64; w <= 256; w *= 2) {
-            const int64_t t = (int64_t)a.tiles_l * ((a.N + w - 1) / w);
-            const int64_t cost = (t + pairs - 1) / pairs * (w + 64);
-            if (cost <= best) { best = cost; bn = w; }
-        }
         a.tiles_c = (a.N + bn - 1) / bn;
+        a.group = 8;
+        const int pairs = sms / 2;
         const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
-        if (tiles > INT32_MAX / 2) return CT_ERANGE;
+        if (tiles > INT32_MAX / 16) return CT_ERANGE;
         CUtensorMap ymap = {};
         const int es = dtype_size(a.out);
         a.vec = aligned(a.y, 16) && a.ldy * es % 16 == 0;
@@ -780,18 +907,15 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
             (a.vec && !encode(&ymap, a.y, a.out == CT_DT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16,
                               es, a.M, a.N, a.ldy * es, bn == 64 && es == 2 ? 64 : 128, 32)))
             return CT_ECUDA;
-        const int n = (int)(tiles < pairs ? tiles : pairs);
+        const int n = (int)(a.splits > 1 || tiles < pairs ? tiles : pairs);
         e = bn == 64    ? launch_wide<64>(lmap, cmap, ymap, a, n, st)
             : bn == 128 ? launch_wide<128>(lmap, cmap, ymap, a, n, st)
                         : launch_wide<256>(lmap, cmap, ymap, a, n, st);
     } else {
-        const int bn = a.M <= 16 ? 16 : a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-        a.tiles_l = nt;
+        a.tiles_l = (a.N + 127) / 128;
         a.tiles_c = (a.M + bn - 1) / bn;
         const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
         if (tiles > INT32_MAX / 16) return CT_ERANGE;
-        a.splits = 1;
-        while (a.splits < 8 && tiles * a.splits * 2 <= sms && a.splits * 2 <= a.KB) a.splits *= 2;
         if (!encode8(&lmap, o.wq, a.N, o.k, o.ldw, BL) || !encode8(&cmap, o.xq, a.M, o.k, o.ldx, bn)) return CT_ECUDA;
         const int grid = (int)tiles * a.splits;
         e = bn == 16   ? launch_narrow<16>(lmap, cmap, a, grid, st)
@@ -821,6 +945,7 @@ MmArgs make_args(int64_t m, int64_t n, int64_t k, const float *ws, int64_t ws_ro
     a.bias = bias; a.y = y; a.ldy = ldy;
     a.M = (int)m; a.N = (int)n; a.KB = (int)((k + BK - 1) / BK);
     a.out = out; a.relu = relu != 0;
+    a.vec4 = aligned(y, 4 * dtype_size(out)) && (m == 1 || ldy % 4 == 0);
     return a;
 }
 
