@@ -52,6 +52,11 @@ constexpr int N_EPI = 8;
 constexpr int TMA_WARP = 8, MMA_WARP = 9, N_MMA = 2;
 constexpr int THREADS = 32 * (MMA_WARP + N_MMA);
 
+// scales are fetched this many of a warp's K blocks at a time, that many
+// ahead: a load takes longer (up to 800 cycles while the tiles stream) than a
+// block should
+constexpr int AHEAD = 4;
+
 // error codes of the bounded waits
 constexpr uint32_t E_TMA = 0x100, E_MMA = 0x200, E_ACC = 0x400, E_EPI = 0x800, E_DRAIN = 0x1000;
 
@@ -292,11 +297,11 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
 #pragma unroll
         for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
 
-        // scales of this warp's next block, fetched ahead: lane j holds
-        // column j's; the warp shares the products through shared memory
+        // scales of this warp's next blocks: lane j holds column j's, and the
+        // warp shares the products through shared memory
         constexpr int NF = (CPW + 31) / 32;
         const int first = GROUPS == 1 ? 0 : half;
-        float nx[NF], nw = 0.f;
+        float nx[AHEAD][NF], nw[AHEAD];
         const float *xp[NF];
         bool xin[NF];
 #pragma unroll
@@ -304,44 +309,56 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
             const int m = c0 + j * 32 + lane;
             xin[j] = j * 32 + lane < CPW && m < a.M;
             xp[j] = a.xs + (int64_t)(xin[j] ? m : 0) * a.xs_row;
-            nx[j] = 0.f;
         }
         const float *wp = a.ws + (int64_t)tl * a.ws_row;
         const auto fetch = [&](int i) {
-            const int64_t kb = kb0 + i;
 #pragma unroll
-            for (int j = 0; j < NF; ++j) nx[j] = xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
-            nw = __ldg(wp + kb * a.ws_blk);
+            for (int u = 0; u < AHEAD; ++u) {
+                const bool in = i + u * GROUPS < nkb;
+                const int64_t kb = kb0 + i + u * GROUPS;
+#pragma unroll
+                for (int j = 0; j < NF; ++j) nx[u][j] = in && xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
+                nw[u] = in ? __ldg(wp + kb * a.ws_blk) : 0.f;
+            }
         };
-        if (first < nkb) fetch(first);
+        fetch(first);
 
         bool ok = true;
-        for (int it = first; it < nkb; it += GROUPS) {
-            const int b = it % NBUF;
-            float *fs = fac + (warp * 2 + (it / GROUPS & 1)) * CPW;
+        for (int its = first; its < nkb && ok; its += AHEAD * GROUPS) {
+            float f[AHEAD][NF];
 #pragma unroll
-            for (int j = 0; j < NF; ++j)
-                if (j * 32 + lane < CPW) fs[j * 32 + lane] = nx[j] * nw;
-            __syncwarp();
-            if (it + GROUPS < nkb) fetch(it + GROUPS);
-            ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-            for (int c = 0; c < CPW; c += LDN) {
-                uint32_t r[LDN];
-                tmem_ld_nw<LDN>(tbase + (uint32_t)(b * BN + c), r);
-                tmem_wait_ld();
+                for (int j = 0; j < NF; ++j) f[u][j] = nx[u][j] * nw[u];
+            if (its + AHEAD * GROUPS < nkb) fetch(its + AHEAD * GROUPS);
 #pragma unroll
-                for (int i = 0; i < LDN; i += 4) {
-                    const ulonglong2 f = *reinterpret_cast<const ulonglong2 *>(fs + c + i);
-                    fma2(acc[(c + i) / 2], f.x, r[i], r[i + 1]);
-                    fma2(acc[(c + i) / 2 + 1], f.y, r[i + 2], r[i + 3]);
+            for (int u = 0; u < AHEAD; ++u) {
+                const int it = its + u * GROUPS, b = it % NBUF;
+                if (it >= nkb) break;
+                float *fs = fac + (warp * 2 + (u & 1)) * CPW;
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+                    if (j * 32 + lane < CPW) fs[j * 32 + lane] = f[u][j];
+                __syncwarp();
+                ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int c = 0; c < CPW; c += LDN) {
+                    uint32_t r[LDN];
+                    tmem_ld_nw<LDN>(tbase + (uint32_t)(b * BN + c), r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < LDN; i += 4) {
+                        const ulonglong2 q = *reinterpret_cast<const ulonglong2 *>(fs + c + i);
+                        fma2(acc[(c + i) / 2], q.x, r[i], r[i + 1]);
+                        fma2(acc[(c + i) / 2 + 1], q.y, r[i + 2], r[i + 3]);
+                    }
                 }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
             }
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
         }
         // Partial sums [column][lane row], over the stages: once both halves
         // are here every copy has landed and every MMA has read it.  (After a
@@ -406,12 +423,13 @@ constexpr int W_BOX_BYTES = 32 * 128;
 
 template <int BN> struct Wide {
     static constexpr int C_BYTES = BN / 2 * BK;            // this CTA's half of the column operand
-    static constexpr int STAGES = BN == 64 ? 8 : 6;
-    static constexpr int BOXES = BN == 256 ? 1 : 2;        // epilogue: 32 rows of 128 bytes on their way to y, for each warp
+    static constexpr int STAGES = BN == 256 ? 4 : 6;
+    static constexpr int BOXES = 2;                        // epilogue: 32 rows of 128 bytes on their way to y, for each warp
     static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
     static constexpr int LDN = BN == 64 ? 16 : 32;         // columns of one TMEM load: an even number of loads
     static constexpr int PITCH = BN + 4;                   // row of partial sums, in floats: 8 rows hit all banks
-    static_assert(BL * PITCH * 4 <= STAGES * (L_BYTES + C_BYTES), "partial sums over the stages");
+    static_assert(BL * PITCH * 4 <= STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES,
+                  "partial sums over the stages and boxes");
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES +
                                    8 * (2 * STAGES + 5) + 16;
     static_assert(STAGES % N_MMA == 0, "a stage is one MMA warp's, see Narrow");
@@ -624,48 +642,63 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 
             const float *xp = a.xs + (int64_t)min(m_warp + lane, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
             const float *wp = a.ws + (int64_t)(min(c0, a.N - 1) / 128) * a.ws_row + kb0 * a.ws_blk;
-            float nx = __ldg(xp), nw = __ldg(wp);
+            float nx[AHEAD], nw[AHEAD];
+            const auto fetch = [&](int kb) {
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u)
+                    if (kb + u < KB) {
+                        nx[u] = __ldg(xp);
+                        nw[u] = __ldg(wp);
+                        xp += a.xs_blk;
+                        wp += a.ws_blk;
+                    }
+            };
+            fetch(0);
             uint32_t r[2][LDN];
             ok = warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)(it >> 1) & 1u, a.err, E_EPI);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             tmem_ld_nw<LDN>(tbase + (uint32_t)((it & 1) * BN), r[0]);
-            for (int kb = 0; kb < KB; ++kb, ++it) {
-                const uint32_t src = tbase + (uint32_t)((it & 1) * BN);
-                const uint64_t f = dup2(nx * nw);
-                if (kb + 1 < KB) {                         // the next block's scales
-                    xp += a.xs_blk;
-                    wp += a.ws_blk;
-                    nx = __ldg(xp);
-                    nw = __ldg(wp);
-                }
-                // LDN columns are on their way while the LDN before are added,
-                // across blocks too
+            for (int kbs = 0; kbs < KB && ok; kbs += AHEAD) {
+                float fs[AHEAD];
 #pragma unroll
-                for (int c = 0; c < CPW; c += LDN) {
-                    const int h = c / LDN & 1;
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    if (c + LDN < CPW) {
-                        tmem_ld_nw<LDN>(src + (uint32_t)(c + LDN), r[h ^ 1]);
-                    } else {
-                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & 1) * 8));
-                        if (kb + 1 < KB) {
-                            ok = warp_wait(smem_u32(&acc_full[(it + 1) & 1]), (uint32_t)((it + 1) >> 1) & 1u, a.err, E_EPI);
-                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                            if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & 1) * BN), r[h ^ 1]);
+                for (int u = 0; u < AHEAD; ++u) fs[u] = nx[u] * nw[u];
+                fetch(kbs + AHEAD);
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u, ++it) {
+                    const int kb = kbs + u;
+                    if (kb >= KB) break;
+                    const uint32_t src = tbase + (uint32_t)((it & 1) * BN);
+                    const uint64_t f = dup2(fs[u]);
+                    // LDN columns are on their way while the LDN before are
+                    // added, across blocks too
+#pragma unroll
+                    for (int c = 0; c < CPW; c += LDN) {
+                        const int h = c / LDN & 1;
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        if (c + LDN < CPW) {
+                            tmem_ld_nw<LDN>(src + (uint32_t)(c + LDN), r[h ^ 1]);
+                        } else {
+                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & 1) * 8));
+                            if (kb + 1 < KB) {
+                                ok = warp_wait(smem_u32(&acc_full[(it + 1) & 1]), (uint32_t)((it + 1) >> 1) & 1u, a.err,
+                                               E_EPI);
+                                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                                if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & 1) * BN), r[h ^ 1]);
+                            }
                         }
-                    }
 #pragma unroll
-                    for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
+                        for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
+                    }
+                    if (!ok) break;
                 }
-                if (!ok) break;
             }
             if (!ok) break;
 
             if (a.splits > 1) {
-                // partial sums [row][column], over the stages (see the narrow kernel); one tile
+                // partial sums [row][column], over the stages and boxes (see the narrow kernel); one tile
                 float *part = (float *)smem + (quad * 32 + lane) * S::PITCH + half * CPW;
                 asm volatile("bar.sync 1, %0;" ::"n"(N_EPI * 32) : "memory");
 #pragma unroll
