@@ -52,9 +52,8 @@ constexpr int N_EPI = 8;
 constexpr int TMA_WARP = 8, MMA_WARP = 9, N_MMA = 2;
 constexpr int THREADS = 32 * (MMA_WARP + N_MMA);
 
-// scales are fetched this many of a warp's K blocks at a time, that many
-// ahead: a load takes longer (up to 800 cycles while the tiles stream) than a
-// block should
+// narrow: scales are fetched this many of a warp's K blocks at a time, that
+// many ahead
 constexpr int AHEAD = 4;
 
 // error codes of the bounded waits
@@ -183,6 +182,11 @@ __device__ __forceinline__ void fma2(uint64_t &acc, uint64_t f, uint32_t p0, uin
 __device__ __forceinline__ uint64_t dup2(float f) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(f));
+    return r;
+}
+__device__ __forceinline__ uint64_t join2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
     return r;
 }
 __device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
@@ -415,10 +419,12 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
 // ---------------------------------------------------------------------------
 // wide: CTA pairs
 // ---------------------------------------------------------------------------
-constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9-10 MMA, 11 idle
-// registers a thread after the split: 2 x 232 + 40 for three warpgroups that
+constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9-10 MMA, 11 scales
+constexpr int SCALE_WARP = 11;
+constexpr int FAC_SLOTS = 4;
+// registers a thread after the split: 2 x 224 + 56 for three warpgroups that
 // were launched with 168 each (3 x 168 = 504)
-constexpr int W_REGS_EPI = 232, W_REGS_REST = 40;
+constexpr int W_REGS_EPI = 224, W_REGS_REST = 56;
 constexpr int W_BOX_BYTES = 32 * 128;
 
 template <int BN> struct Wide {
@@ -431,7 +437,7 @@ template <int BN> struct Wide {
     static_assert(BL * PITCH * 4 <= STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES,
                   "partial sums over the stages and boxes");
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES +
-                                   8 * (2 * STAGES + 5) + 16;
+                                   FAC_SLOTS * 2 * BL * 4 + 8 * (2 * STAGES + 5) + 16;
     static_assert(STAGES % N_MMA == 0, "a stage is one MMA warp's, see Narrow");
 };
 
@@ -466,20 +472,39 @@ __device__ __forceinline__ void tile_at(const MmArgs &a, int t, int &l, int &c) 
     c = r / rows;
 }
 
-// 16 bytes of y from finished values: 4 FP32 or 8 of 16 bits
-template <int SIZE> __device__ __forceinline__ uint4 out16(int out, const float *v) {
-    if constexpr (SIZE == 4) return pack16<float>(v);
-    else return out == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
+// bias and activation on a thread's row, as passes of their own: the code of
+// a tile's end runs once in thousands of cycles, so what it does not need
+// should not be fetched with it
+template <int CPW> __device__ __forceinline__ void finish_row(const MmArgs &a, uint64_t *acc, int c0) {
+    if (a.bias != nullptr) {
+#pragma unroll
+        for (int i = 0; i < CPW / 2; ++i) {
+            float u, v;
+            split2(acc[i], u, v);
+            u += __ldg(a.bias + min(c0 + 2 * i, a.N - 1));
+            v += __ldg(a.bias + min(c0 + 2 * i + 1, a.N - 1));
+            acc[i] = join2(u, v);
+        }
+    }
+    if (a.relu) {
+#pragma unroll
+        for (int i = 0; i < CPW / 2; ++i) {
+            float u, v;
+            split2(acc[i], u, v);
+            acc[i] = join2(relu_keep_nan(u), relu_keep_nan(v));
+        }
+    }
 }
 
 // Rows of y that TMA can address: through shared memory in boxes of 32 rows
 // by COLS columns, 128 bytes (64 where the warp's columns are fewer), swizzled
-// so that the 16-byte pieces of 8 rows hit 8 bank groups, stored by TMA, which clips what lies past the ends, while the next tile's
-// products are added.
-template <int CPW, int COLS, int SIZE, int BOXES>
+// so that the 16-byte pieces of 8 rows hit 8 bank groups, stored by TMA,
+// which clips what lies past the ends, while the next tile's products are added.
+template <typename O, int CPW, int BOXES>
 __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *ymap, const uint64_t *acc, uint8_t *boxes,
                                             uint32_t &stored, int m_warp, int c0, int lane) {
-    constexpr int PER16 = 16 / SIZE;                       // values of 16 bytes
+    constexpr int COLS = 128 / (int)sizeof(O) < CPW ? 128 / (int)sizeof(O) : CPW;
+    constexpr int PER16 = 16 / (int)sizeof(O);             // values of 16 bytes
     constexpr int PIECES = COLS / PER16;                   // 16-byte pieces of a box row
     static_assert((PIECES == 8 || PIECES == 4) && CPW % COLS == 0, "box rows of 128 or 64 bytes");
     const int swz = PIECES == 8 ? lane & 7 : (lane >> 1) & 3;
@@ -495,15 +520,7 @@ __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *
             float v[PER16];
 #pragma unroll
             for (int i = 0; i < PER16 / 2; ++i) split2(acc[(c + j * PER16) / 2 + i], v[2 * i], v[2 * i + 1]);
-            if (a.bias != nullptr) {
-#pragma unroll
-                for (int i = 0; i < PER16; ++i) v[i] += __ldg(a.bias + min(c0 + c + j * PER16 + i, a.N - 1));
-            }
-            if (a.relu) {
-#pragma unroll
-                for (int i = 0; i < PER16; ++i) v[i] = relu_keep_nan(v[i]);
-            }
-            *reinterpret_cast<uint4 *>(box + lane * (PIECES * 16) + ((j ^ swz) * 16)) = out16<SIZE>(a.out, v);
+            *reinterpret_cast<uint4 *>(box + lane * (PIECES * 16) + ((j ^ swz) * 16)) = pack16<O>(v);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -514,7 +531,28 @@ __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *
     }
 }
 
-template <int BN>
+// Rows that start anywhere: 32 x 32 values through shared memory (value (r, c)
+// at column c ^ r: no bank is hit twice), then a row's 32 columns a store.
+template <typename O, int CPW>
+__device__ __forceinline__ void store_lines(const MmArgs &a, const uint64_t *acc, float *sq, int m_warp, int c0, int lane) {
+    const int rows = min(32, a.M - m_warp);
+#pragma unroll
+    for (int c = 0; c < CPW; c += 32) {
+        if (c0 + c >= a.N) break;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2)
+            split2(acc[(c + i) / 2], sq[lane * 32 + (i ^ lane)], sq[lane * 32 + ((i + 1) ^ lane)]);
+        __syncwarp();
+        if (c0 + c + lane < a.N) {
+            O *y = static_cast<O *>(a.y) + (int64_t)m_warp * a.ldy + c0 + c + lane;
+#pragma unroll 4
+            for (int q = 0; q < rows; ++q, y += a.ldy) *y = from_f32<O>(sq[q * 32 + (lane ^ q)]);
+        }
+        __syncwarp();
+    }
+}
+
+template <int BN, bool SPLIT>
 __global__ void __launch_bounds__(W_THREADS, 1)
 fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap,
                 const __grid_constant__ CUtensorMap ymap, const MmArgs a) {
@@ -525,22 +563,24 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     uint8_t *Ls = smem;
     uint8_t *Cs = Ls + S::STAGES * L_BYTES;
     uint8_t *boxes = Cs + S::STAGES * S::C_BYTES;
-    uint64_t *full = (uint64_t *)(boxes + N_EPI * S::BOXES * W_BOX_BYTES);   // even CTA's: both CTAs' copies of a stage
+    float *fac = (float *)(boxes + N_EPI * S::BOXES * W_BOX_BYTES);   // [slot][column half][row]: scale of a block's sums
+    uint64_t *full = (uint64_t *)(fac + FAC_SLOTS * 2 * BL);   // even CTA's: both CTAs' copies of a stage
     uint64_t *empty = full + S::STAGES;                    // each CTA: the pair's MMAs have read the stage
-    uint64_t *acc_full = empty + S::STAGES;                // each CTA: a block's products are in TMEM
+    uint64_t *acc_full = empty + S::STAGES;                // each CTA: a block's products are in TMEM, its scales in fac
     uint64_t *acc_empty = acc_full + 2;                    // even CTA's: both CTAs' epilogues have read them
     uint64_t *mma_done = acc_empty + 2;
     uint32_t *tmem_holder = (uint32_t *)(mma_done + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // a cluster is `splits` pairs, which share a tile's K blocks
-    const uint32_t crank = cluster_ctarank() & 1u, pair = cluster_ctarank() >> 1, even = cluster_ctarank() & ~1u;
+    // SPLIT: a cluster is `splits` pairs, which share one tile's K blocks
+    const uint32_t crank = cluster_ctarank() & 1u, pair = SPLIT ? cluster_ctarank() >> 1 : 0u, even = 2u * pair;
     const bool leader = crank == 0;
     const uint16_t both = (uint16_t)(3u << even);
-    const int cid = (int)(blockIdx.x / (unsigned)(2 * a.splits)), ncl = (int)(gridDim.x / (unsigned)(2 * a.splits));
+    const unsigned ctas = SPLIT ? 2u * (unsigned)a.splits : 2u;
+    const int cid = (int)(blockIdx.x / ctas), ncl = (int)(gridDim.x / ctas);
     const int tiles = a.tiles_l * a.tiles_c;
-    const int kb0 = (int)((int64_t)a.KB * pair / a.splits);
-    const int KB = (int)((int64_t)a.KB * (pair + 1) / a.splits) - kb0;      // this pair's
+    const int kb0 = SPLIT ? (int)((int64_t)a.KB * pair / a.splits) : 0;     // this pair's
+    const int KB = SPLIT ? (int)((int64_t)a.KB * (pair + 1) / a.splits) - kb0 : a.KB;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::STAGES; ++s) {
@@ -548,7 +588,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             mbar_init(smem_u32(&empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&acc_full[b]), 1);
+            mbar_init(smem_u32(&acc_full[b]), 2);
             mbar_init(smem_u32(&acc_empty[b]), 2 * N_EPI);
         }
         mbar_init(smem_u32(mma_done), N_MMA);
@@ -596,6 +636,52 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         mbar_wait(smem_u32(ok ? &empty[j % S::STAGES] : &full[j % S::STAGES]),
                                   (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
             }
+        } else if (warp == SCALE_WARP) {
+            // Scale loads take up to 800 cycles while the tiles stream, so this
+            // warp makes them blocks ahead: 4 rows a lane, both column halves.
+            // Block `it` goes to slot it % 4 once block it - 2 is complete: the
+            // epilogue has then read block it - 4's TMEM, and before it the slot.
+            int it = 0;
+            bool ok = true;
+            for (int t = cid; t < tiles && ok; t += ncl) {
+                int tl, tc;
+                tile_at(a, t, tl, tc);
+                const int m0 = (2 * tl + (int)crank) * BL + lane, last = (a.N - 1) / 128;
+                const float *xp[4], *wp[2];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    xp[i] = a.xs + (int64_t)min(m0 + 32 * i, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    wp[q] = a.ws + (int64_t)min((tc * BN + q * CPW) / 128, last) * a.ws_row + kb0 * a.ws_blk;
+                float x[2][4], w[2][2];                    // two blocks in flight
+                const auto load = [&](int kb, int u) {
+                    if (kb < KB) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[u][i] = __ldg(xp[i] + kb * a.xs_blk);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) w[u][q] = __ldg(wp[q] + kb * a.ws_blk);
+                    }
+                };
+                load(0, 0);
+                load(1, 1);
+                for (int kb = 0; kb < KB && ok; kb += 2) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u, ++it) {
+                        if (kb + u >= KB) break;
+                        ok = it < 2 || warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)((it - 2) >> 1) & 1u, a.err, E_EPI);
+                        if (!ok) break;
+                        float *slot = fac + it % FAC_SLOTS * (2 * BL);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) slot[q * BL + 32 * i + lane] = x[u][i] * w[u][q];
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&acc_full[it & 1]));
+                        load(kb + u + 2, u);
+                    }
+                }
+            }
         } else if (warp < MMA_WARP + N_MMA && leader) {
             constexpr uint32_t idesc = idesc_e4m3(2 * BL, BN);
             if (elect_one()) {
@@ -628,6 +714,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
         const uint32_t acc_empty_even = mapa_shared(smem_u32(acc_empty), even);
         uint8_t *mine = boxes + warp * S::BOXES * W_BOX_BYTES;
+        const float *my_fac = fac + half * BL + quad * 32 + lane;
         uint32_t stored = 0;                               // boxes this warp has stored
         int it = 0;
         bool ok = true;
@@ -640,103 +727,63 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 #pragma unroll
             for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
 
-            const float *xp = a.xs + (int64_t)min(m_warp + lane, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
-            const float *wp = a.ws + (int64_t)(min(c0, a.N - 1) / 128) * a.ws_row + kb0 * a.ws_blk;
-            float nx[AHEAD], nw[AHEAD];
-            const auto fetch = [&](int kb) {
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u)
-                    if (kb + u < KB) {
-                        nx[u] = __ldg(xp);
-                        nw[u] = __ldg(wp);
-                        xp += a.xs_blk;
-                        wp += a.ws_blk;
-                    }
-            };
-            fetch(0);
             uint32_t r[2][LDN];
             ok = warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)(it >> 1) & 1u, a.err, E_EPI);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             tmem_ld_nw<LDN>(tbase + (uint32_t)((it & 1) * BN), r[0]);
-            for (int kbs = 0; kbs < KB && ok; kbs += AHEAD) {
-                float fs[AHEAD];
+            for (int kb = 0; kb < KB && ok; ++kb, ++it) {
+                const uint32_t src = tbase + (uint32_t)((it & 1) * BN);
+                const uint64_t f = dup2(my_fac[it % FAC_SLOTS * (2 * BL)]);
+                // LDN columns are on their way while the LDN before are added,
+                // across blocks too
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) fs[u] = nx[u] * nw[u];
-                fetch(kbs + AHEAD);
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u, ++it) {
-                    const int kb = kbs + u;
-                    if (kb >= KB) break;
-                    const uint32_t src = tbase + (uint32_t)((it & 1) * BN);
-                    const uint64_t f = dup2(fs[u]);
-                    // LDN columns are on their way while the LDN before are
-                    // added, across blocks too
-#pragma unroll
-                    for (int c = 0; c < CPW; c += LDN) {
-                        const int h = c / LDN & 1;
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                        if (c + LDN < CPW) {
-                            tmem_ld_nw<LDN>(src + (uint32_t)(c + LDN), r[h ^ 1]);
-                        } else {
-                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & 1) * 8));
-                            if (kb + 1 < KB) {
-                                ok = warp_wait(smem_u32(&acc_full[(it + 1) & 1]), (uint32_t)((it + 1) >> 1) & 1u, a.err,
-                                               E_EPI);
-                                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                                if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & 1) * BN), r[h ^ 1]);
-                            }
+                for (int c = 0; c < CPW; c += LDN) {
+                    const int h = c / LDN & 1;
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    if (c + LDN < CPW) {
+                        tmem_ld_nw<LDN>(src + (uint32_t)(c + LDN), r[h ^ 1]);
+                    } else {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & 1) * 8));
+                        if (kb + 1 < KB) {
+                            ok = warp_wait(smem_u32(&acc_full[(it + 1) & 1]), (uint32_t)((it + 1) >> 1) & 1u, a.err, E_EPI);
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                            if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & 1) * BN), r[h ^ 1]);
                         }
-#pragma unroll
-                        for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
                     }
-                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
                 }
             }
             if (!ok) break;
 
-            if (a.splits > 1) {
+            if constexpr (SPLIT) {
                 // partial sums [row][column], over the stages and boxes (see the narrow kernel); one tile
                 float *part = (float *)smem + (quad * 32 + lane) * S::PITCH + half * CPW;
                 asm volatile("bar.sync 1, %0;" ::"n"(N_EPI * 32) : "memory");
 #pragma unroll
                 for (int i = 0; i < CPW / 2; i += 2) *reinterpret_cast<ulonglong2 *>(part + 2 * i) = make_ulonglong2(acc[i], acc[i + 1]);
-            } else if (a.vec) {
-                if (a.out == CT_DT_F32) store_boxes<CPW, 32, 4, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
-                else store_boxes<CPW, CPW < 64 ? CPW : 64, 2, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
             } else {
-                // rows that start anywhere: 32 x 32 values through shared memory (value (r, c) at column c ^ r: no
-                // bank is hit twice), then a row's 32 columns a store
-                float *sq = (float *)mine;
-#pragma unroll
-                for (int c = 0; c < CPW; c += 32) {
-                    if (c0 + c < a.N) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2)
-                            split2(acc[(c + i) / 2], sq[lane * 32 + (i ^ lane)], sq[lane * 32 + ((i + 1) ^ lane)]);
-                        __syncwarp();
-                        const int n = c0 + c + lane;
-                        if (n < a.N) {
-                            const float bias = a.bias != nullptr ? __ldg(a.bias + n) : 0.f;
-                            const int rows = min(32, a.M - m_warp);
-#pragma unroll 8
-                            for (int q = 0; q < rows; ++q) {
-                                float v = sq[q * 32 + (lane ^ q)] + bias;
-                                if (a.relu) v = relu_keep_nan(v);
-                                store_out(a, (int64_t)(m_warp + q) * a.ldy + n, v);
-                            }
-                        }
-                        __syncwarp();
-                    }
+                finish_row<CPW>(a, acc, c0);
+                if (a.vec) {
+                    if (a.out == CT_DT_F32) store_boxes<float, CPW, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+                    else if (a.out == CT_DT_F16)
+                        store_boxes<__half, CPW, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+                    else
+                        store_boxes<__nv_bfloat16, CPW, S::BOXES>(a, &ymap, acc, mine, stored, m_warp, c0, lane);
+                } else {
+                    if (a.out == CT_DT_F32) store_lines<float, CPW>(a, acc, (float *)mine, m_warp, c0, lane);
+                    else if (a.out == CT_DT_F16) store_lines<__half, CPW>(a, acc, (float *)mine, m_warp, c0, lane);
+                    else store_lines<__nv_bfloat16, CPW>(a, acc, (float *)mine, m_warp, c0, lane);
                 }
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
-    if (a.splits > 1) {
+    if constexpr (SPLIT) {
         cluster_sync();
         if (warp < N_EPI) {
             // this CTA finishes its share of the columns of its rows, added in the order of the pairs
@@ -830,13 +877,13 @@ cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, cons
                               lmap, cmap, a);
 }
 
-template <int BN>
+template <int BN, bool SPLIT>
 cudaError_t launch_wide(const CUtensorMap &lmap, const CUtensorMap &cmap, const CUtensorMap &ymap, const MmArgs &a,
                         int clusters, cudaStream_t st) {
     static std::atomic<bool> sized[MAX_DEVICES];
-    const cudaError_t e = allow_smem(fp8_wide_kernel<BN>, sized, Wide<BN>::SMEM);
+    const cudaError_t e = allow_smem(fp8_wide_kernel<BN, SPLIT>, sized, Wide<BN>::SMEM);
     if (e != cudaSuccess) return e;
-    return pdl_launch_cluster(fp8_wide_kernel<BN>, dim3((unsigned)(2 * a.splits * clusters)), dim3(W_THREADS), Wide<BN>::SMEM, st, 2 * a.splits,
+    return pdl_launch_cluster(fp8_wide_kernel<BN, SPLIT>, dim3((unsigned)(2 * a.splits * clusters)), dim3(W_THREADS), Wide<BN>::SMEM, st, 2 * a.splits,
                               lmap, cmap, ymap, a);
 }
 
@@ -941,9 +988,14 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
                               es, a.M, a.N, a.ldy * es, bn == 64 && es == 2 ? 64 : 128, 32)))
             return CT_ECUDA;
         const int n = (int)(a.splits > 1 || tiles < pairs ? tiles : pairs);
-        e = bn == 64    ? launch_wide<64>(lmap, cmap, ymap, a, n, st)
-            : bn == 128 ? launch_wide<128>(lmap, cmap, ymap, a, n, st)
-                        : launch_wide<256>(lmap, cmap, ymap, a, n, st);
+        if (a.splits > 1)
+            e = bn == 64    ? launch_wide<64, true>(lmap, cmap, ymap, a, n, st)
+                : bn == 128 ? launch_wide<128, true>(lmap, cmap, ymap, a, n, st)
+                            : launch_wide<256, true>(lmap, cmap, ymap, a, n, st);
+        else
+            e = bn == 64    ? launch_wide<64, false>(lmap, cmap, ymap, a, n, st)
+                : bn == 128 ? launch_wide<128, false>(lmap, cmap, ymap, a, n, st)
+                            : launch_wide<256, false>(lmap, cmap, ymap, a, n, st);
     } else {
         a.tiles_l = (a.N + 127) / 128;
         a.tiles_c = (a.M + bn - 1) / bn;
