@@ -12,9 +12,7 @@
 // MMAs run into another accumulator.
 //
 // Warp roles: 8 epilogue warps (warp w reads TMEM lanes 32 (w % 4) ..), one TMA
-// warp, two MMA warps that take K blocks in turn (testing two barriers and
-// issuing four MMAs and two commits takes one thread 600 cycles, as long as
-// the MMAs of a 256 x 256 tile).  A stage of shared memory
+// warp, one MMA warp (a second one that took K blocks in turn changed nothing).  A stage of shared memory
 // holds one K block of both operands: 128-byte rows, 128-byte swizzle; rows
 // and columns past the ends are the zeros TMA fills in.
 //
@@ -49,8 +47,8 @@ constexpr int BL = 128;                 // lane side of a tile
 constexpr int BK = 128;                 // K block: one scale, one 128-byte row
 constexpr int L_BYTES = BL * BK;
 constexpr int N_EPI = 8;
-constexpr int TMA_WARP = 8, MMA_WARP = 9, N_MMA = 2;
-constexpr int THREADS = 32 * (MMA_WARP + N_MMA);
+constexpr int TMA_WARP = 8, MMA_WARP = 9;
+constexpr int THREADS = 320;
 
 // narrow: scales are fetched this many of a warp's K blocks at a time, that
 // many ahead
@@ -81,8 +79,7 @@ struct MmArgs {
 template <int BN> struct Narrow {
     static constexpr int C_BYTES = BN * BK;
     static constexpr int STAGE = L_BYTES + C_BYTES;
-    // two CTAs share an SM where the tiles are narrow
-    static constexpr int STAGES = BN == 16 ? 6 : BN <= 64 ? 4 : 6;
+    static constexpr int STAGES = BN == 16 ? 10 : BN == 128 ? 6 : 8;
     static constexpr int NBUF = BN <= 64 ? 4 : 2;
     static constexpr int TMEM_COLS = NBUF * BN;
     // up to 64 columns: the two halves of the epilogue warps take K blocks in
@@ -93,9 +90,6 @@ template <int BN> struct Narrow {
     static constexpr int LDN = CPW < 32 ? CPW : 32;        // columns of one TMEM load
     static constexpr int FAC = N_EPI * 2 * CPW * 4;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16;
-    // each stage and each accumulator is one MMA warp's: a barrier's phases are
-    // told apart by parity, so no warp may be a phase ahead of another's wait
-    static_assert(STAGES % N_MMA == 0 && NBUF % N_MMA == 0, "stages and accumulators of one MMA warp");
 };
 
 template <int N> __device__ __forceinline__ void tmem_ld_nw(uint32_t taddr, uint32_t (&r)[N]) {
@@ -271,10 +265,10 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
                           E_DRAIN);
         }
         __syncwarp();
-    } else if (warp >= MMA_WARP) {
+    } else if (warp == MMA_WARP) {
         constexpr uint32_t idesc = idesc_e4m3(BL, BN);
         if (elect_one()) {
-            for (int it = warp - MMA_WARP; it < nkb; it += N_MMA) {
+            for (int it = 0; it < nkb; ++it) {
                 const int s = it % STAGES, b = it % NBUF;
                 if (!mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / NBUF) & 1u) ^ 1u, a.err, E_ACC) ||
                     !mbar_wait(smem_u32(&full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_MMA))
@@ -419,9 +413,9 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
 // ---------------------------------------------------------------------------
 // wide: CTA pairs
 // ---------------------------------------------------------------------------
-constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9-10 MMA, 11 scales
-constexpr int SCALE_WARP = 11;
-constexpr int FAC_SLOTS = 4;
+constexpr int W_THREADS = 384;       // warps 0-7 epilogue, 8 TMA, 9 MMA, 10-11 scales
+constexpr int SCALE_WARP = 10, N_SCALE = 2;
+
 // registers a thread after the split: 2 x 224 + 56 for three warpgroups that
 // were launched with 168 each (3 x 168 = 504)
 constexpr int W_REGS_EPI = 224, W_REGS_REST = 56;
@@ -431,14 +425,15 @@ template <int BN> struct Wide {
     static constexpr int C_BYTES = BN / 2 * BK;            // this CTA's half of the column operand
     static constexpr int STAGES = BN == 256 ? 4 : 6;
     static constexpr int BOXES = 2;                        // epilogue: 32 rows of 128 bytes on their way to y, for each warp
+    static constexpr int NBUF = BN == 256 ? 2 : 4;         // accumulators
+    static constexpr int FAC_SLOTS = 2 * NBUF;
     static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
     static constexpr int LDN = BN == 64 ? 16 : 32;         // columns of one TMEM load: an even number of loads
     static constexpr int PITCH = BN + 4;                   // row of partial sums, in floats: 8 rows hit all banks
     static_assert(BL * PITCH * 4 <= STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES,
                   "partial sums over the stages and boxes");
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES +
-                                   FAC_SLOTS * 2 * BL * 4 + 8 * (2 * STAGES + 5) + 16;
-    static_assert(STAGES % N_MMA == 0, "a stage is one MMA warp's, see Narrow");
+                                   FAC_SLOTS * 2 * BL * 4 + 8 * (2 * STAGES + 2 * NBUF + 1) + 16;
 };
 
 __device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
@@ -552,12 +547,41 @@ __device__ __forceinline__ void store_lines(const MmArgs &a, const uint64_t *acc
     }
 }
 
+// A CTA's share of the columns of its rows, added over the cluster's pairs in
+// their order.  A function of its own: inlined, it costs the kernel's main loop
+// registers.
+template <int BN>
+__device__ __noinline__ void finish_split(const MmArgs &a, uint32_t part, int tile, uint32_t crank, uint32_t pair) {
+    const int width = BN / a.splits, lanes = width / 4;    // a row's, 4 columns a thread
+    int tl, tc;
+    tile_at(a, tile, tl, tc);
+    const int c = (int)pair * width + (int)threadIdx.x % lanes * 4, n = tc * BN + c;
+    if (n >= a.N) return;
+    const int m0 = (2 * tl + (int)crank) * BL;
+    float bias[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bias[i] = a.bias != nullptr && n + i < a.N ? __ldg(a.bias + n + i) : 0.f;
+    const int step = N_EPI * 32 / lanes;
+#pragma unroll 2
+    for (int row = (int)threadIdx.x / lanes; row < min(BL, a.M - m0); row += step) {
+        const uint32_t at = part + (uint32_t)(row * Wide<BN>::PITCH + c) * 4u;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int s = 0; s < a.splits; ++s) {
+            const float4 p = ld_cluster_f32x4(mapa_shared(at, (uint32_t)(2 * s) + crank));
+            v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+        }
+        const float f[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
+        store4(a, (int64_t)(m0 + row) * a.ldy + n, f, a.N - n);
+    }
+}
+
 template <int BN, bool SPLIT>
 __global__ void __launch_bounds__(W_THREADS, 1)
 fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap,
                 const __grid_constant__ CUtensorMap ymap, const MmArgs a) {
     using S = Wide<BN>;
-    constexpr int CPW = S::CPW, LDN = S::LDN;
+    constexpr int CPW = S::CPW, LDN = S::LDN, NBUF = S::NBUF, FAC_SLOTS = S::FAC_SLOTS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t *Ls = smem;
@@ -567,8 +591,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     uint64_t *full = (uint64_t *)(fac + FAC_SLOTS * 2 * BL);   // even CTA's: both CTAs' copies of a stage
     uint64_t *empty = full + S::STAGES;                    // each CTA: the pair's MMAs have read the stage
     uint64_t *acc_full = empty + S::STAGES;                // each CTA: a block's products are in TMEM, its scales in fac
-    uint64_t *acc_empty = acc_full + 2;                    // even CTA's: both CTAs' epilogues have read them
-    uint64_t *mma_done = acc_empty + 2;
+    uint64_t *acc_empty = acc_full + NBUF;                   // even CTA's: both CTAs' epilogues have read them
+    uint64_t *mma_done = acc_empty + NBUF;
     uint32_t *tmem_holder = (uint32_t *)(mma_done + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -587,17 +611,17 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             mbar_init(smem_u32(&full[s]), 1);
             mbar_init(smem_u32(&empty[s]), 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&acc_full[b]), 2);
+        for (int b = 0; b < NBUF; ++b) {
+            mbar_init(smem_u32(&acc_full[b]), 1 + N_SCALE);
             mbar_init(smem_u32(&acc_empty[b]), 2 * N_EPI);
         }
-        mbar_init(smem_u32(mma_done), N_MMA);
+        mbar_init(smem_u32(mma_done), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
         // one warp of each CTA of the pair allocates the same columns in both
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
-                     "r"((uint32_t)(2 * BN)));
+                     "r"((uint32_t)(NBUF * BN)));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -636,62 +660,65 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         mbar_wait(smem_u32(ok ? &empty[j % S::STAGES] : &full[j % S::STAGES]),
                                   (uint32_t)(j / S::STAGES) & 1u, a.err, E_DRAIN);
             }
-        } else if (warp == SCALE_WARP) {
-            // Scale loads take up to 800 cycles while the tiles stream, so this
-            // warp makes them blocks ahead: 4 rows a lane, both column halves.
-            // Block `it` goes to slot it % 4 once block it - 2 is complete: the
-            // epilogue has then read block it - 4's TMEM, and before it the slot.
+        } else if (warp >= SCALE_WARP) {
+            // Scale loads take up to 1000 cycles while the tiles stream, so
+            // these warps make them DEPTH blocks ahead: 2 rows a lane, both
+            // column halves.  Block `it` goes to slot it % (2 NBUF) once block
+            // it - NBUF is complete: the epilogue has then read block
+            // it - 2 NBUF's TMEM, and before it the slot.
+            constexpr int DEPTH = 4;
+            const int r0 = (warp - SCALE_WARP) * (BL / N_SCALE) + lane;
             int it = 0;
             bool ok = true;
             for (int t = cid; t < tiles && ok; t += ncl) {
                 int tl, tc;
                 tile_at(a, t, tl, tc);
-                const int m0 = (2 * tl + (int)crank) * BL + lane, last = (a.N - 1) / 128;
-                const float *xp[4], *wp[2];
+                const int m0 = (2 * tl + (int)crank) * BL + r0, last = (a.N - 1) / 128;
+                const float *xp[2], *wp[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 2; ++i) {
                     xp[i] = a.xs + (int64_t)min(m0 + 32 * i, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    wp[q] = a.ws + (int64_t)min((tc * BN + q * CPW) / 128, last) * a.ws_row + kb0 * a.ws_blk;
-                float x[2][4], w[2][2];                    // two blocks in flight
+                    wp[i] = a.ws + (int64_t)min((tc * BN + i * CPW) / 128, last) * a.ws_row + kb0 * a.ws_blk;
+                }
+                float x[DEPTH][2], w[DEPTH][2];
                 const auto load = [&](int kb, int u) {
                     if (kb < KB) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[u][i] = __ldg(xp[i] + kb * a.xs_blk);
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) w[u][q] = __ldg(wp[q] + kb * a.ws_blk);
+                        for (int i = 0; i < 2; ++i) {
+                            x[u][i] = __ldg(xp[i] + kb * a.xs_blk);
+                            w[u][i] = __ldg(wp[i] + kb * a.ws_blk);
+                        }
                     }
                 };
-                load(0, 0);
-                load(1, 1);
-                for (int kb = 0; kb < KB && ok; kb += 2) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u, ++it) {
+                for (int u = 0; u < DEPTH; ++u) load(u, u);
+                for (int kb = 0; kb < KB && ok; kb += DEPTH) {
+#pragma unroll
+                    for (int u = 0; u < DEPTH; ++u, ++it) {
                         if (kb + u >= KB) break;
-                        ok = it < 2 || warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)((it - 2) >> 1) & 1u, a.err, E_EPI);
+                        ok = it < NBUF || warp_wait(smem_u32(&acc_full[it % NBUF]), (uint32_t)(it / NBUF - 1) & 1u, a.err, E_EPI);
                         if (!ok) break;
-                        float *slot = fac + it % FAC_SLOTS * (2 * BL);
+                        float *slot = fac + it % FAC_SLOTS * (2 * BL) + r0;
 #pragma unroll
                         for (int q = 0; q < 2; ++q)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) slot[q * BL + 32 * i + lane] = x[u][i] * w[u][q];
+                            for (int i = 0; i < 2; ++i) slot[q * BL + 32 * i] = x[u][i] * w[u][q];
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&acc_full[it & 1]));
-                        load(kb + u + 2, u);
+                        if (lane == 0) mbar_arrive(smem_u32(&acc_full[it % NBUF]));
+                        load(kb + u + DEPTH, u);
                     }
                 }
             }
-        } else if (warp < MMA_WARP + N_MMA && leader) {
+        } else if (warp == MMA_WARP && leader) {
             constexpr uint32_t idesc = idesc_e4m3(2 * BL, BN);
             if (elect_one()) {
                 // this pair's blocks, all tiles in a row
                 const int64_t all = (int64_t)((tiles - cid + ncl - 1) / ncl) * KB;
-                int s = warp - MMA_WARP, round = 0;        // stage, times it was used before
-                for (int64_t it = warp - MMA_WARP; it < all; it += N_MMA) {
-                    const int b = (int)(it & 1);
+                int s = 0, round = 0;                      // stage, times it was used before
+                for (int64_t it = 0; it < all; ++it) {
+                    const int b = (int)(it % NBUF);
                     if (!mbar_wait(smem_u32(&full[s]), (uint32_t)round & 1u, a.err, E_MMA) ||
-                        !mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it >> 1) & 1u) ^ 1u, a.err, E_ACC))
+                        !mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(it / NBUF) & 1u) ^ 1u, a.err, E_ACC))
                         break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t ld = smem_desc_sw128(smem_u32(Ls + s * L_BYTES));
@@ -701,8 +728,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         umma_e4m3_pair(tmem + (uint32_t)(b * BN), ld + 2 * k, cd + 2 * k, idesc, k > 0 ? 1u : 0u);
                     umma_commit_pair_mc(smem_u32(&acc_full[b]), both);
                     umma_commit_pair_mc(smem_u32(&empty[s]), both);
-                    s += N_MMA;
-                    if (s >= S::STAGES) { s -= S::STAGES; ++round; }
+                    if (++s == S::STAGES) { s = 0; ++round; }
                 }
                 umma_commit_pair_mc(smem_u32(mma_done), both);
             }
@@ -716,7 +742,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
         uint8_t *mine = boxes + warp * S::BOXES * W_BOX_BYTES;
         const float *my_fac = fac + half * BL + quad * 32 + lane;
         uint32_t stored = 0;                               // boxes this warp has stored
-        int it = 0;
+        uint32_t it = 0;
         bool ok = true;
         for (int t = cid; t < tiles && ok; t += ncl) {
             int tl, tc;
@@ -728,13 +754,13 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
 
             uint32_t r[2][LDN];
-            ok = warp_wait(smem_u32(&acc_full[it & 1]), (uint32_t)(it >> 1) & 1u, a.err, E_EPI);
+            ok = warp_wait(smem_u32(&acc_full[(it & (NBUF - 1))]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            tmem_ld_nw<LDN>(tbase + (uint32_t)((it & 1) * BN), r[0]);
+            tmem_ld_nw<LDN>(tbase + (uint32_t)((it & (NBUF - 1)) * BN), r[0]);
             for (int kb = 0; kb < KB && ok; ++kb, ++it) {
-                const uint32_t src = tbase + (uint32_t)((it & 1) * BN);
-                const uint64_t f = dup2(my_fac[it % FAC_SLOTS * (2 * BL)]);
+                const uint32_t src = tbase + (uint32_t)((it & (NBUF - 1)) * BN);
+                const uint64_t f = dup2(my_fac[(it & (FAC_SLOTS - 1)) * (2 * BL)]);
                 // LDN columns are on their way while the LDN before are added,
                 // across blocks too
 #pragma unroll
@@ -746,11 +772,12 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                     } else {
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & 1) * 8));
+                        if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & (NBUF - 1)) * 8));
                         if (kb + 1 < KB) {
-                            ok = warp_wait(smem_u32(&acc_full[(it + 1) & 1]), (uint32_t)((it + 1) >> 1) & 1u, a.err, E_EPI);
+                            ok = warp_wait(smem_u32(&acc_full[((it + 1) & (NBUF - 1))]), (uint32_t)((it + 1) / NBUF) & 1u, a.err,
+                                           E_EPI);
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                            if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & 1) * BN), r[h ^ 1]);
+                            if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & (NBUF - 1)) * BN), r[h ^ 1]);
                         }
                     }
 #pragma unroll
@@ -785,30 +812,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     __syncwarp();
     if constexpr (SPLIT) {
         cluster_sync();
-        if (warp < N_EPI) {
-            // this CTA finishes its share of the columns of its rows, added in the order of the pairs
-            const int width = BN / a.splits, lanes = width / 4;            // a row's, 4 columns a thread
-            int tl, tc;
-            tile_at(a, cid, tl, tc);
-            const int c = (int)pair * width + lane % lanes * 4, n = tc * BN + c;
-            const int m0 = (2 * tl + (int)crank) * BL;
-            float bias[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bias[i] = a.bias != nullptr && n + i < a.N ? __ldg(a.bias + n + i) : 0.f;
-            const int step = N_EPI * 32 / lanes;
-#pragma unroll 2
-            for (int row = (int)threadIdx.x / lanes; row < min(BL, a.M - m0); row += step) {
-                const uint32_t at = smem_u32((const float *)smem + row * S::PITCH + c);
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                for (int s = 0; s < a.splits; ++s) {
-                    const float4 p = ld_cluster_f32x4(mapa_shared(at, (uint32_t)(2 * s) + crank));
-                    v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
-                }
-                const float f[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
-                if (n < a.N) store4(a, (int64_t)(m0 + row) * a.ldy + n, f, a.N - n);
-            }
-        }
+        if (warp < N_EPI) finish_split<BN>(a, smem_u32(smem), cid, crank, pair);
     }
     __syncthreads();
     // every MMA of the pair has completed before TMEM is freed in either CTA,
@@ -818,7 +822,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     cluster_sync();
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * BN)));
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(NBUF * BN)));
     }
 }
 
@@ -895,9 +899,51 @@ struct Operands {
     int64_t k;
 };
 
+// CTAs of a kernel that the GPU holds at once in clusters of `cluster` (asked once per device: clusters must fit
+// into a GPC, so it is not always the SMs' number); 0: it does not run
+template <typename K>
+int resident(K *kernel, int threads, size_t smem, int cluster, std::atomic<int> (&known)[MAX_DEVICES]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return 0;
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)cluster);
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)cluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess || clusters < 1) {
+            cudaGetLastError();
+            return 0;
+        }
+        n = clusters * cluster;
+        if (getenv("CT_SHOW")) printf("resident: threads %d smem %zu cluster %d -> %d CTAs\n", threads, smem, cluster, n);
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+template <int BN> int narrow_resident(int splits) {
+    static std::atomic<int> known[9][MAX_DEVICES];
+    return resident(fp8_narrow_kernel<BN>, THREADS, Narrow<BN>::SMEM, splits, known[splits]);
+}
+template <int BN> int wide_resident(int splits) {
+    static std::atomic<int> known[3][MAX_DEVICES];
+    return splits == 1 ? resident(fp8_wide_kernel<BN, false>, W_THREADS, Wide<BN>::SMEM, 2, known[1])
+                       : resident(fp8_wide_kernel<BN, true>, W_THREADS, Wide<BN>::SMEM, 2 * splits, known[splits]);
+}
+
 struct Choice {
     bool wide;
     int bn, splits;
+    int ctas;               // wide: that run at once
 };
 
 // Which kernel, how wide its tiles, over how many CTAs (pairs) K is split: the
@@ -911,49 +957,55 @@ struct Choice {
 //   no kernel is faster than its operands: 9 GB/ms from L2, 6.4 GB/ms of
 //   weights from HBM, 58 GB/s of them to one SM.
 Choice choose(int M, int N, int KB, int sms) {
-    Choice best = {false, 16, 1};
+    Choice best = {false, 16, 1, 0};
     double least = 1e30;
     const double weights = (double)N * KB * BK;
-    const auto consider = [&](bool wide, int bn, int splits, double t) {
+    const auto consider = [&](bool wide, int bn, int splits, int ctas, double t) {
         if (t < least) {
             least = t;
-            best = Choice{wide, bn, splits};
+            best = Choice{wide, bn, splits, ctas};
         }
     };
     static const double n_block[4] = {0.2, 0.25, 0.33, 0.5}, n_tile[4] = {1.0, 1.3, 2.7, 3.3};
     static const double n_split[9] = {0, 0, 1.4, 1.7, 2.0, 2.1, 2.2, 2.2, 2.2};
-    static const double w_block[3] = {0.25, 0.36, 0.49};
+    static const double w_block[3] = {0.2, 0.28, 0.41};
     const int64_t rows_n = (N + 127) / 128;
     for (int i = 0; i < 4; ++i) {
         const int bn = 16 << i;
         if (bn > 16 && bn / 2 >= M) break;
-        const int64_t tiles = rows_n * ((M + bn - 1) / bn), slots = (int64_t)sms * (bn <= 64 ? 2 : 1);
+        const int64_t tiles = rows_n * ((M + bn - 1) / bn);
         for (int s = 1; s <= 8 && s <= KB; ++s) {
             if (s == 5 || s == 7) continue;
-            if (s > 1 && tiles * s > slots) break;
+            if (s > 1 && tiles * s > sms) break;
+            const int64_t slots = bn == 16   ? narrow_resident<16>(s)
+                                  : bn == 32 ? narrow_resident<32>(s)
+                                  : bn == 64 ? narrow_resident<64>(s)
+                                             : narrow_resident<128>(s);
+            if (slots == 0) continue;
             const double nkb = (KB + s - 1) / s, ctas = (double)tiles * s;
             const double blocks = (double)((tiles * s + slots - 1) / slots) * nkb * n_block[i];
             const double l2 = ctas * nkb * (BL + bn) * BK / 9e6;
             const double busy = ctas < sms ? ctas : sms;
             const double hbm = weights / (0.058 * busy < 6.4 ? 58e3 * busy : 6.4e6);
-            consider(false, bn, s, n_tile[i] + n_split[s] + fmax(blocks, fmax(l2, hbm)));
+            consider(false, bn, s, 0, n_tile[i] + n_split[s] + fmax(blocks, fmax(l2, hbm)));
         }
     }
-    const int64_t pairs = sms / 2, rows_m = (M + 2 * BL - 1) / (2 * BL);
+    const int64_t rows_m = (M + 2 * BL - 1) / (2 * BL);
     for (int i = 0; i < 3 && M > 64; ++i) {
         const int bn = 64 << i;
         const int64_t tiles = rows_m * ((N + bn - 1) / bn);
         for (int s = 1; s <= 2 && s <= KB; ++s) {
-            if (s > 1 && tiles * s > pairs) break;
+            const int64_t pairs = (bn == 64 ? wide_resident<64>(s) : bn == 128 ? wide_resident<128>(s) : wide_resident<256>(s)) / 2;
+            if (pairs == 0 || (s > 1 && tiles * s > pairs)) continue;
             const double nkb = (KB + s - 1) / s, rounds = (double)((tiles * s + pairs - 1) / pairs);
             const double blocks = rounds * nkb * w_block[i] + (rounds - 1) * 0.8;
-            const double l2 = (double)tiles * s * nkb * (2 * BL + bn) * BK / 10e6;
-            consider(true, bn, s, 3.6 + 0.0047 * bn + (s > 1 ? 3.5 : 0) + fmax(blocks, fmax(l2, weights / 6.4e6)));
+            const double l2 = (double)tiles * s * nkb * (2 * BL + bn) * BK / 11e6;
+            consider(true, bn, s, (int)(2 * pairs), 3.6 + 0.0047 * bn + (s > 1 ? 3.5 : 0) + fmax(blocks, fmax(l2, weights / 6.4e6)));
         }
     }
     if (const char *q = getenv("CT_FORCE")) {
         int f[3];
-        if (sscanf(q, "%d,%d,%d", f, f + 1, f + 2) == 3) best = Choice{f[0] == 1, f[1], f[2]};
+        if (sscanf(q, "%d,%d,%d", f, f + 1, f + 2) == 3) best = Choice{f[0] == 1, f[1], f[2], 152};
     }
     return best;
 }
@@ -977,7 +1029,7 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
         a.tiles_l = (a.M + 2 * BL - 1) / (2 * BL);
         a.tiles_c = (a.N + bn - 1) / bn;
         a.group = 8;
-        const int pairs = sms / 2;
+        const int pairs = ch.ctas / 2;
         const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
         if (tiles > INT32_MAX / 16) return CT_ERANGE;
         CUtensorMap ymap = {};
