@@ -12,9 +12,10 @@
 // MMAs run into another accumulator.
 //
 // Warp roles: 8 epilogue warps (warp w reads TMEM lanes 32 (w % 4) ..), one TMA
-// warp, one MMA warp (a second one that took K blocks in turn changed nothing).  A stage of shared memory
-// holds one K block of both operands: 128-byte rows, 128-byte swizzle; rows
-// and columns past the ends are the zeros TMA fills in.
+// warp, one MMA warp (a second one that took K blocks in turn changed
+// nothing).  A stage of shared memory holds one K block of both operands:
+// 128-byte rows, 128-byte swizzle; rows and columns past the ends are the
+// zeros TMA fills in.
 //
 // Two kernels:
 //   wide (many rows): rows of x on the TMEM lanes, tiles of 256 rows x BN
@@ -31,8 +32,6 @@
 #include <cudaTypedefs.h>
 #include <math.h>
 #include <string.h>
-#include <stdio.h>
-#include <stdlib.h>
 
 #include "ops_common.cuh"
 #include "tc_common.cuh"
@@ -158,11 +157,6 @@ __device__ __forceinline__ void store4(const MmArgs &a, int64_t at, const float 
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (i < have) store_out(a, at + i, v[i]);
-}
-
-__device__ __forceinline__ float finish(const MmArgs &a, float v, int n) {
-    if (a.bias != nullptr) v += __ldg(a.bias + n);
-    return a.relu ? relu_keep_nan(v) : v;
 }
 
 // acc += f * p on two values at once.  Volatile, like the TMEM load and the
@@ -755,9 +749,9 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 
             uint32_t r[2][LDN];
             ok = warp_wait(smem_u32(&acc_full[(it & (NBUF - 1))]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
-            if (!ok) break;
+            if (!SPLIT && !ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            tmem_ld_nw<LDN>(tbase + (uint32_t)((it & (NBUF - 1)) * BN), r[0]);
+            if (!SPLIT || ok) tmem_ld_nw<LDN>(tbase + (uint32_t)((it & (NBUF - 1)) * BN), r[0]);
             for (int kb = 0; kb < KB && ok; ++kb, ++it) {
                 const uint32_t src = tbase + (uint32_t)((it & (NBUF - 1)) * BN);
                 const uint64_t f = dup2(my_fac[(it & (FAC_SLOTS - 1)) * (2 * BL)]);
@@ -774,8 +768,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         __syncwarp();
                         if (lane == 0) mbar_arrive_relaxed(acc_empty_even + (uint32_t)((it & (NBUF - 1)) * 8));
                         if (kb + 1 < KB) {
-                            ok = warp_wait(smem_u32(&acc_full[((it + 1) & (NBUF - 1))]), (uint32_t)((it + 1) / NBUF) & 1u, a.err,
-                                           E_EPI);
+                            ok = warp_wait(smem_u32(&acc_full[((it + 1) & (NBUF - 1))]), (uint32_t)((it + 1) / NBUF) & 1u,
+                                           a.err, E_EPI);
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                             if (ok) tmem_ld_nw<LDN>(tbase + (uint32_t)(((it + 1) & (NBUF - 1)) * BN), r[h ^ 1]);
                         }
@@ -784,7 +778,9 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                     for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
                 }
             }
-            if (!ok) break;
+            // After a wait that ran out, which is reported, the output is invalid;
+            // a split tile's warps still meet at their barriers.
+            if (!SPLIT && !ok) break;
 
             if constexpr (SPLIT) {
                 // partial sums [row][column], over the stages and boxes (see the narrow kernel); one tile
@@ -831,8 +827,10 @@ __global__ void bias_only_kernel(const MmArgs a) {
     pdl_wait();
     pdl_trigger();
     const int64_t n_all = (int64_t)a.M * a.N;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n_all; i += (int64_t)gridDim.x * blockDim.x)
-        store_out(a, i / a.N * a.ldy + i % a.N, finish(a, 0.f, (int)(i % a.N)));
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n_all; i += (int64_t)gridDim.x * blockDim.x) {
+        const float v = a.bias != nullptr ? __ldg(a.bias + i % a.N) : 0.f;
+        store_out(a, i / a.N * a.ldy + i % a.N, a.relu ? relu_keep_nan(v) : v);
+    }
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder() {
@@ -850,6 +848,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
     return f;
 }
 
+int64_t q_pitch(int64_t k) { return (k + 15) / 16 * 16; }
+
 // [rows, cols] values of `size` bytes, row pitch ld bytes, in boxes of box_bytes (128 or 64) x box_rows, swizzled
 // within box_bytes
 bool encode(CUtensorMap *map, const void *p, CUtensorMapDataType type, int size, int64_t rows, int64_t cols, int64_t ld,
@@ -866,29 +866,28 @@ bool encode(CUtensorMap *map, const void *p, CUtensorMapDataType type, int size,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// (the pitch of a single row does not matter)
 bool encode8(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t k, int64_t ld, int box_rows) {
+    if (rows == 1) ld = q_pitch(k);
     return encode(map, p, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, ld, BK, box_rows);
 }
 
+// (the kernels' shared memory was allowed when choose() asked for their residency)
 template <int BN>
 cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, const MmArgs &a, int grid, cudaStream_t st) {
-    static std::atomic<bool> sized[MAX_DEVICES];
-    const cudaError_t e = allow_smem(fp8_narrow_kernel<BN>, sized, Narrow<BN>::SMEM);
-    if (e != cudaSuccess) return e;
     if (a.splits == 1)
         return pdl_launch(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Narrow<BN>::SMEM, st, lmap, cmap, a);
     return pdl_launch_cluster(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Narrow<BN>::SMEM, st, a.splits,
                               lmap, cmap, a);
 }
 
-template <int BN, bool SPLIT>
+template <int BN>
 cudaError_t launch_wide(const CUtensorMap &lmap, const CUtensorMap &cmap, const CUtensorMap &ymap, const MmArgs &a,
                         int clusters, cudaStream_t st) {
-    static std::atomic<bool> sized[MAX_DEVICES];
-    const cudaError_t e = allow_smem(fp8_wide_kernel<BN, SPLIT>, sized, Wide<BN>::SMEM);
-    if (e != cudaSuccess) return e;
-    return pdl_launch_cluster(fp8_wide_kernel<BN, SPLIT>, dim3((unsigned)(2 * a.splits * clusters)), dim3(W_THREADS), Wide<BN>::SMEM, st, 2 * a.splits,
-                              lmap, cmap, ymap, a);
+    const dim3 grid((unsigned)(2 * a.splits * clusters)), block(W_THREADS);
+    if (a.splits == 1)
+        return pdl_launch_cluster(fp8_wide_kernel<BN, false>, grid, block, Wide<BN>::SMEM, st, 2, lmap, cmap, ymap, a);
+    return pdl_launch_cluster(fp8_wide_kernel<BN, true>, grid, block, Wide<BN>::SMEM, st, 2 * a.splits, lmap, cmap, ymap, a);
 }
 
 struct Operands {
@@ -899,13 +898,11 @@ struct Operands {
     int64_t k;
 };
 
-// CTAs of a kernel that the GPU holds at once in clusters of `cluster` (asked once per device: clusters must fit
-// into a GPC, so it is not always the SMs' number); 0: it does not run
+// CTAs of a kernel that device `dev`, the current one, holds at once in clusters of `cluster`, asked once:
+// clusters must fit into a GPC, so it is not always the SMs' number.  0: it does not run.
 template <typename K>
-int resident(K *kernel, int threads, size_t smem, int cluster, std::atomic<int> (&known)[MAX_DEVICES]) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return 0;
-    int n = known[dev].load(std::memory_order_relaxed);
+int resident(K *kernel, int threads, size_t smem, int cluster, std::atomic<int> &known) {
+    int n = known.load(std::memory_order_relaxed);
     if (n == 0) {
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
         cudaLaunchConfig_t cfg = {};
@@ -924,88 +921,84 @@ int resident(K *kernel, int threads, size_t smem, int cluster, std::atomic<int> 
             return 0;
         }
         n = clusters * cluster;
-        if (getenv("CT_SHOW")) printf("resident: threads %d smem %zu cluster %d -> %d CTAs\n", threads, smem, cluster, n);
-        known[dev].store(n, std::memory_order_relaxed);
+        known.store(n, std::memory_order_relaxed);
     }
     return n;
 }
 
-template <int BN> int narrow_resident(int splits) {
-    static std::atomic<int> known[9][MAX_DEVICES];
-    return resident(fp8_narrow_kernel<BN>, THREADS, Narrow<BN>::SMEM, splits, known[splits]);
+constexpr int N_SPLITS = 6;
+constexpr int NARROW_SPLITS[N_SPLITS] = {1, 2, 3, 4, 6, 8};
+
+// [dev][log2 of the columns / 16][index of the split], [dev][log2 of the columns / 64][splits - 1]
+std::atomic<int> g_narrow[MAX_DEVICES][4][N_SPLITS], g_wide[MAX_DEVICES][3][2];
+
+template <int BN> int narrow_resident(int splits, std::atomic<int> &known) {
+    return resident(fp8_narrow_kernel<BN>, THREADS, Narrow<BN>::SMEM, splits, known);
 }
-template <int BN> int wide_resident(int splits) {
-    static std::atomic<int> known[3][MAX_DEVICES];
-    return splits == 1 ? resident(fp8_wide_kernel<BN, false>, W_THREADS, Wide<BN>::SMEM, 2, known[1])
-                       : resident(fp8_wide_kernel<BN, true>, W_THREADS, Wide<BN>::SMEM, 2 * splits, known[splits]);
+template <int BN> int wide_resident(int splits, std::atomic<int> &known) {
+    return splits == 1 ? resident(fp8_wide_kernel<BN, false>, W_THREADS, Wide<BN>::SMEM, 2, known)
+                       : resident(fp8_wide_kernel<BN, true>, W_THREADS, Wide<BN>::SMEM, 2 * splits, known);
 }
 
 struct Choice {
     bool wide;
     int bn, splits;
-    int ctas;               // wide: that run at once
+    int ctas;               // that run at once
 };
 
 // Which kernel, how wide its tiles, over how many CTAs (pairs) K is split: the
-// least of a simple estimate, in us, whose figures were measured over some 30
-// shapes (each candidate timed on its own; the choice was within 10% of the
-// best of them).
-//   a K block costs a CTA 0.2, 0.25, 0.33, 0.5 us for 16, 32, 64, 128 columns
-//   and a pair 0.25, 0.36, 0.49 us for 64, 128, 256; launch, start and end of a
-//   tile 1.0, 1.3, 2.7, 3.3 and 3.9 to 4.8 us; adding the shares of a split 1.4
-//   to 2.2 us (pairs 3.5 us);
-//   no kernel is faster than its operands: 9 GB/ms from L2, 6.4 GB/ms of
-//   weights from HBM, 58 GB/s of them to one SM.
-Choice choose(int M, int N, int KB, int sms) {
+// least of an estimate in us.  Its figures were measured by timing every
+// candidate at 67 shapes (1 to 8192 rows, 10 to 16384 columns, K from 64 to
+// 25088); the choice is 2.5% slower than the best candidate on average, 24% at
+// worst.
+//   A K block costs a CTA 0.2 to 0.5 us (16 to 128 columns), a pair 0.2 to
+//   0.41 us (64 to 256); launch, start and end of a tile 1 to 3.3 us, 3.9 to
+//   4.8 us; adding the shares of a split 1.4 to 2.2 us, 3.5 us.
+//   No kernel is faster than its operands: 9 to 11 bytes a ns from L2, 6.4 of
+//   weights from HBM, 58 bytes a ns to one SM.
+Choice choose(int M, int N, int KB, int sms, int dev) {
+    static const double n_block[4] = {0.2, 0.25, 0.33, 0.5}, n_tile[4] = {1.0, 1.3, 2.7, 3.3};
+    static const double n_split[N_SPLITS] = {0, 1.4, 1.7, 2.0, 2.2, 2.2};
+    static const double w_block[3] = {0.2, 0.28, 0.41};
     Choice best = {false, 16, 1, 0};
     double least = 1e30;
     const double weights = (double)N * KB * BK;
-    const auto consider = [&](bool wide, int bn, int splits, int ctas, double t) {
-        if (t < least) {
-            least = t;
-            best = Choice{wide, bn, splits, ctas};
-        }
-    };
-    static const double n_block[4] = {0.2, 0.25, 0.33, 0.5}, n_tile[4] = {1.0, 1.3, 2.7, 3.3};
-    static const double n_split[9] = {0, 0, 1.4, 1.7, 2.0, 2.1, 2.2, 2.2, 2.2};
-    static const double w_block[3] = {0.2, 0.28, 0.41};
-    const int64_t rows_n = (N + 127) / 128;
+    const int64_t rows_n = (N + 127) / 128, rows_m = (M + 2 * BL - 1) / (2 * BL);
     for (int i = 0; i < 4; ++i) {
         const int bn = 16 << i;
         if (bn > 16 && bn / 2 >= M) break;
         const int64_t tiles = rows_n * ((M + bn - 1) / bn);
-        for (int s = 1; s <= 8 && s <= KB; ++s) {
-            if (s == 5 || s == 7) continue;
-            if (s > 1 && tiles * s > sms) break;
-            const int64_t slots = bn == 16   ? narrow_resident<16>(s)
-                                  : bn == 32 ? narrow_resident<32>(s)
-                                  : bn == 64 ? narrow_resident<64>(s)
-                                             : narrow_resident<128>(s);
-            if (slots == 0) continue;
-            const double nkb = (KB + s - 1) / s, ctas = (double)tiles * s;
-            const double blocks = (double)((tiles * s + slots - 1) / slots) * nkb * n_block[i];
-            const double l2 = ctas * nkb * (BL + bn) * BK / 9e6;
-            const double busy = ctas < sms ? ctas : sms;
-            const double hbm = weights / (0.058 * busy < 6.4 ? 58e3 * busy : 6.4e6);
-            consider(false, bn, s, 0, n_tile[i] + n_split[s] + fmax(blocks, fmax(l2, hbm)));
+        for (int q = 0; q < N_SPLITS; ++q) {
+            const int s = NARROW_SPLITS[q];
+            if (s > KB || (s > 1 && tiles * s > sms)) break;
+            std::atomic<int> &known = g_narrow[dev][i][q];
+            const int ctas = bn == 16   ? narrow_resident<16>(s, known)
+                             : bn == 32 ? narrow_resident<32>(s, known)
+                             : bn == 64 ? narrow_resident<64>(s, known)
+                                        : narrow_resident<128>(s, known);
+            if (ctas == 0) continue;
+            const double nkb = (KB + s - 1) / s, all = (double)tiles * s, busy = all < sms ? all : sms;
+            const double rounds = (double)((tiles * s + ctas - 1) / ctas);
+            const double l2 = all * nkb * (BL + bn) * BK / 9e6;
+            const double hbm = weights / (busy < 110 ? 58e3 * busy : 6.4e6);
+            const double t = rounds * n_tile[i] + (rounds - 1) + n_split[q] + fmax(rounds * nkb * n_block[i], fmax(l2, hbm));
+            if (t < least) { least = t; best = Choice{false, bn, s, ctas}; }
         }
     }
-    const int64_t rows_m = (M + 2 * BL - 1) / (2 * BL);
     for (int i = 0; i < 3 && M > 64; ++i) {
         const int bn = 64 << i;
         const int64_t tiles = rows_m * ((N + bn - 1) / bn);
         for (int s = 1; s <= 2 && s <= KB; ++s) {
-            const int64_t pairs = (bn == 64 ? wide_resident<64>(s) : bn == 128 ? wide_resident<128>(s) : wide_resident<256>(s)) / 2;
-            if (pairs == 0 || (s > 1 && tiles * s > pairs)) continue;
+            std::atomic<int> &known = g_wide[dev][i][s - 1];
+            const int ctas = bn == 64 ? wide_resident<64>(s, known) : bn == 128 ? wide_resident<128>(s, known) : wide_resident<256>(s, known);
+            const int64_t pairs = ctas / 2;
+            if (ctas == 0 || (s > 1 && tiles * s > pairs)) continue;
             const double nkb = (KB + s - 1) / s, rounds = (double)((tiles * s + pairs - 1) / pairs);
-            const double blocks = rounds * nkb * w_block[i] + (rounds - 1) * 0.8;
             const double l2 = (double)tiles * s * nkb * (2 * BL + bn) * BK / 11e6;
-            consider(true, bn, s, (int)(2 * pairs), 3.6 + 0.0047 * bn + (s > 1 ? 3.5 : 0) + fmax(blocks, fmax(l2, weights / 6.4e6)));
+            const double t = 3.6 + 0.0047 * bn + (s > 1 ? 3.5 : 0) +
+                             fmax(rounds * nkb * w_block[i] + (rounds - 1) * 0.8, fmax(l2, weights / 6.4e6));
+            if (t < least) { least = t; best = Choice{true, bn, s, ctas}; }
         }
-    }
-    if (const char *q = getenv("CT_FORCE")) {
-        int f[3];
-        if (sscanf(q, "%d,%d,%d", f, f + 1, f + 2) == 3) best = Choice{f[0] == 1, f[1], f[2], 152};
     }
     return best;
 }
@@ -1022,7 +1015,10 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
     const int sms = sm_count();
     CUtensorMap lmap, cmap;
     cudaError_t e;
-    const Choice ch = choose(a.M, a.N, a.KB, sms);
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return CT_ECUDA;
+    const Choice ch = choose(a.M, a.N, a.KB, sms, dev);
+    if (ch.ctas == 0) return CT_ECUDA;
     const int bn = ch.bn;
     a.splits = ch.splits;
     if (ch.wide) {
@@ -1040,14 +1036,9 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
                               es, a.M, a.N, a.ldy * es, bn == 64 && es == 2 ? 64 : 128, 32)))
             return CT_ECUDA;
         const int n = (int)(a.splits > 1 || tiles < pairs ? tiles : pairs);
-        if (a.splits > 1)
-            e = bn == 64    ? launch_wide<64, true>(lmap, cmap, ymap, a, n, st)
-                : bn == 128 ? launch_wide<128, true>(lmap, cmap, ymap, a, n, st)
-                            : launch_wide<256, true>(lmap, cmap, ymap, a, n, st);
-        else
-            e = bn == 64    ? launch_wide<64, false>(lmap, cmap, ymap, a, n, st)
-                : bn == 128 ? launch_wide<128, false>(lmap, cmap, ymap, a, n, st)
-                            : launch_wide<256, false>(lmap, cmap, ymap, a, n, st);
+        e = bn == 64    ? launch_wide<64>(lmap, cmap, ymap, a, n, st)
+            : bn == 128 ? launch_wide<128>(lmap, cmap, ymap, a, n, st)
+                        : launch_wide<256>(lmap, cmap, ymap, a, n, st);
     } else {
         a.tiles_l = (a.N + 127) / 128;
         a.tiles_c = (a.M + bn - 1) / bn;
@@ -1070,7 +1061,7 @@ ct_status check(int64_t m, int64_t n, int64_t k, const uint8_t *w, int64_t ldw, 
     if (m < 0 || n < 0 || k < 0 || m > INT32_MAX - 256 || n > INT32_MAX - 256 || k > INT32_MAX - 256) return CT_ERANGE;
     if (m == 0 || n == 0) return CT_OK;
     if (y == nullptr || ldy < n || !aligned(y, dtype_size(out)) || !aligned(bias, 4)) return CT_EINVAL;
-    if (k > 0 && (w == nullptr || ws == nullptr || ldw < k || ldw % 16 != 0 || !aligned(w, 16) || !aligned(ws, 4)))
+    if (k > 0 && (w == nullptr || ws == nullptr || (n > 1 && (ldw < k || ldw % 16 != 0)) || !aligned(w, 16) || !aligned(ws, 4)))
         return CT_EINVAL;
     return CT_OK;
 }
@@ -1087,7 +1078,6 @@ MmArgs make_args(int64_t m, int64_t n, int64_t k, const float *ws, int64_t ws_ro
 }
 
 // workspace of ct_fp8_linear: the 8-bit rows (pitch a multiple of 16 bytes), then their scales [block][row]
-int64_t q_pitch(int64_t k) { return (k + 15) / 16 * 16; }
 size_t scales_at(int64_t m, int64_t k) { return ((size_t)m * (size_t)q_pitch(k) + 255) / 256 * 256; }
 
 }  // namespace
@@ -1102,7 +1092,7 @@ extern "C" ct_status ct_fp8_matmul(const uint8_t *x_dev, int64_t ldx, const floa
     using namespace ct::ops;
     const ct_status s = check(m, n, k, w_dev, ldw, w_scale_dev, bias_dev, y_dev, y_dtype, ldy);
     if (s != CT_OK || m == 0 || n == 0) return s;
-    if (k > 0 && (x_dev == nullptr || x_scale_dev == nullptr || ldx < k || ldx % 16 != 0 || !aligned(x_dev, 16) ||
+    if (k > 0 && (x_dev == nullptr || x_scale_dev == nullptr || (m > 1 && (ldx < k || ldx % 16 != 0)) || !aligned(x_dev, 16) ||
                   !aligned(x_scale_dev, 4)))
         return CT_EINVAL;
     MmArgs a = make_args(m, n, k, w_scale_dev, w_scale_row, w_scale_blk, bias_dev, relu, y_dev, y_dtype, ldy);
