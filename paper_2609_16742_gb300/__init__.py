@@ -12,6 +12,7 @@ and there is no fallback: if ``_lib/libct.so`` is missing, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -635,6 +636,13 @@ def ct_fp8_matmul(xq, xs, wq, ws, bias=None, relu: bool = False, out_dtype=None,
     return y
 
 
+@functools.lru_cache(maxsize=256)
+def _linear_workspace(m, k):
+    need = ctypes.c_size_t()
+    _check(lib().ct_fp8_linear_workspace(m, k, ctypes.byref(need)), "ct_fp8_linear_workspace")
+    return need.value
+
+
 def ct_fp8_linear(x, wq, ws, bias=None, relu: bool = False, out_dtype=None, out=None, stream=None):
     """act(x W^T + bias) with 8-bit weights on float32 / float16 / bfloat16
     activations x [m, k], quantised on the way (1 x 128 blocks).  out_dtype: x's
@@ -647,13 +655,10 @@ def ct_fp8_linear(x, wq, ws, bias=None, relu: bool = False, out_dtype=None, out=
     n, w = _fp8_weights(wq, ws, k, dev)
     b = None if bias is None else _vector(bias, "bias", T.f32, n, dev)
     y, code, ldy = _fp8_out(out, x.dtype if out is None and out_dtype is None else out_dtype, m, n, dev)
-    L = _lib or lib()
-    need = ctypes.c_size_t()
-    st = L.ct_fp8_linear_workspace(m, k, need)
-    if not st:
-        work = T.empty(need.value, dtype=T.u8, device=dev)
-        st = L.ct_fp8_linear(x.data_ptr(), T.dtypes[x.dtype], ldx, *w, b, 1 if relu else 0, y.data_ptr(), code, ldy, m, n, k,
-                             work.data_ptr(), need.value, T.raw_stream(dev.index))
+    need = _linear_workspace(m, k)
+    work = T.empty(need, dtype=T.u8, device=dev)
+    st = (_lib or lib()).ct_fp8_linear(x.data_ptr(), T.dtypes[x.dtype], ldx, *w, b, 1 if relu else 0, y.data_ptr(), code, ldy,
+                                       m, n, k, work.data_ptr(), need, T.raw_stream(dev.index))
     if st:
         raise CtError(st, "ct_fp8_linear")
     return y

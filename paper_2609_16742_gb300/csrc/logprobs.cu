@@ -788,6 +788,7 @@ template <typename T, int NT> struct Long : Top<T, NT> {
         uint64_t full[STAGES], empty[STAGES];
         uint64_t left_full[FIN], left_free[FIN];
         typename P::Scratch scratch[FIN];
+        uint64_t join[CT_MAX_TOP_K];
         Left left[FIN];
         Stat total;
     };
@@ -958,26 +959,37 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
     }
     __syncwarp();
     if (splits > 1) {
-        // one row for each cluster: rank 0's first finisher joins the shares, in rank order
+        // one row for each cluster: rank 0's consumer threads join the shares, in rank order
         tc::cluster_sync();
-        if (rank == 0 && warp == NT / 32 + 1) {
-            Stat st = sh.total;
-            for (int p = 1; p < splits; ++p) {
+        if (rank == 0 && tid < NT) {
+            const auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); };
+            int64_t id = -1;
+            const float given = tid == 0 ? given_logit<T>(a, cid, id) : 0.f;
+            Stat st = {-INF, 0.f, 0.f};
+            for (int p = 0; p < splits; ++p) {
                 const uint32_t at = tc::mapa_shared(tc::smem_u32(&sh.total), (uint32_t)p);
                 st = merge(st, Stat{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)});
             }
             const RowResult q = row_result(st);
-            int64_t id = -1;
-            if (lane == 0) {
-                const float given = given_logit<T>(a, cid, id);
-                write_row(a, cid, q, id, given);
-            }
+            if (tid == 0) write_row(a, cid, q, id, given);
             if (k > 0) {
-                for (int i = lane; i < splits * k; i += 32)
-                    sh.scratch[0].cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[i % k]), (uint32_t)(i / k)));
-                __syncwarp();
-                L::select(sh.scratch[0], splits * k, k);
-                if (lane < k) write_top(a, cid, lane, sh.scratch[0].best[lane], q);
+                // splits * k <= CAP keys, several to a thread: a key's place is the number of larger ones
+                const int n = splits * k;
+                uint64_t *cand = sh.scratch[0].cand;
+                for (int i = tid; i < n; i += NT)
+                    cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[i % k]), (uint32_t)(i / k)));
+                sync();
+                if (tid < k) sh.join[tid] = 0;
+                sync();
+                for (int i = tid; i < n; i += NT) {
+                    const uint64_t key = cand[i];
+                    int place = 0;
+#pragma unroll 8
+                    for (int j = 0; j < n; ++j) place += cand[j] > key;
+                    if (key != 0 && place < k) sh.join[place] = key;
+                }
+                sync();
+                if (tid < k) write_top(a, cid, tid, sh.join[tid], q);
             }
         }
         tc::cluster_sync();
