@@ -314,3 +314,25 @@ def test_refusals():
             bad()
         assert ei.value.status == 1
     assert c.ct_ops_device_error() == 0
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 bytes of activations and of results: the rows at the end
+    are the same as those rows alone."""
+    torch = torch_()
+    c = ct()
+    m, n, k = 140000, 16400, 16000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.zeros(m, k, dtype=torch.bfloat16, device="cuda")
+    x[-40:] = torch.randn(40, k, device="cuda", generator=g).bfloat16()
+    q, s = c.ct_fp8_quantize(x)
+    del x
+    ql, sl = q[-40:].clone(), s[-40:].clone()
+    w, ws = c.ct_fp8_quantize(torch.randn(n, k, device="cuda", generator=g), 128)
+    y = c.ct_fp8_matmul(q, s, w, ws, out_dtype=torch.bfloat16)
+    assert c.ct_ops_device_error() == 0
+    assert q.numel() > 2 ** 31 and y.numel() > 2 ** 31
+    assert (y[:-40] == 0).all()
+    xv = ql.float().cpu().numpy().astype(np.float64) * _ops.widen(sl.double().cpu().numpy(), 1, 40, k)
+    wv = w.float().cpu().numpy().astype(np.float64) * _ops.widen(ws.double().cpu().numpy(), 128, n, k)
+    check_product(y[-40:], "bfloat16", xv, wv, None, False, (k + 127) // 128)

@@ -274,3 +274,21 @@ def test_refusals():
                 lambda: c.ct_logprobs_grad(x, ids, v, None, None, v), lambda: c.ct_logprobs_grad(x, ids, v, v, v, out=x.half())):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 bytes of logits: the last rows are the same as those rows alone."""
+    torch = torch_()
+    rows, vocab = 24000, 131077
+    x = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+    x[-300:] = torch.randn(300, vocab, device="cuda").bfloat16() * 3
+    assert x.numel() > 2 ** 31
+    ids = torch.full((rows,), 131076, device="cuda")
+    got = ct().ct_logprobs(x, ids, 5)
+    want = check_forward(x[-7:].clone(), ids[-7:].cpu().numpy(), 5)
+    np.testing.assert_array_equal(got[4][-7:].cpu().numpy(), want[4])
+    for a, b in zip(got[:4], want[:4]):
+        np.testing.assert_allclose(a[-7:].cpu().numpy(), b, rtol=0, atol=1e-4)
+    one = torch.ones(rows, device="cuda")
+    d = ct().ct_logprobs_grad(x, ids, got[2], got[1], one, one, out=x)
+    assert torch.isfinite(d[-300:].float()).all() and (d[-300:, -1] > 0).all() and (d[:3, 0] < 0).all()
