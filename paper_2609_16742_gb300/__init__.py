@@ -595,9 +595,7 @@ def ct_fp8_quantize(x, block_rows: int = 1, q=None, scale=None, stream=None):
     rows, kb = (m + block_rows - 1) // block_rows, (k + 127) // 128
     if q is None:
         ldq = (k + 15) // 16 * 16
-        q = T.empty((m, ldq), dtype=T.e4m3, device=dev)
-        if ldq != k:
-            q = q[:, :k]
+        q = T.empty_strided((m, k), (ldq, 1), dtype=T.e4m3, device=dev)
     else:
         ldq = _matrix(q, "q", T.bytes, (m, k), dev)[2]
     if scale is not None:

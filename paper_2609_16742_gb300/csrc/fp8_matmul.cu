@@ -534,8 +534,14 @@ __device__ __forceinline__ void store_lines(const MmArgs &a, const uint64_t *acc
         __syncwarp();
         if (c0 + c + lane < a.N) {
             O *y = static_cast<O *>(a.y) + (int64_t)m_warp * a.ldy + c0 + c + lane;
-#pragma unroll 4
-            for (int q = 0; q < rows; ++q, y += a.ldy) *y = from_f32<O>(sq[q * 32 + (lane ^ q)]);
+            for (int q = 0; q < rows; q += 8) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = sq[(q + i) * 32 + (lane ^ (q + i))];
+#pragma unroll
+                for (int i = 0; i < 8; ++i, y += a.ldy)
+                    if (q + i < rows) *y = from_f32<O>(v[i]);
+            }
         }
         __syncwarp();
     }
