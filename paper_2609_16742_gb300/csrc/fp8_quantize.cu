@@ -50,13 +50,14 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi, float inv) {
     return r;
 }
 
-// the V values of row `row` from column c0 on: 16 bytes at once (vec), or one
-// by one with zeros past the end
+// the V values of row `row` from column c0 on, wherever they start; zeros past
+// the end of the row
 template <typename T, int V>
-__device__ __forceinline__ void load_values(const QuantArgs &a, int64_t row, int64_t c0, bool vec, uint4 &u) {
+__device__ __forceinline__ void load_values(const QuantArgs &a, int64_t row, int64_t c0, uint4 &u) {
     const T *p = static_cast<const T *>(a.x) + row * a.ldx + c0;
-    if (vec) {
-        u = __ldg(reinterpret_cast<const uint4 *>(p));
+    if (c0 + V <= a.k) {
+        const uint32_t shift = (uint32_t)(uintptr_t)p & 15u;
+        u = shift == 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : load_shifted(p, shift);
     } else {
         float v[V];
 #pragma unroll
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 4) quantize_rows_kernel(const Qua
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             u[i] = make_uint4(0, 0, 0, 0);
-            if (i < rows) load_values<T, V>(a, r0 + i, c0, a.xvec && whole, u[i]);
+            if (i < rows) load_values<T, V>(a, r0 + i, c0, u[i]);
         }
     }
     uint32_t mx[ROWS];
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 2) quantize_blocks_kernel(const
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             u[i] = make_uint4(0, 0, 0, 0);
-            if (r0 + i * ROWS < a.m) load_values<T, V>(a, r0 + i * ROWS, c0, a.xvec && c0 + V <= a.k, u[i]);
+            if (r0 + i * ROWS < a.m) load_values<T, V>(a, r0 + i * ROWS, c0, u[i]);
         }
     }
     uint32_t amax = 0;

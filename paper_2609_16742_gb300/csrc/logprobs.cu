@@ -455,25 +455,6 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
     if (lane < k) write_top(a, r, lane, out, q);
 }
 
-// 16 bytes from `shift` bytes on of the 32 in p, n
-__device__ __forceinline__ uint4 shifted(const uint4 &p, const uint4 &n, uint32_t shift) {
-    const uint32_t bits = (shift & 3u) * 8u;
-    switch (shift >> 2) {
-        case 0:
-            return make_uint4(__funnelshift_r(p.x, p.y, bits), __funnelshift_r(p.y, p.z, bits),
-                              __funnelshift_r(p.z, p.w, bits), __funnelshift_r(p.w, n.x, bits));
-        case 1:
-            return make_uint4(__funnelshift_r(p.y, p.z, bits), __funnelshift_r(p.z, p.w, bits),
-                              __funnelshift_r(p.w, n.x, bits), __funnelshift_r(n.x, n.y, bits));
-        case 2:
-            return make_uint4(__funnelshift_r(p.z, p.w, bits), __funnelshift_r(p.w, n.x, bits),
-                              __funnelshift_r(n.x, n.y, bits), __funnelshift_r(n.y, n.z, bits));
-        default:
-            return make_uint4(__funnelshift_r(p.w, n.x, bits), __funnelshift_r(n.x, n.y, bits),
-                              __funnelshift_r(n.y, n.z, bits), __funnelshift_r(n.z, n.w, bits));
-    }
-}
-
 // ---------------------------------------------------------------------------
 // Top tokens of a row, or of a share of it, that NT threads read in vectors of
 // 16 bytes, thread t vectors t, t + NT, ...  Each thread leaves its largest logit of
@@ -519,8 +500,7 @@ template <typename T, int NT> struct Top {
         const int64_t j = v * E;
         if (j + E <= q.n) {
             if (q.shift == 0) return __ldg(reinterpret_cast<const uint4 *>(q.x + j));
-            const uint4 *at = reinterpret_cast<const uint4 *>((uintptr_t)(q.x + j) & ~(uintptr_t)15);
-            return shifted(__ldg(at), __ldg(at + 1), q.shift);
+            return load_shifted(q.x + j, q.shift);
         }
         float x[E];
 #pragma unroll
