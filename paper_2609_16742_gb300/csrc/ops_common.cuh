@@ -118,6 +118,13 @@ template <typename T> __device__ __forceinline__ uint4 pack16(const float *v) {
 template <> __device__ __forceinline__ uint4 pack16<float>(const float *v) {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
 }
+// 8 bytes of packed values (4 or 2)
+template <typename T> __device__ __forceinline__ uint64_t pack8(const float *v) {
+    return (uint64_t)pack2<T>(v[2], v[3]) << 32 | pack2<T>(v[0], v[1]);
+}
+template <> __device__ __forceinline__ uint64_t pack8<float>(const float *v) {
+    return (uint64_t)__float_as_uint(v[1]) << 32 | __float_as_uint(v[0]);
+}
 #endif
 
 }  // namespace ops
