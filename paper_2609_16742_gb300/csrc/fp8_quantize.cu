@@ -50,19 +50,33 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi, float inv) {
     return r;
 }
 
-// the V values of row `row` from column c0 on, wherever they start; zeros past
-// the end of the row
-template <typename T, int V>
-__device__ __forceinline__ void load_values(const QuantArgs &a, int64_t row, int64_t c0, uint4 &u) {
-    const T *p = static_cast<const T *>(a.x) + row * a.ldx + c0;
-    if (c0 + V <= a.k) {
-        const uint32_t shift = (uint32_t)(uintptr_t)p & 15u;
-        u = shift == 0 ? __ldg(reinterpret_cast<const uint4 *>(p)) : load_shifted(p, shift);
-    } else {
-        float v[V];
+// 16 bytes of values, of which the first `have` are the row's, from wherever
+// they start, of N rows `step` apart (none from row `rows` on): the 16-byte
+// units that hold one of them, all in flight before the first is looked at;
+// zeros for the others
+template <typename T, int N>
+__device__ __forceinline__ void load_any(const QuantArgs &a, int64_t r0, int64_t c0, int64_t step, int rows, int have,
+                                         uint4 (&u)[N]) {
+    constexpr int BATCH = N < 4 ? N : 4;     // registers of 8 units
+    static_assert(N % BATCH == 0, "batches");
+    const uintptr_t p0 = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.x) + r0 * a.ldx + c0);
+    const int64_t pitch = step * a.ldx * (int)sizeof(T);
+    const int bytes = have * (int)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = c0 + i < a.k ? to_f32(p[i]) : 0.f;
-        u = pack16<T>(v);
+    for (int h = 0; h < N; h += BATCH) {
+        uint4 first[BATCH], second[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const uintptr_t p = p0 + (h + i) * pitch;
+            const uint4 *at = reinterpret_cast<const uint4 *>(p & ~(uintptr_t)15);
+            const bool any = h + i < rows && have > 0;
+            first[i] = second[i] = make_uint4(0, 0, 0, 0);
+            if (any) first[i] = __ldg(at);
+            if (any && (int)(p & 15u) + bytes > 16) second[i] = __ldg(at + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+            u[h + i] = first_bytes(shifted_each(first[i], second[i], (uint32_t)(p0 + (h + i) * pitch) & 15u), bytes);
     }
 }
 
@@ -164,11 +178,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 4) quantize_rows_kernel(const Qua
 #pragma unroll
         for (int i = 0; i < ROWS; ++i, p += a.ldx) u[i] = __ldcs(reinterpret_cast<const uint4 *>(p));
     } else {
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            u[i] = make_uint4(0, 0, 0, 0);
-            if (i < rows) load_values<T, V>(a, r0 + i, c0, u[i]);
-        }
+        load_any<T, ROWS>(a, r0, c0, 1, rows, (int)max((int64_t)0, min((int64_t)V, a.k - c0)), u);
     }
     uint32_t mx[ROWS];
     bool odd = false;                        // something that is not finite
@@ -235,11 +245,9 @@ __global__ void __launch_bounds__(BLOCK_THREADS, 2) quantize_blocks_kernel(const
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) u[i] = __ldg(reinterpret_cast<const uint4 *>(p + i * ROWS * a.ldx));
     } else {
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            u[i] = make_uint4(0, 0, 0, 0);
-            if (r0 + i * ROWS < a.m) load_values<T, V>(a, r0 + i * ROWS, c0, u[i]);
-        }
+        const int64_t left = a.m - r0;       // a row in ROWS is this thread's
+        load_any<T, STEPS>(a, r0, c0, ROWS, left <= 0 ? 0 : (int)min((int64_t)STEPS, (left + ROWS - 1) / ROWS),
+                           (int)max((int64_t)0, min((int64_t)V, a.k - c0)), u);
     }
     uint32_t amax = 0;
 #pragma unroll

@@ -102,6 +102,28 @@ __device__ __forceinline__ uint4 load_shifted(const void *p, uint32_t shift) {
     return shifted(__ldg(at), __ldg(at + 1), shift);
 }
 
+// `shifted` for lanes whose shifts differ: no branch, so that the loads of several units stay in flight together
+__device__ __forceinline__ uint4 shifted_each(const uint4 &p, const uint4 &n, uint32_t shift) {
+    const uint32_t bits = (shift & 3u) * 8u;
+    const bool two = shift & 8u, one = shift & 4u;
+    uint32_t w[6] = {two ? p.z : p.x, two ? p.w : p.y, two ? n.x : p.z, two ? n.y : p.w, two ? n.z : n.x, two ? n.w : n.y};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = one ? w[i + 1] : w[i];
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+                      __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+
+// the first `bytes` (0 to 16) of 16, then zeros
+__device__ __forceinline__ uint4 first_bytes(uint4 u, int bytes) {
+    uint32_t *w = &u.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int keep = bytes - 4 * i;
+        if (keep < 4) w[i] = keep <= 0 ? 0u : w[i] & ((1u << (8 * keep)) - 1u);
+    }
+    return u;
+}
+
 // two floats rounded to T, packed in 32 bits (16-bit types)
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
 template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
