@@ -683,8 +683,25 @@ template <typename T, int NT> struct Top {
 // ---------------------------------------------------------------------------
 constexpr int ROW_WARPS = 4;
 
-template <typename T>
-__global__ void __launch_bounds__(32 * ROW_WARPS) logprobs_warp_kernel(const LpArgs a) {
+// VECS vectors that start `shift` (1 to 15) bytes into their first unit
+template <int WS> __device__ __forceinline__ void shift_words(const uint4 (&x)[VECS], const uint4 (&next)[VECS], uint32_t bits, uint32_t (&w)[4 * VECS]) {
+#pragma unroll
+    for (int u = 0; u < VECS; ++u) {
+        const uint32_t s[8] = {x[u].x, x[u].y, x[u].z, x[u].w, next[u].x, next[u].y, next[u].z, next[u].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 * u + i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
+    }
+}
+__device__ __forceinline__ void shift_all(const uint4 (&x)[VECS], const uint4 (&next)[VECS], uint32_t shift, uint32_t (&w)[4 * VECS]) {
+    const uint32_t bits = (shift & 3u) * 8u;
+    if (shift < 4) shift_words<0>(x, next, bits, w);
+    else if (shift < 8) shift_words<1>(x, next, bits, w);
+    else if (shift < 12) shift_words<2>(x, next, bits, w);
+    else shift_words<3>(x, next, bits, w);
+}
+
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_kernel(const LpArgs a) {
     using P = Top<T, 32>;
     __shared__ typename P::Scratch scratch[ROW_WARPS];
     __shared__ typename P::Left lefts[ROW_WARPS];
@@ -704,19 +721,36 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) logprobs_warp_kernel(const LpA
     Sums<T> sums;
     sums.start();
     float mx = -INF, seg_mx = -INF;
-    uint4 x[VECS];
+    const uint4 *units = reinterpret_cast<const uint4 *>((uintptr_t)row & ~(uintptr_t)15);
+    const int vocab = (int)a.vocab;
+    // batch b's 16-byte units that hold one of its values (with `next`, the second ones of rows that start inside one)
+    uint4 x[VECS], next[VECS];
+    const auto load = [&](int b) {
 #pragma unroll
-    for (int u = 0; u < VECS; ++u) x[u] = P::vec(q, u * 32 + lane);
+        for (int u = 0; u < VECS; ++u) {
+            const int v = (b * VECS + u) * 32 + lane, bytes = (vocab - v * P::E) * (int)sizeof(T);
+            if (bytes > 0) x[u] = __ldg(units + v);
+            if (ANY && q.shift > 0 && (int)q.shift + bytes > 16 && bytes > 0) next[u] = __ldg(units + v + 1);
+        }
+    };
+    load(0);
     int seg = 0, seg_left = seg_batches;
     for (int b = 0; b < batches; ++b) {
         uint32_t w[4 * VECS];
+        if (!ANY || q.shift == 0) {
 #pragma unroll
-        for (int u = 0; u < VECS; ++u) {
-            w[4 * u] = x[u].x; w[4 * u + 1] = x[u].y; w[4 * u + 2] = x[u].z; w[4 * u + 3] = x[u].w;
+            for (int u = 0; u < VECS; ++u) {
+                w[4 * u] = x[u].x; w[4 * u + 1] = x[u].y; w[4 * u + 2] = x[u].z; w[4 * u + 3] = x[u].w;
+            }
+        } else {
+            shift_all(x, next, q.shift, w);
         }
         if (b + 1 < batches) {
+            load(b + 1);
+        } else {
 #pragma unroll
-            for (int u = 0; u < VECS; ++u) x[u] = P::vec(q, ((b + 1) * VECS + u) * 32 + lane);
+            for (int i = 0; i < 4 * VECS; ++i)
+                w[i] = Words<T>::mask(w[i], vocab - ((b * VECS + i / 4) * 32 + lane) * P::E - i % 4 * P::W2);
         }
         uint32_t m2 = w[0];
 #pragma unroll
@@ -1100,9 +1134,11 @@ template <typename T> cudaError_t launch_logprobs(const LpArgs &a, cudaStream_t 
                           dim3(32 * SHORT_WARPS), 0, st, a, vec);
     }
     const int64_t row_bytes = a.vocab * (int64_t)sizeof(T);
-    if (row_bytes <= 32768 && a.rows >= 8 * (int64_t)sm_count())
-        return pdl_launch(logprobs_warp_kernel<T>, dim3((unsigned)((a.rows + ROW_WARPS - 1) / ROW_WARPS)),
-                          dim3(32 * ROW_WARPS), 0, st, a);
+    if (row_bytes <= 32768 && a.rows >= 8 * (int64_t)sm_count()) {
+        const dim3 grid((unsigned)((a.rows + ROW_WARPS - 1) / ROW_WARPS)), block(32 * ROW_WARPS);
+        return aligned(a.x, 16) && a.ldx % Vec16<T>::N == 0 ? pdl_launch(logprobs_warp_kernel<T, false>, grid, block, 0, st, a)
+                                                            : pdl_launch(logprobs_warp_kernel<T, true>, grid, block, 0, st, a);
+    }
     return row_bytes < 98304 ? launch_long<T, 128>(a, st) : launch_long<T, 256>(a, st);
 }
 
