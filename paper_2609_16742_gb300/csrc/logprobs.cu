@@ -476,7 +476,7 @@ template <typename T, int NT> struct Top {
     static constexpr int CAP = 8 * CT_MAX_TOP_K;           // candidates; also 8 CTAs' best
     static constexpr int HITS = 8 * (NT < 64 ? NT : 64);   // thread segments looked over again
     struct Scratch {                                       // a finishing warp's
-        uint64_t cand[CAP];
+        alignas(16) uint64_t cand[CAP];
         uint64_t best[CT_MAX_TOP_K];
         int count;
         uint8_t thread[NT];                                // threads, and
@@ -495,17 +495,29 @@ template <typename T, int NT> struct Top {
         int seg_vecs;                                      // vectors of a thread in a segment
         int segs;
     };
-    // the words of vector v, wherever it starts; -inf past the end
-    static __device__ __forceinline__ uint4 vec(const Share &q, int64_t v) {
-        const int64_t j = v * E;
-        if (j + E <= q.n) {
-            if (q.shift == 0) return __ldg(reinterpret_cast<const uint4 *>(q.x + j));
-            return load_shifted(q.x + j, q.shift);
+    // the one or two 16-byte units that hold values of vector v, and its words, -inf past the end: apart, so that
+    // several loads are in flight before the first is looked at
+    struct Units {
+        uint4 p, n;
+    };
+    static __device__ __forceinline__ Units fetch(const Share &q, int64_t v) {
+        const int64_t left = (q.n - v * E) * (int)sizeof(T);
+        const uint4 *at = reinterpret_cast<const uint4 *>((uintptr_t)q.x & ~(uintptr_t)15) + v;
+        Units u = {};
+        if (left > 0) u.p = __ldg(at);
+        if (left > 0 && q.shift > 0 && (int64_t)q.shift + left > 16) u.n = __ldg(at + 1);
+        return u;
+    }
+    static __device__ __forceinline__ uint4 words(const Share &q, int64_t v, const Units &u) {
+        uint4 w = shifted_each(u.p, u.n, q.shift);
+        const int have = (int)max((int64_t)0, min((int64_t)E, q.n - v * E));
+        if (have < E) {
+            w.x = Words<T>::mask(w.x, have);
+            w.y = Words<T>::mask(w.y, have - W2);
+            w.z = Words<T>::mask(w.z, have - 2 * W2);
+            w.w = Words<T>::mask(w.w, have - 3 * W2);
         }
-        float x[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = j + e < q.n ? to_f32(q.x[j + e]) : -INF;
-        return pack16<T>(x);
+        return w;
     }
     // 32 bits ordered like the logits, 0 for none; and the least logit of that order
     static __device__ __forceinline__ uint32_t order(float x) { return (uint32_t)(order_key(x, 0) >> 32); }
@@ -519,54 +531,67 @@ template <typename T, int NT> struct Top {
     static __device__ __forceinline__ int collect(Scratch &sh, const Left &left, const Share &q, uint32_t from) {
         const int lane = threadIdx.x % 32;
         const uint32_t below = (1u << lane) - 1u;
+        const float least = order_value(from);
         // threads
+        float mx[NT / 32];
+#pragma unroll
+        for (int i = 0; i < NT / 32; ++i) mx[i] = left.mx[i * 32 + lane];
         int threads = 0;
-        for (int t = lane; t < NT; t += 32) {
-            const bool hit = order(left.mx[t]) >= from;
-            const uint32_t b = __ballot_sync(~0u, hit);
-            if (hit) sh.thread[threads + __popc(b & below)] = (uint8_t)t;
+#pragma unroll
+        for (int i = 0; i < NT / 32; ++i) {
+            const uint32_t b = __ballot_sync(~0u, mx[i] >= least);
+            if (mx[i] >= least) sh.thread[threads + __popc(b & below)] = (uint8_t)(i * 32 + lane);
             threads += __popc(b);
         }
         __syncwarp();
-        // their segments: 4 threads at a time
+        // their segments: a thread for each lane
         int hits = 0;
-        for (int i = 0; i < threads; i += 4) {
-            const int t = i + lane / SEGMENTS < threads ? sh.thread[i + lane / SEGMENTS] : -1, g = lane % SEGMENTS;
-            const bool hit = t >= 0 && g < q.segs && order(to_f32(left.seg[g][t < 0 ? 0 : t])) >= from;
-            const uint32_t b = __ballot_sync(~0u, hit);
-            if (hits + __popc(b) > HITS) return CAP + 1;
-            if (hit) sh.hit[hits + __popc(b & below)] = (uint16_t)(t * SEGMENTS + g);
-            hits += __popc(b);
+        for (int i = 0; i < threads; i += 32) {
+            const bool live = i + lane < threads;
+            const int t = live ? sh.thread[i + lane] : 0;
+            uint32_t b[SEGMENTS];
+            int n = 0;
+#pragma unroll
+            for (int g = 0; g < SEGMENTS; ++g) {
+                b[g] = __ballot_sync(~0u, live && g < q.segs && to_f32(left.seg[g][t]) >= least);
+                n += __popc(b[g]);
+            }
+            if (hits + n > HITS) return CAP + 1;
+#pragma unroll
+            for (int g = 0; g < SEGMENTS; ++g) {
+                if (b[g] >> lane & 1u) sh.hit[hits + __popc(b[g] & below)] = (uint16_t)(t * SEGMENTS + g);
+                hits += __popc(b[g]);
+            }
         }
         if (lane == 0) sh.count = 0;
         __syncwarp();
-        // their vectors: 8 lanes take those of one segment
-        const float least = order_value(from);
+        // their vectors
         constexpr int AHEAD = 2;                           // loads in flight together
-        for (int i = lane / 8; i < hits; i += 4 * AHEAD) {
-            for (int o = lane % 8; o < q.seg_vecs; o += 8) {
-                uint4 x[AHEAD];
-                uint32_t v[AHEAD];
+        const int all = hits * q.seg_vecs;
+        for (int i = lane; i - lane < all; i += 32 * AHEAD) {
+            Units x[AHEAD];
+            uint32_t v[AHEAD];
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const int h = i + 4 * u < hits ? sh.hit[i + 4 * u] : -1;
-                    v[u] = (uint32_t)((h & (SEGMENTS - 1)) * q.seg_vecs + o) * NT + (uint32_t)(h / SEGMENTS);
-                    if (h >= 0) x[u] = vec(q, v[u]);
-                    else x[u].x = x[u].y = x[u].z = x[u].w = Words<T>::dup(-INF);
-                }
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t at = (uint32_t)(i + 32 * u), h = at / (uint32_t)q.seg_vecs, o = at % (uint32_t)q.seg_vecs;
+                const uint32_t hit = at < (uint32_t)all ? sh.hit[h] : 0;
+                v[u] = (hit % SEGMENTS * (uint32_t)q.seg_vecs + o) * NT + hit / SEGMENTS;
+                x[u] = Units{};
+                if (at < (uint32_t)all) x[u] = fetch(q, v[u]);
+            }
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const uint32_t m2 = Words<T>::max2(Words<T>::max2(x[u].x, x[u].y), Words<T>::max2(x[u].z, x[u].w));
-                    if (Words<T>::largest(m2) >= least) {
-                        float f[E];
-                        unpack16<T>(x[u], f);
+            for (int u = 0; u < AHEAD; ++u) {
+                if (i + 32 * u >= all) break;
+                const uint4 w = words(q, v[u], x[u]);
+                if (Words<T>::largest(Words<T>::max2(Words<T>::max2(w.x, w.y), Words<T>::max2(w.z, w.w))) >= least) {
+                    float f[E];
+                    unpack16<T>(w, f);
 #pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (f[e] >= least) {
-                                const int at = atomicAdd(&sh.count, 1);
-                                if (at < CAP) sh.cand[at] = order_key(f[e], q.j0 + v[u] * E + (uint32_t)e);
-                            }
-                    }
+                    for (int e = 0; e < E; ++e)
+                        if (f[e] >= least) {
+                            const int at = atomicAdd(&sh.count, 1);
+                            if (at < CAP) sh.cand[at] = order_key(f[e], q.j0 + v[u] * E + (uint32_t)e);
+                        }
                 }
             }
         }
@@ -630,7 +655,7 @@ template <typename T, int NT> struct Top {
             // ... and the first that equal it, in the row's order
             for (int64_t v0 = 0; n < k && v0 < vecs; v0 += 32) {
                 float x[E];
-                unpack16<T>(vec(q, v0 + lane), x);
+                unpack16<T>(words(q, v0 + lane, fetch(q, v0 + lane)), x);
                 int have = 0;
 #pragma unroll
                 for (int e = 0; e < E; ++e) have += order(x[e]) == thr;
@@ -661,7 +686,7 @@ template <typename T, int NT> struct Top {
 #pragma unroll 2
             for (int64_t v = lane; v < vecs; v += 32) {
                 float x[E];
-                unpack16<T>(vec(q, v), x);
+                unpack16<T>(words(q, v, fetch(q, v)), x);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const uint64_t key = order_key(x[e], q.j0 + (uint32_t)(v * E + e));
@@ -804,7 +829,9 @@ template <typename T, int NT> struct Long : Top<T, NT> {
         typename P::Scratch scratch[FIN];
         uint64_t join[CT_MAX_TOP_K];
         Left left[FIN];
-        Stat total;
+        Stat total;                                        // a split row's
+        float given;
+        int64_t id;
     };
     static constexpr size_t SMEM = (size_t)STAGES * STAGE + sizeof(Shared) + 16;
     static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory of an SM");
@@ -913,7 +940,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
         for (int64_t r = cid + f * ncl; r < a.rows; r += FIN * ncl, phase ^= 1u) {
             const T *row = static_cast<const T *>(a.x) + r * a.ldx;
             int64_t id = -1;
-            const float given = lane == 0 && splits == 1 ? given_logit<T>(a, r, id) : 0.f;
+            const float given = lane == 0 && rank == 0 ? given_logit<T>(a, r, id) : 0.f;
             tc::warp_wait(tc::smem_u32(&sh.left_full[f]), phase, a.err, E_LOGPROBS);
             const Stat st = warp_merge(lane < NT / 32 ? left.part[lane] : Stat{-INF, 0.f, 0.f});
             if (k > 0) {
@@ -931,6 +958,8 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
                 if (lane < k) write_top(a, r, lane, scratch.best[lane], q);
             } else if (lane == 0) {
                 sh.total = st;
+                sh.id = id;
+                sh.given = given;
             }
             __syncwarp();
         }
@@ -977,29 +1006,30 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
         tc::cluster_sync();
         if (rank == 0 && tid < NT) {
             const auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); };
-            int64_t id = -1;
-            const float given = tid == 0 ? given_logit<T>(a, cid, id) : 0.f;
             Stat st = {-INF, 0.f, 0.f};
-            for (int p = 0; p < splits; ++p) {
-                const uint32_t at = tc::mapa_shared(tc::smem_u32(&sh.total), (uint32_t)p);
-                st = merge(st, Stat{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)});
+            if (lane < splits) {
+                const uint32_t at = tc::mapa_shared(tc::smem_u32(&sh.total), (uint32_t)lane);
+                st = Stat{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)};
             }
-            const RowResult q = row_result(st);
-            if (tid == 0) write_row(a, cid, q, id, given);
+            const RowResult q = row_result(warp_merge(st));
+            if (tid == 0) write_row(a, cid, q, sh.id, sh.given);
             if (k > 0) {
                 // splits * k <= CAP keys, several to a thread: a key's place is the number of larger ones
                 const int n = splits * k;
                 uint64_t *cand = sh.scratch[0].cand;
-                for (int i = tid; i < n; i += NT)
-                    cand[i] = ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[i % k]), (uint32_t)(i / k)));
-                sync();
+                for (int i = tid; i < n + (n & 1); i += NT)
+                    cand[i] = i == n ? 0
+                                     : ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[i % k]), (uint32_t)(i / k)));
                 if (tid < k) sh.join[tid] = 0;
                 sync();
                 for (int i = tid; i < n; i += NT) {
                     const uint64_t key = cand[i];
                     int place = 0;
 #pragma unroll 8
-                    for (int j = 0; j < n; ++j) place += cand[j] > key;
+                    for (int j = 0; j < n; j += 2) {
+                        const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(cand + j);
+                        place += (o.x > key) + (o.y > key);
+                    }
                     if (key != 0 && place < k) sh.join[place] = key;
                 }
                 sync();
