@@ -473,12 +473,11 @@ constexpr int SEGMENTS = 8;                                // of a row, for a th
 template <typename T, int NT> struct Top {
     static constexpr int E = Vec16<T>::N;                  // values of a vector
     static constexpr int W2 = 4 / (int)sizeof(T);          // values of a word
-    static constexpr int CAP = 8 * CT_MAX_TOP_K;           // candidates; also 8 CTAs' best
+    static constexpr int CAP = 8 * CT_MAX_TOP_K;           // candidates
     static constexpr int HITS = 8 * (NT < 64 ? NT : 64);   // thread segments looked over again
     struct Scratch {                                       // a finishing warp's
         alignas(16) uint64_t cand[CAP];
         uint64_t best[CT_MAX_TOP_K];
-        int count;
         uint8_t thread[NT];                                // threads, and
         uint16_t hit[HITS];                                // thread segments (thread * SEGMENTS + segment) with top tokens
     };
@@ -563,9 +562,9 @@ template <typename T, int NT> struct Top {
                 hits += __popc(b[g]);
             }
         }
-        if (lane == 0) sh.count = 0;
         __syncwarp();
         // their vectors
+        int count = 0;
         constexpr int AHEAD = 2;                           // loads in flight together
         const int all = hits * q.seg_vecs;
         for (int i = lane; i - lane < all; i += 32 * AHEAD) {
@@ -581,22 +580,27 @@ template <typename T, int NT> struct Top {
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                if (i + 32 * u >= all) break;
-                const uint4 w = words(q, v[u], x[u]);
-                if (Words<T>::largest(Words<T>::max2(Words<T>::max2(w.x, w.y), Words<T>::max2(w.z, w.w))) >= least) {
-                    float f[E];
-                    unpack16<T>(w, f);
+                if (i - lane + 32 * u >= all) break;
+                uint4 w = words(q, v[u], x[u]);
+                if (i + 32 * u >= all) w.x = w.y = w.z = w.w = Words<T>::dup(-INF);
+                const float top = Words<T>::largest(Words<T>::max2(Words<T>::max2(w.x, w.y), Words<T>::max2(w.z, w.w)));
+                if (__ballot_sync(~0u, top >= least) == 0) continue;
+                float f[E];
+                unpack16<T>(w, f);
+                uint32_t mine = 0;                         // values that reach it, mostly one or none
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (f[e] >= least) {
-                            const int at = atomicAdd(&sh.count, 1);
-                            if (at < CAP) sh.cand[at] = order_key(f[e], q.j0 + v[u] * E + (uint32_t)e);
-                        }
+                for (int e = 0; e < E; ++e) mine |= f[e] >= least ? 1u << e : 0u;
+                for (uint32_t b; (b = __ballot_sync(~0u, mine != 0)) != 0; mine &= mine - 1, count += __popc(b)) {
+                    const int at = count + __popc(b & below), e = __ffs(mine) - 1;
+                    float x = f[0];
+#pragma unroll
+                    for (int n = 1; n < E; ++n) x = e == n ? f[n] : x;
+                    if (mine != 0 && at < CAP) sh.cand[at] = order_key(x, q.j0 + v[u] * E + (uint32_t)e);
                 }
             }
         }
         __syncwarp();
-        return min(sh.count, CAP + 1);
+        return min(count, CAP + 1);
     }
     // sorts the list's best k into sh.best
     static __device__ __forceinline__ void select(Scratch &sh, int n, int k) {
@@ -617,30 +621,33 @@ template <typename T, int NT> struct Top {
         const int lane = threadIdx.x % 32;
         // up to 64 groups of threads, two for each lane
         uint32_t g0 = 0, g1 = 0;
+        if constexpr (NT > 32) {
 #pragma unroll
-        for (int i = 0; i < NT / 32; i += 2) {
-            g0 = max(g0, order(left.mx[i * 32 + lane]));
-            if (NT > 32) g1 = max(g1, order(left.mx[i * 32 + (NT > 32 ? 32 : 0) + lane]));
-        }
-        // sorted by a bitonic network, descending: position lane in g0, 32 + lane in g1
-#pragma unroll
-        for (int size = 2; size <= 64; size *= 2) {
-#pragma unroll
-            for (int d = size / 2; d > 0; d /= 2) {
-                if (d == 32) {
-                    const uint32_t hi = max(g0, g1);
-                    g1 = min(g0, g1);
-                    g0 = hi;
-                } else {
-                    const uint32_t o0 = __shfl_xor_sync(~0u, g0, d), o1 = __shfl_xor_sync(~0u, g1, d);
-                    const bool first = (lane & d) == 0;
-                    const bool down0 = (lane & size) == 0 || size == 64, down1 = ((32 + lane) & size) == 0 || size == 64;
-                    g0 = first == down0 ? max(g0, o0) : min(g0, o0);
-                    g1 = first == down1 ? max(g1, o1) : min(g1, o1);
-                }
+            for (int i = 0; i < NT / 32; i += 2) {
+                g0 = max(g0, order(left.mx[i * 32 + lane]));
+                g1 = max(g1, order(left.mx[i * 32 + 32 + lane]));
+            }
+        } else {                                           // each thread's, of either half of the segments
+            for (int g = 0; g < q.segs; ++g) {
+                const uint32_t o = order(to_f32(left.seg[g][lane]));
+                if (2 * g < q.segs) g0 = max(g0, o);
+                else g1 = max(g1, o);
             }
         }
-        const uint32_t thr = __shfl_sync(~0u, g0, k - 1);  // k <= 32
+        // the k-th largest: the least of those that fewer than k exceed
+        uint32_t *all = reinterpret_cast<uint32_t *>(sh.cand);
+        all[lane] = g0;
+        all[32 + lane] = g1;
+        __syncwarp();
+        int c0 = 0, c1 = 0;
+#pragma unroll
+        for (int i = 0; i < 64; i += 4) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(all + i);
+            c0 += (o.x > g0) + (o.y > g0) + (o.z > g0) + (o.w > g0);
+            c1 += (o.x > g1) + (o.y > g1) + (o.z > g1) + (o.w > g1);
+        }
+        const uint32_t thr = __reduce_min_sync(~0u, min(c0 < k ? g0 : ~0u, c1 < k ? g1 : ~0u));   // k <= 32
+        __syncwarp();
         const int n = collect(sh, left, q, max(thr, 1u));
         if (n <= CAP) select(sh, n, k);
         else top_ties(sh, q, left, k, thr);
@@ -808,6 +815,20 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_ker
 // leave of it meanwhile.
 // ---------------------------------------------------------------------------
 
+constexpr int MAX_SPLITS = 8;                              // CTAs that share a row
+
+// the 32 best keys of two lists, each sorted over the lanes from the best on
+__device__ __forceinline__ uint64_t best32(uint64_t a, uint64_t b) {
+    const int lane = threadIdx.x % 32;
+    a = max(a, __shfl_sync(~0u, b, 31 - lane));            // rises, then falls
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const uint64_t o = __shfl_xor_sync(~0u, a, d);
+        a = (lane & d) == 0 ? max(a, o) : min(a, o);
+    }
+    return a;
+}
+
 // NT consumer threads, a producer warp and FIN finisher warps
 template <typename T, int NT> struct Long : Top<T, NT> {
     using P = Top<T, NT>;
@@ -827,7 +848,6 @@ template <typename T, int NT> struct Long : Top<T, NT> {
         uint64_t full[STAGES], empty[STAGES];
         uint64_t left_full[FIN], left_free[FIN];
         typename P::Scratch scratch[FIN];
-        uint64_t join[CT_MAX_TOP_K];
         Left left[FIN];
         Stat total;                                        // a split row's
         float given;
@@ -1004,36 +1024,25 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
     if (splits > 1) {
         // one row for each cluster: rank 0's consumer threads join the shares, in rank order
         tc::cluster_sync();
-        if (rank == 0 && tid < NT) {
-            const auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory"); };
+        if (rank == 0 && warp == 0) {
+            // lane p: share p's sums; lane i: each share's i-th best token
             Stat st = {-INF, 0.f, 0.f};
             if (lane < splits) {
                 const uint32_t at = tc::mapa_shared(tc::smem_u32(&sh.total), (uint32_t)lane);
                 st = Stat{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)};
             }
+            uint64_t best[MAX_SPLITS];
+#pragma unroll
+            for (int p = 0; p < MAX_SPLITS; ++p)
+                best[p] = p < splits && lane < k ? ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[lane]), (uint32_t)p)) : 0;
             const RowResult q = row_result(warp_merge(st));
-            if (tid == 0) write_row(a, cid, q, sh.id, sh.given);
+            if (lane == 0) write_row(a, cid, q, sh.id, sh.given);
             if (k > 0) {
-                // splits * k <= CAP keys, several to a thread: a key's place is the number of larger ones
-                const int n = splits * k;
-                uint64_t *cand = sh.scratch[0].cand;
-                for (int i = tid; i < n + (n & 1); i += NT)
-                    cand[i] = i == n ? 0
-                                     : ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[i % k]), (uint32_t)(i / k)));
-                if (tid < k) sh.join[tid] = 0;
-                sync();
-                for (int i = tid; i < n; i += NT) {
-                    const uint64_t key = cand[i];
-                    int place = 0;
-#pragma unroll 8
-                    for (int j = 0; j < n; j += 2) {
-                        const ulonglong2 o = *reinterpret_cast<const ulonglong2 *>(cand + j);
-                        place += (o.x > key) + (o.y > key);
-                    }
-                    if (key != 0 && place < k) sh.join[place] = key;
-                }
-                sync();
-                if (tid < k) write_top(a, cid, tid, sh.join[tid], q);
+#pragma unroll
+                for (int n = MAX_SPLITS / 2; n > 0; n /= 2)
+#pragma unroll
+                    for (int p = 0; p < n; ++p) best[p] = best32(best[p], best[p + n]);
+                if (lane < k) write_top(a, cid, lane, best[0], q);
             }
         }
         tc::cluster_sync();
@@ -1148,7 +1157,7 @@ template <typename T, int NT> cudaError_t launch_long(const LpArgs &a, cudaStrea
     const int64_t chunks = (a.vocab + L::CE - 1) / L::CE;
     // few rows: each is shared by a cluster (one row each), so that the whole GPU reads
     int splits = 1;
-    while (splits < 8 && a.rows * splits * 2 <= slots && splits * 2 <= chunks) splits *= 2;
+    while (splits < MAX_SPLITS && a.rows * splits * 2 <= slots && splits * 2 <= chunks) splits *= 2;
     const dim3 block(L::THREADS);
     if (splits > 1)
         return pdl_launch_cluster(logprobs_long_kernel<T, NT>, dim3((unsigned)(a.rows * splits)), block, L::SMEM, st,
