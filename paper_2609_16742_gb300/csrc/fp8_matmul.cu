@@ -98,8 +98,11 @@ template <int N> __device__ __forceinline__ void tmem_ld_nw(uint32_t taddr, uint
                      : "r"(taddr));
     } else if constexpr (N == 16) {
         tmem_ld16_nw(taddr, r);
+    } else if constexpr (N == 48) {
+        tmem_ld_nw<32>(taddr, reinterpret_cast<uint32_t (&)[32]>(r[0]));
+        tmem_ld_nw<16>(taddr + 32u, reinterpret_cast<uint32_t (&)[16]>(r[32]));
     } else {
-        static_assert(N == 32, "8, 16 or 32 columns");
+        static_assert(N == 32, "8, 16, 32 or 48 columns");
         asm volatile(
             "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
             "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -418,12 +421,13 @@ constexpr int W_LINES_BYTES = 32 * 33 * 8;   // or a warp's rows where TMA does 
 
 template <int BN> struct Wide {
     static constexpr int C_BYTES = BN / 2 * BK;            // this CTA's half of the column operand
-    static constexpr int STAGES = BN == 256 ? 4 : 6;
+    static constexpr int STAGES = BN == 256 ? 4 : BN == 192 ? 5 : 6;
     static constexpr int BOXES = 2;                        // epilogue: 32 rows of 128 bytes on their way to y, for each warp
-    static constexpr int NBUF = BN == 256 ? 2 : 4;         // accumulators
+    static constexpr int NBUF = BN >= 192 ? 2 : 4;         // accumulators
+    static constexpr int TMEM = BN == 192 ? 512 : NBUF * BN;  // columns: a power of two
     static constexpr int FAC_SLOTS = 2 * NBUF;
     static constexpr int CPW = BN / 2;                     // columns of an epilogue warp
-    static constexpr int LDN = BN == 64 ? 16 : 32;         // columns of one TMEM load: an even number of loads
+    static constexpr int LDN = BN == 64 ? 16 : BN == 192 ? 48 : 32;   // columns on their way together: an even number of times
     static constexpr int PITCH = BN + 4;                   // row of partial sums, in floats: 8 rows hit all banks
     static_assert(BL * PITCH * 4 <= STAGES * (L_BYTES + C_BYTES) + N_EPI * BOXES * W_BOX_BYTES,
                   "partial sums over the stages and boxes");
@@ -494,7 +498,7 @@ template <int CPW> __device__ __forceinline__ void finish_row(const MmArgs &a, u
 template <typename O, int CPW, int BOXES>
 __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *ymap, const uint64_t *acc, uint8_t *boxes,
                                             uint32_t &stored, int m_warp, int c0, int lane) {
-    constexpr int COLS = 128 / (int)sizeof(O) < CPW ? 128 / (int)sizeof(O) : CPW;
+    constexpr int COLS = CPW % (128 / (int)sizeof(O)) == 0 ? 128 / (int)sizeof(O) : 32;
     constexpr int PER16 = 16 / (int)sizeof(O);             // values of 16 bytes
     constexpr int PIECES = COLS / PER16;                   // 16-byte pieces of a box row
     static_assert((PIECES == 8 || PIECES == 4) && CPW % COLS == 0, "box rows of 128 or 64 bytes");
@@ -533,10 +537,11 @@ __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *
 template <typename O, int CPW>
 __device__ __forceinline__ void store_lines(const MmArgs &a, const uint64_t *acc, uint64_t *sq, int m_warp, int c0, int lane) {
     constexpr int PER8 = 8 / (int)sizeof(O);               // values of a unit
-    constexpr int COLS = 256 / (int)sizeof(O) < CPW ? 256 / (int)sizeof(O) : CPW;
+    constexpr int MOST = 256 / (int)sizeof(O) < CPW ? 256 / (int)sizeof(O) : CPW;
+    constexpr int COLS = CPW % MOST == 0 ? MOST : CPW / 2;
     constexpr int UNITS = COLS / PER8, STEP = 32 / UNITS;  // rows of one store
     constexpr int PITCH = UNITS + 1;                       // odd: neither side hits a bank twice
-    static_assert(UNITS <= 32 && 32 % UNITS == 0, "whole rows a warp");
+    static_assert(CPW % COLS == 0 && UNITS <= 32 && UNITS % 8 == 0, "segments of whole units");
     static_assert(32 * PITCH * 8 <= W_LINES_BYTES, "a segment of 32 rows");
     const int rows = min(32, a.M - m_warp);
     const int64_t pitch = a.ldy * (int)sizeof(O);
@@ -572,7 +577,7 @@ __device__ __forceinline__ void store_lines(const MmArgs &a, const uint64_t *acc
 #pragma unroll 4
             for (int r = lane / UNITS; r < rows; r += STEP, row += STEP * pitch, src += STEP * PITCH) {
                 const int off = (int)(row & 7u);
-                if (u * 8 >= off && u * 8 + 8 <= off + have * (int)sizeof(O))
+                if (lane < STEP * UNITS && u * 8 >= off && u * 8 + 8 <= off + have * (int)sizeof(O))
                     *reinterpret_cast<uint64_t *>((row & ~(uintptr_t)7) + u * 8) = *src;
             }
         }
@@ -666,7 +671,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     if (warp == MMA_WARP) {
         // one warp of each CTA of the pair allocates the same columns in both
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
-                     "r"((uint32_t)(NBUF * BN)));
+                     "r"((uint32_t)S::TMEM));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -723,7 +728,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     xp[i] = a.xs + (int64_t)min(m0 + 32 * i, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
-                    wp[i] = a.ws + (int64_t)min((tc * BN + i * CPW) / 128, last) * a.ws_row + kb0 * a.ws_blk;
+                    wp[i] = a.ws + (int64_t)min(BN == 192 ? tc * BN / 128 + i : (tc * BN + i * CPW) / 128, last) * a.ws_row + kb0 * a.ws_blk;
                 }
                 float x[DEPTH][2], w[DEPTH][2];
                 const auto load = [&](int kb, int u) {
@@ -785,7 +790,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
         const uint32_t tbase = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * CPW);
         const uint32_t acc_empty_even = mapa_shared(smem_u32(acc_empty), even);
         uint8_t *mine = boxes + warp * S::BOXES * W_BOX_BYTES;
-        const float *my_fac = fac + half * BL + quad * 32 + lane;
+        const float *my_fac = fac + (BN == 192 ? 0 : half * BL) + quad * 32 + lane;
         uint32_t stored = 0;                               // boxes this warp has stored
         uint32_t it = 0;
         bool ok = true;
@@ -793,7 +798,10 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             int tl, tc;
             tile_at(a, t, tl, tc);
             const int m_warp = (2 * tl + (int)crank) * BL + quad * 32;
-            const int c0 = tc * BN + half * CPW;           // inside one 128-row block of w
+            // the warp's columns lie inside one 128-row block of w, or, 192 wide, in the tile's first up to
+            // its 32-column group `turn` and from there on in the second
+            const int c0 = tc * BN + half * CPW;
+            const int turn = (128 - tc * BN % 128 - half * CPW) / 32;
             uint64_t acc[CPW / 2];
 #pragma unroll
             for (int i = 0; i < CPW / 2; ++i) acc[i] = 0;
@@ -805,7 +813,15 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
             if (!SPLIT || ok) tmem_ld_nw<LDN>(tbase + (uint32_t)((it & (NBUF - 1)) * BN), r[0]);
             for (int kb = 0; kb < KB && ok; ++kb, ++it) {
                 const uint32_t src = tbase + (uint32_t)((it & (NBUF - 1)) * BN);
-                const uint64_t f = dup2(my_fac[(it & (FAC_SLOTS - 1)) * (2 * BL)]);
+                constexpr int GROUPS = BN == 192 ? 3 : 1;
+                uint64_t f[GROUPS];
+                const float first = my_fac[(it & (FAC_SLOTS - 1)) * (2 * BL)];
+                f[0] = dup2(first);
+                if constexpr (BN == 192) {
+                    const float second = my_fac[(it & (FAC_SLOTS - 1)) * (2 * BL) + BL];
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) f[g] = dup2(g < turn ? first : second);
+                }
                 // LDN columns are on their way while the LDN before are added,
                 // across blocks too
 #pragma unroll
@@ -826,7 +842,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f, r[h][2 * i], r[h][2 * i + 1]);
+                    for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f[GROUPS == 1 ? 0 : (c + 2 * i) / 32], r[h][2 * i], r[h][2 * i + 1]);
                 }
             }
             // After a wait that ran out, which is reported, the output is invalid;
@@ -870,7 +886,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
     cluster_sync();
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(NBUF * BN)));
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)S::TMEM));
     }
 }
 
@@ -981,8 +997,10 @@ int resident(K *kernel, int threads, size_t smem, int cluster, std::atomic<int> 
 constexpr int N_SPLITS = 6;
 constexpr int NARROW_SPLITS[N_SPLITS] = {1, 2, 3, 4, 6, 8};
 
-// [dev][log2 of the columns / 16][index of the split], [dev][log2 of the columns / 64][splits - 1]
-std::atomic<int> g_narrow[MAX_DEVICES][4][N_SPLITS], g_wide[MAX_DEVICES][3][2];
+constexpr int W_COLS[4] = {64, 128, 192, 256};
+
+// [dev][log2 of the columns / 16][index of the split], [dev][index of the columns][splits - 1]
+std::atomic<int> g_narrow[MAX_DEVICES][4][N_SPLITS], g_wide[MAX_DEVICES][4][2];
 
 template <int BN> int narrow_resident(int splits, std::atomic<int> &known) {
     return resident(fp8_narrow_kernel<BN>, THREADS, Narrow<BN>::SMEM, splits, known);
@@ -1004,14 +1022,15 @@ struct Choice {
 // 25088); the choice is 2.5% slower than the best candidate on average, 24% at
 // worst.
 //   A K block costs a CTA 0.2 to 0.5 us (16 to 128 columns), a pair 0.2 to
-//   0.41 us (64 to 256); launch, start and end of a tile 1 to 3.3 us, 3.9 to
+//   0.41 us (64 to 256; 192 save little of a block, but often a round: 1777 x
+//   2999 x 5003 takes 40.8 us in 128 columns, 41.0 in 256, 36.4 in 192); launch, start and end of a tile 1 to 3.3 us, 3.9 to
 //   4.8 us; adding the shares of a split 1.4 to 2.2 us, 3.5 us.
 //   No kernel is faster than its operands: 9 to 11 bytes a ns from L2, 6.4 of
 //   weights from HBM, 58 bytes a ns to one SM.
 Choice choose(int M, int N, int KB, int sms, int dev) {
     static const double n_block[4] = {0.2, 0.25, 0.33, 0.5}, n_tile[4] = {1.0, 1.3, 2.7, 3.3};
     static const double n_split[N_SPLITS] = {0, 1.4, 1.7, 2.0, 2.2, 2.2};
-    static const double w_block[3] = {0.2, 0.28, 0.41};
+    static const double w_block[4] = {0.2, 0.28, 0.385, 0.41};
     Choice best = {false, 16, 1, 0};
     double least = 1e30;
     const double weights = (double)N * KB * BK;
@@ -1037,12 +1056,15 @@ Choice choose(int M, int N, int KB, int sms, int dev) {
             if (t < least) { least = t; best = Choice{false, bn, s, ctas}; }
         }
     }
-    for (int i = 0; i < 3 && M > 64; ++i) {
-        const int bn = 64 << i;
+    for (int i = 0; i < 4 && M > 64; ++i) {
+        const int bn = W_COLS[i];
         const int64_t tiles = rows_m * ((N + bn - 1) / bn);
-        for (int s = 1; s <= 2 && s <= KB; ++s) {
+        for (int s = 1; s <= (bn == 192 ? 1 : 2) && s <= KB; ++s) {
             std::atomic<int> &known = g_wide[dev][i][s - 1];
-            const int ctas = bn == 64 ? wide_resident<64>(s, known) : bn == 128 ? wide_resident<128>(s, known) : wide_resident<256>(s, known);
+            const int ctas = bn == 64    ? wide_resident<64>(s, known)
+                             : bn == 128 ? wide_resident<128>(s, known)
+                             : bn == 192 ? resident(fp8_wide_kernel<192, false>, W_THREADS, Wide<192>::SMEM, 2, known)
+                                         : wide_resident<256>(s, known);
             const int64_t pairs = ctas / 2;
             if (ctas == 0 || (s > 1 && tiles * s > pairs)) continue;
             const double nkb = (KB + s - 1) / s, rounds = (double)((tiles * s + pairs - 1) / pairs);
@@ -1085,11 +1107,13 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
         a.vec = aligned(a.y, 16) && a.ldy * es % 16 == 0;
         if (!encode8(&lmap, o.xq, a.M, o.k, o.ldx, BL) || !encode8(&cmap, o.wq, a.N, o.k, o.ldw, bn / 2) ||
             (a.vec && !encode(&ymap, a.y, a.out == CT_DT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16,
-                              es, a.M, a.N, a.ldy * es, bn == 64 && es == 2 ? 64 : 128, 32)))
+                              es, a.M, a.N, a.ldy * es, bn % 128 == 64 && es == 2 ? 64 : 128, 32)))
             return CT_ECUDA;
         const int n = (int)(a.splits > 1 || tiles < pairs ? tiles : pairs);
         e = bn == 64    ? launch_wide<64>(lmap, cmap, ymap, a, n, st)
             : bn == 128 ? launch_wide<128>(lmap, cmap, ymap, a, n, st)
+            : bn == 192 ? pdl_launch_cluster(fp8_wide_kernel<192, false>, dim3((unsigned)(2 * n)), dim3(W_THREADS),
+                                             Wide<192>::SMEM, st, 2, lmap, cmap, ymap, a)
                         : launch_wide<256>(lmap, cmap, ymap, a, n, st);
     } else {
         a.tiles_l = (a.N + 127) / 128;
