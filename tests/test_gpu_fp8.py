@@ -160,6 +160,35 @@ def test_matmul_exact_on_integers(m, n, k):
         assert np.array_equal(y.cpu().numpy(), ref)
 
 
+@pytest.mark.parametrize("out", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("m,n,k", [(1777, 2999, 1300), (1100, 4001, 300), (2050, 3501, 130), (530, 9600, 256)])
+@pytest.mark.parametrize("lo,pad", [(0, 0), (1, 2), (3, 5), (8, 0)])
+def test_matmul_many_tiles_anywhere(out, m, n, k, lo, pad):
+    """More tiles than the GPU takes at once, into a matrix whose rows start
+    anywhere; nothing beside it is written.  Integers: exact before the one
+    rounding to y's type."""
+    torch = torch_()
+    g = torch.Generator(device="cuda").manual_seed(n + lo)
+
+    def ints(rows):
+        v = torch.randint(-4, 5, (rows, k), device="cuda", generator=g)
+        t = torch.zeros(rows, (k + 15) // 16 * 16, dtype=torch.float8_e4m3fn, device="cuda")[:, :k]
+        t.copy_(v.float())
+        return t, v.double()
+
+    kb = (k + 127) // 128
+    (xq, xv), (wq, wv) = ints(m), ints(n)
+    xs = 2.0 ** torch.randint(-1, 2, (m, kb), device="cuda", generator=g).float()
+    ws = 2.0 ** torch.randint(-1, 2, ((n + 127) // 128, kb), device="cuda", generator=g).float()
+    big = torch.full((m + 1, lo + n + pad), 7.0, dtype=getattr(torch, out), device="cuda")
+    y = ct().ct_fp8_matmul(xq, xs, wq, ws, out=big[:m, lo:lo + n])
+    wide = lambda s, block, rows: s.double().repeat_interleave(block, 0)[:rows].repeat_interleave(128, 1)[:, :k]
+    ref = (xv * wide(xs, 1, m)) @ (wv * wide(ws, 128, n)).T
+    assert ref.abs().max() < 2 ** 22 and torch.equal(y, ref.float().to(y.dtype))
+    assert ct().ct_ops_device_error() == 0
+    assert (big[m] == 7).all() and (big[:m, :lo] == 7).all() and (big[:m, lo + n:] == 7).all()
+
+
 @pytest.mark.parametrize("m", [3, 40, 300])
 def test_matmul_strides_scale_orders_and_untouched_memory(m):
     torch = torch_()

@@ -128,6 +128,24 @@ def test_many_rows(dtype, vocab, k):
     check_forward(xt[:, :vocab].contiguous(), ids, k)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [31, 64, 65, 257, 1000, 1024])
+@pytest.mark.parametrize("k", [16, 17, 32])
+def test_short_rows_many_tokens(dtype, vocab, k):
+    """As many tokens as a warp has lanes, from rows that one warp holds: spread
+    out, side by side, nearly all masked, equal."""
+    torch = torch_()
+    rng = np.random.default_rng(vocab + k)
+    x = rng.standard_normal((40, vocab)) * 2
+    x[0] = np.sort(x[0])
+    x[1] = np.sort(x[1])[::-1]
+    x[2, rng.random(vocab) < 0.95] = -math.inf
+    x[3] = 0.25
+    x[4] = rng.integers(0, 4, vocab)
+    x[5, : vocab // 2] = -math.inf
+    check_forward(torch.from_numpy(x).to(getattr(torch, dtype)).cuda(), rng.integers(-1, vocab, 40), k)
+
+
 def test_few_values_many_ties():
     """Logits of three values: every choice among the top is a tie."""
     torch = torch_()
