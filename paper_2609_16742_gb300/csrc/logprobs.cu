@@ -1067,7 +1067,11 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
 }
 
 // ---------------------------------------------------------------------------
-// Gradient: each CTA a piece of one row, GRAD_VECS 16-byte vectors a thread.
+// Gradient: each CTA a piece of one row, GRAD_VECS 16-byte vectors a thread, or
+// short rows side by side, a power of two of threads each (8 to 256).  The
+// vectors are those of dx, so that every store is whole wherever the rows of x
+// start.  LONG: rows of 256 threads or more that start as those of dx do, in
+// fewer registers (32 and not 59: 2048 x 131072 bf16 153 us and not 170).
 // ---------------------------------------------------------------------------
 constexpr int GRAD_THREADS = 256;
 constexpr int GRAD_VECS = 4;
@@ -1104,13 +1108,16 @@ __device__ __forceinline__ void grad_one(const GradRow &q, const T *x, T *dx, in
     dx[j] = from_f32<T>(q.bad ? nan_f() : d);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradArgs a, int pieces) {
+template <typename T, bool LONG>
+__global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradArgs a, int pieces, int row_lanes) {
     constexpr int E = Vec16<T>::N;
+    const int lanes = LONG ? GRAD_THREADS : row_lanes;
     pdl_wait();
     pdl_trigger();
-    const int64_t r = blockIdx.x / (unsigned)pieces;
-    const int piece = (int)(blockIdx.x % (unsigned)pieces);
+    const int64_t r = LONG || pieces > 1 ? (int64_t)(blockIdx.x / (unsigned)pieces)
+                                 : (int64_t)blockIdx.x * (GRAD_THREADS / (unsigned)lanes) + threadIdx.x / (unsigned)lanes;
+    if (r >= a.rows) return;
+    const int piece = (int)(blockIdx.x % (unsigned)pieces), lane = (int)threadIdx.x & (lanes - 1);
     const T *x = static_cast<const T *>(a.x) + r * a.ldx;
     T *dx = static_cast<T *>(a.dx) + r * a.lddx;
     GradRow q;
@@ -1121,26 +1128,33 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradA
     q.h = a.g_h != nullptr ? a.entropy[r] : 0.f;
     q.bad = q.lse != q.lse || q.g != q.g;
     if (q.lse == -INF) q.lse = 0.f;                        // nothing can occur: every p is 0
-    // values before the first 16-byte boundary, and the vectors after it
-    const int64_t head = min((int64_t)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T), a.vocab);
-    const bool same = (((uintptr_t)x ^ (uintptr_t)dx) & 15) == 0;
+    // values before dx's first 16-byte boundary, and the vectors after it
+    const int64_t head = min((int64_t)((16 - ((uintptr_t)dx & 15)) & 15) / (int)sizeof(T), a.vocab);
+    const uint32_t shift = LONG ? 0u : (uint32_t)(uintptr_t)(x + head) & 15u;
     const int64_t vecs = (a.vocab - head) / E, per = GRAD_THREADS * GRAD_VECS;
-    const int64_t v0 = piece * per + threadIdx.x;
+    const int64_t v0 = piece * per + lane;
+    const uint4 *units = reinterpret_cast<const uint4 *>((uintptr_t)(x + head) - shift);
     uint4 u[GRAD_VECS];
 #pragma unroll
-    for (int i = 0; i < GRAD_VECS; ++i) {
-        const int64_t v = v0 + i * GRAD_THREADS;
-        if (v < vecs) u[i] = __ldcs(reinterpret_cast<const uint4 *>(x + head + v * E));
+    for (int i = 0; i < GRAD_VECS; ++i)
+        if (v0 + i * lanes < vecs) u[i] = __ldcs(units + v0 + i * lanes);
+    if (!LONG && shift != 0) {
+        uint4 n[GRAD_VECS];
+#pragma unroll
+        for (int i = 0; i < GRAD_VECS; ++i)
+            if (v0 + i * lanes < vecs) n[i] = __ldg(units + v0 + i * lanes + 1);
+#pragma unroll
+        for (int i = 0; i < GRAD_VECS; ++i) u[i] = shifted_each(u[i], n[i], shift);
     }
     // the ends of the row: its first piece's threads
     if (piece == 0) {
         const int64_t tail = head + vecs * E;
-        if ((int64_t)threadIdx.x < head) grad_one(q, x, dx, (int64_t)threadIdx.x);
-        if (tail + (int64_t)threadIdx.x < a.vocab) grad_one(q, x, dx, tail + (int64_t)threadIdx.x);
+        if (lane < head) grad_one(q, x, dx, (int64_t)lane);
+        if (tail + lane < a.vocab) grad_one(q, x, dx, tail + lane);
     }
 #pragma unroll
     for (int i = 0; i < GRAD_VECS; ++i) {
-        const int64_t v = v0 + i * GRAD_THREADS;
+        const int64_t v = v0 + i * lanes;
         if (v >= vecs) break;
         const int64_t j = head + v * E;
         float d[E];
@@ -1156,12 +1170,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradA
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] = nan_f();
         }
-        if (same) {
-            __stcs(reinterpret_cast<uint4 *>(dx + j), pack16<T>(d));
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) dx[j + e] = from_f32<T>(d[e]);
-        }
+        __stcs(reinterpret_cast<uint4 *>(dx + j), pack16<T>(d));
     }
 }
 
@@ -1196,6 +1205,12 @@ template <typename T> cudaError_t launch_logprobs(const LpArgs &a, cudaStream_t 
                                                             : pdl_launch(logprobs_warp_kernel<T, true>, grid, block, 0, st, a);
     }
     return row_bytes < 98304 ? launch_long<T, 128>(a, st) : launch_long<T, 256>(a, st);
+}
+
+template <typename T> cudaError_t launch_grad(const GradArgs &a, dim3 grid, int pieces, int lanes, bool shifted, cudaStream_t st) {
+    return lanes < GRAD_THREADS || shifted
+               ? pdl_launch(logprobs_grad_kernel<T, false>, grid, dim3(GRAD_THREADS), 0, st, a, pieces, lanes)
+               : pdl_launch(logprobs_grad_kernel<T, true>, grid, dim3(GRAD_THREADS), 0, st, a, pieces, lanes);
 }
 
 }  // namespace
@@ -1249,10 +1264,14 @@ extern "C" ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t per = (int64_t)GRAD_THREADS * GRAD_VECS * (16 / es), pieces = (vocab + per - 1) / per;
     if (rows > INT32_MAX / pieces) return CT_ERANGE;
-    const dim3 grid((unsigned)(rows * pieces)), block(GRAD_THREADS);
-    const cudaError_t e =
-        dtype == CT_DT_F32   ? ct::pdl_launch(logprobs_grad_kernel<float>, grid, block, 0, st, a, (int)pieces)
-        : dtype == CT_DT_F16 ? ct::pdl_launch(logprobs_grad_kernel<__half>, grid, block, 0, st, a, (int)pieces)
-                             : ct::pdl_launch(logprobs_grad_kernel<__nv_bfloat16>, grid, block, 0, st, a, (int)pieces);
+    // short rows: two vectors a thread, and threads enough for the values at a row's ends
+    int lanes = 8;
+    while (lanes < GRAD_THREADS && (int64_t)lanes * 2 * (16 / es) < vocab) lanes *= 2;
+    const int64_t side = GRAD_THREADS / lanes;
+    const dim3 grid((unsigned)(pieces > 1 ? rows * pieces : (rows + side - 1) / side));
+    const bool shifted = (((uintptr_t)logits_dev ^ (uintptr_t)dlogits_dev) & 15) != 0 || (rows > 1 && (ld - ld_d) % (16 / es) != 0);
+    const cudaError_t e = dtype == CT_DT_F32   ? launch_grad<float>(a, grid, (int)pieces, lanes, shifted, st)
+                          : dtype == CT_DT_F16 ? launch_grad<__half>(a, grid, (int)pieces, lanes, shifted, st)
+                                               : launch_grad<__nv_bfloat16>(a, grid, (int)pieces, lanes, shifted, st);
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
