@@ -246,6 +246,26 @@ def test_gradient_strides():
     assert (buf == 9.0).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [1, 5, 40, 300, 2500, 9001])
+@pytest.mark.parametrize("lo,to", [(0, 1), (1, 0), (3, 5), (7, 7), (2, 10)])
+def test_gradient_starts(dtype, vocab, lo, to):
+    """Logits and gradients whose rows start anywhere: what contiguous ones
+    give, and nothing beside it."""
+    torch = torch_()
+    rows = 67
+    base = torch.randn(rows, vocab + 11, device="cuda").to(getattr(torch, dtype))
+    ids = torch.arange(rows, device="cuda") % vocab
+    one = torch.ones(rows, device="cuda")
+    x = base[:, lo:lo + vocab]
+    _, h, lse, _, _ = ct().ct_logprobs(x, ids)
+    buf = torch.full((rows, vocab + 13), 9.0, dtype=x.dtype, device="cuda")
+    ct().ct_logprobs_grad(x, ids, lse, h, one, one, out=buf[:, to:to + vocab])
+    assert torch.equal(buf[:, to:to + vocab], ct().ct_logprobs_grad(x.contiguous(), ids, lse, h, one, one))
+    buf[:, to:to + vocab] = 9.0
+    assert (buf == 9.0).all()
+
+
 def test_gradient_against_differences():
     """Central differences of the forward kernel, step e = 2^-6: truncation
     e^2 / 6 times a third derivative of at most 6 (|g| + |gh| (8 + entropy)),
