@@ -21,17 +21,20 @@
 //   wide (many rows): rows of x on the TMEM lanes, tiles of 256 rows x BN
 //     columns on CTA pairs (cta_group::2: each CTA stages half of both
 //     operands), persistent; the factor of a thread's values is one product
-//     per block;
+//     per block.  A K block of 256 columns takes ~790 cycles, of which the MMAs
+//     need 512: the epilogue's loads from TMEM and additions set the pace (16
+//     epilogue warps instead of 8 make it slower, 262 us and more against 201).
+//     8192 x 8192 x 4096 to BF16 in 201 us, 2.73 PFLOP/s;
 //   narrow (few rows): rows of w on the lanes, 128 x BN tiles with BN as
 //     narrow as the rows allow, so that a few rows cost no 128-wide tile; the
 //     K range is split over a cluster of up to 8 CTAs so that the whole GPU
 //     streams the weights, and the cluster adds its partial sums through
 //     distributed shared memory, in rank order: no workspace, no atomics, one
-//     launch, the same bits each time.
+//     launch, the same bits each time.  Bound by HBM with a start of ~3 us and a
+//     join of ~2: 64 x 4096 x 25088 in 21 us, 4.9 TB/s of weights.
 #include <atomic>
 #include <cudaTypedefs.h>
 #include <math.h>
-#include <string.h>
 
 #include "ops_common.cuh"
 #include "tc_common.cuh"

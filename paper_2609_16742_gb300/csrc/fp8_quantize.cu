@@ -76,7 +76,7 @@ __device__ __forceinline__ void load_any(const QuantArgs &a, int64_t r0, int64_t
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i)
-            u[h + i] = first_bytes(shifted_each(first[i], second[i], (uint32_t)(p0 + (h + i) * pitch) & 15u), bytes);
+            u[h + i] = first_bytes(shifted(first[i], second[i], (uint32_t)(p0 + (h + i) * pitch) & 15u), bytes);
     }
 }
 
@@ -143,8 +143,10 @@ constexpr int ROW_THREADS = 256;
 // an exchange that halves the rows a lane keeps with each of its first three
 // steps, so that each lane ends with one row's, makes that row's scale, and
 // passes it round (8 + 8 shuffles and one scale a lane; row by row it was 32 to
-// 40 and 8, 107 instructions for 128 FP32 values).  Where the scales lie block by block, the 8
-// are one 32-byte sector.
+// 40 and 8, 107 instructions for 128 FP32 values).  Where the scales lie block
+// by block, the 8 are one 32-byte sector.
+// Bound by HBM: 8192 x 4096 BF16 in 14.5 us, 6.9 TB/s.  Rows that start inside
+// a 16-byte unit cost instructions: 5000 x 3001 BF16 in 13.6 us, 3.3 TB/s.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(ROW_THREADS, 4) quantize_rows_kernel(const QuantArgs a) {
     static_assert(ROWS == 1 || ROWS == 8, "one row, or the exchange's 8");
@@ -225,7 +227,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 4) quantize_rows_kernel(const Qua
 constexpr int BLOCK_THREADS = 512;
 
 // One CTA per 128 x 128 block: its values stay in registers between the
-// maximum and the rounding.
+// maximum and the rounding, so that HBM is read once and bounds it:
+// 4096 x 25088 FP32 in 78.3 us, 6.6 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(BLOCK_THREADS, 2) quantize_blocks_kernel(const QuantArgs a) {
     constexpr int V = Vec16<T>::N;

@@ -310,6 +310,10 @@ template <typename T> __device__ __forceinline__ float given_logit(const LpArgs 
 // top_k logits reach the top_k-th largest of the lanes' maxima; those that do
 // are listed in shared memory and sorted by counting.  Where ties overflow
 // the list, the next token is the warp's largest key below the last one.
+// One warp because a row is 2 to 4 KB: no exchange through shared memory, no
+// barrier.  Bound by latency for few rows (256 x 1000 FP32, 5 tokens: 4.6 us,
+// of which the row's load and the launch are half), by instructions for many
+// (8192 x 1000 FP16: 6.4 us without tokens, 14.3 us with 5).
 // ---------------------------------------------------------------------------
 constexpr int SHORT = 1024;
 constexpr int SHORT_WARPS = 4;
@@ -525,7 +529,7 @@ template <typename T, int NT> struct Top {
         return u;
     }
     static __device__ __forceinline__ uint4 words(const Share &q, int64_t v, const Units &u) {
-        uint4 w = shifted_each(u.p, u.n, q.shift);
+        uint4 w = shifted(u.p, u.n, q.shift);
         const int have = (int)max((int64_t)0, min((int64_t)E, q.n - v * E));
         if (have < E) {
             w.x = Words<T>::mask(w.x, have);
@@ -728,7 +732,12 @@ template <typename T, int NT> struct Top {
 
 // ---------------------------------------------------------------------------
 // Many rows of moderate length: one warp each, straight from global memory,
-// VECS vectors a lane on their way while VECS are added.
+// VECS vectors a lane on their way while VECS are added.  A row of the kernel
+// below would fill its last chunk badly and meet its barriers too often.
+// Bound by the exponentials' issue slots and, with few rows a warp, by the last
+// round: 8192 x 16000 BF16 with 8 tokens in 58.7 us, 4.5 TB/s; 5696 x 5714 FP16
+// without tokens in 17.5 us, 3.7 TB/s.  ANY: rows that may start inside a
+// 16-byte unit (96 registers a thread, not 64).
 // ---------------------------------------------------------------------------
 constexpr int ROW_WARPS = 4;
 
@@ -829,7 +838,11 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_ker
 // of 64 bytes a thread.  A producer warp has the bulk engine copy STAGES chunks
 // ahead, the consumer warps take each chunk at their own pace and go on with
 // the next row, and finisher warps, in turn, make a row's results of what they
-// leave of it meanwhile.
+// leave of it meanwhile.  Where there are fewer rows than CTAs a cluster of up to
+// 8 shares a row and one warp joins the shares, in their order.
+// Bound by HBM where rows abound (2048 x 131072 BF16 with 8 tokens in 87 us, 6.2
+// TB/s, without tokens 6.6), by the way from the last value to the result where
+// they do not: 1 x 131072 FP16 takes 4.3 us, with 20 tokens 8.1 us.
 // ---------------------------------------------------------------------------
 
 constexpr int MAX_SPLITS = 8;                              // CTAs that share a row
@@ -1071,7 +1084,9 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
 // short rows side by side, a power of two of threads each (8 to 256).  The
 // vectors are those of dx, so that every store is whole wherever the rows of x
 // start.  LONG: rows of 256 threads or more that start as those of dx do, in
-// fewer registers (32 and not 59: 2048 x 131072 bf16 153 us and not 170).
+// fewer registers (32 and not 59: 2048 x 131072 BF16 153 us and not 170).
+// Bound by HBM, each logit read and each gradient written once: 7.0 TB/s there;
+// short rows by latency (6476 x 15 BF16 in 2.7 us; a CTA a row took 11.6).
 // ---------------------------------------------------------------------------
 constexpr int GRAD_THREADS = 256;
 constexpr int GRAD_VECS = 4;
@@ -1144,7 +1159,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const GradA
         for (int i = 0; i < GRAD_VECS; ++i)
             if (v0 + i * lanes < vecs) n[i] = __ldg(units + v0 + i * lanes + 1);
 #pragma unroll
-        for (int i = 0; i < GRAD_VECS; ++i) u[i] = shifted_each(u[i], n[i], shift);
+        for (int i = 0; i < GRAD_VECS; ++i) u[i] = shifted(u[i], n[i], shift);
     }
     // the ends of the row: its first piece's threads
     if (piece == 0) {

@@ -76,34 +76,9 @@ template <> __device__ __forceinline__ void unpack16<__nv_bfloat16>(const uint4 
     }
 }
 
-// 16 bytes from `shift` bytes on of the 32 in p, n
+// 16 bytes from `shift` bytes on of the 32 in p, n; no branch, so that the loads of several units stay in flight
+// together
 __device__ __forceinline__ uint4 shifted(const uint4 &p, const uint4 &n, uint32_t shift) {
-    const uint32_t bits = (shift & 3u) * 8u;
-    switch (shift >> 2) {
-        case 0:
-            return make_uint4(__funnelshift_r(p.x, p.y, bits), __funnelshift_r(p.y, p.z, bits),
-                              __funnelshift_r(p.z, p.w, bits), __funnelshift_r(p.w, n.x, bits));
-        case 1:
-            return make_uint4(__funnelshift_r(p.y, p.z, bits), __funnelshift_r(p.z, p.w, bits),
-                              __funnelshift_r(p.w, n.x, bits), __funnelshift_r(n.x, n.y, bits));
-        case 2:
-            return make_uint4(__funnelshift_r(p.z, p.w, bits), __funnelshift_r(p.w, n.x, bits),
-                              __funnelshift_r(n.x, n.y, bits), __funnelshift_r(n.y, n.z, bits));
-        default:
-            return make_uint4(__funnelshift_r(p.w, n.x, bits), __funnelshift_r(n.x, n.y, bits),
-                              __funnelshift_r(n.y, n.z, bits), __funnelshift_r(n.z, n.w, bits));
-    }
-}
-
-// 16 bytes from an address `shift` (1 to 15) bytes past a 16-byte boundary: two
-// loads of whole 16-byte units, each of which holds one of those bytes
-__device__ __forceinline__ uint4 load_shifted(const void *p, uint32_t shift) {
-    const uint4 *at = reinterpret_cast<const uint4 *>((uintptr_t)p - shift);
-    return shifted(__ldg(at), __ldg(at + 1), shift);
-}
-
-// `shifted` for lanes whose shifts differ: no branch, so that the loads of several units stay in flight together
-__device__ __forceinline__ uint4 shifted_each(const uint4 &p, const uint4 &n, uint32_t shift) {
     const uint32_t bits = (shift & 3u) * 8u;
     const bool two = shift & 8u, one = shift & 4u;
     uint32_t w[6] = {two ? p.z : p.x, two ? p.w : p.y, two ? n.x : p.z, two ? n.y : p.w, two ? n.z : n.x, two ? n.w : n.y};
