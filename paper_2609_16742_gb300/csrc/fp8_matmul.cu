@@ -30,13 +30,15 @@
 //     K range is split over a cluster of up to 8 CTAs so that the whole GPU
 //     streams the weights, and the cluster adds its partial sums through
 //     distributed shared memory, in rank order: no workspace, no atomics, one
-//     launch, the same bits each time.  Bound by HBM with a start of ~3 us and a
+//     launch, the same bits each time.  For few rows that are not yet in 8 bits
+//     8 more warps quantise them on the way into shared memory (X: their type;
+//     uint8_t: they are in 8 bits).  Bound by HBM with a start of ~3 us and a
 //     join of ~2: 64 x 4096 x 25088 in 21 us, 4.9 TB/s of weights.
 #include <atomic>
 #include <cudaTypedefs.h>
 #include <math.h>
 
-#include "ops_common.cuh"
+#include "fp8_quantize.cuh"
 #include "tc_common.cuh"
 
 namespace ct {
@@ -75,10 +77,21 @@ struct MmArgs {
     int vec;                            // wide: TMA can address y's rows
     int vec4;                           // 4 values of a row of y, from a multiple of 4 on, are one aligned store
     int early;                          // narrow: the kernel before does not write w
+    const void *x;                      // narrow: rows to quantise, their pitch and length
+    int64_t ldx;
+    int K;
     uint32_t *err;
 };
 
-template <int BN> struct Narrow {
+constexpr int QUANT_WARP = 10, N_QUANT = 8;   // narrow: warps that quantise x
+constexpr int X_SLOTS = 16;             // blocks whose scales are kept: more than stages and accumulators together
+
+template <int BN, typename X = uint8_t> struct Narrow {
+    static constexpr bool QUANT = sizeof(X) > 1;
+    static constexpr int THREADS = ct::ops::THREADS + (QUANT ? 32 * N_QUANT : 0);
+    // teams of the quantising warps, which take K blocks in turn, as what a block costs them is latency: 1 x 4096 x
+    // 25088 FP16 in 24.9 us with one team, 20.9 with two, 19.8 with four; as many as leave a lane 4 rows
+    static constexpr int TEAMS = (BN == 16 ? 4 : 2) / (sizeof(X) == 4 ? 2 : 1);
     static constexpr int C_BYTES = BN * BK;
     static constexpr int STAGE = L_BYTES + C_BYTES;
     static constexpr int STAGES = BN == 16 ? 10 : BN == 128 ? 6 : 8;
@@ -91,7 +104,9 @@ template <int BN> struct Narrow {
     static constexpr int CPW = BN / (2 / GROUPS);          // columns of an epilogue warp
     static constexpr int LDN = CPW < 32 ? CPW : 32;        // columns of one TMEM load
     static constexpr int FAC = N_EPI * 2 * CPW * 4;
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16 +
+                                   (QUANT ? X_SLOTS * BN * 4 : 0);
+    static_assert(STAGES + NBUF < X_SLOTS, "a slot is read before it is written again");
 };
 
 template <int N> __device__ __forceinline__ void tmem_ld_nw(uint32_t taddr, uint32_t (&r)[N]) {
@@ -190,10 +205,86 @@ __device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
 // ---------------------------------------------------------------------------
 // narrow: few rows
 // ---------------------------------------------------------------------------
-template <int BN>
-__global__ void __launch_bounds__(THREADS, 1)
+// Blocks `first`, first + 1, ... of x's BN rows from m0 on, quantised into the
+// stages as TMA would put them there; a row's 16 bytes a lane, the next blocks'
+// on their way meanwhile.
+template <int BN, typename X>
+__device__ __forceinline__ void quantize_stages(const MmArgs &a, uint8_t *Cs, float *xsc, uint64_t *full, uint64_t *empty, int m0,
+                                                int first, int nkb) {
+    using S = Narrow<BN, X>;
+    constexpr int TEAMS = S::TEAMS, V = Vec16<X>::N, G = BK / V;            // lanes a row
+    constexpr int SIDE = 32 * N_QUANT / TEAMS / G, N = BN / SIDE;           // rows at once
+    static_assert(BN % SIDE == 0, "whole passes");
+    const int t = ((int)threadIdx.x - 32 * QUANT_WARP) % (32 * N_QUANT / TEAMS), g = t / G, l = t % G;
+    const int team = ((int)threadIdx.x / 32 - QUANT_WARP) / (N_QUANT / TEAMS);
+    const X *rows = static_cast<const X *>(a.x) + (int64_t)(m0 + g) * a.ldx;
+    constexpr int DEPTH = N >= 4 ? 1 : 4 / N;              // blocks on their way together
+    uint4 u[DEPTH][N], n[DEPTH][N];
+    const auto load = [&](int it, int d) {
+        const int c = (first + it) * BK + l * V, bytes = it < nkb ? max(0, min(V, a.K - c)) * (int)sizeof(X) : 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uintptr_t p = reinterpret_cast<uintptr_t>(rows + (int64_t)(i * SIDE) * a.ldx + c);
+            const uint4 *at = reinterpret_cast<const uint4 *>(p & ~(uintptr_t)15);
+            const bool any = bytes > 0 && m0 + g + i * SIDE < a.M;
+            u[d][i] = n[d][i] = make_uint4(0, 0, 0, 0);
+            if (any) u[d][i] = __ldg(at);
+            if (any && (int)(p & 15u) + bytes > 16) n[d][i] = __ldg(at + 1);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(team + d * TEAMS, d);
+    bool ok = true;
+    for (int base = team; base < nkb && ok; base += DEPTH * TEAMS) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int it = base + d * TEAMS, s = it % S::STAGES, c = (first + it) * BK + l * V;
+            if (it >= nkb) break;
+            uint4 w[N];
+            uint32_t mx[N];
+            bool odd = false;                              // something that is not finite
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uintptr_t p = reinterpret_cast<uintptr_t>(rows + (int64_t)(i * SIDE) * a.ldx + c);
+                w[i] = first_bytes(shifted(u[d][i], n[d][i], (uint32_t)p & 15u), max(0, min(V, a.K - c)) * (int)sizeof(X));
+                mx[i] = largest_any<X>(w[i]);
+                odd |= mx[i] >= 0x7F800000u;
+            }
+            load(it + DEPTH * TEAMS, d);
+            if (__any_sync(~0u, odd)) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) mx[i] = largest<X, V>(w[i]);
+            }
+#pragma unroll
+            for (int e = G / 2; e > 0; e /= 2)
+#pragma unroll
+                for (int i = 0; i < N; ++i) mx[i] = max(mx[i], __shfl_xor_sync(~0u, mx[i], e));
+            ok = warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA);
+            if (!ok) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = g + i * SIDE;
+                float scale, inv;
+                block_scale(mx[i], scale, inv);
+                uint32_t q[V / 4];
+                convert<X, V>(w[i], inv, q);
+                uint8_t *to = Cs + s * S::C_BYTES + r * BK + ((l * V / 16) ^ (r & 7)) * 16 + l * V % 16;
+                if constexpr (V == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(q[0], q[1]);
+                else *reinterpret_cast<uint32_t *>(to) = q[0];
+                if (l == 0) xsc[it % X_SLOTS * BN + r] = scale;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(&full[s]));
+        }
+    }
+}
+
+template <int BN, typename X>
+__global__ void __launch_bounds__((Narrow<BN, X>::THREADS), 1)
 fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant__ CUtensorMap cmap, const MmArgs a) {
-    using S = Narrow<BN>;
+    using S = Narrow<BN, X>;
+    constexpr bool QUANT = S::QUANT;
     constexpr int CPW = S::CPW, LDN = S::LDN, STAGES = S::STAGES, NBUF = S::NBUF, GROUPS = S::GROUPS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -205,6 +296,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
     uint64_t *acc_full = empty + STAGES;
     uint64_t *acc_empty = acc_full + NBUF;
     uint32_t *tmem_holder = (uint32_t *)(acc_empty + NBUF);
+    float *xsc = (float *)(tmem_holder + 4);               // QUANT: [slot][row], scales of x's blocks
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)a.splits);
@@ -215,7 +307,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&full[s]), 1 + (QUANT ? N_QUANT / S::TEAMS : 0));
             mbar_init(smem_u32(&empty[s]), 1);
         }
         for (int b = 0; b < NBUF; ++b) {
@@ -238,12 +330,12 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
     if (warp == TMA_WARP) {
         const auto load_l = [&](int i) {
             const int s = i % STAGES;
-            mbar_arrive_expect_tx(smem_u32(&full[s]), (uint32_t)S::STAGE);
+            mbar_arrive_expect_tx(smem_u32(&full[s]), (uint32_t)(QUANT ? L_BYTES : S::STAGE));
             tma_load_2d(smem_u32(Ls + s * L_BYTES), &lmap, smem_u32(&full[s]), (kb0 + i) * BK, tl * BL);
         };
         const auto load_c = [&](int i) {
             const int s = i % STAGES;
-            tma_load_2d(smem_u32(Cs + s * S::C_BYTES), &cmap, smem_u32(&full[s]), (kb0 + i) * BK, tc * BN);
+            if (!QUANT) tma_load_2d(smem_u32(Cs + s * S::C_BYTES), &cmap, smem_u32(&full[s]), (kb0 + i) * BK, tc * BN);
         };
         // the weights of the first stages may be on their way while the kernel before still quantises x
         const int ahead = a.early ? min(STAGES, nkb) : 0;
@@ -284,6 +376,9 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
             }
         }
         __syncwarp();
+    } else if (QUANT && warp >= QUANT_WARP) {
+        pdl_wait();
+        if constexpr (QUANT) quantize_stages<BN, X>(a, Cs, xsc, full, empty, tc * BN, kb0, nkb);
     } else {
         pdl_wait();
         const int quad = warp & 3, half = warp >> 2;
@@ -315,7 +410,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
                 const bool in = i + u * GROUPS < nkb;
                 const int64_t kb = kb0 + i + u * GROUPS;
 #pragma unroll
-                for (int j = 0; j < NF; ++j) nx[u][j] = in && xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
+                for (int j = 0; j < NF; ++j) nx[u][j] = QUANT ? 1.f : in && xin[j] ? __ldg(xp[j] + kb * a.xs_blk) : 0.f;
                 nw[u] = in ? __ldg(wp + kb * a.ws_blk) : 0.f;
             }
         };
@@ -334,12 +429,20 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
                 const int it = its + u * GROUPS, b = it % NBUF;
                 if (it >= nkb) break;
                 float *fs = fac + (warp * 2 + (u & 1)) * CPW;
+                if (!QUANT) {
 #pragma unroll
-                for (int j = 0; j < NF; ++j)
-                    if (j * 32 + lane < CPW) fs[j * 32 + lane] = f[u][j];
-                __syncwarp();
+                    for (int j = 0; j < NF; ++j)
+                        if (j * 32 + lane < CPW) fs[j * 32 + lane] = f[u][j];
+                    __syncwarp();
+                }
                 ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
                 if (!ok) break;
+                if (QUANT) {                               // x's scales are there with the block
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+                        if (j * 32 + lane < CPW) fs[j * 32 + lane] = f[u][j] * xsc[it % X_SLOTS * BN + cw + j * 32 + lane];
+                    __syncwarp();
+                }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                 for (int c = 0; c < CPW; c += LDN) {
@@ -944,11 +1047,12 @@ bool encode8(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t k, int64_
 }
 
 // (the kernels' shared memory was allowed when choose() asked for their residency)
-template <int BN>
+template <int BN, typename X = uint8_t>
 cudaError_t launch_narrow(const CUtensorMap &lmap, const CUtensorMap &cmap, const MmArgs &a, int grid, cudaStream_t st) {
+    using S = Narrow<BN, X>;
     if (a.splits == 1)
-        return pdl_launch(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Narrow<BN>::SMEM, st, lmap, cmap, a);
-    return pdl_launch_cluster(fp8_narrow_kernel<BN>, dim3((unsigned)grid), dim3(THREADS), Narrow<BN>::SMEM, st, a.splits,
+        return pdl_launch(fp8_narrow_kernel<BN, X>, dim3((unsigned)grid), dim3(S::THREADS), S::SMEM, st, lmap, cmap, a);
+    return pdl_launch_cluster(fp8_narrow_kernel<BN, X>, dim3((unsigned)grid), dim3(S::THREADS), S::SMEM, st, a.splits,
                               lmap, cmap, a);
 }
 
@@ -1005,8 +1109,8 @@ constexpr int W_COLS[4] = {64, 128, 192, 256};
 // [dev][log2 of the columns / 16][index of the split], [dev][index of the columns][splits - 1]
 std::atomic<int> g_narrow[MAX_DEVICES][4][N_SPLITS], g_wide[MAX_DEVICES][4][2];
 
-template <int BN> int narrow_resident(int splits, std::atomic<int> &known) {
-    return resident(fp8_narrow_kernel<BN>, THREADS, Narrow<BN>::SMEM, splits, known);
+template <int BN, typename X = uint8_t> int narrow_resident(int splits, std::atomic<int> &known) {
+    return resident(fp8_narrow_kernel<BN, X>, Narrow<BN, X>::THREADS, Narrow<BN, X>::SMEM, splits, known);
 }
 template <int BN> int wide_resident(int splits, std::atomic<int> &known) {
     return splits == 1 ? resident(fp8_wide_kernel<BN, false>, W_THREADS, Wide<BN>::SMEM, 2, known)
@@ -1017,7 +1121,23 @@ struct Choice {
     bool wide;
     int bn, splits;
     int ctas;               // that run at once
+    double us;              // estimate
 };
+
+// figures of the estimate, see choose()
+constexpr double N_BLOCK[4] = {0.2, 0.25, 0.33, 0.5}, N_TILE[4] = {1.0, 1.3, 2.7, 3.3};
+constexpr double N_SPLIT[N_SPLITS] = {0, 1.4, 1.7, 2.0, 2.2, 2.2};
+
+// of the narrow kernel with tiles of 16 << i columns and split q; `block`: a K block's us
+double narrow_us(int M, int N, int KB, int sms, int i, int q, int ctas, double block) {
+    const int bn = 16 << i, s = NARROW_SPLITS[q];
+    const int64_t tiles = (int64_t)((N + 127) / 128) * ((M + bn - 1) / bn);
+    const double nkb = (KB + s - 1) / s, all = (double)tiles * s, busy = all < sms ? all : sms;
+    const double rounds = (double)((tiles * s + ctas - 1) / ctas);
+    const double l2 = all * nkb * (BL + bn) * BK / 9e6;
+    const double hbm = (double)N * KB * BK / (busy < 110 ? 58e3 * busy : 6.4e6);
+    return rounds * N_TILE[i] + (rounds - 1) + N_SPLIT[q] + fmax(rounds * nkb * block, fmax(l2, hbm));
+}
 
 // Which kernel, how wide its tiles, over how many CTAs (pairs) K is split: the
 // least of an estimate in us.  Its figures were measured by timing every
@@ -1031,11 +1151,8 @@ struct Choice {
 //   No kernel is faster than its operands: 9 to 11 bytes a ns from L2, 6.4 of
 //   weights from HBM, 58 bytes a ns to one SM.
 Choice choose(int M, int N, int KB, int sms, int dev) {
-    static const double n_block[4] = {0.2, 0.25, 0.33, 0.5}, n_tile[4] = {1.0, 1.3, 2.7, 3.3};
-    static const double n_split[N_SPLITS] = {0, 1.4, 1.7, 2.0, 2.2, 2.2};
     static const double w_block[4] = {0.2, 0.28, 0.385, 0.41};
-    Choice best = {false, 16, 1, 0};
-    double least = 1e30;
+    Choice best = {false, 16, 1, 0, 1e30};
     const double weights = (double)N * KB * BK;
     const int64_t rows_n = (N + 127) / 128, rows_m = (M + 2 * BL - 1) / (2 * BL);
     for (int i = 0; i < 4; ++i) {
@@ -1051,12 +1168,8 @@ Choice choose(int M, int N, int KB, int sms, int dev) {
                              : bn == 64 ? narrow_resident<64>(s, known)
                                         : narrow_resident<128>(s, known);
             if (ctas == 0) continue;
-            const double nkb = (KB + s - 1) / s, all = (double)tiles * s, busy = all < sms ? all : sms;
-            const double rounds = (double)((tiles * s + ctas - 1) / ctas);
-            const double l2 = all * nkb * (BL + bn) * BK / 9e6;
-            const double hbm = weights / (busy < 110 ? 58e3 * busy : 6.4e6);
-            const double t = rounds * n_tile[i] + (rounds - 1) + n_split[q] + fmax(rounds * nkb * n_block[i], fmax(l2, hbm));
-            if (t < least) { least = t; best = Choice{false, bn, s, ctas}; }
+            const double t = narrow_us(M, N, KB, sms, i, q, ctas, N_BLOCK[i]);
+            if (t < best.us) best = Choice{false, bn, s, ctas, t};
         }
     }
     for (int i = 0; i < 4 && M > 64; ++i) {
@@ -1074,13 +1187,63 @@ Choice choose(int M, int N, int KB, int sms, int dev) {
             const double l2 = (double)tiles * s * nkb * (2 * BL + bn) * BK / 11e6;
             const double t = 3.6 + 0.0047 * bn + (s > 1 ? 3.5 : 0) +
                              fmax(rounds * nkb * w_block[i] + (rounds - 1) * 0.8, fmax(l2, weights / 6.4e6));
-            if (t < least) { least = t; best = Choice{true, bn, s, ctas}; }
+            if (t < best.us) best = Choice{true, bn, s, ctas, t};
         }
     }
     return best;
 }
 
-ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
+// The same for the kernels that quantise rows of X: one launch less (LAUNCH us),
+// no 8-bit copy, but each CTA quantises the rows it multiplies, which sets the
+// pace of long K: only tiles of 16 and 32 columns do.  In one launch and in two:
+// 256 x 1000 x 512 FP16 5.0 and 5.7 us, 500 x 500 x 500 5.1 and 7.6, 1 x 4096 x
+// 25088 19.8 and 20.9, 256 x 1000 x 4096 13.2 and 10.4.
+constexpr double LAUNCH = 2.0;
+constexpr double Q_BLOCK[2][2] = {{0.35, 0.65}, {0.5, 0.95}};   // 16-bit, FP32 rows
+std::atomic<int> g_quant[MAX_DEVICES][3][2][N_SPLITS];     // [dev][type][log2 of the columns / 16][index of the split]
+
+// It adds in the order that `two`, the choice for 8-bit rows, does: the same
+// bits, so the same split of K over CTAs and, within one, over epilogue halves.
+template <typename X> Choice choose_quantising(const Choice &two, int M, int N, int KB, int sms, int dev, int type) {
+    Choice best = {false, 16, two.splits, 0, 1e30};
+    if (two.ctas == 0 || two.wide || Narrow<16, X>::GROUPS != (two.bn <= 64 ? 2 : 1)) return best;
+    int q = 0;
+    while (NARROW_SPLITS[q] != two.splits) ++q;
+    for (int i = 0; i < 2; ++i) {
+        const int bn = 16 << i;
+        if (bn > 16 && bn / 2 >= M) break;
+        std::atomic<int> &known = g_quant[dev][type][i][q];
+        const int ctas = bn == 16 ? narrow_resident<16, X>(two.splits, known) : narrow_resident<32, X>(two.splits, known);
+        if (ctas == 0) continue;
+        const double t = narrow_us(M, N, KB, sms, i, q, ctas, Q_BLOCK[sizeof(X) == 4][i]);
+        if (t < best.us) best = Choice{false, bn, two.splits, ctas, t};
+    }
+    return best;
+}
+
+// quantises and multiplies in one launch, where that is estimated to take less than `us`; false: it is not
+template <typename X>
+bool quantise_and_multiply(MmArgs a, const Operands &o, const Choice &two, int dev, int type, double us, cudaStream_t st,
+                           ct_status *done) {
+    const Choice ch = choose_quantising<X>(two, a.M, a.N, a.KB, sm_count(), dev, type);
+    a.tiles_l = (a.N + 127) / 128;
+    a.tiles_c = (a.M + ch.bn - 1) / ch.bn;
+    const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
+    if (ch.us >= us || tiles > INT32_MAX / 16) return false;
+    a.splits = ch.splits;
+    a.err = device_error_word();
+    CUtensorMap lmap;
+    if (a.err == nullptr || !encode8(&lmap, o.wq, a.N, o.k, o.ldw, BL)) {
+        *done = CT_ECUDA;
+        return true;
+    }
+    const int grid = (int)tiles * a.splits;
+    const cudaError_t e = ch.bn == 16 ? launch_narrow<16, X>(lmap, lmap, a, grid, st) : launch_narrow<32, X>(lmap, lmap, a, grid, st);
+    *done = e == cudaSuccess ? CT_OK : CT_ECUDA;
+    return true;
+}
+
+ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st, const Choice *chosen = nullptr) {
     if (a.KB == 0) {
         const int64_t grid = ((int64_t)a.M * a.N + 255) / 256;
         return pdl_launch(bias_only_kernel, dim3((unsigned)(grid < 65536 ? grid : 65536)), dim3(256), 0, st, a) == cudaSuccess
@@ -1089,12 +1252,11 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st) {
     }
     a.err = device_error_word();
     if (a.err == nullptr) return CT_ECUDA;
-    const int sms = sm_count();
     CUtensorMap lmap, cmap;
     cudaError_t e;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return CT_ECUDA;
-    const Choice ch = choose(a.M, a.N, a.KB, sms, dev);
+    const Choice ch = chosen != nullptr ? *chosen : choose(a.M, a.N, a.KB, sm_count(), dev);
     if (ch.ctas == 0) return CT_ECUDA;
     const int bn = ch.bn;
     a.splits = ch.splits;
@@ -1204,13 +1366,25 @@ extern "C" ct_status ct_fp8_linear(const void *x_dev, int32_t x_dtype, int64_t l
     if (x_dev == nullptr || ldx < k || !aligned(x_dev, dtype_size(x_dtype))) return CT_EINVAL;
     if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
     if (workspace_bytes < need) return CT_ENOMEM;
+    a.x = x_dev; a.ldx = ldx; a.K = (int)k;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return CT_ECUDA;
+    const Choice two = choose(a.M, a.N, a.KB, sm_count(), dev);
+    const double apart = two.us + LAUNCH + (double)m * k * (dtype_size(x_dtype) + 1) / 6e6;
+    const Operands w = {nullptr, 0, w_dev, ldw, k};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ct_status done = CT_OK;
+    if (x_dtype == CT_DT_F32   ? quantise_and_multiply<float>(a, w, two, dev, 0, apart, st, &done)
+        : x_dtype == CT_DT_F16 ? quantise_and_multiply<__half>(a, w, two, dev, 1, apart, st, &done)
+                               : quantise_and_multiply<__nv_bfloat16>(a, w, two, dev, 2, apart, st, &done))
+        return done;
     uint8_t *q = static_cast<uint8_t *>(workspace_dev);
     float *xs = reinterpret_cast<float *>(q + scales_at(m, k));
-    const ct_status r = quantize(x_dev, x_dtype, m, k, ldx, 1, q, q_pitch(k), xs, 1, m, static_cast<cudaStream_t>(stream));
+    const ct_status r = quantize(x_dev, x_dtype, m, k, ldx, 1, q, q_pitch(k), xs, 1, m, st);
     if (r != CT_OK) return r;
     a.xs = xs; a.xs_row = 1; a.xs_blk = m;
     // the quantisation lets this kernel start only after all work before itself
     // is complete, and does not write w
     a.early = 1;
-    return matmul(a, Operands{q, q_pitch(k), w_dev, ldw, k}, static_cast<cudaStream_t>(stream));
+    return matmul(a, Operands{q, q_pitch(k), w_dev, ldw, k}, st, &two);
 }

@@ -264,6 +264,35 @@ def test_linear_is_quantize_then_matmul(dtype, m, n, k):
     assert ((y.double() - ref).abs() <= 0.13 * mag + 0.01 * ref.abs() + 1e-3).all()
 
 
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 130, 5003), (7, 1000, 25088), (16, 128, 128), (17, 129, 127), (33, 64, 3000),
+                                   (100, 500, 300), (256, 1000, 512), (500, 500, 500), (1000, 100, 1000)])
+def test_linear_of_rows_anywhere(dtype, m, n, k):
+    """The two calls' bits, from rows that start anywhere beside values that must
+    not be read as theirs, with masked, empty and poisoned rows; called back to
+    back."""
+    torch = torch_()
+    c = ct()
+    g = torch.Generator(device="cuda").manual_seed(m + k)
+    base = torch.full((m, k + 9), float("nan"), device="cuda").to(getattr(torch, dtype))
+    wq, ws = c.ct_fp8_quantize(torch.randn(n, k, device="cuda", generator=g), 128)
+    bias = torch.randn(n, device="cuda", generator=g)
+    for lo in (0, 1, 4, 8):
+        x = base[:, lo:lo + k]
+        x.copy_(torch.randn(m, k, device="cuda", generator=g))
+        x[m // 2, :k // 2] = 0
+        if m > 3:
+            x[1], x[2, k // 3], x[3, k - 1] = 0, float("inf"), float("nan")
+        z = c.ct_fp8_matmul(*c.ct_fp8_quantize(x), wq, ws, bias=bias, relu=True, out_dtype=x.dtype)
+        for _ in range(5):
+            y = c.ct_fp8_linear(x, wq, ws, bias=bias, relu=True)
+            assert torch.equal(y.nan_to_num(7.0), z.nan_to_num(7.0)) and torch.equal(y.isnan(), z.isnan())
+        assert c.ct_ops_device_error() == 0
+        if m > 3:
+            assert y[2:4].isnan().all() and not y[1].isnan().any()
+        x.fill_(float("nan"))
+
+
 def test_input_gradient_is_the_product_with_transposed_weights():
     """dx = dy W from the transposed 8-bit weights: the same numbers as the
     64-bit product with the weights the forward pass used, and the directional
