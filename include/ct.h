@@ -534,7 +534,8 @@ ct_status ct_fp8_matmul(const uint8_t *x_dev, int64_t ldx, const float *x_scale_
 
 /* ct_fp8_linear -- a fully-connected layer with 8-bit weights on unquantised
  * activations: ct_fp8_quantize of x (blocks of 1 x 128) and ct_fp8_matmul,
- * with the same results.  workspace_dev (16-byte aligned, at least
+ * with the same results, in one launch where that takes less (few rows or short
+ * ones; the workspace is then not used).  workspace_dev (16-byte aligned, at least
  * ct_fp8_linear_workspace(m, k) bytes) is scratch that must not be used by
  * other work until this call's stream work is done.
  * Errors: those of the two calls; CT_ENOMEM for too small a workspace. */
