@@ -578,7 +578,7 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
                            const float *g_entropy_dev, void *dlogits_dev, int64_t ld_d, void *stream);
 
 /* ct_ops_device_error -- reads and clears the current device's error word of
- * these operators (set by a product whose bounded wait expired: its output
+ * these operators (set by a call whose bounded wait expired: its output
  * is then invalid).  Synchronises the device. */
 ct_status ct_ops_device_error(uint32_t *code);
 

@@ -834,7 +834,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     xp[i] = a.xs + (int64_t)min(m0 + 32 * i, a.M - 1) * a.xs_row + kb0 * a.xs_blk;
-                    wp[i] = a.ws + (int64_t)min(BN == 192 ? tc * BN / 128 + i : (tc * BN + i * CPW) / 128, last) * a.ws_row + kb0 * a.ws_blk;
+                    wp[i] = a.ws + (int64_t)min(BN == 192 ? tc * BN / 128 + i : (tc * BN + i * CPW) / 128, last) * a.ws_row +
+                            kb0 * a.ws_blk;
                 }
                 float x[DEPTH][2], w[DEPTH][2];
                 const auto load = [&](int kb, int u) {
@@ -948,7 +949,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < LDN / 2; ++i) fma2(acc[c / 2 + i], f[GROUPS == 1 ? 0 : (c + 2 * i) / 32], r[h][2 * i], r[h][2 * i + 1]);
+                    for (int i = 0; i < LDN / 2; ++i)
+                        fma2(acc[c / 2 + i], f[GROUPS == 1 ? 0 : (c + 2 * i) / 32], r[h][2 * i], r[h][2 * i + 1]);
                 }
             }
             // After a wait that ran out, which is reported, the output is invalid;
@@ -960,7 +962,8 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constant_
                 float *part = (float *)smem + (quad * 32 + lane) * S::PITCH + half * CPW;
                 asm volatile("bar.sync 1, %0;" ::"n"(N_EPI * 32) : "memory");
 #pragma unroll
-                for (int i = 0; i < CPW / 2; i += 2) *reinterpret_cast<ulonglong2 *>(part + 2 * i) = make_ulonglong2(acc[i], acc[i + 1]);
+                for (int i = 0; i < CPW / 2; i += 2)
+                    *reinterpret_cast<ulonglong2 *>(part + 2 * i) = make_ulonglong2(acc[i], acc[i + 1]);
             } else {
                 finish_row<CPW>(a, acc, c0);
                 if (a.vec) {

@@ -358,7 +358,8 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
     for (int i = 0; i < NW; i += 4) {
         if (i / 4 * 32 * E >= vocab) break;
         uint32_t part[4] = {w[i], w[i + 1], w[i + 2], w[i + 3]};
-        const float ta = Words<T>::largest(Words<T>::max2(w[i], w[i + 2])), tb = Words<T>::largest(Words<T>::max2(w[i + 1], w[i + 3]));
+        const float ta = Words<T>::largest(Words<T>::max2(w[i], w[i + 2]));
+        const float tb = Words<T>::largest(Words<T>::max2(w[i + 1], w[i + 3]));
         sums.add(part, fmaxf(ta, tb));
         ga = fmaxf(ga, ta);
         gb = fmaxf(gb, tb);
@@ -742,7 +743,9 @@ template <typename T, int NT> struct Top {
 constexpr int ROW_WARPS = 4;
 
 // VECS vectors that start `shift` (1 to 15) bytes into their first unit
-template <int WS> __device__ __forceinline__ void shift_words(const uint4 (&x)[VECS], const uint4 (&next)[VECS], uint32_t bits, uint32_t (&w)[4 * VECS]) {
+template <int WS>
+__device__ __forceinline__ void shift_words(const uint4 (&x)[VECS], const uint4 (&next)[VECS], uint32_t bits,
+                                            uint32_t (&w)[4 * VECS]) {
 #pragma unroll
     for (int u = 0; u < VECS; ++u) {
         const uint32_t s[8] = {x[u].x, x[u].y, x[u].z, x[u].w, next[u].x, next[u].y, next[u].z, next[u].w};
@@ -750,7 +753,8 @@ template <int WS> __device__ __forceinline__ void shift_words(const uint4 (&x)[V
         for (int i = 0; i < 4; ++i) w[4 * u + i] = __funnelshift_r(s[WS + i], s[WS + i + 1], bits);
     }
 }
-__device__ __forceinline__ void shift_all(const uint4 (&x)[VECS], const uint4 (&next)[VECS], uint32_t shift, uint32_t (&w)[4 * VECS]) {
+__device__ __forceinline__ void shift_all(const uint4 (&x)[VECS], const uint4 (&next)[VECS], uint32_t shift,
+                                          uint32_t (&w)[4 * VECS]) {
     const uint32_t bits = (shift & 3u) * 8u;
     if (shift < 4) shift_words<0>(x, next, bits, w);
     else if (shift < 8) shift_words<1>(x, next, bits, w);
@@ -1064,7 +1068,9 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
             uint64_t best[MAX_SPLITS];
 #pragma unroll
             for (int p = 0; p < MAX_SPLITS; ++p)
-                best[p] = p < splits && lane < k ? ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[lane]), (uint32_t)p)) : 0;
+                best[p] = p < splits && lane < k
+                              ? ld_cluster_u64(tc::mapa_shared(tc::smem_u32(&sh.scratch[0].best[lane]), (uint32_t)p))
+                              : 0;
             const RowResult q = row_result(warp_merge(st));
             if (lane == 0) write_row(a, cid, q, sh.id, sh.given);
             if (k > 0) {
@@ -1222,7 +1228,8 @@ template <typename T> cudaError_t launch_logprobs(const LpArgs &a, cudaStream_t 
     return row_bytes < 98304 ? launch_long<T, 128>(a, st) : launch_long<T, 256>(a, st);
 }
 
-template <typename T> cudaError_t launch_grad(const GradArgs &a, dim3 grid, int pieces, int lanes, bool shifted, cudaStream_t st) {
+template <typename T>
+cudaError_t launch_grad(const GradArgs &a, dim3 grid, int pieces, int lanes, bool shifted, cudaStream_t st) {
     return lanes < GRAD_THREADS || shifted
                ? pdl_launch(logprobs_grad_kernel<T, false>, grid, dim3(GRAD_THREADS), 0, st, a, pieces, lanes)
                : pdl_launch(logprobs_grad_kernel<T, true>, grid, dim3(GRAD_THREADS), 0, st, a, pieces, lanes);
@@ -1284,7 +1291,8 @@ extern "C" ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int
     while (lanes < GRAD_THREADS && (int64_t)lanes * 2 * (16 / es) < vocab) lanes *= 2;
     const int64_t side = GRAD_THREADS / lanes;
     const dim3 grid((unsigned)(pieces > 1 ? rows * pieces : (rows + side - 1) / side));
-    const bool shifted = (((uintptr_t)logits_dev ^ (uintptr_t)dlogits_dev) & 15) != 0 || (rows > 1 && (ld - ld_d) % (16 / es) != 0);
+    const bool shifted = (((uintptr_t)logits_dev ^ (uintptr_t)dlogits_dev) & 15) != 0 ||
+                         (rows > 1 && (ld - ld_d) % (16 / es) != 0);
     const cudaError_t e = dtype == CT_DT_F32   ? launch_grad<float>(a, grid, (int)pieces, lanes, shifted, st)
                           : dtype == CT_DT_F16 ? launch_grad<__half>(a, grid, (int)pieces, lanes, shifted, st)
                                                : launch_grad<__nv_bfloat16>(a, grid, (int)pieces, lanes, shifted, st);
