@@ -3,7 +3,10 @@
 //
 // With m the row's maximum, Z = sum e^(x - m) and T = sum e^(x - m) (x - m):
 //   lse = m + log Z,   log p[j] = x[j] - lse,   entropy = log Z - T / Z
-// (both terms of the entropy are >= 0: nothing cancels).  A forbidden token
+// (both terms of the entropy are >= 0: nothing cancels, so a confident row's
+// entropy, next to 0, keeps its digits).  A running m is a warp's largest logit
+// so far, the same for its lanes; warps' sums are joined relative to the
+// largest of theirs, which is the row's.  A forbidden token
 // (logit -inf) has probability 0 and adds nothing; where e^(x - m) is 0 the
 // product with x - m is taken as 0, also when x - m overflows to -inf (a mask
 // of the type's lowest value).  Sums are held in FP32.
@@ -54,8 +57,8 @@ __device__ __forceinline__ float ex2(float v) {
     return r;
 }
 
-// Running sums of a set of logits relative to m, one of its logits near the
-// largest, in units of log 2: z = sum 2^u, t = sum 2^u u, u = (x - m) log2(e).
+// Running sums of a set of logits relative to m, the largest of them, in units of
+// log 2: z = sum 2^u, t = sum 2^u u, u = (x - m) log2(e).
 // m = -inf: nothing but -inf so far.
 struct Stat {
     float m, z, t;
@@ -180,8 +183,9 @@ template <typename T> __device__ __noinline__ float2 slow_terms(uint32_t w0, uin
     return r;
 }
 
-// Sums of one thread, relative to one of its logits, m; one more than 8 above it
-// takes its place.
+// Sums of one thread, relative to the largest logit that its warp has met so
+// far, m: a larger one takes its place, once for all lanes.  (With a reference for
+// each lane some lane's changes at nearly every step, and the warp waits for it.)
 //
 // The sums are taken with v = x log2(e) - c, c = m log2(e) rounded: one
 // instruction.  v differs from u by what c was rounded by, the same for every
@@ -191,7 +195,7 @@ template <typename T> __device__ __noinline__ float2 slow_terms(uint32_t w0, uin
 // Where |m| > MODERATE the rounding of c would matter or the type has no such
 // value; there c is 0 and the terms are taken one by one from x - m.
 template <typename T> struct Sums {
-    float m, lim;              // reference; the largest logit it stands for (-inf: none yet)
+    float m, lim;              // reference (0: none yet); the largest logit so far (-inf: none yet)
     float c;
     uint32_t low;
     uint64_t z, t;             // even and odd values'
@@ -205,7 +209,7 @@ template <typename T> struct Sums {
     static __device__ __forceinline__ bool moderate(float m) { return fabsf(m) <= Words<T>::MODERATE; }
     // v - u
     __device__ __forceinline__ float rounded() const { return moderate(m) ? fmaf(m, LOG2E, -c) : 0.f; }
-    __device__ __forceinline__ void raise(float top) {     // top > lim: the largest logit so far
+    __device__ __forceinline__ void raise(float top) {     // top > lim
         const float cn = moderate(top) ? top * LOG2E : 0.f;
         if (lim > -INF) {
             const float d = (m - top) * LOG2E - rounded() + (moderate(top) ? fmaf(top, LOG2E, -cn) : 0.f), f = ex2(d);
@@ -214,12 +218,18 @@ template <typename T> struct Sums {
         }
         m = top;
         c = cn;
-        lim = top + 8.f;
+        lim = top;
         low = Words<T>::dup(top - fmaxf(160.f, fabsf(top) * 0.03125f));
     }
-    // N words; `top`: their largest value
-    template <int N> __device__ __forceinline__ void add(const uint32_t (&w)[N], float top) {
-        if (top > lim) raise(top);
+    // all lanes together, before they add words whose largest value is `top`
+    __device__ __forceinline__ void reference(float top) {
+        if (!__any_sync(~0u, top > lim)) return;
+        float most;
+        asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(most) : "f"(top));   // (past NaN)
+        raise(most);
+    }
+    // N words
+    template <int N> __device__ __forceinline__ void add(const uint32_t (&w)[N]) {
         if (!moderate(m)) {
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
@@ -249,23 +259,26 @@ template <typename T> struct Sums {
         unpair(z, z0, z1);
         unpair(t, t0, t1);
         const float d = -rounded(), f = ex2(d), zs = z0 + z1, ts = t0 + t1;
-        // the reference of a thread that saw only -inf is -inf; a NaN among them stays in z
+        // the reference of a warp that saw only -inf is -inf; a NaN among them stays in z
         return Stat{lim > -INF ? m : -INF, f * zs, f * fmaf(d, zs, ts)};
     }
 };
 
-// over the warp: the largest reference first, then plain sums relative to it
-__device__ __forceinline__ Stat warp_merge(Stat s) {
-    float m = s.m;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-    s = merge(s, Stat{m, 0.f, 0.f});
+// over the warp, whose lanes have the same reference
+__device__ __forceinline__ Stat warp_sum(Stat s) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
         s.z += __shfl_xor_sync(~0u, s.z, d);
         s.t += __shfl_xor_sync(~0u, s.t, d);
     }
     return s;
+}
+// over the warp: the largest reference first, then plain sums relative to it
+__device__ __forceinline__ Stat warp_merge(Stat s) {
+    float m = s.m;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    return warp_sum(merge(s, Stat{m, 0.f, 0.f}));
 }
 
 // what a row's merged sums say
@@ -275,11 +288,12 @@ struct RowResult {
 };
 __device__ __forceinline__ RowResult row_result(const Stat &s) {
     RowResult r;
-    r.bad = !(s.z < INF);
+    r.bad = !(s.z < INF && s.m < INF);
     r.none = s.m == -INF;
     const float lz = log2f(s.z);
     r.lse = r.bad ? nan_f() : r.none ? -INF : fmaf(lz, LN2, s.m);
-    r.entropy = r.bad ? nan_f() : r.none ? 0.f : (lz - s.t / s.z) * LN2;
+    // (Z of one token can round to just below 1)
+    r.entropy = r.bad ? nan_f() : r.none ? 0.f : fmaxf(lz - s.t / s.z, 0.f) * LN2;
     return r;
 }
 
@@ -351,21 +365,24 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
             }
         }
     }
-    Sums<T> sums;
-    sums.start();
     float ga = -INF, gb = -INF;                            // this lane's largest logits, of even and of odd words
 #pragma unroll
     for (int i = 0; i < NW; i += 4) {
         if (i / 4 * 32 * E >= vocab) break;
-        uint32_t part[4] = {w[i], w[i + 1], w[i + 2], w[i + 3]};
-        const float ta = Words<T>::largest(Words<T>::max2(w[i], w[i + 2]));
-        const float tb = Words<T>::largest(Words<T>::max2(w[i + 1], w[i + 3]));
-        sums.add(part, fmaxf(ta, tb));
-        ga = fmaxf(ga, ta);
-        gb = fmaxf(gb, tb);
+        ga = fmaxf(ga, Words<T>::largest(Words<T>::max2(w[i], w[i + 2])));
+        gb = fmaxf(gb, Words<T>::largest(Words<T>::max2(w[i + 1], w[i + 3])));
     }
     const float mx = fmaxf(ga, gb);
-    const RowResult q = row_result(warp_merge(sums.stat()));
+    Sums<T> sums;
+    sums.start();
+    sums.reference(mx);
+#pragma unroll
+    for (int i = 0; i < NW; i += 4) {
+        if (i / 4 * 32 * E >= vocab) break;
+        const uint32_t part[4] = {w[i], w[i + 1], w[i + 2], w[i + 3]};
+        sums.add(part);
+    }
+    const RowResult q = row_result(warp_sum(sums.stat()));
     if (lane == 0) write_row(a, r, q, id, given);
     if (a.top_k == 0) return;
     __shared__ __align__(16) uint64_t lists[SHORT_WARPS][SHORT_CAP];
@@ -818,7 +835,8 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_ker
 #pragma unroll
         for (int i = 1; i < 4 * VECS; ++i) m2 = Words<T>::max2(m2, w[i]);
         const float top = Words<T>::largest(m2);
-        sums.add(w, top);
+        sums.reference(top);
+        sums.add(w);
         seg_mx = fmaxf(seg_mx, top);
         if (--seg_left == 0 || b + 1 == batches) {
             left.seg[seg++][lane] = from_f32<T>(seg_mx);   // exact: a value of this type
@@ -828,7 +846,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_ker
         }
     }
     left.mx[lane] = mx;
-    const RowResult res = row_result(warp_merge(sums.stat()));
+    const RowResult res = row_result(warp_sum(sums.stat()));
     if (lane == 0) write_row(a, r, res, id, given);
     if (a.top_k > 0) {
         __syncwarp();
@@ -930,7 +948,8 @@ template <typename T, int NT> struct Long : Top<T, NT> {
 #pragma unroll
         for (int b = 1; b < 4 * VECS; ++b) m2 = Words<T>::max2(m2, w[b]);
         const float top = Words<T>::largest(m2);
-        sums.add(w, top);
+        sums.reference(top);
+        sums.add(w);
         return top;
     }
 };
@@ -1044,7 +1063,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
                 }
             }
             left.mx[tid] = mx;
-            const Stat st = warp_merge(sums.stat());
+            const Stat st = warp_sum(sums.stat());
             if (lane == 0) left.part[warp] = st;
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(tc::smem_u32(&sh.left_full[f]));
