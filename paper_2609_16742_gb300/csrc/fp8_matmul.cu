@@ -358,6 +358,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
         }
         __syncwarp();
     } else if (warp == MMA_WARP) {
+        pdl_wait();                                        // its waits' limits do not run while the kernel before works
         constexpr uint32_t idesc = idesc_e4m3(BL, BN);
         if (elect_one()) {
             for (int it = 0; it < nkb; ++it) {
