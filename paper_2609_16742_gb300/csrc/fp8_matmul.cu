@@ -84,7 +84,8 @@ struct MmArgs {
 };
 
 constexpr int QUANT_WARP = 10, N_QUANT = 8;   // narrow: warps that quantise x
-constexpr int X_SLOTS = 16;             // blocks whose scales are kept: more than stages and accumulators together
+// blocks whose scales are kept, each with a barrier: more than stages and accumulators together
+constexpr int X_SLOTS = 16;
 
 template <int BN, typename X = uint8_t> struct Narrow {
     static constexpr bool QUANT = sizeof(X) > 1;
@@ -105,8 +106,8 @@ template <int BN, typename X = uint8_t> struct Narrow {
     static constexpr int LDN = CPW < 32 ? CPW : 32;        // columns of one TMEM load
     static constexpr int FAC = N_EPI * 2 * CPW * 4;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + FAC + 8 * (2 * STAGES + 2 * NBUF) + 16 +
-                                   (QUANT ? X_SLOTS * BN * 4 : 0);
-    static_assert(STAGES + NBUF < X_SLOTS, "a slot is read before it is written again");
+                                   (QUANT ? X_SLOTS * (BN * 4 + 8) : 0);
+    static_assert(STAGES + NBUF < X_SLOTS, "a slot is read, and its barrier's phase seen, before it is written again");
 };
 
 template <int N> __device__ __forceinline__ void tmem_ld_nw(uint32_t taddr, uint32_t (&r)[N]) {
@@ -209,8 +210,8 @@ __device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
 // stages as TMA would put them there; a row's 16 bytes a lane, the next blocks'
 // on their way meanwhile.
 template <int BN, typename X>
-__device__ __forceinline__ void quantize_stages(const MmArgs &a, uint8_t *Cs, float *xsc, uint64_t *full, uint64_t *empty, int m0,
-                                                int first, int nkb) {
+__device__ __forceinline__ void quantize_stages(const MmArgs &a, uint8_t *Cs, float *xsc, uint64_t *xs_full, uint64_t *full,
+                                                uint64_t *empty, int m0, int first, int nkb) {
     using S = Narrow<BN, X>;
     constexpr int TEAMS = S::TEAMS, V = Vec16<X>::N, G = BK / V;            // lanes a row
     constexpr int SIDE = 32 * N_QUANT / TEAMS / G, N = BN / SIDE;           // rows at once
@@ -275,7 +276,12 @@ __device__ __forceinline__ void quantize_stages(const MmArgs &a, uint8_t *Cs, fl
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(&full[s]));
+            if (threadIdx.x % 32 == 0) {
+                // the values for the MMAs, the scales for the epilogue: what reaches it by way of the MMAs' completion
+                // orders only what they did
+                mbar_arrive(smem_u32(&xs_full[it % X_SLOTS]));
+                mbar_arrive(smem_u32(&full[s]));
+            }
         }
     }
 }
@@ -296,7 +302,9 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
     uint64_t *acc_full = empty + STAGES;
     uint64_t *acc_empty = acc_full + NBUF;
     uint32_t *tmem_holder = (uint32_t *)(acc_empty + NBUF);
-    float *xsc = (float *)(tmem_holder + 4);               // QUANT: [slot][row], scales of x's blocks
+    // QUANT: a barrier for each slot's scales, [slot][row], of x's blocks
+    uint64_t *xs_full = (uint64_t *)(tmem_holder + 4);
+    float *xsc = (float *)(xs_full + X_SLOTS);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)a.splits);
@@ -314,6 +322,8 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
             mbar_init(smem_u32(&acc_full[b]), 1);
             mbar_init(smem_u32(&acc_empty[b]), N_EPI / GROUPS);
         }
+        if (QUANT)
+            for (int i = 0; i < X_SLOTS; ++i) mbar_init(smem_u32(&xs_full[i]), N_QUANT / S::TEAMS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == MMA_WARP) {
@@ -379,7 +389,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
         __syncwarp();
     } else if (QUANT && warp >= QUANT_WARP) {
         pdl_wait();
-        if constexpr (QUANT) quantize_stages<BN, X>(a, Cs, xsc, full, empty, tc * BN, kb0, nkb);
+        if constexpr (QUANT) quantize_stages<BN, X>(a, Cs, xsc, xs_full, full, empty, tc * BN, kb0, nkb);
     } else {
         pdl_wait();
         const int quad = warp & 3, half = warp >> 2;
@@ -430,20 +440,17 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap lmap, const __grid_constan
                 const int it = its + u * GROUPS, b = it % NBUF;
                 if (it >= nkb) break;
                 float *fs = fac + (warp * 2 + (u & 1)) * CPW;
-                if (!QUANT) {
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-                        if (j * 32 + lane < CPW) fs[j * 32 + lane] = f[u][j];
-                    __syncwarp();
+                if (QUANT) {                               // x's scales, which come before the block's products
+                    ok = warp_wait(smem_u32(&xs_full[it % X_SLOTS]), (uint32_t)(it / X_SLOTS) & 1u, a.err, E_EPI);
+                    if (!ok) break;
                 }
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+                    if (j * 32 + lane < CPW)
+                        fs[j * 32 + lane] = QUANT ? f[u][j] * xsc[it % X_SLOTS * BN + cw + j * 32 + lane] : f[u][j];
+                __syncwarp();
                 ok = warp_wait(smem_u32(&acc_full[b]), (uint32_t)(it / NBUF) & 1u, a.err, E_EPI);
                 if (!ok) break;
-                if (QUANT) {                               // x's scales are there with the block
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-                        if (j * 32 + lane < CPW) fs[j * 32 + lane] = f[u][j] * xsc[it % X_SLOTS * BN + cw + j * 32 + lane];
-                    __syncwarp();
-                }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                 for (int c = 0; c < CPW; c += LDN) {

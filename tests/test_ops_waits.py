@@ -1,6 +1,8 @@
-"""The bounded waits of the 8-bit answer head's kernels, as their source has them (a
-wait that runs out cannot be staged without hanging a kernel): no time limit
-runs while the kernel before is still at work."""
+"""The waits of the 8-bit answer head's kernels, as their source has them (a wait that
+runs out, or a race that memory's latency hides, cannot be staged on a GPU): no
+time limit runs while the kernel before is still at work; what one warp leaves
+for another in shared memory is handed over by a barrier that the writer arrives
+on and the reader waits for."""
 import os
 import re
 
@@ -45,3 +47,18 @@ def test_no_limit_runs_while_the_kernel_before_works(name):
             own = re.search(r"\n {8}(?: {4})*pdl_wait\(\);", part)
             assert first is None or waited or (own and own.start() < first.start()), (kernel, part[:200])
             waited = waited or re.search(r"\n    pdl_wait\(\);", part) is not None
+
+
+def test_scales_are_handed_over_by_a_barrier_of_their_own():
+    """The kernel that quantises x: the scales' writer arrives on the barrier
+    after its last store, the epilogue waits for it before its first read."""
+    text = source("fp8_matmul.cu")
+    writer = next(b for n, b in bodies(text, r"__device__ __forceinline__ void ") if n == "quantize_stages")
+    store, sync = writer.rindex("xsc[it % X_SLOTS"), writer.rindex("__syncwarp()")
+    arrive = writer.find("mbar_arrive(smem_u32(&xs_full[it % X_SLOTS]))")
+    assert store < sync < arrive
+    kernel = next(b for n, b in bodies(text, r"__global__ void __launch_bounds__\([^\n]*\)\s") if n == "fp8_narrow_kernel")
+    assert kernel.count("xsc[it % X_SLOTS") == 1
+    read = kernel.index("xsc[it % X_SLOTS")
+    wait = kernel.rfind("warp_wait(", 0, read)
+    assert kernel[wait:].startswith("warp_wait(smem_u32(&xs_full[it % X_SLOTS]), (uint32_t)(it / X_SLOTS) & 1u")
