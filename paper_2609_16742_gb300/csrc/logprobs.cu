@@ -22,7 +22,7 @@ namespace {
 constexpr float INF = __builtin_huge_valf();
 __device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); }
 
-constexpr uint32_t E_LOGPROBS = 0x2000;      // error code of the bounded waits
+constexpr uint32_t E_LOGPROBS = 0x2000, E_DRAIN = 0x4000;      // error codes of the bounded waits
 
 struct LpArgs {
     const void *x;
@@ -869,6 +869,24 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_ker
 
 constexpr int MAX_SPLITS = 8;                              // CTAs that share a row
 
+// A thread's wait for a barrier's phase, at most `limit` x 2^32 cycles.  Its first
+// wait in vain takes the limit away, so that they do not add up, one for each
+// chunk: each later one ends after 256 polls, 0.3 ms.  (A vote of the warp, or a flag
+// that all threads see, costs every chunk 1 to 2%.)
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, uint32_t *err, int &limit) {
+    const uint32_t b = tc::smem_u32(bar);
+    if (tc::mbar_try_wait(b, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t it = 1;; ++it) {
+        if (tc::mbar_try_wait(b, parity)) return true;
+        if ((it & 255) == 0 && (int)((clock64() - t0) >> 32) >= limit) {
+            atomicOr(err, E_LOGPROBS);
+            limit = 0;
+            return false;
+        }
+    }
+}
+
 // the 32 best keys of two lists, each sorted over the lanes from the best on
 __device__ __forceinline__ uint64_t best32(uint64_t a, uint64_t b) {
     const int lane = threadIdx.x % 32;
@@ -983,16 +1001,19 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
     pdl_wait();
     pdl_trigger();
 
-    // a wait that runs out leaves the results invalid; it is reported
+    // A wait that runs out is reported: the results are invalid.  The producer and the
+    // finishers stop then, consumers run through to the end with next to no more waits.
     if (warp == NT / 32) {
         if (lane == 0) {
             int it = 0;
-            for (int64_t r = cid; r < a.rows; r += ncl) {
+            bool ok = true;
+            for (int64_t r = cid; r < a.rows && ok; r += ncl) {
                 const uint8_t *row = reinterpret_cast<const uint8_t *>(static_cast<const T *>(a.x) + r * a.ldx);
                 const int64_t row_bytes = a.vocab * (int64_t)sizeof(T);
                 for (int ch = ch0; ch < ch1; ++ch, ++it) {
                     const int s = it % STAGES;
-                    tc::mbar_wait(tc::smem_u32(&sh.empty[s]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_LOGPROBS);
+                    ok = tc::mbar_wait(tc::smem_u32(&sh.empty[s]), ((uint32_t)(it / STAGES) & 1u) ^ 1u, a.err, E_LOGPROBS);
+                    if (!ok) break;
                     // whole 16-byte units that hold a value of the chunk
                     const int64_t end = min((int64_t)(ch + 1) * L::CHUNK, row_bytes);
                     const uintptr_t from = (uintptr_t)(row + (int64_t)ch * L::CHUNK) & ~(uintptr_t)15;
@@ -1003,6 +1024,9 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
                                   (uint32_t)(to - from), bar);
                 }
             }
+            // no copy is under way when the CTA ends, whoever gave up
+            for (int j = max(0, it - STAGES); j < it; ++j)
+                tc::mbar_wait(tc::smem_u32(&sh.full[j % STAGES]), (uint32_t)(j / STAGES) & 1u, a.err, E_DRAIN);
         }
         __syncwarp();
     } else if (warp > NT / 32) {
@@ -1014,7 +1038,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
             const T *row = static_cast<const T *>(a.x) + r * a.ldx;
             int64_t id = -1;
             const float given = lane == 0 && rank == 0 ? given_logit<T>(a, r, id) : 0.f;
-            tc::warp_wait(tc::smem_u32(&sh.left_full[f]), phase, a.err, E_LOGPROBS);
+            if (!tc::warp_wait(tc::smem_u32(&sh.left_full[f]), phase, a.err, E_LOGPROBS)) break;
             const Stat st = warp_merge(lane < NT / 32 ? left.part[lane] : Stat{-INF, 0.f, 0.f});
             if (k > 0) {
                 const int64_t v0 = (int64_t)ch0 * L::CE;
@@ -1037,6 +1061,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
             __syncwarp();
         }
     } else {
+        int limit = 1;
         int it = 0, f = 0;                                 // f: whose turn it is to finish the row
         uint32_t phase = 0;
         for (int64_t r = cid; r < a.rows; r += ncl) {
@@ -1050,12 +1075,12 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
                 const int s = it % STAGES;
                 const uint8_t *stage = smem + s * L::STAGE;
                 const int n_valid = (int)min((int64_t)L::CE, a.vocab - (int64_t)ch * L::CE);
-                tc::mbar_wait(tc::smem_u32(&sh.full[s]), (uint32_t)(it / STAGES) & 1u, a.err, E_LOGPROBS);
+                wait_for(&sh.full[s], (uint32_t)(it / STAGES) & 1u, a.err, limit);
                 const float top = L::chunk(stage, shift, n_valid, &sh.empty[s], sums);
                 seg_mx = fmaxf(seg_mx, top);
                 if (--seg_left == 0 || ch + 1 == ch1) {
                     if (seg == 0)                          // the row FIN before is finished
-                        tc::mbar_wait(tc::smem_u32(&sh.left_free[f]), phase ^ 1u, a.err, E_LOGPROBS);
+                        wait_for(&sh.left_free[f], phase ^ 1u, a.err, limit);
                     left.seg[seg++][tid] = from_f32<T>(seg_mx);        // exact: a value of this type
                     mx = fmaxf(mx, seg_mx);
                     seg_mx = -INF;

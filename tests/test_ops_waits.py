@@ -1,6 +1,7 @@
 """The waits of the 8-bit answer head's kernels, as their source has them (a wait that
 runs out, or a race that memory's latency hides, cannot be staged on a GPU): no
-time limit runs while the kernel before is still at work; what one warp leaves
+time limit runs while the kernel before is still at work; what waits in
+vain waits for nothing more but its own copies; what one warp leaves
 for another in shared memory is handed over by a barrier that the writer arrives
 on and the reader waits for."""
 import os
@@ -62,3 +63,33 @@ def test_scales_are_handed_over_by_a_barrier_of_their_own():
     read = kernel.index("xsc[it % X_SLOTS")
     wait = kernel.rfind("warp_wait(", 0, read)
     assert kernel[wait:].startswith("warp_wait(smem_u32(&xs_full[it % X_SLOTS]), (uint32_t)(it / X_SLOTS) & 1u")
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_what_waits_in_vain_waits_for_nothing_more(name):
+    """Every wait's result decides what follows, but for the last ones, for
+    copies and products under way (E_DRAIN)."""
+    text = source(name)
+    for m in WAIT.finditer(text):
+        before = re.sub(r"tc::$", "", text[:m.start()]).rstrip()
+        if before[-1] in ";{})":                       # a statement: its result is dropped
+            assert "E_DRAIN" in text[m.end():text.index(";", m.end())], text[m.start() - 80:m.end() + 80]
+
+
+def test_waits_in_vain_do_not_add_up():
+    """The consumers of long rows do not look at their waits' results: the first that
+    runs out takes the limit away, and nothing gives it back."""
+    text = source("logprobs.cu")
+    wait = next(b for n, b in bodies(text, r"__device__ __forceinline__ bool ") if n == "wait_for")
+    assert re.search(r">= limit\) \{[^}]*limit = 0;\s*return false;", wait)
+    kernel = next(b for n, b in bodies(text, r"__global__ void __launch_bounds__\([^\n]*\)\s") if n == "logprobs_long_kernel")
+    consumers = branches(kernel)[-1]
+    assert "mbar_wait(" not in consumers and "warp_wait(" not in consumers and "wait_for(" in consumers
+    assert consumers.count("limit = ") == 1 and consumers.index("int limit = 1;") < consumers.index("for (")
+
+
+def test_copies_of_long_rows_are_waited_for_by_their_issuer():
+    """... when all is well too: consumers may give up while the last ones are under way."""
+    kernel = next(b for n, b in bodies(source("logprobs.cu"), r"__global__ void __launch_bounds__\([^\n]*\)\s") if n == "logprobs_long_kernel")
+    producer = next(p for p in branches(kernel) if "bulk_load(" in p)
+    assert re.search(r"for \(int j = max\(0, it - STAGES\); j < it; \+\+j\)\s*tc::mbar_wait\(tc::smem_u32\(&sh\.full", producer[producer.index("bulk_load("):])
