@@ -462,8 +462,12 @@ def ct_destroy(m: Model):
 # Outputs that are not given are allocated on the call's stream.  `stream`:
 # None (the current one), a torch stream, or a raw cudaStream_t; inputs made
 # on another stream must be ordered before it by the caller, as for any
-# PyTorch kernel.  The calls are short next to Python's own cost, so the
-# checks read each attribute once and build no message unless they fail.
+# PyTorch kernel.  Autograd does not track these calls: while it records, a
+# tensor that requires a gradient is refused, as its gradient would be lost in
+# silence (pass t.detach(), or call under torch.no_grad()); gradients are calls
+# of their own, ct_logprobs_grad and the product with the transposed weights.
+# The calls are short next to Python's own cost, so the checks read each
+# attribute once and build no message unless they fail.
 # ---------------------------------------------------------------------------
 class _TorchNames:
     """What the operators use of torch, looked up once."""
@@ -476,6 +480,7 @@ class _TorchNames:
         self.dtypes = {torch.float32: CT_DT_F32, torch.float16: CT_DT_F16, torch.bfloat16: CT_DT_BF16}
         self.bytes = {self.e4m3: 0, self.u8: 0}
         self.current_device = torch.cuda.current_device
+        self.recording = torch.is_grad_enabled
         # the raw handle of the current stream; torch.cuda.current_stream builds a Stream object first
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -520,6 +525,10 @@ def _elsewhere(f, device, stream, *args):
         return f(*args)
 
 
+def _tracked(name):
+    return ValueError("%s requires a gradient, which this call does not pass on: detach it, or call under torch.no_grad()" % name)
+
+
 def _bad_matrix(t, name, dtypes, shape, device):
     if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
         return ValueError("%s: a 2-D CUDA tensor of %s is wanted, got %s %s on %s"
@@ -528,6 +537,8 @@ def _bad_matrix(t, name, dtypes, shape, device):
         return ValueError("%s: shape %s is wanted, got %s" % (name, shape, tuple(t.shape)))
     if device is not None and t.device != device:
         return ValueError("%s is on %s, the other tensors on %s" % (name, t.device, device))
+    if t.requires_grad and _names.recording():
+        return _tracked(name)
     return ValueError("%s: its columns must be contiguous (strides %s)" % (name, t.stride()))
 
 
@@ -535,7 +546,7 @@ def _matrix(t, name, dtypes, shape=None, device=None):
     """(rows, columns, row pitch) of a 2-D CUDA tensor with unit column stride."""
     size = t.shape
     if len(size) != 2 or t.dtype not in dtypes or not t.is_cuda or (shape is not None and size != shape) or \
-            (device is not None and t.device != device):
+            (device is not None and t.device != device) or (t.requires_grad and _names.recording()):
         raise _bad_matrix(t, name, dtypes, shape, device)
     m, n = size
     s0, s1 = t.stride()
@@ -548,6 +559,8 @@ def _vector(t, name, dtype, n, device):
     if t.dtype != dtype or t.shape != (n,) or t.device != device or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s: a contiguous %s tensor of %d values on %s is wanted, got %s %s on %s"
                          % (name, dtype, n, device, t.dtype, tuple(t.shape), t.device))
+    if t.requires_grad and _names.recording():
+        raise _tracked(name)
     return t.data_ptr()
 
 
@@ -555,6 +568,8 @@ def _scales(t, name, shape, device):
     if t.shape != shape or t.dtype != _names.f32 or t.device != device:
         raise ValueError("%s: a float32 tensor of shape %s on %s is wanted, got %s %s on %s"
                          % (name, shape, device, t.dtype, tuple(t.shape), t.device))
+    if t.requires_grad and _names.recording():
+        raise _tracked(name)
     s0, s1 = t.stride()
     return t.data_ptr(), s0, s1
 
