@@ -570,8 +570,10 @@ ct_status ct_logprobs(const void *logits_dev, int32_t dtype, int64_t ld, const i
  * rounded once to the logits' type (dlogits_dev: dtype, pitch ld_d; it may
  * be logits_dev itself with the same pitch).  lse_dev and entropy_dev are
  * ct_logprobs' outputs.  g_logprob_dev or g_entropy_dev may be NULL (zero;
- * ids_dev or entropy_dev then too).  0 for tokens that cannot occur; id -1:
- * no g_logprob term; NaN where the row's lse is NaN or its id is out of range.
+ * ids_dev or entropy_dev then too).  Tokens that cannot occur (logit -inf) have
+ * p_j = 0 and gradient 0, but for the given one, which keeps its own term: its
+ * gradient is g_logprob, in a row with nothing left too.  id -1: no g_logprob
+ * term; NaN where the row's lse is NaN or its id is out of range.
  * Errors: CT_EINVAL, CT_ERANGE, CT_ECUDA. */
 ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, const int64_t *ids_dev, int64_t rows,
                            int64_t vocab, const float *lse_dev, const float *entropy_dev, const float *g_logprob_dev,

@@ -705,7 +705,8 @@ def ct_logprobs(logits, ids=None, top_k: int = 0, stream=None):
 
 def ct_logprobs_grad(logits, ids, lse, entropy, g_logprob=None, g_entropy=None, out=None, stream=None):
     """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect
-    to the logits, in their type; lse and entropy are ct_logprobs' outputs.
+    to the logits, in their type; lse and entropy are ct_logprobs' outputs.  A
+    given token keeps its own term g_logprob also where its logit is -inf.
     `out` may be `logits`."""
     T = _names or _T()
     rows, vocab, ld = _matrix(logits, "logits", T.dtypes)
