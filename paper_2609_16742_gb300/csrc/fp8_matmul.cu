@@ -111,17 +111,13 @@ template <int BN, typename X = uint8_t> struct Narrow {
 };
 
 template <int N> __device__ __forceinline__ void tmem_ld_nw(uint32_t taddr, uint32_t (&r)[N]) {
-    if constexpr (N == 8) {
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                     : "r"(taddr));
-    } else if constexpr (N == 16) {
+    if constexpr (N == 16) {
         tmem_ld16_nw(taddr, r);
     } else if constexpr (N == 48) {
         tmem_ld_nw<32>(taddr, reinterpret_cast<uint32_t (&)[32]>(r[0]));
         tmem_ld_nw<16>(taddr + 32u, reinterpret_cast<uint32_t (&)[16]>(r[32]));
     } else {
-        static_assert(N == 32, "8, 16, 32 or 48 columns");
+        static_assert(N == 32, "16, 32 or 48 columns");
         asm volatile(
             "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
             "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -207,81 +203,73 @@ __device__ __forceinline__ void split2(uint64_t v, float &a, float &b) {
 // narrow: few rows
 // ---------------------------------------------------------------------------
 // Blocks `first`, first + 1, ... of x's BN rows from m0 on, quantised into the
-// stages as TMA would put them there; a row's 16 bytes a lane, the next blocks'
-// on their way meanwhile.
+// stages as TMA would put them there; a row's 16 bytes a lane, a team's next
+// block on its way meanwhile.
 template <int BN, typename X>
 __device__ __forceinline__ void quantize_stages(const MmArgs &a, uint8_t *Cs, float *xsc, uint64_t *xs_full, uint64_t *full,
                                                 uint64_t *empty, int m0, int first, int nkb) {
     using S = Narrow<BN, X>;
     constexpr int TEAMS = S::TEAMS, V = Vec16<X>::N, G = BK / V;            // lanes a row
-    constexpr int SIDE = 32 * N_QUANT / TEAMS / G, N = BN / SIDE;           // rows at once
-    static_assert(BN % SIDE == 0, "whole passes");
+    constexpr int SIDE = 32 * N_QUANT / TEAMS / G, N = BN / SIDE;           // rows at once, rows of a lane
+    static_assert(BN % SIDE == 0 && N == 4, "whole passes; the rows that the teams' number is made for");
     const int t = ((int)threadIdx.x - 32 * QUANT_WARP) % (32 * N_QUANT / TEAMS), g = t / G, l = t % G;
     const int team = ((int)threadIdx.x / 32 - QUANT_WARP) / (N_QUANT / TEAMS);
     const X *rows = static_cast<const X *>(a.x) + (int64_t)(m0 + g) * a.ldx;
-    constexpr int DEPTH = N >= 4 ? 1 : 4 / N;              // blocks on their way together
-    uint4 u[DEPTH][N], n[DEPTH][N];
-    const auto load = [&](int it, int d) {
+    uint4 u[N], n[N];
+    const auto load = [&](int it) {
         const int c = (first + it) * BK + l * V, bytes = it < nkb ? max(0, min(V, a.K - c)) * (int)sizeof(X) : 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const uintptr_t p = reinterpret_cast<uintptr_t>(rows + (int64_t)(i * SIDE) * a.ldx + c);
             const uint4 *at = reinterpret_cast<const uint4 *>(p & ~(uintptr_t)15);
             const bool any = bytes > 0 && m0 + g + i * SIDE < a.M;
-            u[d][i] = n[d][i] = make_uint4(0, 0, 0, 0);
-            if (any) u[d][i] = __ldg(at);
-            if (any && (int)(p & 15u) + bytes > 16) n[d][i] = __ldg(at + 1);
+            u[i] = n[i] = make_uint4(0, 0, 0, 0);
+            if (any) u[i] = __ldg(at);
+            if (any && (int)(p & 15u) + bytes > 16) n[i] = __ldg(at + 1);
         }
     };
+    load(team);
+    for (int it = team; it < nkb; it += TEAMS) {
+        const int s = it % S::STAGES, c = (first + it) * BK + l * V;
+        uint4 w[N];
+        uint32_t mx[N];
+        bool odd = false;                                  // something that is not finite
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) load(team + d * TEAMS, d);
-    bool ok = true;
-    for (int base = team; base < nkb && ok; base += DEPTH * TEAMS) {
+        for (int i = 0; i < N; ++i) {
+            const uintptr_t p = reinterpret_cast<uintptr_t>(rows + (int64_t)(i * SIDE) * a.ldx + c);
+            w[i] = first_bytes(shifted(u[i], n[i], (uint32_t)p & 15u), max(0, min(V, a.K - c)) * (int)sizeof(X));
+            mx[i] = largest_any<X>(w[i]);
+            odd |= mx[i] >= 0x7F800000u;
+        }
+        load(it + TEAMS);
+        if (__any_sync(~0u, odd)) {
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int it = base + d * TEAMS, s = it % S::STAGES, c = (first + it) * BK + l * V;
-            if (it >= nkb) break;
-            uint4 w[N];
-            uint32_t mx[N];
-            bool odd = false;                              // something that is not finite
+            for (int i = 0; i < N; ++i) mx[i] = largest<X, V>(w[i]);
+        }
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uintptr_t p = reinterpret_cast<uintptr_t>(rows + (int64_t)(i * SIDE) * a.ldx + c);
-                w[i] = first_bytes(shifted(u[d][i], n[d][i], (uint32_t)p & 15u), max(0, min(V, a.K - c)) * (int)sizeof(X));
-                mx[i] = largest_any<X>(w[i]);
-                odd |= mx[i] >= 0x7F800000u;
-            }
-            load(it + DEPTH * TEAMS, d);
-            if (__any_sync(~0u, odd)) {
+        for (int e = G / 2; e > 0; e /= 2)
 #pragma unroll
-                for (int i = 0; i < N; ++i) mx[i] = largest<X, V>(w[i]);
-            }
+            for (int i = 0; i < N; ++i) mx[i] = max(mx[i], __shfl_xor_sync(~0u, mx[i], e));
+        if (!warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA)) break;
 #pragma unroll
-            for (int e = G / 2; e > 0; e /= 2)
-#pragma unroll
-                for (int i = 0; i < N; ++i) mx[i] = max(mx[i], __shfl_xor_sync(~0u, mx[i], e));
-            ok = warp_wait(smem_u32(&empty[s]), ((uint32_t)(it / S::STAGES) & 1u) ^ 1u, a.err, E_TMA);
-            if (!ok) break;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int r = g + i * SIDE;
-                float scale, inv;
-                block_scale(mx[i], scale, inv);
-                uint32_t q[V / 4];
-                convert<X, V>(w[i], inv, q);
-                uint8_t *to = Cs + s * S::C_BYTES + r * BK + ((l * V / 16) ^ (r & 7)) * 16 + l * V % 16;
-                if constexpr (V == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(q[0], q[1]);
-                else *reinterpret_cast<uint32_t *>(to) = q[0];
-                if (l == 0) xsc[it % X_SLOTS * BN + r] = scale;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (threadIdx.x % 32 == 0) {
-                // the values for the MMAs, the scales for the epilogue: what reaches it by way of the MMAs' completion
-                // orders only what they did
-                mbar_arrive(smem_u32(&xs_full[it % X_SLOTS]));
-                mbar_arrive(smem_u32(&full[s]));
-            }
+        for (int i = 0; i < N; ++i) {
+            const int r = g + i * SIDE;
+            float scale, inv;
+            block_scale(mx[i], scale, inv);
+            uint32_t q[V / 4];
+            convert<X, V>(w[i], inv, q);
+            uint8_t *to = Cs + s * S::C_BYTES + r * BK + ((l * V / 16) ^ (r & 7)) * 16 + l * V % 16;
+            if constexpr (V == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(q[0], q[1]);
+            else *reinterpret_cast<uint32_t *>(to) = q[0];
+            if (l == 0) xsc[it % X_SLOTS * BN + r] = scale;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) {
+            // the values for the MMAs, the scales for the epilogue: what reaches it by way of the MMAs' completion
+            // orders only what they did
+            mbar_arrive(smem_u32(&xs_full[it % X_SLOTS]));
+            mbar_arrive(smem_u32(&full[s]));
         }
     }
 }
