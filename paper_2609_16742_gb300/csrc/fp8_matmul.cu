@@ -74,7 +74,7 @@ struct MmArgs {
     int tiles_l, tiles_c;               // tiles along the lane side and along the columns
     int splits;                         // CTAs of a cluster that share a tile's K blocks
     int group;                          // wide: row tiles walked together
-    int vec;                            // wide: TMA can address y's rows
+    int vec;                            // wide: TMA can address y's rows, and they are whole 16-byte units
     int vec4;                           // 4 values of a row of y, from a multiple of 4 on, are one aligned store
     int early;                          // narrow: the kernel before does not write w
     const void *x;                      // narrow: rows to quantise, their pitch and length
@@ -593,7 +593,7 @@ template <int CPW> __device__ __forceinline__ void finish_row(const MmArgs &a, u
     }
 }
 
-// Rows of y that TMA can address: through shared memory in boxes of 32 rows
+// Rows of y that TMA can address, of whole 16-byte units: through shared memory in boxes of 32 rows
 // by COLS columns, 128 bytes (64 where the warp's columns are fewer), swizzled
 // so that the 16-byte pieces of 8 rows hit 8 bank groups, stored by TMA,
 // which clips what lies past the ends, while the next tile's products are added.
@@ -628,7 +628,7 @@ __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *
     }
 }
 
-// Rows that start anywhere: segments of 256 bytes of a row (fewer where the
+// Rows that start or end anywhere: segments of 256 bytes of a row (fewer where the
 // warp's columns are fewer) through shared memory.  A lane moves its row up to
 // its place in the aligned 8-byte units of y, then the warp stores rows of
 // units, and what is left at a segment's ends value by value.  Few instructions
@@ -1268,7 +1268,9 @@ ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st, const Choice *cho
         if (tiles > INT32_MAX / 16) return CT_ERANGE;
         CUtensorMap ymap = {};
         const int es = dtype_size(a.out);
-        a.vec = aligned(a.y, 16) && a.ldy * es % 16 == 0;
+        // TMA clips a store at the 16-byte unit in which a row ends, not at the row's end: what lies beside y in a
+        // wider matrix would be written
+        a.vec = aligned(a.y, 16) && a.ldy * es % 16 == 0 && (int64_t)a.N * es % 16 == 0;
         if (!encode8(&lmap, o.xq, a.M, o.k, o.ldx, BL) || !encode8(&cmap, o.wq, a.N, o.k, o.ldw, bn / 2) ||
             (a.vec && !encode(&ymap, a.y, a.out == CT_DT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16,
                               es, a.M, a.N, a.ldy * es, bn % 128 == 64 && es == 2 ? 64 : 128, 32)))
