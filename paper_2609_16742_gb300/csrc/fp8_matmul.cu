@@ -1220,26 +1220,29 @@ template <typename X> Choice choose_quantising(const Choice &two, int M, int N, 
     return best;
 }
 
-// quantises and multiplies in one launch, where that is estimated to take less than `us`; false: it is not
-template <typename X>
-bool quantise_and_multiply(MmArgs a, const Operands &o, const Choice &two, int dev, int type, double us, cudaStream_t st,
-                           ct_status *done) {
-    const Choice ch = choose_quantising<X>(two, a.M, a.N, a.KB, sm_count(), dev, type);
+// The kernel that quantises and multiplies rows of `type` in one launch, where that is estimated to take less than a
+// launch for each (`two`: the product's); ctas = 0: it is not.
+Choice choose_one_launch(const Choice &two, int M, int N, int64_t k, int dev, int type) {
+    const int KB = (int)((k + BK - 1) / BK), sms = sm_count();
+    Choice ch = type == CT_DT_F32   ? choose_quantising<float>(two, M, N, KB, sms, dev, 0)
+                : type == CT_DT_F16 ? choose_quantising<__half>(two, M, N, KB, sms, dev, 1)
+                                    : choose_quantising<__nv_bfloat16>(two, M, N, KB, sms, dev, 2);
+    const double apart = two.us + LAUNCH + (double)M * k * (dtype_size(type) + 1) / 6e6;
+    const int64_t tiles = (int64_t)((N + 127) / 128) * ((M + ch.bn - 1) / ch.bn);
+    if (ch.us >= apart || tiles > INT32_MAX / 16) ch.ctas = 0;
+    return ch;
+}
+
+template <typename X> ct_status quantise_and_multiply(MmArgs a, const Operands &o, const Choice &ch, cudaStream_t st) {
     a.tiles_l = (a.N + 127) / 128;
     a.tiles_c = (a.M + ch.bn - 1) / ch.bn;
-    const int64_t tiles = (int64_t)a.tiles_l * a.tiles_c;
-    if (ch.us >= us || tiles > INT32_MAX / 16) return false;
     a.splits = ch.splits;
     a.err = device_error_word();
     CUtensorMap lmap;
-    if (a.err == nullptr || !encode8(&lmap, o.wq, a.N, o.k, o.ldw, BL)) {
-        *done = CT_ECUDA;
-        return true;
-    }
-    const int grid = (int)tiles * a.splits;
+    if (a.err == nullptr || !encode8(&lmap, o.wq, a.N, o.k, o.ldw, BL)) return CT_ECUDA;
+    const int grid = a.tiles_l * a.tiles_c * a.splits;
     const cudaError_t e = ch.bn == 16 ? launch_narrow<16, X>(lmap, lmap, a, grid, st) : launch_narrow<32, X>(lmap, lmap, a, grid, st);
-    *done = e == cudaSuccess ? CT_OK : CT_ECUDA;
-    return true;
+    return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
 
 ct_status matmul(MmArgs a, const Operands &o, cudaStream_t st, const Choice *chosen = nullptr) {
@@ -1371,14 +1374,13 @@ extern "C" ct_status ct_fp8_linear(const void *x_dev, int32_t x_dtype, int64_t l
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return CT_ECUDA;
     const Choice two = choose(a.M, a.N, a.KB, sm_count(), dev);
-    const double apart = two.us + LAUNCH + (double)m * k * (dtype_size(x_dtype) + 1) / 6e6;
     const Operands w = {nullptr, 0, w_dev, ldw, k};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    ct_status done = CT_OK;
-    if (x_dtype == CT_DT_F32   ? quantise_and_multiply<float>(a, w, two, dev, 0, apart, st, &done)
-        : x_dtype == CT_DT_F16 ? quantise_and_multiply<__half>(a, w, two, dev, 1, apart, st, &done)
-                               : quantise_and_multiply<__nv_bfloat16>(a, w, two, dev, 2, apart, st, &done))
-        return done;
+    const Choice one = choose_one_launch(two, a.M, a.N, k, dev, x_dtype);
+    if (one.ctas > 0)
+        return x_dtype == CT_DT_F32   ? quantise_and_multiply<float>(a, w, one, st)
+               : x_dtype == CT_DT_F16 ? quantise_and_multiply<__half>(a, w, one, st)
+                                      : quantise_and_multiply<__nv_bfloat16>(a, w, one, st);
     uint8_t *q = static_cast<uint8_t *>(workspace_dev);
     float *xs = reinterpret_cast<float *>(q + scales_at(m, k));
     const ct_status r = quantize(x_dev, x_dtype, m, k, ldx, 1, q, q_pitch(k), xs, 1, m, st);
@@ -1388,4 +1390,24 @@ extern "C" ct_status ct_fp8_linear(const void *x_dev, int32_t x_dtype, int64_t l
     // is complete, and does not write w
     a.early = 1;
     return matmul(a, Operands{q, q_pitch(k), w_dev, ldw, k}, st, &two);
+}
+
+// Which kernel a product of these sizes takes (x_dtype -1), or a linear layer on
+// rows of x_dtype: {quantises in the launch, wide, columns of a tile, splits of
+// K}.  Not part of the interface: the tests ask it whether they reach every kernel.
+extern "C" ct_status ct_internal_fp8_kernel(int64_t m, int64_t n, int64_t k, int32_t x_dtype, int32_t *kernel) {
+    using namespace ct::ops;
+    if (kernel == nullptr || (x_dtype != -1 && !dtype_ok(x_dtype))) return CT_EINVAL;
+    if (m < 1 || n < 1 || k < 1 || m > INT32_MAX - 256 || n > INT32_MAX - 256 || k > INT32_MAX - 256) return CT_ERANGE;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= MAX_DEVICES) return CT_ECUDA;
+    Choice ch = choose((int)m, (int)n, (int)((k + BK - 1) / BK), sm_count(), dev);
+    const Choice one = x_dtype < 0 ? Choice{} : choose_one_launch(ch, (int)m, (int)n, k, dev, x_dtype);
+    if (one.ctas > 0) ch = one;
+    if (ch.ctas == 0) return CT_ECUDA;
+    kernel[0] = one.ctas > 0;
+    kernel[1] = ch.wide;
+    kernel[2] = ch.bn;
+    kernel[3] = ch.splits;
+    return CT_OK;
 }
