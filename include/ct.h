@@ -513,11 +513,12 @@ ct_status ct_fp8_quantize(const void *x_dev, int32_t dtype, int64_t m, int64_t k
                           void *stream);
 
 /* ct_fp8_matmul -- y = act(x w^T + bias) for 8-bit operands (as
- * ct_fp8_quantize writes them, or any e4m3 values with any finite FP32
- * scales):
+ * ct_fp8_quantize writes them, or any e4m3 values with FP32 scales):
  *   y[m, n] = act( sum_b xs[m, b] ws[n / 128, b] sum_{k in block b} xq[m, k] wq[n, k] + bias[n] )
  * on the tcgen05 tensor cores, with the scaled block sums and the rest in FP32
- * and one rounding to y's type.  act: ReLU that keeps NaN (relu != 0), or
+ * and one rounding to y's type.  A block's two scales are applied as one FP32
+ * factor, xs ws: where that exceeds FP32's range the block's sums are infinite or
+ * NaN, below 2^-126 it loses digits.  act: ReLU that keeps NaN (relu != 0), or
  * none.  bias_dev: FP32 [n] or NULL.
  *   x_dev uint8 [m, k], pitch ldx; its scales at row * x_scale_row + block * x_scale_blk.
  *   w_dev uint8 [n, k], pitch ldw; its scales at (row / 128) * w_scale_row + block * w_scale_blk.
