@@ -24,7 +24,8 @@
 //     per block.  A K block of 256 columns takes ~790 cycles, of which the MMAs
 //     need 512: the epilogue's loads from TMEM and additions set the pace (16
 //     epilogue warps instead of 8 make it slower, 262 us and more against 201).
-//     8192 x 8192 x 4096 to BF16 in 201 us, 2.73 PFLOP/s;
+//     8192 x 8192 x 4096 to BF16 in 200 us, 2.75 PFLOP/s, at 2070 MHz, in 222 us
+//     after 0.1 s at the power limit (1.84 GHz);
 //   narrow (few rows): rows of w on the lanes, 128 x BN tiles with BN as
 //     narrow as the rows allow, so that a few rows cost no 128-wide tile; the
 //     K range is split over a cluster of up to 8 CTAs so that the whole GPU
@@ -33,7 +34,7 @@
 //     launch, the same bits each time.  For few rows that are not yet in 8 bits
 //     8 more warps quantise them on the way into shared memory (X: their type;
 //     uint8_t: they are in 8 bits).  Bound by HBM with a start of ~3 us and a
-//     join of ~2: 64 x 4096 x 25088 in 21 us, 4.9 TB/s of weights.
+//     join of ~2: 64 x 4096 x 25088 in 21.7 us, 4.7 TB/s of weights.
 #include <atomic>
 #include <cudaTypedefs.h>
 #include <math.h>
@@ -634,8 +635,8 @@ __device__ __forceinline__ void store_boxes(const MmArgs &a, const CUtensorMap *
 // units, and what is left at a segment's ends value by value.  Few instructions
 // decide: two warps a scheduler are all that run here, and the products of the
 // next tile wait.  (4170 x 7300 x 1018 to 16 bits: 56.7 us with single values
-// from 32 x 32 squares, 48.9 us with the shift at the second step, 41.6 us this
-// way, 34.8 us where TMA can address the rows, with 7296 columns.)
+// from 32 x 32 squares, 48.9 us with the shift at the second step, 41.4 us this
+// way, 34.5 us where TMA can address the rows, with 7296 columns.)
 template <typename O, int CPW>
 __device__ __forceinline__ void store_lines(const MmArgs &a, const uint64_t *acc, uint64_t *sq, int m_warp, int c0, int lane) {
     constexpr int PER8 = 8 / (int)sizeof(O);               // values of a unit
@@ -1139,14 +1140,15 @@ double narrow_us(int M, int N, int KB, int sms, int i, int q, int ctas, double b
 }
 
 // Which kernel, how wide its tiles, over how many CTAs (pairs) K is split: the
-// least of an estimate in us.  Its figures were measured by timing every
-// candidate at 67 shapes (1 to 8192 rows, 10 to 16384 columns, K from 64 to
-// 25088); the choice is 2.5% slower than the best candidate on average, 24% at
-// worst.
+// least of an estimate in us, whose figures were fitted to every candidate's
+// times at 67 shapes.  At 72 shapes (1 to 8000 rows, 16 to 15618 columns, K from
+// 64 to 25088) the choice is 4.3% slower than the best candidate on average,
+// 48% at worst (8000 x 100 x 1000: 9.6 us in narrow tiles, 6.5 in wide ones).
 //   A K block costs a CTA 0.2 to 0.5 us (16 to 128 columns), a pair 0.2 to
-//   0.41 us (64 to 256; 192 save little of a block, but often a round: 1777 x
-//   2999 x 5003 takes 40.8 us in 128 columns, 41.0 in 256, 36.4 in 192); launch, start and end of a tile 1 to 3.3 us, 3.9 to
-//   4.8 us; adding the shares of a split 1.4 to 2.2 us, 3.5 us.
+//   0.41 us (64 to 256; 192 a little less than 256, which counts where neither
+//   fills its last round: 1777 x 2999 x 5003, two rounds of either, takes 40.8
+//   and 44.8 us, 42.3 in 128 columns); launch, start and end of a tile 1 to 3.3
+//   us, 3.9 to 4.8 us; adding the shares of a split 1.4 to 2.2 us, 3.5 us.
 //   No kernel is faster than its operands: 9 to 11 bytes a ns from L2, 6.4 of
 //   weights from HBM, 58 bytes a ns to one SM.
 Choice choose(int M, int N, int KB, int sms, int dev) {
@@ -1195,8 +1197,8 @@ Choice choose(int M, int N, int KB, int sms, int dev) {
 // The same for the kernels that quantise rows of X: one launch less (LAUNCH us),
 // no 8-bit copy, but each CTA quantises the rows it multiplies, which sets the
 // pace of long K: only tiles of 16 and 32 columns do.  In one launch and in two:
-// 256 x 1000 x 512 FP16 5.0 and 5.7 us, 500 x 500 x 500 5.1 and 7.6, 1 x 4096 x
-// 25088 19.8 and 20.9, 256 x 1000 x 4096 13.2 and 10.4.
+// 256 x 1000 x 512 FP16 5.1 and 6.0 us, 500 x 500 x 500 5.1 and 8.1, 1 x 4096 x
+// 25088 20.0 and 21.3, 256 x 1000 x 4096 13.6 and 10.9.
 constexpr double LAUNCH = 2.0;
 constexpr double Q_BLOCK[2][2] = {{0.35, 0.65}, {0.5, 0.95}};   // 16-bit, FP32 rows
 std::atomic<int> g_quant[MAX_DEVICES][3][2][N_SPLITS];     // [dev][type][log2 of the columns / 16][index of the split]

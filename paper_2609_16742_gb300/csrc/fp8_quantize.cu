@@ -79,8 +79,8 @@ constexpr int ROW_THREADS = 256;
 // passes it round (8 + 8 shuffles and one scale a lane; row by row it was 32 to
 // 40 and 8, 107 instructions for 128 FP32 values).  Where the scales lie block
 // by block, the 8 are one 32-byte sector.
-// Bound by HBM: 8192 x 4096 BF16 in 14.5 us, 6.9 TB/s.  Rows that start inside
-// a 16-byte unit cost instructions: 5000 x 3001 BF16 in 13.6 us, 3.3 TB/s.
+// Bound by HBM: 8192 x 4096 BF16 in 14.9 us, 6.8 TB/s.  Rows that start inside
+// a 16-byte unit cost instructions: 5000 x 3001 BF16 in 13.2 us, 3.4 TB/s.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(ROW_THREADS, 4) quantize_rows_kernel(const QuantArgs a) {
     static_assert(ROWS == 1 || ROWS == 8, "one row, or the exchange's 8");

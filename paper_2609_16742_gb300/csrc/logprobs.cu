@@ -325,9 +325,9 @@ template <typename T> __device__ __forceinline__ float given_logit(const LpArgs 
 // are listed in shared memory and sorted by counting.  Where ties overflow
 // the list, the next token is the warp's largest key below the last one.
 // One warp because a row is 2 to 4 KB: no exchange through shared memory, no
-// barrier.  Bound by latency for few rows (256 x 1000 FP32, 5 tokens: 4.6 us,
+// barrier.  Bound by latency for few rows (256 x 1000 FP32, 5 tokens: 4.3 us,
 // of which the row's load and the launch are half), by instructions for many
-// (8192 x 1000 FP16: 6.4 us without tokens, 14.3 us with 5).
+// (8192 x 1000 FP16: 7.4 us without tokens, 14.2 us with 5).
 // ---------------------------------------------------------------------------
 constexpr int SHORT = 1024;
 constexpr int SHORT_WARPS = 4;
@@ -390,8 +390,8 @@ __global__ void __launch_bounds__(32 * SHORT_WARPS) logprobs_short_kernel(const 
     const int k = a.top_k;
     // The k-th largest of the lanes' maxima, the least of those that fewer than k
     // exceed: one a lane for few tokens, two where the 32nd of 32 would list too
-    // much (8192 x 1000 FP16, 5 and 32 tokens: 14.3 and 73 us with one, 16.1 and
-    // 24.8 us with two).
+    // much (8192 x 1000 FP16, 5 and 32 tokens: 14 and 73 us with one, 16 and 26 us
+    // with two).
     const bool few = k <= 16;
     float *groups = reinterpret_cast<float *>(list);
     if (few) ga = mx;
@@ -752,9 +752,10 @@ template <typename T, int NT> struct Top {
 // Many rows of moderate length: one warp each, straight from global memory,
 // VECS vectors a lane on their way while VECS are added.  A row of the kernel
 // below would fill its last chunk badly and meet its barriers too often.
-// Bound by the exponentials' issue slots and, with few rows a warp, by the last
-// round: 8192 x 16000 BF16 with 8 tokens in 58.7 us, 4.5 TB/s; 5696 x 5714 FP16
-// without tokens in 17.5 us, 3.7 TB/s.  ANY: rows that may start inside a
+// Bound by waiting: 26 of the 32 warps that an SM holds are active, and a warp has
+// no load on its way while it finishes a row (issue slots are 67% busy, DRAM 61%,
+// the exponentials' pipe 27%): 8192 x 16000 BF16 with 8 tokens in 58.7 us, 4.5
+// TB/s; 5696 x 5714 FP16 without tokens in 16.7 us, 3.9 TB/s.  ANY: rows that may start inside a
 // 16-byte unit (96 registers a thread, not 64).
 // ---------------------------------------------------------------------------
 constexpr int ROW_WARPS = 4;
@@ -862,9 +863,9 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, ANY ? 5 : 8) logprobs_warp_ker
 // the next row, and finisher warps, in turn, make a row's results of what they
 // leave of it meanwhile.  Where there are fewer rows than CTAs a cluster of up to
 // 8 shares a row and one warp joins the shares, in their order.
-// Bound by HBM where rows abound (2048 x 131072 BF16 with 8 tokens in 87 us, 6.2
-// TB/s, without tokens 6.6), by the way from the last value to the result where
-// they do not: 1 x 131072 FP16 takes 4.3 us, with 20 tokens 8.1 us.
+// Bound by HBM where rows abound (2048 x 131072 BF16 with 8 tokens in 88 us, 6.1
+// TB/s, without tokens 6.5), by the way from the last value to the result where
+// they do not: 1 x 131072 FP16 takes 3.5 us, with 20 tokens 7.8 us.
 // ---------------------------------------------------------------------------
 
 constexpr int MAX_SPLITS = 8;                              // CTAs that share a row
@@ -1136,7 +1137,7 @@ __global__ void __launch_bounds__(Long<T, NT>::THREADS, Long<T, NT>::CTAS) logpr
 // start.  LONG: rows of 256 threads or more that start as those of dx do, in
 // fewer registers (32 and not 59: 2048 x 131072 BF16 153 us and not 170).
 // Bound by HBM, each logit read and each gradient written once: 7.0 TB/s there;
-// short rows by latency (6476 x 15 BF16 in 2.7 us; a CTA a row took 11.6).
+// short rows by latency (6476 x 15 BF16 in 2.1 us; a CTA a row took 11.6).
 // ---------------------------------------------------------------------------
 constexpr int GRAD_THREADS = 256;
 constexpr int GRAD_VECS = 4;
