@@ -14,24 +14,23 @@ from test_gpu_fp8 import check_product
 
 pytestmark = pytest.mark.gpu
 
-# (m, n, k), (wide, columns of a tile), K split
-PRODUCTS = [((711, 18, 711), (0, 16), False), ((203, 283, 2218), (0, 16), True), ((128, 49, 2932), (0, 16), True),
-            ((17, 10781, 1658), (0, 32), False), ((107, 1271, 4664), (0, 32), True), ((351, 265, 5598), (0, 32), True),
-            ((495, 2296, 82), (0, 64), False), ((1660, 328, 673), (0, 64), False), ((580, 408, 3957), (0, 64), True),
-            ((42, 1824, 8091), (0, 64), True), ((1356, 1098, 251), (0, 128), False), ((700, 2000, 128), (0, 128), False),
-            ((1568, 156, 5544), (0, 128), True), ((117, 5768, 4353), (0, 128), True),
-            ((3000, 300, 1000), (1, 64), False), ((700, 1000, 2000), (1, 64), False), ((7269, 33, 5011), (1, 64), True),
-            ((6838, 11, 5042), (1, 64), True), ((700, 2000, 1000), (1, 128), False), ((6499, 549, 402), (1, 128), False),
-            ((1243, 796, 6318), (1, 128), True), ((3933, 197, 5705), (1, 128), True), ((417, 11892, 162), (1, 192), False),
-            ((1818, 1626, 985), (1, 192), False), ((193, 16071, 167), (1, 256), False), ((3869, 2119, 427), (1, 256), False),
-            ((182, 5321, 7519), (1, 256), True), ((6673, 149, 7341), (1, 256), True)]
+# sizes by the kernel that they take on a GB300, several of each: how many clusters a device holds at once may move one
+PRODUCTS = [(711, 18, 711), (36, 26, 110), (203, 283, 2218), (128, 49, 2932),              # narrow, 16 columns: whole K, split K
+            (17, 10781, 1658), (2984, 13, 20), (107, 1271, 4664), (351, 265, 5598),        # 32
+            (495, 2296, 82), (1660, 328, 673), (580, 408, 3957), (42, 1824, 8091),         # 64
+            (1356, 1098, 251), (700, 2000, 128), (1568, 156, 5544), (117, 5768, 4353),     # 128
+            (3000, 300, 1000), (700, 1000, 2000), (7269, 33, 5011), (6838, 11, 5042),      # wide, 64 columns
+            (700, 2000, 1000), (6499, 549, 402), (1243, 796, 6318), (3933, 197, 5705),     # 128
+            (417, 11892, 162), (1818, 1626, 985),                                          # 192: whole K only
+            (193, 16071, 167), (3869, 2119, 427), (182, 5321, 7519), (6673, 149, 7341)]    # 256
 
-# type of x, (m, n, k), columns of a tile, K split
-LINEARS = [("float32", (259, 1422, 154), 32, False), ("float16", (259, 1422, 154), 32, False), ("bfloat16", (206, 2000, 154), 32, False),
-           ("float32", (1330, 155, 214), 32, False), ("float32", (682, 41, 4402), 32, True), ("float16", (585, 42, 4575), 32, True),
-           ("bfloat16", (833, 71, 2325), 32, True), ("float32", (67, 416, 1697), 16, True), ("float16", (147, 218, 3206), 16, True),
-           ("bfloat16", (242, 20, 4653), 16, True), ("float32", (356, 67, 266), 16, False), ("float16", (59, 266, 534), 16, False),
-           ("bfloat16", (55, 99, 1594), 16, False)]
+# type of x, (m, n, k): quantised in the launch, 32 columns, whole K and split K, then 16 columns
+LINEARS = [("float32", (259, 1422, 154)), ("float16", (259, 1422, 154)), ("bfloat16", (206, 2000, 154)),
+           ("float32", (1330, 155, 214)), ("float16", (2465, 65, 73)), ("bfloat16", (1232, 474, 46)),
+           ("float32", (682, 41, 4402)), ("float16", (585, 42, 4575)), ("bfloat16", (833, 71, 2325)),
+           ("float32", (421, 62, 3969)), ("float16", (293, 100, 4006)), ("bfloat16", (665, 32, 6467)),
+           ("float32", (67, 416, 1697)), ("float16", (147, 218, 3206)), ("bfloat16", (242, 20, 4653)),
+           ("float32", (356, 67, 266)), ("float16", (59, 266, 534)), ("bfloat16", (55, 99, 1594))]
 
 
 def kernel(m, n, k, x_dtype=-1):
@@ -46,17 +45,13 @@ def kernel(m, n, k, x_dtype=-1):
 
 
 def test_the_lists_reach_every_kernel():
-    kinds = {(w, s) for _, w, s in PRODUCTS}
-    assert kinds == {((0, bn), s) for bn in (16, 32, 64, 128) for s in (False, True)} | \
-        {((1, bn), s) for bn in (64, 128, 256) for s in (False, True)} | {((1, 192), False)}
-    assert {(d, bn, s) for d, _, bn, s in LINEARS} == {(d, bn, s) for d in ("float32", "float16", "bfloat16") for bn in (16, 32)
-                                                       for s in (False, True)}
-    for size, (wide, bn), split in PRODUCTS:
-        q, w, b, s = kernel(*size)
-        assert (q, w, b, s > 1) == (0, wide, bn, split), (size, (q, w, b, s))
-    for dtype, size, bn, split in LINEARS:
-        q, w, b, s = kernel(*size, x_dtype=["float32", "float16", "bfloat16"].index(dtype))
-        assert (q, w, b, s > 1) == (1, 0, bn, split), (dtype, size, (q, w, b, s))
+    """(wide, columns, K split), and (type, columns, K split) of what quantises in the launch."""
+    products = [kernel(*size) for size in PRODUCTS]
+    assert {(w, bn, s > 1) for _, w, bn, s in products} == {(0, bn, s) for bn in (16, 32, 64, 128) for s in (False, True)} | \
+        {(1, bn, s) for bn in (64, 128, 256) for s in (False, True)} | {(1, 192, False)}
+    types = ["float32", "float16", "bfloat16"]
+    linears = [(d, kernel(*size, x_dtype=types.index(d))) for d, size in LINEARS]
+    assert {(d, bn, s > 1) for d, (q, _, bn, s) in linears if q} == {(d, bn, s) for d in types for bn in (16, 32) for s in (False, True)}
 
 
 def ints(g, rows, k):
@@ -67,7 +62,7 @@ def ints(g, rows, k):
     return t, v.double()
 
 
-@pytest.mark.parametrize("size", [p[0] for p in PRODUCTS], ids=lambda s: "%dx%dx%d" % s)
+@pytest.mark.parametrize("size", PRODUCTS, ids=lambda s: "%dx%dx%d" % s)
 def test_products(size):
     import torch
     m, n, k = size
@@ -92,7 +87,7 @@ def test_products(size):
     assert c.ct_ops_device_error() == 0
 
 
-@pytest.mark.parametrize("dtype,size", [(d, s) for d, s, _, _ in LINEARS])
+@pytest.mark.parametrize("dtype,size", LINEARS)
 def test_linear_layers_in_one_launch(dtype, size):
     import torch
     m, n, k = size
