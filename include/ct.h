@@ -580,6 +580,118 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
                            int64_t vocab, const float *lse_dev, const float *entropy_dev, const float *g_logprob_dev,
                            const float *g_entropy_dev, void *dlogits_dev, int64_t ld_d, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Adapting and answering: what trains beside the answer head's frozen 8-bit
+ * weights, and how its logits become tokens.  The rules of the operators above
+ * hold (current device, asynchronous on `stream`, nothing kept or allocated,
+ * a dimension of 0 is valid, the same inputs give the same bits).  A workspace
+ * (16-byte aligned, at least the bytes its query gives) is scratch that no other
+ * work may use until this call's stream work is done. */
+
+/* ct_adapters -- low-rank adapters of many requests at once, added to what the
+ * shared projection gave, in place:
+ *   y[t] = act( y[t] + scale[i] B[i] (A[i] x[t]) ),  i = ids[t]
+ * with every sum, the products A x among them, in FP32 or better and one
+ * rounding to y's type.
+ *   y_dev [t, n] (y_dtype, pitch ldy), x_dev [t, k] (x_dtype, pitch ldx).
+ *   a_dev, b_dev (both `dtype`): A[i] is [rank, k], its rows a_row apart, one
+ *     adapter a_adapter after another; B[i] is [n, rank], rows b_row apart,
+ *     b_adapter.  A stride of 0 is valid (adapters that share a matrix).
+ *   ids_dev int64 [t]: the adapter of each row, in any order.  -1: none, the row
+ *     only takes part in act; any other id outside [0, adapters): the row
+ *     becomes NaN.  NULL: every row has adapter 0.
+ *   scale_dev FP32 [adapters] or NULL (1).
+ *   act: ReLU that keeps NaN (relu != 0), or none.
+ * x_dtype is `dtype` or CT_DT_F32; rank <= CT_MAX_RANK.  NaN and infinities stay in
+ * their row, or in the rows of their adapter.
+ * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row),
+ * CT_ERANGE (sizes, rank), CT_ENOMEM (workspace), CT_ECUDA. */
+#define CT_MAX_RANK 128
+ct_status ct_adapters_workspace(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n, size_t *bytes);
+ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, const void *x_dev, int32_t x_dtype, int64_t ldx,
+                      const void *a_dev, int64_t a_adapter, int64_t a_row, const void *b_dev, int64_t b_adapter,
+                      int64_t b_row, int32_t dtype, const int64_t *ids_dev, const float *scale_dev, int64_t t,
+                      int64_t adapters, int64_t rank, int64_t k, int64_t n, int32_t relu, void *workspace_dev,
+                      size_t workspace_bytes, void *stream);
+
+/* ct_adapters_grad -- gradients of ct_adapters (without act) for the gradient
+ * dy [t, n] of its output:
+ *   v = A[i] x[t],  u = scale[i] B[i]^T dy[t]  for every row t of adapter i = ids[t]
+ *   dA[i] = sum_t u x[t]^T,  dB[i] = scale[i] sum_t dy[t] v^T,  dx[t] += A[i]^T u
+ * with FP32 sums, rounded once.  dy_dev is `dtype` or CT_DT_F32 (pitch lddy).
+ *   dx_dev [t, k] (dx_dtype, pitch lddx) or NULL: added to in place (the shared
+ *     projection's part, or zeros).  Rows without an adapter are left as they
+ *     are; a row whose id is out of range becomes NaN and adds to nothing else.
+ *   da_dev [adapters, rank, k], db_dev [adapters, n, rank]: contiguous, of type
+ *     grad_dtype (`dtype` or CT_DT_F32).  An adapter without rows gets zeros.
+ * Errors: as for ct_adapters. */
+ct_status ct_adapters_grad_workspace(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n, size_t *bytes);
+ct_status ct_adapters_grad(const void *dy_dev, int32_t dy_dtype, int64_t lddy, const void *x_dev, int32_t x_dtype,
+                           int64_t ldx, const void *a_dev, int64_t a_adapter, int64_t a_row, const void *b_dev,
+                           int64_t b_adapter, int64_t b_row, int32_t dtype, const int64_t *ids_dev,
+                           const float *scale_dev, int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n,
+                           void *dx_dev, int32_t dx_dtype, int64_t lddx, void *da_dev, void *db_dev, int32_t grad_dtype,
+                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* ct_clip_grads -- the norm of the values of many tensors together, the norm of
+ * each, and the values scaled so that the norm is at most max_norm:
+ *   norm = sqrt(sum of squares) (kind CT_NORM_2) or the largest magnitude (CT_NORM_INF),
+ *   dst = src * min(1, max_norm / norm),  rounded once to its type.
+ * tensors: host array of n ct_tensor (copied by the call): rows x cols values with
+ * row pitches; dst == src with the same pitch: in place, and nothing is written where
+ * the factor is 1.  Tensors must not overlap one another.  norms_dev FP32 [n],
+ * norm_dev FP32 [1].  Sums are FP32 over at most 1024 values, then FP64; squares
+ * that leave FP32's range are scaled.  A norm that is NaN or, in FP32, infinite
+ * scales nothing: values stay as they are (dst gets a copy), the norms tell.
+ * Errors: CT_EINVAL (type, kind, null or misaligned pointers, pitch, max_norm NaN or
+ * negative, tensors that overlap), CT_ERANGE (sizes), CT_ENOMEM, CT_ECUDA. */
+typedef enum { CT_NORM_2 = 0, CT_NORM_INF = 1 } ct_norm_kind;
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t rows, cols, ld_src, ld_dst;
+    int64_t dtype; /* ct_dtype */
+} ct_tensor;
+ct_status ct_clip_grads_workspace(const ct_tensor *tensors, int64_t n, size_t *bytes);
+ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t kind, double max_norm, float *norms_dev,
+                        float *norm_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* ct_verify_drafts -- drafted tokens held against the target's probabilities, with
+ * given random numbers.  Sequence b has the drafts offsets[b] to offsets[b + 1] - 1
+ * (d of them; at most max_drafts are looked at) and d + 1 rows of target logits from
+ * row offsets[b] + b on: one for each draft, and one after the last.
+ *   p_j, q_j = softmax(target row j / T), softmax(draft row j / T)
+ * Without draft logits q_j is 1 at the draft and 0 elsewhere.  Draft x_j stands while
+ * those before it stand and uniform[j] q_j(x_j) < p_j(x_j).  The token after the
+ * last that stands is the one of largest w / noise[b], the lowest index among
+ * equals: w = max(p_j - q_j, 0) if draft j fell (p_j where that is 0 everywhere), and
+ * p_d if none fell.  With independent uniform numbers and exponentially distributed
+ * noise the tokens are distributed as the target's.  T = temperature[b] (NULL: 1);
+ * below 1e-30 it counts as 0: the target's most probable token (lowest index among
+ * equals), drafts stand while they are that, and log probabilities are those at 1.
+ *   logits_dev [drafts + sequences, vocab], draft_logits_dev [drafts, vocab] or NULL:
+ *     dtype, pitches ld and ld_draft.  drafts_dev int64 [drafts], uniform_dev FP32
+ *     [drafts], offsets_dev int64 [sequences + 1] (ascending, within [0, drafts]: what is
+ *     outside is clamped), noise_dev FP32 [sequences, vocab] (> 0, pitch ld_noise),
+ *     temperature_dev FP32 [sequences] or NULL.
+ *   accepted_dev int64 [sequences]: drafts that stand.
+ *   token_dev int64, logprob_dev FP32 [sequences, max_drafts + 1]: the drafts that stand
+ *     and the token after them, then -1 and 0; the target's log probability of each.
+ * A target logit of -inf cannot occur.  A draft outside [0, vocab) falls.  Where a
+ * NaN or +inf stands in a row that is needed (up to the first draft that falls), or T is
+ * NaN, negative or infinite, the sequence ends: token -1, log probability NaN; a row in
+ * which nothing can occur: token -1, log probability -inf.
+ * Errors: CT_EINVAL (type, null or misaligned pointers, pitch), CT_ERANGE (sizes,
+ * max_drafts > CT_MAX_DRAFTS), CT_ENOMEM, CT_ECUDA. */
+#define CT_MAX_DRAFTS 64
+ct_status ct_verify_drafts_workspace(int64_t sequences, int64_t drafts, int64_t vocab, int64_t max_drafts, size_t *bytes);
+ct_status ct_verify_drafts(const void *logits_dev, int32_t dtype, int64_t ld, const void *draft_logits_dev,
+                           int64_t ld_draft, const int64_t *drafts_dev, const int64_t *offsets_dev,
+                           const float *uniform_dev, const float *noise_dev, int64_t ld_noise,
+                           const float *temperature_dev, int64_t sequences, int64_t drafts, int64_t vocab,
+                           int64_t max_drafts, int64_t *accepted_dev, int64_t *token_dev, float *logprob_dev,
+                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* ct_ops_device_error -- reads and clears the current device's error word of
  * these operators (set by a call whose bounded wait expired: its output
  * is then invalid).  Synchronises the device. */

@@ -43,11 +43,16 @@ EXPORTS = ["ct_build", "ct_set_threshold", "ct_get_threshold", "ct_infer", "ct_i
            "ct_reexecute_noalloc", "ct_campaign_batched", "ct_resolve_roles",
            "ct_reexecute_prepare", "ct_infer_batches", "ct_run_host_batches",
            "ct_fp8_quantize", "ct_fp8_matmul", "ct_fp8_linear", "ct_fp8_linear_workspace",
-           "ct_logprobs", "ct_logprobs_grad", "ct_ops_device_error"]
+           "ct_logprobs", "ct_logprobs_grad", "ct_ops_device_error",
+           "ct_adapters", "ct_adapters_workspace", "ct_adapters_grad", "ct_adapters_grad_workspace",
+           "ct_clip_grads", "ct_clip_grads_workspace", "ct_verify_drafts", "ct_verify_drafts_workspace"]
 
 CT_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
 CT_DT_F32, CT_DT_F16, CT_DT_BF16 = 0, 1, 2
 CT_MAX_TOP_K = 32
+CT_MAX_RANK = 128
+CT_MAX_DRAFTS = 64
+CT_NORM_2, CT_NORM_INF = 0, 1
 
 
 class CtError(RuntimeError):
@@ -126,6 +131,17 @@ def lib():
             "ct_logprobs": [vp, i32, i64, vp, i64, i64, i32, vp, vp, vp, vp, vp, vp],
             "ct_logprobs_grad": [vp, i32, i64, vp, i64, i64, vp, vp, vp, vp, vp, i64, vp],
             "ct_ops_device_error": [P(ctypes.c_uint32)],
+            "ct_adapters_workspace": [i64, i64, i64, i64, i64, P(ctypes.c_size_t)],
+            "ct_adapters": [vp, i32, i64, vp, i32, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, i64, i64, i64, i64, i64, i32, vp,
+                            ctypes.c_size_t, vp],
+            "ct_adapters_grad_workspace": [i64, i64, i64, i64, i64, P(ctypes.c_size_t)],
+            "ct_adapters_grad": [vp, i32, i64, vp, i32, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, i64, i64, i64, i64, i64,
+                                 vp, i32, i64, vp, vp, i32, vp, ctypes.c_size_t, vp],
+            "ct_clip_grads_workspace": [vp, i64, P(ctypes.c_size_t)],
+            "ct_clip_grads": [vp, i64, i32, dbl, vp, vp, vp, ctypes.c_size_t, vp],
+            "ct_verify_drafts_workspace": [i64, i64, i64, i64, P(ctypes.c_size_t)],
+            "ct_verify_drafts": [vp, i32, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, i64, i64, i64, vp, vp, vp, vp,
+                                 ctypes.c_size_t, vp],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -730,6 +746,245 @@ def ct_logprobs_grad(logits, ids, lse, entropy, g_logprob=None, g_entropy=None, 
     if st:
         raise CtError(st, "ct_logprobs_grad")
     return out
+
+
+# ---------------------------------------------------------------------------
+# Adapting and answering: what trains beside the head's frozen 8-bit weights, and
+# how its rows of logits become tokens.  The rules of the operators above hold.
+# ---------------------------------------------------------------------------
+def _bad_stack(t, name, dtype, shape, device):
+    if t.dim() != 3 or t.dtype != dtype or t.device != device or (shape is not None and tuple(t.shape) != shape):
+        return ValueError("%s: a 3-D tensor of %s%s on %s is wanted, got %s %s on %s"
+                          % (name, dtype, "" if shape is None else " of shape %s" % (shape,), device, t.dtype, tuple(t.shape), t.device))
+    if t.requires_grad and _names.recording():
+        return _tracked(name)
+    return ValueError("%s: its columns must be contiguous (strides %s)" % (name, t.stride()))
+
+
+def _stack(t, name, dtype, shape, device):
+    """(its address, matrix stride, row stride) of a stack of matrices with unit column stride."""
+    size = t.shape
+    if len(size) != 3 or t.dtype != dtype or t.device != device or (shape is not None and size != shape) or \
+            (t.requires_grad and _names.recording()):
+        raise _bad_stack(t, name, dtype, shape, device)
+    s0, s1, s2 = t.stride()
+    if s2 != 1 and size[2] > 1:
+        raise _bad_stack(t, name, dtype, shape, device)
+    return t.data_ptr(), s0, s1
+
+
+def _adapters(x, a, b, ids, scale):
+    """(rows, adapters, rank, k, n, x's pitch, pointer arguments) of checked adapters for activations x."""
+    T = _names
+    t, k, ldx = _matrix(x, "x", T.dtypes)
+    dev, dt = x.device, a.dtype
+    if dt not in T.dtypes or (x.dtype != dt and x.dtype != T.f32):
+        raise ValueError("a: float32, float16 or bfloat16 is wanted, and x of its type or float32; got a %s, x %s" % (dt, x.dtype))
+    ap = _stack(a, "a", dt, None, dev)
+    count, rank = a.shape[0], a.shape[1]
+    if a.shape[2] != k:
+        raise ValueError("a has %d columns, x %d" % (a.shape[2], k))
+    if b.dim() != 3:
+        raise _bad_stack(b, "b", dt, None, dev)
+    n = b.shape[1]
+    bp = _stack(b, "b", dt, (count, n, rank), dev)
+    if rank > CT_MAX_RANK:
+        raise ValueError("a: a rank of at most %d is wanted, got %d" % (CT_MAX_RANK, rank))
+    if ids is None:
+        if count != 1:
+            raise ValueError("ids are needed where there are %d adapters" % count)
+        idp = None
+    else:
+        idp = _vector(ids, "ids", T.i64, t, dev)
+    sp = None if scale is None else _vector(scale, "scale", T.f32, count, dev)
+    return t, count, rank, k, n, ldx, ap + bp + (T.dtypes[dt], idp, sp)
+
+
+@functools.lru_cache(maxsize=256)
+def _adapters_workspace(grad, t, count, rank, k, n):
+    need = ctypes.c_size_t()
+    name = "ct_adapters_grad_workspace" if grad else "ct_adapters_workspace"
+    _check(getattr(lib(), name)(t, count, rank, k, n, ctypes.byref(need)), name)
+    return need.value
+
+
+def ct_adapters(y, x, a, b, ids=None, scale=None, relu: bool = False, stream=None):
+    """y [t, n] += scale[i] * (x A[i]^T) B[i]^T in place, with i = ids[row], then
+    a ReLU if asked: low-rank adapters a [adapters, rank, k], b [adapters, n,
+    rank] beside the shared projection that gave y.  ids int64 [t] in any order
+    (-1: no adapter; None: one adapter for all rows); scale float32
+    [adapters].  a and b are of one type, x of that or float32, y of any.
+    Returns y."""
+    T = _names or _T()
+    t, count, rank, k, n, ldx, w = _adapters(x, a, b, ids, scale)
+    dev = x.device
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_adapters, dev, stream, y, x, a, b, ids, scale, relu)
+    ldy = _matrix(y, "y", T.dtypes, (t, n), dev)[2]
+    need = _adapters_workspace(False, t, count, rank, k, n)
+    work = T.empty(need, dtype=T.u8, device=dev)
+    st = (_lib or lib()).ct_adapters(y.data_ptr(), T.dtypes[y.dtype], ldy, x.data_ptr(), T.dtypes[x.dtype], ldx, *w, t, count, rank,
+                                     k, n, 1 if relu else 0, work.data_ptr(), need, T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_adapters")
+    return y
+
+
+def ct_adapters_grad(dy, x, a, b, ids=None, scale=None, dx=None, grad_dtype=None, stream=None):
+    """(dx, da, db): gradients of ct_adapters (without its ReLU) for the gradient
+    dy [t, n] of its output.  dx [t, k], if given, is added to in place (the shared
+    projection's part; None: not wanted).  da and db are new, of a's type or
+    grad_dtype = float32; dy is of a's type or float32."""
+    T = _names or _T()
+    t, count, rank, k, n, ldx, w = _adapters(x, a, b, ids, scale)
+    dev = x.device
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_adapters_grad, dev, stream, dy, x, a, b, ids, scale, dx, grad_dtype)
+    dt = a.dtype
+    lddy = _matrix(dy, "dy", (dt, T.f32), (t, n), dev)[2]
+    if grad_dtype is None:
+        grad_dtype = dt
+    elif grad_dtype != dt and grad_dtype != T.f32:
+        raise ValueError("grad_dtype: %s or float32 is wanted, got %s" % (dt, grad_dtype))
+    dxp, dx_code, lddx = None, CT_DT_F32, 0
+    if dx is not None:
+        lddx = _matrix(dx, "dx", T.dtypes, (t, k), dev)[2]
+        dxp, dx_code = dx.data_ptr(), T.dtypes[dx.dtype]
+    da = T.empty((count, rank, k), dtype=grad_dtype, device=dev)
+    db = T.empty((count, n, rank), dtype=grad_dtype, device=dev)
+    need = _adapters_workspace(True, t, count, rank, k, n)
+    work = T.empty(need, dtype=T.u8, device=dev)
+    st = (_lib or lib()).ct_adapters_grad(dy.data_ptr(), T.dtypes[dy.dtype], lddy, x.data_ptr(), T.dtypes[x.dtype], ldx, *w, t, count,
+                                          rank, k, n, dxp, dx_code, lddx, da.data_ptr(), db.data_ptr(), T.dtypes[grad_dtype],
+                                          work.data_ptr(), need, T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_adapters_grad")
+    return dx, da, db
+
+
+def _layout(t, name, device):
+    """(rows, columns, row pitch) of a tensor whose values are dense in memory in some order of its dimensions, or a matrix with a pitch."""
+    T = _names
+    if t.dtype not in T.dtypes or t.device != device:
+        raise ValueError("%s: a tensor of %s on %s is wanted, got %s on %s"
+                         % (name, "/".join(str(d) for d in T.dtypes), device, t.dtype, t.device))
+    if t.requires_grad and T.recording():
+        raise _tracked(name)
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
+        return t.shape[0], t.shape[1], t.stride(0)
+    size = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != size:
+            raise ValueError("%s: dense values or a matrix with contiguous columns are wanted, got shape %s strides %s"
+                             % (name, tuple(t.shape), t.stride()))
+        size *= n
+    return 1, size, size
+
+
+def ct_clip_grads(grads, max_norm, kind: float = 2.0, out=None, stream=None):
+    """(norm, norms): the norm of the values of all tensors `grads` together
+    (float32, no dimension) and of each (float32 [len(grads)]), and the values
+    times min(1, max_norm / norm), in place or into `out` (tensors of the same
+    types, shapes and strides).  kind: 2 or infinity.  A norm that is NaN or infinite scales
+    nothing.  Types may differ from tensor to tensor; none may overlap another."""
+    T = _names or _T()
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if not grads:
+        raise ValueError("grads: at least one tensor is wanted")
+    if len(outs) != len(grads):
+        raise ValueError("out: %d tensors are wanted, got %d" % (len(grads), len(outs)))
+    if kind != 2 and kind != float("inf"):
+        raise ValueError("kind is 2 or infinity, got %r" % (kind,))
+    max_norm = float(max_norm)
+    if not max_norm >= 0:
+        raise ValueError("max_norm: a number of at least 0 is wanted, got %r" % (max_norm,))
+    dev = grads[0].device
+    if dev.type != "cuda":
+        raise ValueError("grads[0]: a CUDA tensor is wanted, got one on %s" % dev)
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_clip_grads, dev, stream, grads, max_norm, kind, out)
+    table, codes = [], T.dtypes
+    for i, t in enumerate(grads):
+        rows, cols, ld = _layout(t, "grads[%d]" % i, dev)
+        o, ldo = t, ld
+        if out is not None:
+            o = outs[i]
+            if o.dtype != t.dtype or o.shape != t.shape:
+                raise ValueError("out[%d]: %s %s is wanted, got %s %s" % (i, t.dtype, tuple(t.shape), o.dtype, tuple(o.shape)))
+            _, _, ldo = _layout(o, "out[%d]" % i, dev)
+            if o.stride() != t.stride() and not (rows == 1 and t.is_contiguous() and o.is_contiguous()):
+                # matrices of different pitches
+                if t.dim() != 2 or (t.shape[1] > 1 and (t.stride(1) != 1 or o.stride(1) != 1)):
+                    raise ValueError("out[%d]: strides %s are wanted, got %s" % (i, t.stride(), o.stride()))
+                rows, cols = t.shape
+                ld, ldo = t.stride(0), o.stride(0)
+        table += (t.data_ptr(), o.data_ptr(), rows, cols, ld, ldo, codes[t.dtype])
+    n = len(grads)
+    table = (ctypes.c_int64 * len(table))(*table)
+    norm = T.empty((), dtype=T.f32, device=dev)
+    norms = T.empty(n, dtype=T.f32, device=dev)
+    L = _lib or lib()
+    need = ctypes.c_size_t()
+    _check(L.ct_clip_grads_workspace(table, n, ctypes.byref(need)), "ct_clip_grads_workspace")
+    work = T.empty(need.value, dtype=T.u8, device=dev)
+    st = L.ct_clip_grads(table, n, CT_NORM_2 if kind == 2 else CT_NORM_INF, max_norm, norms.data_ptr(), norm.data_ptr(),
+                         work.data_ptr(), need.value, T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_clip_grads")
+    return norm, norms
+
+
+@functools.lru_cache(maxsize=256)
+def _verify_workspace(sequences, drafts, vocab, most):
+    need = ctypes.c_size_t()
+    _check(lib().ct_verify_drafts_workspace(sequences, drafts, vocab, most, ctypes.byref(need)), "ct_verify_drafts_workspace")
+    return need.value
+
+
+def ct_verify_drafts(logits, drafts, offsets, max_drafts: int, uniform, noise, draft_logits=None, temperature=None, stream=None):
+    """(accepted, token, logprob): drafted tokens held against the target's
+    probabilities.  Sequence b has the drafts offsets[b] to offsets[b + 1] - 1 of
+    drafts (int64) and as many rows of logits and one more, from row offsets[b] + b
+    on; draft_logits [drafts, vocab] are what the drafts were drawn from (None: they
+    are certain).  uniform float32 [drafts] in [0, 1) and noise float32 [sequences,
+    vocab], exponentially distributed, are the random numbers; temperature
+    float32 [sequences] (None: 1; 0: the most probable token).
+    accepted int64 [sequences]; token int64 and logprob float32 [sequences,
+    max_drafts + 1]: the drafts that stand and the token after them, then -1 and 0."""
+    T = _names or _T()
+    rows, vocab, ld = _matrix(logits, "logits", T.dtypes)
+    dev = logits.device
+    if stream is not None or dev.index != T.current_device():
+        return _elsewhere(ct_verify_drafts, dev, stream, logits, drafts, offsets, max_drafts, uniform, noise, draft_logits, temperature)
+    if drafts.dim() != 1 or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("drafts and offsets: 1-D tensors are wanted, got shapes %s and %s" % (tuple(drafts.shape), tuple(offsets.shape)))
+    count, batch = drafts.shape[0], offsets.shape[0] - 1
+    if rows != count + batch:
+        raise ValueError("logits: %d rows are wanted (%d drafts, %d sequences), got %d" % (count + batch, count, batch, rows))
+    if not 0 <= max_drafts <= CT_MAX_DRAFTS:
+        raise ValueError("max_drafts is 0 to %d, got %r" % (CT_MAX_DRAFTS, max_drafts))
+    dp, op = _vector(drafts, "drafts", T.i64, count, dev), _vector(offsets, "offsets", T.i64, batch + 1, dev)
+    up = _vector(uniform, "uniform", T.f32, count, dev)
+    ldn = _matrix(noise, "noise", (T.f32,), (batch, vocab), dev)[2]
+    tp = None if temperature is None else _vector(temperature, "temperature", T.f32, batch, dev)
+    qp, ldq = None, 0
+    if draft_logits is not None:
+        ldq = _matrix(draft_logits, "draft_logits", (logits.dtype,), (count, vocab), dev)[2]
+        qp = draft_logits.data_ptr()
+    accepted = T.empty(batch, dtype=T.i64, device=dev)
+    token = T.empty((batch, max_drafts + 1), dtype=T.i64, device=dev)
+    logprob = T.empty((batch, max_drafts + 1), dtype=T.f32, device=dev)
+    need = _verify_workspace(batch, count, vocab, max_drafts)
+    work = T.empty(need, dtype=T.u8, device=dev)
+    st = (_lib or lib()).ct_verify_drafts(logits.data_ptr(), T.dtypes[logits.dtype], ld, qp, ldq, dp, op, up, noise.data_ptr(), ldn, tp,
+                                          batch, count, vocab, max_drafts, accepted.data_ptr(), token.data_ptr(), logprob.data_ptr(),
+                                          work.data_ptr(), need, T.raw_stream(dev.index))
+    if st:
+        raise CtError(st, "ct_verify_drafts")
+    return accepted, token, logprob
 
 
 def ct_ops_device_error() -> int:
