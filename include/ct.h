@@ -602,11 +602,13 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
  *     becomes NaN.  NULL: every row has adapter 0.
  *   scale_dev FP32 [adapters] or NULL (1).
  *   act: ReLU that keeps NaN (relu != 0), or none.
- * x_dtype is `dtype` or CT_DT_F32; rank <= CT_MAX_RANK.  NaN and infinities stay in
+ * x_dtype is `dtype` or CT_DT_F32; rank <= CT_MAX_RANK, adapters <=
+ * CT_MAX_ADAPTERS.  NaN and infinities stay in
  * their row, or in the rows of their adapter.
  * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row),
  * CT_ERANGE (sizes, rank), CT_ENOMEM (workspace), CT_ECUDA. */
 #define CT_MAX_RANK 128
+#define CT_MAX_ADAPTERS 65534
 ct_status ct_adapters_workspace(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n, size_t *bytes);
 ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, const void *x_dev, int32_t x_dtype, int64_t ldx,
                       const void *a_dev, int64_t a_adapter, int64_t a_row, const void *b_dev, int64_t b_adapter,

@@ -51,6 +51,7 @@ CT_NOALLOC_SCRATCH_BYTES = 16 * 1024 * 1024
 CT_DT_F32, CT_DT_F16, CT_DT_BF16 = 0, 1, 2
 CT_MAX_TOP_K = 32
 CT_MAX_RANK = 128
+CT_MAX_ADAPTERS = 65534
 CT_MAX_DRAFTS = 64
 CT_NORM_2, CT_NORM_INF = 0, 1
 

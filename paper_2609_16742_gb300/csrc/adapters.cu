@@ -5,96 +5,370 @@
 //   u[t] = scale[i] B[i]^T dy[t],  dx[t] += A[i]^T u[t],
 //   dA[i] = sum_t u[t] x[t]^T,  dB[i] = sum_t dy[t] v[t]^T
 //
-// v and u are FP32: they are short, and rounding them to 16 bits would cost the
-// result as much as its own rounding does.
-#include "ops_common.cuh"
+// v and u carry more than 16 bits: they are short, and rounding them would cost the result
+// as much as its own rounding does.
+//
+// Many rows are put in the order of their adapters first (one CTA: a counting sort, two where there are more than 254
+// adapters), then go through the tensor cores in tiles of 128 rows of one adapter (adapters_shrink.cu,
+// adapters_expand.cu, adapters_outer.cu).  Few rows, of about as many adapters, take the two kernels here instead,
+// which are bound by the adapters' bytes and the launches: the first row of each adapter speaks for all of its rows.
+#include "adapters.cuh"
 
 namespace ct {
 namespace ops {
 namespace {
 
-constexpr int THREADS = 256;
+// ---------------------------------------------------------------- the rows' order
 
-// a tensor of one of the three types
-struct Any {
-    const void *p;
-    int64_t ld;                                   // of rows
-    int64_t la;                                   // of adapters
-    int32_t dtype;
-    __device__ __forceinline__ float at(int64_t i) const {
-        return dtype == CT_DT_F32   ? static_cast<const float *>(p)[i]
-               : dtype == CT_DT_F16 ? to_f32(static_cast<const __half *>(p)[i])
-                                    : to_f32(static_cast<const __nv_bfloat16 *>(p)[i]);
-    }
+constexpr int ORDER_THREADS = 1024, ORDER_WARPS = 32, BINS = 256;
+
+struct OrderArgs {
+    const int64_t *ids;
+    int64_t t;
+    int adapters;
+    int32_t *order, *spare;                       // [t]
+    int32_t *first, *end;                         // [adapters + 2]
+    AdTile *tiles;
+    int32_t *n_tiles;
 };
 
-__device__ __forceinline__ void put(void *p, int32_t dtype, int64_t i, float v) {
+__device__ __forceinline__ int key_of(const OrderArgs &a, int64_t t) {
+    const int64_t i = a.ids[t];
+    return i == -1 ? 0 : i >= 0 && i < a.adapters ? (int)i + 1 : a.adapters + 1;
+}
+
+// exclusive sum over the block's threads; total: of all
+__device__ __forceinline__ int block_sum(int v, int *warps, int &total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int w = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += w;
+    }
+    __syncthreads();
+    if (lane == 31) warps[warp] = s;
+    __syncthreads();
+    if (warp == 0) {
+        int w = warps[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += x;
+        }
+        warps[lane] = w;
+    }
+    __syncthreads();
+    total = warps[31];
+    return s - v + (warp > 0 ? warps[warp - 1] : 0);
+}
+
+__global__ void __launch_bounds__(ORDER_THREADS) order_kernel(const OrderArgs a) {
+    __shared__ int count[ORDER_WARPS][BINS];
+    __shared__ int sums[32];
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, keys = a.adapters + 2;
+    for (int k = tid; k < keys; k += ORDER_THREADS) a.first[k] = a.end[k] = 0;
+    // each warp has a run of the rows; a digit's rows keep their order within and between the runs
+    const int64_t run = (a.t + 32 * ORDER_WARPS - 1) / (32 * ORDER_WARPS) * 32;
+    const int64_t r0 = min(warp * run, a.t), r1 = min(r0 + run, a.t);
+    const int passes = keys <= BINS ? 1 : 2;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int32_t *from = pass == 0 ? nullptr : a.spare;
+        int32_t *to = pass + 1 == passes ? a.order : a.spare;
+        for (int b = lane; b < BINS; b += 32) count[warp][b] = 0;
+        __syncwarp();
+        for (int64_t p = r0; p < r1; p += 32) {
+            const bool have = p + lane < r1;
+            const int d = have ? key_of(a, from != nullptr ? from[p + lane] : p + lane) >> (8 * pass) & (BINS - 1) : BINS;
+            const uint32_t same = __match_any_sync(0xffffffffu, d);
+            if (have && lane == __ffs(same) - 1) count[warp][d] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        // where each warp's rows of each digit go: thread i has digit i / 4, warps 8 (i % 4) to + 7
+        int mine[8], s = 0, total;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            mine[w] = count[tid % 4 * 8 + w][tid / 4];
+            s += mine[w];
+        }
+        s = block_sum(s, sums, total);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            count[tid % 4 * 8 + w][tid / 4] = s;
+            s += mine[w];
+        }
+        __syncthreads();
+        for (int64_t p = r0; p < r1; p += 32) {
+            const bool have = p + lane < r1;
+            const int64_t row = have ? (from != nullptr ? from[p + lane] : p + lane) : 0;
+            const int d = have ? key_of(a, row) >> (8 * pass) & (BINS - 1) : BINS;
+            const uint32_t same = __match_any_sync(0xffffffffu, d);
+            if (have) to[count[warp][d] + __popc(same & ((1u << lane) - 1u))] = (int32_t)row;
+            __syncwarp();
+            if (have && lane == __ffs(same) - 1) count[warp][d] += __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+    }
+    for (int64_t p = tid; p < a.t; p += ORDER_THREADS) {
+        const int k = key_of(a, a.order[p]);
+        if (p == 0 || key_of(a, a.order[p - 1]) != k) a.first[k] = (int32_t)p;
+        if (p + 1 == a.t || key_of(a, a.order[p + 1]) != k) a.end[k] = (int32_t)p + 1;
+    }
+    __syncthreads();
+    // tiles: each thread has a run of the keys
+    const int per = (keys + ORDER_THREADS - 1) / ORDER_THREADS, k0 = min(tid * per, keys), k1 = min(k0 + per, keys);
+    int n = 0, total;
+    for (int k = k0; k < k1; ++k) n += (a.end[k] - a.first[k] + AD_ROWS - 1) / AD_ROWS;
+    int at = block_sum(n, sums, total);
+    for (int k = k0; k < k1; ++k)
+        for (int s = a.first[k]; s < a.end[k]; s += AD_ROWS) a.tiles[at++] = {s, k};
+    if (tid == 0) *a.n_tiles = total;
+}
+
+// ---------------------------------------------------------------- few rows
+
+constexpr int FEW = 128;                          // most rows of this kind
+constexpr int FEW_THREADS = 256, FEW_WARPS = 8;
+constexpr int FEW_J = 4, FEW_R = 4;               // a warp's rows of A, of x
+
+struct FewArgs {
+    const void *x;
+    int64_t ldx;
+    const void *a;
+    int64_t a_adapter, a_row;
+    const void *b;
+    int64_t b_adapter, b_row;
+    const int64_t *ids;
+    const float *scale;
+    int t, adapters, rank;
+    int64_t k, n;
+    float *v;                                     // [t][rank]
+    void *y;
+    int32_t y_dtype;
+    int64_t ldy;
+    int relu, whole;                              // bits: x, a, b
+};
+
+// The rows that row `lead` speaks for: all with its id, if it is the first of them.  Returns their number, 0 if it is not.
+__device__ __forceinline__ int speak_for(const int64_t *ids, int t, int lead, int16_t *rows, int64_t &id) {
+    __shared__ int found, before;
+    const int tid = threadIdx.x;
+    if (ids == nullptr) {
+        id = 0;
+        for (int i = tid; i < t; i += blockDim.x) rows[i] = (int16_t)i;
+        __syncthreads();
+        return lead == 0 ? t : 0;
+    }
+    id = ids[lead];
+    if (tid < 32) {
+        int n = 0, early = 0;
+        for (int i0 = 0; i0 < t; i0 += 32) {
+            const int i = i0 + tid;
+            const bool same = i < t && ids[i] == id;
+            const uint32_t all = __ballot_sync(0xffffffffu, same);
+            if (same) rows[n + __popc(all & ((1u << tid) - 1u))] = (int16_t)i;
+            early |= __any_sync(0xffffffffu, same && i < lead);
+            n += __popc(all);
+        }
+        if (tid == 0) {
+            found = n;
+            before = early;
+        }
+    }
+    __syncthreads();
+    return before ? 0 : found;
+}
+
+// v = scale A x.  A cluster for each row that may speak, its CTAs share the long axis; warps share the rows of A, and the axis again
+// where those are few.
+template <typename TX, typename TM> __global__ void __launch_bounds__(FEW_THREADS) few_shrink_kernel(const FewArgs a, int splits) {
+    __shared__ int16_t rows[FEW];
+    __shared__ float part[FEW_WARPS][FEW_J][FEW_R];
+    __shared__ float sums[CT_MAX_RANK][FEW_R + 1];
+    pdl_wait();
+    pdl_trigger();
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int64_t id;
+    const int n = speak_for(a.ids, a.t, (int)(blockIdx.x / (unsigned)splits), rows, id);
+    if (n == 0 || id < 0 || id >= a.adapters) return;                            // the whole cluster alike
+    const TM *m = static_cast<const TM *>(a.a) + id * a.a_adapter;
+    const float scale = a.scale != nullptr ? a.scale[id] : 1.f;
+    const bool x_whole = a.whole & 1, m_whole = a.whole & 2;
+    // pieces of 256 values (a warp's 32 x 8)
+    const int64_t pieces = (a.k + 255) / 256, p0 = pieces * rank / splits, p1 = pieces * (rank + 1) / splits;
+    const int groups = (a.rank + FEW_J - 1) / FEW_J, ways = groups >= FEW_WARPS ? 1 : FEW_WARPS / groups;
+    for (int r0 = 0; r0 < n; r0 += FEW_R) {
+        for (int g0 = 0; g0 < groups; g0 += FEW_WARPS / ways) {
+            const int g = g0 + warp / ways, way = warp % ways;
+            float acc[FEW_J][FEW_R];
+#pragma unroll
+            for (int j = 0; j < FEW_J; ++j)
+#pragma unroll
+                for (int r = 0; r < FEW_R; ++r) acc[j][r] = 0.f;
+            if (g < groups && warp < groups * ways) {
+#pragma unroll 2
+                for (int64_t p = p0 + way; p < p1; p += ways) {
+                    const int64_t c = p * 256 + lane * 8;
+                    Eight<TM> em[FEW_J];
+                    Eight<TX> ex[FEW_R];
+#pragma unroll
+                    for (int j = 0; j < FEW_J; ++j)
+                        em[j] = c < a.k && g * FEW_J + j < a.rank ? load_eight(m + (g * FEW_J + j) * a.a_row, c, a.k, m_whole) : zero_eight<TM>();
+#pragma unroll
+                    for (int r = 0; r < FEW_R; ++r)
+                        ex[r] = c < a.k && r0 + r < n ? load_eight(static_cast<const TX *>(a.x) + rows[r0 + r] * a.ldx, c, a.k, x_whole)
+                                                      : zero_eight<TX>();
+                    float fm[FEW_J][8];
+#pragma unroll
+                    for (int j = 0; j < FEW_J; ++j) {
+                        unpack16<TM>(em[j].u[0], fm[j]);
+                        if constexpr (sizeof(TM) == 4) unpack16<TM>(em[j].u[1], fm[j] + 4);
+                    }
+#pragma unroll
+                    for (int r = 0; r < FEW_R; ++r) {
+                        if (r0 + r >= n) break;
+                        float fx[8];
+                        unpack16<TX>(ex[r].u[0], fx);
+                        if constexpr (sizeof(TX) == 4) unpack16<TX>(ex[r].u[1], fx + 4);
+#pragma unroll
+                        for (int j = 0; j < FEW_J; ++j)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) acc[j][r] = fmaf(fm[j][e], fx[e], acc[j][r]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < FEW_J; ++j)
+#pragma unroll
+                for (int r = 0; r < FEW_R; ++r) {
+                    if (r0 + r >= n) break;
+#pragma unroll
+                    for (int s = 16; s > 0; s >>= 1) acc[j][r] += __shfl_xor_sync(0xffffffffu, acc[j][r], s);
+                    if (lane == 0) part[warp][j][r] = acc[j][r];
+                }
+            __syncthreads();
+            // the warps that shared the axis, in their order
+            for (int i = tid; i < FEW_WARPS / ways * FEW_J * FEW_R; i += FEW_THREADS) {
+                const int w = i / (FEW_J * FEW_R), j = i / FEW_R % FEW_J, r = i % FEW_R, at = (g0 + w) * FEW_J + j;
+                if (at >= a.rank || r0 + r >= n) continue;
+                float s = 0.f;
+                for (int q = 0; q < ways; ++q) s += part[w * ways + q][j][r];
+                sums[at][r] = s;
+            }
+            __syncthreads();
+        }
+        if (splits > 1) tc::cluster_sync();
+        if (rank == 0)
+            for (int i = tid; i < a.rank * FEW_R; i += FEW_THREADS) {
+                const int j = i / FEW_R, r = i % FEW_R;
+                if (r0 + r >= n) continue;
+                float s = 0.f;
+                for (int q = 0; q < splits; ++q) s += splits > 1 ? ld_peer_f32(tc::smem_u32(&sums[j][r]), q) : sums[j][r];
+                a.v[rows[r0 + r] * a.rank + j] = s * scale;
+            }
+        if (splits > 1) tc::cluster_sync();       // the sums have been read
+        else __syncthreads();
+    }
+}
+
+__device__ __forceinline__ float few_get(const void *p, int dtype, int64_t i) {
+    return dtype == CT_DT_F32   ? static_cast<const float *>(p)[i]
+           : dtype == CT_DT_F16 ? to_f32(static_cast<const __half *>(p)[i])
+                                : to_f32(static_cast<const __nv_bfloat16 *>(p)[i]);
+}
+__device__ __forceinline__ void few_put(void *p, int dtype, int64_t i, float v) {
     if (dtype == CT_DT_F32) static_cast<float *>(p)[i] = v;
     else if (dtype == CT_DT_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
     else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
 
-__device__ __forceinline__ int64_t adapter_of(const int64_t *ids, int64_t t) { return ids != nullptr ? ids[t] : 0; }
-
-// v[t][j] = scale sum_c m[i](j, c) x[t][c]; m(j, c) at j * sj + c * sc.  A warp for each j, a block for each row.
-__global__ void __launch_bounds__(THREADS) shrink_kernel(Any x, Any m, int64_t sj, int64_t sc, const int64_t *ids, const float *scale,
-                                                         int64_t adapters, int rank, int64_t cols, float *v) {
+// y = act(y + B v): a thread for each column.  The ids and the matrix do not hang on the kernel before, which has itself waited for
+// all before it: they are on their way before its end is waited for.
+constexpr int FEW_COLS = 128;
+template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_kernel(const FewArgs a) {
+    __shared__ int16_t rows[FEW];
+    __shared__ float vs[8][CT_MAX_RANK];
+    if (a.rank == 0) pdl_wait();                  // no kernel of this call before it
+    int64_t id;
+    const int n = speak_for(a.ids, a.t, (int)blockIdx.x, rows, id);
+    const int64_t c = (int64_t)blockIdx.y * FEW_COLS + threadIdx.x;
+    const bool mine = c < a.n, out = id < -1 || id >= a.adapters, product = id >= 0 && !out;
+    if (n == 0 || (id == -1 && !a.relu)) {
+        pdl_wait();
+        return;
+    }
+    const TM *m = static_cast<const TM *>(a.b) + (product ? id * a.b_adapter + c * a.b_row : 0);
+    const bool m_whole = a.whole & 4;
+    constexpr int AHEAD = 4;                      // 32 values of a row of B
+    Eight<TM> em[AHEAD];
+    if (product && mine)
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (j * 8 < a.rank) em[j] = load_eight(m, j * 8, a.rank, m_whole);
     pdl_wait();
-    pdl_trigger();
-    const int64_t t = blockIdx.x, i = adapter_of(ids, t);
-    if (i < 0 || i >= adapters) return;
-    const int lane = threadIdx.x & 31;
-    const float s = scale != nullptr ? scale[i] : 1.f;
-    for (int j = threadIdx.x >> 5; j < rank; j += THREADS / 32) {
-        double sum = 0.0;
-        for (int64_t c0 = 0; c0 < cols; c0 += 1024) {
-            float part = 0.f;
-            for (int64_t c = c0 + lane; c < min(c0 + 1024, cols); c += 32) part = fmaf(x.at(t * x.ld + c), m.at(i * m.la + j * sj + c * sc), part);
-            sum += part;
+    for (int r0 = 0; r0 < n; r0 += 8) {
+        const int nr = min(8, n - r0);
+        float acc[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) acc[r] = mine && r < nr ? few_get(a.y, a.y_dtype, rows[r0 + r] * a.ldy + c) : 0.f;
+        float add[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) add[r] = 0.f;
+        if (product) {
+            for (int i = threadIdx.x; i < nr * a.rank; i += FEW_COLS) vs[i / a.rank][i % a.rank] = a.v[rows[r0 + i / a.rank] * a.rank + i % a.rank];
+            __syncthreads();
+            if (mine)
+                for (int j0 = 0; j0 < a.rank; j0 += 8 * AHEAD) {
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j) {
+                        const int at = j0 + j * 8;
+                        if (at >= a.rank) break;
+                        const Eight<TM> e = j0 == 0 ? em[j] : load_eight(m, at, a.rank, m_whole);
+                        float f[8];
+                        unpack16<TM>(e.u[0], f);
+                        if constexpr (sizeof(TM) == 4) unpack16<TM>(e.u[1], f + 4);
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            if (r >= nr) break;
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (at + q < a.rank) add[r] = fmaf(f[q], vs[r][at + q], add[r]);
+                        }
+                    }
+                }
+            __syncthreads();
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) v[t * rank + j] = (float)(sum * s);
+        for (int r = 0; r < 8; ++r) {
+            if (!mine || r >= nr) break;
+            float v = acc[r] + add[r];
+            if (a.relu) v = v < 0.f ? 0.f : v;
+            few_put(a.y, a.y_dtype, rows[r0 + r] * a.ldy + c, out ? __uint_as_float(0x7FC00000u) : v);
+        }
     }
 }
 
-// y[t][c] = act(y[t][c] + sum_j m[i](c, j) v[t][j]); m(c, j) at c * sc + j * sj
-__global__ void __launch_bounds__(THREADS) expand_kernel(void *y, int32_t y_dtype, int64_t ldy, Any m, int64_t sc, int64_t sj,
-                                                         const int64_t *ids, int64_t adapters, int rank, int64_t cols, int relu,
-                                                         const float *v) {
-    pdl_wait();
-    pdl_trigger();
-    const int64_t t = blockIdx.x, i = adapter_of(ids, t);
-    if (i == -1 && !relu) return;
-    const bool out = i < -1 || i >= adapters;
-    const Any yv = {y, ldy, 0, y_dtype};
-    for (int64_t c = blockIdx.y * (int64_t)THREADS + threadIdx.x; c < cols; c += (int64_t)gridDim.y * THREADS) {
-        float s = 0.f;
-        if (i >= 0 && !out)
-            for (int j = 0; j < rank; ++j) s = fmaf(m.at(i * m.la + c * sc + j * sj), v[t * rank + j], s);
-        s += yv.at(t * ldy + c);
-        if (relu) s = s < 0.f ? 0.f : s;
-        put(y, y_dtype, t * ldy + c, out ? __uint_as_float(0x7FC00000u) : s);
+template <typename TX, typename TM> cudaError_t few(const FewArgs &a, cudaStream_t st) {
+    if (a.rank > 0) {
+        // four blocks for each SM, with two pieces of the axis at least for each warp that shares it
+        const int64_t pieces = (a.k + 255) / 256;
+        const int lead = a.ids != nullptr ? a.t : 1, speak = lead < a.adapters ? lead : a.adapters;
+        int splits = 1;
+        while (splits < 8 && speak * splits < 4 * sm_count() && pieces >= 4 * splits) splits *= 2;
+        const cudaError_t e = splits > 1 ? pdl_launch_cluster(few_shrink_kernel<TX, TM>, dim3((unsigned)(lead * splits)), dim3(FEW_THREADS), 0,
+                                                              st, splits, a, splits)
+                                         : pdl_launch(few_shrink_kernel<TX, TM>, dim3((unsigned)lead), dim3(FEW_THREADS), 0, st, a, splits);
+        if (e != cudaSuccess) return e;
     }
+    const dim3 grid((unsigned)(a.ids != nullptr ? a.t : 1), (unsigned)((a.n + FEW_COLS - 1) / FEW_COLS));
+    return pdl_launch(few_expand_kernel<TM>, grid, dim3(FEW_COLS), 0, st, a);
 }
 
-// g[i](j, c) = sum over the rows t of adapter i of v[t][j] x[t][c]; a block: 256 c of one j of one adapter.  g at j * gj + c * gc.
-__global__ void __launch_bounds__(THREADS) outer_kernel(Any x, const float *v, const int64_t *ids, int64_t rows, int rank, int64_t cols,
-                                                        void *g, int32_t g_dtype, int64_t gj, int64_t gc) {
-    pdl_wait();
-    pdl_trigger();
-    const int64_t i = blockIdx.z, c = blockIdx.x * (int64_t)THREADS + threadIdx.x;
-    const int j = blockIdx.y;
-    if (c >= cols) return;
-    double sum = 0.0;
-    for (int64_t t0 = 0; t0 < rows; t0 += 64) {
-        float part = 0.f;
-        for (int64_t t = t0; t < min(t0 + 64, rows); ++t)
-            if (adapter_of(ids, t) == i) part = fmaf(v[t * rank + j], x.at(t * x.ld + c), part);
-        sum += part;
-    }
-    put(g, g_dtype, i * rank * cols + j * gj + c * gc, (float)sum);
-}
+// ---------------------------------------------------------------- host
 
 inline bool adapter_matrix_ok(const void *p, int64_t sa, int64_t sr, int64_t adapters, int64_t rows, int64_t cols, int es) {
     if (adapters == 0 || rows == 0 || cols == 0) return true;
@@ -105,26 +379,61 @@ inline bool matrix_ok(const void *p, int64_t ld, int64_t rows, int64_t cols, int
     return p != nullptr && aligned(p, es) && (rows == 1 || ld >= cols);
 }
 inline bool sizes_ok(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n) {
-    return t >= 0 && t <= INT32_MAX && adapters >= 0 && adapters <= 65535 && rank >= 0 && rank <= CT_MAX_RANK && k >= 0 && k <= INT32_MAX &&
-           n >= 0 && n <= INT32_MAX;
+    return t >= 0 && t <= INT32_MAX && adapters >= 0 && adapters <= CT_MAX_ADAPTERS && rank >= 0 && rank <= CT_MAX_RANK && k >= 0 &&
+           k <= INT32_MAX && n >= 0 && n <= INT32_MAX;
 }
-inline size_t part_bytes(int64_t t, int64_t rank) { return ((size_t)t * (size_t)rank * 4 + 15) / 16 * 16; }
+inline int64_t tiles_of(int64_t t, int64_t adapters, bool ordered) {
+    const int64_t most = (t + AD_ROWS - 1) / AD_ROWS;
+    if (!ordered) return most;
+    const int64_t partly = t < adapters + 2 ? t : adapters + 2;
+    return most + partly;
+}
 
-cudaError_t shrink(const Any &x, const Any &m, int64_t sj, int64_t sc, const int64_t *ids, const float *scale, int64_t t, int64_t adapters,
-                   int rank, int64_t cols, float *v, cudaStream_t st) {
-    return pdl_launch(shrink_kernel, dim3((unsigned)t), dim3(THREADS), 0, st, x, m, sj, sc, ids, scale, adapters, rank, cols, v);
+// The workspace: vectors (BF16 parts by slots; few rows: FP32), the order.
+struct Space {
+    size_t v, u, order, spare, first, end, tiles, n_tiles, total;
+};
+inline size_t up(size_t n) { return (n + 255) / 256 * 256; }
+Space space_of(int64_t t, int64_t adapters, int64_t rank, bool grad) {
+    Space s;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up(bytes);
+        return here;
+    };
+    const size_t vec = (size_t)t * (size_t)ad_padded(rank) * 2 * 3;
+    s.v = take(vec);
+    s.u = take(grad ? vec : 0);
+    s.order = take((size_t)t * 4);
+    s.spare = take((size_t)t * 4);
+    s.first = take((size_t)(adapters + 2) * 4);
+    s.end = take((size_t)(adapters + 2) * 4);
+    s.tiles = take((size_t)tiles_of(t, adapters, true) * sizeof(AdTile));
+    s.n_tiles = take(4);
+    s.total = at;
+    return s;
 }
-cudaError_t expand(void *y, int32_t y_dtype, int64_t ldy, const Any &m, int64_t sc, int64_t sj, const int64_t *ids, int64_t t,
-                   int64_t adapters, int rank, int64_t cols, int relu, const float *v, cudaStream_t st) {
-    const int64_t by = (cols + THREADS - 1) / THREADS;
-    return pdl_launch(expand_kernel, dim3((unsigned)t, (unsigned)(by < 256 ? by : 256)), dim3(THREADS), 0, st, y, y_dtype, ldy, m, sc, sj,
-                      ids, adapters, rank, cols, relu, v);
+
+cudaError_t make_order(AdOrder &o, const int64_t *ids, int64_t t, int64_t adapters, const Space &s, char *w, cudaStream_t st) {
+    o = {nullptr, nullptr, nullptr, nullptr, nullptr, t, (int)adapters};
+    if (ids == nullptr) return cudaSuccess;
+    OrderArgs a = {ids, t, (int)adapters, reinterpret_cast<int32_t *>(w + s.order), reinterpret_cast<int32_t *>(w + s.spare),
+                   reinterpret_cast<int32_t *>(w + s.first), reinterpret_cast<int32_t *>(w + s.end), reinterpret_cast<AdTile *>(w + s.tiles),
+                   reinterpret_cast<int32_t *>(w + s.n_tiles)};
+    o.order = a.order;
+    o.first = a.first;
+    o.end = a.end;
+    o.tiles = a.tiles;
+    o.n_tiles = a.n_tiles;
+    return pdl_launch(order_kernel, dim3(1), dim3(ORDER_THREADS), 0, st, a);
 }
-cudaError_t outer(const Any &x, const float *v, const int64_t *ids, int64_t t, int64_t adapters, int rank, int64_t cols, void *g,
-                  int32_t g_dtype, int64_t gj, int64_t gc, cudaStream_t st) {
-    return pdl_launch(outer_kernel, dim3((unsigned)((cols + THREADS - 1) / THREADS), (unsigned)rank, (unsigned)adapters), dim3(THREADS), 0,
-                      st, x, v, ids, t, rank, cols, g, g_dtype, gj, gc);
+
+// whether the rows of the adapters' matrices start on 16 bytes (a stride that is not walked does not matter)
+inline bool stack_whole(const void *p, int64_t sa, int64_t sr, int64_t adapters, int64_t rows, int es) {
+    return aligned(p, 16) && (adapters <= 1 || sa * es % 16 == 0) && (rows <= 1 || sr * es % 16 == 0);
 }
+inline bool all_whole(const void *p, int64_t ld, int64_t rows, int es) { return aligned(p, 16) && (rows <= 1 || ld * es % 16 == 0); }
 }  // namespace
 }  // namespace ops
 }  // namespace ct
@@ -133,7 +442,7 @@ extern "C" ct_status ct_adapters_workspace(int64_t t, int64_t adapters, int64_t 
     using namespace ct::ops;
     if (bytes == nullptr) return CT_EINVAL;
     if (!sizes_ok(t, adapters, rank, k, n)) return CT_ERANGE;
-    *bytes = part_bytes(t, rank);
+    *bytes = space_of(t, adapters, rank, false).total;
     return CT_OK;
 }
 
@@ -146,19 +455,38 @@ extern "C" ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, cons
     if (!dtype_ok(y_dtype) || !dtype_ok(dtype) || (x_dtype != dtype && x_dtype != CT_DT_F32)) return CT_EINVAL;
     if (!sizes_ok(t, adapters, rank, k, n)) return CT_ERANGE;
     if (t == 0 || n == 0) return CT_OK;
-    const int es = dtype_size(dtype);
-    if (!matrix_ok(y_dev, ldy, t, n, dtype_size(y_dtype)) || !matrix_ok(x_dev, ldx, t, k, dtype_size(x_dtype)) ||
+    const int es = dtype_size(dtype), xs = dtype_size(x_dtype), ys = dtype_size(y_dtype);
+    if (!matrix_ok(y_dev, ldy, t, n, ys) || !matrix_ok(x_dev, ldx, t, k, xs) ||
         !adapter_matrix_ok(a_dev, a_adapter, a_row, adapters, rank, k, es) ||
         !adapter_matrix_ok(b_dev, b_adapter, b_row, adapters, n, rank, es) || !aligned(ids_dev, 8) || !aligned(scale_dev, 4))
         return CT_EINVAL;
     if (ids_dev == nullptr && adapters == 0) return CT_EINVAL;
-    if (part_bytes(t, rank) > 0 && (workspace_dev == nullptr || !aligned(workspace_dev, 16))) return CT_EINVAL;
-    if (workspace_bytes < part_bytes(t, rank)) return CT_ENOMEM;
+    const Space s = space_of(t, adapters, rank, false);
+    if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
+    if (workspace_bytes < s.total) return CT_ENOMEM;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    float *v = static_cast<float *>(workspace_dev);
-    cudaError_t e = cudaSuccess;
-    if (rank > 0) e = shrink({x_dev, ldx, 0, x_dtype}, {a_dev, 0, a_adapter, dtype}, a_row, 1, ids_dev, scale_dev, t, adapters, (int)rank, k, v, st);
-    if (e == cudaSuccess) e = expand(y_dev, y_dtype, ldy, {b_dev, 0, b_adapter, dtype}, b_row, 1, ids_dev, t, adapters, (int)rank, n, relu != 0, v, st);
+    char *w = static_cast<char *>(workspace_dev);
+    const bool xw = all_whole(x_dev, ldx, t, xs), aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, es),
+               bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, es), yw = all_whole(y_dev, ldy, t, ys);
+    cudaError_t e;
+    // few rows, and adapters enough that hardly 16 rows have the same one
+    if (t <= FEW && t <= 16 * adapters) {
+        const FewArgs f = {x_dev, ldx, a_dev, a_adapter, a_row, b_dev, b_adapter, b_row, ids_dev, scale_dev, (int)t, (int)adapters, (int)rank, k,
+                           n, reinterpret_cast<float *>(w + s.v), y_dev, y_dtype, ldy, relu != 0, (int)xw | (int)aw << 1 | (int)bw << 2};
+        if (dtype == CT_DT_F32) e = few<float, float>(f, st);
+        else if (dtype == CT_DT_F16) e = x_dtype == CT_DT_F32 ? few<float, __half>(f, st) : few<__half, __half>(f, st);
+        else e = x_dtype == CT_DT_F32 ? few<float, __nv_bfloat16>(f, st) : few<__nv_bfloat16, __nv_bfloat16>(f, st);
+        return e == cudaSuccess ? CT_OK : CT_ECUDA;
+    }
+    AdOrder o;
+    e = make_order(o, ids_dev, t, adapters, s, w, st);
+    const int tiles = (int)tiles_of(t, adapters, ids_dev != nullptr), parts = y_dtype == CT_DT_F32 ? 3 : 2;
+    if (e == cudaSuccess && rank > 0 && adapters > 0)
+        e = ad_shrink({x_dev, ldx, k, a_dev, a_adapter, a_row, scale_dev, (int)rank, (int)xw | (int)aw << 1, w + s.v, parts}, x_dtype, dtype,
+                      false, o, tiles, st);
+    if (e == cudaSuccess)
+        e = ad_expand({y_dev, y_dtype, ldy, n, b_dev, b_adapter, b_row, (int)rank, (int)yw | (int)bw << 1, relu != 0, w + s.v, parts, 0}, dtype,
+                      false, o, tiles, st);
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
 
@@ -166,7 +494,7 @@ extern "C" ct_status ct_adapters_grad_workspace(int64_t t, int64_t adapters, int
     using namespace ct::ops;
     if (bytes == nullptr) return CT_EINVAL;
     if (!sizes_ok(t, adapters, rank, k, n)) return CT_ERANGE;
-    *bytes = 2 * part_bytes(t, rank);
+    *bytes = space_of(t, adapters, rank, true).total;
     return CT_OK;
 }
 
@@ -181,30 +509,43 @@ extern "C" ct_status ct_adapters_grad(const void *dy_dev, int32_t dy_dtype, int6
         (grad_dtype != dtype && grad_dtype != CT_DT_F32) || (dx_dev != nullptr && !dtype_ok(dx_dtype)))
         return CT_EINVAL;
     if (!sizes_ok(t, adapters, rank, k, n)) return CT_ERANGE;
-    const int es = dtype_size(dtype), ges = dtype_size(grad_dtype);
-    if (!matrix_ok(dy_dev, lddy, t, n, dtype_size(dy_dtype)) || !matrix_ok(x_dev, ldx, t, k, dtype_size(x_dtype)) ||
+    const int es = dtype_size(dtype), ges = dtype_size(grad_dtype), xs = dtype_size(x_dtype), dys = dtype_size(dy_dtype);
+    const int dxs = dx_dev != nullptr ? dtype_size(dx_dtype) : 4;
+    if (!matrix_ok(dy_dev, lddy, t, n, dys) || !matrix_ok(x_dev, ldx, t, k, xs) ||
         !adapter_matrix_ok(a_dev, a_adapter, a_row, adapters, rank, k, es) ||
         !adapter_matrix_ok(b_dev, b_adapter, b_row, adapters, n, rank, es) || !aligned(ids_dev, 8) || !aligned(scale_dev, 4) ||
-        (dx_dev != nullptr && !matrix_ok(dx_dev, lddx, t, k, dtype_size(dx_dtype))) ||
+        (dx_dev != nullptr && !matrix_ok(dx_dev, lddx, t, k, dxs)) ||
         (adapters * rank * k > 0 && (da_dev == nullptr || !aligned(da_dev, ges))) ||
         (adapters * rank * n > 0 && (db_dev == nullptr || !aligned(db_dev, ges))))
         return CT_EINVAL;
     if (ids_dev == nullptr && adapters == 0 && t > 0) return CT_EINVAL;
-    const size_t part = part_bytes(t, rank);
-    if (part > 0 && (workspace_dev == nullptr || !aligned(workspace_dev, 16))) return CT_EINVAL;
-    if (workspace_bytes < 2 * part) return CT_ENOMEM;
+    const Space s = space_of(t, adapters, rank, true);
+    if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
+    if (workspace_bytes < s.total) return CT_ENOMEM;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    float *v = static_cast<float *>(workspace_dev), *u = v + part / 4;
-    const Any x = {x_dev, ldx, 0, x_dtype}, dy = {dy_dev, lddy, 0, dy_dtype}, a = {a_dev, 0, a_adapter, dtype}, b = {b_dev, 0, b_adapter, dtype};
-    const int r = (int)rank;
-    cudaError_t e = cudaSuccess;
-    if (t > 0 && rank > 0) {
-        e = shrink(x, a, a_row, 1, ids_dev, scale_dev, t, adapters, r, k, v, st);
-        if (e == cudaSuccess) e = shrink(dy, b, 1, b_row, ids_dev, scale_dev, t, adapters, r, n, u, st);
+    char *w = static_cast<char *>(workspace_dev);
+    const bool xw = all_whole(x_dev, ldx, t, xs), dyw = all_whole(dy_dev, lddy, t, dys), dxw = all_whole(dx_dev, lddx, t, dxs);
+    const bool aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, es), bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, es);
+    const int r = (int)rank, tiles = (int)tiles_of(t, adapters, ids_dev != nullptr);
+    // three parts of the short vectors where a result of 32 bits hangs on them
+    if (t == 0) ids_dev = nullptr;                // zeros for all, no rows to order
+    const int v_parts = grad_dtype == CT_DT_F32 ? 3 : 2;
+    const int u_parts = grad_dtype == CT_DT_F32 || (dx_dev != nullptr && dx_dtype == CT_DT_F32) ? 3 : 2;
+    AdOrder o;
+    cudaError_t e = make_order(o, ids_dev, t, adapters, s, w, st);
+    if (e == cudaSuccess && t > 0 && adapters * rank > 0) {
+        e = ad_shrink({x_dev, ldx, k, a_dev, a_adapter, a_row, scale_dev, r, (int)xw | (int)aw << 1, w + s.v, v_parts}, x_dtype, dtype, false, o,
+                      tiles, st);
+        if (e == cudaSuccess)
+            e = ad_shrink({dy_dev, lddy, n, b_dev, b_adapter, b_row, scale_dev, r, (int)dyw | (int)bw << 1, w + s.u, u_parts}, dy_dtype, dtype,
+                          true, o, tiles, st);
     }
     if (e == cudaSuccess && t > 0 && k > 0 && dx_dev != nullptr)
-        e = expand(dx_dev, dx_dtype, lddx, a, 1, a_row, ids_dev, t, adapters, r, k, 0, u, st);
-    if (e == cudaSuccess && adapters * rank * k > 0) e = outer(x, u, ids_dev, t, adapters, r, k, da_dev, grad_dtype, k, 1, st);
-    if (e == cudaSuccess && adapters * rank * n > 0) e = outer(dy, v, ids_dev, t, adapters, r, n, db_dev, grad_dtype, 1, rank, st);
+        e = ad_expand({dx_dev, dx_dtype, lddx, k, a_dev, a_adapter, a_row, r, (int)dxw | (int)aw << 1, 0, w + s.u,
+                       dx_dtype == CT_DT_F32 ? 3 : 2, 0}, dtype, true, o, tiles, st);
+    if (e == cudaSuccess && adapters * rank * k > 0)
+        e = ad_outer({x_dev, ldx, k, w + s.u, grad_dtype == CT_DT_F32 ? 3 : 2, r, (int)xw, da_dev, grad_dtype, 0}, x_dtype, o, st);
+    if (e == cudaSuccess && adapters * rank * n > 0)
+        e = ad_outer({dy_dev, lddy, n, w + s.v, v_parts, r, (int)dyw, db_dev, grad_dtype, 1}, dy_dtype, o, st);
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }

@@ -1,0 +1,204 @@
+// What the adapters' kernels share: the rows' order by adapter, tiles of 16-bit
+// parts in shared memory, and products of those on the tensor cores.
+//
+// The long products (rows by many) run as mma.sync on 16-bit operands with FP32
+// sums.  BF16 values are taken as they are.  FP16 and FP32 values, and the short FP32
+// vectors between two products, are taken apart into BF16 parts of 8 bits each
+// (v = hi + mid + lo; two parts hold an FP16 value), and the products of parts
+// that matter are added: those of parts p and q with p + q <= 1 where the result has 16
+// bits (the rest is below 2^-15 of a term), with p + q <= 2 where it has 32 (2^-22).
+// FP16 by FP16 runs as it is.
+#pragma once
+#include "ops_common.cuh"
+#include "tc_common.cuh"
+
+namespace ct {
+namespace ops {
+
+constexpr int AD_THREADS = 256;                   // 8 warps: 4 over a tile's rows, 2 over its columns
+constexpr int AD_ROWS = 128;                      // rows of a tile
+constexpr int AD_STEP = 64;                       // values along the long axis for each step
+
+// Rows of one adapter: order[slot0 .. slot0 + rows).  key 0: rows without an adapter, 1 + i: adapter i, 1 + adapters: ids out of range.
+struct AdTile {
+    int32_t slot0, key;
+};
+
+// The rows in the order of their adapters (each adapter's in their own), on the device; all null where every row has adapter 0.
+struct AdOrder {
+    const int32_t *order;                         // [t]
+    const int32_t *first, *end;                   // [adapters + 2]: the slots of each key
+    const AdTile *tiles;
+    const int32_t *n_tiles;
+    int64_t t;
+    int adapters;
+};
+
+#ifdef __CUDACC__
+struct AdRows {
+    int64_t slot0;
+    int rows, key;
+};
+__device__ __forceinline__ AdRows ad_tile(const AdOrder &o, int tile) {
+    if (o.order == nullptr) {
+        const int64_t s = (int64_t)tile * AD_ROWS;
+        return {s, (int)(o.t - s < AD_ROWS ? o.t - s : AD_ROWS), 1};
+    }
+    if (tile >= *o.n_tiles) return {0, 0, 0};
+    const AdTile d = o.tiles[tile];
+    const int left = o.end[d.key] - d.slot0;
+    return {d.slot0, left < AD_ROWS ? left : AD_ROWS, d.key};
+}
+
+// BF16 parts that hold a value
+template <typename T> struct Parts { static constexpr int N = 1; };
+template <> struct Parts<__half> { static constexpr int N = 2; };
+template <> struct Parts<float> { static constexpr int N = 3; };
+
+// Eight values of a row as they lie in memory.
+template <typename T> struct Eight {
+    uint4 u[sizeof(T) / 2];
+};
+
+// 16 bytes from any address on, of which `bytes` are wanted (the others become 0); reads aligned units that hold a wanted byte only
+__device__ __forceinline__ uint4 load_any(const char *p, int bytes) {
+    if (bytes <= 0) return make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t shift = (uint32_t)(uintptr_t)p & 15u;
+    const uint4 *q = reinterpret_cast<const uint4 *>(p - shift);
+    uint4 a = __ldg(q);
+    if (shift != 0) {
+        uint4 b = make_uint4(0u, 0u, 0u, 0u);
+        if ((int)shift + bytes > 16) b = __ldg(q + 1);
+        a = shifted(a, b, shift);
+    }
+    return bytes >= 16 ? a : first_bytes(a, bytes);
+}
+
+// values c to c + 7 of a row of `cols`; zeros behind its end.  whole: the row starts on 16 bytes
+template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T *row, int64_t c, int64_t cols, bool whole) {
+    Eight<T> e;
+    const char *p = reinterpret_cast<const char *>(row + c);
+    if (whole && c + 8 <= cols) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    } else {
+        const int64_t left = (cols - c) * (int64_t)sizeof(T);
+        const int bytes = left > 64 ? 64 : (int)left;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = load_any(p + 16 * i, bytes - 16 * i);
+    }
+    return e;
+}
+template <typename T> __device__ __forceinline__ Eight<T> zero_eight() {
+    Eight<T> e;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = make_uint4(0u, 0u, 0u, 0u);
+    return e;
+}
+
+// what is left of v after its BF16 rounding h; nothing where h is infinite or NaN, so that those stay what they are
+__device__ __forceinline__ float rest_of(float v, float h) {
+    const float r = v - h;
+    return fabsf(r) < __builtin_huge_valf() ? r : 0.f;
+}
+__device__ __forceinline__ uint32_t split2(float &a, float &b) {
+    const uint32_t w = pack2<__nv_bfloat16>(a, b);
+    a = rest_of(a, __uint_as_float(w << 16));
+    b = rest_of(b, __uint_as_float(w & 0xFFFF0000u));
+    return w;
+}
+// eight values as N parts of 16 bytes
+template <int N, typename T> __device__ __forceinline__ void split8(const Eight<T> &e, uint4 (&out)[N]) {
+    if constexpr (N == 1) {
+        out[0] = e.u[0];
+    } else {
+        float v[8];
+        unpack16<T>(e.u[0], v);
+        if constexpr (sizeof(T) == 4) unpack16<T>(e.u[1], v + 4);
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            out[p].x = split2(v[0], v[1]);
+            out[p].y = split2(v[2], v[3]);
+            out[p].z = split2(v[4], v[5]);
+            out[p].w = split2(v[6], v[7]);
+        }
+    }
+}
+
+__device__ __forceinline__ void sts16(uint32_t addr, const uint4 &v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void sts4(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void ldsm_x4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t (&r)[4]) { tc::ldsm_x4(addr, r[0], r[1], r[2], r[3]); }
+
+// D += A (16 x 16) B (16 x 8), 16-bit operands, FP32 sums
+template <bool F16> __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Row pitch in bytes of a tile of `width` 16-bit values: 16 more than the values, so that eight rows of a matrix lie in different banks.
+__host__ __device__ constexpr int ad_pitch(int width) { return 2 * width + 16; }
+
+__device__ __forceinline__ float ld_peer_f32(uint32_t addr, int rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_shared(addr, (uint32_t)rank)) : "memory");
+    return v;
+}
+#endif
+
+inline bool rows_whole(const void *p, int64_t ld_bytes) { return aligned(p, 16) && ld_bytes % 16 == 0; }
+
+// One product with a matrix of the adapters.  `whole`: bit 0: x's rows start on 16 bytes, bit 1: the matrix's do.
+struct AdShrink {
+    const void *x;
+    int64_t ldx, cols;
+    const void *m;
+    int64_t m_adapter, m_row;
+    const float *scale;
+    int rank, whole;
+    void *v;                                      // BF16 [parts][t][padded rank], by slots
+    int parts;
+};
+struct AdExpand {
+    void *y;
+    int32_t y_dtype;
+    int64_t ldy, cols;
+    const void *m;
+    int64_t m_adapter, m_row;
+    int rank, whole, relu;
+    const void *v;
+    int parts;
+    int64_t per;                                  // columns of a block
+};
+struct AdOuter {
+    const void *x;
+    int64_t ldx, cols;
+    const void *v;
+    int parts;
+    int rank, whole;
+    void *g;                                      // [adapters][rank][cols], or [adapters][cols][rank] where by_cols
+    int32_t g_dtype;
+    int by_cols;
+};
+
+inline int ad_padded(int64_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+
+// trans: the matrix has the rank along its rows ([cols, rank]) for shrink, the columns along its rows ([rank, cols]) for expand
+cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
+cudaError_t ad_expand(const AdExpand &a, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
+cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st);
+
+}  // namespace ops
+}  // namespace ct

@@ -1,0 +1,283 @@
+// The second product of an adapter: its short vectors against the many rows of B (or columns of A), added to y in place.
+//
+//   y[t][c] = act(y[t][c] + sum_j m[i](c, j) v[t][j])
+//
+// Bound by y's bytes, read once and written once.  A CTA holds the parts of 128 vectors in shared memory and goes along y
+// in steps of 64 columns.  The columns of a step are dealt to the tensor cores' so that a thread's sums are eight
+// neighbouring columns of a row: y goes from memory to registers and back without shared memory where its rows start on
+// 16 bytes.
+#include "adapters.cuh"
+
+namespace ct {
+namespace ops {
+namespace {
+
+template <typename TM, int RP, bool TRANS> struct Expand {
+    static constexpr int PM = Parts<TM>::N;
+    static constexpr int LV = ad_pitch(RP), LM = ad_pitch(TRANS ? AD_STEP : RP);
+    static constexpr int V_BYTES = AD_ROWS * LV, M_ROWS = TRANS ? RP : AD_STEP, M_BYTES = M_ROWS * LM;
+    static constexpr int WIDE = 33, OUT = 8 * 8 * WIDE * 4;                      // 8 x 32 sums of each warp, where rows start anywhere
+    static constexpr int M_VECS = M_ROWS * (TRANS ? AD_STEP / 8 : RP / 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
+    static int smem(int parts, bool out) { return parts * V_BYTES + 2 * PM * M_BYTES + (out ? OUT : 0); }
+};
+
+// eight neighbouring values of a row of y, from 16 bytes on
+__device__ __forceinline__ void y_load(const char *p, int dtype, float *v) {
+    uint4 u = *reinterpret_cast<const uint4 *>(p);
+    if (dtype == CT_DT_F32) {
+        unpack16<float>(u, v);
+        u = *reinterpret_cast<const uint4 *>(p + 16);
+        unpack16<float>(u, v + 4);
+    } else if (dtype == CT_DT_F16) {
+        unpack16<__half>(u, v);
+    } else {
+        unpack16<__nv_bfloat16>(u, v);
+    }
+}
+__device__ __forceinline__ void y_store(char *p, int dtype, const float *v) {
+    if (dtype == CT_DT_F32) {
+        *reinterpret_cast<uint4 *>(p) = pack16<float>(v);
+        *reinterpret_cast<uint4 *>(p + 16) = pack16<float>(v + 4);
+    } else {
+        *reinterpret_cast<uint4 *>(p) = dtype == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
+    }
+}
+__device__ __forceinline__ float y_one(const char *p, int dtype) {
+    return dtype == CT_DT_F32   ? *reinterpret_cast<const float *>(p)
+           : dtype == CT_DT_F16 ? to_f32(*reinterpret_cast<const __half *>(p))
+                                : to_f32(*reinterpret_cast<const __nv_bfloat16 *>(p));
+}
+__device__ __forceinline__ void y_put(char *p, int dtype, float v) {
+    if (dtype == CT_DT_F32) *reinterpret_cast<float *>(p) = v;
+    else if (dtype == CT_DT_F16) *reinterpret_cast<__half *>(p) = __float2half_rn(v);
+    else *reinterpret_cast<__nv_bfloat16 *>(p) = __float2bfloat16_rn(v);
+}
+
+template <typename TM, int RP, bool TRANS>
+__global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, const AdOrder o) {
+    using S = Expand<TM, RP, TRANS>;
+    extern __shared__ __align__(128) unsigned char sm[];
+    __shared__ int32_t rows[AD_ROWS];
+    pdl_wait();
+    pdl_trigger();
+    const AdRows tile = ad_tile(o, (int)blockIdx.x);
+    const int64_t c_from = (int64_t)blockIdx.y * a.per, c_to = min(c_from + a.per, a.cols);
+    if (tile.rows == 0 || c_from >= c_to || (tile.key == 0 && !a.relu)) return;
+    const bool out = tile.key > o.adapters, none = tile.key == 0;               // NaN; act alone
+    const uint32_t base = tc::smem_u32(sm), bm0 = base + a.parts * S::V_BYTES;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
+    const bool m_whole = a.whole & 2, y_whole = a.whole & 1;
+    const int ys = a.y_dtype == CT_DT_F32 ? 4 : 2;
+    if (tid < AD_ROWS) rows[tid] = tid < tile.rows ? (o.order != nullptr ? o.order[tile.slot0 + tid] : (int32_t)(tile.slot0 + tid)) : -1;
+
+    const bool product = !out && !none && a.rank > 0;
+    const TM *m = static_cast<const TM *>(a.m) + (product ? (int64_t)(tile.key - 1) * a.m_adapter : 0);
+    Eight<TM> em[S::MV];
+    auto fetch = [&](int64_t c0) {
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            const int v = tid + i * AD_THREADS;
+            em[i] = zero_eight<TM>();
+            if (v < S::M_VECS) {
+                if constexpr (TRANS) {
+                    const int j = v / 8;
+                    const int64_t c = c0 + v % 8 * 8;
+                    if (j < a.rank && c < a.cols) em[i] = load_eight(m + j * a.m_row, c, a.cols, m_whole);
+                } else {
+                    const int64_t c = c0 + v / (RP / 8);
+                    const int j = v % (RP / 8) * 8;
+                    if (c < a.cols && j < a.rank) em[i] = load_eight(m + c * a.m_row, j, a.rank, m_whole);
+                }
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        const uint32_t bm = bm0 + buf * (S::PM * S::M_BYTES);
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            const int v = tid + i * AD_THREADS;
+            if (v >= S::M_VECS) continue;
+            uint4 p[S::PM];
+            split8<S::PM>(em[i], p);
+#pragma unroll
+            for (int q = 0; q < S::PM; ++q) {
+                const uint32_t at = bm + q * S::M_BYTES;
+                if constexpr (TRANS) {
+                    // chunk t of 32 columns: its pair q is what thread t of a quad sums as its pair of tile q
+                    const uint32_t row = at + v / 8 * S::LM + (v % 8 / 4) * 64 + (v % 4) * 4;
+                    sts4(row, p[q].x);
+                    sts4(row + 16, p[q].y);
+                    sts4(row + 32, p[q].z);
+                    sts4(row + 48, p[q].w);
+                } else {
+                    sts16(at + v / (RP / 8) * S::LM + v % (RP / 8) * 16, p[q]);
+                }
+            }
+        }
+    };
+    if (product) {
+        fetch(c_from);
+        for (int v = tid; v < a.parts * AD_ROWS * (RP / 8); v += AD_THREADS) {
+            const int p = v / (AD_ROWS * (RP / 8)), r = v / (RP / 8) % AD_ROWS, j = v % (RP / 8);
+            uint4 u = make_uint4(0u, 0u, 0u, 0u);
+            if (r < tile.rows) u = *(reinterpret_cast<const uint4 *>(a.v) + ((p * o.t + tile.slot0 + r) * (RP / 8) + j));
+            sts16(base + p * S::V_BYTES + r * S::LV + j * 16, u);
+        }
+        store(0);
+    }
+    __syncthreads();
+    // this thread's rows: lane / 4 + 8 i of the warp's 32
+    char *yr[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int32_t t = rows[wm * 32 + i * 8 + (lane >> 2)];
+        yr[i] = t >= 0 ? static_cast<char *>(a.y) + (int64_t)t * a.ldy * ys : nullptr;
+    }
+    const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
+    const float nan = __uint_as_float(0x7FC00000u);
+    int buf = 0;
+    for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, buf ^= 1) {
+        const bool more = product && c0 + AD_STEP < c_to;
+        if (more) fetch(c0 + AD_STEP);
+        const int64_t mine = c0 + wn * 32 + (lane & 3) * 8;
+        const bool whole = y_whole && mine + 8 <= c_to;
+        float y[4][8];
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (yr[i] != nullptr) y_load(yr[i] + mine * ys, a.y_dtype, y[i]);
+        }
+        float acc[2][4][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
+        if (product) {
+            const uint32_t bm = bm0 + buf * (S::PM * S::M_BYTES);
+#pragma unroll
+            for (int k = 0; k < RP; k += 16)
+                for (int p = 0; p < a.parts; ++p) {
+                    uint32_t fa[2][4];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        ldsm_x4(base + p * S::V_BYTES + (wm * 32 + i * 16 + (q8 & 1) * 8 + r8) * S::LV + (k + (q8 >> 1) * 8) * 2, fa[i]);
+#pragma unroll
+                    for (int q = 0; q < S::PM; ++q) {
+                        if (p + q > most) break;
+#pragma unroll
+                        for (int j = 0; j < 4; j += 2) {
+                            uint32_t b[4];
+                            const int n = j + (q8 >> 1);
+                            if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + wn * 64 + n * 16, b);
+                            else ldsm_x4(bm + q * S::M_BYTES + (wn * 32 + 8 * (r8 >> 1) + 2 * n + (r8 & 1)) * S::LM + (k + (q8 & 1) * 8) * 2, b);
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                mma16<false>(acc[i][j], fa[i], b[0], b[1]);
+                                mma16<false>(acc[i][j + 1], fa[i], b[2], b[3]);
+                            }
+                        }
+                    }
+                }
+        }
+        if (y_whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (yr[i] == nullptr) continue;
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] = acc[i >> 1][j][(i & 1) * 2];
+                    v[2 * j + 1] = acc[i >> 1][j][(i & 1) * 2 + 1];
+                }
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] += y[i][e];
+                        if (a.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
+                        if (out) v[e] = nan;
+                    }
+                    y_store(yr[i] + mine * ys, a.y_dtype, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (mine + e >= c_to) break;
+                        char *at = yr[i] + (mine + e) * ys;
+                        float w = v[e] + y_one(at, a.y_dtype);
+                        if (a.relu) w = w < 0.f ? 0.f : w;
+                        y_put(at, a.y_dtype, out ? nan : w);
+                    }
+                }
+            }
+        } else {
+            // rows that start anywhere: eight rows of the warp's sums at a time turn in shared memory, so that lanes are neighbouring columns
+            float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + 2 * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
+            const int64_t c = c0 + wn * 32 + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float old[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int32_t t = rows[wm * 32 + i * 8 + r];
+                    old[r] = t >= 0 && c < c_to ? y_one(static_cast<char *>(a.y) + ((int64_t)t * a.ldy + c) * ys, a.y_dtype) : 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) w[(lane >> 2) * S::WIDE + (lane & 3) * 8 + 2 * j + e] = acc[i >> 1][j][(i & 1) * 2 + e];
+                __syncwarp();
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int32_t t = rows[wm * 32 + i * 8 + r];
+                    if (t < 0 || c >= c_to) continue;
+                    float v = w[r * S::WIDE + lane] + old[r];
+                    if (a.relu) v = v < 0.f ? 0.f : v;
+                    y_put(static_cast<char *>(a.y) + ((int64_t)t * a.ldy + c) * ys, a.y_dtype, out ? nan : v);
+                }
+                __syncwarp();
+            }
+        }
+        if (more) store(buf ^ 1);
+        __syncthreads();
+    }
+}
+
+template <typename TM, int RP, bool TRANS> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
+    using S = Expand<TM, RP, TRANS>;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = expand_kernel<TM, RP, TRANS>;
+    const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3, true));
+    if (e != cudaSuccess) return e;
+    // columns of a block: as many as leave each SM three blocks, at most 1024
+    AdExpand a = q;
+    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
+    int64_t parts = (3 * (int64_t)sm_count() + tiles - 1) / tiles;
+    if (parts < (steps + 15) / 16) parts = (steps + 15) / 16;
+    if (parts > steps) parts = steps;
+    if (parts > 65535) parts = 65535;
+    a.per = (steps + parts - 1) / parts * AD_STEP;
+    const dim3 grid((unsigned)tiles, (unsigned)((a.cols + a.per - 1) / a.per));
+    return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts, !(a.whole & 1)), st, a, o);
+}
+template <typename TM, bool TRANS> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
+    switch (ad_padded(a.rank)) {
+        case 16: return launch<TM, 16, TRANS>(a, o, tiles, st);
+        case 32: return launch<TM, 32, TRANS>(a, o, tiles, st);
+        case 64: return launch<TM, 64, TRANS>(a, o, tiles, st);
+        default: return launch<TM, 128, TRANS>(a, o, tiles, st);
+    }
+}
+template <bool TRANS> cudaError_t by_type(const AdExpand &a, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
+    return dtype == CT_DT_F32   ? by_rank<float, TRANS>(a, o, tiles, st)
+           : dtype == CT_DT_F16 ? by_rank<__half, TRANS>(a, o, tiles, st)
+                                : by_rank<__nv_bfloat16, TRANS>(a, o, tiles, st);
+}
+}  // namespace
+
+cudaError_t ad_expand(const AdExpand &a, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
+    return trans ? by_type<true>(a, dtype, o, tiles, st) : by_type<false>(a, dtype, o, tiles, st);
+}
+
+}  // namespace ops
+}  // namespace ct

@@ -1,0 +1,225 @@
+// The gradients of an adapter's matrices: sums over its rows of outer products.
+//
+//   g[i](c, j) = sum over the rows t of adapter i of x[t][c] v[t][j]
+//
+// (x: the activations and v: the gradient's short vectors, or the other way round.)  Bound by x's bytes, with 2 rank operations
+// for each value and part of v.  A CTA takes 128 columns of one adapter's rows, 64 rows at a time: both operands lie in
+// shared memory with the summed rows along their own rows, as the transposing matrix loads want them.  A cluster's CTAs
+// share the rows and add their sums in rank order, so every sum has one order.
+#include "adapters.cuh"
+
+namespace ct {
+namespace ops {
+namespace {
+
+constexpr int COLS = 128;
+
+template <typename TX, int RP> struct Outer {
+    static constexpr int PX = Parts<TX>::N;
+    static constexpr int LX = ad_pitch(COLS), LV = ad_pitch(RP);
+    static constexpr int X_BYTES = AD_STEP * LX, V_BYTES = AD_STEP * LV;
+    static constexpr int XV = AD_STEP * (COLS / 8) / AD_THREADS;                  // 4
+    static constexpr int V_VECS = AD_STEP * (RP / 8), VV = (V_VECS + AD_THREADS - 1) / AD_THREADS;
+    static constexpr int NT = RP / 16, SUM = COLS * (RP + 1) * 4;
+    // The tensor cores cut off what they add: sums go from their accumulators into others after 128 rows, or after each 16 where
+    // x's values are several parts.
+    static constexpr bool EACH = PX > 1;
+    static constexpr int FLUSH = 2;
+    static int smem(int parts) {
+        const int two = 2 * (PX * X_BYTES + parts * V_BYTES);
+        return two > SUM ? two : SUM;
+    }
+};
+
+template <typename TX, int RP>
+__global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, const AdOrder o, int splits) {
+    using S = Outer<TX, RP>;
+    extern __shared__ __align__(128) unsigned char sm[];
+    pdl_wait();
+    pdl_trigger();
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, adapter = blockIdx.y;
+    const int64_t cols0 = (int64_t)(blockIdx.x / (unsigned)splits) * COLS;
+    const int64_t from = o.order != nullptr ? o.first[adapter + 1] : 0, to = o.order != nullptr ? o.end[adapter + 1] : adapter == 0 ? o.t : 0;
+    const int64_t steps = (to - from + AD_STEP - 1) / AD_STEP;
+    const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
+    const uint32_t base = tc::smem_u32(sm);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
+    const int buf_bytes = S::PX * S::X_BYTES + a.parts * S::V_BYTES;
+    const bool x_whole = a.whole & 1;
+
+    Eight<TX> ex[S::XV];
+    uint4 ev[3][S::VV];
+    const int64_t xc = cols0 + (tid % (COLS / 8)) * 8;
+    auto fetch = [&](int64_t s) {
+        const int64_t t0 = from + s * AD_STEP;
+#pragma unroll
+        for (int i = 0; i < S::XV; ++i) {
+            const int64_t t = t0 + tid / (COLS / 8) + i * (AD_THREADS / (COLS / 8));
+            ex[i] = zero_eight<TX>();
+            if (t < to && xc < a.cols)
+                ex[i] = load_eight(static_cast<const TX *>(a.x) + (o.order != nullptr ? (int64_t)o.order[t] : t) * a.ldx, xc, a.cols, x_whole);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            if (p >= a.parts) break;
+#pragma unroll
+            for (int i = 0; i < S::VV; ++i) {
+                const int v = tid + i * AD_THREADS;
+                const int64_t t = t0 + v / (RP / 8);
+                ev[p][i] = make_uint4(0u, 0u, 0u, 0u);
+                if (v < S::V_VECS && t < to) ev[p][i] = *(reinterpret_cast<const uint4 *>(a.v) + ((p * o.t + t) * (RP / 8) + v % (RP / 8)));
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        const uint32_t bx = base + buf * buf_bytes, bv = bx + S::PX * S::X_BYTES;
+#pragma unroll
+        for (int i = 0; i < S::XV; ++i) {
+            uint4 p[S::PX];
+            split8<S::PX>(ex[i], p);
+#pragma unroll
+            for (int q = 0; q < S::PX; ++q)
+                sts16(bx + q * S::X_BYTES + (tid / (COLS / 8) + i * (AD_THREADS / (COLS / 8))) * S::LX + tid % (COLS / 8) * 16, p[q]);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            if (p >= a.parts) break;
+#pragma unroll
+            for (int i = 0; i < S::VV; ++i) {
+                const int v = tid + i * AD_THREADS;
+                if (v < S::V_VECS) sts16(bv + p * S::V_BYTES + v / (RP / 8) * S::LV + v % (RP / 8) * 16, ev[p][i]);
+            }
+        }
+    };
+    float acc[2][S::NT][4], sum[2][S::NT][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = sum[i][j][e] = 0.f;
+    auto flush = [&]() {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum[i][j][e] += acc[i][j][e];
+                    acc[i][j][e] = 0.f;
+                }
+    };
+    const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
+    auto compute = [&](int buf) {
+        const uint32_t bx = base + buf * buf_bytes, bv = bx + S::PX * S::X_BYTES;
+#pragma unroll
+        for (int k = 0; k < AD_STEP; k += 16) {
+            uint32_t fa[S::PX][2][4];
+#pragma unroll
+            for (int p = 0; p < S::PX; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    ldsm_x4_t(bx + p * S::X_BYTES + (k + (q8 >> 1) * 8 + r8) * S::LX + (wm * 32 + i * 16 + (q8 & 1) * 8) * 2, fa[p][i]);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                if (q >= a.parts) break;
+                if constexpr (RP == 16) {
+                    uint32_t b[4];
+                    ldsm_x4_t(bv + q * S::V_BYTES + (k + (q8 & 1) * 8 + r8) * S::LV + wn * 16, b);
+#pragma unroll
+                    for (int p = 0; p < S::PX; ++p)
+                        if (p + q <= most)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) mma16<false>(acc[i][0], fa[p][i], b[0], b[1]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < S::NT; j += 2) {
+                        uint32_t b[4];
+                        ldsm_x4_t(bv + q * S::V_BYTES + (k + (q8 & 1) * 8 + r8) * S::LV + (wn * (RP / 2) + j * 8 + (q8 >> 1) * 8) * 2, b);
+#pragma unroll
+                        for (int p = 0; p < S::PX; ++p)
+                            if (p + q <= most)
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    mma16<false>(acc[i][j], fa[p][i], b[0], b[1]);
+                                    mma16<false>(acc[i][j + 1], fa[p][i], b[2], b[3]);
+                                }
+                    }
+                }
+            }
+            if constexpr (S::EACH) flush();
+        }
+    };
+    if (s0 < s1) {
+        fetch(s0);
+        store(0);
+        __syncthreads();
+        for (int64_t s = s0; s < s1; ++s) {
+            const int buf = (int)(s - s0) & 1;
+            if (s + 1 < s1) fetch(s + 1);
+            compute(buf);
+            if (!S::EACH && (int)(s - s0) % S::FLUSH == S::FLUSH - 1) flush();
+            if (s + 1 < s1) store(buf ^ 1);
+            __syncthreads();
+        }
+    }
+    flush();
+
+    float *fs = reinterpret_cast<float *>(sm);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                fs[(wm * 32 + i * 16 + (e >> 1) * 8 + (lane >> 2)) * (RP + 1) + wn * (RP / 2) + j * 8 + (lane & 3) * 2 + (e & 1)] = sum[i][j][e];
+    if (splits > 1) tc::cluster_sync();
+    else __syncthreads();
+    const int c0 = COLS * rank / splits, c1 = COLS * (rank + 1) / splits, wide = c1 - c0;
+    const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
+    for (int v = tid; v < wide * a.rank; v += AD_THREADS) {
+        const int c = c0 + (a.by_cols ? v / a.rank : v % wide), j = a.by_cols ? v % a.rank : v / wide;
+        if (cols0 + c >= a.cols) continue;
+        const int at = c * (RP + 1) + j;
+        float x = 0.f;
+        for (int q = 0; q < splits; ++q) x += splits > 1 ? ld_peer_f32(base + at * 4, q) : fs[at];
+        const int64_t to_at = g0 + (a.by_cols ? (cols0 + c) * a.rank + j : j * a.cols + cols0 + c);
+        if (a.g_dtype == CT_DT_F32) static_cast<float *>(a.g)[to_at] = x;
+        else if (a.g_dtype == CT_DT_F16) static_cast<__half *>(a.g)[to_at] = __float2half_rn(x);
+        else static_cast<__nv_bfloat16 *>(a.g)[to_at] = __float2bfloat16_rn(x);
+    }
+    if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
+}
+
+template <typename TX, int RP> cudaError_t launch(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
+    using S = Outer<TX, RP>;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = outer_kernel<TX, RP>;
+    const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3));
+    if (e != cudaSuccess) return e;
+    // two CTAs for each SM, with two steps of an adapter's share of the rows at least for each
+    const int64_t blocks = (a.cols + COLS - 1) / COLS, steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP;
+    int splits = 1;
+    while (splits < 8 && blocks * o.adapters * splits < 2 * sm_count() && steps >= 4 * splits) splits *= 2;
+    const dim3 grid((unsigned)(blocks * splits), (unsigned)o.adapters);
+    if (splits == 1) return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, a, o, splits);
+    return pdl_launch_cluster(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, splits, a, o, splits);
+}
+template <typename TX> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
+    switch (ad_padded(a.rank)) {
+        case 16: return launch<TX, 16>(a, o, st);
+        case 32: return launch<TX, 32>(a, o, st);
+        case 64: return launch<TX, 64>(a, o, st);
+        default: return launch<TX, 128>(a, o, st);
+    }
+}
+}  // namespace
+
+cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st) {
+    return x_dtype == CT_DT_F32   ? by_rank<float>(a, o, st)
+           : x_dtype == CT_DT_F16 ? by_rank<__half>(a, o, st)
+                                  : by_rank<__nv_bfloat16>(a, o, st);
+}
+
+}  // namespace ops
+}  // namespace ct

@@ -1,0 +1,248 @@
+// The first product of an adapter: many rows, their long axis against the few rows of A (or B transposed).
+//
+//   v[t][j] = scale[i] sum_c x[t][c] m[i](j, c)
+//
+// Bound by x's bytes: 2 rank operations for each value.  A tile of 128 rows goes along the long axis in steps of 64; a
+// cluster's CTAs share the axis, add their sums through distributed shared memory in rank order, and write v in BF16
+// parts, as the next products take it.
+#include "adapters.cuh"
+
+namespace ct {
+namespace ops {
+namespace {
+
+template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
+    static constexpr bool F16 = sizeof(TX) == 2 && Parts<TX>::N == 2 && Parts<TM>::N == 2;
+    static constexpr int PX = F16 ? 1 : Parts<TX>::N, PM = F16 ? 1 : Parts<TM>::N;
+    static constexpr int LX = ad_pitch(AD_STEP), LM = ad_pitch(TRANS ? RP : AD_STEP);
+    static constexpr int X_BYTES = AD_ROWS * LX, M_ROWS = TRANS ? AD_STEP : RP, M_BYTES = M_ROWS * LM;
+    static constexpr int BUF = PX * X_BYTES + PM * M_BYTES;
+    static constexpr int SUM = AD_ROWS * (RP + 1) * 4;
+    static constexpr int SMEM = 2 * BUF > SUM ? 2 * BUF : SUM;
+    static constexpr int XV = AD_ROWS * 8 / AD_THREADS;                          // vectors of 8 values a thread loads
+    static constexpr int M_VECS = M_ROWS * (TRANS ? RP / 8 : 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
+    static constexpr int NT = RP / 16;                                           // 8-column tiles of a warp
+    // The tensor cores cut off what they add: sums go from their accumulators into others after 256 values, or after each 16
+    // where a value is several products.
+    static constexpr bool EACH = PX * PM > 1;
+    static constexpr int FLUSH = 4;
+};
+
+template <typename TX, typename TM, int RP, bool TRANS>
+__global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, const AdOrder o, int splits) {
+    using S = Shrink<TX, TM, RP, TRANS>;
+    extern __shared__ __align__(128) unsigned char sm[];
+    pdl_wait();
+    pdl_trigger();
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0;
+    const AdRows tile = ad_tile(o, (int)(blockIdx.x / (unsigned)splits));
+    if (tile.rows == 0 || tile.key == 0 || tile.key > o.adapters) return;       // the whole cluster alike
+    const int adapter = tile.key - 1;
+    const uint32_t base = tc::smem_u32(sm);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
+    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
+    const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
+    const bool x_whole = a.whole & 1, m_whole = a.whole & 2;
+
+    // this thread's vectors: of x, rows tid / 8 + 32 i, 8 values at 8 (tid % 8)
+    const TX *xr[S::XV];
+    const int xc = (tid & 7) * 8;
+#pragma unroll
+    for (int i = 0; i < S::XV; ++i) {
+        const int r = tid / 8 + 32 * i;
+        const int64_t s = tile.slot0 + r;
+        xr[i] = r < tile.rows ? static_cast<const TX *>(a.x) + (o.order != nullptr ? (int64_t)o.order[s] : s) * a.ldx : nullptr;
+    }
+    const TM *m = static_cast<const TM *>(a.m) + adapter * a.m_adapter;
+    Eight<TX> ex[S::XV];
+    Eight<TM> em[S::MV];
+    auto fetch = [&](int64_t s) {
+        const int64_t c0 = s * AD_STEP;
+#pragma unroll
+        for (int i = 0; i < S::XV; ++i) ex[i] = xr[i] != nullptr && c0 + xc < a.cols ? load_eight(xr[i], c0 + xc, a.cols, x_whole) : zero_eight<TX>();
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            const int v = tid + i * AD_THREADS;
+            em[i] = zero_eight<TM>();
+            if (v < S::M_VECS) {
+                if constexpr (TRANS) {
+                    const int64_t c = c0 + v / (RP / 8);
+                    const int j = v % (RP / 8) * 8;
+                    if (c < a.cols && j < a.rank) em[i] = load_eight(m + c * a.m_row, j, a.rank, m_whole);
+                } else {
+                    const int j = v / 8;
+                    const int64_t c = c0 + v % 8 * 8;
+                    if (j < a.rank && c < a.cols) em[i] = load_eight(m + j * a.m_row, c, a.cols, m_whole);
+                }
+            }
+        }
+    };
+    auto store = [&](int buf) {
+        const uint32_t bx = base + buf * S::BUF, bm = bx + S::PX * S::X_BYTES;
+#pragma unroll
+        for (int i = 0; i < S::XV; ++i) {
+            uint4 p[S::PX];
+            split8<S::PX>(ex[i], p);
+#pragma unroll
+            for (int q = 0; q < S::PX; ++q) sts16(bx + q * S::X_BYTES + (tid / 8 + 32 * i) * S::LX + xc * 2, p[q]);
+        }
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            const int v = tid + i * AD_THREADS;
+            if (v >= S::M_VECS) continue;
+            uint4 p[S::PM];
+            split8<S::PM>(em[i], p);
+            const int w = TRANS ? RP / 8 : 8;
+#pragma unroll
+            for (int q = 0; q < S::PM; ++q) sts16(bm + q * S::M_BYTES + v / w * S::LM + v % w * 16, p[q]);
+        }
+    };
+
+    float acc[2][S::NT][4], sum[2][S::NT][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = sum[i][j][e] = 0.f;
+    auto flush = [&]() {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum[i][j][e] += acc[i][j][e];
+                    acc[i][j][e] = 0.f;
+                }
+    };
+    const int q8 = lane >> 3, r8 = lane & 7;
+    auto compute = [&](int buf) {
+        const uint32_t bx = base + buf * S::BUF, bm = bx + S::PX * S::X_BYTES;
+#pragma unroll
+        for (int k = 0; k < AD_STEP; k += 16) {
+            uint32_t fa[S::PX][2][4];
+#pragma unroll
+            for (int p = 0; p < S::PX; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    ldsm_x4(bx + p * S::X_BYTES + (wm * 32 + i * 16 + (q8 & 1) * 8 + r8) * S::LX + (k + (q8 >> 1) * 8) * 2, fa[p][i]);
+            if constexpr (RP == 16) {
+                // one 8-column tile a warp: both halves of k by lanes 0 to 15's addresses
+#pragma unroll
+                for (int q = 0; q < S::PM; ++q) {
+                    uint32_t b[4];
+                    if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + wn * 16, b);
+                    else ldsm_x4(bm + q * S::M_BYTES + (wn * 8 + r8) * S::LM + (k + (q8 & 1) * 8) * 2, b);
+#pragma unroll
+                    for (int p = 0; p < S::PX; ++p)
+                        if (p + q <= 2)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) mma16<S::F16>(acc[i][0], fa[p][i], b[0], b[1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < S::NT; j += 2)
+#pragma unroll
+                    for (int q = 0; q < S::PM; ++q) {
+                        uint32_t b[4];
+                        const int n = wn * (RP / 2) + j * 8 + (q8 >> 1) * 8;
+                        if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + n * 2, b);
+                        else ldsm_x4(bm + q * S::M_BYTES + (n + r8) * S::LM + (k + (q8 & 1) * 8) * 2, b);
+#pragma unroll
+                        for (int p = 0; p < S::PX; ++p)
+                            if (p + q <= 2)
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    mma16<S::F16>(acc[i][j], fa[p][i], b[0], b[1]);
+                                    mma16<S::F16>(acc[i][j + 1], fa[p][i], b[2], b[3]);
+                                }
+                    }
+            }
+            if constexpr (S::EACH) flush();
+        }
+    };
+
+    if (s0 < s1) {
+        fetch(s0);
+        store(0);
+        __syncthreads();
+        for (int64_t s = s0; s < s1; ++s) {
+            const int buf = (int)(s - s0) & 1;
+            if (s + 1 < s1) fetch(s + 1);
+            compute(buf);
+            if (!S::EACH && (int)(s - s0) % S::FLUSH == S::FLUSH - 1) flush();
+            if (s + 1 < s1) store(buf ^ 1);
+            __syncthreads();
+        }
+    }
+    flush();
+
+    // the tile's sums of this CTA, then of all of the cluster
+    float *fs = reinterpret_cast<float *>(sm);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                fs[(wm * 32 + i * 16 + (e >> 1) * 8 + (lane >> 2)) * (RP + 1) + wn * (RP / 2) + j * 8 + (lane & 3) * 2 + (e & 1)] = sum[i][j][e];
+    if (splits > 1) tc::cluster_sync();
+    else __syncthreads();
+    const float scale = a.scale != nullptr ? a.scale[adapter] : 1.f;
+    const int r0 = AD_ROWS * rank / splits, r1 = AD_ROWS * (rank + 1) / splits;
+    for (int v = tid; v < (r1 - r0) * (RP / 2); v += AD_THREADS) {
+        const int r = r0 + v / (RP / 2), j = v % (RP / 2) * 2;
+        if (r >= tile.rows) break;
+        const int at = r * (RP + 1) + j;
+        float x = 0.f, y = 0.f;
+        for (int c = 0; c < splits; ++c) {
+            x += splits > 1 ? ld_peer_f32(base + at * 4, c) : fs[at];
+            y += splits > 1 ? ld_peer_f32(base + (at + 1) * 4, c) : fs[at + 1];
+        }
+        x = j < a.rank ? x * scale : 0.f;         // 0 and not 0 times what x holds
+        y = j + 1 < a.rank ? y * scale : 0.f;
+        uint32_t *out = static_cast<uint32_t *>(a.v) + ((tile.slot0 + r) * RP + j) / 2;
+        for (int p = 0; p < a.parts; ++p) out[p * (o.t * RP / 2)] = split2(x, y);
+    }
+    if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
+}
+
+template <typename TX, typename TM, int RP, bool TRANS>
+cudaError_t launch(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t st) {
+    using S = Shrink<TX, TM, RP, TRANS>;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = shrink_kernel<TX, TM, RP, TRANS>;
+    const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
+    if (e != cudaSuccess) return e;
+    // two CTAs for each SM, with four steps at least for each
+    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
+    int splits = 1;
+    while (splits < 8 && (int64_t)tiles * splits < 2 * sm_count() && steps >= 8 * splits) splits *= 2;
+    if (splits == 1) return pdl_launch(kernel, dim3((unsigned)tiles), dim3(AD_THREADS), S::SMEM, st, a, o, splits);
+    return pdl_launch_cluster(kernel, dim3((unsigned)(tiles * splits)), dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits);
+}
+template <typename TX, typename TM, bool TRANS>
+cudaError_t by_rank(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t st) {
+    switch (ad_padded(a.rank)) {
+        case 16: return launch<TX, TM, 16, TRANS>(a, o, tiles, st);
+        case 32: return launch<TX, TM, 32, TRANS>(a, o, tiles, st);
+        case 64: return launch<TX, TM, 64, TRANS>(a, o, tiles, st);
+        default: return launch<TX, TM, 128, TRANS>(a, o, tiles, st);
+    }
+}
+template <bool TRANS> cudaError_t by_type(const AdShrink &a, int x_dtype, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
+    if (dtype == CT_DT_F32) return by_rank<float, float, TRANS>(a, o, tiles, st);
+    if (dtype == CT_DT_F16)
+        return x_dtype == CT_DT_F32 ? by_rank<float, __half, TRANS>(a, o, tiles, st) : by_rank<__half, __half, TRANS>(a, o, tiles, st);
+    return x_dtype == CT_DT_F32 ? by_rank<float, __nv_bfloat16, TRANS>(a, o, tiles, st)
+                                : by_rank<__nv_bfloat16, __nv_bfloat16, TRANS>(a, o, tiles, st);
+}
+}  // namespace
+
+cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
+    return trans ? by_type<true>(a, x_dtype, dtype, o, tiles, st) : by_type<false>(a, x_dtype, dtype, o, tiles, st);
+}
+
+}  // namespace ops
+}  // namespace ct

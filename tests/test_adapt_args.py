@@ -31,7 +31,7 @@ def test_adapters(ct):
                 dict(b=D + 1), dict(ids=E + 4), dict(s=E + 2), dict(w=None), dict(w=E + 8), dict(ids=None, count=0)):
         assert call(**bad) == 1, bad
     for bad in (dict(t=-1), dict(count=-1), dict(rank=129), dict(rank=-1), dict(k=-1), dict(n=-1), dict(t=2 ** 31), dict(k=2 ** 31, ldx=2 ** 31),
-                dict(n=2 ** 31), dict(count=65536)):
+                dict(n=2 ** 31), dict(count=65535)):
         assert call(**bad) == 5, bad
     assert call(wb=0) == 2
     assert call(t=0, y=None, x=None) == 0 and call(n=0, y=None, b=None) == 0
@@ -46,7 +46,7 @@ def test_adapters_grad(ct):
                 dict(b=None), dict(da=None), dict(db=None), dict(lddy=7), dict(ldx=15), dict(lddx=15), dict(ar=15), dict(br=3), dict(dy=A + 1),
                 dict(dx=A + 2), dict(da=B + 1), dict(db=C + 1), dict(ids=E + 1), dict(s=E + 1), dict(w=None), dict(w=E + 4)):
         assert call(**bad) == 1, bad
-    for bad in (dict(t=-1), dict(rank=129), dict(k=2 ** 31, ldx=2 ** 31, lddx=2 ** 31), dict(count=65536)):
+    for bad in (dict(t=-1), dict(rank=129), dict(k=2 ** 31, ldx=2 ** 31, lddx=2 ** 31), dict(count=65535)):
         assert call(**bad) == 5, bad
     assert call(wb=0) == 2
     assert call(t=0, count=0) == 0
