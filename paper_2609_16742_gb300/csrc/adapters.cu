@@ -150,7 +150,7 @@ struct FewArgs {
     void *y;
     int32_t y_dtype;
     int64_t ldy;
-    int relu, whole;                              // bits: x, a, b
+    int relu;
 };
 
 // The rows that row `lead` speaks for: all with its id, if it is the first of them.  Returns their number, 0 if it is not.
@@ -197,7 +197,6 @@ template <typename TX, typename TM> __global__ void __launch_bounds__(FEW_THREAD
     if (n == 0 || id < 0 || id >= a.adapters) return;                            // the whole cluster alike
     const TM *m = static_cast<const TM *>(a.a) + id * a.a_adapter;
     const float scale = a.scale != nullptr ? a.scale[id] : 1.f;
-    const bool x_whole = a.whole & 1, m_whole = a.whole & 2;
     // pieces of 256 values (a warp's 32 x 8)
     const int64_t pieces = (a.k + 255) / 256, p0 = pieces * rank / splits, p1 = pieces * (rank + 1) / splits;
     const int groups = (a.rank + FEW_J - 1) / FEW_J, ways = groups >= FEW_WARPS ? 1 : FEW_WARPS / groups;
@@ -209,31 +208,41 @@ template <typename TX, typename TM> __global__ void __launch_bounds__(FEW_THREAD
             for (int j = 0; j < FEW_J; ++j)
 #pragma unroll
                 for (int r = 0; r < FEW_R; ++r) acc[j][r] = 0.f;
-            if (g < groups && warp < groups * ways) {
+            if (g < groups) {
 #pragma unroll 2
                 for (int64_t p = p0 + way; p < p1; p += ways) {
                     const int64_t c = p * 256 + lane * 8;
-                    Eight<TM> em[FEW_J];
-                    Eight<TX> ex[FEW_R];
+                    const int left = left_of(c, a.k);
+                    const TM *mp[FEW_J];
+                    const TX *xp[FEW_R];
+                    Units<TM> um[FEW_J];
+                    Units<TX> ux[FEW_R];
 #pragma unroll
-                    for (int j = 0; j < FEW_J; ++j)
-                        em[j] = c < a.k && g * FEW_J + j < a.rank ? load_eight(m + (g * FEW_J + j) * a.a_row, c, a.k, m_whole) : zero_eight<TM>();
+                    for (int j = 0; j < FEW_J; ++j) {
+                        const bool there = left > 0 && g * FEW_J + j < a.rank;
+                        mp[j] = m + (there ? (g * FEW_J + j) * a.a_row + c : 0);
+                        um[j] = load_units(mp[j], there ? left : 0);
+                    }
 #pragma unroll
-                    for (int r = 0; r < FEW_R; ++r)
-                        ex[r] = c < a.k && r0 + r < n ? load_eight(static_cast<const TX *>(a.x) + rows[r0 + r] * a.ldx, c, a.k, x_whole)
-                                                      : zero_eight<TX>();
+                    for (int r = 0; r < FEW_R; ++r) {
+                        const bool there = left > 0 && r0 + r < n;
+                        xp[r] = static_cast<const TX *>(a.x) + (there ? rows[r0 + r] * a.ldx + c : 0);
+                        ux[r] = load_units(xp[r], there ? left : 0);
+                    }
                     float fm[FEW_J][8];
 #pragma unroll
                     for (int j = 0; j < FEW_J; ++j) {
-                        unpack16<TM>(em[j].u[0], fm[j]);
-                        if constexpr (sizeof(TM) == 4) unpack16<TM>(em[j].u[1], fm[j] + 4);
+                        const Eight<TM> e = take_eight(um[j], mp[j], left);
+                        unpack16<TM>(e.u[0], fm[j]);
+                        if constexpr (sizeof(TM) == 4) unpack16<TM>(e.u[1], fm[j] + 4);
                     }
 #pragma unroll
                     for (int r = 0; r < FEW_R; ++r) {
                         if (r0 + r >= n) break;
                         float fx[8];
-                        unpack16<TX>(ex[r].u[0], fx);
-                        if constexpr (sizeof(TX) == 4) unpack16<TX>(ex[r].u[1], fx + 4);
+                        const Eight<TX> e = take_eight(ux[r], xp[r], left);
+                        unpack16<TX>(e.u[0], fx);
+                        if constexpr (sizeof(TX) == 4) unpack16<TX>(e.u[1], fx + 4);
 #pragma unroll
                         for (int j = 0; j < FEW_J; ++j)
 #pragma unroll
@@ -301,14 +310,17 @@ template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_ke
         pdl_wait();
         return;
     }
-    const TM *m = static_cast<const TM *>(a.b) + (product ? id * a.b_adapter + c * a.b_row : 0);
-    const bool m_whole = a.whole & 4;
+    const TM *m = static_cast<const TM *>(a.b) + (product && mine ? id * a.b_adapter + c * a.b_row : 0);
     constexpr int AHEAD = 4;                      // 32 values of a row of B
-    Eight<TM> em[AHEAD];
-    if (product && mine)
+    Units<TM> um[AHEAD];
+    auto fetch = [&](int j0) {
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-            if (j * 8 < a.rank) em[j] = load_eight(m, j * 8, a.rank, m_whole);
+        for (int j = 0; j < AHEAD; ++j) {
+            const int left = product && mine ? left_of(j0 + j * 8, a.rank) : 0;
+            um[j] = load_units(m + (left > 0 ? j0 + j * 8 : 0), left);
+        }
+    };
+    fetch(0);
     pdl_wait();
     for (int r0 = 0; r0 < n; r0 += 8) {
         const int nr = min(8, n - r0);
@@ -323,11 +335,12 @@ template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_ke
             __syncthreads();
             if (mine)
                 for (int j0 = 0; j0 < a.rank; j0 += 8 * AHEAD) {
+                    if (j0 > 0 || (r0 > 0 && a.rank > 8 * AHEAD)) fetch(j0);
 #pragma unroll
                     for (int j = 0; j < AHEAD; ++j) {
                         const int at = j0 + j * 8;
                         if (at >= a.rank) break;
-                        const Eight<TM> e = j0 == 0 ? em[j] : load_eight(m, at, a.rank, m_whole);
+                        const Eight<TM> e = take_eight(um[j], m + at, left_of(at, a.rank));
                         float f[8];
                         unpack16<TM>(e.u[0], f);
                         if constexpr (sizeof(TM) == 4) unpack16<TM>(e.u[1], f + 4);
@@ -429,11 +442,13 @@ cudaError_t make_order(AdOrder &o, const int64_t *ids, int64_t t, int64_t adapte
     return pdl_launch(order_kernel, dim3(1), dim3(ORDER_THREADS), 0, st, a);
 }
 
-// whether the rows of the adapters' matrices start on 16 bytes (a stride that is not walked does not matter)
-inline bool stack_whole(const void *p, int64_t sa, int64_t sr, int64_t adapters, int64_t rows, int es) {
-    return aligned(p, 16) && (adapters <= 1 || sa * es % 16 == 0) && (rows <= 1 || sr * es % 16 == 0);
+// whether rows start on 16 bytes and are a multiple of 8 values long (a stride that is not walked does not matter)
+inline bool whole(const void *p, int64_t ld, int64_t rows, int64_t cols, int es) {
+    return aligned(p, 16) && cols % 8 == 0 && (rows <= 1 || ld * es % 16 == 0);
 }
-inline bool all_whole(const void *p, int64_t ld, int64_t rows, int es) { return aligned(p, 16) && (rows <= 1 || ld * es % 16 == 0); }
+inline bool stack_whole(const void *p, int64_t sa, int64_t sr, int64_t adapters, int64_t rows, int64_t cols, int es) {
+    return whole(p, sr, rows, cols, es) && (adapters <= 1 || sa * es % 16 == 0);
+}
 }  // namespace
 }  // namespace ops
 }  // namespace ct
@@ -466,18 +481,18 @@ extern "C" ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, cons
     if (workspace_bytes < s.total) return CT_ENOMEM;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *w = static_cast<char *>(workspace_dev);
-    const bool xw = all_whole(x_dev, ldx, t, xs), aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, es),
-               bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, es), yw = all_whole(y_dev, ldy, t, ys);
     cudaError_t e;
     // few rows, and adapters enough that hardly 16 rows have the same one
     if (t <= FEW && t <= 16 * adapters) {
         const FewArgs f = {x_dev, ldx, a_dev, a_adapter, a_row, b_dev, b_adapter, b_row, ids_dev, scale_dev, (int)t, (int)adapters, (int)rank, k,
-                           n, reinterpret_cast<float *>(w + s.v), y_dev, y_dtype, ldy, relu != 0, (int)xw | (int)aw << 1 | (int)bw << 2};
+                           n, reinterpret_cast<float *>(w + s.v), y_dev, y_dtype, ldy, relu != 0};
         if (dtype == CT_DT_F32) e = few<float, float>(f, st);
         else if (dtype == CT_DT_F16) e = x_dtype == CT_DT_F32 ? few<float, __half>(f, st) : few<__half, __half>(f, st);
         else e = x_dtype == CT_DT_F32 ? few<float, __nv_bfloat16>(f, st) : few<__nv_bfloat16, __nv_bfloat16>(f, st);
         return e == cudaSuccess ? CT_OK : CT_ECUDA;
     }
+    const bool xw = whole(x_dev, ldx, t, k, xs), aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, k, es),
+               bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, rank, es), yw = whole(y_dev, ldy, t, n, ys);
     AdOrder o;
     e = make_order(o, ids_dev, t, adapters, s, w, st);
     const int tiles = (int)tiles_of(t, adapters, ids_dev != nullptr), parts = y_dtype == CT_DT_F32 ? 3 : 2;
@@ -524,8 +539,8 @@ extern "C" ct_status ct_adapters_grad(const void *dy_dev, int32_t dy_dtype, int6
     if (workspace_bytes < s.total) return CT_ENOMEM;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *w = static_cast<char *>(workspace_dev);
-    const bool xw = all_whole(x_dev, ldx, t, xs), dyw = all_whole(dy_dev, lddy, t, dys), dxw = all_whole(dx_dev, lddx, t, dxs);
-    const bool aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, es), bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, es);
+    const bool xw = whole(x_dev, ldx, t, k, xs), dyw = whole(dy_dev, lddy, t, n, dys), dxw = whole(dx_dev, lddx, t, k, dxs);
+    const bool aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, k, es), bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, rank, es);
     const int r = (int)rank, tiles = (int)tiles_of(t, adapters, ids_dev != nullptr);
     // three parts of the short vectors where a result of 32 bits hangs on them
     if (t == 0) ids_dev = nullptr;                // zeros for all, no rows to order

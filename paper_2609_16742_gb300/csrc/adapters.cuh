@@ -60,41 +60,72 @@ template <typename T> struct Eight {
     uint4 u[sizeof(T) / 2];
 };
 
-// 16 bytes from any address on, of which `bytes` are wanted (the others become 0); reads aligned units that hold a wanted byte only
-__device__ __forceinline__ uint4 load_any(const char *p, int bytes) {
-    if (bytes <= 0) return make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t shift = (uint32_t)(uintptr_t)p & 15u;
-    const uint4 *q = reinterpret_cast<const uint4 *>(p - shift);
-    uint4 a = __ldg(q);
-    if (shift != 0) {
-        uint4 b = make_uint4(0u, 0u, 0u, 0u);
-        if ((int)shift + bytes > 16) b = __ldg(q + 1);
-        a = shifted(a, b, shift);
-    }
-    return bytes >= 16 ? a : first_bytes(a, bytes);
+// 16 bytes, or zeros: one instruction and no branch, so that many are on their way together
+__device__ __forceinline__ uint4 ldg_if(const void *p, bool wanted) {
+    uint4 v;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+        "@p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+        : "l"(p), "r"((int)wanted));
+    return v;
 }
 
-// values c to c + 7 of a row of `cols`; zeros behind its end.  whole: the row starts on 16 bytes
-template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T *row, int64_t c, int64_t cols, bool whole) {
+// the same of what a kernel before wrote, or this one writes
+__device__ __forceinline__ uint4 ld_if(const void *p, bool wanted) {
+    uint4 v;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+        "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+        : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+        : "l"(p), "r"((int)wanted)
+        : "memory");
+    return v;
+}
+
+// Eight values on their way: the aligned units that hold them.  A unit that holds no wanted byte is not read.
+template <typename T> struct Units {
+    uint4 u[sizeof(T) / 2 + 1];
+};
+// left: values of the row from the first on (8 or more, fewer at its end, 0: none)
+template <typename T> __device__ __forceinline__ Units<T> load_units(const T *p, int left) {
+    constexpr int N = (int)sizeof(T) / 2;
+    const uint32_t shift = (uint32_t)(uintptr_t)p & 15u;
+    const char *q = reinterpret_cast<const char *>(p) - shift;
+    const int bytes = (left > 8 ? 8 : left) * (int)sizeof(T) + (int)shift;       // from q on
+    Units<T> r;
+#pragma unroll
+    for (int i = 0; i <= N; ++i) r.u[i] = ldg_if(q + 16 * i, left > 0 && bytes > 16 * i);
+    return r;
+}
+template <typename T> __device__ __forceinline__ Eight<T> take_eight(const Units<T> &r, const T *p, int left) {
+    constexpr int N = (int)sizeof(T) / 2;
+    const uint32_t shift = (uint32_t)(uintptr_t)p & 15u;
     Eight<T> e;
-    const char *p = reinterpret_cast<const char *>(row + c);
-    if (whole && c + 8 <= cols) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
-    } else {
-        const int64_t left = (cols - c) * (int64_t)sizeof(T);
-        const int bytes = left > 64 ? 64 : (int)left;
+    for (int i = 0; i < N; ++i) e.u[i] = shifted(r.u[i], r.u[i + 1], shift);
+    if (left < 8) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = load_any(p + 16 * i, bytes - 16 * i);
+        for (int i = 0; i < N; ++i) {
+            const int bytes = left * (int)sizeof(T) - 16 * i;
+            e.u[i] = bytes <= 0 ? make_uint4(0u, 0u, 0u, 0u) : bytes >= 16 ? e.u[i] : first_bytes(e.u[i], bytes);
+        }
     }
     return e;
 }
-template <typename T> __device__ __forceinline__ Eight<T> zero_eight() {
-    Eight<T> e;
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = make_uint4(0u, 0u, 0u, 0u);
-    return e;
+__device__ __forceinline__ int left_of(int64_t c, int64_t cols) { return c >= cols ? 0 : cols - c > 8 ? 8 : (int)(cols - c); }
+
+// 16 bytes from global to shared memory, or zeros there
+__device__ __forceinline__ void copy16_if(uint32_t to, const void *from, bool wanted) {
+    const int bytes = wanted ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // what is left of v after its BF16 rounding h; nothing where h is infinite or NaN, so that those stay what they are
 __device__ __forceinline__ float rest_of(float v, float h) {
@@ -158,9 +189,8 @@ __device__ __forceinline__ float ld_peer_f32(uint32_t addr, int rank) {
 }
 #endif
 
-inline bool rows_whole(const void *p, int64_t ld_bytes) { return aligned(p, 16) && ld_bytes % 16 == 0; }
-
-// One product with a matrix of the adapters.  `whole`: bit 0: x's rows start on 16 bytes, bit 1: the matrix's do.
+// One product with a matrix of the adapters.  `whole`: bit 0: x's (y's) rows start on 16 bytes and are a multiple of 8 values long, bit 1:
+// the matrix's.
 struct AdShrink {
     const void *x;
     int64_t ldx, cols;

@@ -12,26 +12,35 @@ namespace ct {
 namespace ops {
 namespace {
 
-template <typename TM, int RP, bool TRANS> struct Expand {
-    static constexpr int PM = Parts<TM>::N;
+// FAST: the matrix's values are one part and its rows whole: its copies run from global to shared memory, two steps ahead.
+// Otherwise they go through registers, a step ahead.
+template <typename TM, int RP, bool TRANS, bool FAST> struct Expand {
+    static constexpr int PM = Parts<TM>::N, STAGES = FAST ? 3 : 2;
     static constexpr int LV = ad_pitch(RP), LM = ad_pitch(TRANS ? AD_STEP : RP);
     static constexpr int V_BYTES = AD_ROWS * LV, M_ROWS = TRANS ? RP : AD_STEP, M_BYTES = M_ROWS * LM;
     static constexpr int WIDE = 33, OUT = 8 * 8 * WIDE * 4;                      // 8 x 32 sums of each warp, where rows start anywhere
     static constexpr int M_VECS = M_ROWS * (TRANS ? AD_STEP / 8 : RP / 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
-    static int smem(int parts, bool out) { return parts * V_BYTES + 2 * PM * M_BYTES + (out ? OUT : 0); }
+    static int smem(int parts, bool out) { return parts * V_BYTES + STAGES * PM * M_BYTES + (out ? OUT : 0); }
 };
 
 // eight neighbouring values of a row of y, from 16 bytes on
-__device__ __forceinline__ void y_load(const char *p, int dtype, float *v) {
-    uint4 u = *reinterpret_cast<const uint4 *>(p);
+struct YEight {
+    uint4 u[2];
+};
+__device__ __forceinline__ YEight y_load(const char *p, int dtype, bool wanted) {
+    YEight e;
+    e.u[0] = ld_if(p, wanted);
+    e.u[1] = ld_if(p + 16, wanted && dtype == CT_DT_F32);
+    return e;
+}
+__device__ __forceinline__ void y_values(const YEight &e, int dtype, float *v) {
     if (dtype == CT_DT_F32) {
-        unpack16<float>(u, v);
-        u = *reinterpret_cast<const uint4 *>(p + 16);
-        unpack16<float>(u, v + 4);
+        unpack16<float>(e.u[0], v);
+        unpack16<float>(e.u[1], v + 4);
     } else if (dtype == CT_DT_F16) {
-        unpack16<__half>(u, v);
+        unpack16<__half>(e.u[0], v);
     } else {
-        unpack16<__nv_bfloat16>(u, v);
+        unpack16<__nv_bfloat16>(e.u[0], v);
     }
 }
 __device__ __forceinline__ void y_store(char *p, int dtype, const float *v) {
@@ -53,9 +62,9 @@ __device__ __forceinline__ void y_put(char *p, int dtype, float v) {
     else *reinterpret_cast<__nv_bfloat16 *>(p) = __float2bfloat16_rn(v);
 }
 
-template <typename TM, int RP, bool TRANS>
+template <typename TM, int RP, bool TRANS, bool FAST>
 __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, const AdOrder o) {
-    using S = Expand<TM, RP, TRANS>;
+    using S = Expand<TM, RP, TRANS, FAST>;
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ int32_t rows[AD_ROWS];
     pdl_wait();
@@ -66,86 +75,135 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     const bool out = tile.key > o.adapters, none = tile.key == 0;               // NaN; act alone
     const uint32_t base = tc::smem_u32(sm), bm0 = base + a.parts * S::V_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
-    const bool m_whole = a.whole & 2, y_whole = a.whole & 1;
+    const bool y_whole = a.whole & 1;
     const int ys = a.y_dtype == CT_DT_F32 ? 4 : 2;
     if (tid < AD_ROWS) rows[tid] = tid < tile.rows ? (o.order != nullptr ? o.order[tile.slot0 + tid] : (int32_t)(tile.slot0 + tid)) : -1;
 
     const bool product = !out && !none && a.rank > 0;
     const TM *m = static_cast<const TM *>(a.m) + (product ? (int64_t)(tile.key - 1) * a.m_adapter : 0);
-    Eight<TM> em[S::MV];
-    auto fetch = [&](int64_t c0) {
+    // the matrix's vector v of a step: its address and how many of its values are there
+    auto m_at = [&](int64_t c0, int v, int &left) -> const TM * {
+        if constexpr (TRANS) {
+            const int j = v / 8;
+            const int64_t c = c0 + v % 8 * 8;
+            left = v < S::M_VECS && j < a.rank ? left_of(c, a.cols) : 0;
+            return m + (left > 0 ? j * a.m_row + c : 0);
+        } else {
+            const int64_t c = c0 + v / (RP / 8);
+            const int j = v % (RP / 8) * 8;
+            left = v < S::M_VECS && c < a.cols ? left_of(j, a.rank) : 0;
+            return m + (left > 0 ? c * a.m_row + j : 0);
+        }
+    };
+    // Where it goes.  With the columns along its rows, chunk t of 32 columns is dealt out: its pair q is what thread t of a quad sums as
+    // its pair of tile q.
+    auto put = [&](uint32_t at, int v, const uint4 &w) {
+        if constexpr (TRANS) {
+            const uint32_t row = at + v / 8 * S::LM + (v % 8 / 4) * 64 + (v % 4) * 4;
+            sts4(row, w.x);
+            sts4(row + 16, w.y);
+            sts4(row + 32, w.z);
+            sts4(row + 48, w.w);
+        } else {
+            sts16(at + v / (RP / 8) * S::LM + v % (RP / 8) * 16, w);
+        }
+    };
+    Units<TM> um[S::MV];
+    auto copy = [&](int64_t c0, int buf) {
+        const uint32_t bm = bm0 + buf * S::M_BYTES;
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
             const int v = tid + i * AD_THREADS;
-            em[i] = zero_eight<TM>();
-            if (v < S::M_VECS) {
-                if constexpr (TRANS) {
-                    const int j = v / 8;
-                    const int64_t c = c0 + v % 8 * 8;
-                    if (j < a.rank && c < a.cols) em[i] = load_eight(m + j * a.m_row, c, a.cols, m_whole);
-                } else {
-                    const int64_t c = c0 + v / (RP / 8);
-                    const int j = v % (RP / 8) * 8;
-                    if (c < a.cols && j < a.rank) em[i] = load_eight(m + c * a.m_row, j, a.rank, m_whole);
-                }
+            int left;
+            const TM *p = m_at(c0, v, left);
+            if (v >= S::M_VECS) continue;
+            if constexpr (TRANS) {
+                const uint32_t row = bm + v / 8 * S::LM + (v % 8 / 4) * 64 + (v % 4) * 4;
+                const int bytes = left > 0 ? 4 : 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(row + 16 * q), "l"(reinterpret_cast<const char *>(p) + 4 * q), "r"(bytes) : "memory");
+            } else {
+                copy16_if(bm + v / (RP / 8) * S::LM + v % (RP / 8) * 16, p, left > 0);
             }
         }
     };
-    auto store = [&](int buf) {
+    auto fetch = [&](int64_t c0) {
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            int left;
+            const TM *p = m_at(c0, tid + i * AD_THREADS, left);
+            um[i] = load_units(p, left);
+        }
+    };
+    auto store = [&](int64_t c0, int buf) {
         const uint32_t bm = bm0 + buf * (S::PM * S::M_BYTES);
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
             const int v = tid + i * AD_THREADS;
-            if (v >= S::M_VECS) continue;
+            int left;
+            const TM *at = m_at(c0, v, left);
             uint4 p[S::PM];
-            split8<S::PM>(em[i], p);
+            split8<S::PM>(take_eight(um[i], at, left), p);
+            if (v < S::M_VECS)
 #pragma unroll
-            for (int q = 0; q < S::PM; ++q) {
-                const uint32_t at = bm + q * S::M_BYTES;
-                if constexpr (TRANS) {
-                    // chunk t of 32 columns: its pair q is what thread t of a quad sums as its pair of tile q
-                    const uint32_t row = at + v / 8 * S::LM + (v % 8 / 4) * 64 + (v % 4) * 4;
-                    sts4(row, p[q].x);
-                    sts4(row + 16, p[q].y);
-                    sts4(row + 32, p[q].z);
-                    sts4(row + 48, p[q].w);
-                } else {
-                    sts16(at + v / (RP / 8) * S::LM + v % (RP / 8) * 16, p[q]);
-                }
-            }
+                for (int q = 0; q < S::PM; ++q) put(bm + q * S::M_BYTES, v, p[q]);
         }
     };
     if (product) {
-        fetch(c_from);
+        if constexpr (FAST) {
+#pragma unroll
+            for (int i = 0; i < S::STAGES - 1; ++i) {
+                if (c_from + i * AD_STEP < c_to) copy(c_from + i * AD_STEP, i);
+                copies_end();
+            }
+        } else {
+            fetch(c_from);
+        }
         for (int v = tid; v < a.parts * AD_ROWS * (RP / 8); v += AD_THREADS) {
             const int p = v / (AD_ROWS * (RP / 8)), r = v / (RP / 8) % AD_ROWS, j = v % (RP / 8);
-            uint4 u = make_uint4(0u, 0u, 0u, 0u);
-            if (r < tile.rows) u = *(reinterpret_cast<const uint4 *>(a.v) + ((p * o.t + tile.slot0 + r) * (RP / 8) + j));
-            sts16(base + p * S::V_BYTES + r * S::LV + j * 16, u);
+            const bool there = r < tile.rows;
+            sts16(base + p * S::V_BYTES + r * S::LV + j * 16,
+                  ld_if(static_cast<const uint4 *>(a.v) + (there ? (p * o.t + tile.slot0 + r) * (RP / 8) + j : 0), there));
         }
-        store(0);
+        if constexpr (!FAST) store(c_from, 0);
     }
     __syncthreads();
     // this thread's rows: lane / 4 + 8 i of the warp's 32
     char *yr[4];
+    bool yh[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int32_t t = rows[wm * 32 + i * 8 + (lane >> 2)];
-        yr[i] = t >= 0 ? static_cast<char *>(a.y) + (int64_t)t * a.ldy * ys : nullptr;
+        yh[i] = t >= 0;
+        yr[i] = static_cast<char *>(a.y) + (yh[i] ? (int64_t)t * a.ldy * ys : 0);
     }
     const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
     const float nan = __uint_as_float(0x7FC00000u);
-    int buf = 0;
-    for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, buf ^= 1) {
-        const bool more = product && c0 + AD_STEP < c_to;
-        if (more) fetch(c0 + AD_STEP);
-        const int64_t mine = c0 + wn * 32 + (lane & 3) * 8;
-        const bool whole = y_whole && mine + 8 <= c_to;
-        float y[4][8];
-        if (whole) {
+    const int64_t mine0 = wn * 32 + (lane & 3) * 8;
+    YEight ahead[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (yr[i] != nullptr) y_load(yr[i] + mine * ys, a.y_dtype, y[i]);
+    for (int i = 0; i < 4; ++i) ahead[i] = y_load(yr[i] + (c_from + mine0) * ys, a.y_dtype, y_whole && yh[i] && c_from + mine0 < c_to);
+    int at = 0;
+    for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, ++at) {
+        const bool more = product && c0 + AD_STEP < c_to;
+        const int buf = at % S::STAGES;
+        if constexpr (FAST) {
+            if (product) {
+                copies_wait<S::STAGES - 2>();
+                __syncthreads();
+                if (c0 + (S::STAGES - 1) * AD_STEP < c_to) copy(c0 + (S::STAGES - 1) * AD_STEP, (at + S::STAGES - 1) % S::STAGES);
+                copies_end();
+            }
+        } else if (more) {
+            fetch(c0 + AD_STEP);
+        }
+        const int64_t mine = c0 + mine0, next = mine + AD_STEP;
+        YEight y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            y[i] = ahead[i];
+            ahead[i] = y_load(yr[i] + next * ys, a.y_dtype, y_whole && yh[i] && next < c_to);
         }
         float acc[2][4][4];
 #pragma unroll
@@ -184,35 +242,21 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         if (y_whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (yr[i] == nullptr) continue;
-                float v[8];
+                float v[8], w[8];
+                y_values(y[i], a.y_dtype, w);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    v[2 * j] = acc[i >> 1][j][(i & 1) * 2];
-                    v[2 * j + 1] = acc[i >> 1][j][(i & 1) * 2 + 1];
+                    v[2 * j] = acc[i >> 1][j][(i & 1) * 2] + w[2 * j];
+                    v[2 * j + 1] = acc[i >> 1][j][(i & 1) * 2 + 1] + w[2 * j + 1];
                 }
-                if (whole) {
+                if (a.relu || out)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[e] += y[i][e];
-                        if (a.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
-                        if (out) v[e] = nan;
-                    }
-                    y_store(yr[i] + mine * ys, a.y_dtype, v);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (mine + e >= c_to) break;
-                        char *at = yr[i] + (mine + e) * ys;
-                        float w = v[e] + y_one(at, a.y_dtype);
-                        if (a.relu) w = w < 0.f ? 0.f : w;
-                        y_put(at, a.y_dtype, out ? nan : w);
-                    }
-                }
+                    for (int e = 0; e < 8; ++e) v[e] = out ? nan : v[e] < 0.f ? 0.f : v[e];
+                if (yh[i] && mine < c_to) y_store(yr[i] + mine * ys, a.y_dtype, v);
             }
         } else {
             // rows that start anywhere: eight rows of the warp's sums at a time turn in shared memory, so that lanes are neighbouring columns
-            float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + 2 * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
+            float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + S::STAGES * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
             const int64_t c = c0 + wn * 32 + lane;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -238,15 +282,18 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
                 __syncwarp();
             }
         }
-        if (more) store(buf ^ 1);
-        __syncthreads();
+        if constexpr (!FAST) {
+            if (more) store(c0 + AD_STEP, (at + 1) % S::STAGES);
+            __syncthreads();
+        }
     }
+    if constexpr (FAST) copies_wait<0>();
 }
 
-template <typename TM, int RP, bool TRANS> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
-    using S = Expand<TM, RP, TRANS>;
+template <typename TM, int RP, bool TRANS, bool FAST> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
+    using S = Expand<TM, RP, TRANS, FAST>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = expand_kernel<TM, RP, TRANS>;
+    auto *kernel = expand_kernel<TM, RP, TRANS, FAST>;
     const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3, true));
     if (e != cudaSuccess) return e;
     // columns of a block: as many as leave each SM three blocks, at most 1024
@@ -260,18 +307,19 @@ template <typename TM, int RP, bool TRANS> cudaError_t launch(const AdExpand &q,
     const dim3 grid((unsigned)tiles, (unsigned)((a.cols + a.per - 1) / a.per));
     return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts, !(a.whole & 1)), st, a, o);
 }
-template <typename TM, bool TRANS> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
+template <typename TM, bool TRANS, bool FAST> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TM, 16, TRANS>(a, o, tiles, st);
-        case 32: return launch<TM, 32, TRANS>(a, o, tiles, st);
-        case 64: return launch<TM, 64, TRANS>(a, o, tiles, st);
-        default: return launch<TM, 128, TRANS>(a, o, tiles, st);
+        case 16: return launch<TM, 16, TRANS, FAST>(a, o, tiles, st);
+        case 32: return launch<TM, 32, TRANS, FAST>(a, o, tiles, st);
+        case 64: return launch<TM, 64, TRANS, FAST>(a, o, tiles, st);
+        default: return launch<TM, 128, TRANS, FAST>(a, o, tiles, st);
     }
 }
 template <bool TRANS> cudaError_t by_type(const AdExpand &a, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
-    return dtype == CT_DT_F32   ? by_rank<float, TRANS>(a, o, tiles, st)
-           : dtype == CT_DT_F16 ? by_rank<__half, TRANS>(a, o, tiles, st)
-                                : by_rank<__nv_bfloat16, TRANS>(a, o, tiles, st);
+    if (dtype == CT_DT_BF16 && (a.whole & 2)) return by_rank<__nv_bfloat16, TRANS, true>(a, o, tiles, st);
+    return dtype == CT_DT_F32   ? by_rank<float, TRANS, false>(a, o, tiles, st)
+           : dtype == CT_DT_F16 ? by_rank<__half, TRANS, false>(a, o, tiles, st)
+                                : by_rank<__nv_bfloat16, TRANS, false>(a, o, tiles, st);
 }
 }  // namespace
 

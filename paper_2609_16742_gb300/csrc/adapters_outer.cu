@@ -14,8 +14,10 @@ namespace {
 
 constexpr int COLS = 128;
 
-template <typename TX, int RP> struct Outer {
-    static constexpr int PX = Parts<TX>::N;
+// FAST: values are one part and rows whole: copies run from global to shared memory, two steps ahead.  Otherwise values go through
+// registers, a step ahead.
+template <typename TX, int RP, bool FAST> struct Outer {
+    static constexpr int PX = Parts<TX>::N, STAGES = FAST ? 3 : 2;
     static constexpr int LX = ad_pitch(COLS), LV = ad_pitch(RP);
     static constexpr int X_BYTES = AD_STEP * LX, V_BYTES = AD_STEP * LV;
     static constexpr int XV = AD_STEP * (COLS / 8) / AD_THREADS;                  // 4
@@ -26,14 +28,14 @@ template <typename TX, int RP> struct Outer {
     static constexpr bool EACH = PX > 1;
     static constexpr int FLUSH = 2;
     static int smem(int parts) {
-        const int two = 2 * (PX * X_BYTES + parts * V_BYTES);
-        return two > SUM ? two : SUM;
+        const int all = STAGES * (PX * X_BYTES + parts * V_BYTES);
+        return all > SUM ? all : SUM;
     }
 };
 
-template <typename TX, int RP>
+template <typename TX, int RP, bool FAST>
 __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, const AdOrder o, int splits) {
-    using S = Outer<TX, RP>;
+    using S = Outer<TX, RP, FAST>;
     extern __shared__ __align__(128) unsigned char sm[];
     pdl_wait();
     pdl_trigger();
@@ -45,41 +47,68 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
     const uint32_t base = tc::smem_u32(sm);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
     const int buf_bytes = S::PX * S::X_BYTES + a.parts * S::V_BYTES;
-    const bool x_whole = a.whole & 1;
 
-    Eight<TX> ex[S::XV];
-    uint4 ev[3][S::VV];
+    // this thread's vectors: of x, rows tid / 16 + 16 i, 8 values at 8 (tid % 16)
+    constexpr int RUN = AD_THREADS / (COLS / 8);
     const int64_t xc = cols0 + (tid % (COLS / 8)) * 8;
-    auto fetch = [&](int64_t s) {
-        const int64_t t0 = from + s * AD_STEP;
+    const int x_left = left_of(xc, a.cols), x_to = tid / (COLS / 8) * S::LX + tid % (COLS / 8) * 16;
+    const TX *x0 = static_cast<const TX *>(a.x) + (x_left > 0 ? xc : 0);
+    auto x_at = [&](int64_t s, int i, int &left) -> const TX * {
+        const int64_t t = from + s * AD_STEP + tid / (COLS / 8) + i * RUN;
+        left = t < to ? x_left : 0;
+        return x0 + (left > 0 ? (o.order != nullptr ? (int64_t)o.order[t] : t) * a.ldx : 0);
+    };
+    auto v_at = [&](int64_t s, int p, int v, bool &there) -> const uint4 * {
+        const int64_t t = from + s * AD_STEP + v / (RP / 8);
+        there = v < S::V_VECS && t < to;
+        return static_cast<const uint4 *>(a.v) + (there ? (p * o.t + t) * (RP / 8) + v % (RP / 8) : 0);
+    };
+    auto v_to = [&](int v) { return v / (RP / 8) * S::LV + v % (RP / 8) * 16; };
+    auto copy = [&](int64_t s, int buf) {
+        const uint32_t bx = base + buf * buf_bytes, bv = bx + S::X_BYTES;
 #pragma unroll
         for (int i = 0; i < S::XV; ++i) {
-            const int64_t t = t0 + tid / (COLS / 8) + i * (AD_THREADS / (COLS / 8));
-            ex[i] = zero_eight<TX>();
-            if (t < to && xc < a.cols)
-                ex[i] = load_eight(static_cast<const TX *>(a.x) + (o.order != nullptr ? (int64_t)o.order[t] : t) * a.ldx, xc, a.cols, x_whole);
+            int left;
+            const TX *p = x_at(s, i, left);
+            copy16_if(bx + x_to + i * RUN * S::LX, p, left > 0);
         }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            if (p >= a.parts) break;
+        for (int p = 0; p < a.parts; ++p)
 #pragma unroll
             for (int i = 0; i < S::VV; ++i) {
                 const int v = tid + i * AD_THREADS;
-                const int64_t t = t0 + v / (RP / 8);
-                ev[p][i] = make_uint4(0u, 0u, 0u, 0u);
-                if (v < S::V_VECS && t < to) ev[p][i] = *(reinterpret_cast<const uint4 *>(a.v) + ((p * o.t + t) * (RP / 8) + v % (RP / 8)));
+                bool there;
+                const uint4 *at = v_at(s, p, v, there);
+                if (v < S::V_VECS) copy16_if(bv + p * S::V_BYTES + v_to(v), at, there);
             }
-        }
     };
-    auto store = [&](int buf) {
+    Units<TX> ux[S::XV];
+    uint4 ev[3][S::VV];
+    auto fetch = [&](int64_t s) {
+#pragma unroll
+        for (int i = 0; i < S::XV; ++i) {
+            int left;
+            const TX *p = x_at(s, i, left);
+            ux[i] = load_units(p, left);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+            for (int i = 0; i < S::VV; ++i) {
+                bool there;
+                const uint4 *at = v_at(s, p, tid + i * AD_THREADS, there);
+                ev[p][i] = ld_if(at, there && p < a.parts);
+            }
+    };
+    auto store = [&](int64_t s, int buf) {
         const uint32_t bx = base + buf * buf_bytes, bv = bx + S::PX * S::X_BYTES;
 #pragma unroll
         for (int i = 0; i < S::XV; ++i) {
+            int left;
+            const TX *at = x_at(s, i, left);
             uint4 p[S::PX];
-            split8<S::PX>(ex[i], p);
+            split8<S::PX>(take_eight(ux[i], at, left), p);
 #pragma unroll
-            for (int q = 0; q < S::PX; ++q)
-                sts16(bx + q * S::X_BYTES + (tid / (COLS / 8) + i * (AD_THREADS / (COLS / 8))) * S::LX + tid % (COLS / 8) * 16, p[q]);
+            for (int q = 0; q < S::PX; ++q) sts16(bx + q * S::X_BYTES + x_to + i * RUN * S::LX, p[q]);
         }
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
@@ -87,7 +116,7 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
 #pragma unroll
             for (int i = 0; i < S::VV; ++i) {
                 const int v = tid + i * AD_THREADS;
-                if (v < S::V_VECS) sts16(bv + p * S::V_BYTES + v / (RP / 8) * S::LV + v % (RP / 8) * 16, ev[p][i]);
+                if (v < S::V_VECS) sts16(bv + p * S::V_BYTES + v_to(v), ev[p][i]);
             }
         }
     };
@@ -150,16 +179,33 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
             if constexpr (S::EACH) flush();
         }
     };
-    if (s0 < s1) {
+    if constexpr (FAST) {
+#pragma unroll
+        for (int i = 0; i < S::STAGES - 1; ++i) {
+            if (s0 + i < s1) copy(s0 + i, i);
+            copies_end();
+        }
+        for (int64_t s = s0; s < s1; ++s) {
+            const int at = (int)(s - s0);
+            copies_wait<S::STAGES - 2>();
+            __syncthreads();
+            if (s + S::STAGES - 1 < s1) copy(s + S::STAGES - 1, (at + S::STAGES - 1) % S::STAGES);
+            copies_end();
+            compute(at % S::STAGES);
+            if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
+        }
+        copies_wait<0>();
+        __syncthreads();
+    } else if (s0 < s1) {
         fetch(s0);
-        store(0);
+        store(s0, 0);
         __syncthreads();
         for (int64_t s = s0; s < s1; ++s) {
-            const int buf = (int)(s - s0) & 1;
+            const int at = (int)(s - s0);
             if (s + 1 < s1) fetch(s + 1);
-            compute(buf);
-            if (!S::EACH && (int)(s - s0) % S::FLUSH == S::FLUSH - 1) flush();
-            if (s + 1 < s1) store(buf ^ 1);
+            compute(at & 1);
+            if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
+            if (s + 1 < s1) store(s + 1, at & 1 ^ 1);
             __syncthreads();
         }
     }
@@ -191,10 +237,10 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
-template <typename TX, int RP> cudaError_t launch(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
-    using S = Outer<TX, RP>;
+template <typename TX, int RP, bool FAST> cudaError_t launch(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
+    using S = Outer<TX, RP, FAST>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = outer_kernel<TX, RP>;
+    auto *kernel = outer_kernel<TX, RP, FAST>;
     const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3));
     if (e != cudaSuccess) return e;
     // two CTAs for each SM, with two steps of an adapter's share of the rows at least for each
@@ -205,20 +251,21 @@ template <typename TX, int RP> cudaError_t launch(const AdOuter &a, const AdOrde
     if (splits == 1) return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, a, o, splits);
     return pdl_launch_cluster(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, splits, a, o, splits);
 }
-template <typename TX> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
+template <typename TX, bool FAST> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TX, 16>(a, o, st);
-        case 32: return launch<TX, 32>(a, o, st);
-        case 64: return launch<TX, 64>(a, o, st);
-        default: return launch<TX, 128>(a, o, st);
+        case 16: return launch<TX, 16, FAST>(a, o, st);
+        case 32: return launch<TX, 32, FAST>(a, o, st);
+        case 64: return launch<TX, 64, FAST>(a, o, st);
+        default: return launch<TX, 128, FAST>(a, o, st);
     }
 }
 }  // namespace
 
 cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st) {
-    return x_dtype == CT_DT_F32   ? by_rank<float>(a, o, st)
-           : x_dtype == CT_DT_F16 ? by_rank<__half>(a, o, st)
-                                  : by_rank<__nv_bfloat16>(a, o, st);
+    if (x_dtype == CT_DT_BF16 && (a.whole & 1)) return by_rank<__nv_bfloat16, true>(a, o, st);
+    return x_dtype == CT_DT_F32   ? by_rank<float, false>(a, o, st)
+           : x_dtype == CT_DT_F16 ? by_rank<__half, false>(a, o, st)
+                                  : by_rank<__nv_bfloat16, false>(a, o, st);
 }
 
 }  // namespace ops

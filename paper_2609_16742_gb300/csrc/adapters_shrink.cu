@@ -11,14 +11,17 @@ namespace ct {
 namespace ops {
 namespace {
 
-template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
+// FAST: values are one part and rows whole: copies run from global to shared memory, STAGES - 1 steps ahead.  Otherwise values go
+// through registers, a step ahead.
+template <typename TX, typename TM, int RP, bool TRANS, bool FAST> struct Shrink {
     static constexpr bool F16 = sizeof(TX) == 2 && Parts<TX>::N == 2 && Parts<TM>::N == 2;
     static constexpr int PX = F16 ? 1 : Parts<TX>::N, PM = F16 ? 1 : Parts<TM>::N;
     static constexpr int LX = ad_pitch(AD_STEP), LM = ad_pitch(TRANS ? RP : AD_STEP);
     static constexpr int X_BYTES = AD_ROWS * LX, M_ROWS = TRANS ? AD_STEP : RP, M_BYTES = M_ROWS * LM;
+    static constexpr int STAGES = FAST ? (RP == 128 ? 3 : 4) : 2;
     static constexpr int BUF = PX * X_BYTES + PM * M_BYTES;
     static constexpr int SUM = AD_ROWS * (RP + 1) * 4;
-    static constexpr int SMEM = 2 * BUF > SUM ? 2 * BUF : SUM;
+    static constexpr int SMEM = STAGES * BUF > SUM ? STAGES * BUF : SUM;
     static constexpr int XV = AD_ROWS * 8 / AD_THREADS;                          // vectors of 8 values a thread loads
     static constexpr int M_VECS = M_ROWS * (TRANS ? RP / 8 : 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
     static constexpr int NT = RP / 16;                                           // 8-column tiles of a warp
@@ -28,9 +31,9 @@ template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
     static constexpr int FLUSH = 4;
 };
 
-template <typename TX, typename TM, int RP, bool TRANS>
+template <typename TX, typename TM, int RP, bool TRANS, bool FAST>
 __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, const AdOrder o, int splits) {
-    using S = Shrink<TX, TM, RP, TRANS>;
+    using S = Shrink<TX, TM, RP, TRANS, FAST>;
     extern __shared__ __align__(128) unsigned char sm[];
     pdl_wait();
     pdl_trigger();
@@ -42,59 +45,84 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
     const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
     const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
-    const bool x_whole = a.whole & 1, m_whole = a.whole & 2;
 
     // this thread's vectors: of x, rows tid / 8 + 32 i, 8 values at 8 (tid % 8)
     const TX *xr[S::XV];
+    bool xh[S::XV];
     const int xc = (tid & 7) * 8;
 #pragma unroll
     for (int i = 0; i < S::XV; ++i) {
         const int r = tid / 8 + 32 * i;
         const int64_t s = tile.slot0 + r;
-        xr[i] = r < tile.rows ? static_cast<const TX *>(a.x) + (o.order != nullptr ? (int64_t)o.order[s] : s) * a.ldx : nullptr;
+        xh[i] = r < tile.rows;
+        xr[i] = static_cast<const TX *>(a.x) + (xh[i] ? (o.order != nullptr ? (int64_t)o.order[s] : s) * a.ldx : 0);
     }
     const TM *m = static_cast<const TM *>(a.m) + adapter * a.m_adapter;
-    Eight<TX> ex[S::XV];
-    Eight<TM> em[S::MV];
-    auto fetch = [&](int64_t s) {
+    // the matrix's vector v of a step: its address, how many of its values are there, where it goes
+    auto m_at = [&](int64_t s, int v, int &left) -> const TM * {
         const int64_t c0 = s * AD_STEP;
+        if constexpr (TRANS) {
+            const int64_t c = c0 + v / (RP / 8);
+            const int j = v % (RP / 8) * 8;
+            left = v < S::M_VECS && c < a.cols ? left_of(j, a.rank) : 0;
+            return m + (left > 0 ? c * a.m_row + j : 0);
+        } else {
+            const int j = v / 8;
+            const int64_t c = c0 + v % 8 * 8;
+            left = v < S::M_VECS && j < a.rank ? left_of(c, a.cols) : 0;
+            return m + (left > 0 ? j * a.m_row + c : 0);
+        }
+    };
+    auto m_to = [&](int v) { return v / (TRANS ? RP / 8 : 8) * S::LM + v % (TRANS ? RP / 8 : 8) * 16; };
+    const int x_to = tid / 8 * S::LX + xc * 2;
+    Units<TX> ux[S::XV];
+    Units<TM> um[S::MV];
+    auto copy = [&](int64_t s, int buf) {
+        const uint32_t bx = base + buf * S::BUF, bm = bx + S::X_BYTES;
+        const int64_t c = s * AD_STEP + xc;
 #pragma unroll
-        for (int i = 0; i < S::XV; ++i) ex[i] = xr[i] != nullptr && c0 + xc < a.cols ? load_eight(xr[i], c0 + xc, a.cols, x_whole) : zero_eight<TX>();
+        for (int i = 0; i < S::XV; ++i) copy16_if(bx + x_to + 32 * i * S::LX, xr[i] + (c < a.cols ? c : 0), xh[i] && c < a.cols);
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
             const int v = tid + i * AD_THREADS;
-            em[i] = zero_eight<TM>();
-            if (v < S::M_VECS) {
-                if constexpr (TRANS) {
-                    const int64_t c = c0 + v / (RP / 8);
-                    const int j = v % (RP / 8) * 8;
-                    if (c < a.cols && j < a.rank) em[i] = load_eight(m + c * a.m_row, j, a.rank, m_whole);
-                } else {
-                    const int j = v / 8;
-                    const int64_t c = c0 + v % 8 * 8;
-                    if (j < a.rank && c < a.cols) em[i] = load_eight(m + j * a.m_row, c, a.cols, m_whole);
-                }
-            }
+            int left;
+            const TM *p = m_at(s, v, left);
+            if (v < S::M_VECS) copy16_if(bm + m_to(v), p, left > 0);
         }
     };
-    auto store = [&](int buf) {
+    auto fetch = [&](int64_t s) {
+        const int64_t c = s * AD_STEP + xc;
+        const int n = left_of(c, a.cols);
+#pragma unroll
+        for (int i = 0; i < S::XV; ++i) ux[i] = load_units(xr[i] + (n > 0 ? c : 0), xh[i] ? n : 0);
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            int left;
+            const TM *p = m_at(s, tid + i * AD_THREADS, left);
+            um[i] = load_units(p, left);
+        }
+    };
+    auto store = [&](int64_t s, int buf) {
         const uint32_t bx = base + buf * S::BUF, bm = bx + S::PX * S::X_BYTES;
+        const int64_t c = s * AD_STEP + xc;
+        const int n = left_of(c, a.cols);
 #pragma unroll
         for (int i = 0; i < S::XV; ++i) {
             uint4 p[S::PX];
-            split8<S::PX>(ex[i], p);
+            split8<S::PX>(take_eight(ux[i], xr[i] + (n > 0 ? c : 0), xh[i] ? n : 0), p);
 #pragma unroll
-            for (int q = 0; q < S::PX; ++q) sts16(bx + q * S::X_BYTES + (tid / 8 + 32 * i) * S::LX + xc * 2, p[q]);
+            for (int q = 0; q < S::PX; ++q) sts16(bx + q * S::X_BYTES + x_to + 32 * i * S::LX, p[q]);
         }
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
             const int v = tid + i * AD_THREADS;
-            if (v >= S::M_VECS) continue;
+            int left;
+            const TM *at = m_at(s, v, left);
             uint4 p[S::PM];
-            split8<S::PM>(em[i], p);
-            const int w = TRANS ? RP / 8 : 8;
+            split8<S::PM>(take_eight(um[i], at, left), p);
+            if (v < S::M_VECS)
 #pragma unroll
-            for (int q = 0; q < S::PM; ++q) sts16(bm + q * S::M_BYTES + v / w * S::LM + v % w * 16, p[q]);
+                for (int q = 0; q < S::PM; ++q) sts16(bm + q * S::M_BYTES + m_to(v), p[q]);
         }
     };
 
@@ -163,16 +191,33 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
         }
     };
 
-    if (s0 < s1) {
+    if constexpr (FAST) {
+#pragma unroll
+        for (int i = 0; i < S::STAGES - 1; ++i) {
+            if (s0 + i < s1) copy(s0 + i, i);
+            copies_end();
+        }
+        for (int64_t s = s0; s < s1; ++s) {
+            const int at = (int)(s - s0);
+            copies_wait<S::STAGES - 2>();
+            __syncthreads();
+            if (s + S::STAGES - 1 < s1) copy(s + S::STAGES - 1, (at + S::STAGES - 1) % S::STAGES);
+            copies_end();
+            compute(at % S::STAGES);
+            if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
+        }
+        copies_wait<0>();
+        __syncthreads();
+    } else if (s0 < s1) {
         fetch(s0);
-        store(0);
+        store(s0, 0);
         __syncthreads();
         for (int64_t s = s0; s < s1; ++s) {
-            const int buf = (int)(s - s0) & 1;
+            const int at = (int)(s - s0);
             if (s + 1 < s1) fetch(s + 1);
-            compute(buf);
-            if (!S::EACH && (int)(s - s0) % S::FLUSH == S::FLUSH - 1) flush();
-            if (s + 1 < s1) store(buf ^ 1);
+            compute(at & 1);
+            if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
+            if (s + 1 < s1) store(s + 1, at & 1 ^ 1);
             __syncthreads();
         }
     }
@@ -208,11 +253,11 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
-template <typename TX, typename TM, int RP, bool TRANS>
+template <typename TX, typename TM, int RP, bool TRANS, bool FAST>
 cudaError_t launch(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t st) {
-    using S = Shrink<TX, TM, RP, TRANS>;
+    using S = Shrink<TX, TM, RP, TRANS, FAST>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = shrink_kernel<TX, TM, RP, TRANS>;
+    auto *kernel = shrink_kernel<TX, TM, RP, TRANS, FAST>;
     const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
     if (e != cudaSuccess) return e;
     // two CTAs for each SM, with four steps at least for each
@@ -222,21 +267,25 @@ cudaError_t launch(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t 
     if (splits == 1) return pdl_launch(kernel, dim3((unsigned)tiles), dim3(AD_THREADS), S::SMEM, st, a, o, splits);
     return pdl_launch_cluster(kernel, dim3((unsigned)(tiles * splits)), dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits);
 }
-template <typename TX, typename TM, bool TRANS>
+template <typename TX, typename TM, bool TRANS, bool FAST>
 cudaError_t by_rank(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TX, TM, 16, TRANS>(a, o, tiles, st);
-        case 32: return launch<TX, TM, 32, TRANS>(a, o, tiles, st);
-        case 64: return launch<TX, TM, 64, TRANS>(a, o, tiles, st);
-        default: return launch<TX, TM, 128, TRANS>(a, o, tiles, st);
+        case 16: return launch<TX, TM, 16, TRANS, FAST>(a, o, tiles, st);
+        case 32: return launch<TX, TM, 32, TRANS, FAST>(a, o, tiles, st);
+        case 64: return launch<TX, TM, 64, TRANS, FAST>(a, o, tiles, st);
+        default: return launch<TX, TM, 128, TRANS, FAST>(a, o, tiles, st);
     }
 }
 template <bool TRANS> cudaError_t by_type(const AdShrink &a, int x_dtype, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
-    if (dtype == CT_DT_F32) return by_rank<float, float, TRANS>(a, o, tiles, st);
-    if (dtype == CT_DT_F16)
-        return x_dtype == CT_DT_F32 ? by_rank<float, __half, TRANS>(a, o, tiles, st) : by_rank<__half, __half, TRANS>(a, o, tiles, st);
-    return x_dtype == CT_DT_F32 ? by_rank<float, __nv_bfloat16, TRANS>(a, o, tiles, st)
-                                : by_rank<__nv_bfloat16, __nv_bfloat16, TRANS>(a, o, tiles, st);
+    const bool fast = a.whole == 3;
+    if (dtype == CT_DT_F32) return by_rank<float, float, TRANS, false>(a, o, tiles, st);
+    if (dtype == CT_DT_F16) {
+        if (x_dtype == CT_DT_F32) return by_rank<float, __half, TRANS, false>(a, o, tiles, st);
+        return fast ? by_rank<__half, __half, TRANS, true>(a, o, tiles, st) : by_rank<__half, __half, TRANS, false>(a, o, tiles, st);
+    }
+    if (x_dtype == CT_DT_F32) return by_rank<float, __nv_bfloat16, TRANS, false>(a, o, tiles, st);
+    return fast ? by_rank<__nv_bfloat16, __nv_bfloat16, TRANS, true>(a, o, tiles, st)
+                : by_rank<__nv_bfloat16, __nv_bfloat16, TRANS, false>(a, o, tiles, st);
 }
 }  // namespace
 
