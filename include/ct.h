@@ -654,7 +654,7 @@ typedef struct {
     int64_t rows, cols, ld_src, ld_dst;
     int64_t dtype; /* ct_dtype */
 } ct_tensor;
-ct_status ct_clip_grads_workspace(const ct_tensor *tensors, int64_t n, size_t *bytes);
+ct_status ct_clip_grads_workspace(int64_t n, int64_t values, size_t *bytes); /* values: of all tensors */
 ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t kind, double max_norm, float *norms_dev,
                         float *norm_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 

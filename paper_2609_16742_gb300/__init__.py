@@ -11,8 +11,10 @@ and there is no fallback: if ``_lib/libct.so`` is missing, every call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
+import operator
 import os
 from typing import List, Optional, Sequence
 
@@ -138,7 +140,7 @@ def lib():
             "ct_adapters_grad_workspace": [i64, i64, i64, i64, i64, P(ctypes.c_size_t)],
             "ct_adapters_grad": [vp, i32, i64, vp, i32, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, i64, i64, i64, i64, i64,
                                  vp, i32, i64, vp, vp, i32, vp, ctypes.c_size_t, vp],
-            "ct_clip_grads_workspace": [vp, i64, P(ctypes.c_size_t)],
+            "ct_clip_grads_workspace": [i64, i64, P(ctypes.c_size_t)],
             "ct_clip_grads": [vp, i64, i32, dbl, vp, vp, vp, ctypes.c_size_t, vp],
             "ct_verify_drafts_workspace": [i64, i64, i64, i64, P(ctypes.c_size_t)],
             "ct_verify_drafts": [vp, i32, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, i64, i64, i64, vp, vp, vp, vp,
@@ -496,6 +498,9 @@ class _TorchNames:
         self.f32, self.u8, self.i64, self.e4m3 = torch.float32, torch.uint8, torch.int64, torch.float8_e4m3fn
         self.dtypes = {torch.float32: CT_DT_F32, torch.float16: CT_DT_F16, torch.bfloat16: CT_DT_BF16}
         self.bytes = {self.e4m3: 0, self.u8: 0}
+        tensor, get = torch.Tensor, operator.attrgetter
+        self.is_contiguous, self.get_device, self.numel, self.data_ptr = tensor.is_contiguous, tensor.get_device, tensor.numel, tensor.data_ptr
+        self.requires_grad, self.dtype, self.shape = get("requires_grad"), get("dtype"), get("shape")
         self.current_device = torch.cuda.current_device
         self.recording = torch.is_grad_enabled
         # the raw handle of the current stream; torch.cuda.current_stream builds a Stream object first
@@ -863,16 +868,11 @@ def ct_adapters_grad(dy, x, a, b, ids=None, scale=None, dx=None, grad_dtype=None
     return dx, da, db
 
 
-def _layout(t, name, device):
+def _layout(t, name):
     """(rows, columns, row pitch) of a tensor whose values are dense in memory in some order of its dimensions, or a matrix with a pitch."""
-    T = _names
-    if t.dtype not in T.dtypes or t.device != device:
-        raise ValueError("%s: a tensor of %s on %s is wanted, got %s on %s"
-                         % (name, "/".join(str(d) for d in T.dtypes), device, t.dtype, t.device))
-    if t.requires_grad and T.recording():
-        raise _tracked(name)
     if t.is_contiguous():
-        return 1, t.numel(), t.numel()
+        n = t.numel()
+        return 1, n, n
     if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
         return t.shape[0], t.shape[1], t.stride(0)
     size = 1
@@ -884,6 +884,75 @@ def _layout(t, name, device):
     return 1, size, size
 
 
+def _bad_values(t, name, device):
+    if t.dtype in _names.dtypes and t.device == device:
+        return _tracked(name)
+    return ValueError("%s: a tensor of %s on %s is wanted, got %s on %s"
+                      % (name, "/".join(str(d) for d in _names.dtypes), device, t.dtype, t.device))
+
+
+def _dense_table(grads, outs, index):
+    """(values, table) of ct_tensor rows where every tensor is contiguous and nothing is to be refused, else None.  Attributes are
+    taken of all tensors at a time: a loop over them would cost more than the kernels."""
+    T = _names
+    every = grads if outs is grads else grads + outs
+    if not all(map(T.is_contiguous, every)) or set(map(T.get_device, every)) != {index} or \
+            (T.recording() and any(map(T.requires_grad, every))):
+        return None
+    types = list(map(T.dtype, grads))
+    codes = list(map(T.dtypes.get, types))
+    if None in codes:
+        return None
+    n, numel, ptr = len(grads), list(map(T.numel, grads)), list(map(T.data_ptr, grads))
+    to = ptr
+    if outs is not grads:
+        if list(map(T.dtype, outs)) != types or list(map(T.shape, outs)) != list(map(T.shape, grads)):
+            return None
+        to = list(map(T.data_ptr, outs))
+    table = array.array("q", bytes(56 * n))
+    sizes = array.array("q", numel)
+    table[0::7], table[1::7], table[2::7] = array.array("q", ptr), array.array("q", to), array.array("q", [1]) * n
+    table[3::7] = table[4::7] = table[5::7] = sizes
+    table[6::7] = array.array("q", codes)
+    return sum(numel), table
+
+
+def _clip_table(grads, out, dev):
+    """(values, table) of ct_tensor rows, tensor by tensor."""
+    index, codes, recording, values, table = dev.index, _names.dtypes, _names.recording(), 0, []
+    for i, t in enumerate(grads):
+        code = codes.get(t.dtype)
+        if code is None or t.get_device() != index or (recording and t.requires_grad):
+            raise _bad_values(t, "grads[%d]" % i, dev)
+        rows, cols, ld = _layout(t, "grads[%d]" % i)
+        p, ldo = t.data_ptr(), ld
+        o = p
+        if out is not None:
+            q = out[i]
+            if q.dtype != t.dtype or q.shape != t.shape:
+                raise ValueError("out[%d]: %s %s is wanted, got %s %s" % (i, t.dtype, tuple(t.shape), q.dtype, tuple(q.shape)))
+            if q.get_device() != index or (recording and q.requires_grad):
+                raise _bad_values(q, "out[%d]" % i, dev)
+            o = q.data_ptr()
+            ldo = _layout(q, "out[%d]" % i)[2]
+            if q.stride() != t.stride() and not (t.is_contiguous() and q.is_contiguous()):
+                # matrices of different pitches
+                if t.dim() != 2 or (t.shape[1] > 1 and (t.stride(1) != 1 or q.stride(1) != 1)):
+                    raise ValueError("out[%d]: strides %s are wanted, got %s" % (i, t.stride(), q.stride()))
+                rows, cols = t.shape
+                ld, ldo = t.stride(0), q.stride(0)
+        values += rows * cols
+        table += (p, o, rows, cols, ld, ldo, code)
+    return values, array.array("q", table)
+
+
+@functools.lru_cache(maxsize=256)
+def _clip_workspace(n, values):
+    need = ctypes.c_size_t()
+    _check(lib().ct_clip_grads_workspace(n, values, ctypes.byref(need)), "ct_clip_grads_workspace")
+    return need.value
+
+
 def ct_clip_grads(grads, max_norm, kind: float = 2.0, out=None, stream=None):
     """(norm, norms): the norm of the values of all tensors `grads` together
     (float32, no dimension) and of each (float32 [len(grads)]), and the values
@@ -892,11 +961,13 @@ def ct_clip_grads(grads, max_norm, kind: float = 2.0, out=None, stream=None):
     nothing.  Types may differ from tensor to tensor; none may overlap another."""
     T = _names or _T()
     grads = list(grads)
-    outs = grads if out is None else list(out)
     if not grads:
         raise ValueError("grads: at least one tensor is wanted")
-    if len(outs) != len(grads):
-        raise ValueError("out: %d tensors are wanted, got %d" % (len(grads), len(outs)))
+    n = len(grads)
+    if out is not None:
+        out = list(out)
+        if len(out) != n:
+            raise ValueError("out: %d tensors are wanted, got %d" % (n, len(out)))
     if kind != 2 and kind != float("inf"):
         raise ValueError("kind is 2 or infinity, got %r" % (kind,))
     max_norm = float(max_norm)
@@ -907,32 +978,15 @@ def ct_clip_grads(grads, max_norm, kind: float = 2.0, out=None, stream=None):
         raise ValueError("grads[0]: a CUDA tensor is wanted, got one on %s" % dev)
     if stream is not None or dev.index != T.current_device():
         return _elsewhere(ct_clip_grads, dev, stream, grads, max_norm, kind, out)
-    table, codes = [], T.dtypes
-    for i, t in enumerate(grads):
-        rows, cols, ld = _layout(t, "grads[%d]" % i, dev)
-        o, ldo = t, ld
-        if out is not None:
-            o = outs[i]
-            if o.dtype != t.dtype or o.shape != t.shape:
-                raise ValueError("out[%d]: %s %s is wanted, got %s %s" % (i, t.dtype, tuple(t.shape), o.dtype, tuple(o.shape)))
-            _, _, ldo = _layout(o, "out[%d]" % i, dev)
-            if o.stride() != t.stride() and not (rows == 1 and t.is_contiguous() and o.is_contiguous()):
-                # matrices of different pitches
-                if t.dim() != 2 or (t.shape[1] > 1 and (t.stride(1) != 1 or o.stride(1) != 1)):
-                    raise ValueError("out[%d]: strides %s are wanted, got %s" % (i, t.stride(), o.stride()))
-                rows, cols = t.shape
-                ld, ldo = t.stride(0), o.stride(0)
-        table += (t.data_ptr(), o.data_ptr(), rows, cols, ld, ldo, codes[t.dtype])
-    n = len(grads)
-    table = (ctypes.c_int64 * len(table))(*table)
+    index = dev.index
+    fast = _dense_table(grads, grads if out is None else out, index)
+    values, table = fast if fast is not None else _clip_table(grads, out, dev)
     norm = T.empty((), dtype=T.f32, device=dev)
     norms = T.empty(n, dtype=T.f32, device=dev)
-    L = _lib or lib()
-    need = ctypes.c_size_t()
-    _check(L.ct_clip_grads_workspace(table, n, ctypes.byref(need)), "ct_clip_grads_workspace")
-    work = T.empty(need.value, dtype=T.u8, device=dev)
-    st = L.ct_clip_grads(table, n, CT_NORM_2 if kind == 2 else CT_NORM_INF, max_norm, norms.data_ptr(), norm.data_ptr(),
-                         work.data_ptr(), need.value, T.raw_stream(dev.index))
+    need = _clip_workspace(n, values)
+    work = T.empty(need, dtype=T.u8, device=dev)
+    st = (_lib or lib()).ct_clip_grads(table.buffer_info()[0], n, CT_NORM_2 if kind == 2 else CT_NORM_INF, max_norm, norms.data_ptr(),
+                                       norm.data_ptr(), work.data_ptr(), need, T.raw_stream(index))
     if st:
         raise CtError(st, "ct_clip_grads")
     return norm, norms

@@ -18,8 +18,10 @@ namespace ct {
 namespace ops {
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int64_t LEAST = 4096, MOST = 1024 * THREADS;   // values of a block
+constexpr int64_t BLOCKS = 1216;                  // wanted: 8 for each of 152 SMs
+constexpr int UNROLL = 4;                         // 16-byte loads of a thread on their way together
 
 struct ClipTensor {
     const void *src;
@@ -33,9 +35,11 @@ struct ClipTensor {
 template <int N> struct Table {
     ClipTensor t[N];
     int n;                                        // tensors here
+    int blocks;                                   // blocks here
     int base;                                     // blocks of the launches before
     int first;                                    // tensors of the launches before
     int64_t chunk;                                // values of a block
+    float keep;                                   // share of a block's values, the last ones, that may stay in L2 for the second pass
 };
 constexpr int SMALL = 48, LARGE = 480;            // 2.7 and 27 KB of arguments (at most 32,764 bytes)
 
@@ -51,6 +55,12 @@ __device__ __forceinline__ float load(const ClipTensor &t, int64_t i) {
            : t.dtype == CT_DT_F16 ? to_f32(static_cast<const __half *>(t.src)[at])
                                   : to_f32(static_cast<const __nv_bfloat16 *>(t.src)[at]);
 }
+__device__ __forceinline__ void store(const ClipTensor &t, int64_t i, float v) {
+    const int64_t r = t.rows == 1 ? 0 : i / t.cols, at = r * t.ld_dst + (i - r * t.cols);
+    if (t.dtype == CT_DT_F32) static_cast<float *>(t.dst)[at] = v;
+    else if (t.dtype == CT_DT_F16) static_cast<__half *>(t.dst)[at] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16 *>(t.dst)[at] = __float2bfloat16_rn(v);
+}
 
 __device__ __forceinline__ float join_top(float a, float b) { return a != a ? a : (b != b ? b : fmaxf(a, b)); }
 
@@ -64,30 +74,89 @@ template <typename TAB> __device__ __forceinline__ int find(const TAB &tab, int 
     return lo;
 }
 
+// A block's run of a dense tensor: values before the first 16-byte boundary, 16-byte vectors, values behind them.
+struct Run {
+    int64_t i0, i1, head, vecs;
+    __device__ __forceinline__ Run(const void *src, int size, int64_t from, int64_t to) : i0(from), i1(to) {
+        const int64_t off = (int64_t)((16 - ((uintptr_t)src + (uintptr_t)(from * size)) % 16) % 16) / size;
+        head = off < to - from ? off : to - from;
+        vecs = (to - from - head) * size / 16;
+    }
+};
+
+struct Found {
+    float s, m;
+};
+__device__ __forceinline__ void see(Found &f, float v) {
+    f.s = fmaf(v, v, f.s);
+    f.m = fmaxf(f.m, fabsf(v));
+}
+// f(v) for the values of vectors from to to - 1 that are the thread's; KEEP: by loads that leave them in L2
+template <typename T, bool KEEP, typename F> __device__ __forceinline__ void each_vector(const uint4 *q, int64_t from, int64_t to, F f) {
+    constexpr int E = 16 / (int)sizeof(T);
+    int64_t v = from + threadIdx.x;
+    for (; v + (UNROLL - 1) * THREADS < to; v += (int64_t)THREADS * UNROLL) {
+        uint4 u[UNROLL];
+#pragma unroll
+        for (int i = 0; i < UNROLL; ++i) u[i] = KEEP ? q[v + i * THREADS] : __ldcs(q + v + i * THREADS);
+#pragma unroll
+        for (int i = 0; i < UNROLL; ++i) {
+            float x[E];
+            unpack16<T>(u[i], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f(x[e]);
+        }
+    }
+    for (; v < to; v += THREADS) {
+        float x[E];
+        unpack16<T>(q[v], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(x[e]);
+    }
+}
+// f(v) for every value of the thread's share of a run; the last `keep` of its vectors stay in L2
+template <typename T, typename F> __device__ __forceinline__ void each_value(const T *src, const Run &r, float keep, F f) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const T *p = src + r.i0;
+    const int tid = threadIdx.x;
+    if (tid < r.head) f(to_f32(p[tid]));
+    const int64_t tail = r.head + r.vecs * E;
+    if (tail + tid < r.i1 - r.i0) f(to_f32(p[tail + tid]));
+    const uint4 *q = reinterpret_cast<const uint4 *>(p + r.head);
+    const int64_t far = (int64_t)((float)r.vecs * (1.f - keep));
+    each_vector<T, false>(q, 0, far, f);
+    each_vector<T, true>(q, far, r.vecs, f);
+}
+template <typename F> __device__ __forceinline__ void each_value(const ClipTensor &t, int64_t i0, int64_t i1, float keep, F f) {
+    if (t.rows > 1) {
+        for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) f(load(t, i));
+    } else if (t.dtype == CT_DT_F32) {
+        each_value(static_cast<const float *>(t.src), Run(t.src, 4, i0, i1), keep, f);
+    } else if (t.dtype == CT_DT_F16) {
+        each_value(static_cast<const __half *>(t.src), Run(t.src, 2, i0, i1), keep, f);
+    } else {
+        each_value(static_cast<const __nv_bfloat16 *>(t.src), Run(t.src, 2, i0, i1), keep, f);
+    }
+}
+
 template <int N> __global__ void __launch_bounds__(THREADS) clip_parts_kernel(const __grid_constant__ Table<N> tab, Part *parts) {
     pdl_wait();
     pdl_trigger();
     const ClipTensor &t = tab.t[find(tab, (int)blockIdx.x)];
     const int64_t total = t.rows * t.cols, i0 = (int64_t)((int)blockIdx.x - t.block0) * tab.chunk, i1 = min(i0 + tab.chunk, total);
-    float s = 0.f, m = 0.f;
-    for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) {
-        const float v = load(t, i);
-        s = fmaf(v, v, s);
-        m = fmaxf(m, fabsf(v));
-    }
-    double sum = s;
-    if (s == s && m > 0.f && m < __builtin_huge_valf() && (m > 0x1p55f || m < 0x1p-50f)) {
+    Found f = {0.f, 0.f};
+    each_value(t, i0, i1, tab.keep, [&](float v) { see(f, v); });
+    double sum = f.s;
+    float m = f.m;
+    if (f.s == f.s && m > 0.f && m < __builtin_huge_valf() && (m > 0x1p55f || m < 0x1p-50f)) {
         const int e = ilogbf(m);
-        s = 0.f;
-        for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) {
-            const float v = ldexpf(load(t, i), -e);
-            s = fmaf(v, v, s);
-        }
-        sum = ldexp((double)s, 2 * e);
+        f.s = 0.f;
+        each_value(t, i0, i1, tab.keep, [&](float v) { see(f, ldexpf(v, -e)); });
+        sum = ldexp((double)f.s, 2 * e);
     }
-    if (s != s) m = s;
-    __shared__ double ss[THREADS / 32];
-    __shared__ float sm[THREADS / 32];
+    if (f.s != f.s) m = f.s;
+    __shared__ double ss[WARPS];
+    __shared__ float sm[WARPS];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -99,7 +168,7 @@ template <int N> __global__ void __launch_bounds__(THREADS) clip_parts_kernel(co
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < THREADS / 32; ++w) {
+        for (int w = 1; w < WARPS; ++w) {
             sum += ss[w];
             m = join_top(m, sm[w]);
         }
@@ -107,28 +176,85 @@ template <int N> __global__ void __launch_bounds__(THREADS) clip_parts_kernel(co
     }
 }
 
-// What the launches hand on: sums over the tensors so far, then the factor.
-struct Found {
-    double sum;
-    float top;
-    float factor;
-};
+// values of a run times c into dst, whose run starts at the same place of a 16-byte unit; from its end on, which the first pass has
+// left in L2
+template <typename T> __device__ __forceinline__ void scale_run(const T *src, T *dst, const Run &r, float c) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const T *p = src + r.i0;
+    T *d = dst + r.i0;
+    const int tid = threadIdx.x;
+    if (tid < r.head) d[tid] = from_f32<T>(to_f32(p[tid]) * c);
+    const int64_t tail = r.head + r.vecs * E;
+    if (tail + tid < r.i1 - r.i0) d[tail + tid] = from_f32<T>(to_f32(p[tail + tid]) * c);
+    const uint4 *q = reinterpret_cast<const uint4 *>(p + r.head);
+    uint4 *w = reinterpret_cast<uint4 *>(d + r.head);
+    int64_t v = r.vecs - 1 - tid;
+    for (; v - (UNROLL - 1) * THREADS >= 0; v -= (int64_t)THREADS * UNROLL) {
+        uint4 u[UNROLL];
+#pragma unroll
+        for (int i = 0; i < UNROLL; ++i) u[i] = __ldcs(q + v - i * THREADS);
+#pragma unroll
+        for (int i = 0; i < UNROLL; ++i) {
+            float x[E];
+            unpack16<T>(u[i], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] *= c;
+            __stcs(w + v - i * THREADS, pack16<T>(x));
+        }
+    }
+    for (; v >= 0; v -= THREADS) {
+        float x[E];
+        unpack16<T>(__ldcs(q + v), x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] *= c;
+        __stcs(w + v, pack16<T>(x));
+    }
+}
+template <typename T> __device__ __forceinline__ bool scale_dense(const ClipTensor &t, int64_t i0, int64_t i1, float c) {
+    if (((uintptr_t)t.src - (uintptr_t)t.dst) % 16 != 0) return false;
+    scale_run(static_cast<const T *>(t.src), static_cast<T *>(t.dst), Run(t.src, (int)sizeof(T), i0, i1), c);
+    return true;
+}
 
-// One block: the norms of a launch's tensors from their blocks' parts, a warp a
-// tensor, each in the order of its values; after the last launch's the factor.
-constexpr int JOIN_WARPS = 32;
-template <int N> __global__ void __launch_bounds__(32 * JOIN_WARPS)
-clip_join_kernel(const __grid_constant__ Table<N> tab, const Part *parts, int blocks, Found *found, float *norms, int kind,
-                 double max_norm, float *norm, int last) {
+// Every block joins the parts of all blocks, in one order, to the factor; the blocks share the tensors' own norms among them.  Then
+// each scales its run.
+template <int N> __global__ void __launch_bounds__(THREADS)
+clip_scale_kernel(const __grid_constant__ Table<N> tab, const Part *parts, int all, int kind, double max_norm, float *norms, float *norm) {
     pdl_wait();
     pdl_trigger();
-    __shared__ double ss[N];
-    __shared__ float sm[N];
+    __shared__ double ss[WARPS];
+    __shared__ float sm[WARPS], factor;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = warp; i < tab.n; i += JOIN_WARPS) {
-        const int p0 = tab.t[i].block0, p1 = i + 1 < tab.n ? tab.t[i + 1].block0 : blocks;
-        double sum = 0.0;
-        float m = 0.f;
+    double sum = 0.0;
+    float m = 0.f;
+    for (int i = threadIdx.x; i < all; i += THREADS) {
+        const Part p = parts[i];
+        sum += p.sum;
+        m = join_top(m, p.top);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        m = join_top(m, __shfl_xor_sync(0xffffffffu, m, o));
+    }
+    if (lane == 0) {
+        ss[warp] = sum;
+        sm[warp] = m;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < WARPS; ++w) {
+            sum += ss[w];
+            m = join_top(m, sm[w]);
+        }
+        const double v = kind == CT_NORM_2 ? sqrt(sum) : (double)m;
+        factor = isfinite((float)v) && v > max_norm ? (float)(max_norm / v) : 1.f;
+        if (blockIdx.x == 0 && tab.first == 0) *norm = (float)v;
+    }
+    for (int i = (int)blockIdx.x + (int)gridDim.x * warp; i < tab.n; i += (int)gridDim.x * WARPS) {
+        const int p0 = tab.t[i].block0, p1 = i + 1 < tab.n ? tab.t[i + 1].block0 : tab.blocks;
+        sum = 0.0;
+        m = 0.f;
         for (int p = p0 + lane; p < p1; p += 32) {
             sum += parts[tab.base + p].sum;
             m = join_top(m, parts[tab.base + p].top);
@@ -138,43 +264,23 @@ clip_join_kernel(const __grid_constant__ Table<N> tab, const Part *parts, int bl
             sum += __shfl_xor_sync(0xffffffffu, sum, o);
             m = join_top(m, __shfl_xor_sync(0xffffffffu, m, o));
         }
-        if (lane == 0) {
-            ss[i] = sum;
-            sm[i] = m;
-            norms[tab.first + i] = kind == CT_NORM_2 ? (float)sqrt(sum) : m;
-        }
+        if (lane == 0) norms[tab.first + i] = kind == CT_NORM_2 ? (float)sqrt(sum) : m;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        Found f = tab.first > 0 ? *found : Found{0.0, 0.f, 1.f};
-        for (int i = 0; i < tab.n; ++i) {
-            f.sum += ss[i];
-            f.top = join_top(f.top, sm[i]);
-        }
-        if (last) {
-            const double v = kind == CT_NORM_2 ? sqrt(f.sum) : (double)f.top;
-            *norm = (float)v;
-            f.factor = isfinite((float)v) && v > max_norm ? (float)(max_norm / v) : 1.f;
-        }
-        *found = f;
-    }
-}
-
-template <int N> __global__ void __launch_bounds__(THREADS) clip_scale_kernel(const __grid_constant__ Table<N> tab, const Found *found) {
-    pdl_wait();
-    pdl_trigger();
-    const ClipTensor &t = tab.t[find(tab, (int)blockIdx.x)];
-    const float c = found->factor;
+    const float c = factor;
+    const int block = tab.blocks - 1 - (int)blockIdx.x;
+    if (block < 0) return;
+    const ClipTensor &t = tab.t[find(tab, block)];
     if (c == 1.f && t.src == t.dst) return;
-    const int64_t total = t.rows * t.cols, i0 = (int64_t)((int)blockIdx.x - t.block0) * tab.chunk, i1 = min(i0 + tab.chunk, total);
-    for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) {
-        const float v = load(t, i);
-        const int64_t r = t.rows == 1 ? 0 : i / t.cols, at = r * t.ld_dst + (i - r * t.cols);
-        const float o = c == 1.f ? v : v * c;
-        if (t.dtype == CT_DT_F32) static_cast<float *>(t.dst)[at] = o;
-        else if (t.dtype == CT_DT_F16) static_cast<__half *>(t.dst)[at] = __float2half_rn(o);
-        else static_cast<__nv_bfloat16 *>(t.dst)[at] = __float2bfloat16_rn(o);
+    const int64_t i0 = (int64_t)(block - t.block0) * tab.chunk, i1 = min(i0 + tab.chunk, t.rows * t.cols);
+    if (t.rows == 1) {
+        // 1 times a value is the value, but for a NaN, whose bits need not stay: it stays one
+        if (t.dtype == CT_DT_F32 ? scale_dense<float>(t, i0, i1, c)
+            : t.dtype == CT_DT_F16 ? scale_dense<__half>(t, i0, i1, c)
+                                   : scale_dense<__nv_bfloat16>(t, i0, i1, c))
+            return;
     }
+    for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) store(t, i, load(t, i) * c);
 }
 
 inline bool tensor_ok(const ct_tensor &t) {
@@ -203,31 +309,26 @@ bool overlap(std::vector<Range> &v) {
 
 // values of a block: blocks enough for the whole GPU, with something to do for each
 int64_t chunk_of(int64_t total) {
-    const int64_t want = (total + 1215) / 1216;   // 8 blocks of each of 152 SMs
-    const int64_t c = (want + 1023) / 1024 * 1024;
+    const int64_t c = ((total + BLOCKS - 1) / BLOCKS + 1023) / 1024 * 1024;
     return c < LEAST ? LEAST : c > MOST ? MOST : c;
 }
+// at most so many blocks: each tensor may end with a part of one
+inline int64_t blocks_most(int64_t n, int64_t total) { return total / chunk_of(total) + n; }
 
-ct_status measure(const ct_tensor *t, int64_t n, int64_t *total, int64_t *blocks) {
-    if (n < 0 || n > INT32_MAX) return CT_ERANGE;
-    if (n > 0 && t == nullptr) return CT_EINVAL;
-    *total = 0;
-    for (int64_t i = 0; i < n; ++i) {
-        if (t[i].rows < 0 || t[i].cols < 0 || (t[i].rows > 0 && t[i].cols > (INT64_MAX >> 8) / t[i].rows)) return CT_ERANGE;
-        *total += t[i].rows * t[i].cols;
-        if (*total > INT64_MAX >> 8) return CT_ERANGE;
-    }
-    const int64_t chunk = chunk_of(*total);
-    *blocks = 0;
-    for (int64_t i = 0; i < n; ++i) *blocks += (t[i].rows * t[i].cols + chunk - 1) / chunk;
-    return *blocks > INT32_MAX ? CT_ERANGE : CT_OK;
+ct_status sizes(int64_t n, int64_t total) {
+    return n < 0 || total < 0 || n > INT32_MAX / 2 || total > INT64_MAX >> 8 || blocks_most(n, total) > INT32_MAX ? CT_ERANGE : CT_OK;
 }
 
+// What of the second pass may come from L2: a part of it, next to what is being written.
+constexpr double L2_SHARE = 64e6;
+
 template <int N>
-cudaError_t launch(const ct_tensor *t, int64_t n, int64_t chunk, int kind, double max_norm, float *norms, float *norm, Part *parts,
-                   Found *found, cudaStream_t st) {
+cudaError_t launch(const ct_tensor *t, int64_t n, int64_t total, double bytes, int kind, double max_norm, float *norms, float *norm,
+                   Part *parts, cudaStream_t st) {
     Table<N> tab;
-    tab.chunk = chunk;
+    tab.chunk = chunk_of(total);
+    tab.keep = bytes > L2_SHARE ? (float)(L2_SHARE / bytes) : 1.f;
+    int all = 0;
     for (int pass = 0; pass < 2; ++pass) {
         tab.base = 0;
         for (int64_t first = 0; first < n || first == 0; first += N) {
@@ -239,17 +340,17 @@ cudaError_t launch(const ct_tensor *t, int64_t n, int64_t chunk, int kind, doubl
                 const bool flat = q.rows <= 1 || (q.ld_src == q.cols && q.ld_dst == q.cols);
                 tab.t[i] = {q.src, q.dst, flat ? 1 : q.rows, flat ? q.rows * q.cols : q.cols, q.ld_src, q.ld_dst, (int32_t)q.dtype,
                             (int32_t)blocks};
-                blocks += (q.rows * q.cols + chunk - 1) / chunk;
+                blocks += (q.rows * q.cols + tab.chunk - 1) / tab.chunk;
             }
+            tab.blocks = (int)blocks;
             cudaError_t e = cudaSuccess;
-            const dim3 grid((unsigned)blocks), block(THREADS);
+            const dim3 block(THREADS);
             if (pass == 0) {
-                if (blocks > 0) e = pdl_launch(clip_parts_kernel<N>, grid, block, 0, st, tab, parts);
-                if (e == cudaSuccess)
-                    e = pdl_launch(clip_join_kernel<N>, dim3(1), dim3(32 * JOIN_WARPS), 0, st, tab, (const Part *)parts, (int)blocks,
-                                   found, norms, kind, max_norm, norm, (int)(first + N >= n));
-            } else if (blocks > 0) {
-                e = pdl_launch(clip_scale_kernel<N>, grid, block, 0, st, tab, (const Found *)found);
+                all += (int)blocks;
+                if (blocks > 0) e = pdl_launch(clip_parts_kernel<N>, dim3((unsigned)blocks), block, 0, st, tab, parts);
+            } else {
+                e = pdl_launch(clip_scale_kernel<N>, dim3((unsigned)(blocks > 0 ? blocks : 1)), block, 0, st, tab, (const Part *)parts, all,
+                               kind, max_norm, norms, norm);
             }
             if (e != cudaSuccess) return e;
             tab.base += (int)blocks;
@@ -261,12 +362,11 @@ cudaError_t launch(const ct_tensor *t, int64_t n, int64_t chunk, int kind, doubl
 }  // namespace ops
 }  // namespace ct
 
-extern "C" ct_status ct_clip_grads_workspace(const ct_tensor *tensors, int64_t n, size_t *bytes) {
+extern "C" ct_status ct_clip_grads_workspace(int64_t n, int64_t values, size_t *bytes) {
     using namespace ct::ops;
     if (bytes == nullptr) return CT_EINVAL;
-    int64_t total, blocks;
-    const ct_status s = measure(tensors, n, &total, &blocks);
-    if (s == CT_OK) *bytes = sizeof(Found) + sizeof(Part) * (size_t)blocks;
+    const ct_status s = sizes(n, values);
+    if (s == CT_OK) *bytes = sizeof(Part) * (size_t)(blocks_most(n, values) + 1);
     return s;
 }
 
@@ -274,14 +374,22 @@ extern "C" ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t 
                                    float *norm_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
     using namespace ct::ops;
     if ((kind != CT_NORM_2 && kind != CT_NORM_INF) || !(max_norm >= 0.0)) return CT_EINVAL;
-    int64_t total, blocks;
-    const ct_status s = measure(tensors, n, &total, &blocks);
-    if (s != CT_OK) return s;
-    if (norm_dev == nullptr || !aligned(norm_dev, 4) || (n > 0 && (norms_dev == nullptr || !aligned(norms_dev, 4)))) return CT_EINVAL;
-    for (int64_t i = 0; i < n; ++i)
-        if (tensors[i].dtype < CT_DT_F32 || tensors[i].dtype > CT_DT_BF16 || !tensor_ok(tensors[i])) return CT_EINVAL;
+    if (n < 0 || n > INT32_MAX / 2) return CT_ERANGE;
+    if (norm_dev == nullptr || !aligned(norm_dev, 4) || (n > 0 && (tensors == nullptr || norms_dev == nullptr || !aligned(norms_dev, 4))))
+        return CT_EINVAL;
+    int64_t total = 0;
+    double bytes = 0.0;
+    for (int64_t i = 0; i < n; ++i) {
+        const ct_tensor &t = tensors[i];
+        if (t.rows < 0 || t.cols < 0 || (t.rows > 0 && t.cols > (INT64_MAX >> 8) / t.rows)) return CT_ERANGE;
+        if (t.dtype < CT_DT_F32 || t.dtype > CT_DT_BF16 || !tensor_ok(t)) return CT_EINVAL;
+        total += t.rows * t.cols;
+        if (total > INT64_MAX >> 8) return CT_ERANGE;
+        bytes += (double)(t.rows * t.cols) * dtype_size((int)t.dtype);
+    }
+    if (sizes(n, total) != CT_OK) return CT_ERANGE;
     if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
-    if (workspace_bytes < sizeof(Found) + sizeof(Part) * (size_t)blocks) return CT_ENOMEM;
+    if (workspace_bytes < sizeof(Part) * (size_t)(blocks_most(n, total) + 1)) return CT_ENOMEM;
     try {
         std::vector<Range> v;
         v.reserve(2 * (size_t)n);
@@ -301,11 +409,9 @@ extern "C" ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t 
     } catch (const std::exception &) {
         return CT_ENOMEM;
     }
-    Found *found = static_cast<Found *>(workspace_dev);
-    Part *parts = reinterpret_cast<Part *>(found + 1);
+    Part *parts = static_cast<Part *>(workspace_dev);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int64_t chunk = chunk_of(total);
-    const cudaError_t e = n <= SMALL ? launch<SMALL>(tensors, n, chunk, kind, max_norm, norms_dev, norm_dev, parts, found, st)
-                                     : launch<LARGE>(tensors, n, chunk, kind, max_norm, norms_dev, norm_dev, parts, found, st);
+    const cudaError_t e = n <= SMALL ? launch<SMALL>(tensors, n, total, bytes, kind, max_norm, norms_dev, norm_dev, parts, st)
+                                     : launch<LARGE>(tensors, n, total, bytes, kind, max_norm, norms_dev, norm_dev, parts, st);
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
