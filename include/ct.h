@@ -666,7 +666,8 @@ ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t kind, doubl
  * Without draft logits q_j is 1 at the draft and 0 elsewhere.  Draft x_j stands while
  * those before it stand and uniform[j] q_j(x_j) < p_j(x_j).  The token after the
  * last that stands is the one of largest w / noise[b], the lowest index among
- * equals: w = max(p_j - q_j, 0) if draft j fell (p_j where that is 0 everywhere), and
+ * equals: w = max(p_j - q_j, 0) if draft j fell (differences below 2^-20 of p_j count as
+ * 0; p_j where all are 0), and
  * p_d if none fell.  With independent uniform numbers and exponentially distributed
  * noise the tokens are distributed as the target's.  T = temperature[b] (NULL: 1);
  * below 1e-30 it counts as 0: the target's most probable token (lowest index among

@@ -9,9 +9,13 @@
 // sum, so its outcome hangs on no order of addition; ties go to the lower index.
 //
 // A row's maximum m and Z = sum e^((x - m) / T) come from parts of the row, each held
-// in FP32 relative to its own maximum and joined in FP64; the comparisons that decide
-// are made in FP64.
+// in FP32 relative to its own maximum; comparisons that are close are made in FP64.
+//
+// Two launches.  The first reads every row once, a warp for each piece of a row, and is bound by HBM (it has about the
+// least time that one exponential for each value leaves, too).  The second decides, a cluster for each sequence, and reads
+// the row of the draft that fell, the draft's, and the noise: the rows mostly from L2.
 #include "ops_common.cuh"
+#include "tc_common.cuh"
 
 namespace ct {
 namespace ops {
@@ -20,9 +24,6 @@ namespace {
 constexpr float INF = __builtin_huge_valf();
 __device__ __forceinline__ float nan_f() { return __uint_as_float(0x7FC00000u); }
 constexpr float LOG2E = 1.4426950408889634f;
-
-constexpr int THREADS = 512;
-constexpr int64_t PIECE = 16384;                  // values of a row that a block looks at
 
 struct VerifyArgs {
     const void *x, *q;
@@ -36,10 +37,11 @@ struct VerifyArgs {
     float *logprob;
 };
 
-// what a piece of a row holds: its largest logit (NaN for a NaN or +inf in it), the lowest index that has it, and sum e^((x - m) / T)
+// What a piece of a row holds: its largest logit, sum e^((x - m) / T) (NaN where a NaN or +inf is in it), and, for greedy sequences, the
+// lowest index that has the largest.
 struct Piece {
     float m, z;
-    int64_t at;
+    int32_t at, pad;
 };
 
 struct Sequence {
@@ -61,43 +63,117 @@ __device__ __forceinline__ Sequence sequence(const VerifyArgs &a, int64_t b) {
     return s;
 }
 
-template <typename T> __device__ __forceinline__ Piece scan(const T *x, int64_t j0, int64_t j1, float heat) {
-    Piece p = {-INF, 0.f, -1};
-    bool bad = false;
-    const float c = heat * LOG2E;
-    for (int64_t j = j0 + threadIdx.x; j < j1; j += THREADS) {
-        const float v = to_f32(x[j]);
-        bad |= !(v < INF);
-        if (v > p.m) {
-            p.z = p.z * exp2f((p.m - v) * c) + 1.f;
-            p.m = v;
-            p.at = j;
-        } else if (v > -INF) {
-            p.z += exp2f((v - p.m) * c);
-        }
-    }
-    if (bad) p.m = nan_f();
-    return p;
-}
-
-__device__ __forceinline__ Piece join(const Piece &a, const Piece &b, float heat) {
-    if (a.m != a.m) return a;
-    if (b.m != b.m) return b;
-    Piece r;
-    r.m = fmaxf(a.m, b.m);
-    const float c = heat * LOG2E;
-    r.z = (a.m == -INF ? 0.f : a.z * exp2f((a.m - r.m) * c)) + (b.m == -INF ? 0.f : b.z * exp2f((b.m - r.m) * c));
-    r.at = a.m > b.m || (a.m == b.m && (uint64_t)a.at < (uint64_t)b.at) ? a.at : b.at;
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 
-// pieces of rows: a block's row is blockIdx.x / pieces; the target's rows of all sequences, then the drafts'
+// ---------------------------------------------------------------- rows
+
+constexpr int ROW_WARPS = 4;
+constexpr int BATCH = 4;                          // vectors of 16 bytes that a lane takes at a time
+
+struct Stat {
+    float m, z;
+    int32_t at;
+};
+
+// N values, all of them from index `at` on (ARG: their order matters)
+template <int N, bool ARG> __device__ __forceinline__ void see(Stat &s, const float (&v)[N], float c, const int32_t (&at)[N]) {
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+    const float m = fmaxf(s.m, top), ref = m == -INF ? 0.f : m;
+    if (ARG && top > s.m) {
+        int32_t first = INT32_MAX;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (v[i] == top && at[i] < first) first = at[i];
+        s.at = first;
+    }
+    float z = s.z * ex2((s.m - ref) * c);         // s.m = -inf: s.z is 0, and stays it
+#pragma unroll
+    for (int i = 0; i < N; ++i) z += ex2((v[i] - ref) * c);                     // +inf and NaN give NaN
+    s.m = m;
+    s.z = z;
+}
+
+__device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c) {
+    Stat r;
+    r.m = fmaxf(a.m, b.m);
+    const float ref = r.m == -INF ? 0.f : r.m;
+    r.z = a.z * ex2((a.m - ref) * c) + b.z * ex2((b.m - ref) * c);
+    r.at = a.m > b.m || (a.m == b.m && a.at < b.at) ? a.at : b.at;
+    return r;
+}
+
+// values j0 to j1 - 1 of a row, by a warp
+template <typename T, bool ARG> __device__ __forceinline__ Stat scan(const T *x, int64_t j0, int64_t j1, float c) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+    Stat s = {-INF, 0.f, INT32_MAX};
+    const T *p = x + j0;
+    const int n = (int)(j1 - j0), off = (int)((16 - (uintptr_t)p % 16) % 16) / (int)sizeof(T), head = off < n ? off : n;
+    const int vecs = (n - head) / E, tail = head + vecs * E;
+    if (lane < head || lane < n - tail) {
+        const float v[2] = {lane < head ? to_f32(p[lane]) : -INF, lane < n - tail ? to_f32(p[tail + lane]) : -INF};
+        const int32_t at[2] = {(int32_t)j0 + lane, (int32_t)j0 + tail + lane};
+        see<2, ARG>(s, v, c, at);
+    }
+    const uint4 *q = reinterpret_cast<const uint4 *>(p + head);
+    int v0 = lane;
+    if (v0 + 32 * (BATCH - 1) < vecs) {
+        uint4 u[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) u[i] = q[v0 + 32 * i];
+        while (true) {
+            // the next batch is on its way while this one is worked on; behind the end, the last one again
+            const int next = v0 + 32 * BATCH, safe = next + 32 * (BATCH - 1) < vecs ? next : v0;
+            uint4 w[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) w[i] = q[safe + 32 * i];
+            float v[BATCH * E];
+            int32_t at[BATCH * E];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                unpack16<T>(u[i], v + i * E);
+                if (ARG)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) at[i * E + e] = (int32_t)j0 + head + (v0 + 32 * i) * E + e;
+            }
+            see<BATCH * E, ARG>(s, v, c, at);
+            v0 = next;
+            if (safe != next) break;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) u[i] = w[i];
+        }
+    }
+    for (; v0 < vecs; v0 += 32) {
+        float v[E];
+        int32_t at[E];
+        unpack16<T>(q[v0], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) at[e] = (int32_t)j0 + head + v0 * E + e;
+        see<E, ARG>(s, v, c, at);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const Stat b = {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o), __shfl_xor_sync(0xffffffffu, s.at, o)};
+        s = join(s, b, c);
+    }
+    return s;
+}
+
+// pieces of rows, a warp for each: the target's rows of all sequences, then the drafts'
 template <typename T>
-__global__ void __launch_bounds__(THREADS) verify_rows_kernel(VerifyArgs a, int pieces, Piece *out) {
+__global__ void __launch_bounds__(32 * ROW_WARPS) verify_rows_kernel(const VerifyArgs a, int pieces, int per, int64_t all, Piece *out) {
     pdl_wait();
     pdl_trigger();
-    const int64_t row = blockIdx.x / (unsigned)pieces, targets = a.count + a.sequences;
-    const int piece = (int)(blockIdx.x % (unsigned)pieces);
+    const int64_t unit = (int64_t)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5);
+    if (unit >= all) return;
+    const int64_t row = unit / pieces, targets = a.count + a.sequences;
+    const int piece = (int)(unit - row * pieces);
     const bool draft = row >= targets;
     const int64_t at = draft ? row - targets : row;
     // the sequence of the row: the last whose rows begin at or before it
@@ -109,167 +185,293 @@ __global__ void __launch_bounds__(THREADS) verify_rows_kernel(VerifyArgs a, int 
     }
     const Sequence s = sequence(a, lo);
     const T *x = draft ? static_cast<const T *>(a.q) + at * a.ldq : static_cast<const T *>(a.x) + at * a.ldx;
-    const int64_t j0 = piece * PIECE, j1 = min(j0 + PIECE, a.vocab);
-    Piece p = scan(x, j0, j1, s.heat);
-    __shared__ Piece sp[THREADS];
-    sp[threadIdx.x] = p;
-    __syncthreads();
-    for (int o = THREADS / 2; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) sp[threadIdx.x] = join(sp[threadIdx.x], sp[threadIdx.x + o], s.heat);
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) out[blockIdx.x] = sp[0];
+    const int64_t j0 = (int64_t)piece * per, j1 = min(j0 + per, a.vocab);
+    const float c = s.heat * LOG2E;
+    const Stat r = s.greedy ? scan<T, true>(x, j0, j1, c) : scan<T, false>(x, j0, j1, c);
+    if ((threadIdx.x & 31) == 0) out[unit] = {r.m, r.z, r.at, 0};
 }
 
-// a whole row: lse relative to its maximum, in FP64 (log sum e^((x - m) / T))
+// ---------------------------------------------------------------- sequences
+
+constexpr int THREADS = 512, WARPS = THREADS / 32;
+
+// a whole row: its largest logit and sum e^((x - m) / T); bad: a NaN or +inf in it
 struct Row {
-    float m;
-    double logz;
-    int64_t at;
+    float m, z;
+    int32_t at;
+    bool bad;
 };
 
-__device__ __forceinline__ Row row_of(const Piece *p, int pieces, float heat) {
-    Row r = {-INF, 0.0, -1};
-    double z = 0.0;
-    for (int i = 0; i < pieces; ++i) {
-        if (p[i].m != p[i].m) return {p[i].m, 0.0, -1};
-        if (p[i].m > r.m) {
-            r.m = p[i].m;
-            r.at = p[i].at;
+// by a warp
+__device__ __forceinline__ Row row_of(const Piece *p, int pieces, float c) {
+    const int lane = threadIdx.x & 31;
+    Row r = {-INF, 0.f, INT32_MAX, false};
+    for (int i = lane; i < pieces; i += 32) {
+        const Piece q = p[i];
+        if (q.m > r.m || (q.m == r.m && q.at < r.at)) {
+            r.m = q.m;
+            r.at = q.at;
         }
     }
-    if (r.m == -INF) return r;
-    for (int i = 0; i < pieces; ++i)
-        if (p[i].m > -INF) z += (double)p[i].z * exp((double)(p[i].m - r.m) * (double)heat);
-    r.logz = log(z);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m = __shfl_xor_sync(0xffffffffu, r.m, o);
+        const int32_t at = __shfl_xor_sync(0xffffffffu, r.at, o);
+        if (m > r.m || (m == r.m && at < r.at)) {
+            r.m = m;
+            r.at = at;
+        }
+    }
+    const float ref = r.m == -INF ? 0.f : r.m;
+    for (int i = lane; i < pieces; i += 32) r.z += p[i].z * exp2f((p[i].m - ref) * c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
+    r.bad = !(r.z < INF) || r.m == INF;
+    if (r.m == -INF) r.at = -1;
     return r;
 }
 
-// log probability of a logit, in FP64
-__device__ __forceinline__ double logp_of(const Row &r, float x, float heat) {
-    return x == -INF ? -(double)INF : ((double)x - (double)r.m) * (double)heat - r.logz;
+// whether u q < p:  log(u zp / zq) + (xq - mq) / T < (x - m) / T.  In FP32 where that is clear (each term's error is a few 2^-23 of it);
+// FP64 is slow here (two operations a cycle for an SM) and left to what is close.
+__device__ __forceinline__ bool stands(float u, const Row &p, float x, bool have, const Row &q, float xq, float heat) {
+    if (have && !(xq > -INF)) return true;        // q is 0, p is not
+    const float l0 = logf(u), l1 = have ? logf(p.z) - logf(q.z) : logf(p.z), l2 = (x - p.m) * heat, l3 = have ? (xq - q.m) * heat : 0.f;
+    const float far = l0 + l1 + l3 - l2;
+    if (fabsf(far) > 1e-5f * (1.f + fabsf(l0) + fabsf(l2) + fabsf(l3) + 32.f)) return far < 0.f;
+    if (!(u > 0.f)) return u == 0.f;              // a NaN stands for nothing
+    double ratio = (double)u * (double)p.z, lq = 0.0;
+    if (have) {
+        ratio /= (double)q.z;
+        lq = ((double)xq - (double)q.m) * (double)heat;
+    }
+    return log(ratio) + lq < ((double)x - (double)p.m) * (double)heat;
+}
+
+struct Best {
+    float score;
+    int32_t at;                                   // -1: none
+};
+__device__ __forceinline__ bool better(float s, int32_t at, const Best &b) {
+    return at >= 0 && (b.at < 0 || s > b.score || (s == b.score && at < b.at));
+}
+
+// p, or p - q, from logits: each an exponential times the reciprocal of its row's sum, so that equal logits of equal rows come out at
+// most a few 2^-24 apart (sums of the same numbers in two orders).  A difference below 2^-20 of p is none: equal rows leave nothing,
+// and not what rounding leaves.
+struct Weigh {
+    float pm, pz, qm, qz, c;
+    int32_t out;                                  // the token that does not count, or -1
+};
+// The quotient's 2^-22 next to w's own error is nothing.  A weight of 0, and a NaN, win nothing.
+template <bool REST> __device__ __forceinline__ void race(Best &b, const Weigh &w, float x, float q, float e, int32_t j) {
+    float p = ex2((x - w.pm) * w.c) * w.pz;
+    if (REST) {
+        const float r = fmaf(-ex2((q - w.qm) * w.c), w.qz, p);
+        p = r > p * 0x1p-20f ? r : 0.f;
+    } else {
+        p = j == w.out ? 0.f : p;
+    }
+    const float s = __fdividef(p, e);
+    if (s > b.score) b = {s, j};
+}
+
+// the best of values j0 to j1 - 1, a thread's: each thread's values come in ascending order
+template <typename T, bool REST>
+__device__ __forceinline__ Best run_race(const T *x, const T *q, const float *e, int64_t j0, int64_t j1, const Weigh &w) {
+    constexpr int E = 16 / (int)sizeof(T);
+    Best b = {0.f, -1};
+    if (((uintptr_t)(x + j0) | (uintptr_t)(e + j0) | (REST ? (uintptr_t)(q + j0) : 0)) % 16 == 0) {
+        const int vecs = (int)((j1 - j0) / E);
+        const uint4 *px = reinterpret_cast<const uint4 *>(x + j0), *pq = reinterpret_cast<const uint4 *>(REST ? q + j0 : x + j0);
+        const uint4 *pe = reinterpret_cast<const uint4 *>(e + j0);
+        constexpr int G = 2;                      // vectors whose loads are on their way together
+        for (int v0 = threadIdx.x; v0 < vecs; v0 += G * THREADS) {
+            uint4 ux[G], uq[G], ue[G][E / 4];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int v = v0 + g * THREADS < vecs ? v0 + g * THREADS : v0;  // the same again behind the end: it wins nothing more
+                ux[g] = px[v];
+                if (REST) uq[g] = pq[v];
+#pragma unroll
+                for (int i = 0; i < E / 4; ++i) ue[g][i] = __ldcs(pe + v * (E / 4) + i);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int v = v0 + g * THREADS < vecs ? v0 + g * THREADS : v0;
+                float fx[E], fq[E] = {}, fe[E];
+                unpack16<T>(ux[g], fx);
+                if (REST) unpack16<T>(uq[g], fq);
+#pragma unroll
+                for (int i = 0; i < E / 4; ++i) unpack16<float>(ue[g][i], fe + 4 * i);
+#pragma unroll
+                for (int i = 0; i < E; ++i) race<REST>(b, w, fx[i], fq[i], fe[i], (int32_t)j0 + v * E + i);
+            }
+        }
+        for (int64_t j = j0 + (int64_t)vecs * E + threadIdx.x; j < j1; j += THREADS)
+            race<REST>(b, w, to_f32(x[j]), REST ? to_f32(q[j]) : 0.f, e[j], (int32_t)j);
+        return b;
+    }
+    int64_t j = j0 + threadIdx.x;
+    for (; j + 3 * THREADS < j1; j += 4 * THREADS) {
+        float fx[4], fq[4] = {}, fe[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fx[i] = to_f32(x[j + i * THREADS]);
+            if (REST) fq[i] = to_f32(q[j + i * THREADS]);
+            fe[i] = __ldcs(e + j + i * THREADS);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) race<REST>(b, w, fx[i], fq[i], fe[i], (int32_t)j + i * THREADS);
+    }
+    for (; j < j1; j += THREADS) race<REST>(b, w, to_f32(x[j]), REST ? to_f32(q[j]) : 0.f, e[j], (int32_t)j);
+    return b;
 }
 
 enum { STANDS = 0, FALLS = 1, BAD = 2 };
 
 template <typename T>
-__global__ void __launch_bounds__(THREADS) verify_draw_kernel(VerifyArgs a, int pieces, const Piece *parts) {
+__global__ void __launch_bounds__(THREADS, 2) verify_draw_kernel(const VerifyArgs a, int pieces, const Piece *parts, int splits) {
+    __shared__ int verdict[CT_MAX_DRAFTS + 1];
+    __shared__ Row target[CT_MAX_DRAFTS + 1], draft[CT_MAX_DRAFTS + 1];
+    __shared__ Best found[WARPS];
+    __shared__ Best mine;                         // this CTA's, read by the others
     pdl_wait();
     pdl_trigger();
-    const int64_t b = blockIdx.x;
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t b = blockIdx.x / (unsigned)splits;
     const Sequence s = sequence(a, b);
     const int64_t row0 = s.from + b, targets = a.count + a.sequences;
     const T *tx = static_cast<const T *>(a.x), *tq = static_cast<const T *>(a.q);
-    __shared__ int verdict[CT_MAX_DRAFTS + 1];
-    __shared__ double lps[CT_MAX_DRAFTS + 1];
-    __shared__ Row target, draft;
+    const float c = s.heat * LOG2E;
+    // the rows, a warp for each: the target's d + 1, the draft's d
+    const int rows = s.d + 1 + (tq != nullptr && !s.greedy ? s.d : 0);
+    for (int i = warp; i < rows; i += WARPS) {
+        const bool t = i <= s.d;
+        const Row r = row_of(parts + (t ? row0 + i : targets + s.from + i - s.d - 1) * pieces, pieces, c);
+        if (lane == 0) (t ? target[i] : draft[i - s.d - 1]) = r;
+    }
+    __syncthreads();
     if ((int)threadIdx.x <= s.d) {
         const int j = threadIdx.x;
-        const Row p = row_of(parts + (row0 + j) * pieces, pieces, s.heat);
+        const Row p = target[j];
         int v = BAD;
-        double lp = 0.0;
-        if (!s.bad && p.m == p.m) {
+        if (!s.bad && !p.bad) {
             v = FALLS;
             if (j < s.d) {
                 const int64_t id = a.drafts[s.from + j];
                 const bool there = id >= 0 && id < a.vocab;
-                lp = there ? logp_of(p, to_f32(tx[(row0 + j) * a.ldx + id]), s.heat) : -(double)INF;
+                const float x = there ? to_f32(tx[(row0 + j) * a.ldx + id]) : -INF;
                 if (s.greedy) {
                     v = there && id == p.at ? STANDS : FALLS;
-                } else {
-                    double lq = 0.0;
-                    bool fine = true;
-                    if (tq != nullptr) {
-                        const Row q = row_of(parts + (targets + s.from + j) * pieces, pieces, s.heat);
-                        fine = q.m == q.m;
-                        lq = there && q.m > -INF ? logp_of(q, to_f32(tq[(s.from + j) * a.ldq + id]), s.heat) : -(double)INF;
-                    }
-                    v = !fine ? BAD : there && lp > -(double)INF && log((double)a.uniform[s.from + j]) + lq < lp ? STANDS : FALLS;
+                } else if (tq != nullptr && draft[j].bad) {
+                    v = BAD;
+                } else if (x > -INF) {
+                    const float xq = tq != nullptr ? to_f32(tq[(s.from + j) * a.ldq + id]) : 0.f;
+                    v = stands(a.uniform[s.from + j], p, x, tq != nullptr, draft[j], xq, s.heat) ? STANDS : FALLS;
                 }
             }
         }
         verdict[j] = v;
-        lps[j] = lp;
     }
     __syncthreads();
     int n = 0;
     while (n < s.d && verdict[n] == STANDS) ++n;
     const bool bad = verdict[n] == BAD, fell = n < s.d;
-    if (threadIdx.x == 0) {
-        target = row_of(parts + (row0 + n) * pieces, pieces, s.heat);
-        if (fell && tq != nullptr) draft = row_of(parts + (targets + s.from + n) * pieces, pieces, s.heat);
-    }
-    __syncthreads();
     int64_t token = -1;
     if (!bad && s.greedy) {
-        token = target.at;
+        token = target[n].at;
     } else if (!bad) {
         const T *x = tx + (row0 + n) * a.ldx, *q = fell && tq != nullptr ? tq + (s.from + n) * a.ldq : nullptr;
         const float *e = a.noise + b * a.ld_noise;
-        const int64_t id = fell ? a.drafts[s.from + n] : -1;
-        // the best of w / E with the draft's part taken out, and without
-        float best[2] = {0.f, 0.f};
-        int64_t at[2] = {-1, -1};
-        const float c = s.heat * LOG2E, pz = (float)(-target.logz * 1.4426950408889634), qz = (float)(-draft.logz * 1.4426950408889634);
-        for (int64_t j = threadIdx.x; j < a.vocab; j += THREADS) {
-            const float v = to_f32(x[j]);
-            if (!(v > -INF)) continue;
-            const float p = exp2f(fmaf(v - target.m, c, pz)), w = to_f32(q != nullptr ? q[j] : T());
-            const float r = !fell             ? p
-                            : q != nullptr    ? p - (w > -INF ? exp2f(fmaf(w - draft.m, c, qz)) : 0.f)
-                            : j == id         ? 0.f
-                                              : p;
-            const float s0 = r / e[j], s1 = p / e[j];
-            if (r > 0.f && s0 > best[0]) { best[0] = s0; at[0] = j; }
-            if (p > 0.f && s1 > best[1]) { best[1] = s1; at[1] = j; }
-        }
-        __shared__ float sb[2][THREADS];
-        __shared__ int64_t sa[2][THREADS];
-        for (int k = 0; k < 2; ++k) {
-            sb[k][threadIdx.x] = best[k];
-            sa[k][threadIdx.x] = at[k];
-        }
-        __syncthreads();
-        for (int o = THREADS / 2; o > 0; o >>= 1) {
-            if ((int)threadIdx.x < o)
-                for (int k = 0; k < 2; ++k) {
-                    const float v = sb[k][threadIdx.x + o];
-                    const int64_t i = sa[k][threadIdx.x + o];
-                    if (v > sb[k][threadIdx.x] || (v == sb[k][threadIdx.x] && (uint64_t)i < (uint64_t)sa[k][threadIdx.x])) {
-                        sb[k][threadIdx.x] = v;
-                        sa[k][threadIdx.x] = i;
-                    }
-                }
+        const int64_t id = fell && q == nullptr ? a.drafts[s.from + n] : -1;
+        const Row p = target[n];
+        // the draft's part: its row, or all of its token
+        bool rest = fell && tq != nullptr && draft[n].m > -INF;
+        const Weigh w = {p.m, 1.f / p.z, rest ? draft[n].m : 0.f, rest ? 1.f / draft[n].z : 0.f, c, -1};
+        Weigh w0 = w;
+        if (id >= 0 && id < a.vocab) w0.out = (int32_t)id;
+        const bool empty = p.m == -INF;
+        // pieces that start on 16 bytes wherever the rows do
+        const int64_t per = (a.vocab + 8 * splits - 1) / (8 * splits) * 8, j0 = min(per * rank, a.vocab), j1 = min(j0 + per, a.vocab);
+        // once with the draft's part taken out; where that leaves nothing, without
+        for (int round = 0; round < 2; ++round) {
+            Best m = {0.f, -1};
+            if (!empty) m = rest ? run_race<T, true>(x, q, e, j0, j1, w) : run_race<T, false>(x, q, e, j0, j1, round == 0 ? w0 : w);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const float sc = __shfl_xor_sync(0xffffffffu, m.score, o);
+                const int32_t at = __shfl_xor_sync(0xffffffffu, m.at, o);
+                if (better(sc, at, m)) m = {sc, at};
+            }
+            if (lane == 0) found[warp] = m;
             __syncthreads();
+            if (threadIdx.x == 0) {
+                for (int i = 1; i < WARPS; ++i)
+                    if (better(found[i].score, found[i].at, m)) m = found[i];
+                mine = m;
+            }
+            __syncthreads();
+            m = mine;
+            if (splits > 1) {
+                tc::cluster_sync();
+                m = {0.f, -1};
+                for (int r = 0; r < splits; ++r) {
+                    const uint32_t at = tc::mapa_shared(tc::smem_u32(&mine), (uint32_t)r);
+                    float sc;
+                    int32_t i;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(sc) : "r"(at) : "memory");
+                    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(i) : "r"(at + 4) : "memory");
+                    if (better(sc, i, m)) m = {sc, i};
+                }
+                tc::cluster_sync();               // all have read, before a CTA leaves or goes round again
+            } else {
+                __syncthreads();
+            }
+            token = m.at;
+            if (token >= 0 || empty || (!rest && w0.out < 0)) break;            // the whole cluster alike
+            rest = false;
         }
-        token = sa[0][0] >= 0 ? sa[0][0] : sa[1][0];
     }
+    if (rank != 0) return;
     if (threadIdx.x == 0) a.accepted[b] = n;
     if ((int)threadIdx.x <= a.most) {
         const int j = threadIdx.x;
-        int64_t id = -1;
+        const int64_t id = j < n ? a.drafts[s.from + j] : j == n ? token : -1;
         float lp = 0.f;
-        if (j < n) {
-            id = a.drafts[s.from + j];
-            lp = (float)lps[j];
-        } else if (j == n) {
-            id = token;
-            lp = bad ? nan_f() : token < 0 ? -INF : (float)logp_of(target, to_f32(tx[(row0 + n) * a.ldx + token]), s.heat);
-        }
+        if (j <= n) lp = j == n && bad ? nan_f() : id < 0 ? -INF : (to_f32(tx[(row0 + j) * a.ldx + id]) - target[j].m) * s.heat - logf(target[j].z);
         a.token[b * (a.most + 1) + j] = id;
         a.logprob[b * (a.most + 1) + j] = lp;
     }
 }
 
+// ---------------------------------------------------------------- host
+
 inline int64_t rows_of(int64_t sequences, int64_t drafts) { return 2 * drafts + sequences; }
-inline int64_t pieces_of(int64_t vocab) { return vocab > PIECE ? (vocab + PIECE - 1) / PIECE : 1; }
+// Values of a piece: the warps of a few rows share them in pieces of 2048 (two batches of 16-bit values); where there are many rows, longer
+// pieces leave less to join.
+inline int64_t per_of(int64_t rows, int64_t vocab) {
+    int64_t per = 2048;
+    while (per < 16384 && rows * ((vocab + per - 1) / per) > 32 * 152) per *= 2;
+    return per;
+}
+inline int64_t pieces_of(int64_t rows, int64_t vocab) {
+    const int64_t per = per_of(rows, vocab);
+    return vocab > per ? (vocab + per - 1) / per : 1;
+}
 
 template <typename T> cudaError_t launch(const VerifyArgs &a, Piece *parts, cudaStream_t st) {
-    const int pieces = (int)pieces_of(a.vocab);
-    const int64_t rows = a.count + a.sequences + (a.q != nullptr ? a.count : 0);
-    const cudaError_t e = pdl_launch(verify_rows_kernel<T>, dim3((unsigned)(rows * pieces)), dim3(THREADS), 0, st, a, pieces, parts);
+    const int64_t most = rows_of(a.sequences, a.count), rows = a.q != nullptr ? most : a.count + a.sequences;
+    const int pieces = (int)pieces_of(most, a.vocab), per = (int)per_of(most, a.vocab);
+    const int64_t all = rows * pieces;
+    const cudaError_t e = pdl_launch(verify_rows_kernel<T>, dim3((unsigned)((all + ROW_WARPS - 1) / ROW_WARPS)), dim3(32 * ROW_WARPS), 0, st, a,
+                                     pieces, per, all, parts);
     if (e != cudaSuccess) return e;
-    return pdl_launch(verify_draw_kernel<T>, dim3((unsigned)a.sequences), dim3(THREADS), 0, st, a, pieces, (const Piece *)parts);
+    // few sequences: clusters share a sequence's row, as many CTAs as are resident together (two for each SM)
+    int splits = 1;
+    while (splits < 8 && a.sequences * splits <= sm_count() && a.vocab >= 4096 * splits) splits *= 2;
+    if (splits == 1) return pdl_launch(verify_draw_kernel<T>, dim3((unsigned)a.sequences), dim3(THREADS), 0, st, a, pieces, (const Piece *)parts, splits);
+    return pdl_launch_cluster(verify_draw_kernel<T>, dim3((unsigned)(a.sequences * splits)), dim3(THREADS), 0, st, splits, a, pieces,
+                              (const Piece *)parts, splits);
 }
 }  // namespace
 }  // namespace ops
@@ -278,10 +480,10 @@ template <typename T> cudaError_t launch(const VerifyArgs &a, Piece *parts, cuda
 extern "C" ct_status ct_verify_drafts_workspace(int64_t sequences, int64_t drafts, int64_t vocab, int64_t max_drafts, size_t *bytes) {
     using namespace ct::ops;
     if (bytes == nullptr) return CT_EINVAL;
-    if (sequences < 0 || drafts < 0 || vocab < 0 || sequences > INT32_MAX || drafts > INT32_MAX / 2 || vocab > INT32_MAX ||
-        max_drafts < 0 || max_drafts > CT_MAX_DRAFTS || rows_of(sequences, drafts) * pieces_of(vocab) > INT32_MAX)
+    if (sequences < 0 || drafts < 0 || vocab < 0 || sequences > INT32_MAX / 8 || drafts > INT32_MAX / 2 || vocab > INT32_MAX ||
+        max_drafts < 0 || max_drafts > CT_MAX_DRAFTS || rows_of(sequences, drafts) * pieces_of(rows_of(sequences, drafts), vocab) > INT32_MAX)
         return CT_ERANGE;
-    *bytes = sizeof(Piece) * (size_t)(rows_of(sequences, drafts) * pieces_of(vocab));
+    *bytes = sizeof(Piece) * (size_t)(rows_of(sequences, drafts) * pieces_of(rows_of(sequences, drafts), vocab));
     return CT_OK;
 }
 
