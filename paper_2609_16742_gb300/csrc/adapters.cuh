@@ -1,8 +1,9 @@
 // What the adapters' kernels share: the rows' order by adapter, tiles of 16-bit
 // parts in shared memory, and products of those on the tensor cores.
 //
-// The long products (rows by many) run as mma.sync on 16-bit operands with FP32
-// sums.  BF16 values are taken as they are.  FP16 and FP32 values, and the short FP32
+// The long products (rows by many) run on the tensor cores with 16-bit operands and FP32
+// sums: as tcgen05.mma where rows are 16-bit values that can be copied as they lie
+// (adapters_tc.cu), else as mma.sync on what has gone through registers.  BF16 values are taken as they are.  FP16 and FP32 values, and the short FP32
 // vectors between two products, are taken apart into BF16 parts of 8 bits each
 // (v = hi + mid + lo; two parts hold an FP16 value), and the products of parts
 // that matter are added: those of parts p and q with p + q <= 1 where the result has 16
@@ -229,6 +230,12 @@ inline int ad_padded(int64_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 
 cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
 cudaError_t ad_expand(const AdExpand &a, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
 cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st);
+
+// The same on tcgen05, for 16-bit values in whole rows; splits: CTAs of a cluster that share the summed axis.
+cudaError_t ad_shrink_tc(const AdShrink &a, bool bf16, bool trans, const AdOrder &o, int tiles, int splits, cudaStream_t st);
+cudaError_t ad_expand_tc(const AdExpand &a, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
+bool ad_outer_tc_takes(int64_t rank, int parts);
+cudaError_t ad_outer_tc(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st);
 
 }  // namespace ops
 }  // namespace ct

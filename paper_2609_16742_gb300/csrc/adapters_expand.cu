@@ -12,15 +12,13 @@ namespace ct {
 namespace ops {
 namespace {
 
-// FAST: the matrix's values are one part and its rows whole: its copies run from global to shared memory, two steps ahead.
-// Otherwise they go through registers, a step ahead.
-template <typename TM, int RP, bool TRANS, bool FAST> struct Expand {
-    static constexpr int PM = Parts<TM>::N, STAGES = FAST ? 3 : 2;
+template <typename TM, int RP, bool TRANS> struct Expand {
+    static constexpr int PM = Parts<TM>::N;
     static constexpr int LV = ad_pitch(RP), LM = ad_pitch(TRANS ? AD_STEP : RP);
     static constexpr int V_BYTES = AD_ROWS * LV, M_ROWS = TRANS ? RP : AD_STEP, M_BYTES = M_ROWS * LM;
     static constexpr int WIDE = 33, OUT = 8 * 8 * WIDE * 4;                      // 8 x 32 sums of each warp, where rows start anywhere
     static constexpr int M_VECS = M_ROWS * (TRANS ? AD_STEP / 8 : RP / 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
-    static int smem(int parts, bool out) { return parts * V_BYTES + STAGES * PM * M_BYTES + (out ? OUT : 0); }
+    static int smem(int parts, bool out) { return parts * V_BYTES + 2 * PM * M_BYTES + (out ? OUT : 0); }
 };
 
 // eight neighbouring values of a row of y, from 16 bytes on
@@ -62,9 +60,9 @@ __device__ __forceinline__ void y_put(char *p, int dtype, float v) {
     else *reinterpret_cast<__nv_bfloat16 *>(p) = __float2bfloat16_rn(v);
 }
 
-template <typename TM, int RP, bool TRANS, bool FAST>
+template <typename TM, int RP, bool TRANS>
 __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, const AdOrder o) {
-    using S = Expand<TM, RP, TRANS, FAST>;
+    using S = Expand<TM, RP, TRANS>;
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ int32_t rows[AD_ROWS];
     pdl_wait();
@@ -109,25 +107,6 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         }
     };
     Units<TM> um[S::MV];
-    auto copy = [&](int64_t c0, int buf) {
-        const uint32_t bm = bm0 + buf * S::M_BYTES;
-#pragma unroll
-        for (int i = 0; i < S::MV; ++i) {
-            const int v = tid + i * AD_THREADS;
-            int left;
-            const TM *p = m_at(c0, v, left);
-            if (v >= S::M_VECS) continue;
-            if constexpr (TRANS) {
-                const uint32_t row = bm + v / 8 * S::LM + (v % 8 / 4) * 64 + (v % 4) * 4;
-                const int bytes = left > 0 ? 4 : 0;
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(row + 16 * q), "l"(reinterpret_cast<const char *>(p) + 4 * q), "r"(bytes) : "memory");
-            } else {
-                copy16_if(bm + v / (RP / 8) * S::LM + v % (RP / 8) * 16, p, left > 0);
-            }
-        }
-    };
     auto fetch = [&](int64_t c0) {
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
@@ -151,22 +130,14 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         }
     };
     if (product) {
-        if constexpr (FAST) {
-#pragma unroll
-            for (int i = 0; i < S::STAGES - 1; ++i) {
-                if (c_from + i * AD_STEP < c_to) copy(c_from + i * AD_STEP, i);
-                copies_end();
-            }
-        } else {
-            fetch(c_from);
-        }
+        fetch(c_from);
         for (int v = tid; v < a.parts * AD_ROWS * (RP / 8); v += AD_THREADS) {
             const int p = v / (AD_ROWS * (RP / 8)), r = v / (RP / 8) % AD_ROWS, j = v % (RP / 8);
             const bool there = r < tile.rows;
             sts16(base + p * S::V_BYTES + r * S::LV + j * 16,
                   ld_if(static_cast<const uint4 *>(a.v) + (there ? (p * o.t + tile.slot0 + r) * (RP / 8) + j : 0), there));
         }
-        if constexpr (!FAST) store(c_from, 0);
+        store(c_from, 0);
     }
     __syncthreads();
     // this thread's rows: lane / 4 + 8 i of the warp's 32
@@ -184,20 +155,10 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     YEight ahead[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) ahead[i] = y_load(yr[i] + (c_from + mine0) * ys, a.y_dtype, y_whole && yh[i] && c_from + mine0 < c_to);
-    int at = 0;
-    for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, ++at) {
+    int buf = 0;
+    for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, buf ^= 1) {
         const bool more = product && c0 + AD_STEP < c_to;
-        const int buf = at % S::STAGES;
-        if constexpr (FAST) {
-            if (product) {
-                copies_wait<S::STAGES - 2>();
-                __syncthreads();
-                if (c0 + (S::STAGES - 1) * AD_STEP < c_to) copy(c0 + (S::STAGES - 1) * AD_STEP, (at + S::STAGES - 1) % S::STAGES);
-                copies_end();
-            }
-        } else if (more) {
-            fetch(c0 + AD_STEP);
-        }
+        if (more) fetch(c0 + AD_STEP);
         const int64_t mine = c0 + mine0, next = mine + AD_STEP;
         YEight y[4];
 #pragma unroll
@@ -256,7 +217,7 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
             }
         } else {
             // rows that start anywhere: eight rows of the warp's sums at a time turn in shared memory, so that lanes are neighbouring columns
-            float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + S::STAGES * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
+            float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + 2 * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
             const int64_t c = c0 + wn * 32 + lane;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -282,18 +243,15 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
                 __syncwarp();
             }
         }
-        if constexpr (!FAST) {
-            if (more) store(c0 + AD_STEP, (at + 1) % S::STAGES);
-            __syncthreads();
-        }
+        if (more) store(c0 + AD_STEP, buf ^ 1);
+        __syncthreads();
     }
-    if constexpr (FAST) copies_wait<0>();
 }
 
-template <typename TM, int RP, bool TRANS, bool FAST> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
-    using S = Expand<TM, RP, TRANS, FAST>;
+template <typename TM, int RP, bool TRANS> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
+    using S = Expand<TM, RP, TRANS>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = expand_kernel<TM, RP, TRANS, FAST>;
+    auto *kernel = expand_kernel<TM, RP, TRANS>;
     const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3, true));
     if (e != cudaSuccess) return e;
     // columns of a block: as many as leave each SM three blocks, at most 1024
@@ -307,23 +265,23 @@ template <typename TM, int RP, bool TRANS, bool FAST> cudaError_t launch(const A
     const dim3 grid((unsigned)tiles, (unsigned)((a.cols + a.per - 1) / a.per));
     return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts, !(a.whole & 1)), st, a, o);
 }
-template <typename TM, bool TRANS, bool FAST> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
+template <typename TM, bool TRANS> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TM, 16, TRANS, FAST>(a, o, tiles, st);
-        case 32: return launch<TM, 32, TRANS, FAST>(a, o, tiles, st);
-        case 64: return launch<TM, 64, TRANS, FAST>(a, o, tiles, st);
-        default: return launch<TM, 128, TRANS, FAST>(a, o, tiles, st);
+        case 16: return launch<TM, 16, TRANS>(a, o, tiles, st);
+        case 32: return launch<TM, 32, TRANS>(a, o, tiles, st);
+        case 64: return launch<TM, 64, TRANS>(a, o, tiles, st);
+        default: return launch<TM, 128, TRANS>(a, o, tiles, st);
     }
 }
 template <bool TRANS> cudaError_t by_type(const AdExpand &a, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
-    if (dtype == CT_DT_BF16 && (a.whole & 2)) return by_rank<__nv_bfloat16, TRANS, true>(a, o, tiles, st);
-    return dtype == CT_DT_F32   ? by_rank<float, TRANS, false>(a, o, tiles, st)
-           : dtype == CT_DT_F16 ? by_rank<__half, TRANS, false>(a, o, tiles, st)
-                                : by_rank<__nv_bfloat16, TRANS, false>(a, o, tiles, st);
+    return dtype == CT_DT_F32   ? by_rank<float, TRANS>(a, o, tiles, st)
+           : dtype == CT_DT_F16 ? by_rank<__half, TRANS>(a, o, tiles, st)
+                                : by_rank<__nv_bfloat16, TRANS>(a, o, tiles, st);
 }
 }  // namespace
 
 cudaError_t ad_expand(const AdExpand &a, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
+    if (dtype == CT_DT_BF16 && a.whole == 3) return ad_expand_tc(a, trans, o, tiles, st);
     return trans ? by_type<true>(a, dtype, o, tiles, st) : by_type<false>(a, dtype, o, tiles, st);
 }
 

@@ -14,10 +14,8 @@ namespace {
 
 constexpr int COLS = 128;
 
-// FAST: values are one part and rows whole: copies run from global to shared memory, two steps ahead.  Otherwise values go through
-// registers, a step ahead.
-template <typename TX, int RP, bool FAST> struct Outer {
-    static constexpr int PX = Parts<TX>::N, STAGES = FAST ? 3 : 2;
+template <typename TX, int RP> struct Outer {
+    static constexpr int PX = Parts<TX>::N;
     static constexpr int LX = ad_pitch(COLS), LV = ad_pitch(RP);
     static constexpr int X_BYTES = AD_STEP * LX, V_BYTES = AD_STEP * LV;
     static constexpr int XV = AD_STEP * (COLS / 8) / AD_THREADS;                  // 4
@@ -28,14 +26,14 @@ template <typename TX, int RP, bool FAST> struct Outer {
     static constexpr bool EACH = PX > 1;
     static constexpr int FLUSH = 2;
     static int smem(int parts) {
-        const int all = STAGES * (PX * X_BYTES + parts * V_BYTES);
+        const int all = 2 * (PX * X_BYTES + parts * V_BYTES);
         return all > SUM ? all : SUM;
     }
 };
 
-template <typename TX, int RP, bool FAST>
+template <typename TX, int RP>
 __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, const AdOrder o, int splits) {
-    using S = Outer<TX, RP, FAST>;
+    using S = Outer<TX, RP>;
     extern __shared__ __align__(128) unsigned char sm[];
     pdl_wait();
     pdl_trigger();
@@ -64,23 +62,6 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
         return static_cast<const uint4 *>(a.v) + (there ? (p * o.t + t) * (RP / 8) + v % (RP / 8) : 0);
     };
     auto v_to = [&](int v) { return v / (RP / 8) * S::LV + v % (RP / 8) * 16; };
-    auto copy = [&](int64_t s, int buf) {
-        const uint32_t bx = base + buf * buf_bytes, bv = bx + S::X_BYTES;
-#pragma unroll
-        for (int i = 0; i < S::XV; ++i) {
-            int left;
-            const TX *p = x_at(s, i, left);
-            copy16_if(bx + x_to + i * RUN * S::LX, p, left > 0);
-        }
-        for (int p = 0; p < a.parts; ++p)
-#pragma unroll
-            for (int i = 0; i < S::VV; ++i) {
-                const int v = tid + i * AD_THREADS;
-                bool there;
-                const uint4 *at = v_at(s, p, v, there);
-                if (v < S::V_VECS) copy16_if(bv + p * S::V_BYTES + v_to(v), at, there);
-            }
-    };
     Units<TX> ux[S::XV];
     uint4 ev[3][S::VV];
     auto fetch = [&](int64_t s) {
@@ -179,24 +160,7 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
             if constexpr (S::EACH) flush();
         }
     };
-    if constexpr (FAST) {
-#pragma unroll
-        for (int i = 0; i < S::STAGES - 1; ++i) {
-            if (s0 + i < s1) copy(s0 + i, i);
-            copies_end();
-        }
-        for (int64_t s = s0; s < s1; ++s) {
-            const int at = (int)(s - s0);
-            copies_wait<S::STAGES - 2>();
-            __syncthreads();
-            if (s + S::STAGES - 1 < s1) copy(s + S::STAGES - 1, (at + S::STAGES - 1) % S::STAGES);
-            copies_end();
-            compute(at % S::STAGES);
-            if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
-        }
-        copies_wait<0>();
-        __syncthreads();
-    } else if (s0 < s1) {
+    if (s0 < s1) {
         fetch(s0);
         store(s0, 0);
         __syncthreads();
@@ -237,35 +201,36 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
-template <typename TX, int RP, bool FAST> cudaError_t launch(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
-    using S = Outer<TX, RP, FAST>;
+template <typename TX, int RP> cudaError_t launch(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st) {
+    using S = Outer<TX, RP>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = outer_kernel<TX, RP, FAST>;
+    auto *kernel = outer_kernel<TX, RP>;
     const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3));
     if (e != cudaSuccess) return e;
-    // two CTAs for each SM, with two steps of an adapter's share of the rows at least for each
-    const int64_t blocks = (a.cols + COLS - 1) / COLS, steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP;
-    int splits = 1;
-    while (splits < 8 && blocks * o.adapters * splits < 2 * sm_count() && steps >= 4 * splits) splits *= 2;
+    const int64_t blocks = (a.cols + COLS - 1) / COLS;
     const dim3 grid((unsigned)(blocks * splits), (unsigned)o.adapters);
     if (splits == 1) return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, a, o, splits);
     return pdl_launch_cluster(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, splits, a, o, splits);
 }
-template <typename TX, bool FAST> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, cudaStream_t st) {
+template <typename TX> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TX, 16, FAST>(a, o, st);
-        case 32: return launch<TX, 32, FAST>(a, o, st);
-        case 64: return launch<TX, 64, FAST>(a, o, st);
-        default: return launch<TX, 128, FAST>(a, o, st);
+        case 16: return launch<TX, 16>(a, o, splits, st);
+        case 32: return launch<TX, 32>(a, o, splits, st);
+        case 64: return launch<TX, 64>(a, o, splits, st);
+        default: return launch<TX, 128>(a, o, splits, st);
     }
 }
 }  // namespace
 
 cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st) {
-    if (x_dtype == CT_DT_BF16 && (a.whole & 1)) return by_rank<__nv_bfloat16, true>(a, o, st);
-    return x_dtype == CT_DT_F32   ? by_rank<float, false>(a, o, st)
-           : x_dtype == CT_DT_F16 ? by_rank<__half, false>(a, o, st)
-                                  : by_rank<__nv_bfloat16, false>(a, o, st);
+    // two CTAs for each SM, with two steps of an adapter's share of the rows at least for each
+    const int64_t blocks = (a.cols + COLS - 1) / COLS, steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP;
+    int splits = 1;
+    while (splits < 8 && blocks * o.adapters * splits < 2 * sm_count() && steps >= 4 * splits) splits *= 2;
+    if (x_dtype == CT_DT_BF16 && (a.whole & 1) && ad_outer_tc_takes(a.rank, a.parts)) return ad_outer_tc(a, o, splits, st);
+    return x_dtype == CT_DT_F32   ? by_rank<float>(a, o, splits, st)
+           : x_dtype == CT_DT_F16 ? by_rank<__half>(a, o, splits, st)
+                                  : by_rank<__nv_bfloat16>(a, o, splits, st);
 }
 
 }  // namespace ops

@@ -11,17 +11,14 @@ namespace ct {
 namespace ops {
 namespace {
 
-// FAST: values are one part and rows whole: copies run from global to shared memory, STAGES - 1 steps ahead.  Otherwise values go
-// through registers, a step ahead.
-template <typename TX, typename TM, int RP, bool TRANS, bool FAST> struct Shrink {
+template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
     static constexpr bool F16 = sizeof(TX) == 2 && Parts<TX>::N == 2 && Parts<TM>::N == 2;
     static constexpr int PX = F16 ? 1 : Parts<TX>::N, PM = F16 ? 1 : Parts<TM>::N;
     static constexpr int LX = ad_pitch(AD_STEP), LM = ad_pitch(TRANS ? RP : AD_STEP);
     static constexpr int X_BYTES = AD_ROWS * LX, M_ROWS = TRANS ? AD_STEP : RP, M_BYTES = M_ROWS * LM;
-    static constexpr int STAGES = FAST ? (RP == 128 ? 3 : 4) : 2;
     static constexpr int BUF = PX * X_BYTES + PM * M_BYTES;
     static constexpr int SUM = AD_ROWS * (RP + 1) * 4;
-    static constexpr int SMEM = STAGES * BUF > SUM ? STAGES * BUF : SUM;
+    static constexpr int SMEM = 2 * BUF > SUM ? 2 * BUF : SUM;
     static constexpr int XV = AD_ROWS * 8 / AD_THREADS;                          // vectors of 8 values a thread loads
     static constexpr int M_VECS = M_ROWS * (TRANS ? RP / 8 : 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
     static constexpr int NT = RP / 16;                                           // 8-column tiles of a warp
@@ -31,9 +28,9 @@ template <typename TX, typename TM, int RP, bool TRANS, bool FAST> struct Shrink
     static constexpr int FLUSH = 4;
 };
 
-template <typename TX, typename TM, int RP, bool TRANS, bool FAST>
+template <typename TX, typename TM, int RP, bool TRANS>
 __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, const AdOrder o, int splits) {
-    using S = Shrink<TX, TM, RP, TRANS, FAST>;
+    using S = Shrink<TX, TM, RP, TRANS>;
     extern __shared__ __align__(128) unsigned char sm[];
     pdl_wait();
     pdl_trigger();
@@ -77,19 +74,6 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
     const int x_to = tid / 8 * S::LX + xc * 2;
     Units<TX> ux[S::XV];
     Units<TM> um[S::MV];
-    auto copy = [&](int64_t s, int buf) {
-        const uint32_t bx = base + buf * S::BUF, bm = bx + S::X_BYTES;
-        const int64_t c = s * AD_STEP + xc;
-#pragma unroll
-        for (int i = 0; i < S::XV; ++i) copy16_if(bx + x_to + 32 * i * S::LX, xr[i] + (c < a.cols ? c : 0), xh[i] && c < a.cols);
-#pragma unroll
-        for (int i = 0; i < S::MV; ++i) {
-            const int v = tid + i * AD_THREADS;
-            int left;
-            const TM *p = m_at(s, v, left);
-            if (v < S::M_VECS) copy16_if(bm + m_to(v), p, left > 0);
-        }
-    };
     auto fetch = [&](int64_t s) {
         const int64_t c = s * AD_STEP + xc;
         const int n = left_of(c, a.cols);
@@ -191,24 +175,7 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
         }
     };
 
-    if constexpr (FAST) {
-#pragma unroll
-        for (int i = 0; i < S::STAGES - 1; ++i) {
-            if (s0 + i < s1) copy(s0 + i, i);
-            copies_end();
-        }
-        for (int64_t s = s0; s < s1; ++s) {
-            const int at = (int)(s - s0);
-            copies_wait<S::STAGES - 2>();
-            __syncthreads();
-            if (s + S::STAGES - 1 < s1) copy(s + S::STAGES - 1, (at + S::STAGES - 1) % S::STAGES);
-            copies_end();
-            compute(at % S::STAGES);
-            if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
-        }
-        copies_wait<0>();
-        __syncthreads();
-    } else if (s0 < s1) {
+    if (s0 < s1) {
         fetch(s0);
         store(s0, 0);
         __syncthreads();
@@ -253,44 +220,41 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
-template <typename TX, typename TM, int RP, bool TRANS, bool FAST>
-cudaError_t launch(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t st) {
-    using S = Shrink<TX, TM, RP, TRANS, FAST>;
+template <typename TX, typename TM, int RP, bool TRANS>
+cudaError_t launch(const AdShrink &a, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+    using S = Shrink<TX, TM, RP, TRANS>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = shrink_kernel<TX, TM, RP, TRANS, FAST>;
+    auto *kernel = shrink_kernel<TX, TM, RP, TRANS>;
     const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
     if (e != cudaSuccess) return e;
-    // two CTAs for each SM, with four steps at least for each
-    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
-    int splits = 1;
-    while (splits < 8 && (int64_t)tiles * splits < 2 * sm_count() && steps >= 8 * splits) splits *= 2;
     if (splits == 1) return pdl_launch(kernel, dim3((unsigned)tiles), dim3(AD_THREADS), S::SMEM, st, a, o, splits);
     return pdl_launch_cluster(kernel, dim3((unsigned)(tiles * splits)), dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits);
 }
-template <typename TX, typename TM, bool TRANS, bool FAST>
-cudaError_t by_rank(const AdShrink &a, const AdOrder &o, int tiles, cudaStream_t st) {
+template <typename TX, typename TM, bool TRANS>
+cudaError_t by_rank(const AdShrink &a, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TX, TM, 16, TRANS, FAST>(a, o, tiles, st);
-        case 32: return launch<TX, TM, 32, TRANS, FAST>(a, o, tiles, st);
-        case 64: return launch<TX, TM, 64, TRANS, FAST>(a, o, tiles, st);
-        default: return launch<TX, TM, 128, TRANS, FAST>(a, o, tiles, st);
+        case 16: return launch<TX, TM, 16, TRANS>(a, o, tiles, splits, st);
+        case 32: return launch<TX, TM, 32, TRANS>(a, o, tiles, splits, st);
+        case 64: return launch<TX, TM, 64, TRANS>(a, o, tiles, splits, st);
+        default: return launch<TX, TM, 128, TRANS>(a, o, tiles, splits, st);
     }
 }
-template <bool TRANS> cudaError_t by_type(const AdShrink &a, int x_dtype, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
-    const bool fast = a.whole == 3;
-    if (dtype == CT_DT_F32) return by_rank<float, float, TRANS, false>(a, o, tiles, st);
-    if (dtype == CT_DT_F16) {
-        if (x_dtype == CT_DT_F32) return by_rank<float, __half, TRANS, false>(a, o, tiles, st);
-        return fast ? by_rank<__half, __half, TRANS, true>(a, o, tiles, st) : by_rank<__half, __half, TRANS, false>(a, o, tiles, st);
-    }
-    if (x_dtype == CT_DT_F32) return by_rank<float, __nv_bfloat16, TRANS, false>(a, o, tiles, st);
-    return fast ? by_rank<__nv_bfloat16, __nv_bfloat16, TRANS, true>(a, o, tiles, st)
-                : by_rank<__nv_bfloat16, __nv_bfloat16, TRANS, false>(a, o, tiles, st);
+template <bool TRANS> cudaError_t by_type(const AdShrink &a, int x_dtype, int dtype, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+    if (dtype == CT_DT_F32) return by_rank<float, float, TRANS>(a, o, tiles, splits, st);
+    if (dtype == CT_DT_F16)
+        return x_dtype == CT_DT_F32 ? by_rank<float, __half, TRANS>(a, o, tiles, splits, st) : by_rank<__half, __half, TRANS>(a, o, tiles, splits, st);
+    return x_dtype == CT_DT_F32 ? by_rank<float, __nv_bfloat16, TRANS>(a, o, tiles, splits, st)
+                                : by_rank<__nv_bfloat16, __nv_bfloat16, TRANS>(a, o, tiles, splits, st);
 }
 }  // namespace
 
 cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
-    return trans ? by_type<true>(a, x_dtype, dtype, o, tiles, st) : by_type<false>(a, x_dtype, dtype, o, tiles, st);
+    // two CTAs for each SM, with four steps at least for each
+    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
+    int splits = 1;
+    while (splits < 8 && (int64_t)tiles * splits < 2 * sm_count() && steps >= 8 * splits) splits *= 2;
+    if (a.whole == 3 && dtype != CT_DT_F32 && x_dtype == dtype) return ad_shrink_tc(a, dtype == CT_DT_BF16, trans, o, tiles, splits, st);
+    return trans ? by_type<true>(a, x_dtype, dtype, o, tiles, splits, st) : by_type<false>(a, x_dtype, dtype, o, tiles, splits, st);
 }
 
 }  // namespace ops

@@ -1,0 +1,608 @@
+// The adapters' products of many rows on the tcgen05 tensor cores, for 16-bit values in whole rows (16-byte starts, a multiple
+// of 8 values): what shrink_kernel, expand_kernel and outer_kernel compute, in the same order of tiles and splits.
+//
+// At rank 64 a value of x takes part in 128 operations, so that HBM's rate asks for some 420 TFLOP/s: more than mma.sync
+// reaches here (175 measured), a quarter of what tcgen05.mma does.  All threads copy (rows come in any order: cp.async, 16
+// bytes a thread, into the swizzled layouts that the tensor cores read), one issues the products; sums lie in tensor
+// memory and are moved to registers after every 256 values (the tensor cores cut off what they add) while the next go on into
+// other columns.  Operands whose summed axis runs along their rows in memory are read as they lie (MN-major).
+//
+// Every wait is bounded: one that runs out sets the operators' error word, ends the work after the copies and products under way,
+// and frees the tensor memory.
+#include "adapters.cuh"
+
+namespace ct {
+namespace ops {
+namespace {
+
+constexpr uint32_t E_ADAPTERS = 0x8000;
+
+// shared-memory operand: byte distances between atoms along MN (lbo) and along K or, K-major, along MN (sbo)
+enum { SW128 = 2, SW64 = 4, SW32 = 6 };
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_t sbo, int swizzle) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)((sbo >> 4) & 0x3FFF) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)swizzle << 61;
+}
+// instruction descriptor: FP32 sums of two FP16 or two BF16 operands; a_mn, b_mn: the summed axis runs along the operand's rows
+__host__ __device__ constexpr uint32_t product(bool bf16, bool a_mn, bool b_mn, int m, int n) {
+    return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 |
+           (uint32_t)(m >> 4) << 24;
+}
+
+// A matrix of `width` 16-bit values a row, MN-major or K-major alike: blocks of 64 values a row (128 bytes), or narrower ones.
+template <int WIDTH> struct Tile {
+    static constexpr int ROW = WIDTH >= 64 ? 128 : 2 * WIDTH;                    // bytes of a row in a block
+    static constexpr int SWIZZLE = ROW == 128 ? SW128 : ROW == 64 ? SW64 : SW32;
+    static constexpr int CHUNKS = WIDTH / 8;                                     // 16-byte chunks of a row, of all blocks
+    // chunk c of row r of a block of `rows` rows
+    static __device__ __forceinline__ uint32_t at(int r, int c, int rows) {
+        if (ROW == 128) return (uint32_t)((c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+        if (ROW == 64) return (uint32_t)(r * 64 + ((c ^ (r >> 1 & 3)) << 4));
+        return (uint32_t)(r * 32 + ((c ^ (r >> 2 & 1)) << 4));
+    }
+};
+
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = tc::tmem_done(r[i]);
+}
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// what this thread wrote to shared memory is seen by the tensor cores
+__device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// the barriers that a CTA's products arrive on, and its tensor memory
+template <int BARS, int COLUMNS> __device__ __forceinline__ uint32_t tensor_begin(uint64_t (&bars)[BARS], uint32_t &holder) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < BARS; ++i) tc::mbar_init(tc::smem_u32(&bars[i]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < 32) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tc::smem_u32(&holder)), "r"((uint32_t)COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    return holder;
+}
+template <int COLUMNS> __device__ __forceinline__ void tensor_end(uint32_t addr) {
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (threadIdx.x < 32) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"((uint32_t)COLUMNS));
+}
+constexpr int columns_of(int n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
+
+constexpr int FLUSH = 4;                          // steps whose sums stay in the tensor cores' accumulators: 256 values
+
+// ---------------------------------------------------------------- shrink
+
+template <int RP> struct Shrink {
+    static constexpr int X_BYTES = AD_ROWS * 128, M_BYTES = RP * 128, STAGE = X_BYTES + M_BYTES, STAGES = RP == 128 ? 3 : 4;
+    static constexpr int SMEM = STAGES * STAGE + 1024, COLUMNS = columns_of(2 * RP);
+    static constexpr int MV = (RP * 8 + AD_THREADS - 1) / AD_THREADS;
+};
+
+template <typename T, int RP, bool TRANS>
+__global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink a, const AdOrder o, int splits, uint32_t *err) {
+    using S = Shrink<RP>;
+    extern __shared__ unsigned char raw[];
+    __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
+    __shared__ uint32_t holder;
+    pdl_wait();
+    pdl_trigger();
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0;
+    const AdRows tile = ad_tile(o, (int)(blockIdx.x / (unsigned)splits));
+    if (tile.rows == 0 || tile.key == 0 || tile.key > o.adapters) return;       // the whole cluster alike
+    const int adapter = tile.key - 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tmem = tensor_begin<S::STAGES + 3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
+    const uint32_t base = (tc::smem_u32(raw) + 1023u) & ~1023u;
+    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
+    const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
+    const int n = (int)(s1 - s0);
+
+    const T *xr[4];
+    bool xh[4];
+    const int xc = (tid & 7) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = tid / 8 + 32 * i;
+        const int64_t s = tile.slot0 + r;
+        xh[i] = r < tile.rows;
+        xr[i] = static_cast<const T *>(a.x) + (xh[i] ? (o.order != nullptr ? (int64_t)o.order[s] : s) * a.ldx : 0);
+    }
+    const T *m = static_cast<const T *>(a.m) + adapter * a.m_adapter;
+    using MT = Tile<TRANS ? RP : AD_STEP>;
+    const uint32_t x_to = Tile<AD_STEP>::at(tid / 8, tid & 7, AD_ROWS);
+    auto copy = [&](int step) {
+        const uint32_t bx = base + (step % S::STAGES) * S::STAGE, bm = bx + S::X_BYTES;
+        const int64_t c0 = (s0 + step) * AD_STEP, c = c0 + xc;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) copy16_if(bx + x_to + 32 * i * 128, xr[i] + (c < a.cols ? c : 0), xh[i] && c < a.cols);
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS;
+            if (v >= RP * 8) break;
+            const int64_t cm = TRANS ? c0 + r : c0 + q * 8;
+            const int j = TRANS ? q * 8 : r;
+            const bool there = cm < a.cols && j < a.rank;
+            copy16_if(bm + MT::at(r, q, TRANS ? AD_STEP : RP), m + (there ? (TRANS ? cm * a.m_row + j : j * a.m_row + cm) : 0), there);
+        }
+    };
+    float sum[RP / 2];
+#pragma unroll
+    for (int j = 0; j < RP / 2; ++j) sum[j] = 0.f;
+    bool ok = true;
+    int groups = 0;                               // whose sums are in registers
+    const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * (RP / 2);
+    auto collect = [&]() {
+        ok = ok && tc::mbar_wait(bar + 8 * (S::STAGES + (groups & 1)), (groups >> 1) & 1, err, E_ADAPTERS);
+        __syncwarp();
+        fence_after();
+#pragma unroll
+        for (int j = 0; j < RP / 2; j += 8) {
+            float v[8];
+            tmem_ld8(mine + (groups & 1) * RP + j, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[j + e] += v[e];
+        }
+        fence_before();
+        ++groups;
+    };
+#pragma unroll
+    for (int i = 0; i < S::STAGES - 1; ++i) {
+        if (i < n) copy(i);
+        copies_end();
+    }
+    constexpr uint32_t how = product(Parts<T>::N == 1, false, TRANS, AD_ROWS, RP);
+    int at = 0;
+    for (; at < n; ++at) {
+        copies_wait<S::STAGES - 2>();
+        fence_operands();
+        if (!__syncthreads_and(ok)) break;
+        if (warp == 0 && tc::elect_one()) {
+            fence_after();
+            const uint32_t bx = base + (at % S::STAGES) * S::STAGE, bm = bx + S::X_BYTES;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t da = operand(bx + 32 * k, 16, 1024, SW128);
+                const uint64_t db = TRANS ? operand(bm + 16 * k * MT::ROW, AD_STEP * 128, 8 * MT::ROW, MT::SWIZZLE)
+                                          : operand(bm + 32 * k, 16, 1024, SW128);
+                tc::umma_f16(tmem + (at / FLUSH & 1) * RP, da, db, how, at % FLUSH > 0 || k > 0);
+            }
+            tc::umma_commit(bar + 8 * (at % S::STAGES));
+            if (at % FLUSH == FLUSH - 1 || at == n - 1) tc::umma_commit(bar + 8 * (S::STAGES + (at / FLUSH & 1)));
+        }
+        __syncwarp();
+        if (at > 0 && at + S::STAGES - 1 < n)
+            ok = ok && tc::mbar_wait(bar + 8 * ((at - 1) % S::STAGES), (at - 1) / S::STAGES & 1, err, E_ADAPTERS);
+        if (ok && at + S::STAGES - 1 < n) copy(at + S::STAGES - 1);
+        copies_end();
+        if (at % FLUSH == 1 && at > FLUSH) collect();
+    }
+    copies_wait<0>();
+    if (at == n) {
+        while (groups < (n + FLUSH - 1) / FLUSH) collect();
+    } else if (warp == 0 && tc::elect_one()) {
+        tc::umma_commit(bar + 8 * (S::STAGES + 2));                              // gave up: what was issued, before its memory goes
+    }
+    if (at < n) tc::mbar_wait(bar + 8 * (S::STAGES + 2), 0, err, E_ADAPTERS);
+    tensor_end<S::COLUMNS>(tmem);
+
+    // the tile's sums of this CTA, then of all of the cluster
+    float *fs = reinterpret_cast<float *>(raw);
+    const int row = (warp & 3) * 32 + lane;
+#pragma unroll
+    for (int j = 0; j < RP / 2; ++j) fs[row * (RP + 1) + (warp >> 2) * (RP / 2) + j] = sum[j];
+    if (splits > 1) tc::cluster_sync();
+    else __syncthreads();
+    const float scale = a.scale != nullptr ? a.scale[adapter] : 1.f;
+    const uint32_t peer = tc::smem_u32(raw);
+    const int r0 = AD_ROWS * rank / splits, r1 = AD_ROWS * (rank + 1) / splits;
+    for (int v = tid; v < (r1 - r0) * (RP / 2); v += AD_THREADS) {
+        const int r = r0 + v / (RP / 2), j = v % (RP / 2) * 2;
+        if (r >= tile.rows) break;
+        const int f = r * (RP + 1) + j;
+        float x = 0.f, y = 0.f;
+        for (int c = 0; c < splits; ++c) {
+            x += splits > 1 ? ld_peer_f32(peer + f * 4, c) : fs[f];
+            y += splits > 1 ? ld_peer_f32(peer + (f + 1) * 4, c) : fs[f + 1];
+        }
+        x = j < a.rank ? x * scale : 0.f;         // 0 and not 0 times what x holds
+        y = j + 1 < a.rank ? y * scale : 0.f;
+        uint32_t *out = static_cast<uint32_t *>(a.v) + ((tile.slot0 + r) * RP + j) / 2;
+        for (int p = 0; p < a.parts; ++p) out[p * (o.t * RP / 2)] = split2(x, y);
+    }
+    if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
+}
+
+// ---------------------------------------------------------------- expand
+
+// Columns of a block: 256 bytes of y a row.  A thread has one row and half of them.
+template <int RP, int YS> struct Expand {
+    static constexpr int COLS = 256 / YS, HALF = COLS / 2, V_BYTES = AD_ROWS * 2 * RP, M_BYTES = COLS * 2 * RP, STAGES = 3;
+    static constexpr int COLUMNS = columns_of(2 * COLS);
+    static int smem(int parts) { return parts * V_BYTES + STAGES * M_BYTES + 1024; }
+    static constexpr int MV = COLS * (RP / 8) / AD_THREADS > 0 ? COLS * (RP / 8) / AD_THREADS : 1;
+};
+
+template <int RP, bool TRANS, int YS>
+__global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a, const AdOrder o, uint32_t *err) {
+    using S = Expand<RP, YS>;
+    extern __shared__ unsigned char raw[];
+    __shared__ uint64_t bars[3];                  // a block's products are done (two, in turn); all
+    __shared__ uint32_t holder;
+    pdl_wait();
+    pdl_trigger();
+    const AdRows tile = ad_tile(o, (int)blockIdx.x);
+    const int64_t c_from = (int64_t)blockIdx.y * a.per, c_to = min(c_from + a.per, a.cols);
+    if (tile.rows == 0 || c_from >= c_to || (tile.key == 0 && !a.relu)) return;
+    const bool out = tile.key > o.adapters, none = tile.key == 0;               // NaN; act alone
+    const bool product_wanted = !out && !none;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tmem = tensor_begin<3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
+    const uint32_t vb = (tc::smem_u32(raw) + 1023u) & ~1023u, mb = vb + a.parts * S::V_BYTES;
+    const __nv_bfloat16 *m = static_cast<const __nv_bfloat16 *>(a.m) + (product_wanted ? (int64_t)(tile.key - 1) * a.m_adapter : 0);
+    const int n = (int)((c_to - c_from + S::COLS - 1) / S::COLS);
+    using VT = Tile<RP>;
+    using MT = Tile<TRANS ? S::COLS : RP>;
+    auto copy = [&](int b) {
+        const uint32_t bm = mb + (b % S::STAGES) * S::M_BYTES;
+        const int64_t c0 = c_from + (int64_t)b * S::COLS;
+#pragma unroll
+        for (int i = 0; i < S::MV; ++i) {
+            const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS;
+            if (v >= S::COLS * (RP / 8)) break;
+            const int64_t c = TRANS ? c0 + q * 8 : c0 + r;
+            const int j = TRANS ? r : q * 8;
+            const bool there = c < a.cols && j < a.rank;
+            copy16_if(bm + MT::at(r, q, TRANS ? RP : S::COLS), m + (there ? (TRANS ? j * a.m_row + c : c * a.m_row + j) : 0), there);
+        }
+    };
+    if (product_wanted) {
+        for (int v = tid; v < a.parts * AD_ROWS * (RP / 8); v += AD_THREADS) {
+            const int p = v / (AD_ROWS * (RP / 8)), r = v / (RP / 8) % AD_ROWS, q = v % (RP / 8);
+            const bool there = r < tile.rows;
+            copy16_if(vb + p * S::V_BYTES + VT::at(r, q, AD_ROWS),
+                      static_cast<const uint4 *>(a.v) + (there ? (p * o.t + tile.slot0 + r) * (RP / 8) + q : 0), there);
+        }
+#pragma unroll
+        for (int i = 0; i < S::STAGES - 1; ++i) {
+            if (i < n) copy(i);
+            copies_end();
+        }
+    }
+    // this thread's row and half of a block's columns
+    const int row = (warp & 3) * 32 + lane, half = (warp >> 2) * S::HALF;
+    const bool have = row < tile.rows;
+    const int64_t t = have ? (o.order != nullptr ? (int64_t)o.order[tile.slot0 + row] : tile.slot0 + row) : 0;
+    char *y0 = static_cast<char *>(a.y) + t * a.ldy * YS;
+    const float nan = __uint_as_float(0x7FC00000u);
+    uint4 y[8];                                   // 128 bytes
+    auto y_fetch = [&](int b) {
+        const int64_t c = c_from + (int64_t)b * S::COLS + half;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = ld_if(y0 + (c + i * (16 / YS)) * YS, have && c + i * (16 / YS) < c_to);
+    };
+    const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21) + (uint32_t)half;
+    // adds a block's sums (none where there is no product) to y
+    auto finish = [&](int b) {
+        const int64_t c0 = c_from + (int64_t)b * S::COLS + half;
+#pragma unroll
+        for (int j = 0; j < S::HALF; j += 8) {
+            float v[8], w[8];
+            if (product_wanted) {
+                tmem_ld8(mine + (b & 1) * S::COLS + j, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 0.f;
+            }
+            if constexpr (YS == 4) {
+                unpack16<float>(y[j / 4], w);
+                unpack16<float>(y[j / 4 + 1], w + 4);
+            } else if (a.y_dtype == CT_DT_F16) {
+                unpack16<__half>(y[j / 8], w);
+            } else {
+                unpack16<__nv_bfloat16>(y[j / 8], w);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += w[e];
+            if (a.relu || out)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = out ? nan : v[e] < 0.f ? 0.f : v[e];
+            if (have && c0 + j < c_to) {
+                char *p = y0 + (c0 + j) * YS;
+                if constexpr (YS == 4) {
+                    *reinterpret_cast<uint4 *>(p) = pack16<float>(v);
+                    *reinterpret_cast<uint4 *>(p + 16) = pack16<float>(v + 4);
+                } else {
+                    *reinterpret_cast<uint4 *>(p) = a.y_dtype == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
+                }
+            }
+        }
+    };
+    bool ok = true;
+    constexpr uint32_t how = product(true, false, TRANS, AD_ROWS, S::COLS);
+    int b = 0;
+    if (product_wanted) {
+        for (; b < n; ++b) {
+            copies_wait<S::STAGES - 2>();
+            fence_operands();
+            fence_before();
+            if (!__syncthreads_and(ok)) break;
+            if (warp == 0 && tc::elect_one()) {
+                fence_after();
+                const uint32_t bm = mb + (b % S::STAGES) * S::M_BYTES;
+                for (int p = 0; p < a.parts; ++p)
+#pragma unroll
+                    for (int k = 0; k < RP / 16; ++k) {
+                        // 16 values along the rank: 32 bytes of a row, in the next block of 64 after four
+                        const uint32_t av = vb + p * S::V_BYTES + (k >> 2) * AD_ROWS * 128 + (k & 3) * 32;
+                        const uint64_t da = operand(av, 16, 8 * VT::ROW, VT::SWIZZLE);
+                        const uint64_t db = TRANS ? operand(bm + 16 * k * 128, RP * 128, 1024, SW128)
+                                                  : operand(bm + (k >> 2) * S::COLS * 128 + (k & 3) * 32, 16, 8 * MT::ROW, MT::SWIZZLE);
+                        tc::umma_f16(tmem + (b & 1) * S::COLS, da, db, how, p > 0 || k > 0);
+                    }
+                tc::umma_commit(bar + 8 * (b & 1));
+            }
+            __syncwarp();
+            if (b > 0) {
+                ok = ok && tc::mbar_wait(bar + 8 * (b - 1 & 1), (b - 1) >> 1 & 1, err, E_ADAPTERS);
+                __syncwarp();
+                if (ok && b + S::STAGES - 1 < n) copy(b + S::STAGES - 1);       // into the stage whose products are done
+            } else if (S::STAGES - 1 < n) {
+                copy(S::STAGES - 1);
+            }
+            copies_end();
+            if (b > 0 && ok) {
+                fence_after();
+                finish(b - 1);
+            }
+            y_fetch(b);
+        }
+        copies_wait<0>();
+        if (b == n) {
+            ok = ok && tc::mbar_wait(bar + 8 * (n - 1 & 1), (n - 1) >> 1 & 1, err, E_ADAPTERS);
+            __syncwarp();
+            fence_after();
+            if (ok) finish(n - 1);
+        } else {
+            if (warp == 0 && tc::elect_one()) tc::umma_commit(bar + 16);        // gave up: what was issued, before its memory goes
+            tc::mbar_wait(bar + 16, 0, err, E_ADAPTERS);
+        }
+    } else {
+        for (; b < n; ++b) {
+            y_fetch(b);
+            finish(b);
+        }
+    }
+    tensor_end<S::COLUMNS>(tmem);
+}
+
+// ---------------------------------------------------------------- outer
+
+constexpr int OUTER_COLS = 128;
+
+// The parts of v lie side by side as columns of one product; their sums are added when they are moved to registers.
+template <int RP, int PARTS> struct Outer {
+    static constexpr int N = RP * PARTS, X_BYTES = AD_STEP * OUTER_COLS * 2, V_BYTES = AD_STEP * 2 * RP, STAGE = X_BYTES + PARTS * V_BYTES;
+    static constexpr int STAGES = STAGE <= 24576 ? 4 : STAGE <= 32768 ? 3 : 4, SMEM = STAGES * STAGE + 1024, COLUMNS = columns_of(2 * N);
+    static constexpr int SUM = OUTER_COLS * (RP + 1) * 4;
+    static constexpr int VV = (AD_STEP * (RP / 8) * PARTS + AD_THREADS - 1) / AD_THREADS;
+    static_assert(N <= 256 && SUM <= SMEM, "one product's columns, and the sums in the stages' memory");
+};
+
+template <int RP, int PARTS>
+__global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const AdOuter a, const AdOrder o, int splits, uint32_t *err) {
+    using S = Outer<RP, PARTS>;
+    extern __shared__ unsigned char raw[];
+    __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
+    __shared__ uint32_t holder;
+    pdl_wait();
+    pdl_trigger();
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, adapter = blockIdx.y;
+    const int64_t cols0 = (int64_t)(blockIdx.x / (unsigned)splits) * OUTER_COLS;
+    const int64_t from = o.order != nullptr ? o.first[adapter + 1] : 0, to = o.order != nullptr ? o.end[adapter + 1] : adapter == 0 ? o.t : 0;
+    const int64_t steps = (to - from + AD_STEP - 1) / AD_STEP;
+    const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
+    const int n = (int)(s1 - s0), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t tmem = tensor_begin<S::STAGES + 3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
+    const uint32_t base = (tc::smem_u32(raw) + 1023u) & ~1023u;
+    using XT = Tile<OUTER_COLS>;
+    using VT = Tile<RP>;
+    const int64_t xc = cols0 + (tid & 15) * 8;
+    const __nv_bfloat16 *x0 = static_cast<const __nv_bfloat16 *>(a.x) + (xc < a.cols ? xc : 0);
+    auto copy = [&](int step) {
+        const uint32_t bx = base + (step % S::STAGES) * S::STAGE, bv = bx + S::X_BYTES;
+        const int64_t t0 = from + (s0 + step) * AD_STEP;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = tid / 16 + 16 * i;
+            const int64_t t = t0 + r;
+            const bool there = t < to && xc < a.cols;
+            copy16_if(bx + XT::at(r, tid & 15, AD_STEP), x0 + (there ? (o.order != nullptr ? (int64_t)o.order[t] : t) * a.ldx : 0), there);
+        }
+#pragma unroll
+        for (int i = 0; i < S::VV; ++i) {
+            const int v = tid + i * AD_THREADS, p = v / (AD_STEP * (RP / 8)), r = v / (RP / 8) % AD_STEP, q = v % (RP / 8);
+            if (v >= AD_STEP * (RP / 8) * PARTS) break;
+            const int64_t t = t0 + r;
+            const bool there = t < to;
+            copy16_if(bv + p * S::V_BYTES + VT::at(r, q, AD_STEP), static_cast<const uint4 *>(a.v) + (there ? (p * o.t + t) * (RP / 8) + q : 0), there);
+        }
+    };
+    float sum[RP / 2];
+#pragma unroll
+    for (int j = 0; j < RP / 2; ++j) sum[j] = 0.f;
+    bool ok = true;
+    int groups = 0;                               // whose sums are in registers
+    const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21) + (uint32_t)(warp >> 2) * (RP / 2);
+    auto collect = [&]() {
+        ok = ok && tc::mbar_wait(bar + 8 * (S::STAGES + (groups & 1)), (groups >> 1) & 1, err, E_ADAPTERS);
+        __syncwarp();
+        fence_after();
+#pragma unroll
+        for (int j = 0; j < RP / 2; j += 8) {
+            float all[8], v[8];
+            tmem_ld8(mine + (groups & 1) * S::N + (PARTS - 1) * RP + j, all);
+#pragma unroll
+            for (int p = PARTS - 2; p >= 0; --p) {                               // the least parts first
+                tmem_ld8(mine + (groups & 1) * S::N + p * RP + j, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) all[e] += v[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[j + e] += all[e];
+        }
+        fence_before();
+        ++groups;
+    };
+#pragma unroll
+    for (int i = 0; i < S::STAGES - 1; ++i) {
+        if (i < n) copy(i);
+        copies_end();
+    }
+    constexpr uint32_t how = product(true, true, true, OUTER_COLS, S::N);
+    int at = 0;
+    for (; at < n; ++at) {
+        copies_wait<S::STAGES - 2>();
+        fence_operands();
+        if (!__syncthreads_and(ok)) break;
+        if (warp == 0 && tc::elect_one()) {
+            fence_after();
+            const uint32_t bx = base + (at % S::STAGES) * S::STAGE, bv = bx + S::X_BYTES;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                tc::umma_f16(tmem + (at / FLUSH & 1) * S::N, operand(bx + 16 * k * 128, AD_STEP * 128, 1024, SW128),
+                             operand(bv + 16 * k * VT::ROW, AD_STEP * VT::ROW, 8 * VT::ROW, VT::SWIZZLE), how, at % FLUSH > 0 || k > 0);
+            tc::umma_commit(bar + 8 * (at % S::STAGES));
+            if (at % FLUSH == FLUSH - 1 || at == n - 1) tc::umma_commit(bar + 8 * (S::STAGES + (at / FLUSH & 1)));
+        }
+        __syncwarp();
+        if (at > 0 && at + S::STAGES - 1 < n)
+            ok = ok && tc::mbar_wait(bar + 8 * ((at - 1) % S::STAGES), (at - 1) / S::STAGES & 1, err, E_ADAPTERS);
+        if (ok && at + S::STAGES - 1 < n) copy(at + S::STAGES - 1);
+        copies_end();
+        if (at % FLUSH == 1 && at > FLUSH) collect();
+    }
+    copies_wait<0>();
+    if (at == n) {
+        while (groups < (n + FLUSH - 1) / FLUSH) collect();
+    } else if (warp == 0 && tc::elect_one()) {
+        tc::umma_commit(bar + 8 * (S::STAGES + 2));                              // gave up: what was issued, before its memory goes
+    }
+    if (at < n) tc::mbar_wait(bar + 8 * (S::STAGES + 2), 0, err, E_ADAPTERS);
+    tensor_end<S::COLUMNS>(tmem);
+
+    float *fs = reinterpret_cast<float *>(raw);
+    const int col = (warp & 3) * 32 + lane;
+#pragma unroll
+    for (int j = 0; j < RP / 2; ++j) fs[col * (RP + 1) + (warp >> 2) * (RP / 2) + j] = sum[j];
+    if (splits > 1) tc::cluster_sync();
+    else __syncthreads();
+    const uint32_t peer = tc::smem_u32(raw);
+    const int c0 = OUTER_COLS * rank / splits, c1 = OUTER_COLS * (rank + 1) / splits, wide = c1 - c0;
+    const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
+    for (int v = tid; v < wide * a.rank; v += AD_THREADS) {
+        const int c = c0 + (a.by_cols ? v / a.rank : v % wide), j = a.by_cols ? v % a.rank : v / wide;
+        if (cols0 + c >= a.cols) continue;
+        const int f = c * (RP + 1) + j;
+        float x = 0.f;
+        for (int q = 0; q < splits; ++q) x += splits > 1 ? ld_peer_f32(peer + f * 4, q) : fs[f];
+        const int64_t to_at = g0 + (a.by_cols ? (cols0 + c) * a.rank + j : j * a.cols + cols0 + c);
+        if (a.g_dtype == CT_DT_F32) static_cast<float *>(a.g)[to_at] = x;
+        else static_cast<__nv_bfloat16 *>(a.g)[to_at] = __float2bfloat16_rn(x);
+    }
+    if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
+}
+
+// ---------------------------------------------------------------- host
+
+template <typename T, int RP, bool TRANS> cudaError_t shrink(const AdShrink &a, const AdOrder &o, int tiles, int splits, uint32_t *err, cudaStream_t st) {
+    using S = Shrink<RP>;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = shrink_tc_kernel<T, RP, TRANS>;
+    const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
+    if (e != cudaSuccess) return e;
+    if (splits == 1) return pdl_launch(kernel, dim3((unsigned)tiles), dim3(AD_THREADS), S::SMEM, st, a, o, splits, err);
+    return pdl_launch_cluster(kernel, dim3((unsigned)(tiles * splits)), dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits, err);
+}
+template <typename T, bool TRANS> cudaError_t shrink_rank(const AdShrink &a, const AdOrder &o, int tiles, int splits, uint32_t *err, cudaStream_t st) {
+    switch (ad_padded(a.rank)) {
+        case 16: return shrink<T, 16, TRANS>(a, o, tiles, splits, err, st);
+        case 32: return shrink<T, 32, TRANS>(a, o, tiles, splits, err, st);
+        case 64: return shrink<T, 64, TRANS>(a, o, tiles, splits, err, st);
+        default: return shrink<T, 128, TRANS>(a, o, tiles, splits, err, st);
+    }
+}
+
+template <int RP, bool TRANS, int YS> cudaError_t expand(const AdExpand &q, const AdOrder &o, int tiles, uint32_t *err, cudaStream_t st) {
+    using S = Expand<RP, YS>;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = expand_tc_kernel<RP, TRANS, YS>;
+    const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3));
+    if (e != cudaSuccess) return e;
+    // columns of a CTA: as many as leave each SM four of them, at most 16 blocks
+    AdExpand a = q;
+    const int64_t blocks = (a.cols + S::COLS - 1) / S::COLS;
+    int64_t parts = (4 * (int64_t)sm_count() + tiles - 1) / tiles;
+    if (parts < (blocks + 15) / 16) parts = (blocks + 15) / 16;
+    if (parts > blocks) parts = blocks;
+    if (parts > 65535) parts = 65535;
+    a.per = (blocks + parts - 1) / parts * S::COLS;
+    const dim3 grid((unsigned)tiles, (unsigned)((a.cols + a.per - 1) / a.per));
+    return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, a, o, err);
+}
+template <bool TRANS, int YS> cudaError_t expand_rank(const AdExpand &a, const AdOrder &o, int tiles, uint32_t *err, cudaStream_t st) {
+    switch (ad_padded(a.rank)) {
+        case 16: return expand<16, TRANS, YS>(a, o, tiles, err, st);
+        case 32: return expand<32, TRANS, YS>(a, o, tiles, err, st);
+        case 64: return expand<64, TRANS, YS>(a, o, tiles, err, st);
+        default: return expand<128, TRANS, YS>(a, o, tiles, err, st);
+    }
+}
+
+template <int RP, int PARTS> cudaError_t outer(const AdOuter &a, const AdOrder &o, int splits, uint32_t *err, cudaStream_t st) {
+    using S = Outer<RP, PARTS>;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = outer_tc_kernel<RP, PARTS>;
+    const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)((a.cols + OUTER_COLS - 1) / OUTER_COLS * splits), (unsigned)o.adapters);
+    if (splits == 1) return pdl_launch(kernel, grid, dim3(AD_THREADS), S::SMEM, st, a, o, splits, err);
+    return pdl_launch_cluster(kernel, grid, dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits, err);
+}
+}  // namespace
+
+cudaError_t ad_shrink_tc(const AdShrink &a, bool bf16, bool trans, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+    uint32_t *err = device_error_word();
+    if (err == nullptr) return cudaErrorUnknown;
+    if (bf16) return trans ? shrink_rank<__nv_bfloat16, true>(a, o, tiles, splits, err, st) : shrink_rank<__nv_bfloat16, false>(a, o, tiles, splits, err, st);
+    return trans ? shrink_rank<__half, true>(a, o, tiles, splits, err, st) : shrink_rank<__half, false>(a, o, tiles, splits, err, st);
+}
+cudaError_t ad_expand_tc(const AdExpand &a, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
+    uint32_t *err = device_error_word();
+    if (err == nullptr) return cudaErrorUnknown;
+    if (a.y_dtype == CT_DT_F32) return trans ? expand_rank<true, 4>(a, o, tiles, err, st) : expand_rank<false, 4>(a, o, tiles, err, st);
+    return trans ? expand_rank<true, 2>(a, o, tiles, err, st) : expand_rank<false, 2>(a, o, tiles, err, st);
+}
+bool ad_outer_tc_takes(int64_t rank, int parts) { return ad_padded(rank) * parts <= 256; }
+cudaError_t ad_outer_tc(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st) {
+    uint32_t *err = device_error_word();
+    if (err == nullptr) return cudaErrorUnknown;
+    switch (ad_padded(a.rank)) {
+        case 16: return a.parts == 2 ? outer<16, 2>(a, o, splits, err, st) : outer<16, 3>(a, o, splits, err, st);
+        case 32: return a.parts == 2 ? outer<32, 2>(a, o, splits, err, st) : outer<32, 3>(a, o, splits, err, st);
+        case 64: return a.parts == 2 ? outer<64, 2>(a, o, splits, err, st) : outer<64, 3>(a, o, splits, err, st);
+        default: return outer<128, 2>(a, o, splits, err, st);
+    }
+}
+
+}  // namespace ops
+}  // namespace ct

@@ -451,7 +451,7 @@ inline int64_t rows_of(int64_t sequences, int64_t drafts) { return 2 * drafts + 
 // pieces leave less to join.
 inline int64_t per_of(int64_t rows, int64_t vocab) {
     int64_t per = 2048;
-    while (per < 16384 && rows * ((vocab + per - 1) / per) > 32 * 152) per *= 2;
+    while (per < 8192 && rows * ((vocab + per - 1) / per) > 32 * 152) per *= 2;
     return per;
 }
 inline int64_t pieces_of(int64_t rows, int64_t vocab) {

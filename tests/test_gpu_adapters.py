@@ -14,6 +14,8 @@ PAIRS = [("float32", "float32"), ("float16", "float16"), ("bfloat16", "bfloat16"
 # rows, k, n, rank, adapters
 SIZES = [(1, 16, 10, 1, 1), (1, 4096, 512, 16, 8), (3, 257, 129, 5, 4), (17, 64, 64, 8, 17), (33, 1000, 31, 20, 3), (64, 128, 256, 16, 64),
          (130, 72, 264, 64, 1), (200, 520, 1000, 128, 2), (257, 320, 96, 33, 5), (700, 136, 200, 32, 3), (1500, 48, 40, 4, 2)]
+# rows that can be copied as they lie, the long axes shared by several CTAs
+WHOLE = [(300, 4104, 72, 16, 1), (400, 1032, 136, 8, 3), (129, 8, 2056, 24, 2), (3000, 136, 264, 64, 2), (150, 2120, 648, 128, 1), (2000, 520, 24, 40, 300)]
 
 
 def np64(t):
@@ -97,6 +99,22 @@ def test_gradients(size, xt, wt):
         assert (into[ids == -1] == dx[ids == -1]).all()
         alone = ct().ct_adapters_grad(dy, x, a, b, ids, scale, grad_dtype=torch.float32 if gt == "float32" else None)
         assert alone[0] is None and (alone[1] == got[1]).all() and (alone[2] == got[2]).all()
+
+
+@pytest.mark.parametrize("wt", ["bfloat16", "float16"])
+@pytest.mark.parametrize("size", WHOLE)
+def test_whole_rows(size, wt):
+    import torch
+    t, k, n, rank, count = size
+    x, a, b, ids, scale = made(t, k, n, rank, count, wt, wt, seed=6)
+    for dt in (wt, "float32"):
+        y, dx = like(t, n, dt, 1), like(t, k, dt, 4)
+        for relu in (False, True):
+            check(y, x, a, b, ids, scale, relu, ct().ct_adapters(y.clone(), x, a, b, ids, scale, relu=relu))
+        dy = like(t, n, wt, 3)
+        got = ct().ct_adapters_grad(dy, x, a, b, ids, scale, dx=dx.clone(), grad_dtype=getattr(torch, dt))
+        check_grad(dy, x, a, b, ids, scale, dx, got)
+    assert ct().ct_ops_device_error() == 0
 
 
 def test_gradients_agree_with_differences():
