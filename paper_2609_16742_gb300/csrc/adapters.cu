@@ -32,8 +32,7 @@ struct OrderArgs {
     int32_t *n_tiles;
 };
 
-__device__ __forceinline__ int key_of(const OrderArgs &a, int64_t t) {
-    const int64_t i = a.ids[t];
+__device__ __forceinline__ int key_of(const OrderArgs &a, int64_t i) {
     return i == -1 ? 0 : i >= 0 && i < a.adapters ? (int)i + 1 : a.adapters + 1;
 }
 
@@ -63,29 +62,50 @@ __device__ __forceinline__ int block_sum(int v, int *warps, int &total) {
     return s - v + (warp > 0 ? warps[warp - 1] : 0);
 }
 
+// f(key, row, have) for a run of rows, 32 at a time in their order; the ids of eight such groups are on their way together
+template <typename F> __device__ __forceinline__ void each_row(const OrderArgs &a, const int32_t *from, int64_t r0, int64_t r1, F f) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t p = r0; p < r1; p += 256) {
+        int32_t row[8];
+        int64_t id[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t at = min(p + 32 * i + lane, r1 - 1);
+            row[i] = from != nullptr ? from[at] : (int32_t)at;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) id[i] = a.ids[row[i]];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (p + 32 * i >= r1) break;
+            f(key_of(a, id[i]), row[i], p + 32 * i + lane < r1);
+        }
+    }
+}
+
 __global__ void __launch_bounds__(ORDER_THREADS) order_kernel(const OrderArgs a) {
     __shared__ int count[ORDER_WARPS][BINS];
     __shared__ int sums[32];
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, keys = a.adapters + 2;
-    for (int k = tid; k < keys; k += ORDER_THREADS) a.first[k] = a.end[k] = 0;
     // each warp has a run of the rows; a digit's rows keep their order within and between the runs
     const int64_t run = (a.t + 32 * ORDER_WARPS - 1) / (32 * ORDER_WARPS) * 32;
     const int64_t r0 = min(warp * run, a.t), r1 = min(r0 + run, a.t);
     const int passes = keys <= BINS ? 1 : 2;
+    if (passes == 2)
+        for (int k = tid; k < keys; k += ORDER_THREADS) a.first[k] = a.end[k] = 0;
     for (int pass = 0; pass < passes; ++pass) {
         const int32_t *from = pass == 0 ? nullptr : a.spare;
         int32_t *to = pass + 1 == passes ? a.order : a.spare;
         for (int b = lane; b < BINS; b += 32) count[warp][b] = 0;
         __syncwarp();
-        for (int64_t p = r0; p < r1; p += 32) {
-            const bool have = p + lane < r1;
-            const int d = have ? key_of(a, from != nullptr ? from[p + lane] : p + lane) >> (8 * pass) & (BINS - 1) : BINS;
+        each_row(a, from, r0, r1, [&](int key, int32_t, bool have) {
+            const int d = have ? key >> (8 * pass) & (BINS - 1) : BINS;
             const uint32_t same = __match_any_sync(0xffffffffu, d);
             if (have && lane == __ffs(same) - 1) count[warp][d] += __popc(same);
             __syncwarp();
-        }
+        });
         __syncthreads();
         // where each warp's rows of each digit go: thread i has digit i / 4, warps 8 (i % 4) to + 7
         int mine[8], s = 0, total;
@@ -95,30 +115,36 @@ __global__ void __launch_bounds__(ORDER_THREADS) order_kernel(const OrderArgs a)
             s += mine[w];
         }
         s = block_sum(s, sums, total);
+        if (passes == 1) {
+            // one digit is the whole key: its run of the slots
+            if (tid % 4 == 0 && tid / 4 < keys) a.first[tid / 4] = s;
+            if (tid % 4 == 0 && tid > 0 && tid / 4 <= keys) a.end[tid / 4 - 1] = s;
+            if (keys == BINS && tid == 0) a.end[keys - 1] = total;
+        }
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             count[tid % 4 * 8 + w][tid / 4] = s;
             s += mine[w];
         }
         __syncthreads();
-        for (int64_t p = r0; p < r1; p += 32) {
-            const bool have = p + lane < r1;
-            const int64_t row = have ? (from != nullptr ? from[p + lane] : p + lane) : 0;
-            const int d = have ? key_of(a, row) >> (8 * pass) & (BINS - 1) : BINS;
+        each_row(a, from, r0, r1, [&](int key, int32_t row, bool have) {
+            const int d = have ? key >> (8 * pass) & (BINS - 1) : BINS;
             const uint32_t same = __match_any_sync(0xffffffffu, d);
-            if (have) to[count[warp][d] + __popc(same & ((1u << lane) - 1u))] = (int32_t)row;
+            if (have) to[count[warp][d] + __popc(same & ((1u << lane) - 1u))] = row;
             __syncwarp();
             if (have && lane == __ffs(same) - 1) count[warp][d] += __popc(same);
             __syncwarp();
+        });
+        __syncthreads();
+    }
+    if (passes == 2) {
+        for (int64_t p = tid; p < a.t; p += ORDER_THREADS) {
+            const int k = key_of(a, a.ids[a.order[p]]);
+            if (p == 0 || key_of(a, a.ids[a.order[p - 1]]) != k) a.first[k] = (int32_t)p;
+            if (p + 1 == a.t || key_of(a, a.ids[a.order[p + 1]]) != k) a.end[k] = (int32_t)p + 1;
         }
         __syncthreads();
     }
-    for (int64_t p = tid; p < a.t; p += ORDER_THREADS) {
-        const int k = key_of(a, a.order[p]);
-        if (p == 0 || key_of(a, a.order[p - 1]) != k) a.first[k] = (int32_t)p;
-        if (p + 1 == a.t || key_of(a, a.order[p + 1]) != k) a.end[k] = (int32_t)p + 1;
-    }
-    __syncthreads();
     // tiles: each thread has a run of the keys
     const int per = (keys + ORDER_THREADS - 1) / ORDER_THREADS, k0 = min(tid * per, keys), k1 = min(k0 + per, keys);
     int n = 0, total;
@@ -183,15 +209,92 @@ __device__ __forceinline__ int speak_for(const int64_t *ids, int t, int lead, in
     return before ? 0 : found;
 }
 
+// Eight values on their way; WHOLE: rows start on 16 bytes and are a multiple of 8 values long.
+template <typename T, bool WHOLE> struct Way {
+    Eight<T> e;
+    __device__ __forceinline__ void go(const T *p, int left) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.u[i] = ldg_if(reinterpret_cast<const uint4 *>(p) + i, left > 0);
+    }
+    __device__ __forceinline__ void take(const T *, int, float (&v)[8]) const {
+        unpack16<T>(e.u[0], v);
+        if constexpr (sizeof(T) == 4) unpack16<T>(e.u[1], v + 4);
+    }
+};
+template <typename T> struct Way<T, false> {
+    Units<T> u;
+    __device__ __forceinline__ void go(const T *p, int left) { u = load_units(p, left); }
+    __device__ __forceinline__ void take(const T *p, int left, float (&v)[8]) const {
+        const Eight<T> e = take_eight(u, p, left);
+        unpack16<T>(e.u[0], v);
+        if constexpr (sizeof(T) == 4) unpack16<T>(e.u[1], v + 4);
+    }
+};
+
+// Sums of FEW_J rows of A (from j0 on) by R rows of x over every ways-th piece of 256 values, a warp's; into part.
+template <typename TX, typename TM, bool WHOLE, int R>
+__device__ __forceinline__ void few_dot(const FewArgs &a, const TM *m, const int16_t *rows, int have, int j0, int64_t p0, int64_t p1, int ways,
+                                        float (&part)[FEW_J][FEW_R]) {
+    constexpr int U = R == 1 ? 4 : 1;             // pieces whose loads are on their way together
+    const int lane = threadIdx.x & 31;
+    const TX *xr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) xr[r] = static_cast<const TX *>(a.x) + (r < have ? rows[r] * a.ldx : 0);
+    float acc[FEW_J][R];
+#pragma unroll
+    for (int j = 0; j < FEW_J; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[j][r] = 0.f;
+    for (int64_t p = p0; p < p1; p += (int64_t)U * ways) {
+        Way<TM, WHOLE> wm[U][FEW_J];
+        Way<TX, WHOLE> wx[U][R];
+        int left[U];
+        int64_t c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            c[u] = (p + (int64_t)u * ways) * 256 + lane * 8;
+            left[u] = p + (int64_t)u * ways < p1 ? left_of(c[u], a.k) : 0;
+            if (left[u] == 0) c[u] = 0;
+#pragma unroll
+            for (int j = 0; j < FEW_J; ++j) wm[u][j].go(m + (j0 + j < a.rank ? (j0 + j) * a.a_row + c[u] : 0), j0 + j < a.rank ? left[u] : 0);
+#pragma unroll
+            for (int r = 0; r < R; ++r) wx[u][r].go(xr[r] + c[u], r < have ? left[u] : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float fx[R][8];
+#pragma unroll
+            for (int r = 0; r < R; ++r) wx[u][r].take(xr[r] + c[u], r < have ? left[u] : 0, fx[r]);
+#pragma unroll
+            for (int j = 0; j < FEW_J; ++j) {
+                float fm[8];
+                wm[u][j].take(m + (j0 + j < a.rank ? (j0 + j) * a.a_row + c[u] : 0), j0 + j < a.rank ? left[u] : 0, fm);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[j][r] = fmaf(fm[e], fx[r][e], acc[j][r]);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < FEW_J; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) acc[j][r] += __shfl_xor_sync(0xffffffffu, acc[j][r], s);
+            if (lane == 0) part[j][r] = acc[j][r];
+        }
+}
+
 // v = scale A x.  A cluster for each row that may speak, its CTAs share the long axis; warps share the rows of A, and the axis again
 // where those are few.
-template <typename TX, typename TM> __global__ void __launch_bounds__(FEW_THREADS) few_shrink_kernel(const FewArgs a, int splits) {
+template <typename TX, typename TM, bool WHOLE> __global__ void __launch_bounds__(FEW_THREADS) few_shrink_kernel(const FewArgs a, int splits) {
     __shared__ int16_t rows[FEW];
     __shared__ float part[FEW_WARPS][FEW_J][FEW_R];
-    __shared__ float sums[CT_MAX_RANK][FEW_R + 1];
+    __shared__ float sums[CT_MAX_RANK][FEW_R];
     pdl_wait();
     pdl_trigger();
-    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, tid = threadIdx.x, warp = tid >> 5;
     int64_t id;
     const int n = speak_for(a.ids, a.t, (int)(blockIdx.x / (unsigned)splits), rows, id);
     if (n == 0 || id < 0 || id >= a.adapters) return;                            // the whole cluster alike
@@ -203,62 +306,10 @@ template <typename TX, typename TM> __global__ void __launch_bounds__(FEW_THREAD
     for (int r0 = 0; r0 < n; r0 += FEW_R) {
         for (int g0 = 0; g0 < groups; g0 += FEW_WARPS / ways) {
             const int g = g0 + warp / ways, way = warp % ways;
-            float acc[FEW_J][FEW_R];
-#pragma unroll
-            for (int j = 0; j < FEW_J; ++j)
-#pragma unroll
-                for (int r = 0; r < FEW_R; ++r) acc[j][r] = 0.f;
             if (g < groups) {
-#pragma unroll 2
-                for (int64_t p = p0 + way; p < p1; p += ways) {
-                    const int64_t c = p * 256 + lane * 8;
-                    const int left = left_of(c, a.k);
-                    const TM *mp[FEW_J];
-                    const TX *xp[FEW_R];
-                    Units<TM> um[FEW_J];
-                    Units<TX> ux[FEW_R];
-#pragma unroll
-                    for (int j = 0; j < FEW_J; ++j) {
-                        const bool there = left > 0 && g * FEW_J + j < a.rank;
-                        mp[j] = m + (there ? (g * FEW_J + j) * a.a_row + c : 0);
-                        um[j] = load_units(mp[j], there ? left : 0);
-                    }
-#pragma unroll
-                    for (int r = 0; r < FEW_R; ++r) {
-                        const bool there = left > 0 && r0 + r < n;
-                        xp[r] = static_cast<const TX *>(a.x) + (there ? rows[r0 + r] * a.ldx + c : 0);
-                        ux[r] = load_units(xp[r], there ? left : 0);
-                    }
-                    float fm[FEW_J][8];
-#pragma unroll
-                    for (int j = 0; j < FEW_J; ++j) {
-                        const Eight<TM> e = take_eight(um[j], mp[j], left);
-                        unpack16<TM>(e.u[0], fm[j]);
-                        if constexpr (sizeof(TM) == 4) unpack16<TM>(e.u[1], fm[j] + 4);
-                    }
-#pragma unroll
-                    for (int r = 0; r < FEW_R; ++r) {
-                        if (r0 + r >= n) break;
-                        float fx[8];
-                        const Eight<TX> e = take_eight(ux[r], xp[r], left);
-                        unpack16<TX>(e.u[0], fx);
-                        if constexpr (sizeof(TX) == 4) unpack16<TX>(e.u[1], fx + 4);
-#pragma unroll
-                        for (int j = 0; j < FEW_J; ++j)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) acc[j][r] = fmaf(fm[j][e], fx[e], acc[j][r]);
-                    }
-                }
+                if (n - r0 == 1) few_dot<TX, TM, WHOLE, 1>(a, m, rows + r0, 1, g * FEW_J, p0 + way, p1, ways, part[warp]);
+                else few_dot<TX, TM, WHOLE, FEW_R>(a, m, rows + r0, n - r0, g * FEW_J, p0 + way, p1, ways, part[warp]);
             }
-#pragma unroll
-            for (int j = 0; j < FEW_J; ++j)
-#pragma unroll
-                for (int r = 0; r < FEW_R; ++r) {
-                    if (r0 + r >= n) break;
-#pragma unroll
-                    for (int s = 16; s > 0; s >>= 1) acc[j][r] += __shfl_xor_sync(0xffffffffu, acc[j][r], s);
-                    if (lane == 0) part[warp][j][r] = acc[j][r];
-                }
             __syncthreads();
             // the warps that shared the axis, in their order
             for (int i = tid; i < FEW_WARPS / ways * FEW_J * FEW_R; i += FEW_THREADS) {
@@ -271,14 +322,21 @@ template <typename TX, typename TM> __global__ void __launch_bounds__(FEW_THREAD
             __syncthreads();
         }
         if (splits > 1) tc::cluster_sync();
-        if (rank == 0)
-            for (int i = tid; i < a.rank * FEW_R; i += FEW_THREADS) {
-                const int j = i / FEW_R, r = i % FEW_R;
-                if (r0 + r >= n) continue;
-                float s = 0.f;
-                for (int q = 0; q < splits; ++q) s += splits > 1 ? ld_peer_f32(tc::smem_u32(&sums[j][r]), q) : sums[j][r];
-                a.v[rows[r0 + r] * a.rank + j] = s * scale;
+        // the CTAs of the cluster share the sums
+        for (int i = tid + FEW_THREADS * rank; i < a.rank * FEW_R; i += FEW_THREADS * splits) {
+            const int j = i / FEW_R, r = i % FEW_R;
+            if (r0 + r >= n) continue;
+            float s = sums[j][r];
+            if (splits > 1) {
+                float p[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) p[q] = q < splits ? ld_peer_f32(tc::smem_u32(&sums[j][r]), q) : 0.f;
+                s = p[0];
+#pragma unroll
+                for (int q = 1; q < 8; ++q) s += p[q];
             }
+            a.v[rows[r0 + r] * a.rank + j] = s * scale;
+        }
         if (splits > 1) tc::cluster_sync();       // the sums have been read
         else __syncthreads();
     }
@@ -365,20 +423,26 @@ template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_ke
     }
 }
 
-template <typename TX, typename TM> cudaError_t few(const FewArgs &a, cudaStream_t st) {
+template <typename TX, typename TM, bool WHOLE> cudaError_t few_as(const FewArgs &a, cudaStream_t st) {
     if (a.rank > 0) {
-        // four blocks for each SM, with two pieces of the axis at least for each warp that shares it
+        // as many blocks as are resident together (three for each SM), with a piece of the axis at least for each warp that shares it
         const int64_t pieces = (a.k + 255) / 256;
         const int lead = a.ids != nullptr ? a.t : 1, speak = lead < a.adapters ? lead : a.adapters;
-        int splits = 1;
-        while (splits < 8 && speak * splits < 4 * sm_count() && pieces >= 4 * splits) splits *= 2;
-        const cudaError_t e = splits > 1 ? pdl_launch_cluster(few_shrink_kernel<TX, TM>, dim3((unsigned)(lead * splits)), dim3(FEW_THREADS), 0,
-                                                              st, splits, a, splits)
-                                         : pdl_launch(few_shrink_kernel<TX, TM>, dim3((unsigned)lead), dim3(FEW_THREADS), 0, st, a, splits);
+        const int groups = (a.rank + FEW_J - 1) / FEW_J, ways = groups >= FEW_WARPS ? 1 : FEW_WARPS / groups;
+        int splits = 3 * sm_count() / speak;
+        if (splits > 8) splits = 8;
+        if (splits > pieces / ways) splits = (int)(pieces / ways);
+        if (splits < 1) splits = 1;
+        const cudaError_t e = splits > 1 ? pdl_launch_cluster(few_shrink_kernel<TX, TM, WHOLE>, dim3((unsigned)(lead * splits)),
+                                                              dim3(FEW_THREADS), 0, st, splits, a, splits)
+                                         : pdl_launch(few_shrink_kernel<TX, TM, WHOLE>, dim3((unsigned)lead), dim3(FEW_THREADS), 0, st, a, splits);
         if (e != cudaSuccess) return e;
     }
     const dim3 grid((unsigned)(a.ids != nullptr ? a.t : 1), (unsigned)((a.n + FEW_COLS - 1) / FEW_COLS));
     return pdl_launch(few_expand_kernel<TM>, grid, dim3(FEW_COLS), 0, st, a);
+}
+template <typename TX, typename TM> cudaError_t few(const FewArgs &a, bool whole, cudaStream_t st) {
+    return whole ? few_as<TX, TM, true>(a, st) : few_as<TX, TM, false>(a, st);
 }
 
 // ---------------------------------------------------------------- host
@@ -481,18 +545,18 @@ extern "C" ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, cons
     if (workspace_bytes < s.total) return CT_ENOMEM;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *w = static_cast<char *>(workspace_dev);
+    const bool xw = whole(x_dev, ldx, t, k, xs), aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, k, es),
+               bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, rank, es), yw = whole(y_dev, ldy, t, n, ys);
     cudaError_t e;
     // few rows, and adapters enough that hardly 16 rows have the same one
     if (t <= FEW && t <= 16 * adapters) {
         const FewArgs f = {x_dev, ldx, a_dev, a_adapter, a_row, b_dev, b_adapter, b_row, ids_dev, scale_dev, (int)t, (int)adapters, (int)rank, k,
                            n, reinterpret_cast<float *>(w + s.v), y_dev, y_dtype, ldy, relu != 0};
-        if (dtype == CT_DT_F32) e = few<float, float>(f, st);
-        else if (dtype == CT_DT_F16) e = x_dtype == CT_DT_F32 ? few<float, __half>(f, st) : few<__half, __half>(f, st);
-        else e = x_dtype == CT_DT_F32 ? few<float, __nv_bfloat16>(f, st) : few<__nv_bfloat16, __nv_bfloat16>(f, st);
+        if (dtype == CT_DT_F32) e = few<float, float>(f, xw && aw, st);
+        else if (dtype == CT_DT_F16) e = x_dtype == CT_DT_F32 ? few<float, __half>(f, xw && aw, st) : few<__half, __half>(f, xw && aw, st);
+        else e = x_dtype == CT_DT_F32 ? few<float, __nv_bfloat16>(f, xw && aw, st) : few<__nv_bfloat16, __nv_bfloat16>(f, xw && aw, st);
         return e == cudaSuccess ? CT_OK : CT_ECUDA;
     }
-    const bool xw = whole(x_dev, ldx, t, k, xs), aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, k, es),
-               bw = stack_whole(b_dev, b_adapter, b_row, adapters, n, rank, es), yw = whole(y_dev, ldy, t, n, ys);
     AdOrder o;
     e = make_order(o, ids_dev, t, adapters, s, w, st);
     const int tiles = (int)tiles_of(t, adapters, ids_dev != nullptr), parts = y_dtype == CT_DT_F32 ? 3 : 2;

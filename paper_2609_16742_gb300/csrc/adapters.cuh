@@ -35,6 +35,40 @@ struct AdOrder {
     int adapters;
 };
 
+// One product with a matrix of the adapters.  `whole`: bit 0: x's (y's) rows start on 16 bytes and are a multiple of 8 values long, bit 1:
+// the matrix's.
+struct AdShrink {
+    const void *x;
+    int64_t ldx, cols;
+    const void *m;
+    int64_t m_adapter, m_row;
+    const float *scale;
+    int rank, whole;
+    void *v;                                      // BF16 [parts][t][padded rank], by slots
+    int parts;
+};
+struct AdExpand {
+    void *y;
+    int32_t y_dtype;
+    int64_t ldy, cols;
+    const void *m;
+    int64_t m_adapter, m_row;
+    int rank, whole, relu;
+    const void *v;
+    int parts;
+    int64_t per;                                  // columns of a block
+};
+struct AdOuter {
+    const void *x;
+    int64_t ldx, cols;
+    const void *v;
+    int parts;
+    int rank, whole;
+    void *g;                                      // [adapters][rank][cols], or [adapters][cols][rank] where by_cols
+    int32_t g_dtype;
+    int by_cols;
+};
+
 #ifdef __CUDACC__
 struct AdRows {
     int64_t slot0;
@@ -125,6 +159,10 @@ __device__ __forceinline__ void copy16_if(uint32_t to, const void *from, bool wa
     const int bytes = wanted ? 16 : 0;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void copy4_if(uint32_t to, const void *from, bool wanted) {
+    const int bytes = wanted ? 4 : 0;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -183,46 +221,93 @@ template <bool F16> __device__ __forceinline__ void mma16(float (&d)[4], const u
 // Row pitch in bytes of a tile of `width` 16-bit values: 16 more than the values, so that eight rows of a matrix lie in different banks.
 __host__ __device__ constexpr int ad_pitch(int width) { return 2 * width + 16; }
 
+// four neighbouring sums of all CTAs of a cluster (up to 8), added in rank order; the loads are on their way together
+__device__ __forceinline__ void sum_peers(uint32_t addr, int splits, float (&v)[4]) {
+    float p[8][4];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const uint32_t at = tc::mapa_shared(addr, (uint32_t)(c < splits ? c : 0));
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %5, 0;\n\t"
+            "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+            "@p ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n\t}"
+            : "=&f"(p[c][0]), "=&f"(p[c][1]), "=&f"(p[c][2]), "=&f"(p[c][3])
+            : "r"(at), "r"((int)(c < splits))
+            : "memory");
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = p[0][e];
+#pragma unroll
+        for (int c = 1; c < 8; ++c) v[e] += p[c][e];
+    }
+}
 __device__ __forceinline__ float ld_peer_f32(uint32_t addr, int rank) {
     float v;
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_shared(addr, (uint32_t)rank)) : "memory");
     return v;
 }
-#endif
+// A tile's sums in shared memory: rows of `width` and four more, so that eight rows' 16 bytes lie in different banks.
+__host__ __device__ constexpr int sums_pitch(int width) { return width + 4; }
 
-// One product with a matrix of the adapters.  `whole`: bit 0: x's (y's) rows start on 16 bytes and are a multiple of 8 values long, bit 1:
-// the matrix's.
-struct AdShrink {
-    const void *x;
-    int64_t ldx, cols;
-    const void *m;
-    int64_t m_adapter, m_row;
-    const float *scale;
-    int rank, whole;
-    void *v;                                      // BF16 [parts][t][padded rank], by slots
-    int parts;
-};
-struct AdExpand {
-    void *y;
-    int32_t y_dtype;
-    int64_t ldy, cols;
-    const void *m;
-    int64_t m_adapter, m_row;
-    int rank, whole, relu;
-    const void *v;
-    int parts;
-    int64_t per;                                  // columns of a block
-};
-struct AdOuter {
-    const void *x;
-    int64_t ldx, cols;
-    const void *v;
-    int parts;
-    int rank, whole;
-    void *g;                                      // [adapters][rank][cols], or [adapters][cols][rank] where by_cols
-    int32_t g_dtype;
-    int by_cols;
-};
+// v of a tile: the cluster's sums (fs, at `addr` in each CTA) times scale, 0 behind the rank, in BF16 parts
+template <int RP>
+__device__ __forceinline__ void write_vectors(const AdShrink &a, const AdOrder &o, const AdRows &tile, int adapter, const float *fs, int rank, int splits) {
+    const float scale = a.scale != nullptr ? a.scale[adapter] : 1.f;
+    const uint32_t addr = tc::smem_u32(fs);
+    const int r0 = AD_ROWS * rank / splits, r1 = AD_ROWS * (rank + 1) / splits;
+    for (int i = threadIdx.x; i < (r1 - r0) * (RP / 4); i += AD_THREADS) {
+        const int r = r0 + i / (RP / 4), j = i % (RP / 4) * 4;
+        if (r >= tile.rows) break;
+        float v[4];
+        if (splits > 1) {
+            sum_peers(addr + (r * sums_pitch(RP) + j) * 4, splits, v);
+        } else {
+            const float4 w = *reinterpret_cast<const float4 *>(fs + r * sums_pitch(RP) + j);
+            v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = j + e < a.rank ? v[e] * scale : 0.f;  // 0 and not 0 times what x holds
+        uint2 *out = static_cast<uint2 *>(a.v) + ((tile.slot0 + r) * RP + j) / 4;
+        for (int p = 0; p < a.parts; ++p) {
+            uint2 w;
+            w.x = split2(v[0], v[1]);
+            w.y = split2(v[2], v[3]);
+            out[p * (o.t * RP / 4)] = w;
+        }
+    }
+}
+
+__device__ __forceinline__ void put_as(void *p, int dtype, int64_t i, float v) {
+    if (dtype == CT_DT_F32) static_cast<float *>(p)[i] = v;
+    else if (dtype == CT_DT_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
+}
+// a gradient's 128 columns from cols0 on: the cluster's sums, each CTA its share of the columns
+template <int RP>
+__device__ __forceinline__ void write_gradient(const AdOuter &a, int adapter, int64_t cols0, const float *fs, int rank, int splits) {
+    constexpr int COLS = 128;
+    const uint32_t addr = tc::smem_u32(fs);
+    const int c0 = COLS * rank / splits, wide = COLS * (rank + 1) / splits - c0, fours = (a.rank + 3) / 4;
+    const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
+    for (int i = threadIdx.x; i < wide * fours; i += AD_THREADS) {
+        // neighbouring threads: neighbouring values of the gradient
+        const int c = c0 + (a.by_cols ? i / fours : i % wide), j = (a.by_cols ? i % fours : i / wide) * 4;
+        if (cols0 + c >= a.cols) continue;
+        float v[4];
+        if (splits > 1) {
+            sum_peers(addr + (c * sums_pitch(RP) + j) * 4, splits, v);
+        } else {
+            const float4 w = *reinterpret_cast<const float4 *>(fs + c * sums_pitch(RP) + j);
+            v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j + e < a.rank) put_as(a.g, a.g_dtype, g0 + (a.by_cols ? (cols0 + c) * a.rank + j + e : (j + e) * a.cols + cols0 + c), v[e]);
+    }
+}
+#endif
 
 inline int ad_padded(int64_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 

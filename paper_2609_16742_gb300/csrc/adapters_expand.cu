@@ -49,15 +49,24 @@ __device__ __forceinline__ void y_store(char *p, int dtype, const float *v) {
         *reinterpret_cast<uint4 *>(p) = dtype == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
     }
 }
-__device__ __forceinline__ float y_one(const char *p, int dtype) {
-    return dtype == CT_DT_F32   ? *reinterpret_cast<const float *>(p)
-           : dtype == CT_DT_F16 ? to_f32(*reinterpret_cast<const __half *>(p))
-                                : to_f32(*reinterpret_cast<const __nv_bfloat16 *>(p));
-}
 __device__ __forceinline__ void y_put(char *p, int dtype, float v) {
     if (dtype == CT_DT_F32) *reinterpret_cast<float *>(p) = v;
     else if (dtype == CT_DT_F16) *reinterpret_cast<__half *>(p) = __float2half_rn(v);
     else *reinterpret_cast<__nv_bfloat16 *>(p) = __float2bfloat16_rn(v);
+}
+
+// one value of y, or 0: no branch, so that many are on their way together
+__device__ __forceinline__ float y_one_if(const char *p, int dtype, bool wanted) {
+    uint32_t v;
+    if (dtype == CT_DT_F32) {
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.b32 %0, 0;\n\t@p ld.global.b32 %0, [%1];\n\t}"
+                     : "=&r"(v) : "l"(p), "r"((int)wanted) : "memory");
+        return __uint_as_float(v);
+    }
+    uint16_t h;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.b16 %0, 0;\n\t@p ld.global.b16 %0, [%1];\n\t}"
+                 : "=&h"(h) : "l"(p), "r"((int)wanted) : "memory");
+    return dtype == CT_DT_F16 ? __half2float(__ushort_as_half(h)) : __uint_as_float((uint32_t)h << 16);
 }
 
 template <typename TM, int RP, bool TRANS>
@@ -225,7 +234,8 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     const int32_t t = rows[wm * 32 + i * 8 + r];
-                    old[r] = t >= 0 && c < c_to ? y_one(static_cast<char *>(a.y) + ((int64_t)t * a.ldy + c) * ys, a.y_dtype) : 0.f;
+                    const bool there = t >= 0 && c < c_to;
+                    old[r] = y_one_if(static_cast<char *>(a.y) + (there ? ((int64_t)t * a.ldy + c) * ys : 0), a.y_dtype, there);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)

@@ -20,7 +20,7 @@ template <typename TX, int RP> struct Outer {
     static constexpr int X_BYTES = AD_STEP * LX, V_BYTES = AD_STEP * LV;
     static constexpr int XV = AD_STEP * (COLS / 8) / AD_THREADS;                  // 4
     static constexpr int V_VECS = AD_STEP * (RP / 8), VV = (V_VECS + AD_THREADS - 1) / AD_THREADS;
-    static constexpr int NT = RP / 16, SUM = COLS * (RP + 1) * 4;
+    static constexpr int NT = RP / 16, SUM = COLS * sums_pitch(RP) * 4;
     // The tensor cores cut off what they add: sums go from their accumulators into others after 128 rows, or after each 16 where
     // x's values are several parts.
     static constexpr bool EACH = PX > 1;
@@ -182,22 +182,10 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
         for (int j = 0; j < S::NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                fs[(wm * 32 + i * 16 + (e >> 1) * 8 + (lane >> 2)) * (RP + 1) + wn * (RP / 2) + j * 8 + (lane & 3) * 2 + (e & 1)] = sum[i][j][e];
+                fs[(wm * 32 + i * 16 + (e >> 1) * 8 + (lane >> 2)) * sums_pitch(RP) + wn * (RP / 2) + j * 8 + (lane & 3) * 2 + (e & 1)] = sum[i][j][e];
     if (splits > 1) tc::cluster_sync();
     else __syncthreads();
-    const int c0 = COLS * rank / splits, c1 = COLS * (rank + 1) / splits, wide = c1 - c0;
-    const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
-    for (int v = tid; v < wide * a.rank; v += AD_THREADS) {
-        const int c = c0 + (a.by_cols ? v / a.rank : v % wide), j = a.by_cols ? v % a.rank : v / wide;
-        if (cols0 + c >= a.cols) continue;
-        const int at = c * (RP + 1) + j;
-        float x = 0.f;
-        for (int q = 0; q < splits; ++q) x += splits > 1 ? ld_peer_f32(base + at * 4, q) : fs[at];
-        const int64_t to_at = g0 + (a.by_cols ? (cols0 + c) * a.rank + j : j * a.cols + cols0 + c);
-        if (a.g_dtype == CT_DT_F32) static_cast<float *>(a.g)[to_at] = x;
-        else if (a.g_dtype == CT_DT_F16) static_cast<__half *>(a.g)[to_at] = __float2half_rn(x);
-        else static_cast<__nv_bfloat16 *>(a.g)[to_at] = __float2bfloat16_rn(x);
-    }
+    write_gradient<RP>(a, adapter, cols0, fs, rank, splits);
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
@@ -223,10 +211,12 @@ template <typename TX> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, i
 }  // namespace
 
 cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st) {
-    // two CTAs for each SM, with two steps of an adapter's share of the rows at least for each
+    // as many CTAs as are resident together (two for each SM), with two steps of an adapter's share of the rows at least for each
     const int64_t blocks = (a.cols + COLS - 1) / COLS, steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP;
-    int splits = 1;
-    while (splits < 8 && blocks * o.adapters * splits < 2 * sm_count() && steps >= 4 * splits) splits *= 2;
+    const int64_t most = 2 * sm_count() / (blocks * o.adapters);
+    int splits = (int)(most < 8 ? most : 8);
+    if (splits > steps / 2) splits = (int)(steps / 2);
+    if (splits < 1) splits = 1;
     if (x_dtype == CT_DT_BF16 && (a.whole & 1) && ad_outer_tc_takes(a.rank, a.parts)) return ad_outer_tc(a, o, splits, st);
     return x_dtype == CT_DT_F32   ? by_rank<float>(a, o, splits, st)
            : x_dtype == CT_DT_F16 ? by_rank<__half>(a, o, splits, st)

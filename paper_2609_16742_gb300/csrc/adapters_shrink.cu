@@ -17,7 +17,7 @@ template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
     static constexpr int LX = ad_pitch(AD_STEP), LM = ad_pitch(TRANS ? RP : AD_STEP);
     static constexpr int X_BYTES = AD_ROWS * LX, M_ROWS = TRANS ? AD_STEP : RP, M_BYTES = M_ROWS * LM;
     static constexpr int BUF = PX * X_BYTES + PM * M_BYTES;
-    static constexpr int SUM = AD_ROWS * (RP + 1) * 4;
+    static constexpr int SUM = AD_ROWS * sums_pitch(RP) * 4;
     static constexpr int SMEM = 2 * BUF > SUM ? 2 * BUF : SUM;
     static constexpr int XV = AD_ROWS * 8 / AD_THREADS;                          // vectors of 8 values a thread loads
     static constexpr int M_VECS = M_ROWS * (TRANS ? RP / 8 : 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
@@ -198,25 +198,10 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
         for (int j = 0; j < S::NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                fs[(wm * 32 + i * 16 + (e >> 1) * 8 + (lane >> 2)) * (RP + 1) + wn * (RP / 2) + j * 8 + (lane & 3) * 2 + (e & 1)] = sum[i][j][e];
+                fs[(wm * 32 + i * 16 + (e >> 1) * 8 + (lane >> 2)) * sums_pitch(RP) + wn * (RP / 2) + j * 8 + (lane & 3) * 2 + (e & 1)] = sum[i][j][e];
     if (splits > 1) tc::cluster_sync();
     else __syncthreads();
-    const float scale = a.scale != nullptr ? a.scale[adapter] : 1.f;
-    const int r0 = AD_ROWS * rank / splits, r1 = AD_ROWS * (rank + 1) / splits;
-    for (int v = tid; v < (r1 - r0) * (RP / 2); v += AD_THREADS) {
-        const int r = r0 + v / (RP / 2), j = v % (RP / 2) * 2;
-        if (r >= tile.rows) break;
-        const int at = r * (RP + 1) + j;
-        float x = 0.f, y = 0.f;
-        for (int c = 0; c < splits; ++c) {
-            x += splits > 1 ? ld_peer_f32(base + at * 4, c) : fs[at];
-            y += splits > 1 ? ld_peer_f32(base + (at + 1) * 4, c) : fs[at + 1];
-        }
-        x = j < a.rank ? x * scale : 0.f;         // 0 and not 0 times what x holds
-        y = j + 1 < a.rank ? y * scale : 0.f;
-        uint32_t *out = static_cast<uint32_t *>(a.v) + ((tile.slot0 + r) * RP + j) / 2;
-        for (int p = 0; p < a.parts; ++p) out[p * (o.t * RP / 2)] = split2(x, y);
-    }
+    write_vectors<RP>(a, o, tile, adapter, fs, rank, splits);
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
@@ -249,10 +234,11 @@ template <bool TRANS> cudaError_t by_type(const AdShrink &a, int x_dtype, int dt
 }  // namespace
 
 cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
-    // two CTAs for each SM, with four steps at least for each
-    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
-    int splits = 1;
-    while (splits < 8 && (int64_t)tiles * splits < 2 * sm_count() && steps >= 8 * splits) splits *= 2;
+    // as many CTAs as are resident together (two for each SM), with two steps at least for each
+    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP, most = 2 * sm_count() / tiles;
+    int splits = (int)(most < 8 ? most : 8);
+    if (splits > steps / 2) splits = (int)(steps / 2);
+    if (splits < 1) splits = 1;
     if (a.whole == 3 && dtype != CT_DT_F32 && x_dtype == dtype) return ad_shrink_tc(a, dtype == CT_DT_BF16, trans, o, tiles, splits, st);
     return trans ? by_type<true>(a, x_dtype, dtype, o, tiles, splits, st) : by_type<false>(a, x_dtype, dtype, o, tiles, splits, st);
 }

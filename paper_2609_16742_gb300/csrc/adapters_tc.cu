@@ -92,7 +92,7 @@ template <int RP> struct Shrink {
 template <typename T, int RP, bool TRANS>
 __global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink a, const AdOrder o, int splits, uint32_t *err) {
     using S = Shrink<RP>;
-    extern __shared__ unsigned char raw[];
+    extern __shared__ __align__(128) unsigned char raw[];
     __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
     __shared__ uint32_t holder;
     pdl_wait();
@@ -196,46 +196,54 @@ __global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink
     tensor_end<S::COLUMNS>(tmem);
 
     // the tile's sums of this CTA, then of all of the cluster
-    float *fs = reinterpret_cast<float *>(raw);
-    const int row = (warp & 3) * 32 + lane;
+    float *fs = reinterpret_cast<float *>(raw) + ((warp & 3) * 32 + lane) * sums_pitch(RP) + (warp >> 2) * (RP / 2);
 #pragma unroll
-    for (int j = 0; j < RP / 2; ++j) fs[row * (RP + 1) + (warp >> 2) * (RP / 2) + j] = sum[j];
+    for (int j = 0; j < RP / 2; j += 4) *reinterpret_cast<float4 *>(fs + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
     if (splits > 1) tc::cluster_sync();
     else __syncthreads();
-    const float scale = a.scale != nullptr ? a.scale[adapter] : 1.f;
-    const uint32_t peer = tc::smem_u32(raw);
-    const int r0 = AD_ROWS * rank / splits, r1 = AD_ROWS * (rank + 1) / splits;
-    for (int v = tid; v < (r1 - r0) * (RP / 2); v += AD_THREADS) {
-        const int r = r0 + v / (RP / 2), j = v % (RP / 2) * 2;
-        if (r >= tile.rows) break;
-        const int f = r * (RP + 1) + j;
-        float x = 0.f, y = 0.f;
-        for (int c = 0; c < splits; ++c) {
-            x += splits > 1 ? ld_peer_f32(peer + f * 4, c) : fs[f];
-            y += splits > 1 ? ld_peer_f32(peer + (f + 1) * 4, c) : fs[f + 1];
-        }
-        x = j < a.rank ? x * scale : 0.f;         // 0 and not 0 times what x holds
-        y = j + 1 < a.rank ? y * scale : 0.f;
-        uint32_t *out = static_cast<uint32_t *>(a.v) + ((tile.slot0 + r) * RP + j) / 2;
-        for (int p = 0; p < a.parts; ++p) out[p * (o.t * RP / 2)] = split2(x, y);
-    }
+    write_vectors<RP>(a, o, tile, adapter, reinterpret_cast<const float *>(raw), rank, splits);
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
 // ---------------------------------------------------------------- expand
 
-// Columns of a block: 256 bytes of y a row.  A thread has one row and half of them.
+// Columns of a block: 256 bytes of y a row.  Its columns are dealt to the products' so that what the four lanes of a quad
+// read from tensor memory for a row are 16 neighbouring bytes of y each: column c = 4 W g + W t + 2 q + e (W = 16 bytes of values, t < 4,
+// e < 2) is the product's column 4 W g + 8 q + 2 t + e.
 template <int RP, int YS> struct Expand {
-    static constexpr int COLS = 256 / YS, HALF = COLS / 2, V_BYTES = AD_ROWS * 2 * RP, M_BYTES = COLS * 2 * RP, STAGES = 3;
+    static constexpr int COLS = 256 / YS, HALF = COLS / 2, W = 16 / YS, V_BYTES = AD_ROWS * 2 * RP, M_BYTES = COLS * 2 * RP, STAGES = 3;
     static constexpr int COLUMNS = columns_of(2 * COLS);
     static int smem(int parts) { return parts * V_BYTES + STAGES * M_BYTES + 1024; }
     static constexpr int MV = COLS * (RP / 8) / AD_THREADS > 0 ? COLS * (RP / 8) / AD_THREADS : 1;
+    static __device__ __forceinline__ int dealt(int c) { return c / (4 * W) * (4 * W) + c % W / 2 * 8 + c % (4 * W) / W * 2 + c % 2; }
 };
+
+// W columns' sums of rows lane / 4 and lane / 4 + 8 of 16 rows: columns W (lane % 4) on of 4 W
+template <int W> __device__ __forceinline__ void tmem_quads(uint32_t addr, float (&lo)[W], float (&hi)[W]) {
+    uint32_t r[2 * W];
+    if constexpr (W == 8)
+        asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                       "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                     : "r"(addr));
+    else
+        asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int q = 0; q < W / 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            lo[2 * q + e] = tc::tmem_done(r[4 * q + e]);
+            hi[2 * q + e] = tc::tmem_done(r[4 * q + 2 + e]);
+        }
+}
 
 template <int RP, bool TRANS, int YS>
 __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a, const AdOrder o, uint32_t *err) {
     using S = Expand<RP, YS>;
-    extern __shared__ unsigned char raw[];
+    extern __shared__ __align__(128) unsigned char raw[];
     __shared__ uint64_t bars[3];                  // a block's products are done (two, in turn); all
     __shared__ uint32_t holder;
     pdl_wait();
@@ -262,7 +270,17 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
             const int64_t c = TRANS ? c0 + q * 8 : c0 + r;
             const int j = TRANS ? r : q * 8;
             const bool there = c < a.cols && j < a.rank;
-            copy16_if(bm + MT::at(r, q, TRANS ? RP : S::COLS), m + (there ? (TRANS ? j * a.m_row + c : c * a.m_row + j) : 0), there);
+            if constexpr (TRANS) {
+                // four pairs of columns, each to its place
+                const char *p = reinterpret_cast<const char *>(m + (there ? j * a.m_row + c : 0));
+#pragma unroll
+                for (int i2 = 0; i2 < 4; ++i2) {
+                    const int to = S::dealt(q * 8 + 2 * i2);
+                    copy4_if(bm + MT::at(r, to / 8, RP) + to % 8 * 2, p + 4 * i2, there);
+                }
+            } else {
+                copy16_if(bm + MT::at(S::dealt(r), q, S::COLS), m + (there ? c * a.m_row + j : 0), there);
+            }
         }
     };
     if (product_wanted) {
@@ -278,54 +296,59 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
             copies_end();
         }
     }
-    // this thread's row and half of a block's columns
-    const int row = (warp & 3) * 32 + lane, half = (warp >> 2) * S::HALF;
-    const bool have = row < tile.rows;
-    const int64_t t = have ? (o.order != nullptr ? (int64_t)o.order[tile.slot0 + row] : tile.slot0 + row) : 0;
-    char *y0 = static_cast<char *>(a.y) + t * a.ldy * YS;
-    const float nan = __uint_as_float(0x7FC00000u);
-    uint4 y[8];                                   // 128 bytes
-    auto y_fetch = [&](int b) {
-        const int64_t c = c_from + (int64_t)b * S::COLS + half;
+    // This thread's rows: lane / 4 + 8 i of the warp's 32; its columns: W from W (lane % 4) on of each 4 W of the warp's half.
+    constexpr int W = S::W, G = S::HALF / (4 * W);
+    const int half = (warp >> 2) * S::HALF, lane_c = half + (lane & 3) * W;
+    char *yr[4];
+    bool have[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = ld_if(y0 + (c + i * (16 / YS)) * YS, have && c + i * (16 / YS) < c_to);
+    for (int i = 0; i < 4; ++i) {
+        const int row = (warp & 3) * 32 + i * 8 + (lane >> 2);
+        have[i] = row < tile.rows;
+        yr[i] = static_cast<char *>(a.y) + (have[i] ? (o.order != nullptr ? (int64_t)o.order[tile.slot0 + row] : tile.slot0 + row) * a.ldy * YS : 0);
+    }
+    const float nan = __uint_as_float(0x7FC00000u);
+    uint4 y[G][4];
+    auto y_fetch = [&](int b) {
+        const int64_t c = c_from + (int64_t)b * S::COLS + lane_c;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[g][i] = ld_if(yr[i] + (c + g * 4 * W) * YS, have[i] && c + g * 4 * W < c_to);
     };
     const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21) + (uint32_t)half;
     // adds a block's sums (none where there is no product) to y
     auto finish = [&](int b) {
-        const int64_t c0 = c_from + (int64_t)b * S::COLS + half;
+        const int64_t c = c_from + (int64_t)b * S::COLS + lane_c;
 #pragma unroll
-        for (int j = 0; j < S::HALF; j += 8) {
-            float v[8], w[8];
-            if (product_wanted) {
-                tmem_ld8(mine + (b & 1) * S::COLS + j, v);
-            } else {
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.f;
-            }
-            if constexpr (YS == 4) {
-                unpack16<float>(y[j / 4], w);
-                unpack16<float>(y[j / 4 + 1], w + 4);
-            } else if (a.y_dtype == CT_DT_F16) {
-                unpack16<__half>(y[j / 8], w);
-            } else {
-                unpack16<__nv_bfloat16>(y[j / 8], w);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += w[e];
-            if (a.relu || out)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = out ? nan : v[e] < 0.f ? 0.f : v[e];
-            if (have && c0 + j < c_to) {
-                char *p = y0 + (c0 + j) * YS;
-                if constexpr (YS == 4) {
-                    *reinterpret_cast<uint4 *>(p) = pack16<float>(v);
-                    *reinterpret_cast<uint4 *>(p + 16) = pack16<float>(v + 4);
+            for (int h = 0; h < 2; ++h) {
+                float v[2][W];
+                if (product_wanted) {
+                    tmem_quads<W>(mine + ((uint32_t)h << 20) + (b & 1) * S::COLS + g * 4 * W, v[0], v[1]);
                 } else {
-                    *reinterpret_cast<uint4 *>(p) = a.y_dtype == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
+#pragma unroll
+                    for (int e = 0; e < W; ++e) v[0][e] = v[1][e] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float w[W];
+                    if constexpr (YS == 4) unpack16<float>(y[g][2 * h + i], w);
+                    else if (a.y_dtype == CT_DT_F16) unpack16<__half>(y[g][2 * h + i], w);
+                    else unpack16<__nv_bfloat16>(y[g][2 * h + i], w);
+#pragma unroll
+                    for (int e = 0; e < W; ++e) w[e] += v[i][e];
+                    if (a.relu || out)
+#pragma unroll
+                        for (int e = 0; e < W; ++e) w[e] = out ? nan : w[e] < 0.f ? 0.f : w[e];
+                    if (have[2 * h + i] && c + g * 4 * W < c_to) {
+                        uint4 *p = reinterpret_cast<uint4 *>(yr[2 * h + i] + (c + g * 4 * W) * YS);
+                        if constexpr (YS == 4) *p = pack16<float>(w);
+                        else *p = a.y_dtype == CT_DT_F16 ? pack16<__half>(w) : pack16<__nv_bfloat16>(w);
+                    }
                 }
             }
-        }
     };
     bool ok = true;
     constexpr uint32_t how = product(true, false, TRANS, AD_ROWS, S::COLS);
@@ -393,7 +416,7 @@ constexpr int OUTER_COLS = 128;
 template <int RP, int PARTS> struct Outer {
     static constexpr int N = RP * PARTS, X_BYTES = AD_STEP * OUTER_COLS * 2, V_BYTES = AD_STEP * 2 * RP, STAGE = X_BYTES + PARTS * V_BYTES;
     static constexpr int STAGES = STAGE <= 24576 ? 4 : STAGE <= 32768 ? 3 : 4, SMEM = STAGES * STAGE + 1024, COLUMNS = columns_of(2 * N);
-    static constexpr int SUM = OUTER_COLS * (RP + 1) * 4;
+    static constexpr int SUM = OUTER_COLS * sums_pitch(RP) * 4;
     static constexpr int VV = (AD_STEP * (RP / 8) * PARTS + AD_THREADS - 1) / AD_THREADS;
     static_assert(N <= 256 && SUM <= SMEM, "one product's columns, and the sums in the stages' memory");
 };
@@ -401,7 +424,7 @@ template <int RP, int PARTS> struct Outer {
 template <int RP, int PARTS>
 __global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const AdOuter a, const AdOrder o, int splits, uint32_t *err) {
     using S = Outer<RP, PARTS>;
-    extern __shared__ unsigned char raw[];
+    extern __shared__ __align__(128) unsigned char raw[];
     __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
     __shared__ uint32_t holder;
     pdl_wait();
@@ -500,25 +523,12 @@ __global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const AdOuter a, c
     if (at < n) tc::mbar_wait(bar + 8 * (S::STAGES + 2), 0, err, E_ADAPTERS);
     tensor_end<S::COLUMNS>(tmem);
 
-    float *fs = reinterpret_cast<float *>(raw);
-    const int col = (warp & 3) * 32 + lane;
+    float *fs = reinterpret_cast<float *>(raw) + ((warp & 3) * 32 + lane) * sums_pitch(RP) + (warp >> 2) * (RP / 2);
 #pragma unroll
-    for (int j = 0; j < RP / 2; ++j) fs[col * (RP + 1) + (warp >> 2) * (RP / 2) + j] = sum[j];
+    for (int j = 0; j < RP / 2; j += 4) *reinterpret_cast<float4 *>(fs + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
     if (splits > 1) tc::cluster_sync();
     else __syncthreads();
-    const uint32_t peer = tc::smem_u32(raw);
-    const int c0 = OUTER_COLS * rank / splits, c1 = OUTER_COLS * (rank + 1) / splits, wide = c1 - c0;
-    const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
-    for (int v = tid; v < wide * a.rank; v += AD_THREADS) {
-        const int c = c0 + (a.by_cols ? v / a.rank : v % wide), j = a.by_cols ? v % a.rank : v / wide;
-        if (cols0 + c >= a.cols) continue;
-        const int f = c * (RP + 1) + j;
-        float x = 0.f;
-        for (int q = 0; q < splits; ++q) x += splits > 1 ? ld_peer_f32(peer + f * 4, q) : fs[f];
-        const int64_t to_at = g0 + (a.by_cols ? (cols0 + c) * a.rank + j : j * a.cols + cols0 + c);
-        if (a.g_dtype == CT_DT_F32) static_cast<float *>(a.g)[to_at] = x;
-        else static_cast<__nv_bfloat16 *>(a.g)[to_at] = __float2bfloat16_rn(x);
-    }
+    write_gradient<RP>(a, adapter, cols0, reinterpret_cast<const float *>(raw), rank, splits);
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
@@ -548,11 +558,11 @@ template <int RP, bool TRANS, int YS> cudaError_t expand(const AdExpand &q, cons
     auto *kernel = expand_tc_kernel<RP, TRANS, YS>;
     const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3));
     if (e != cudaSuccess) return e;
-    // columns of a CTA: as many as leave each SM four of them, at most 16 blocks
+    // columns of a CTA: as many as leave each SM two CTAs, which are resident together, at most 32 blocks
     AdExpand a = q;
     const int64_t blocks = (a.cols + S::COLS - 1) / S::COLS;
-    int64_t parts = (4 * (int64_t)sm_count() + tiles - 1) / tiles;
-    if (parts < (blocks + 15) / 16) parts = (blocks + 15) / 16;
+    int64_t parts = 2 * (int64_t)sm_count() / tiles;
+    if (parts < (blocks + 31) / 32) parts = (blocks + 31) / 32;
     if (parts > blocks) parts = blocks;
     if (parts > 65535) parts = 65535;
     a.per = (blocks + parts - 1) / parts * S::COLS;
