@@ -46,6 +46,7 @@ struct AdShrink {
     int rank, whole;
     void *v;                                      // BF16 [parts][t][padded rank], by slots
     int parts;
+    bool first;                                   // launched right behind the ordering of the rows
 };
 struct AdExpand {
     void *y;
@@ -67,6 +68,11 @@ struct AdOuter {
     void *g;                                      // [adapters][rank][cols], or [adapters][cols][rank] where by_cols
     int32_t g_dtype;
     int by_cols;
+};
+// One or two of them: blocks of 128 columns, the first one's, then the second one's.
+struct AdOuters {
+    AdOuter a[2];
+    int first;                                    // blocks of the first
 };
 
 #ifdef __CUDACC__
@@ -284,7 +290,8 @@ __device__ __forceinline__ void put_as(void *p, int dtype, int64_t i, float v) {
     else if (dtype == CT_DT_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
     else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
 }
-// a gradient's 128 columns from cols0 on: the cluster's sums, each CTA its share of the columns
+// A gradient's 128 columns from cols0 on: the cluster's sums, each CTA its share of the columns.  (Sharing the rank instead, for whole
+// runs of columns where those run along the gradient's rows: 30 us for 8192 x 4096 x 64, against 27.)
 template <int RP>
 __device__ __forceinline__ void write_gradient(const AdOuter &a, int adapter, int64_t cols0, const float *fs, int rank, int splits) {
     constexpr int COLS = 128;
@@ -309,18 +316,45 @@ __device__ __forceinline__ void write_gradient(const AdOuter &a, int adapter, in
 }
 #endif
 
+// A launch that may begin while the kernel before ends, or (early: 0) not.  CTAs that are let in early go to whichever SMs are free first, two to
+// one and none to another, where a kernel has not many more than the SMs hold: 8192 rows at rank 64 took 97 us with early launches of all
+// kernels, 86 without.  So the tcgen05 kernels wait where they have more CTAs than there are SMs, unless the kernel before is the ordering of the
+// rows (one CTA).  The others, which hold fewer registers and less shared memory, lose more by the gap (1777 rows: 144 us, against 135).
+template <typename... KArgs, typename... Args>
+inline cudaError_t ad_launch(void (*kernel)(KArgs...), dim3 grid, size_t smem, cudaStream_t st, int cluster, bool early, Args &&...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(AD_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = early || (int64_t)grid.x * grid.y <= sm_count();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 inline int ad_padded(int64_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 
-// trans: the matrix has the rank along its rows ([cols, rank]) for shrink, the columns along its rows ([rank, cols]) for expand
-cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
+// The products of x with A^T ([rank, cols]; AD_FORWARD), of dy with B ([cols, rank], the rank along its rows; AD_BACKWARD), or of a[0] the one and
+// of a[1] the other in one launch (AD_BOTH: of one rank and one type of rows).
+enum AdWhich { AD_FORWARD = 0, AD_BACKWARD = 1, AD_BOTH = 2 };
+cudaError_t ad_shrink(const AdShrink (&a)[2], AdWhich which, int x_dtype, int dtype, const AdOrder &o, int tiles, cudaStream_t st);
+// trans: the matrix has the columns along its rows ([rank, cols])
 cudaError_t ad_expand(const AdExpand &a, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
-cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st);
+// two products of the same rank and number of parts, of x's of one type, in one launch (n = 2), or one (n = 1)
+cudaError_t ad_outer(const AdOuter (&a)[2], int n, int x_dtype, const AdOrder &o, cudaStream_t st);
 
 // The same on tcgen05, for 16-bit values in whole rows; splits: CTAs of a cluster that share the summed axis.
-cudaError_t ad_shrink_tc(const AdShrink &a, bool bf16, bool trans, const AdOrder &o, int tiles, int splits, cudaStream_t st);
+cudaError_t ad_shrink_tc(const AdShrink (&a)[2], AdWhich which, bool bf16, const AdOrder &o, int tiles, int splits, cudaStream_t st);
 cudaError_t ad_expand_tc(const AdExpand &a, bool trans, const AdOrder &o, int tiles, cudaStream_t st);
 bool ad_outer_tc_takes(int64_t rank, int parts);
-cudaError_t ad_outer_tc(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st);
+cudaError_t ad_outer_tc(const AdOuters &two, int blocks, const AdOrder &o, int splits, cudaStream_t st);
 
 }  // namespace ops
 }  // namespace ct

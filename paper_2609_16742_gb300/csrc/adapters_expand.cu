@@ -69,7 +69,8 @@ __device__ __forceinline__ float y_one_if(const char *p, int dtype, bool wanted)
     return dtype == CT_DT_F16 ? __half2float(__ushort_as_half(h)) : __uint_as_float((uint32_t)h << 16);
 }
 
-template <typename TM, int RP, bool TRANS>
+// YW: y's rows are whole
+template <typename TM, int RP, bool TRANS, bool YW>
 __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, const AdOrder o) {
     using S = Expand<TM, RP, TRANS>;
     extern __shared__ __align__(128) unsigned char sm[];
@@ -82,7 +83,6 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     const bool out = tile.key > o.adapters, none = tile.key == 0;               // NaN; act alone
     const uint32_t base = tc::smem_u32(sm), bm0 = base + a.parts * S::V_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
-    const bool y_whole = a.whole & 1;
     const int ys = a.y_dtype == CT_DT_F32 ? 4 : 2;
     if (tid < AD_ROWS) rows[tid] = tid < tile.rows ? (o.order != nullptr ? o.order[tile.slot0 + tid] : (int32_t)(tile.slot0 + tid)) : -1;
 
@@ -160,21 +160,37 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     }
     const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
     const float nan = __uint_as_float(0x7FC00000u);
-    const int64_t mine0 = wn * 32 + (lane & 3) * 8;
-    YEight ahead[4];
+    // y a step ahead: eight neighbouring values of each of the thread's rows, or, of rows that start anywhere, one column's of all of the warp's
+    const int64_t mine0 = wn * 32 + (YW ? (lane & 3) * 8 : lane);
+    YEight ahead[YW ? 4 : 1];
+    float column[YW ? 1 : 32];
+    auto y_fetch = [&](int64_t c0) {
+        const int64_t c = c0 + mine0;
+        if constexpr (YW) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) ahead[i] = y_load(yr[i] + (c_from + mine0) * ys, a.y_dtype, y_whole && yh[i] && c_from + mine0 < c_to);
+            for (int i = 0; i < 4; ++i) ahead[i] = y_load(yr[i] + c * ys, a.y_dtype, yh[i] && c < c_to);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 32; ++r) {
+                const int32_t t = rows[wm * 32 + r];
+                const bool there = t >= 0 && c < c_to;
+                column[r] = y_one_if(static_cast<char *>(a.y) + (there ? ((int64_t)t * a.ldy + c) * ys : 0), a.y_dtype, there);
+            }
+        }
+    };
+    y_fetch(c_from);
     int buf = 0;
     for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, buf ^= 1) {
         const bool more = product && c0 + AD_STEP < c_to;
         if (more) fetch(c0 + AD_STEP);
-        const int64_t mine = c0 + mine0, next = mine + AD_STEP;
-        YEight y[4];
+        const int64_t mine = c0 + mine0;
+        YEight y[YW ? 4 : 1];
+        float old[YW ? 1 : 32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y[i] = ahead[i];
-            ahead[i] = y_load(yr[i] + next * ys, a.y_dtype, y_whole && yh[i] && next < c_to);
-        }
+        for (int i = 0; i < (YW ? 4 : 1); ++i) y[i] = ahead[i];
+#pragma unroll
+        for (int i = 0; i < (YW ? 1 : 32); ++i) old[i] = column[i];
+        y_fetch(c0 + AD_STEP);
         float acc[2][4][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -209,7 +225,7 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
                     }
                 }
         }
-        if (y_whole) {
+        if constexpr (YW) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float v[8], w[8];
@@ -227,16 +243,8 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         } else {
             // rows that start anywhere: eight rows of the warp's sums at a time turn in shared memory, so that lanes are neighbouring columns
             float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + 2 * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
-            const int64_t c = c0 + wn * 32 + lane;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float old[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const int32_t t = rows[wm * 32 + i * 8 + r];
-                    const bool there = t >= 0 && c < c_to;
-                    old[r] = y_one_if(static_cast<char *>(a.y) + (there ? ((int64_t)t * a.ldy + c) * ys : 0), a.y_dtype, there);
-                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -245,10 +253,10 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     const int32_t t = rows[wm * 32 + i * 8 + r];
-                    if (t < 0 || c >= c_to) continue;
-                    float v = w[r * S::WIDE + lane] + old[r];
+                    if (t < 0 || mine >= c_to) continue;
+                    float v = w[r * S::WIDE + lane] + old[i * 8 + r];
                     if (a.relu) v = v < 0.f ? 0.f : v;
-                    y_put(static_cast<char *>(a.y) + ((int64_t)t * a.ldy + c) * ys, a.y_dtype, out ? nan : v);
+                    y_put(static_cast<char *>(a.y) + ((int64_t)t * a.ldy + mine) * ys, a.y_dtype, out ? nan : v);
                 }
                 __syncwarp();
             }
@@ -258,11 +266,11 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     }
 }
 
-template <typename TM, int RP, bool TRANS> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
+template <typename TM, int RP, bool TRANS, bool YW> cudaError_t launch(const AdExpand &q, const AdOrder &o, int tiles, cudaStream_t st) {
     using S = Expand<TM, RP, TRANS>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = expand_kernel<TM, RP, TRANS>;
-    const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3, true));
+    auto *kernel = expand_kernel<TM, RP, TRANS, YW>;
+    const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3, !YW));
     if (e != cudaSuccess) return e;
     // columns of a block: as many as leave each SM three blocks, at most 1024
     AdExpand a = q;
@@ -273,26 +281,27 @@ template <typename TM, int RP, bool TRANS> cudaError_t launch(const AdExpand &q,
     if (parts > 65535) parts = 65535;
     a.per = (steps + parts - 1) / parts * AD_STEP;
     const dim3 grid((unsigned)tiles, (unsigned)((a.cols + a.per - 1) / a.per));
-    return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts, !(a.whole & 1)), st, a, o);
+    return ad_launch(kernel, grid, (size_t)S::smem(a.parts, !YW), st, 1, true, a, o);
 }
-template <typename TM, bool TRANS> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
+template <typename TM, bool TRANS, bool YW> cudaError_t by_rank(const AdExpand &a, const AdOrder &o, int tiles, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
-        case 16: return launch<TM, 16, TRANS>(a, o, tiles, st);
-        case 32: return launch<TM, 32, TRANS>(a, o, tiles, st);
-        case 64: return launch<TM, 64, TRANS>(a, o, tiles, st);
-        default: return launch<TM, 128, TRANS>(a, o, tiles, st);
+        case 16: return launch<TM, 16, TRANS, YW>(a, o, tiles, st);
+        case 32: return launch<TM, 32, TRANS, YW>(a, o, tiles, st);
+        case 64: return launch<TM, 64, TRANS, YW>(a, o, tiles, st);
+        default: return launch<TM, 128, TRANS, YW>(a, o, tiles, st);
     }
 }
-template <bool TRANS> cudaError_t by_type(const AdExpand &a, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
-    return dtype == CT_DT_F32   ? by_rank<float, TRANS>(a, o, tiles, st)
-           : dtype == CT_DT_F16 ? by_rank<__half, TRANS>(a, o, tiles, st)
-                                : by_rank<__nv_bfloat16, TRANS>(a, o, tiles, st);
+template <bool TRANS, bool YW> cudaError_t by_type(const AdExpand &a, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
+    return dtype == CT_DT_F32   ? by_rank<float, TRANS, YW>(a, o, tiles, st)
+           : dtype == CT_DT_F16 ? by_rank<__half, TRANS, YW>(a, o, tiles, st)
+                                : by_rank<__nv_bfloat16, TRANS, YW>(a, o, tiles, st);
 }
 }  // namespace
 
 cudaError_t ad_expand(const AdExpand &a, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
     if (dtype == CT_DT_BF16 && a.whole == 3) return ad_expand_tc(a, trans, o, tiles, st);
-    return trans ? by_type<true>(a, dtype, o, tiles, st) : by_type<false>(a, dtype, o, tiles, st);
+    if (a.whole & 1) return trans ? by_type<true, true>(a, dtype, o, tiles, st) : by_type<false, true>(a, dtype, o, tiles, st);
+    return trans ? by_type<true, false>(a, dtype, o, tiles, st) : by_type<false, false>(a, dtype, o, tiles, st);
 }
 
 }  // namespace ops

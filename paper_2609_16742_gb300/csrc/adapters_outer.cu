@@ -32,13 +32,15 @@ template <typename TX, int RP> struct Outer {
 };
 
 template <typename TX, int RP>
-__global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, const AdOrder o, int splits) {
+__global__ void __launch_bounds__(AD_THREADS) outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int splits) {
     using S = Outer<TX, RP>;
     extern __shared__ __align__(128) unsigned char sm[];
     pdl_wait();
     pdl_trigger();
     const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, adapter = blockIdx.y;
-    const int64_t cols0 = (int64_t)(blockIdx.x / (unsigned)splits) * COLS;
+    const int block = (int)(blockIdx.x / (unsigned)splits);
+    const AdOuter &a = two.a[block >= two.first];
+    const int64_t cols0 = (int64_t)(block >= two.first ? block - two.first : block) * COLS;
     const int64_t from = o.order != nullptr ? o.first[adapter + 1] : 0, to = o.order != nullptr ? o.end[adapter + 1] : adapter == 0 ? o.t : 0;
     const int64_t steps = (to - from + AD_STEP - 1) / AD_STEP;
     const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
@@ -189,38 +191,39 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const AdOuter a, cons
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
-template <typename TX, int RP> cudaError_t launch(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st) {
+template <typename TX, int RP> cudaError_t launch(const AdOuters &two, int blocks, const AdOrder &o, int splits, cudaStream_t st) {
     using S = Outer<TX, RP>;
     static std::atomic<bool> sized[MAX_DEVICES];
     auto *kernel = outer_kernel<TX, RP>;
     const cudaError_t e = allow_smem(kernel, sized, (size_t)S::smem(3));
     if (e != cudaSuccess) return e;
-    const int64_t blocks = (a.cols + COLS - 1) / COLS;
     const dim3 grid((unsigned)(blocks * splits), (unsigned)o.adapters);
-    if (splits == 1) return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, a, o, splits);
-    return pdl_launch_cluster(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, splits, a, o, splits);
+    const size_t smem = (size_t)S::smem(two.a[0].parts);
+    return ad_launch(kernel, grid, smem, st, splits, true, two, o, splits);
 }
-template <typename TX> cudaError_t by_rank(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st) {
-    switch (ad_padded(a.rank)) {
-        case 16: return launch<TX, 16>(a, o, splits, st);
-        case 32: return launch<TX, 32>(a, o, splits, st);
-        case 64: return launch<TX, 64>(a, o, splits, st);
-        default: return launch<TX, 128>(a, o, splits, st);
+template <typename TX> cudaError_t by_rank(const AdOuters &two, int blocks, const AdOrder &o, int splits, cudaStream_t st) {
+    switch (ad_padded(two.a[0].rank)) {
+        case 16: return launch<TX, 16>(two, blocks, o, splits, st);
+        case 32: return launch<TX, 32>(two, blocks, o, splits, st);
+        case 64: return launch<TX, 64>(two, blocks, o, splits, st);
+        default: return launch<TX, 128>(two, blocks, o, splits, st);
     }
 }
 }  // namespace
 
-cudaError_t ad_outer(const AdOuter &a, int x_dtype, const AdOrder &o, cudaStream_t st) {
+cudaError_t ad_outer(const AdOuter (&a)[2], int n, int x_dtype, const AdOrder &o, cudaStream_t st) {
+    const int first = (int)((a[0].cols + COLS - 1) / COLS), blocks = first + (n > 1 ? (int)((a[1].cols + COLS - 1) / COLS) : 0);
     // as many CTAs as are resident together (two for each SM), with two steps of an adapter's share of the rows at least for each
-    const int64_t blocks = (a.cols + COLS - 1) / COLS, steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP;
-    const int64_t most = 2 * sm_count() / (blocks * o.adapters);
+    const int64_t steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP, most = 2 * sm_count() / ((int64_t)blocks * o.adapters);
     int splits = (int)(most < 8 ? most : 8);
     if (splits > steps / 2) splits = (int)(steps / 2);
     if (splits < 1) splits = 1;
-    if (x_dtype == CT_DT_BF16 && (a.whole & 1) && ad_outer_tc_takes(a.rank, a.parts)) return ad_outer_tc(a, o, splits, st);
-    return x_dtype == CT_DT_F32   ? by_rank<float>(a, o, splits, st)
-           : x_dtype == CT_DT_F16 ? by_rank<__half>(a, o, splits, st)
-                                  : by_rank<__nv_bfloat16>(a, o, splits, st);
+    const AdOuters two = {{a[0], a[n - 1]}, first};
+    if (x_dtype == CT_DT_BF16 && (a[0].whole & a[n - 1].whole & 1) && ad_outer_tc_takes(a[0].rank, a[0].parts))
+        return ad_outer_tc(two, blocks, o, splits, st);
+    return x_dtype == CT_DT_F32   ? by_rank<float>(two, blocks, o, splits, st)
+           : x_dtype == CT_DT_F16 ? by_rank<__half>(two, blocks, o, splits, st)
+                                  : by_rank<__nv_bfloat16>(two, blocks, o, splits, st);
 }
 
 }  // namespace ops

@@ -29,14 +29,8 @@ template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
 };
 
 template <typename TX, typename TM, int RP, bool TRANS>
-__global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, const AdOrder o, int splits) {
+__device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o, const AdRows &tile, int rank, int splits, unsigned char *sm) {
     using S = Shrink<TX, TM, RP, TRANS>;
-    extern __shared__ __align__(128) unsigned char sm[];
-    pdl_wait();
-    pdl_trigger();
-    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0;
-    const AdRows tile = ad_tile(o, (int)(blockIdx.x / (unsigned)splits));
-    if (tile.rows == 0 || tile.key == 0 || tile.key > o.adapters) return;       // the whole cluster alike
     const int adapter = tile.key - 1;
     const uint32_t base = tc::smem_u32(sm);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
@@ -205,42 +199,67 @@ __global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const AdShrink a, co
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
 }
 
-template <typename TX, typename TM, int RP, bool TRANS>
-cudaError_t launch(const AdShrink &a, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
-    using S = Shrink<TX, TM, RP, TRANS>;
-    static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = shrink_kernel<TX, TM, RP, TRANS>;
-    const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
-    if (e != cudaSuccess) return e;
-    if (splits == 1) return pdl_launch(kernel, dim3((unsigned)tiles), dim3(AD_THREADS), S::SMEM, st, a, o, splits);
-    return pdl_launch_cluster(kernel, dim3((unsigned)(tiles * splits)), dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits);
+struct AdShrinks {
+    AdShrink a[2];
+};
+// WHICH as AdWhich: both: the tiles of the first, then those of the second
+template <typename TX, typename TM, int RP, int WHICH>
+__global__ void __launch_bounds__(AD_THREADS) shrink_kernel(const __grid_constant__ AdShrinks two, const AdOrder o, int tiles, int splits) {
+    extern __shared__ __align__(128) unsigned char sm[];
+    pdl_wait();
+    pdl_trigger();
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0;
+    int t = (int)(blockIdx.x / (unsigned)splits);
+    const bool second = WHICH == AD_BACKWARD || (WHICH == AD_BOTH && t >= tiles);
+    if (WHICH == AD_BOTH && second) t -= tiles;
+    const AdShrink &a = two.a[WHICH == AD_BOTH && second];
+    const AdRows tile = ad_tile(o, t);
+    if (tile.rows == 0 || tile.key == 0 || tile.key > o.adapters) return;       // the whole cluster alike
+    if (WHICH == AD_FORWARD || (WHICH == AD_BOTH && !second)) shrink_tile<TX, TM, RP, false>(a, o, tile, rank, splits, sm);
+    else shrink_tile<TX, TM, RP, true>(a, o, tile, rank, splits, sm);
 }
-template <typename TX, typename TM, bool TRANS>
-cudaError_t by_rank(const AdShrink &a, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
-    switch (ad_padded(a.rank)) {
-        case 16: return launch<TX, TM, 16, TRANS>(a, o, tiles, splits, st);
-        case 32: return launch<TX, TM, 32, TRANS>(a, o, tiles, splits, st);
-        case 64: return launch<TX, TM, 64, TRANS>(a, o, tiles, splits, st);
-        default: return launch<TX, TM, 128, TRANS>(a, o, tiles, splits, st);
+
+template <typename TX, typename TM, int RP, int WHICH>
+cudaError_t launch(const AdShrinks &two, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+    constexpr int F = Shrink<TX, TM, RP, false>::SMEM, B = Shrink<TX, TM, RP, true>::SMEM;
+    constexpr int SMEM = WHICH == AD_FORWARD ? F : WHICH == AD_BACKWARD ? B : F > B ? F : B;
+    static std::atomic<bool> sized[MAX_DEVICES];
+    auto *kernel = shrink_kernel<TX, TM, RP, WHICH>;
+    const cudaError_t e = allow_smem(kernel, sized, SMEM);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)((WHICH == AD_BOTH ? 2 : 1) * tiles * splits));
+    return ad_launch(kernel, grid, SMEM, st, splits, true, two, o, tiles, splits);
+}
+template <typename TX, typename TM, int WHICH> cudaError_t by_rank(const AdShrinks &two, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+    switch (ad_padded(two.a[0].rank)) {
+        case 16: return launch<TX, TM, 16, WHICH>(two, o, tiles, splits, st);
+        case 32: return launch<TX, TM, 32, WHICH>(two, o, tiles, splits, st);
+        case 64: return launch<TX, TM, 64, WHICH>(two, o, tiles, splits, st);
+        default: return launch<TX, TM, 128, WHICH>(two, o, tiles, splits, st);
     }
 }
-template <bool TRANS> cudaError_t by_type(const AdShrink &a, int x_dtype, int dtype, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
-    if (dtype == CT_DT_F32) return by_rank<float, float, TRANS>(a, o, tiles, splits, st);
+template <int WHICH> cudaError_t by_type(const AdShrinks &two, int x_dtype, int dtype, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+    if (dtype == CT_DT_F32) return by_rank<float, float, WHICH>(two, o, tiles, splits, st);
     if (dtype == CT_DT_F16)
-        return x_dtype == CT_DT_F32 ? by_rank<float, __half, TRANS>(a, o, tiles, splits, st) : by_rank<__half, __half, TRANS>(a, o, tiles, splits, st);
-    return x_dtype == CT_DT_F32 ? by_rank<float, __nv_bfloat16, TRANS>(a, o, tiles, splits, st)
-                                : by_rank<__nv_bfloat16, __nv_bfloat16, TRANS>(a, o, tiles, splits, st);
+        return x_dtype == CT_DT_F32 ? by_rank<float, __half, WHICH>(two, o, tiles, splits, st) : by_rank<__half, __half, WHICH>(two, o, tiles, splits, st);
+    return x_dtype == CT_DT_F32 ? by_rank<float, __nv_bfloat16, WHICH>(two, o, tiles, splits, st)
+                                : by_rank<__nv_bfloat16, __nv_bfloat16, WHICH>(two, o, tiles, splits, st);
 }
 }  // namespace
 
-cudaError_t ad_shrink(const AdShrink &a, int x_dtype, int dtype, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
+cudaError_t ad_shrink(const AdShrink (&a)[2], AdWhich which, int x_dtype, int dtype, const AdOrder &o, int tiles, cudaStream_t st) {
+    const int64_t cols = which == AD_BOTH && a[1].cols > a[0].cols ? a[1].cols : a[0].cols;
     // as many CTAs as are resident together (two for each SM), with two steps at least for each
-    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP, most = 2 * sm_count() / tiles;
+    const int64_t steps = (cols + AD_STEP - 1) / AD_STEP, most = 2 * sm_count() / ((which == AD_BOTH ? 2 : 1) * (int64_t)tiles);
     int splits = (int)(most < 8 ? most : 8);
     if (splits > steps / 2) splits = (int)(steps / 2);
     if (splits < 1) splits = 1;
-    if (a.whole == 3 && dtype != CT_DT_F32 && x_dtype == dtype) return ad_shrink_tc(a, dtype == CT_DT_BF16, trans, o, tiles, splits, st);
-    return trans ? by_type<true>(a, x_dtype, dtype, o, tiles, splits, st) : by_type<false>(a, x_dtype, dtype, o, tiles, splits, st);
+    const int whole = a[0].whole & a[which == AD_BOTH].whole;
+    if (whole == 3 && dtype != CT_DT_F32 && x_dtype == dtype) return ad_shrink_tc(a, which, dtype == CT_DT_BF16, o, tiles, splits, st);
+    const AdShrinks two = {{a[0], a[1]}};
+    return which == AD_FORWARD    ? by_type<AD_FORWARD>(two, x_dtype, dtype, o, tiles, splits, st)
+           : which == AD_BACKWARD ? by_type<AD_BACKWARD>(two, x_dtype, dtype, o, tiles, splits, st)
+                                  : by_type<AD_BOTH>(two, x_dtype, dtype, o, tiles, splits, st);
 }
 
 }  // namespace ops

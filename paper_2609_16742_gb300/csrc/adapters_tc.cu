@@ -56,7 +56,8 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 // what this thread wrote to shared memory is seen by the tensor cores
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// the barriers that a CTA's products arrive on, and its tensor memory
+// The barriers that a CTA's products arrive on, and its tensor memory.  It is taken after the kernel before has ended and before the next may
+// begin: no CTA holds some while it waits for a kernel that may want it.
 template <int BARS, int COLUMNS> __device__ __forceinline__ uint32_t tensor_begin(uint64_t (&bars)[BARS], uint32_t &holder) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < BARS; ++i) tc::mbar_init(tc::smem_u32(&bars[i]), 1);
@@ -90,50 +91,59 @@ template <int RP> struct Shrink {
 };
 
 template <typename T, int RP, bool TRANS>
-__global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink a, const AdOrder o, int splits, uint32_t *err) {
+__device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o, const AdRows &tile, int rank, int splits, unsigned char *raw,
+                                            uint32_t bar, uint32_t tmem, uint32_t *err) {
     using S = Shrink<RP>;
-    extern __shared__ __align__(128) unsigned char raw[];
-    __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
-    __shared__ uint32_t holder;
-    pdl_wait();
-    pdl_trigger();
-    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0;
-    const AdRows tile = ad_tile(o, (int)(blockIdx.x / (unsigned)splits));
-    if (tile.rows == 0 || tile.key == 0 || tile.key > o.adapters) return;       // the whole cluster alike
-    const int adapter = tile.key - 1, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t tmem = tensor_begin<S::STAGES + 3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = (tc::smem_u32(raw) + 1023u) & ~1023u;
-    const int64_t steps = (a.cols + AD_STEP - 1) / AD_STEP;
-    const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
-    const int n = (int)(s1 - s0);
+    const int adapter = tile.key - 1, steps = (int)((a.cols + AD_STEP - 1) / AD_STEP);
+    const int s0 = (int)((int64_t)steps * rank / splits), n = (int)((int64_t)steps * (rank + 1) / splits) - s0;
 
-    const T *xr[4];
-    bool xh[4];
-    const int xc = (tid & 7) * 8;
+    // Each thread's copies, a step's worth further on with each step: of x, rows tid / 8 + 32 i, 16 bytes at 16 (tid % 8)
+    const char *xp[4], *mp[S::MV];
+    bool xh[4], mh[S::MV];
+    const int64_t c0 = (int64_t)s0 * AD_STEP;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = tid / 8 + 32 * i;
         const int64_t s = tile.slot0 + r;
         xh[i] = r < tile.rows;
-        xr[i] = static_cast<const T *>(a.x) + (xh[i] ? (o.order != nullptr ? (int64_t)o.order[s] : s) * a.ldx : 0);
+        xp[i] = reinterpret_cast<const char *>(static_cast<const T *>(a.x) +
+                                               (xh[i] ? (o.order != nullptr ? (int64_t)o.order[s] : s) * a.ldx : 0) + c0 + (tid & 7) * 8);
     }
-    const T *m = static_cast<const T *>(a.m) + adapter * a.m_adapter;
     using MT = Tile<TRANS ? RP : AD_STEP>;
-    const uint32_t x_to = Tile<AD_STEP>::at(tid / 8, tid & 7, AD_ROWS);
-    auto copy = [&](int step) {
-        const uint32_t bx = base + (step % S::STAGES) * S::STAGE, bm = bx + S::X_BYTES;
-        const int64_t c0 = (s0 + step) * AD_STEP, c = c0 + xc;
+    uint32_t m_to[S::MV];
+    int m_left[S::MV];                            // steps whose values are there
 #pragma unroll
-        for (int i = 0; i < 4; ++i) copy16_if(bx + x_to + 32 * i * 128, xr[i] + (c < a.cols ? c : 0), xh[i] && c < a.cols);
+    for (int i = 0; i < S::MV; ++i) {
+        const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS, j = TRANS ? q * 8 : r;
+        const int64_t c = c0 + (TRANS ? r : q * 8);
+        mh[i] = v < RP * 8;
+        m_to[i] = MT::at(r, q, TRANS ? AD_STEP : RP);
+        m_left[i] = j < a.rank && c < a.cols ? (int)((a.cols - c + AD_STEP - 1) / AD_STEP) : 0;
+        mp[i] = reinterpret_cast<const char *>(static_cast<const T *>(a.m) + adapter * a.m_adapter +
+                                               (m_left[i] > 0 ? (TRANS ? c * a.m_row + j : j * a.m_row + c) : 0));
+    }
+    const int64_t m_step = 2 * (TRANS ? AD_STEP * a.m_row : AD_STEP);
+    const int x_left = c0 + (tid & 7) * 8 < a.cols ? (int)((a.cols - c0 - (tid & 7) * 8 + AD_STEP - 1) / AD_STEP) : 0;
+    const uint32_t x_to = Tile<AD_STEP>::at(tid / 8, tid & 7, AD_ROWS);
+    int to_copy = 0, copy_stage = 0;              // the next step to copy, its stage
+    auto copy = [&]() {
+        const uint32_t bx = base + copy_stage * S::STAGE, bm = bx + S::X_BYTES;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool there = xh[i] && to_copy < x_left;
+            copy16_if(bx + x_to + 32 * i * 128, there ? xp[i] : static_cast<const char *>(a.x), there);
+            xp[i] += 2 * AD_STEP;
+        }
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
-            const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS;
-            if (v >= RP * 8) break;
-            const int64_t cm = TRANS ? c0 + r : c0 + q * 8;
-            const int j = TRANS ? q * 8 : r;
-            const bool there = cm < a.cols && j < a.rank;
-            copy16_if(bm + MT::at(r, q, TRANS ? AD_STEP : RP), m + (there ? (TRANS ? cm * a.m_row + j : j * a.m_row + cm) : 0), there);
+            const bool there = to_copy < m_left[i];
+            if (mh[i]) copy16_if(bm + m_to[i], there ? mp[i] : static_cast<const char *>(a.m), there);
+            mp[i] += m_step;
         }
+        ++to_copy;
+        copy_stage = copy_stage + 1 == S::STAGES ? 0 : copy_stage + 1;
     };
     float sum[RP / 2];
 #pragma unroll
@@ -157,18 +167,19 @@ __global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink
     };
 #pragma unroll
     for (int i = 0; i < S::STAGES - 1; ++i) {
-        if (i < n) copy(i);
+        if (i < n) copy();
         copies_end();
     }
     constexpr uint32_t how = product(Parts<T>::N == 1, false, TRANS, AD_ROWS, RP);
-    int at = 0;
+    int at = 0, stage = 0, before = S::STAGES - 1;                               // the step, its stage, that of the step before
+    uint32_t done = 0;                            // bit s: parity of stage s's next end of products
     for (; at < n; ++at) {
         copies_wait<S::STAGES - 2>();
         fence_operands();
         if (!__syncthreads_and(ok)) break;
         if (warp == 0 && tc::elect_one()) {
             fence_after();
-            const uint32_t bx = base + (at % S::STAGES) * S::STAGE, bm = bx + S::X_BYTES;
+            const uint32_t bx = base + stage * S::STAGE, bm = bx + S::X_BYTES;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const uint64_t da = operand(bx + 32 * k, 16, 1024, SW128);
@@ -176,15 +187,22 @@ __global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink
                                           : operand(bm + 32 * k, 16, 1024, SW128);
                 tc::umma_f16(tmem + (at / FLUSH & 1) * RP, da, db, how, at % FLUSH > 0 || k > 0);
             }
-            tc::umma_commit(bar + 8 * (at % S::STAGES));
+            tc::umma_commit(bar + 8 * stage);
             if (at % FLUSH == FLUSH - 1 || at == n - 1) tc::umma_commit(bar + 8 * (S::STAGES + (at / FLUSH & 1)));
         }
         __syncwarp();
-        if (at > 0 && at + S::STAGES - 1 < n)
-            ok = ok && tc::mbar_wait(bar + 8 * ((at - 1) % S::STAGES), (at - 1) / S::STAGES & 1, err, E_ADAPTERS);
-        if (ok && at + S::STAGES - 1 < n) copy(at + S::STAGES - 1);
+        if (at + S::STAGES - 1 < n) {
+            // into the stage of the step before, once its products are done
+            if (at > 0) {
+                ok = ok && tc::mbar_wait(bar + 8 * before, done >> before & 1, err, E_ADAPTERS);
+                done ^= 1u << before;
+            }
+            if (ok) copy();
+        }
         copies_end();
         if (at % FLUSH == 1 && at > FLUSH) collect();
+        before = stage;
+        stage = stage + 1 == S::STAGES ? 0 : stage + 1;
     }
     copies_wait<0>();
     if (at == n) {
@@ -203,6 +221,46 @@ __global__ void __launch_bounds__(AD_THREADS, 2) shrink_tc_kernel(const AdShrink
     else __syncthreads();
     write_vectors<RP>(a, o, tile, adapter, reinterpret_cast<const float *>(raw), rank, splits);
     if (splits > 1) tc::cluster_sync();           // no CTA leaves while another reads its sums
+}
+
+// The rows of x that a CTA would have if they were in order already, on their way to L2 while the order is made (which touches
+// nothing of x, and has itself waited for all before it).
+__device__ __forceinline__ void shrink_ahead(const AdShrink &a, int size, int64_t t, int tile, int rank, int splits) {
+    const int steps = (int)((a.cols + AD_STEP - 1) / AD_STEP), s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
+    const int64_t row = (int64_t)tile * AD_ROWS + threadIdx.x / 2;
+    if (row >= t) return;
+    const char *p = static_cast<const char *>(a.x) + row * a.ldx * size;
+    for (int s = s0 + (threadIdx.x & 1); s < s1; s += 2) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + (int64_t)s * AD_STEP * size));
+}
+
+// x A^T, or (WHICH 1) dy B, or both: the tiles of the first, then those of the second
+struct AdShrinks {
+    AdShrink a[2];
+};
+constexpr int FORWARD = AD_FORWARD, BACKWARD = AD_BACKWARD, BOTH = AD_BOTH;
+template <typename T, int RP, int WHICH>
+__global__ void __launch_bounds__(AD_THREADS, 2)
+shrink_tc_kernel(const __grid_constant__ AdShrinks two, const AdOrder o, int tiles, int splits, uint32_t *err) {
+    using S = Shrink<RP>;
+    extern __shared__ __align__(128) unsigned char raw[];
+    __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
+    __shared__ uint32_t holder;
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0;
+    int t = (int)(blockIdx.x / (unsigned)splits);
+    const bool second = WHICH == BACKWARD || (WHICH == BOTH && t >= tiles);
+    if (WHICH == BOTH && second) t -= tiles;
+    const AdShrink &a = two.a[WHICH == BOTH && second];
+    if (a.first && o.order != nullptr) shrink_ahead(a, 2, o.t, t, rank, splits);
+    pdl_wait();
+    const uint32_t tmem = tensor_begin<S::STAGES + 3, S::COLUMNS>(bars, holder);
+    pdl_trigger();
+    const AdRows tile = ad_tile(o, t);
+    if (tile.rows == 0 || tile.key == 0 || tile.key > o.adapters) {             // the whole cluster alike
+        tensor_end<S::COLUMNS>(tmem);
+        return;
+    }
+    if (WHICH == FORWARD || (WHICH == BOTH && !second)) shrink_tile<T, RP, false>(a, o, tile, rank, splits, raw, tc::smem_u32(bars), tmem, err);
+    else shrink_tile<T, RP, true>(a, o, tile, rank, splits, raw, tc::smem_u32(bars), tmem, err);
 }
 
 // ---------------------------------------------------------------- expand
@@ -246,41 +304,55 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
     extern __shared__ __align__(128) unsigned char raw[];
     __shared__ uint64_t bars[3];                  // a block's products are done (two, in turn); all
     __shared__ uint32_t holder;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_wait();
+    const uint32_t tmem = tensor_begin<3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
     pdl_trigger();
     const AdRows tile = ad_tile(o, (int)blockIdx.x);
     const int64_t c_from = (int64_t)blockIdx.y * a.per, c_to = min(c_from + a.per, a.cols);
-    if (tile.rows == 0 || c_from >= c_to || (tile.key == 0 && !a.relu)) return;
+    if (tile.rows == 0 || c_from >= c_to || (tile.key == 0 && !a.relu)) {
+        tensor_end<S::COLUMNS>(tmem);
+        return;
+    }
     const bool out = tile.key > o.adapters, none = tile.key == 0;               // NaN; act alone
     const bool product_wanted = !out && !none;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t tmem = tensor_begin<3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
     const uint32_t vb = (tc::smem_u32(raw) + 1023u) & ~1023u, mb = vb + a.parts * S::V_BYTES;
     const __nv_bfloat16 *m = static_cast<const __nv_bfloat16 *>(a.m) + (product_wanted ? (int64_t)(tile.key - 1) * a.m_adapter : 0);
     const int n = (int)((c_to - c_from + S::COLS - 1) / S::COLS);
     using VT = Tile<RP>;
     using MT = Tile<TRANS ? S::COLS : RP>;
+    // each thread's copies of the matrix, a block further on with each block
+    const char *mp[S::MV];
+    uint32_t m_to[S::MV];
+    int m_left[S::MV];                            // blocks whose values are there
+#pragma unroll
+    for (int i = 0; i < S::MV; ++i) {
+        const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS, j = TRANS ? r : q * 8;
+        const int64_t c = c_from + (TRANS ? q * 8 : r);
+        m_left[i] = v < S::COLS * (RP / 8) ? j < a.rank && c < a.cols ? (int)((a.cols - c + S::COLS - 1) / S::COLS) : 0 : -1;
+        m_to[i] = MT::at(TRANS ? r : S::dealt(r), q, TRANS ? RP : S::COLS);
+        mp[i] = reinterpret_cast<const char *>(m + (m_left[i] > 0 ? (TRANS ? j * a.m_row + c : c * a.m_row + j) : 0));
+    }
+    const int64_t m_step = 2 * (TRANS ? S::COLS : S::COLS * a.m_row);
     auto copy = [&](int b) {
         const uint32_t bm = mb + (b % S::STAGES) * S::M_BYTES;
-        const int64_t c0 = c_from + (int64_t)b * S::COLS;
 #pragma unroll
         for (int i = 0; i < S::MV; ++i) {
-            const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS;
-            if (v >= S::COLS * (RP / 8)) break;
-            const int64_t c = TRANS ? c0 + q * 8 : c0 + r;
-            const int j = TRANS ? r : q * 8;
-            const bool there = c < a.cols && j < a.rank;
+            if (m_left[i] < 0) break;
+            const bool there = b < m_left[i];
+            const char *p = there ? mp[i] : reinterpret_cast<const char *>(m);
             if constexpr (TRANS) {
                 // four pairs of columns, each to its place
-                const char *p = reinterpret_cast<const char *>(m + (there ? j * a.m_row + c : 0));
+                const int v = tid + i * AD_THREADS, r = v / MT::CHUNKS, q = v % MT::CHUNKS;
 #pragma unroll
                 for (int i2 = 0; i2 < 4; ++i2) {
                     const int to = S::dealt(q * 8 + 2 * i2);
                     copy4_if(bm + MT::at(r, to / 8, RP) + to % 8 * 2, p + 4 * i2, there);
                 }
             } else {
-                copy16_if(bm + MT::at(S::dealt(r), q, S::COLS), m + (there ? c * a.m_row + j : 0), there);
+                copy16_if(bm + m_to[i], p, there);
             }
+            mp[i] += m_step;
         }
     };
     if (product_wanted) {
@@ -308,17 +380,20 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
         yr[i] = static_cast<char *>(a.y) + (have[i] ? (o.order != nullptr ? (int64_t)o.order[tile.slot0 + row] : tile.slot0 + row) * a.ldy * YS : 0);
     }
     const float nan = __uint_as_float(0x7FC00000u);
-    uint4 y[G][4];
-    auto y_fetch = [&](int b) {
+    using Y = uint4[G][4];
+    Y even, odd;                                  // y of the blocks of even and of odd number, two ahead
+    auto y_fetch = [&](int b, Y &y) {
         const int64_t c = c_from + (int64_t)b * S::COLS + lane_c;
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[g][i] = ld_if(yr[i] + (c + g * 4 * W) * YS, have[i] && c + g * 4 * W < c_to);
     };
+    y_fetch(0, even);
+    y_fetch(1, odd);
     const uint32_t mine = tmem + ((uint32_t)(warp & 3) << 21) + (uint32_t)half;
     // adds a block's sums (none where there is no product) to y
-    auto finish = [&](int b) {
+    auto finish = [&](int b, const Y &y) {
         const int64_t c = c_from + (int64_t)b * S::COLS + lane_c;
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -352,57 +427,66 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
     };
     bool ok = true;
     constexpr uint32_t how = product(true, false, TRANS, AD_ROWS, S::COLS);
+    // one block's products on their way, those of the block before (whose y is given) into y, the y of the block after next
+    auto advance = [&](int b, Y &y) -> bool {
+        copies_wait<S::STAGES - 2>();
+        fence_operands();
+        fence_before();
+        if (!__syncthreads_and(ok)) return false;
+        if (warp == 0 && tc::elect_one()) {
+            fence_after();
+            const uint32_t bm = mb + (b % S::STAGES) * S::M_BYTES;
+            for (int p = 0; p < a.parts; ++p)
+#pragma unroll
+                for (int k = 0; k < RP / 16; ++k) {
+                    // 16 values along the rank: 32 bytes of a row, in the next block of 64 after four
+                    const uint32_t av = vb + p * S::V_BYTES + (k >> 2) * AD_ROWS * 128 + (k & 3) * 32;
+                    const uint64_t da = operand(av, 16, 8 * VT::ROW, VT::SWIZZLE);
+                    const uint64_t db = TRANS ? operand(bm + 16 * k * 128, RP * 128, 1024, SW128)
+                                              : operand(bm + (k >> 2) * S::COLS * 128 + (k & 3) * 32, 16, 8 * MT::ROW, MT::SWIZZLE);
+                    tc::umma_f16(tmem + (b & 1) * S::COLS, da, db, how, p > 0 || k > 0);
+                }
+            tc::umma_commit(bar + 8 * (b & 1));
+        }
+        __syncwarp();
+        if (b > 0) {
+            ok = ok && tc::mbar_wait(bar + 8 * (b - 1 & 1), (b - 1) >> 1 & 1, err, E_ADAPTERS);
+            __syncwarp();
+        }
+        if (ok && b + S::STAGES - 1 < n) copy(b + S::STAGES - 1);               // into the stage whose products are done
+        copies_end();
+        if (b > 0 && ok) {
+            fence_after();
+            finish(b - 1, y);
+            y_fetch(b + 1, y);
+        }
+        return true;
+    };
     int b = 0;
     if (product_wanted) {
-        for (; b < n; ++b) {
-            copies_wait<S::STAGES - 2>();
-            fence_operands();
-            fence_before();
-            if (!__syncthreads_and(ok)) break;
-            if (warp == 0 && tc::elect_one()) {
-                fence_after();
-                const uint32_t bm = mb + (b % S::STAGES) * S::M_BYTES;
-                for (int p = 0; p < a.parts; ++p)
-#pragma unroll
-                    for (int k = 0; k < RP / 16; ++k) {
-                        // 16 values along the rank: 32 bytes of a row, in the next block of 64 after four
-                        const uint32_t av = vb + p * S::V_BYTES + (k >> 2) * AD_ROWS * 128 + (k & 3) * 32;
-                        const uint64_t da = operand(av, 16, 8 * VT::ROW, VT::SWIZZLE);
-                        const uint64_t db = TRANS ? operand(bm + 16 * k * 128, RP * 128, 1024, SW128)
-                                                  : operand(bm + (k >> 2) * S::COLS * 128 + (k & 3) * 32, 16, 8 * MT::ROW, MT::SWIZZLE);
-                        tc::umma_f16(tmem + (b & 1) * S::COLS, da, db, how, p > 0 || k > 0);
-                    }
-                tc::umma_commit(bar + 8 * (b & 1));
-            }
-            __syncwarp();
-            if (b > 0) {
-                ok = ok && tc::mbar_wait(bar + 8 * (b - 1 & 1), (b - 1) >> 1 & 1, err, E_ADAPTERS);
-                __syncwarp();
-                if (ok && b + S::STAGES - 1 < n) copy(b + S::STAGES - 1);       // into the stage whose products are done
-            } else if (S::STAGES - 1 < n) {
-                copy(S::STAGES - 1);
-            }
-            copies_end();
-            if (b > 0 && ok) {
-                fence_after();
-                finish(b - 1);
-            }
-            y_fetch(b);
+        for (; b < n; b += 2) {
+            if (!advance(b, odd)) break;
+            if (b + 1 < n && !advance(b + 1, even)) break;
         }
         copies_wait<0>();
-        if (b == n) {
+        if (b >= n) {
             ok = ok && tc::mbar_wait(bar + 8 * (n - 1 & 1), (n - 1) >> 1 & 1, err, E_ADAPTERS);
             __syncwarp();
             fence_after();
-            if (ok) finish(n - 1);
+            if (ok && (n & 1)) finish(n - 1, even);
+            else if (ok) finish(n - 1, odd);
         } else {
             if (warp == 0 && tc::elect_one()) tc::umma_commit(bar + 16);        // gave up: what was issued, before its memory goes
             tc::mbar_wait(bar + 16, 0, err, E_ADAPTERS);
         }
     } else {
-        for (; b < n; ++b) {
-            y_fetch(b);
-            finish(b);
+        for (; b < n; b += 2) {
+            finish(b, even);
+            y_fetch(b + 2, even);
+            if (b + 1 < n) {
+                finish(b + 1, odd);
+                y_fetch(b + 3, odd);
+            }
         }
     }
     tensor_end<S::COLUMNS>(tmem);
@@ -422,43 +506,67 @@ template <int RP, int PARTS> struct Outer {
 };
 
 template <int RP, int PARTS>
-__global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const AdOuter a, const AdOrder o, int splits, uint32_t *err) {
+__global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int splits, uint32_t *err) {
     using S = Outer<RP, PARTS>;
     extern __shared__ __align__(128) unsigned char raw[];
     __shared__ uint64_t bars[S::STAGES + 3];      // a stage's products are done; a group's sums are there (two, in turn); all
     __shared__ uint32_t holder;
+    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, adapter = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int block = (int)(blockIdx.x / (unsigned)splits);
+    const AdOuter &a = two.a[block >= two.first];
+    const int64_t cols0 = (int64_t)(block >= two.first ? block - two.first : block) * OUTER_COLS;
     pdl_wait();
-    pdl_trigger();
-    const int rank = splits > 1 ? (int)tc::cluster_ctarank() : 0, adapter = blockIdx.y;
-    const int64_t cols0 = (int64_t)(blockIdx.x / (unsigned)splits) * OUTER_COLS;
-    const int64_t from = o.order != nullptr ? o.first[adapter + 1] : 0, to = o.order != nullptr ? o.end[adapter + 1] : adapter == 0 ? o.t : 0;
-    const int64_t steps = (to - from + AD_STEP - 1) / AD_STEP;
-    const int64_t s0 = steps * rank / splits, s1 = steps * (rank + 1) / splits;
-    const int n = (int)(s1 - s0), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t tmem = tensor_begin<S::STAGES + 3, S::COLUMNS>(bars, holder), bar = tc::smem_u32(bars);
     const uint32_t base = (tc::smem_u32(raw) + 1023u) & ~1023u;
+    pdl_trigger();
+    const int64_t from = o.order != nullptr ? o.first[adapter + 1] : 0, to = o.order != nullptr ? o.end[adapter + 1] : adapter == 0 ? o.t : 0;
+    const int64_t steps = (to - from + AD_STEP - 1) / AD_STEP;
+    const int64_t s0 = steps * rank / splits, t0 = from + s0 * AD_STEP;
+    const int n = (int)(steps * (rank + 1) / splits - s0), left = (int)min((int64_t)n * AD_STEP, to - t0);      // steps, rows
     using XT = Tile<OUTER_COLS>;
     using VT = Tile<RP>;
+    // Each thread's copies, 64 rows further on with each step: of x, rows tid / 16 + 16 i, 16 bytes at 16 (tid % 16)
     const int64_t xc = cols0 + (tid & 15) * 8;
-    const __nv_bfloat16 *x0 = static_cast<const __nv_bfloat16 *>(a.x) + (xc < a.cols ? xc : 0);
-    auto copy = [&](int step) {
-        const uint32_t bx = base + (step % S::STAGES) * S::STAGE, bv = bx + S::X_BYTES;
-        const int64_t t0 = from + (s0 + step) * AD_STEP;
+    const bool x_there = xc < a.cols;
+    const char *x0 = reinterpret_cast<const char *>(static_cast<const __nv_bfloat16 *>(a.x) + (x_there ? xc : 0));
+    const uint32_t x_to = XT::at(tid / 16, tid & 15, AD_STEP);
+    int32_t next[4];                              // the rows of the next step to copy
+    auto rows_of = [&](int step) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = tid / 16 + 16 * i;
-            const int64_t t = t0 + r;
-            const bool there = t < to && xc < a.cols;
-            copy16_if(bx + XT::at(r, tid & 15, AD_STEP), x0 + (there ? (o.order != nullptr ? (int64_t)o.order[t] : t) * a.ldx : 0), there);
+            const int r = step * AD_STEP + tid / 16 + 16 * i;
+            next[i] = o.order == nullptr ? (int32_t)(t0 + r) : r < left ? o.order[t0 + r] : 0;
+        }
+    };
+    rows_of(0);
+    const uint4 *vp[S::VV];
+    uint32_t v_to[S::VV];
+    int v_row[S::VV];
+#pragma unroll
+    for (int i = 0; i < S::VV; ++i) {
+        const int v = tid + i * AD_THREADS, p = v / (AD_STEP * (RP / 8)), r = v / (RP / 8) % AD_STEP, q = v % (RP / 8);
+        v_row[i] = v < AD_STEP * (RP / 8) * PARTS ? r : INT32_MAX / 2;
+        v_to[i] = p * S::V_BYTES + VT::at(r, q, AD_STEP);
+        vp[i] = static_cast<const uint4 *>(a.v) + ((p < PARTS ? p : 0) * o.t + t0 + r) * (RP / 8) + q;
+    }
+    int to_copy = 0, copy_stage = 0;              // the next step to copy, its stage
+    auto copy = [&]() {
+        const uint32_t bx = base + copy_stage * S::STAGE, bv = bx + S::X_BYTES;
+        const int rest = left - to_copy * AD_STEP;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool there = x_there && tid / 16 + 16 * i < rest;
+            copy16_if(bx + x_to + 16 * i * 128, x0 + (there ? (int64_t)next[i] * a.ldx * 2 : 0), there);
         }
 #pragma unroll
         for (int i = 0; i < S::VV; ++i) {
-            const int v = tid + i * AD_THREADS, p = v / (AD_STEP * (RP / 8)), r = v / (RP / 8) % AD_STEP, q = v % (RP / 8);
-            if (v >= AD_STEP * (RP / 8) * PARTS) break;
-            const int64_t t = t0 + r;
-            const bool there = t < to;
-            copy16_if(bv + p * S::V_BYTES + VT::at(r, q, AD_STEP), static_cast<const uint4 *>(a.v) + (there ? (p * o.t + t) * (RP / 8) + q : 0), there);
+            const bool there = v_row[i] < rest;
+            if (v_row[i] < AD_STEP) copy16_if(bv + v_to[i], there ? vp[i] : static_cast<const uint4 *>(a.v), there);
+            vp[i] += AD_STEP * (RP / 8);
         }
+        ++to_copy;
+        copy_stage = copy_stage + 1 == S::STAGES ? 0 : copy_stage + 1;
+        rows_of(to_copy);
     };
     float sum[RP / 2];
 #pragma unroll
@@ -488,31 +596,39 @@ __global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const AdOuter a, c
     };
 #pragma unroll
     for (int i = 0; i < S::STAGES - 1; ++i) {
-        if (i < n) copy(i);
+        if (i < n) copy();
         copies_end();
     }
     constexpr uint32_t how = product(true, true, true, OUTER_COLS, S::N);
-    int at = 0;
+    int at = 0, stage = 0, before = S::STAGES - 1;                               // the step, its stage, that of the step before
+    uint32_t done = 0;                            // bit s: parity of stage s's next end of products
     for (; at < n; ++at) {
         copies_wait<S::STAGES - 2>();
         fence_operands();
         if (!__syncthreads_and(ok)) break;
         if (warp == 0 && tc::elect_one()) {
             fence_after();
-            const uint32_t bx = base + (at % S::STAGES) * S::STAGE, bv = bx + S::X_BYTES;
+            const uint32_t bx = base + stage * S::STAGE, bv = bx + S::X_BYTES;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 tc::umma_f16(tmem + (at / FLUSH & 1) * S::N, operand(bx + 16 * k * 128, AD_STEP * 128, 1024, SW128),
                              operand(bv + 16 * k * VT::ROW, AD_STEP * VT::ROW, 8 * VT::ROW, VT::SWIZZLE), how, at % FLUSH > 0 || k > 0);
-            tc::umma_commit(bar + 8 * (at % S::STAGES));
+            tc::umma_commit(bar + 8 * stage);
             if (at % FLUSH == FLUSH - 1 || at == n - 1) tc::umma_commit(bar + 8 * (S::STAGES + (at / FLUSH & 1)));
         }
         __syncwarp();
-        if (at > 0 && at + S::STAGES - 1 < n)
-            ok = ok && tc::mbar_wait(bar + 8 * ((at - 1) % S::STAGES), (at - 1) / S::STAGES & 1, err, E_ADAPTERS);
-        if (ok && at + S::STAGES - 1 < n) copy(at + S::STAGES - 1);
+        if (at + S::STAGES - 1 < n) {
+            // into the stage of the step before, once its products are done
+            if (at > 0) {
+                ok = ok && tc::mbar_wait(bar + 8 * before, done >> before & 1, err, E_ADAPTERS);
+                done ^= 1u << before;
+            }
+            if (ok) copy();
+        }
         copies_end();
         if (at % FLUSH == 1 && at > FLUSH) collect();
+        before = stage;
+        stage = stage + 1 == S::STAGES ? 0 : stage + 1;
     }
     copies_wait<0>();
     if (at == n) {
@@ -534,21 +650,21 @@ __global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const AdOuter a, c
 
 // ---------------------------------------------------------------- host
 
-template <typename T, int RP, bool TRANS> cudaError_t shrink(const AdShrink &a, const AdOrder &o, int tiles, int splits, uint32_t *err, cudaStream_t st) {
+template <typename T, int RP, int WHICH> cudaError_t shrink(const AdShrinks &two, const AdOrder &o, int tiles, int splits, uint32_t *err, cudaStream_t st) {
     using S = Shrink<RP>;
     static std::atomic<bool> sized[MAX_DEVICES];
-    auto *kernel = shrink_tc_kernel<T, RP, TRANS>;
+    auto *kernel = shrink_tc_kernel<T, RP, WHICH>;
     const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
     if (e != cudaSuccess) return e;
-    if (splits == 1) return pdl_launch(kernel, dim3((unsigned)tiles), dim3(AD_THREADS), S::SMEM, st, a, o, splits, err);
-    return pdl_launch_cluster(kernel, dim3((unsigned)(tiles * splits)), dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits, err);
+    const dim3 grid((unsigned)((WHICH == BOTH ? 2 : 1) * tiles * splits));
+    return ad_launch(kernel, grid, S::SMEM, st, splits, two.a[0].first && o.order != nullptr, two, o, tiles, splits, err);
 }
-template <typename T, bool TRANS> cudaError_t shrink_rank(const AdShrink &a, const AdOrder &o, int tiles, int splits, uint32_t *err, cudaStream_t st) {
-    switch (ad_padded(a.rank)) {
-        case 16: return shrink<T, 16, TRANS>(a, o, tiles, splits, err, st);
-        case 32: return shrink<T, 32, TRANS>(a, o, tiles, splits, err, st);
-        case 64: return shrink<T, 64, TRANS>(a, o, tiles, splits, err, st);
-        default: return shrink<T, 128, TRANS>(a, o, tiles, splits, err, st);
+template <typename T, int WHICH> cudaError_t shrink_rank(const AdShrinks &two, const AdOrder &o, int tiles, int splits, uint32_t *err, cudaStream_t st) {
+    switch (ad_padded(two.a[0].rank)) {
+        case 16: return shrink<T, 16, WHICH>(two, o, tiles, splits, err, st);
+        case 32: return shrink<T, 32, WHICH>(two, o, tiles, splits, err, st);
+        case 64: return shrink<T, 64, WHICH>(two, o, tiles, splits, err, st);
+        default: return shrink<T, 128, WHICH>(two, o, tiles, splits, err, st);
     }
 }
 
@@ -567,7 +683,7 @@ template <int RP, bool TRANS, int YS> cudaError_t expand(const AdExpand &q, cons
     if (parts > 65535) parts = 65535;
     a.per = (blocks + parts - 1) / parts * S::COLS;
     const dim3 grid((unsigned)tiles, (unsigned)((a.cols + a.per - 1) / a.per));
-    return pdl_launch(kernel, grid, dim3(AD_THREADS), (size_t)S::smem(a.parts), st, a, o, err);
+    return ad_launch(kernel, grid, (size_t)S::smem(a.parts), st, 1, false, a, o, err);
 }
 template <bool TRANS, int YS> cudaError_t expand_rank(const AdExpand &a, const AdOrder &o, int tiles, uint32_t *err, cudaStream_t st) {
     switch (ad_padded(a.rank)) {
@@ -578,23 +694,28 @@ template <bool TRANS, int YS> cudaError_t expand_rank(const AdExpand &a, const A
     }
 }
 
-template <int RP, int PARTS> cudaError_t outer(const AdOuter &a, const AdOrder &o, int splits, uint32_t *err, cudaStream_t st) {
+template <int RP, int PARTS> cudaError_t outer(const AdOuters &two, int blocks, const AdOrder &o, int splits, uint32_t *err, cudaStream_t st) {
     using S = Outer<RP, PARTS>;
     static std::atomic<bool> sized[MAX_DEVICES];
     auto *kernel = outer_tc_kernel<RP, PARTS>;
     const cudaError_t e = allow_smem(kernel, sized, S::SMEM);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)((a.cols + OUTER_COLS - 1) / OUTER_COLS * splits), (unsigned)o.adapters);
-    if (splits == 1) return pdl_launch(kernel, grid, dim3(AD_THREADS), S::SMEM, st, a, o, splits, err);
-    return pdl_launch_cluster(kernel, grid, dim3(AD_THREADS), S::SMEM, st, splits, a, o, splits, err);
+    const dim3 grid((unsigned)(blocks * splits), (unsigned)o.adapters);
+    return ad_launch(kernel, grid, S::SMEM, st, splits, false, two, o, splits, err);
 }
 }  // namespace
 
-cudaError_t ad_shrink_tc(const AdShrink &a, bool bf16, bool trans, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
+cudaError_t ad_shrink_tc(const AdShrink (&a)[2], AdWhich which, bool bf16, const AdOrder &o, int tiles, int splits, cudaStream_t st) {
     uint32_t *err = device_error_word();
     if (err == nullptr) return cudaErrorUnknown;
-    if (bf16) return trans ? shrink_rank<__nv_bfloat16, true>(a, o, tiles, splits, err, st) : shrink_rank<__nv_bfloat16, false>(a, o, tiles, splits, err, st);
-    return trans ? shrink_rank<__half, true>(a, o, tiles, splits, err, st) : shrink_rank<__half, false>(a, o, tiles, splits, err, st);
+    const AdShrinks two = {{a[0], a[1]}};
+    if (bf16)
+        return which == AD_FORWARD    ? shrink_rank<__nv_bfloat16, FORWARD>(two, o, tiles, splits, err, st)
+               : which == AD_BACKWARD ? shrink_rank<__nv_bfloat16, BACKWARD>(two, o, tiles, splits, err, st)
+                                      : shrink_rank<__nv_bfloat16, BOTH>(two, o, tiles, splits, err, st);
+    return which == AD_FORWARD    ? shrink_rank<__half, FORWARD>(two, o, tiles, splits, err, st)
+           : which == AD_BACKWARD ? shrink_rank<__half, BACKWARD>(two, o, tiles, splits, err, st)
+                                  : shrink_rank<__half, BOTH>(two, o, tiles, splits, err, st);
 }
 cudaError_t ad_expand_tc(const AdExpand &a, bool trans, const AdOrder &o, int tiles, cudaStream_t st) {
     uint32_t *err = device_error_word();
@@ -603,14 +724,15 @@ cudaError_t ad_expand_tc(const AdExpand &a, bool trans, const AdOrder &o, int ti
     return trans ? expand_rank<true, 2>(a, o, tiles, err, st) : expand_rank<false, 2>(a, o, tiles, err, st);
 }
 bool ad_outer_tc_takes(int64_t rank, int parts) { return ad_padded(rank) * parts <= 256; }
-cudaError_t ad_outer_tc(const AdOuter &a, const AdOrder &o, int splits, cudaStream_t st) {
+cudaError_t ad_outer_tc(const AdOuters &two, int blocks, const AdOrder &o, int splits, cudaStream_t st) {
     uint32_t *err = device_error_word();
     if (err == nullptr) return cudaErrorUnknown;
-    switch (ad_padded(a.rank)) {
-        case 16: return a.parts == 2 ? outer<16, 2>(a, o, splits, err, st) : outer<16, 3>(a, o, splits, err, st);
-        case 32: return a.parts == 2 ? outer<32, 2>(a, o, splits, err, st) : outer<32, 3>(a, o, splits, err, st);
-        case 64: return a.parts == 2 ? outer<64, 2>(a, o, splits, err, st) : outer<64, 3>(a, o, splits, err, st);
-        default: return outer<128, 2>(a, o, splits, err, st);
+    const bool p2 = two.a[0].parts == 2;
+    switch (ad_padded(two.a[0].rank)) {
+        case 16: return p2 ? outer<16, 2>(two, blocks, o, splits, err, st) : outer<16, 3>(two, blocks, o, splits, err, st);
+        case 32: return p2 ? outer<32, 2>(two, blocks, o, splits, err, st) : outer<32, 3>(two, blocks, o, splits, err, st);
+        case 64: return p2 ? outer<64, 2>(two, blocks, o, splits, err, st) : outer<64, 3>(two, blocks, o, splits, err, st);
+        default: return outer<128, 2>(two, blocks, o, splits, err, st);
     }
 }
 
