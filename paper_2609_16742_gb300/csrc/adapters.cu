@@ -179,34 +179,35 @@ struct FewArgs {
     int relu;
 };
 
-// The rows that row `lead` speaks for: all with its id, if it is the first of them.  Returns their number, 0 if it is not.
+// The rows that row `lead` speaks for: all with its id, if it is the first of them.  Returns their number, 0 if it is not.  At least FEW
+// threads.
 __device__ __forceinline__ int speak_for(const int64_t *ids, int t, int lead, int16_t *rows, int64_t &id) {
-    __shared__ int found, before;
-    const int tid = threadIdx.x;
+    __shared__ uint32_t masks[FEW / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (ids == nullptr) {
         id = 0;
-        for (int i = tid; i < t; i += blockDim.x) rows[i] = (int16_t)i;
+        if (tid < t) rows[tid] = (int16_t)tid;
         __syncthreads();
         return lead == 0 ? t : 0;
     }
+    const int64_t mine = tid < t ? ids[tid] : 0;
     id = ids[lead];
-    if (tid < 32) {
-        int n = 0, early = 0;
-        for (int i0 = 0; i0 < t; i0 += 32) {
-            const int i = i0 + tid;
-            const bool same = i < t && ids[i] == id;
-            const uint32_t all = __ballot_sync(0xffffffffu, same);
-            if (same) rows[n + __popc(all & ((1u << tid) - 1u))] = (int16_t)i;
-            early |= __any_sync(0xffffffffu, same && i < lead);
-            n += __popc(all);
-        }
-        if (tid == 0) {
-            found = n;
-            before = early;
-        }
-    }
+    const bool same = tid < t && mine == id;
+    const uint32_t all = __ballot_sync(0xffffffffu, same);
+    if (lane == 0 && warp < FEW / 32) masks[warp] = all;
     __syncthreads();
-    return before ? 0 : found;
+    int n = 0, before = 0;
+    bool first = true;
+#pragma unroll
+    for (int w = 0; w < FEW / 32; ++w) {
+        if (w < warp) before += __popc(masks[w]);
+        n += __popc(masks[w]);
+        const uint32_t early = lead >= 32 * (w + 1) ? 0xffffffffu : lead <= 32 * w ? 0u : (1u << (lead - 32 * w)) - 1u;
+        first = first && (masks[w] & early) == 0;
+    }
+    if (same) rows[before + __popc(all & ((1u << lane) - 1u))] = (int16_t)tid;
+    __syncthreads();
+    return first ? n : 0;
 }
 
 // Eight values on their way; WHOLE: rows start on 16 bytes and are a multiple of 8 values long.
@@ -425,11 +426,11 @@ template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_ke
 
 template <typename TX, typename TM, bool WHOLE> cudaError_t few_as(const FewArgs &a, cudaStream_t st) {
     if (a.rank > 0) {
-        // as many blocks as are resident together (three for each SM), with a piece of the axis at least for each warp that shares it
+        // as many blocks as are resident together (two for each SM), with a piece of the axis at least for each warp that shares it
         const int64_t pieces = (a.k + 255) / 256;
         const int lead = a.ids != nullptr ? a.t : 1, speak = lead < a.adapters ? lead : a.adapters;
         const int groups = (a.rank + FEW_J - 1) / FEW_J, ways = groups >= FEW_WARPS ? 1 : FEW_WARPS / groups;
-        int splits = 3 * sm_count() / speak;
+        int splits = 2 * sm_count() / speak;
         if (splits > 8) splits = 8;
         if (splits > pieces / ways) splits = (int)(pieces / ways);
         if (splits < 1) splits = 1;

@@ -107,6 +107,8 @@ def test_whole_rows(size, wt):
     import torch
     t, k, n, rank, count = size
     x, a, b, ids, scale = made(t, k, n, rank, count, wt, wt, seed=6)
+    y = like(t, n, "float16", 1)
+    check(y, x, a, b, ids, scale, False, ct().ct_adapters(y.clone(), x, a, b, ids, scale))
     for dt in (wt, "float32"):
         y, dx = like(t, n, dt, 1), like(t, k, dt, 4)
         for relu in (False, True):
