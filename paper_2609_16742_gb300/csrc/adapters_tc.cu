@@ -166,15 +166,15 @@ __device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o,
         ++groups;
     };
 #pragma unroll
-    for (int i = 0; i < S::STAGES - 1; ++i) {
+    for (int i = 0; i < S::STAGES; ++i) {
         if (i < n) copy();
         copies_end();
     }
     constexpr uint32_t how = product(Parts<T>::N == 1, false, TRANS, AD_ROWS, RP);
-    int at = 0, stage = 0, before = S::STAGES - 1;                               // the step, its stage, that of the step before
+    int at = 0, stage = 0;                        // the step, its stage
     uint32_t done = 0;                            // bit s: parity of stage s's next end of products
     for (; at < n; ++at) {
-        copies_wait<S::STAGES - 2>();
+        copies_wait<S::STAGES - 1>();
         fence_operands();
         if (!__syncthreads_and(ok)) break;
         if (warp == 0 && tc::elect_one()) {
@@ -191,17 +191,14 @@ __device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o,
             if (at % FLUSH == FLUSH - 1 || at == n - 1) tc::umma_commit(bar + 8 * (S::STAGES + (at / FLUSH & 1)));
         }
         __syncwarp();
-        if (at + S::STAGES - 1 < n) {
-            // into the stage of the step before, once its products are done
-            if (at > 0) {
-                ok = ok && tc::mbar_wait(bar + 8 * before, done >> before & 1, err, E_ADAPTERS);
-                done ^= 1u << before;
-            }
+        if (at + S::STAGES < n) {
+            // the stage again, once its products are done: they take a fraction of the time that the next stages' copies do
+            ok = ok && tc::mbar_wait(bar + 8 * stage, done >> stage & 1, err, E_ADAPTERS);
+            done ^= 1u << stage;
             if (ok) copy();
         }
         copies_end();
         if (at % FLUSH == 1 && at > FLUSH) collect();
-        before = stage;
         stage = stage + 1 == S::STAGES ? 0 : stage + 1;
     }
     copies_wait<0>();
@@ -595,15 +592,15 @@ __global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const __grid_const
         ++groups;
     };
 #pragma unroll
-    for (int i = 0; i < S::STAGES - 1; ++i) {
+    for (int i = 0; i < S::STAGES; ++i) {
         if (i < n) copy();
         copies_end();
     }
     constexpr uint32_t how = product(true, true, true, OUTER_COLS, S::N);
-    int at = 0, stage = 0, before = S::STAGES - 1;                               // the step, its stage, that of the step before
+    int at = 0, stage = 0;                        // the step, its stage
     uint32_t done = 0;                            // bit s: parity of stage s's next end of products
     for (; at < n; ++at) {
-        copies_wait<S::STAGES - 2>();
+        copies_wait<S::STAGES - 1>();
         fence_operands();
         if (!__syncthreads_and(ok)) break;
         if (warp == 0 && tc::elect_one()) {
@@ -617,17 +614,14 @@ __global__ void __launch_bounds__(AD_THREADS) outer_tc_kernel(const __grid_const
             if (at % FLUSH == FLUSH - 1 || at == n - 1) tc::umma_commit(bar + 8 * (S::STAGES + (at / FLUSH & 1)));
         }
         __syncwarp();
-        if (at + S::STAGES - 1 < n) {
-            // into the stage of the step before, once its products are done
-            if (at > 0) {
-                ok = ok && tc::mbar_wait(bar + 8 * before, done >> before & 1, err, E_ADAPTERS);
-                done ^= 1u << before;
-            }
+        if (at + S::STAGES < n) {
+            // the stage again, once its products are done: they take a fraction of the time that the next stages' copies do
+            ok = ok && tc::mbar_wait(bar + 8 * stage, done >> stage & 1, err, E_ADAPTERS);
+            done ^= 1u << stage;
             if (ok) copy();
         }
         copies_end();
         if (at % FLUSH == 1 && at > FLUSH) collect();
-        before = stage;
         stage = stage + 1 == S::STAGES ? 0 : stage + 1;
     }
     copies_wait<0>();

@@ -39,7 +39,6 @@ template <int N> struct Table {
     int base;                                     // blocks of the launches before
     int first;                                    // tensors of the launches before
     int64_t chunk;                                // values of a block
-    float keep;                                   // share of a block's values, the last ones, that may stay in L2 for the second pass
 };
 constexpr int SMALL = 48, LARGE = 480;            // 2.7 and 27 KB of arguments (at most 32,764 bytes)
 
@@ -91,14 +90,20 @@ __device__ __forceinline__ void see(Found &f, float v) {
     f.s = fmaf(v, v, f.s);
     f.m = fmaxf(f.m, fabsf(v));
 }
-// f(v) for the values of vectors from to to - 1 that are the thread's; KEEP: by loads that leave them in L2
-template <typename T, bool KEEP, typename F> __device__ __forceinline__ void each_vector(const uint4 *q, int64_t from, int64_t to, F f) {
+// f(v) for every value of the thread's share of a run
+template <typename T, typename F> __device__ __forceinline__ void each_value(const T *src, const Run &r, F f) {
     constexpr int E = 16 / (int)sizeof(T);
-    int64_t v = from + threadIdx.x;
-    for (; v + (UNROLL - 1) * THREADS < to; v += (int64_t)THREADS * UNROLL) {
+    const T *p = src + r.i0;
+    const int tid = threadIdx.x;
+    if (tid < r.head) f(to_f32(p[tid]));
+    const int64_t tail = r.head + r.vecs * E;
+    if (tail + tid < r.i1 - r.i0) f(to_f32(p[tail + tid]));
+    const uint4 *q = reinterpret_cast<const uint4 *>(p + r.head);
+    int64_t v = tid;
+    for (; v + (UNROLL - 1) * THREADS < r.vecs; v += (int64_t)THREADS * UNROLL) {
         uint4 u[UNROLL];
 #pragma unroll
-        for (int i = 0; i < UNROLL; ++i) u[i] = KEEP ? q[v + i * THREADS] : __ldcs(q + v + i * THREADS);
+        for (int i = 0; i < UNROLL; ++i) u[i] = q[v + i * THREADS];
 #pragma unroll
         for (int i = 0; i < UNROLL; ++i) {
             float x[E];
@@ -107,35 +112,22 @@ template <typename T, bool KEEP, typename F> __device__ __forceinline__ void eac
             for (int e = 0; e < E; ++e) f(x[e]);
         }
     }
-    for (; v < to; v += THREADS) {
+    for (; v < r.vecs; v += THREADS) {
         float x[E];
         unpack16<T>(q[v], x);
 #pragma unroll
         for (int e = 0; e < E; ++e) f(x[e]);
     }
 }
-// f(v) for every value of the thread's share of a run; the last `keep` of its vectors stay in L2
-template <typename T, typename F> __device__ __forceinline__ void each_value(const T *src, const Run &r, float keep, F f) {
-    constexpr int E = 16 / (int)sizeof(T);
-    const T *p = src + r.i0;
-    const int tid = threadIdx.x;
-    if (tid < r.head) f(to_f32(p[tid]));
-    const int64_t tail = r.head + r.vecs * E;
-    if (tail + tid < r.i1 - r.i0) f(to_f32(p[tail + tid]));
-    const uint4 *q = reinterpret_cast<const uint4 *>(p + r.head);
-    const int64_t far = (int64_t)((float)r.vecs * (1.f - keep));
-    each_vector<T, false>(q, 0, far, f);
-    each_vector<T, true>(q, far, r.vecs, f);
-}
-template <typename F> __device__ __forceinline__ void each_value(const ClipTensor &t, int64_t i0, int64_t i1, float keep, F f) {
+template <typename F> __device__ __forceinline__ void each_value(const ClipTensor &t, int64_t i0, int64_t i1, F f) {
     if (t.rows > 1) {
         for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) f(load(t, i));
     } else if (t.dtype == CT_DT_F32) {
-        each_value(static_cast<const float *>(t.src), Run(t.src, 4, i0, i1), keep, f);
+        each_value(static_cast<const float *>(t.src), Run(t.src, 4, i0, i1), f);
     } else if (t.dtype == CT_DT_F16) {
-        each_value(static_cast<const __half *>(t.src), Run(t.src, 2, i0, i1), keep, f);
+        each_value(static_cast<const __half *>(t.src), Run(t.src, 2, i0, i1), f);
     } else {
-        each_value(static_cast<const __nv_bfloat16 *>(t.src), Run(t.src, 2, i0, i1), keep, f);
+        each_value(static_cast<const __nv_bfloat16 *>(t.src), Run(t.src, 2, i0, i1), f);
     }
 }
 
@@ -145,13 +137,13 @@ template <int N> __global__ void __launch_bounds__(THREADS) clip_parts_kernel(co
     const ClipTensor &t = tab.t[find(tab, (int)blockIdx.x)];
     const int64_t total = t.rows * t.cols, i0 = (int64_t)((int)blockIdx.x - t.block0) * tab.chunk, i1 = min(i0 + tab.chunk, total);
     Found f = {0.f, 0.f};
-    each_value(t, i0, i1, tab.keep, [&](float v) { see(f, v); });
+    each_value(t, i0, i1, [&](float v) { see(f, v); });
     double sum = f.s;
     float m = f.m;
     if (f.s == f.s && m > 0.f && m < __builtin_huge_valf() && (m > 0x1p55f || m < 0x1p-50f)) {
         const int e = ilogbf(m);
         f.s = 0.f;
-        each_value(t, i0, i1, tab.keep, [&](float v) { see(f, ldexpf(v, -e)); });
+        each_value(t, i0, i1, [&](float v) { see(f, ldexpf(v, -e)); });
         sum = ldexp((double)f.s, 2 * e);
     }
     if (f.s != f.s) m = f.s;
@@ -176,8 +168,8 @@ template <int N> __global__ void __launch_bounds__(THREADS) clip_parts_kernel(co
     }
 }
 
-// values of a run times c into dst, whose run starts at the same place of a 16-byte unit; from its end on, which the first pass has
-// left in L2
+// values of a run times c into dst, whose run starts at the same place of a 16-byte unit; from its end on, which was read last and may be
+// in L2 still
 template <typename T> __device__ __forceinline__ void scale_run(const T *src, T *dst, const Run &r, float c) {
     constexpr int E = 16 / (int)sizeof(T);
     const T *p = src + r.i0;
@@ -319,15 +311,11 @@ ct_status sizes(int64_t n, int64_t total) {
     return n < 0 || total < 0 || n > INT32_MAX / 2 || total > INT64_MAX >> 8 || blocks_most(n, total) > INT32_MAX ? CT_ERANGE : CT_OK;
 }
 
-// What of the second pass may come from L2: a part of it, next to what is being written.
-constexpr double L2_SHARE = 64e6;
-
 template <int N>
-cudaError_t launch(const ct_tensor *t, int64_t n, int64_t total, double bytes, int kind, double max_norm, float *norms, float *norm,
+cudaError_t launch(const ct_tensor *t, int64_t n, int64_t total, int kind, double max_norm, float *norms, float *norm,
                    Part *parts, cudaStream_t st) {
     Table<N> tab;
     tab.chunk = chunk_of(total);
-    tab.keep = bytes > L2_SHARE ? (float)(L2_SHARE / bytes) : 1.f;
     int all = 0;
     for (int pass = 0; pass < 2; ++pass) {
         tab.base = 0;
@@ -378,14 +366,12 @@ extern "C" ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t 
     if (norm_dev == nullptr || !aligned(norm_dev, 4) || (n > 0 && (tensors == nullptr || norms_dev == nullptr || !aligned(norms_dev, 4))))
         return CT_EINVAL;
     int64_t total = 0;
-    double bytes = 0.0;
     for (int64_t i = 0; i < n; ++i) {
         const ct_tensor &t = tensors[i];
         if (t.rows < 0 || t.cols < 0 || (t.rows > 0 && t.cols > (INT64_MAX >> 8) / t.rows)) return CT_ERANGE;
         if (t.dtype < CT_DT_F32 || t.dtype > CT_DT_BF16 || !tensor_ok(t)) return CT_EINVAL;
         total += t.rows * t.cols;
         if (total > INT64_MAX >> 8) return CT_ERANGE;
-        bytes += (double)(t.rows * t.cols) * dtype_size((int)t.dtype);
     }
     if (sizes(n, total) != CT_OK) return CT_ERANGE;
     if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
@@ -411,7 +397,7 @@ extern "C" ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t 
     }
     Part *parts = static_cast<Part *>(workspace_dev);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = n <= SMALL ? launch<SMALL>(tensors, n, total, bytes, kind, max_norm, norms_dev, norm_dev, parts, st)
-                                     : launch<LARGE>(tensors, n, total, bytes, kind, max_norm, norms_dev, norm_dev, parts, st);
+    const cudaError_t e = n <= SMALL ? launch<SMALL>(tensors, n, total, kind, max_norm, norms_dev, norm_dev, parts, st)
+                                     : launch<LARGE>(tensors, n, total, kind, max_norm, norms_dev, norm_dev, parts, st);
     return e == cudaSuccess ? CT_OK : CT_ECUDA;
 }
