@@ -166,7 +166,8 @@ def run_reference(args, wl, rank, world):
 
 
 # sources of the operators that stand beside the networks: no inference launches one of their kernels
-OPERATOR_SOURCES = ("fp8_matmul.cu", "fp8_quantize.cu", "fp8_quantize.cuh", "logprobs.cu", "ops.cu", "ops_common.cuh")
+OPERATOR_SOURCES = ("fp8_matmul.cu", "fp8_quantize.cu", "fp8_quantize.cuh", "logprobs.cu", "ops.cu", "ops_common.cuh", "adapters.cu", "adapters.cuh",
+                    "adapters_expand.cu", "adapters_outer.cu", "adapters_shrink.cu", "adapters_tc.cu", "clip.cu", "verify.cu")
 
 
 def source_fingerprint(csrc=os.path.join(ROOT, "paper_2609_16742_gb300", "csrc")):

@@ -591,8 +591,9 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
 /* ct_adapters -- low-rank adapters of many requests at once, added to what the
  * shared projection gave, in place:
  *   y[t] = act( y[t] + scale[i] B[i] (A[i] x[t]) ),  i = ids[t]
- * with every sum, the products A x among them, in FP32 or better and one
- * rounding to y's type.
+ * with FP32 sums and one rounding to y's type; the short vectors A x go on from
+ * the first product to the second with 16 significant bits at least where y has 16
+ * bits, with 24 where it has 32.
  *   y_dev [t, n] (y_dtype, pitch ldy), x_dev [t, k] (x_dtype, pitch ldx).
  *   a_dev, b_dev (both `dtype`): A[i] is [rank, k], its rows a_row apart, one
  *     adapter a_adapter after another; B[i] is [n, rank], rows b_row apart,
@@ -604,7 +605,7 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
  *   act: ReLU that keeps NaN (relu != 0), or none.
  * x_dtype is `dtype` or CT_DT_F32; rank <= CT_MAX_RANK, adapters <=
  * CT_MAX_ADAPTERS.  NaN and infinities stay in
- * their row, or in the rows of their adapter.
+ * their row, or in the rows of their adapter; what an infinity gives may be NaN.
  * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row),
  * CT_ERANGE (sizes, rank), CT_ENOMEM (workspace), CT_ECUDA. */
 #define CT_MAX_RANK 128
@@ -620,7 +621,8 @@ ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, const void *x_d
  * dy [t, n] of its output:
  *   v = A[i] x[t],  u = scale[i] B[i]^T dy[t]  for every row t of adapter i = ids[t]
  *   dA[i] = sum_t u x[t]^T,  dB[i] = scale[i] sum_t dy[t] v^T,  dx[t] += A[i]^T u
- * with FP32 sums, rounded once.  dy_dev is `dtype` or CT_DT_F32 (pitch lddy).
+ * with FP32 sums, rounded once (v and u go on as above, by the results' types).
+ * dy_dev is `dtype` or CT_DT_F32 (pitch lddy).
  *   dx_dev [t, k] (dx_dtype, pitch lddx) or NULL: added to in place (the shared
  *     projection's part, or zeros).  Rows without an adapter are left as they
  *     are; a row whose id is out of range becomes NaN and adds to nothing else.

@@ -172,18 +172,18 @@ __device__ __forceinline__ void copy4_if(uint32_t to, const void *from, bool wan
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// what is left of v after its BF16 rounding h; nothing where h is infinite or NaN, so that those stay what they are
-__device__ __forceinline__ float rest_of(float v, float h) {
-    const float r = v - h;
-    return fabsf(r) < __builtin_huge_valf() ? r : 0.f;
-}
-__device__ __forceinline__ uint32_t split2(float &a, float &b) {
+// two values in BF16, and what is left of them (nothing of an infinite or NaN one: CLEAN)
+template <bool CLEAN> __device__ __forceinline__ uint32_t split2(float &a, float &b) {
     const uint32_t w = pack2<__nv_bfloat16>(a, b);
-    a = rest_of(a, __uint_as_float(w << 16));
-    b = rest_of(b, __uint_as_float(w & 0xFFFF0000u));
+    a -= __uint_as_float(w << 16);
+    b -= __uint_as_float(w & 0xFFFF0000u);
+    if (CLEAN) {
+        a = fabsf(a) < __builtin_huge_valf() ? a : 0.f;
+        b = fabsf(b) < __builtin_huge_valf() ? b : 0.f;
+    }
     return w;
 }
-// eight values as N parts of 16 bytes
+// eight values as N parts of 16 bytes; what an infinite one gives is NaN, as infinity - infinity
 template <int N, typename T> __device__ __forceinline__ void split8(const Eight<T> &e, uint4 (&out)[N]) {
     if constexpr (N == 1) {
         out[0] = e.u[0];
@@ -193,10 +193,10 @@ template <int N, typename T> __device__ __forceinline__ void split8(const Eight<
         if constexpr (sizeof(T) == 4) unpack16<T>(e.u[1], v + 4);
 #pragma unroll
         for (int p = 0; p < N; ++p) {
-            out[p].x = split2(v[0], v[1]);
-            out[p].y = split2(v[2], v[3]);
-            out[p].z = split2(v[4], v[5]);
-            out[p].w = split2(v[6], v[7]);
+            out[p].x = split2<false>(v[0], v[1]);
+            out[p].y = split2<false>(v[2], v[3]);
+            out[p].z = split2<false>(v[4], v[5]);
+            out[p].w = split2<false>(v[6], v[7]);
         }
     }
 }
@@ -278,8 +278,8 @@ __device__ __forceinline__ void write_vectors(const AdShrink &a, const AdOrder &
         uint2 *out = static_cast<uint2 *>(a.v) + ((tile.slot0 + r) * RP + j) / 4;
         for (int p = 0; p < a.parts; ++p) {
             uint2 w;
-            w.x = split2(v[0], v[1]);
-            w.y = split2(v[2], v[3]);
+            w.x = split2<true>(v[0], v[1]);
+            w.y = split2<true>(v[2], v[3]);
             out[p * (o.t * RP / 4)] = w;
         }
     }

