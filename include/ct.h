@@ -676,8 +676,9 @@ ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t kind, doubl
  * equals), drafts stand while they are that, and log probabilities are those at 1.
  *   logits_dev [drafts + sequences, vocab], draft_logits_dev [drafts, vocab] or NULL:
  *     dtype, pitches ld and ld_draft.  drafts_dev int64 [drafts], uniform_dev FP32
- *     [drafts], offsets_dev int64 [sequences + 1] (ascending, within [0, drafts]: what is
- *     outside is clamped), noise_dev FP32 [sequences, vocab] (> 0, pitch ld_noise),
+ *     [drafts], offsets_dev int64 [sequences + 1] (ascending; what is outside [0, drafts] is
+ *     clamped; where they descend results mean nothing, but nothing beside the
+ *     tensors is touched), noise_dev FP32 [sequences, vocab] (> 0, pitch ld_noise),
  *     temperature_dev FP32 [sequences] or NULL.
  *   accepted_dev int64 [sequences]: drafts that stand.
  *   token_dev int64, logprob_dev FP32 [sequences, max_drafts + 1]: the drafts that stand

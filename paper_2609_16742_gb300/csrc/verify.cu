@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) verify_rows_kernel(const Verif
     int64_t lo = 0, hi = a.sequences - 1;
     while (lo < hi) {
         const int64_t mid = (lo + hi + 1) / 2;
-        if (a.offsets[mid] + (draft ? 0 : mid) <= at) lo = mid;
+        if (min(max(a.offsets[mid], (int64_t)0), a.count) + (draft ? 0 : mid) <= at) lo = mid;
         else hi = mid - 1;
     }
     const Sequence s = sequence(a, lo);
@@ -228,7 +228,8 @@ __device__ __forceinline__ Row row_of(const Piece *p, int pieces, float c) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) r.z += __shfl_xor_sync(0xffffffffu, r.z, o);
     r.bad = !(r.z < INF) || r.m == INF;
-    if (r.m == -INF) r.at = -1;
+    // INT32_MAX: a row that offsets which descend give to two sequences, the other one not greedy
+    if (r.m == -INF || r.at == INT32_MAX) r.at = -1;
     return r;
 }
 

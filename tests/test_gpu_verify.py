@@ -157,6 +157,24 @@ def test_offsets_out_of_order_or_range():
         check(args, 5, run(c, args, 5))
 
 
+def test_clamped_offsets_with_temperatures():
+    """Ascending offsets that begin before 0 and end behind the drafts: each row goes by its own sequence's temperature."""
+    import torch
+    x, drafts, _, u, noise, q, _ = made([3, 3, 3], 3000, "float32")
+    for off, heat in (([-7, -2, 4, 9], [0.3, 0.0, 1.0]), ([0, 4, 30, 40], [0.0, 0.5, 0.0]), ([-9, -8, -7, 2], [0.0, 0.7, 0.0]), ([12, 13, 14, 15], [0.0, 1.0, 0.2])):
+        args = (x, drafts, torch.tensor(off, device="cuda"), u, noise, q, torch.tensor(heat, device="cuda"))
+        check(args, 5, run(ct(), args, 5))
+
+
+def test_descending_offsets_among_greedy_sequences_touch_nothing_else():
+    import torch
+    x, drafts, _, u, noise, q, _ = made([3, 3, 3], 3000, "float32")
+    for off in ([9, 5, 2, 0], [4, 2, 9, 1], [0, 20, 9, 9]):
+        for heat in ([0.0, 1.0, 0.0], [1.0, 0.0, 1.0]):
+            n, token, lp = run(ct(), (x, drafts, torch.tensor(off, device="cuda"), u, noise, q, torch.tensor(heat, device="cuda")), 5)
+            assert 0 <= int(n.min()) and int(n.max()) <= 5 and int(token.min()) >= -1 and int(token.max()) < 3000
+
+
 def test_more_drafts_than_are_looked_at():
     args = made([6, 2, 9], 300, "float32")
     check(args, 3, run(ct(), args, 3))
