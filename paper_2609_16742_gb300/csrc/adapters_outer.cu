@@ -212,9 +212,61 @@ template <typename TX> cudaError_t by_rank(const AdOuters &two, int blocks, cons
         default: return launch<TX, 128>(two, blocks, o, splits, st);
     }
 }
+// Adapters of a few rows each: a tile's start and end would cost more than its products.  A thread has a column, eight of the rank at a
+// time, and adds in FP32 row by row.
+constexpr int FEW_COLS = 256, FEW_ROWS = 64;
+template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int rp) {
+    __shared__ float vs[FEW_ROWS][8];
+    __shared__ int32_t rows[FEW_ROWS];
+    pdl_wait();
+    pdl_trigger();
+    const int block = blockIdx.x, tid = threadIdx.x, adapter = blockIdx.y;
+    const AdOuter &a = two.a[block >= two.first];
+    const int64_t c = (int64_t)(block >= two.first ? block - two.first : block) * FEW_COLS + tid;
+    const int from = o.first[adapter + 1], to = o.end[adapter + 1];
+    const bool mine = c < a.cols;
+    const TX *x = static_cast<const TX *>(a.x) + (mine ? c : 0);
+    const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v);
+    const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
+    for (int j0 = 0; j0 < a.rank; j0 += 8) {
+        float acc[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        for (int t0 = from; t0 < to; t0 += FEW_ROWS) {
+            const int n = min(FEW_ROWS, to - t0);
+            __syncthreads();
+            for (int i = tid; i < n * 8; i += FEW_COLS) {
+                const int64_t at = (int64_t)(t0 + i / 8) * rp + j0 + i % 8;
+                float s = 0.f;
+                for (int p = a.parts - 1; p >= 0; --p) s += __bfloat162float(v[p * (o.t * rp) + at]);       // the least part first: exact
+                vs[i / 8][i % 8] = s;
+            }
+            if (tid < n) rows[tid] = o.order[t0 + tid];
+            __syncthreads();
+#pragma unroll 8
+            for (int i = 0; i < n; ++i) {
+                const float w = mine ? to_f32(x[(int64_t)rows[i] * a.ldx]) : 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, vs[i][j], acc[j]);
+            }
+        }
+        if (mine)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j0 + j < a.rank) put_as(a.g, a.g_dtype, g0 + (a.by_cols ? c * a.rank + j0 + j : (j0 + j) * a.cols + c), acc[j]);
+    }
+}
+template <typename TX> cudaError_t few(const AdOuter (&a)[2], int n, const AdOrder &o, cudaStream_t st) {
+    const int first = (int)((a[0].cols + FEW_COLS - 1) / FEW_COLS), blocks = first + (n > 1 ? (int)((a[1].cols + FEW_COLS - 1) / FEW_COLS) : 0);
+    const AdOuters two = {{a[0], a[n - 1]}, first};
+    return pdl_launch(few_outer_kernel<TX>, dim3((unsigned)blocks, (unsigned)o.adapters), dim3(FEW_COLS), 0, st, two, o, ad_padded(a[0].rank));
+}
 }  // namespace
 
 cudaError_t ad_outer(const AdOuter (&a)[2], int n, int x_dtype, const AdOrder &o, cudaStream_t st) {
+    // 16 rows an adapter at most, on average
+    if (o.order != nullptr && o.t <= 16 * (int64_t)o.adapters)
+        return x_dtype == CT_DT_F32 ? few<float>(a, n, o, st) : x_dtype == CT_DT_F16 ? few<__half>(a, n, o, st) : few<__nv_bfloat16>(a, n, o, st);
     const int first = (int)((a[0].cols + COLS - 1) / COLS), blocks = first + (n > 1 ? (int)((a[1].cols + COLS - 1) / COLS) : 0);
     // as many CTAs as are resident together (two for each SM), with two steps of an adapter's share of the rows at least for each
     const int64_t steps = (o.t / o.adapters + AD_STEP - 1) / AD_STEP, most = 2 * sm_count() / ((int64_t)blocks * o.adapters);

@@ -15,7 +15,7 @@ PAIRS = [("float32", "float32"), ("float16", "float16"), ("bfloat16", "bfloat16"
 SIZES = [(1, 16, 10, 1, 1), (1, 4096, 512, 16, 8), (3, 257, 129, 5, 4), (17, 64, 64, 8, 17), (33, 1000, 31, 20, 3), (64, 128, 256, 16, 64),
          (130, 72, 264, 64, 1), (200, 520, 1000, 128, 2), (257, 320, 96, 33, 5), (700, 136, 200, 32, 3), (1500, 48, 40, 4, 2)]
 # rows that can be copied as they lie, the long axes shared by several CTAs
-WHOLE = [(300, 4104, 72, 16, 1), (400, 1032, 136, 8, 3), (129, 8, 2056, 24, 2), (3000, 136, 264, 64, 2), (150, 2120, 648, 128, 1), (2000, 520, 24, 40, 300)]
+WHOLE = [(300, 4104, 72, 16, 1), (400, 1032, 136, 8, 3), (129, 8, 2056, 24, 2), (3000, 136, 264, 64, 2), (150, 2120, 648, 128, 1), (2000, 520, 24, 40, 300), (300, 72, 520, 16, 40)]
 
 
 def np64(t):
@@ -117,6 +117,16 @@ def test_whole_rows(size, wt):
         got = ct().ct_adapters_grad(dy, x, a, b, ids, scale, dx=dx.clone(), grad_dtype=getattr(torch, dt))
         check_grad(dy, x, a, b, ids, scale, dx, got)
     assert ct().ct_ops_device_error() == 0
+
+
+def test_many_rows_of_one_adapter_among_many_adapters():
+    """Rows enough for one adapter of many: the kernels for few rows an adapter on many of one."""
+    import torch
+    x, a, b, ids, scale = made(700, 136, 300, 12, 64, "bfloat16", "bfloat16", seed=4)
+    ids[ids > 2] = 7
+    dx = like(700, 136, "float32", 4)
+    dy = like(700, 300, "bfloat16", 3)
+    check_grad(dy, x, a, b, ids, scale, dx, ct().ct_adapters_grad(dy, x, a, b, ids, scale, dx=dx.clone(), grad_dtype=torch.float32))
 
 
 def test_gradients_agree_with_differences():
