@@ -52,32 +52,25 @@ __device__ __forceinline__ void y_store(char *p, int dtype, const float *v) {
         *reinterpret_cast<uint4 *>(p) = dtype == CT_DT_F16 ? pack16<__half>(v) : pack16<__nv_bfloat16>(v);
     }
 }
-__device__ __forceinline__ void y_put(char *p, int dtype, float v) {
-    if (dtype == CT_DT_F32) *reinterpret_cast<float *>(p) = v;
-    else if (dtype == CT_DT_F16) *reinterpret_cast<__half *>(p) = __float2half_rn(v);
-    else *reinterpret_cast<__nv_bfloat16 *>(p) = __float2bfloat16_rn(v);
-}
-
-// one value of y, or 0: no branch, so that many are on their way together
-__device__ __forceinline__ float y_one_if(const char *p, int dtype, bool wanted) {
+// The bits of one value of y, or 0: no branch and nothing done with them yet (a value that is converted, or passes the end of a branch, is
+// waited for), and no order among other accesses to memory (none is of the same value), so that many are on their way together.
+__device__ __forceinline__ uint32_t y_bits_if(const char *p, bool wide, bool wanted) {
     uint32_t v;
-    if (dtype == CT_DT_F32) {
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.b32 %0, 0;\n\t@p ld.global.b32 %0, [%1];\n\t}"
-                     : "=&r"(v) : "l"(p), "r"((int)wanted) : "memory");
-        return __uint_as_float(v);
-    }
-    uint16_t h;
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\tmov.b16 %0, 0;\n\t@p ld.global.b16 %0, [%1];\n\t}"
-                 : "=&h"(h) : "l"(p), "r"((int)wanted) : "memory");
-    return dtype == CT_DT_F16 ? __half2float(__ushort_as_half(h)) : __uint_as_float((uint32_t)h << 16);
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tsetp.ne.b32 q, %3, 0;\n\tmov.b32 %0, 0;\n\t"
+                 "@p ld.global.b32 %0, [%1];\n\t@q ld.global.u16 %0, [%1];\n\t}"
+                 : "=&r"(v) : "l"(p), "r"((int)(wanted && wide)), "r"((int)(wanted && !wide)));
+    return v;
+}
+__device__ __forceinline__ float y_of_bits(uint32_t v, int dtype) {
+    return dtype == CT_DT_F32 ? __uint_as_float(v) : dtype == CT_DT_F16 ? __half2float(__ushort_as_half((unsigned short)v)) : __uint_as_float(v << 16);
 }
 
 // YW: y's rows are whole
 template <typename TM, int RP, bool TRANS, bool YW>
-__global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, const AdOrder o) {
+__global__ void __launch_bounds__(AD_THREADS, 2) expand_kernel(const AdExpand a, const AdOrder o) {
     using S = Expand<TM, RP, TRANS>;
     extern __shared__ __align__(128) unsigned char sm[];
-    __shared__ int32_t rows[AD_ROWS];
+    __shared__ char *rows[AD_ROWS];               // where the rows of y begin; null: no row
     pdl_wait();
     pdl_trigger();
     const AdRows tile = ad_tile(o, (int)blockIdx.x);
@@ -87,7 +80,9 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     const uint32_t base = tc::smem_u32(sm), bm0 = base + a.parts * S::V_BYTES;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wm = warp & 3, wn = warp >> 2;
     const int ys = a.y_dtype == CT_DT_F32 ? 4 : 2;
-    if (tid < AD_ROWS) rows[tid] = tid < tile.rows ? (o.order != nullptr ? o.order[tile.slot0 + tid] : (int32_t)(tile.slot0 + tid)) : -1;
+    if (tid < AD_ROWS)
+        rows[tid] = tid < tile.rows ? static_cast<char *>(a.y) + (o.order != nullptr ? (int64_t)o.order[tile.slot0 + tid] : tile.slot0 + tid) * a.ldy * ys
+                                    : nullptr;
 
     const bool product = !out && !none && a.rank > 0;
     const TM *m = static_cast<const TM *>(a.m) + (product ? (int64_t)(tile.key - 1) * a.m_adapter : 0);
@@ -146,10 +141,12 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         for (int v = tid; v < a.parts * AD_ROWS * (RP / 8); v += AD_THREADS) {
             const int p = v / (AD_ROWS * (RP / 8)), r = v / (RP / 8) % AD_ROWS, j = v % (RP / 8);
             const bool there = r < tile.rows;
-            sts16(base + p * S::V_BYTES + r * S::LV + j * 16,
-                  ld_if(static_cast<const uint4 *>(a.v) + (there ? (p * o.t + tile.slot0 + r) * (RP / 8) + j : 0), there));
+            copy16_if(base + p * S::V_BYTES + r * S::LV + j * 16,
+                      static_cast<const uint4 *>(a.v) + (there ? (p * o.t + tile.slot0 + r) * (RP / 8) + j : 0), there);
         }
+        copies_end();
         store(c_from, 0);
+        copies_wait<0>();
     }
     __syncthreads();
     // this thread's rows: lane / 4 + 8 i of the warp's 32
@@ -157,16 +154,16 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
     bool yh[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int32_t t = rows[wm * 32 + i * 8 + (lane >> 2)];
-        yh[i] = t >= 0;
-        yr[i] = static_cast<char *>(a.y) + (yh[i] ? (int64_t)t * a.ldy * ys : 0);
+        char *p = rows[wm * 32 + i * 8 + (lane >> 2)];
+        yh[i] = p != nullptr;
+        yr[i] = yh[i] ? p : static_cast<char *>(a.y);
     }
     const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
     const float nan = __uint_as_float(0x7FC00000u);
     // y a step ahead: eight neighbouring values of each of the thread's rows, or, of rows that start anywhere, one column's of all of the warp's
     const int64_t mine0 = wn * 32 + (YW ? (lane & 3) * 8 : lane);
     YEight ahead[YW ? 4 : 1];
-    float column[YW ? 1 : 32];
+    uint32_t column[YW ? 1 : 32];
     auto y_fetch = [&](int64_t c0) {
         const int64_t c = c0 + mine0;
         if constexpr (YW) {
@@ -175,12 +172,12 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         } else {
 #pragma unroll
             for (int r = 0; r < 32; ++r) {
-                const int32_t t = rows[wm * 32 + r];
-                const bool there = t >= 0 && c < c_to;
-                column[r] = y_one_if(static_cast<char *>(a.y) + (there ? ((int64_t)t * a.ldy + c) * ys : 0), a.y_dtype, there);
+                const char *p = rows[wm * 32 + r];
+                column[r] = y_bits_if(p + c * ys, ys == 4, p != nullptr && c < c_to);
             }
         }
     };
+    const bool busy = wm * 32 < tile.rows;        // else the warp has no rows
     y_fetch(c_from);
     int buf = 0;
     for (int64_t c0 = c_from; c0 < c_to; c0 += AD_STEP, buf ^= 1) {
@@ -188,12 +185,11 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
         if (more) fetch(c0 + AD_STEP);
         const int64_t mine = c0 + mine0;
         YEight y[YW ? 4 : 1];
-        float old[YW ? 1 : 32];
+        if constexpr (YW) {
 #pragma unroll
-        for (int i = 0; i < (YW ? 4 : 1); ++i) y[i] = ahead[i];
-#pragma unroll
-        for (int i = 0; i < (YW ? 1 : 32); ++i) old[i] = column[i];
-        y_fetch(c0 + AD_STEP);
+            for (int i = 0; i < 4; ++i) y[i] = ahead[i];
+            y_fetch(c0 + AD_STEP);
+        }
         float acc[2][4][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -201,7 +197,7 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
-        if (product) {
+        if (product && busy) {
             const uint32_t bm = bm0 + buf * (S::PM * S::M_BYTES);
 #pragma unroll
             for (int k = 0; k < RP; k += 16)
@@ -244,22 +240,41 @@ __global__ void __launch_bounds__(AD_THREADS) expand_kernel(const AdExpand a, co
                 if (yh[i] && mine < c_to) y_store(yr[i] + mine * ys, a.y_dtype, v);
             }
         } else {
-            // rows that start anywhere: eight rows of the warp's sums at a time turn in shared memory, so that lanes are neighbouring columns
+            // rows that start anywhere: eight rows of the warp's sums at a time turn in shared memory, so that lanes are neighbouring columns;
+            // as a value is done, that of the next step takes its register
             float *w = reinterpret_cast<float *>(sm + a.parts * S::V_BYTES + 2 * S::PM * S::M_BYTES) + warp * 8 * S::WIDE;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                if (wm * 32 + i * 8 >= tile.rows) break;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) w[(lane >> 2) * S::WIDE + (lane & 3) * 8 + 2 * j + e] = acc[i >> 1][j][(i & 1) * 2 + e];
                 __syncwarp();
+                char *at[8];
+                bool there[8];
+                float v[8];
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    const int32_t t = rows[wm * 32 + i * 8 + r];
-                    if (t < 0 || mine >= c_to) continue;
-                    float v = w[r * S::WIDE + lane] + old[i * 8 + r];
-                    if (a.relu) v = v < 0.f ? 0.f : v;
-                    y_put(static_cast<char *>(a.y) + ((int64_t)t * a.ldy + mine) * ys, a.y_dtype, out ? nan : v);
+                    char *p = rows[wm * 32 + i * 8 + r];
+                    there[r] = p != nullptr && mine < c_to;
+                    at[r] = p + mine * ys;
+                    v[r] = w[r * S::WIDE + lane] + y_of_bits(column[i * 8 + r], a.y_dtype);
+                }
+                if (a.relu || out)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) v[r] = out ? nan : v[r] < 0.f ? 0.f : v[r];
+                const bool next = mine + AD_STEP < c_to;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) column[i * 8 + r] = y_bits_if(at[r] + AD_STEP * ys, ys == 4, there[r] && next);
+                if (ys == 4) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (there[r]) *reinterpret_cast<float *>(at[r]) = v[r];
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (there[r]) *reinterpret_cast<uint16_t *>(at[r]) = (uint16_t)(a.y_dtype == CT_DT_F16 ? pack2<__half>(v[r], 0.f) : pack2<__nv_bfloat16>(v[r], 0.f));
                 }
                 __syncwarp();
             }

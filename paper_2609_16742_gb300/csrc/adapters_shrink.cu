@@ -126,7 +126,9 @@ __device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o,
                 }
     };
     const int q8 = lane >> 3, r8 = lane & 7;
+    const bool busy = wm * 32 < tile.rows;        // else the warp has no rows
     auto compute = [&](int buf) {
+        if (!busy) return;
         const uint32_t bx = base + buf * S::BUF, bm = bx + S::PX * S::X_BYTES;
 #pragma unroll
         for (int k = 0; k < AD_STEP; k += 16) {
