@@ -8,8 +8,9 @@
 // 16 bytes.
 //
 // What comes here: matrices of FP32 or FP16 values (several parts), rows that start anywhere.  Bound by instructions and their latency: 1777 x
-// 5003 FP32 values of y that start anywhere, FP16 matrices of rank 20, take 35 us (five products of parts; 42 before y's bits
+// 5003 FP32 values of y that start anywhere, FP16 matrices of rank 20, take 33 us (five products of parts; 42 before y's bits
 // came a step ahead without branches or conversions, rows' addresses lay in shared memory and warps without rows idled).
+// FP32 of rank 128, 8192 x 2048: 177 us, 278 with a number of parts that the loop did not know and the matrix's read again for each of v's.
 #include "adapters.cuh"
 
 namespace ct {
@@ -22,6 +23,8 @@ template <typename TM, int RP, bool TRANS> struct Expand {
     static constexpr int V_BYTES = AD_ROWS * LV, M_ROWS = TRANS ? RP : AD_STEP, M_BYTES = M_ROWS * LM;
     static constexpr int WIDE = 33, OUT = 8 * 8 * WIDE * 4;                      // 8 x 32 sums of each warp, where rows start anywhere
     static constexpr int M_VECS = M_ROWS * (TRANS ? AD_STEP / 8 : RP / 8), MV = (M_VECS + AD_THREADS - 1) / AD_THREADS;
+    // blocks that an SM's memory holds
+    static constexpr int blocks(bool out) { return 3 * V_BYTES + 2 * PM * M_BYTES + (out ? OUT : 0) <= 112 * 1024 ? 2 : 1; }
     static int smem(int parts, bool out) { return parts * V_BYTES + 2 * PM * M_BYTES + (out ? OUT : 0); }
 };
 
@@ -68,7 +71,7 @@ __device__ __forceinline__ float y_of_bits(uint32_t v, int dtype) {
 
 // YW: y's rows are whole
 template <typename TM, int RP, bool TRANS, bool YW>
-__global__ void __launch_bounds__(AD_THREADS, 2) expand_kernel(const AdExpand a, const AdOrder o) {
+__global__ void __launch_bounds__(AD_THREADS, Expand<TM, RP, TRANS>::blocks(!YW)) expand_kernel(const AdExpand a, const AdOrder o) {
     using S = Expand<TM, RP, TRANS>;
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ char *rows[AD_ROWS];               // where the rows of y begin; null: no row
@@ -159,7 +162,50 @@ __global__ void __launch_bounds__(AD_THREADS, 2) expand_kernel(const AdExpand a,
         yh[i] = p != nullptr;
         yr[i] = yh[i] ? p : static_cast<char *>(a.y);
     }
-    const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
+    const int q8 = lane >> 3, r8 = lane & 7;
+    auto products = [&](auto parts, uint32_t bm, float (&acc)[2][4][4]) {
+        constexpr int PV = decltype(parts)::value, MOST = PV == 2 ? 1 : 2;
+        // two blocks on an SM, 16-bit values and eight values of y ahead: the parts one by one, as registers end
+        // (8192 x 4096 FP16, rank 64: 123 us, 135 with all at once; rank 16: 61, 69)
+        constexpr int UNROLLED = S::blocks(!YW) == 2 && YW && S::PM < 3 ? 1 : PV;
+        auto columns = [&](int k, int q, int j, uint32_t (&b)[4]) {
+            const int n = j + (q8 >> 1);
+            if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + wn * 64 + n * 16, b);
+            else ldsm_x4(bm + q * S::M_BYTES + (wn * 32 + 8 * (r8 >> 1) + 2 * n + (r8 & 1)) * S::LM + (k + (q8 & 1) * 8) * 2, b);
+        };
+#pragma unroll
+        for (int k = 0; k < RP; k += 16) {
+            // with the registers of one block on an SM, the matrix's parts are read once for all of the vectors'
+            constexpr bool HELD = S::blocks(!YW) == 1;
+            uint32_t held[HELD ? S::PM : 1][2][4];
+            if constexpr (HELD)
+#pragma unroll
+                for (int q = 0; q < S::PM; ++q)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) columns(k, q, 2 * j, held[q][j]);
+#pragma unroll UNROLLED
+            for (int p = 0; p < PV; ++p) {
+                uint32_t fa[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    ldsm_x4(base + p * S::V_BYTES + (wm * 32 + i * 16 + (q8 & 1) * 8 + r8) * S::LV + (k + (q8 >> 1) * 8) * 2, fa[i]);
+#pragma unroll
+                for (int q = 0; q < S::PM; ++q) {
+                    if (p + q > MOST) continue;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t(&b)[4] = held[HELD ? q : 0][j];
+                        if constexpr (!HELD) columns(k, q, 2 * j, b);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            mma16<false>(acc[i][2 * j], fa[i], b[0], b[1]);
+                            mma16<false>(acc[i][2 * j + 1], fa[i], b[2], b[3]);
+                        }
+                    }
+                }
+            }
+        }
+    };
     const float nan = __uint_as_float(0x7FC00000u);
     // y a step ahead: eight neighbouring values of each of the thread's rows, or, of rows that start anywhere, one column's of all of the warp's
     const int64_t mine0 = wn * 32 + (YW ? (lane & 3) * 8 : lane);
@@ -200,30 +246,9 @@ __global__ void __launch_bounds__(AD_THREADS, 2) expand_kernel(const AdExpand a,
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
         if (product && busy) {
             const uint32_t bm = bm0 + buf * (S::PM * S::M_BYTES);
-#pragma unroll
-            for (int k = 0; k < RP; k += 16)
-                for (int p = 0; p < a.parts; ++p) {
-                    uint32_t fa[2][4];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        ldsm_x4(base + p * S::V_BYTES + (wm * 32 + i * 16 + (q8 & 1) * 8 + r8) * S::LV + (k + (q8 >> 1) * 8) * 2, fa[i]);
-#pragma unroll
-                    for (int q = 0; q < S::PM; ++q) {
-                        if (p + q > most) break;
-#pragma unroll
-                        for (int j = 0; j < 4; j += 2) {
-                            uint32_t b[4];
-                            const int n = j + (q8 >> 1);
-                            if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + wn * 64 + n * 16, b);
-                            else ldsm_x4(bm + q * S::M_BYTES + (wn * 32 + 8 * (r8 >> 1) + 2 * n + (r8 & 1)) * S::LM + (k + (q8 & 1) * 8) * 2, b);
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                mma16<false>(acc[i][j], fa[i], b[0], b[1]);
-                                mma16<false>(acc[i][j + 1], fa[i], b[2], b[3]);
-                            }
-                        }
-                    }
-                }
+            // the number of parts is fixed in the loop, so that its loads go ahead of its products
+            if (a.parts == 2) products(std::integral_constant<int, 2>(), bm, acc);
+            else products(std::integral_constant<int, 3>(), bm, acc);
         }
         if constexpr (YW) {
 #pragma unroll

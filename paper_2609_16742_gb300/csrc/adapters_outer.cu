@@ -214,7 +214,7 @@ template <typename TX> cudaError_t by_rank(const AdOuters &two, int blocks, cons
 }
 // Adapters of a few rows each: a tile's start and end would cost more than its products.  A thread has a column, eight of the rank at a
 // time, and adds in FP32 row by row.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 70 us
-// for both gradients; the whole call takes 336 us, 424 with tiles here.
+// for both gradients; the whole call takes 332 us, 424 with tiles here.
 constexpr int FEW_COLS = 256, FEW_ROWS = 64;
 template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int rp) {
     __shared__ float vs[FEW_ROWS][8];
