@@ -28,14 +28,17 @@ template <typename TX, int RP> struct Outer {
     // x's values are several parts.
     static constexpr bool EACH = PX > 1;
     static constexpr int FLUSH = 2;
+    // Ranks to 32: one buffer and two blocks on an SM, which wait for their rows in turn (8192 rows, 6144 FP32 columns, rank 16: 214 us,
+    // 272 with two buffers and one block).  Above, the sums' registers leave room for one block.
+    static constexpr int BLOCKS = RP <= 32 ? 2 : 1, BUFFERS = BLOCKS == 2 ? 1 : 2;
     static int smem(int parts) {
-        const int all = 2 * (PX * X_BYTES + parts * V_BYTES);
+        const int all = BUFFERS * (PX * X_BYTES + parts * V_BYTES);
         return all > SUM ? all : SUM;
     }
 };
 
 template <typename TX, int RP>
-__global__ void __launch_bounds__(AD_THREADS) outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int splits) {
+__global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int splits) {
     using S = Outer<TX, RP>;
     extern __shared__ __align__(128) unsigned char sm[];
     pdl_wait();
@@ -172,9 +175,10 @@ __global__ void __launch_bounds__(AD_THREADS) outer_kernel(const __grid_constant
         for (int64_t s = s0; s < s1; ++s) {
             const int at = (int)(s - s0);
             if (s + 1 < s1) fetch(s + 1);
-            compute(at & 1);
+            compute(S::BUFFERS == 2 ? at & 1 : 0);
             if (!S::EACH && at % S::FLUSH == S::FLUSH - 1) flush();
-            if (s + 1 < s1) store(s + 1, at & 1 ^ 1);
+            if constexpr (S::BUFFERS == 1) __syncthreads();
+            if (s + 1 < s1) store(s + 1, S::BUFFERS == 2 ? at & 1 ^ 1 : 0);
             __syncthreads();
         }
     }
