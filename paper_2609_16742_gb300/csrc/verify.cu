@@ -80,14 +80,15 @@ struct Stat {
     int32_t at;
 };
 
-// N values, all of them from index `at` on (ARG: their order matters)
+// N values and their indices, in any order (ARG: the lowest index of the largest is wanted)
 template <int N, bool ARG> __device__ __forceinline__ void see(Stat &s, const float (&v)[N], float c, const int32_t (&at)[N]) {
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
     const float m = fmaxf(s.m, top), ref = m == -INF ? 0.f : m;
-    if (ARG && top > s.m) {
-        int32_t first = INT32_MAX;
+    if (ARG && top >= s.m) {
+        // a lane's values behind a piece's last 16-byte unit come before those of the units, so that an equal one may have a lower index
+        int32_t first = top > s.m ? INT32_MAX : s.at;
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (v[i] == top && at[i] < first) first = at[i];
