@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
         return;
     }
     const bool out = tile.key > o.adapters, none = tile.key == 0;               // NaN; act alone
-    const bool product_wanted = !out && !none;
+    const bool product_wanted = !out && !none && a.rank > 0;                     // rank 0: no vectors have been written
     const uint32_t vb = (tc::smem_u32(raw) + 1023u) & ~1023u, mb = vb + a.parts * S::V_BYTES;
     const __nv_bfloat16 *m = static_cast<const __nv_bfloat16 *>(a.m) + (product_wanted ? (int64_t)(tile.key - 1) * a.m_adapter : 0);
     const int n = (int)((c_to - c_from + S::COLS - 1) / S::COLS);

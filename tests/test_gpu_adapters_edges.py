@@ -1,0 +1,33 @@
+"""Adapters and their gradients at the ends of their ranges: nothing of the rank."""
+import pytest
+
+from _gpu import ct
+from test_gpu_adapters import like
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"float32": 0, "float16": 1, "bfloat16": 2}
+
+
+@pytest.mark.parametrize("wt", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("t", [5, 300])
+def test_rank_0_leaves_what_it_is_added_to(t, wt):
+    """Through the C entries, with a workspace that holds NaN: nothing of it goes into a result."""
+    import torch
+    c, count, k, n = ct(), 2, 64, 48
+    dt = getattr(torch, wt)
+    x, a = like(t, k, wt, 1), torch.zeros(count, 0, k, dtype=dt, device="cuda")
+    b = torch.ones(count, n, 8, dtype=dt, device="cuda")[:, :, :0]       # columns of a wider matrix
+    ids = torch.arange(t, device="cuda") % count
+    work = torch.full((1 << 20,), 0xFF, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    for out in (wt, "float32"):
+        y, dx = like(t, n, out, 2), like(t, k, out, 3)
+        got, into = y.clone(), dx.clone()
+        weights = (a.data_ptr(), a.stride(0), a.stride(1), b.data_ptr(), b.stride(0), b.stride(1), CODE[wt], ids.data_ptr(), None, t, count, 0, k, n)
+        assert c.lib().ct_adapters(got.data_ptr(), CODE[out], n, x.data_ptr(), CODE[wt], k, *weights, 0, work.data_ptr(), 1 << 20, stream) == 0
+        assert torch.equal(got, y)
+        dy = like(t, n, wt, 4)
+        assert c.lib().ct_adapters_grad(dy.data_ptr(), CODE[wt], n, x.data_ptr(), CODE[wt], k, *weights, into.data_ptr(), CODE[out], k, None, None,
+                                        CODE[wt], work.data_ptr(), 1 << 20, stream) == 0
+        assert torch.equal(into, dx)
