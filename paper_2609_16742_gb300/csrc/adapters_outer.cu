@@ -217,9 +217,10 @@ template <typename TX> cudaError_t by_rank(const AdOuters &two, int blocks, cons
     }
 }
 // Adapters of a few rows each: a tile's start and end would cost more than its products.  A thread has a column, eight of the rank at a
-// time, and adds in FP32 row by row.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 70 us
+// time, and adds in FP32 row by row; as all rows may be one adapter's, 64 of them go into a sum, 8 of those into the next, and those into the
+// last.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 70 us
 // for both gradients; the whole call takes 332 us, 424 with tiles here.
-constexpr int FEW_COLS = 256, FEW_ROWS = 64;
+constexpr int FEW_COLS = 256, FEW_ROWS = 64, FEW_BLOCKS = 8;
 template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int rp) {
     __shared__ float vs[FEW_ROWS][8];
     __shared__ int32_t rows[FEW_ROWS];
@@ -234,9 +235,10 @@ template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_ker
     const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v);
     const int64_t g0 = (int64_t)adapter * a.rank * a.cols;
     for (int j0 = 0; j0 < a.rank; j0 += 8) {
-        float acc[8];
+        float acc[8], some[8], sum[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        for (int j = 0; j < 8; ++j) acc[j] = some[j] = sum[j] = 0.f;
+        int blocks = 0;
         for (int t0 = from; t0 < to; t0 += FEW_ROWS) {
             const int n = min(FEW_ROWS, to - t0);
             __syncthreads();
@@ -254,11 +256,21 @@ template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_ker
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, vs[i][j], acc[j]);
             }
+            const bool full = ++blocks % FEW_BLOCKS == 0 || t0 + FEW_ROWS >= to;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                some[j] += acc[j];
+                acc[j] = 0.f;
+                if (full) {
+                    sum[j] += some[j];
+                    some[j] = 0.f;
+                }
+            }
         }
         if (mine)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j0 + j < a.rank) put_as(a.g, a.g_dtype, g0 + (a.by_cols ? c * a.rank + j0 + j : (j0 + j) * a.cols + c), acc[j]);
+                if (j0 + j < a.rank) put_as(a.g, a.g_dtype, g0 + (a.by_cols ? c * a.rank + j0 + j : (j0 + j) * a.cols + c), sum[j]);
     }
 }
 template <typename TX> cudaError_t few(const AdOuter (&a)[2], int n, const AdOrder &o, cudaStream_t st) {

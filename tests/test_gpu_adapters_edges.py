@@ -1,6 +1,7 @@
-"""Adapters and their gradients at the ends of their ranges: nothing of the rank."""
+"""Adapters and their gradients at the ends of their ranges: nothing of the rank, many rows of one adapter."""
 import pytest
 
+import _adapt as ref
 from _gpu import ct
 from test_gpu_adapters import like
 
@@ -31,3 +32,24 @@ def test_rank_0_leaves_what_it_is_added_to(t, wt):
         assert c.lib().ct_adapters_grad(dy.data_ptr(), CODE[wt], n, x.data_ptr(), CODE[wt], k, *weights, into.data_ptr(), CODE[out], k, None, None,
                                         CODE[wt], work.data_ptr(), 1 << 20, stream) == 0
         assert torch.equal(into, dx)
+
+
+def test_many_equal_rows_of_one_adapter_among_many():
+    """Sums of equal positive terms, in which each addition could be rounded the same way: all rows have one adapter of so many that the kernel
+    for a few rows an adapter takes them."""
+    import torch
+    c = ct()
+    for t, count in ((8192, 512), (65536, 4096)):
+        v = 1.0 + 2.0 ** -12 * (1 - 2.0 ** -8)      # just under half a step more, from 4096 on
+        x = torch.full((t, 8), v, device="cuda")
+        a, b = torch.zeros(count, 2, 8, device="cuda"), torch.zeros(count, 12, 2, device="cuda")
+        a[7, :, 0], b[7, 0] = 1.0, 1.0
+        dy = torch.zeros(t, 12, device="cuda")
+        dy[:, 0] = 1.0
+        ids = torch.full((t,), 7, device="cuda")
+        _, da, db = c.ct_adapters_grad(dy, x, a, b, ids)
+        # u = 1 and A x = v for every row: t v in every place that is not 0
+        bound = (ref.UNIT * ref.steps(t) + ref.PARTS["float32"] + ref.HALF["float32"]) * t * v
+        for got in (da[7], db[7, 0]):
+            assert (got.double() - t * v).abs().max() <= bound
+        assert (db[7, 1:] == 0).all() and (da[:7] == 0).all() and (db[8:] == 0).all()
