@@ -365,8 +365,8 @@ template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_ke
     __shared__ float vs[8][CT_MAX_RANK];
     if (a.rank == 0) pdl_wait();                  // no kernel of this call before it
     int64_t id;
-    const int n = speak_for(a.ids, a.t, (int)blockIdx.x, rows, id);
-    const int64_t c = (int64_t)blockIdx.y * FEW_COLS + threadIdx.x;
+    const int n = speak_for(a.ids, a.t, (int)blockIdx.y, rows, id);
+    const int64_t c = (int64_t)blockIdx.x * FEW_COLS + threadIdx.x;
     const bool mine = c < a.n, out = id < -1 || id >= a.adapters, product = id >= 0 && !out;
     if (n == 0 || (id == -1 && !a.relu)) {
         pdl_wait();
@@ -442,7 +442,8 @@ template <typename TX, typename TM, bool WHOLE> cudaError_t few_as(const FewArgs
                                          : pdl_launch(few_shrink_kernel<TX, TM, WHOLE>, dim3((unsigned)lead), dim3(FEW_THREADS), 0, st, a, splits);
         if (e != cudaSuccess) return e;
     }
-    const dim3 grid((unsigned)(a.ids != nullptr ? a.t : 1), (unsigned)((a.n + FEW_COLS - 1) / FEW_COLS));
+    // the columns along x: y ends at 65535 blocks
+    const dim3 grid((unsigned)((a.n + FEW_COLS - 1) / FEW_COLS), (unsigned)(a.ids != nullptr ? a.t : 1));
     return pdl_launch(few_expand_kernel<TM>, grid, dim3(FEW_COLS), 0, st, a);
 }
 template <typename TX, typename TM> cudaError_t few(const FewArgs &a, bool whole, cudaStream_t st) {

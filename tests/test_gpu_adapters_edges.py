@@ -1,4 +1,5 @@
-"""Adapters and their gradients at the ends of their ranges: nothing of the rank, many rows of one adapter."""
+"""Adapters and their gradients at the ends of their ranges: nothing of the rank, many rows of one adapter, very long
+rows."""
 import pytest
 
 import _adapt as ref
@@ -53,3 +54,26 @@ def test_many_equal_rows_of_one_adapter_among_many():
         for got in (da[7], db[7, 0]):
             assert (got.double() - t * v).abs().max() <= bound
         assert (db[7, 1:] == 0).all() and (da[:7] == 0).all() and (db[8:] == 0).all()
+
+
+@pytest.mark.parametrize("t", [1, 3, 40])
+def test_few_rows_of_very_many_columns(t):
+    """More columns than 65535 blocks of 128 have."""
+    import torch
+    n = 128 * 65535 + 77
+    x, a = like(t, 16, "bfloat16", 1), like(8, 16, "bfloat16", 2).view(8, 1, 16)
+    b = torch.zeros(8, n, 1, dtype=torch.bfloat16, device="cuda")
+    b[:, ::1000003] = 1.0
+    b[:, -1] = 2.0
+    y = torch.zeros(t, n, dtype=torch.float32, device="cuda")
+    ids = torch.arange(t, device="cuda") % 8
+    v = (x.double() * a[ids, 0].double()).sum(dim=1)
+    ct().ct_adapters(y, x, a, b, ids)
+    want = torch.zeros(t, n, device="cuda")
+    want[:, ::1000003] = 1.0
+    want[:, -1] = 2.0
+    bound = (ref.UNIT * ref.steps(16) + ref.PARTS["float32"]) * 2 * (x.double() * a[ids, 0].double()).abs().sum(dim=1)
+    for r in range(t):
+        at = torch.nonzero(want[r])[:, 0]
+        assert torch.equal(torch.nonzero(y[r])[:, 0], at) or float(v[r]) == 0
+        assert (y[r, at].double() - want[r, at].double() * v[r]).abs().max() <= bound[r]
