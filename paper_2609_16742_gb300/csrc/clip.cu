@@ -23,7 +23,8 @@ namespace ops {
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int64_t LEAST = 4096, MOST = 1024 * THREADS;   // values of a block
+// values of a block; at most as many as leave a thread 1024 with its value before the first 16-byte unit and its one behind the last
+constexpr int64_t LEAST = 4096, MOST = 1016 * THREADS;
 constexpr int64_t BLOCKS = 1216;                  // wanted: 8 for each of 152 SMs
 constexpr int UNROLL = 4;                         // 16-byte loads of a thread on their way together
 
