@@ -606,7 +606,9 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
  * x_dtype is `dtype` or CT_DT_F32; rank <= CT_MAX_RANK, adapters <=
  * CT_MAX_ADAPTERS.  NaN and infinities stay in
  * their row, or in the rows of their adapter; what an infinity gives may be NaN.
- * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row),
+ * y may be x; it must share no value with B or the ids.
+ * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row, shared
+ * memory),
  * CT_ERANGE (sizes, rank), CT_ENOMEM (workspace), CT_ECUDA. */
 #define CT_MAX_RANK 128
 #define CT_MAX_ADAPTERS 65534
@@ -628,6 +630,8 @@ ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, const void *x_d
  *     are; a row whose id is out of range becomes NaN and adds to nothing else.
  *   da_dev [adapters, rank, k], db_dev [adapters, n, rank]: contiguous, of type
  *     grad_dtype (`dtype` or CT_DT_F32).  An adapter without rows gets zeros.
+ * dx must share no value with dy, x or A, and da and db none with dy, x, dx or one
+ * another (other columns or rows of one matrix are fine).
  * Errors: as for ct_adapters. */
 ct_status ct_adapters_grad_workspace(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n, size_t *bytes);
 ct_status ct_adapters_grad(const void *dy_dev, int32_t dy_dtype, int64_t lddy, const void *x_dev, int32_t x_dtype,

@@ -819,8 +819,8 @@ def ct_adapters(y, x, a, b, ids=None, scale=None, relu: bool = False, stream=Non
     a ReLU if asked: low-rank adapters a [adapters, rank, k], b [adapters, n,
     rank] beside the shared projection that gave y.  ids int64 [t] in any order
     (-1: no adapter; None: one adapter for all rows); scale float32
-    [adapters].  a and b are of one type, x of that or float32, y of any.
-    Returns y."""
+    [adapters].  a and b are of one type, x of that or float32, y of any; y may
+    be x, and shares no value with b or ids.  Returns y."""
     T = _names or _T()
     t, count, rank, k, n, ldx, w = _adapters(x, a, b, ids, scale)
     dev = x.device
@@ -839,8 +839,9 @@ def ct_adapters(y, x, a, b, ids=None, scale=None, relu: bool = False, stream=Non
 def ct_adapters_grad(dy, x, a, b, ids=None, scale=None, dx=None, grad_dtype=None, stream=None):
     """(dx, da, db): gradients of ct_adapters (without its ReLU) for the gradient
     dy [t, n] of its output.  dx [t, k], if given, is added to in place (the shared
-    projection's part; None: not wanted).  da and db are new, of a's type or
-    grad_dtype = float32; dy is of a's type or float32."""
+    projection's part; None: not wanted) and shares no value with dy, x or a.  da
+    and db are new, of a's type or grad_dtype = float32; dy is of a's type or
+    float32."""
     T = _names or _T()
     t, count, rank, k, n, ldx, w = _adapters(x, a, b, ids, scale)
     dev = x.device

@@ -518,6 +518,17 @@ inline bool whole(const void *p, int64_t ld, int64_t rows, int64_t cols, int es)
 inline bool stack_whole(const void *p, int64_t sa, int64_t sr, int64_t adapters, int64_t rows, int64_t cols, int es) {
     return whole(p, sr, rows, cols, es) && (adapters <= 1 || sa * es % 16 == 0);
 }
+
+// whether a matrix lies on one of a stack's
+bool on_stack(const Span &m, const void *p, int64_t sa, int64_t sr, int64_t adapters, int64_t rows, int64_t cols, int es) {
+    if (adapters == 0 || rows == 0 || cols == 0) return false;
+    Span one = span(p, rows, cols, sr, es);
+    const Span all = {one.at, 1, (int64_t)(one.end() - one.at) + (adapters - 1) * sa * es, 0};
+    if (!share(m, all)) return false;
+    for (int64_t i = 0; i < adapters; ++i, one.at += (uintptr_t)(sa * es))
+        if (share(m, one)) return true;
+    return false;
+}
 }  // namespace
 }  // namespace ops
 }  // namespace ct
@@ -548,6 +559,9 @@ extern "C" ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, cons
     const Space s = space_of(t, adapters, rank, false);
     if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
     if (workspace_bytes < s.total) return CT_ENOMEM;
+    // y is written while b and the ids are read; x and a have been read by then
+    const Span y = span(y_dev, t, n, ldy, ys);
+    if (on_stack(y, b_dev, b_adapter, b_row, adapters, n, rank, es) || (ids_dev != nullptr && share(y, span(ids_dev, 1, t, t, 8)))) return CT_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *w = static_cast<char *>(workspace_dev);
     const bool xw = whole(x_dev, ldx, t, k, xs), aw = stack_whole(a_dev, a_adapter, a_row, adapters, rank, k, es),
@@ -607,6 +621,12 @@ extern "C" ct_status ct_adapters_grad(const void *dy_dev, int32_t dy_dtype, int6
     const Space s = space_of(t, adapters, rank, true);
     if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
     if (workspace_bytes < s.total) return CT_ENOMEM;
+    // dx is written while a is read and before x and dy are read again, da and db while those are
+    const Span x = span(x_dev, t, k, ldx, xs), dy = span(dy_dev, t, n, lddy, dys), dx = span(dx_dev, dx_dev != nullptr ? t : 0, k, lddx, dxs);
+    const Span da = span(da_dev, adapters * rank, k, k, ges), db = span(db_dev, adapters * n, rank, rank, ges);
+    if (share(dx, x) || share(dx, dy) || on_stack(dx, a_dev, a_adapter, a_row, adapters, rank, k, es) || share(da, x) || share(da, dy) ||
+        share(da, dx) || share(db, x) || share(db, dy) || share(db, dx) || share(da, db))
+        return CT_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *w = static_cast<char *>(workspace_dev);
     const bool xw = whole(x_dev, ldx, t, k, xs), dyw = whole(dy_dev, lddy, t, n, dys), dxw = whole(dx_dev, lddx, t, k, dxs);

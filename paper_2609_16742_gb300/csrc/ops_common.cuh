@@ -18,6 +18,49 @@ inline int dtype_size(int dtype) { return dtype == CT_DT_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == CT_DT_F32 || dtype == CT_DT_F16 || dtype == CT_DT_BF16; }
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+// Memory that a call reads or writes: rows of `width` bytes, `pitch` bytes apart (0: all the same; else at least `width`).
+struct Span {
+    uintptr_t at;
+    int64_t rows, width, pitch;
+    uintptr_t end() const { return at + (uintptr_t)(rows - 1) * (uintptr_t)pitch + (uintptr_t)width; }
+};
+inline Span span(const void *p, int64_t rows, int64_t cols, int64_t ld, int size) {
+    return {(uintptr_t)p, cols > 0 ? rows : 0, cols * size, rows > 1 ? ld * size : 0};
+}
+// Whether two have a byte in common.  Rows of one pitch (columns of one matrix) are compared at once, others row by row of the one that has
+// fewer, where their ranges cross.
+inline bool share(Span a, Span b) {
+    if (a.pitch == 0 && a.rows > 1) a.rows = 1;
+    if (b.pitch == 0 && b.rows > 1) b.rows = 1;
+    if (a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0 || a.at >= b.end() || b.at >= a.end()) return false;
+    if (a.rows > b.rows) {
+        const Span c = a;
+        a = b;
+        b = c;
+    }
+    if (b.rows == 1) return true;
+    // b's first row that ends behind byte s of its store, were there rows before its own and behind them
+    const auto first = [&](int64_t s) {
+        const int64_t d = s - b.width, q = d / b.pitch;
+        return (d % b.pitch < 0 ? q - 1 : q) + 1;
+    };
+    const int64_t d = (int64_t)(a.at - b.at);     // of a's first row, from b's
+    if (a.rows > 1 && a.pitch == b.pitch) {
+        // row i of a meets b's rows j + i and j + 1 + i, or one of them, or none
+        for (int64_t j = first(d), k = j + 1; j <= k; ++j)
+            if (j * b.pitch < d + a.width && j < b.rows && j + a.rows > 0) return true;
+        return false;
+    }
+    const int64_t last = (int64_t)(b.end() - b.at);
+    for (int64_t i = d + a.width > 0 ? 0 : -(d + a.width) / a.pitch + 1; i < a.rows; ++i) {
+        const int64_t s = d + i * a.pitch;
+        if (s >= last) return false;
+        const int64_t j = s < b.width ? 0 : first(s);
+        if (j < b.rows && j * b.pitch < s + a.width) return true;
+    }
+    return false;
+}
+
 constexpr int MAX_DEVICES = 64;
 
 // Error word of the current device, OR-ed into by kernels whose bounded wait

@@ -1,10 +1,10 @@
 """Adapters and their gradients at the ends of their ranges: nothing of the rank, many rows of one adapter, very long
-rows."""
+rows, memory that is shared."""
 import pytest
 
 import _adapt as ref
 from _gpu import ct
-from test_gpu_adapters import like
+from test_gpu_adapters import check_grad, like, made
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +77,44 @@ def test_few_rows_of_very_many_columns(t):
         at = torch.nonzero(want[r])[:, 0]
         assert torch.equal(torch.nonzero(y[r])[:, 0], at) or float(v[r]) == 0
         assert (y[r, at].double() - want[r, at].double() * v[r]).abs().max() <= bound[r]
+
+
+def test_tensors_that_share_memory():
+    """dx is written while x, dy and a are still to be read: it may lie beside them in one matrix, but not on them."""
+    import torch
+    c = ct()
+    for t in (20, 300):
+        x, a, b, ids, scale = made(t, 24, 40, 4, 2, "float32", "float32")
+        y = like(t, 40, "float32", 1)
+        for dx in (x, x[:, :24]):
+            with pytest.raises(c.CtError):
+                c.ct_adapters_grad(y, x, a, b, ids, scale, dx=dx)
+        big = torch.zeros(t, 100, device="cuda")
+        dy, x2, dx = big[:, :40].copy_(y), big[:, 40:64].copy_(x), big[:, 64:88].copy_(like(t, 24, "float32", 2))
+        with pytest.raises(c.CtError):
+            c.ct_adapters_grad(dy, x2, a, b, ids, scale, dx=big[:, 39:63])
+        with pytest.raises(c.CtError):
+            c.ct_adapters_grad(dy, x2, a, b, ids, scale, dx=big[:, 63:87])
+        with pytest.raises(c.CtError):
+            c.ct_adapters_grad(dy[:-1], x2[:-1], a, b, ids[:-1], scale, dx=big[1:, 30:54])
+        with pytest.raises(c.CtError):
+            c.ct_adapters(big[:, 8:48], x, a, big.view(-1)[:320].view(2, 40, 4), ids, scale)
+        before = dx.clone()
+        check_grad(dy, x2, a, b, ids, scale, before, c.ct_adapters_grad(dy, x2, a, b, ids, scale, dx=dx))
+        assert (big[:, 88:] == 0).all()
+        # rows of different pitches in one store, one behind the other's values
+        store = torch.zeros(4 * t, 32, device="cuda")
+        x3, dx3 = store[::2][:t, :24].copy_(x), store[1::2][:t, 4:28].copy_(before)
+        check_grad(y, x3, a, b, ids, scale, before, c.ct_adapters_grad(y, x3, a, b, ids, scale, dx=dx3))
+        x4, dx4 = store[::4][:t, :24].copy_(x), store[1::2][:t, 8:32].copy_(before)
+        check_grad(y, x4, a, b, ids, scale, before, c.ct_adapters_grad(y, x4, a, b, ids, scale, dx=dx4))
+        with pytest.raises(c.CtError):
+            c.ct_adapters_grad(y, store[::4][:t, :24], a, b, ids, scale, dx=store[::2][:t, 8:32])
+
+
+def test_y_that_is_x():
+    """x has been read before y is written: a layer that adds to its own input."""
+    for t in (3, 300):
+        x, a, b, ids, scale = made(t, 64, 64, 8, 3, "bfloat16", "bfloat16")
+        y = x.clone()
+        assert (ct().ct_adapters(y, y, a, b, ids, scale) == ct().ct_adapters(x.clone(), x, a, b, ids, scale)).all()
