@@ -503,6 +503,8 @@ class _TorchNames:
         self.requires_grad, self.dtype, self.shape = get("requires_grad"), get("dtype"), get("shape")
         self.current_device = torch.cuda.current_device
         self.recording = torch.is_grad_enabled
+        # of tensors written in place, so that autograd notices where a graph still wants what was there
+        self.raise_versions = torch.autograd.graph.increment_version
         # the raw handle of the current stream; torch.cuda.current_stream builds a Stream object first
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -833,6 +835,7 @@ def ct_adapters(y, x, a, b, ids=None, scale=None, relu: bool = False, stream=Non
                                      k, n, 1 if relu else 0, work.data_ptr(), need, T.raw_stream(dev.index))
     if st:
         raise CtError(st, "ct_adapters")
+    T.raise_versions(y)
     return y
 
 
@@ -866,6 +869,8 @@ def ct_adapters_grad(dy, x, a, b, ids=None, scale=None, dx=None, grad_dtype=None
                                           work.data_ptr(), need, T.raw_stream(dev.index))
     if st:
         raise CtError(st, "ct_adapters_grad")
+    if dx is not None:
+        T.raise_versions(dx)
     return dx, da, db
 
 
@@ -990,6 +995,7 @@ def ct_clip_grads(grads, max_norm, kind: float = 2.0, out=None, stream=None):
                                        norm.data_ptr(), work.data_ptr(), need, T.raw_stream(index))
     if st:
         raise CtError(st, "ct_clip_grads")
+    T.raise_versions(grads if out is None else out)
     return norm, norms
 
 

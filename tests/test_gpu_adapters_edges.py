@@ -1,5 +1,6 @@
 """Adapters and their gradients at the ends of their ranges: nothing of the rank, many rows of one adapter, very long
-rows, memory that is shared."""
+rows, memory that is shared,
+versions."""
 import pytest
 
 import _adapt as ref
@@ -118,3 +119,29 @@ def test_y_that_is_x():
         x, a, b, ids, scale = made(t, 64, 64, 8, 3, "bfloat16", "bfloat16")
         y = x.clone()
         assert (ct().ct_adapters(y, y, a, b, ids, scale) == ct().ct_adapters(x.clone(), x, a, b, ids, scale)).all()
+
+
+def test_results_in_place_raise_the_tensors_versions():
+    """So that autograd notices where a graph still wants what was there."""
+    import torch
+    c = ct()
+    for t in (4, 300):
+        x, a, b, ids, scale = made(t, 32, 24, 4, 2, "float32", "float32")
+        y, dx = like(t, 24, "float32", 1), like(t, 32, "float32", 2)
+        at = y._version, dx._version, x._version
+        c.ct_adapters(y, x, a, b, ids, scale)
+        c.ct_adapters_grad(y, x, a, b, ids, scale, dx=dx)
+        assert y._version == at[0] + 1 and dx._version == at[1] + 1 and x._version == at[2]
+        c.ct_adapters(y, x, a, b, ids, scale, stream=torch.cuda.Stream())
+        assert y._version == at[0] + 2
+        torch.cuda.synchronize()
+        w = torch.ones(t, 24, device="cuda", requires_grad=True)
+        loss = (w * y).sum()
+        with torch.no_grad():
+            c.ct_adapters(y, x, a, b, ids, scale)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():
+        z = torch.zeros(4, 24, device="cuda")
+        c.ct_adapters(z, x[:4].clone(), a, b, ids[:4].clone(), scale)
+    c.ct_adapters(z, x[:4], a, b, ids[:4], scale)                       # no version to raise
