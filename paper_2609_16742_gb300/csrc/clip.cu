@@ -219,8 +219,8 @@ template <int N> __global__ void __launch_bounds__(THREADS)
 clip_scale_kernel(const __grid_constant__ Table<N> tab, const Part *parts, int all, int kind, double max_norm, float *norms, float *norm) {
     pdl_wait();
     pdl_trigger();
-    __shared__ double ss[WARPS];
-    __shared__ float sm[WARPS], factor;
+    __shared__ double ss[WARPS], factor;
+    __shared__ float sm[WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     double sum = 0.0;
     float m = 0.f;
@@ -245,7 +245,7 @@ clip_scale_kernel(const __grid_constant__ Table<N> tab, const Part *parts, int a
             m = join_top(m, sm[w]);
         }
         const double v = kind == CT_NORM_2 ? sqrt(sum) : (double)m;
-        factor = isfinite((float)v) && v > max_norm ? (float)(max_norm / v) : 1.f;
+        factor = isfinite((float)v) && v > max_norm ? max_norm / v : 1.0;
         if (blockIdx.x == 0 && tab.first == 0) *norm = (float)v;
     }
     for (int i = (int)blockIdx.x + (int)gridDim.x * warp; i < tab.n; i += (int)gridDim.x * WARPS) {
@@ -264,12 +264,19 @@ clip_scale_kernel(const __grid_constant__ Table<N> tab, const Part *parts, int a
         if (lane == 0) norms[tab.first + i] = kind == CT_NORM_2 ? (float)sqrt(sum) : m;
     }
     __syncthreads();
-    const float c = factor;
+    const double whole = factor;
+    const float c = (float)whole;
     const int block = tab.blocks - 1 - (int)blockIdx.x;
     if (block < 0) return;
     const ClipTensor &t = tab.t[find(tab, block)];
     if (c == 1.f && t.src == t.dst) return;
     const int64_t i0 = (int64_t)(block - t.block0) * tab.chunk, i1 = min(i0 + tab.chunk, t.rows * t.cols);
+    if (whole != 0.0 && c < 0x1p-126f) {
+        // A factor below the normal 32-bit numbers, of a norm that is large next to max_norm: its products with the largest values are in
+        // their range, and are taken in FP64 (slow here, and rare).
+        for (int64_t i = i0 + threadIdx.x; i < i1; i += THREADS) store(t, i, (float)(load(t, i) * whole));
+        return;
+    }
     if (t.rows == 1) {
         // 1 times a value is the value, but for a NaN, whose bits need not stay: it stays one
         if (t.dtype == CT_DT_F32 ? scale_dense<float>(t, i0, i1, c)

@@ -1,8 +1,10 @@
-"""Clipping beside autograd."""
+"""Clipping at the ends of its ranges, and beside autograd."""
+import math
+
 import pytest
 
 from _gpu import ct
-from test_gpu_clip import TYPES, made
+from test_gpu_clip import TYPES, check, made
 
 pytestmark = pytest.mark.gpu
 
@@ -17,3 +19,23 @@ def test_results_raise_the_tensors_versions():
         assert [t._version for t in grads + out] == at[:len(grads)] + [v + 1 for v in at[len(grads):]]
         c.ct_clip_grads(grads, 0.5)
         assert [t._version for t in grads] == [v + 1 for v in at[:len(grads)]]
+
+
+@pytest.mark.parametrize("kind", [2.0, math.inf])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("scale,max_norm", [(1e20, 1e-20), (1e30, 1e-12), (1e36, 1e-36), (1e-2, 1e-41), (1e36, 1e-300), (1e3, 1e-34), (1e30, 5e-324)])
+def test_factors_below_the_range_of_32_bits(scale, max_norm, dtype, kind):
+    """max_norm / norm has no normal 32-bit number, the values times it have."""
+    import torch
+    for sizes in ([5, 70001], [1]):
+        grads = made(sizes, [dtype], scale=scale)
+        before = [g.clone() for g in grads]
+        out = [torch.full_like(g, 3.0) for g in grads]
+        got = ct().ct_clip_grads(grads, max_norm, kind, out=out)
+        check(before, out, max_norm, kind, got)
+        assert all(torch.equal(g, b) for g, b in zip(grads, before))
+        ct().ct_clip_grads(grads, max_norm, kind)
+        assert all(torch.equal(g, o) for g, o in zip(grads, out))
+    pitched = made([300], [dtype], scale=scale)[0].view(20, 15)[:, 2:13]
+    before = [pitched.clone()]
+    check(before, [pitched], max_norm, kind, ct().ct_clip_grads([pitched], max_norm, kind))
