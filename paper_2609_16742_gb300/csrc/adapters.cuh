@@ -7,8 +7,9 @@
 // vectors between two products, are taken apart into BF16 parts of 8 bits each
 // (v = hi + mid + lo; two parts hold an FP16 value), and the products of parts
 // that matter are added: those of parts p and q with p + q <= 1 where the result has 16
-// bits (the rest is below 2^-15 of a term), with p + q <= 2 where it has 32 (2^-22).
-// FP16 by FP16 runs as it is.
+// bits (the rest is below 2^-15 of a term), with p + q <= 2 where it has 32 (2^-22),
+// the least first: of the largest FP32 values hi + mid alone can be infinite.
+// FP16 by FP16 runs as it is.  (Parts end at 2^-133, BF16's smallest step: FP32 values below 2^-110 keep fewer than 24 bits.)
 #pragma once
 #include "ops_common.cuh"
 #include "tc_common.cuh"
@@ -172,9 +173,20 @@ __device__ __forceinline__ void copy4_if(uint32_t to, const void *from, bool wan
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// two values in BF16, and what is left of them (nothing of an infinite or NaN one: CLEAN)
-template <bool CLEAN> __device__ __forceinline__ uint32_t split2(float &a, float &b) {
-    const uint32_t w = pack2<__nv_bfloat16>(a, b);
+// Two values in BF16, and what is left of them (nothing of an infinite or NaN one: CLEAN).  FIRST: of FP32 values as they are.  The largest of
+// those are nearer to infinity than to a BF16 value: they get the largest there is, and the next part has the rest.  (An infinity does so
+// too, and goes on as the next part; where that is cleaned away it keeps its first.)
+template <bool CLEAN, bool FIRST> __device__ __forceinline__ uint32_t split2(float &a, float &b) {
+    uint32_t w;
+    if constexpr (FIRST && CLEAN) {
+        constexpr float MOST = 0x1.FEp127f;
+        w = pack2<__nv_bfloat16>(fabsf(a) < __builtin_huge_valf() ? fminf(fmaxf(a, -MOST), MOST) : a,
+                                 fabsf(b) < __builtin_huge_valf() ? fminf(fmaxf(b, -MOST), MOST) : b);
+    } else if constexpr (FIRST) {
+        asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(b), "f"(a));
+    } else {
+        w = pack2<__nv_bfloat16>(a, b);
+    }
     a -= __uint_as_float(w << 16);
     b -= __uint_as_float(w & 0xFFFF0000u);
     if (CLEAN) {
@@ -183,7 +195,15 @@ template <bool CLEAN> __device__ __forceinline__ uint32_t split2(float &a, float
     }
     return w;
 }
-// eight values as N parts of 16 bytes; what an infinite one gives is NaN, as infinity - infinity
+template <bool FIRST> __device__ __forceinline__ uint4 split_part(float (&v)[8]) {
+    uint4 w;
+    w.x = split2<false, FIRST>(v[0], v[1]);
+    w.y = split2<false, FIRST>(v[2], v[3]);
+    w.z = split2<false, FIRST>(v[4], v[5]);
+    w.w = split2<false, FIRST>(v[6], v[7]);
+    return w;
+}
+// eight values as N parts of 16 bytes; the third of an infinite one is NaN, as infinity - infinity
 template <int N, typename T> __device__ __forceinline__ void split8(const Eight<T> &e, uint4 (&out)[N]) {
     if constexpr (N == 1) {
         out[0] = e.u[0];
@@ -191,13 +211,9 @@ template <int N, typename T> __device__ __forceinline__ void split8(const Eight<
         float v[8];
         unpack16<T>(e.u[0], v);
         if constexpr (sizeof(T) == 4) unpack16<T>(e.u[1], v + 4);
+        out[0] = split_part<sizeof(T) == 4>(v);
 #pragma unroll
-        for (int p = 0; p < N; ++p) {
-            out[p].x = split2<false>(v[0], v[1]);
-            out[p].y = split2<false>(v[2], v[3]);
-            out[p].z = split2<false>(v[4], v[5]);
-            out[p].w = split2<false>(v[6], v[7]);
-        }
+        for (int p = 1; p < N; ++p) out[p] = split_part<false>(v);
     }
 }
 
@@ -278,8 +294,8 @@ __device__ __forceinline__ void write_vectors(const AdShrink &a, const AdOrder &
         uint2 *out = static_cast<uint2 *>(a.v) + ((tile.slot0 + r) * RP + j) / 4;
         for (int p = 0; p < a.parts; ++p) {
             uint2 w;
-            w.x = split2<true>(v[0], v[1]);
-            w.y = split2<true>(v[2], v[3]);
+            w.x = p == 0 ? split2<true, true>(v[0], v[1]) : split2<true, false>(v[0], v[1]);
+            w.y = p == 0 ? split2<true, true>(v[2], v[3]) : split2<true, false>(v[2], v[3]);
             out[p * (o.t * RP / 4)] = w;
         }
     }

@@ -165,6 +165,8 @@ __global__ void __launch_bounds__(AD_THREADS, Expand<TM, RP, TRANS>::blocks(!YW)
     const int q8 = lane >> 3, r8 = lane & 7;
     auto products = [&](auto parts, uint32_t bm, float (&acc)[2][4][4]) {
         constexpr int PV = decltype(parts)::value, MOST = PV == 2 ? 1 : 2;
+        // y of 16 bits has no values so near the end of the range (8192 rows, 4096 to 4096 FP16, rank 64: a call of 147 us, 152 with the least first)
+        constexpr bool LEAST_FIRST = PV == 3;
         // two blocks on an SM, 16-bit values and eight values of y ahead: the parts one by one, as registers end
         // (8192 x 4096 FP16, rank 64: 123 us, 135 with all at once; rank 16: 61, 69)
         constexpr int UNROLLED = S::blocks(!YW) == 2 && YW && S::PM < 3 ? 1 : PV;
@@ -184,13 +186,15 @@ __global__ void __launch_bounds__(AD_THREADS, Expand<TM, RP, TRANS>::blocks(!YW)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) columns(k, q, 2 * j, held[q][j]);
 #pragma unroll UNROLLED
-            for (int p = 0; p < PV; ++p) {
+            for (int ip = 0; ip < PV; ++ip) {
+                const int p = LEAST_FIRST ? PV - 1 - ip : ip;
                 uint32_t fa[2][4];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     ldsm_x4(base + p * S::V_BYTES + (wm * 32 + i * 16 + (q8 & 1) * 8 + r8) * S::LV + (k + (q8 >> 1) * 8) * 2, fa[i]);
 #pragma unroll
-                for (int q = 0; q < S::PM; ++q) {
+                for (int iq = 0; iq < S::PM; ++iq) {
+                    const int q = LEAST_FIRST ? S::PM - 1 - iq : iq;
                     if (p + q > MOST) continue;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {

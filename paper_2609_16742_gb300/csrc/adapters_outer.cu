@@ -139,13 +139,13 @@ __global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kerne
                 for (int i = 0; i < 2; ++i)
                     ldsm_x4_t(bx + p * S::X_BYTES + (k + (q8 >> 1) * 8 + r8) * S::LX + (wm * 32 + i * 16 + (q8 & 1) * 8) * 2, fa[p][i]);
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {
-                if (q >= a.parts) break;
+            for (int q = 2; q >= 0; --q) {
+                if (q >= a.parts) continue;
                 if constexpr (RP == 16) {
                     uint32_t b[4];
                     ldsm_x4_t(bv + q * S::V_BYTES + (k + (q8 & 1) * 8 + r8) * S::LV + wn * 16, b);
 #pragma unroll
-                    for (int p = 0; p < S::PX; ++p)
+                    for (int p = S::PX - 1; p >= 0; --p)
                         if (p + q <= most)
 #pragma unroll
                             for (int i = 0; i < 2; ++i) mma16<false>(acc[i][0], fa[p][i], b[0], b[1]);
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kerne
                         uint32_t b[4];
                         ldsm_x4_t(bv + q * S::V_BYTES + (k + (q8 & 1) * 8 + r8) * S::LV + (wn * (RP / 2) + j * 8 + (q8 >> 1) * 8) * 2, b);
 #pragma unroll
-                        for (int p = 0; p < S::PX; ++p)
+                        for (int p = S::PX - 1; p >= 0; --p)
                             if (p + q <= most)
 #pragma unroll
                                 for (int i = 0; i < 2; ++i) {

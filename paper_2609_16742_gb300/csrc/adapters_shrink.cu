@@ -31,6 +31,9 @@ template <typename TX, typename TM, int RP, bool TRANS> struct Shrink {
     static constexpr int FLUSH = 4;
 };
 
+// the i-th part to take of n: FP32's three from the least on
+__device__ __forceinline__ constexpr int least(int i, int n) { return n == 3 ? 2 - i : i; }
+
 template <typename TX, typename TM, int RP, bool TRANS>
 __device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o, const AdRows &tile, int rank, int splits, unsigned char *sm) {
     using S = Shrink<TX, TM, RP, TRANS>;
@@ -141,13 +144,14 @@ __device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o,
             if constexpr (RP == 16) {
                 // one 8-column tile a warp: both halves of k by lanes 0 to 15's addresses
 #pragma unroll
-                for (int q = 0; q < S::PM; ++q) {
+                for (int iq = 0; iq < S::PM; ++iq) {
+                    const int q = least(iq, S::PM);
                     uint32_t b[4];
                     if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + wn * 16, b);
                     else ldsm_x4(bm + q * S::M_BYTES + (wn * 8 + r8) * S::LM + (k + (q8 & 1) * 8) * 2, b);
 #pragma unroll
-                    for (int p = 0; p < S::PX; ++p)
-                        if (p + q <= 2)
+                    for (int ip = 0; ip < S::PX; ++ip)
+                        if (const int p = least(ip, S::PX); p + q <= 2)
 #pragma unroll
                             for (int i = 0; i < 2; ++i) mma16<S::F16>(acc[i][0], fa[p][i], b[0], b[1]);
                 }
@@ -155,14 +159,15 @@ __device__ __forceinline__ void shrink_tile(const AdShrink &a, const AdOrder &o,
 #pragma unroll
                 for (int j = 0; j < S::NT; j += 2)
 #pragma unroll
-                    for (int q = 0; q < S::PM; ++q) {
+                    for (int iq = 0; iq < S::PM; ++iq) {
+                        const int q = least(iq, S::PM);
                         uint32_t b[4];
                         const int n = wn * (RP / 2) + j * 8 + (q8 >> 1) * 8;
                         if constexpr (TRANS) ldsm_x4_t(bm + q * S::M_BYTES + (k + (q8 & 1) * 8 + r8) * S::LM + n * 2, b);
                         else ldsm_x4(bm + q * S::M_BYTES + (n + r8) * S::LM + (k + (q8 & 1) * 8) * 2, b);
 #pragma unroll
-                        for (int p = 0; p < S::PX; ++p)
-                            if (p + q <= 2)
+                        for (int ip = 0; ip < S::PX; ++ip)
+                            if (const int p = least(ip, S::PX); p + q <= 2)
 #pragma unroll
                                 for (int i = 0; i < 2; ++i) {
                                     mma16<S::F16>(acc[i][j], fa[p][i], b[0], b[1]);

@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
         if (warp == 0 && tc::elect_one()) {
             fence_after();
             const uint32_t bm = mb + (b % S::STAGES) * S::M_BYTES;
-            for (int p = 0; p < a.parts; ++p)
+            for (int p = a.parts - 1; p >= 0; --p)
 #pragma unroll
                 for (int k = 0; k < RP / 16; ++k) {
                     // 16 values along the rank: 32 bytes of a row, in the next block of 64 after four
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(AD_THREADS) expand_tc_kernel(const AdExpand a,
                     const uint64_t da = operand(av, 16, 8 * VT::ROW, VT::SWIZZLE);
                     const uint64_t db = TRANS ? operand(bm + 16 * k * 128, RP * 128, 1024, SW128)
                                               : operand(bm + (k >> 2) * S::COLS * 128 + (k & 3) * 32, 16, 8 * MT::ROW, MT::SWIZZLE);
-                    tc::umma_f16(tmem + (b & 1) * S::COLS, da, db, how, p > 0 || k > 0);
+                    tc::umma_f16(tmem + (b & 1) * S::COLS, da, db, how, p < a.parts - 1 || k > 0);
                 }
             tc::umma_commit(bar + 8 * (b & 1));
         }

@@ -1,11 +1,10 @@
 """Adapters and their gradients at the ends of their ranges: nothing of the rank, many rows of one adapter, very long
-rows, memory that is shared,
-versions."""
+rows, memory that is shared, tensors' versions, the largest values."""
 import pytest
 
 import _adapt as ref
 from _gpu import ct
-from test_gpu_adapters import check_grad, like, made
+from test_gpu_adapters import check, check_grad, like, made
 
 pytestmark = pytest.mark.gpu
 
@@ -145,3 +144,52 @@ def test_results_in_place_raise_the_tensors_versions():
         z = torch.zeros(4, 24, device="cuda")
         c.ct_adapters(z, x[:4].clone(), a, b, ids[:4].clone(), scale)
     c.ct_adapters(z, x[:4], a, b, ids[:4], scale)                       # no version to raise
+
+
+@pytest.mark.parametrize("xt,wt", [("float32", "float32"), ("float32", "float16"), ("float32", "bfloat16")])
+@pytest.mark.parametrize("t", [6, 300])
+def test_the_largest_values_stay_finite(t, xt, wt):
+    """The largest finite FP32 values are nearer to infinity than to any smaller BF16 value: their products with small numbers are finite."""
+    import torch
+    c, k, n, rank = ct(), 40, 24, 4
+    top = torch.finfo(torch.float32).max
+    small, a, b, ids, scale = made(t, k, n, rank, 3, xt, wt)
+    ids.clamp_(min=0)
+    x = small.clone()
+    x[:, 3], x[1, 7], x[:, 11] = top, -top, top * (1 - 2.0 ** -9)
+    a *= 2.0 ** -10
+    b *= 2.0 ** -10
+    for yt in ("float32", wt) if wt != "float16" else ("float32",):
+        y = like(t, n, yt, 1)
+        got = c.ct_adapters(y.clone(), x, a, b, ids, scale)
+        assert got.isfinite().all()
+        check(y, x, a, b, ids, scale, False, got)
+    small_dy = like(t, n, "float32", 3) * 2.0 ** -20
+    dy = small_dy.clone()
+    dy[2, 5], dy[:, 9] = -top, top
+    dx = like(t, k, "float32", 4)
+    for g, h in ((dy, small * 2.0 ** -20), (small_dy, x)):
+        got = c.ct_adapters_grad(g, h, a, b, ids, scale, dx=dx.clone(), grad_dtype=torch.float32)
+        assert all(v.isfinite().all() for v in got)
+        check_grad(g, h, a, b, ids, scale, dx, got)
+
+
+@pytest.mark.parametrize("t", [6, 300])
+def test_the_largest_weights_and_vectors_stay_finite(t):
+    import torch
+    c, k, n, rank = ct(), 40, 24, 4
+    top = torch.finfo(torch.float32).max
+    x = torch.zeros(t, k, device="cuda")
+    x[:, 3] = 1.0
+    x[1, 3] = -1.0
+    a = like(rank, k, "float32", 1).view(1, rank, k) * 2.0 ** -10
+    a[0, 1, 3], a[0, 2, 3] = top, -top                  # v is as large
+    b = like(n, rank, "float32", 2).view(1, n, rank) * 2.0 ** -10
+    y = like(t, n, "float32", 1)
+    got = c.ct_adapters(y.clone(), x, a, b)
+    assert got.isfinite().all()
+    check(y, x, a, b, None, None, False, got)
+    dy, dx = like(t, n, "float32", 3) * 2.0 ** -20, torch.zeros(t, k, device="cuda")
+    got = c.ct_adapters_grad(dy, x, a, b, dx=dx.clone())
+    assert all(g.isfinite().all() for g in got)
+    check_grad(dy, x, a, b, None, None, dx, got)
