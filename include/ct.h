@@ -604,7 +604,7 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
  *   scale_dev FP32 [adapters] or NULL (1).
  *   act: ReLU that keeps NaN (relu != 0), or none.
  * x_dtype is `dtype` or CT_DT_F32; rank <= CT_MAX_RANK, adapters <=
- * CT_MAX_ADAPTERS.  NaN and infinities stay in
+ * CT_MAX_ADAPTERS, t <= 2^31 - 2^16, k and n < 2^31.  NaN and infinities stay in
  * their row, or in the rows of their adapter; what an infinity gives may be NaN.
  * y may be x; it must share no value with B or the ids.
  * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row, shared

@@ -460,8 +460,10 @@ inline bool matrix_ok(const void *p, int64_t ld, int64_t rows, int64_t cols, int
     if (rows == 0 || cols == 0) return true;
     return p != nullptr && aligned(p, es) && (rows == 1 || ld >= cols);
 }
+// slots are counted in 32 bits, up to a few tiles and steps past the last
+constexpr int64_t ROWS_MOST = ((int64_t)1 << 31) - (1 << 16);
 inline bool sizes_ok(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n) {
-    return t >= 0 && t <= INT32_MAX && adapters >= 0 && adapters <= CT_MAX_ADAPTERS && rank >= 0 && rank <= CT_MAX_RANK && k >= 0 &&
+    return t >= 0 && t <= ROWS_MOST && adapters >= 0 && adapters <= CT_MAX_ADAPTERS && rank >= 0 && rank <= CT_MAX_RANK && k >= 0 &&
            k <= INT32_MAX && n >= 0 && n <= INT32_MAX;
 }
 inline int64_t tiles_of(int64_t t, int64_t adapters, bool ordered) {
