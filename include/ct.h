@@ -608,8 +608,7 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
  * their row, or in the rows of their adapter; what an infinity gives may be NaN.
  * y may be x; it must share no value with B or the ids.
  * Errors: CT_EINVAL (types, null or misaligned pointers, pitches below a row, shared
- * memory),
- * CT_ERANGE (sizes, rank), CT_ENOMEM (workspace), CT_ECUDA. */
+ * memory), CT_ERANGE (sizes, rank), CT_ENOMEM (workspace), CT_ECUDA. */
 #define CT_MAX_RANK 128
 #define CT_MAX_ADAPTERS 65534
 ct_status ct_adapters_workspace(int64_t t, int64_t adapters, int64_t rank, int64_t k, int64_t n, size_t *bytes);
@@ -647,7 +646,8 @@ ct_status ct_adapters_grad(const void *dy_dev, int32_t dy_dtype, int64_t lddy, c
  *   dst = src * min(1, max_norm / norm),  rounded once to its type.
  * tensors: host array of n ct_tensor (copied by the call): rows x cols values with
  * row pitches; dst == src with the same pitch: in place, and nothing is written where
- * the factor is 1.  Tensors must not overlap one another.  norms_dev FP32 [n],
+ * the factor is 1.  Tensors must share no value with one another (other rows or
+ * columns of one matrix are fine).  norms_dev FP32 [n],
  * norm_dev FP32 [1].  Sums are FP32 over at most 1024 values, then FP64; squares
  * that leave FP32's range are scaled.  A norm that is NaN or, in FP32, infinite
  * scales nothing: values stay as they are (dst gets a copy), the norms tell.

@@ -294,20 +294,17 @@ inline bool tensor_ok(const ct_tensor &t) {
            (t.rows == 1 || (t.ld_src >= t.cols && t.ld_dst >= t.cols));
 }
 
-// bytes from a tensor's first value to behind its last
-struct Range {
-    uintptr_t from, to;
-    int64_t row, pitch;                           // bytes
-};
-
-// whether two ranges touch: side by side as columns of one matrix is fine
-bool overlap(std::vector<Range> &v) {
-    std::sort(v.begin(), v.end(), [](const Range &a, const Range &b) { return a.from < b.from; });
-    for (size_t i = 0; i < v.size(); ++i)
-        for (size_t j = i + 1; j < v.size() && v[j].from < v[i].to; ++j) {
-            const int64_t pitch = v[i].pitch, off = (int64_t)((v[j].from - v[i].from) % (uintptr_t)(pitch > 0 ? pitch : 1));
-            if (pitch == 0 || pitch != v[j].pitch || off < v[i].row || off + v[j].row > pitch) return true;
+// whether two tensors have a value in common: side by side as columns of one matrix, which many may be, is seen without a look at their rows
+bool overlap(std::vector<Span> &v) {
+    std::sort(v.begin(), v.end(), [](const Span &a, const Span &b) { return a.at < b.at; });
+    for (size_t i = 0; i < v.size(); ++i) {
+        const uintptr_t end = v[i].end();
+        for (size_t j = i + 1; j < v.size() && v[j].at < end; ++j) {
+            const int64_t pitch = v[i].pitch, off = (int64_t)((v[j].at - v[i].at) % (uintptr_t)(pitch > 0 ? pitch : 1));
+            if (pitch > 0 && pitch == v[j].pitch && off >= v[i].width && off + v[j].width <= pitch) continue;
+            if (share(v[i], v[j])) return true;
         }
+    }
     return false;
 }
 
@@ -389,19 +386,15 @@ extern "C" ct_status ct_clip_grads(const ct_tensor *tensors, int64_t n, int32_t 
     if (workspace_dev == nullptr || !aligned(workspace_dev, 16)) return CT_EINVAL;
     if (workspace_bytes < sizeof(Part) * (size_t)(blocks_most(n, total) + 1)) return CT_ENOMEM;
     try {
-        std::vector<Range> v;
+        std::vector<Span> v;
         v.reserve(2 * (size_t)n);
         for (int64_t i = 0; i < n; ++i) {
             const ct_tensor &t = tensors[i];
             if (t.rows == 0 || t.cols == 0) continue;
-            const int64_t size = dtype_size((int)t.dtype), rows = t.rows - 1;
-            const auto range = [&](const void *p, int64_t ld) {
-                const uintptr_t at = (uintptr_t)p;
-                v.push_back({at, at + (uintptr_t)((rows * ld + t.cols) * size), t.cols * size, rows > 0 ? ld * size : 0});
-            };
-            range(t.dst, t.ld_dst);
-            if (t.src != t.dst) range(t.src, t.ld_src);
-            else if (rows > 0 && t.ld_src != t.ld_dst) return CT_EINVAL;
+            const int size = dtype_size((int)t.dtype);
+            v.push_back(span(t.dst, t.rows, t.cols, t.ld_dst, size));
+            if (t.src != t.dst) v.push_back(span(t.src, t.rows, t.cols, t.ld_src, size));
+            else if (t.rows > 1 && t.ld_src != t.ld_dst) return CT_EINVAL;
         }
         if (overlap(v)) return CT_EINVAL;
     } catch (const std::exception &) {
