@@ -132,9 +132,11 @@ def draw_answers(draft_logits, target_logits, seed=0, temperature=None):
     rows, n = target_logits.shape
     g = torch.Generator(device=target_logits.device).manual_seed(seed)
     draft_logits = draft_logits.to(target_logits.dtype)
-    heat = 1.0 if temperature is None else temperature[:, None].clamp(min=1e-6)
+    # drafts are drawn from what they are verified by; below 1e-30 the most probable class is taken
+    heat = 1.0 if temperature is None else temperature[:, None].clamp(min=1e-30)
     first = torch.empty(rows, n, device=draft_logits.device).exponential_(generator=g)
-    drafts = (draft_logits.float() / heat - torch.log(first)).argmax(dim=1)
+    x = draft_logits.float()
+    drafts = ((x - x.amax(dim=1, keepdim=True)) / heat - torch.log(first)).argmax(dim=1)
     noise = torch.empty(rows, n, device=draft_logits.device).exponential_(generator=g)
     uniform = torch.rand(rows, device=draft_logits.device, generator=g)
     # each row is a sequence of one draft; the row after it, which a longer answer would go on from, is the same again
