@@ -351,11 +351,6 @@ __device__ __forceinline__ float few_get(const void *p, int dtype, int64_t i) {
            : dtype == CT_DT_F16 ? to_f32(static_cast<const __half *>(p)[i])
                                 : to_f32(static_cast<const __nv_bfloat16 *>(p)[i]);
 }
-__device__ __forceinline__ void few_put(void *p, int dtype, int64_t i, float v) {
-    if (dtype == CT_DT_F32) static_cast<float *>(p)[i] = v;
-    else if (dtype == CT_DT_F16) static_cast<__half *>(p)[i] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v);
-}
 
 // y = act(y + B v): a thread for each column.  The ids and the matrix do not hang on the kernel before, which has itself waited for
 // all before it: they are on their way before its end is waited for.
@@ -422,7 +417,7 @@ template <typename TM> __global__ void __launch_bounds__(FEW_COLS) few_expand_ke
             if (!mine || r >= nr) break;
             float v = acc[r] + add[r];
             if (a.relu) v = v < 0.f ? 0.f : v;
-            few_put(a.y, a.y_dtype, rows[r0 + r] * a.ldy + c, out ? __uint_as_float(0x7FC00000u) : v);
+            put_as(a.y, a.y_dtype, rows[r0 + r] * a.ldy + c, out ? __uint_as_float(0x7FC00000u) : v);
         }
     }
 }

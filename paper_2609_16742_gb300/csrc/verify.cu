@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(THREADS, 2) verify_draw_kernel(const VerifyArg
 
 inline int64_t rows_of(int64_t sequences, int64_t drafts) { return 2 * drafts + sequences; }
 // Values of a piece: the warps of a few rows share them in pieces of 2048 (two batches of 16-bit values); where there are many rows, longer
-// pieces leave less to join.
+// pieces leave less to join.  (152: a GB300's SMs; the workspace's size hangs on no device.)
 inline int64_t per_of(int64_t rows, int64_t vocab) {
     int64_t per = 2048;
     while (per < 8192 && rows * ((vocab + per - 1) / per) > 32 * 152) per *= 2;
