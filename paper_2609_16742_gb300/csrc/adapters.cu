@@ -5,8 +5,8 @@
 //   u[t] = scale[i] B[i]^T dy[t],  dx[t] += A[i]^T u[t],
 //   dA[i] = sum_t u[t] x[t]^T,  dB[i] = sum_t dy[t] v[t]^T
 //
-// v and u carry more than 16 bits: they are short, and rounding them would cost the result
-// as much as its own rounding does.
+// v and u carry at least 16 bits: they are short, and rounding them to a result's 8 or 11 would cost it as much
+// as its own rounding does.
 //
 // Many rows are put in the order of their adapters first (one CTA: a counting sort, two where there are more than 254
 // adapters), then go through the tensor cores in tiles of 128 rows of one adapter (adapters_shrink.cu,

@@ -6,6 +6,7 @@
 // for each value and part of v.  A CTA takes 128 columns of one adapter's rows, 64 rows at a time: both operands lie in
 // shared memory with the summed rows along their own rows, as the transposing matrix loads want them.  A cluster's CTAs
 // share the rows and add their sums in rank order, so every sum has one order.
+// Of each 16 rows, the products of the least parts are added first.
 //
 // What comes here: FP32 and FP16 values (several parts), rows that start anywhere, and three parts of a rank above 64.  Bound by instructions
 // and their latency: three adapters of rank 20 over 1777 rows take 21 us for 5003 FP16 columns, 19 us for 2999 FP32 ones.
@@ -127,8 +128,10 @@ __global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kerne
                     acc[i][j][e] = 0.f;
                 }
     };
-    const int q8 = lane >> 3, r8 = lane & 7, most = a.parts == 2 ? 1 : 2;
-    auto compute = [&](int buf) {
+    const int q8 = lane >> 3, r8 = lane & 7;
+    // the number of v's parts is fixed in the loop (FP32 rank 128, 8192 rows, 2048 columns twice: 305 us, 323 where it is not)
+    auto compute_as = [&](auto parts, int buf) {
+        constexpr int PV = decltype(parts)::value, most = PV == 2 ? 1 : 2;
         const uint32_t bx = base + buf * buf_bytes, bv = bx + S::PX * S::X_BYTES;
 #pragma unroll
         for (int k = 0; k < AD_STEP; k += 16) {
@@ -139,8 +142,7 @@ __global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kerne
                 for (int i = 0; i < 2; ++i)
                     ldsm_x4_t(bx + p * S::X_BYTES + (k + (q8 >> 1) * 8 + r8) * S::LX + (wm * 32 + i * 16 + (q8 & 1) * 8) * 2, fa[p][i]);
 #pragma unroll
-            for (int q = 2; q >= 0; --q) {
-                if (q >= a.parts) continue;
+            for (int q = PV - 1; q >= 0; --q) {
                 if constexpr (RP == 16) {
                     uint32_t b[4];
                     ldsm_x4_t(bv + q * S::V_BYTES + (k + (q8 & 1) * 8 + r8) * S::LV + wn * 16, b);
@@ -167,6 +169,10 @@ __global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kerne
             }
             if constexpr (S::EACH) flush();
         }
+    };
+    auto compute = [&](int buf) {
+        if (a.parts == 2) compute_as(std::integral_constant<int, 2>(), buf);
+        else compute_as(std::integral_constant<int, 3>(), buf);
     };
     if (s0 < s1) {
         fetch(s0);
@@ -218,8 +224,8 @@ template <typename TX> cudaError_t by_rank(const AdOuters &two, int blocks, cons
 }
 // Adapters of a few rows each: a tile's start and end would cost more than its products.  A thread has a column, eight of the rank at a
 // time, and adds in FP32 row by row; as all rows may be one adapter's, 64 of them go into a sum, 8 of those into the next, and those into the
-// last.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 70 us
-// for both gradients; the whole call takes 332 us, 424 with tiles here.
+// last.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 76 us
+// for both gradients, 73 with one sum; the whole call takes 300 us, 346 with tiles here.
 constexpr int FEW_COLS = 256, FEW_ROWS = 64, FEW_BLOCKS = 8;
 template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int rp) {
     __shared__ float vs[FEW_ROWS][8];
