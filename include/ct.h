@@ -593,7 +593,8 @@ ct_status ct_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, co
  *   y[t] = act( y[t] + scale[i] B[i] (A[i] x[t]) ),  i = ids[t]
  * with FP32 sums and one rounding to y's type; the short vectors A x go on from
  * the first product to the second with 16 significant bits at least where y has 16
- * bits, with 24 where it has 32.
+ * bits, with 24 where it has 32, and an FP32 B counts with as many (values below
+ * 2^-110 keep fewer: steps end at 2^-133).
  *   y_dev [t, n] (y_dtype, pitch ldy), x_dev [t, k] (x_dtype, pitch ldx).
  *   a_dev, b_dev (both `dtype`): A[i] is [rank, k], its rows a_row apart, one
  *     adapter a_adapter after another; B[i] is [n, rank], rows b_row apart,
@@ -622,7 +623,8 @@ ct_status ct_adapters(void *y_dev, int32_t y_dtype, int64_t ldy, const void *x_d
  * dy [t, n] of its output:
  *   v = A[i] x[t],  u = scale[i] B[i]^T dy[t]  for every row t of adapter i = ids[t]
  *   dA[i] = sum_t u x[t]^T,  dB[i] = scale[i] sum_t dy[t] v^T,  dx[t] += A[i]^T u
- * with FP32 sums, rounded once (v and u go on as above, by the results' types).
+ * with FP32 sums, rounded once (v, u and FP32 values of x, dy and A go on as above,
+ * by the results' types).
  * dy_dev is `dtype` or CT_DT_F32 (pitch lddy).
  *   dx_dev [t, k] (dx_dtype, pitch lddx) or NULL: added to in place (the shared
  *     projection's part, or zeros).  Rows without an adapter are left as they

@@ -19,7 +19,9 @@ learn for N steps to answer as the protected network does (their gradients are
 clipped to a norm of 1).  With --draw an answer is drawn instead of taken: the
 8-bit head drafts a class for each image and the protected network's
 probabilities decide whether it stands, so that what is answered is distributed as
-the protected network's answers are.
+the protected network's answers are.  That shows how ct_verify_drafts is called; with the
+protected network's logits at hand for one answer an image, a draw from them would
+do, and drafts save time only where several of them go before one run of the target.
 """
 import argparse
 import os

@@ -9,7 +9,7 @@
 // Of each 16 rows, the products of the least parts are added first.
 //
 // What comes here: FP32 and FP16 values (several parts), rows that start anywhere, and three parts of a rank above 64.  Bound by instructions
-// and their latency: three adapters of rank 20 over 1777 rows take 21 us for 5003 FP16 columns, 19 us for 2999 FP32 ones.
+// and their latency: three adapters of rank 20 over 1777 rows take 21 us for 5003 FP16 columns, 16 us for 2999 FP32 ones.
 #include "adapters.cuh"
 
 namespace ct {
@@ -29,8 +29,8 @@ template <typename TX, int RP> struct Outer {
     // x's values are several parts.
     static constexpr bool EACH = PX > 1;
     static constexpr int FLUSH = 2;
-    // Ranks to 32: one buffer and two blocks on an SM, which wait for their rows in turn (8192 rows, 6144 FP32 columns, rank 16: 214 us,
-    // 272 with two buffers and one block).  Above, the sums' registers leave room for one block.
+    // Ranks to 32: one buffer and two blocks on an SM, which wait for their rows in turn (8192 rows, 6144 FP32 columns twice, rank 16:
+    // 163 us, 316 with two buffers and one block).  Above, the sums' registers leave room for one block.
     static constexpr int BLOCKS = RP <= 32 ? 2 : 1, BUFFERS = BLOCKS == 2 ? 1 : 2;
     static int smem(int parts) {
         const int all = BUFFERS * (PX * X_BYTES + parts * V_BYTES);
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(AD_THREADS, Outer<TX, RP>::BLOCKS) outer_kerne
                 }
     };
     const int q8 = lane >> 3, r8 = lane & 7;
-    // the number of v's parts is fixed in the loop (FP32 rank 128, 8192 rows, 2048 columns twice: 305 us, 323 where it is not)
+    // the number of v's parts is fixed in the loop (FP32 rank 128, 8192 rows, 2048 to 2048: a call of 662 us, 680 where it is not)
     auto compute_as = [&](auto parts, int buf) {
         constexpr int PV = decltype(parts)::value, most = PV == 2 ? 1 : 2;
         const uint32_t bx = base + buf * buf_bytes, bv = bx + S::PX * S::X_BYTES;
@@ -224,8 +224,8 @@ template <typename TX> cudaError_t by_rank(const AdOuters &two, int blocks, cons
 }
 // Adapters of a few rows each: a tile's start and end would cost more than its products.  A thread has a column, eight of the rank at a
 // time, and adds in FP32 row by row; as all rows may be one adapter's, 64 of them go into a sum, 8 of those into the next, and those into the
-// last.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 76 us
-// for both gradients, 73 with one sum; the whole call takes 300 us, 346 with tiles here.
+// last.  414 rows of 44 adapters, 9924 and 21143 columns, rank 16, BF16: 97 us
+// for both gradients, 91 with one sum; the whole call takes 300 us, 346 with tiles here.
 constexpr int FEW_COLS = 256, FEW_ROWS = 64, FEW_BLOCKS = 8;
 template <typename TX> __global__ void __launch_bounds__(FEW_COLS) few_outer_kernel(const __grid_constant__ AdOuters two, const AdOrder o, int rp) {
     __shared__ float vs[FEW_ROWS][8];

@@ -7,7 +7,7 @@
 // parts, as the next products take it.
 //
 // What comes here has gone through registers: FP32 rows, rows that start anywhere or end within 16 bytes.  Bound by instructions and their
-// latency, with few warps an SM: 1777 rows of 5003 FP16 values at rank 20 take 18.6 us, of 2999 FP32 ones 20 us.
+// latency, with few warps an SM: 1777 rows of 5003 FP16 values at rank 20 take 16 us, of 2999 FP32 ones 19 us.
 #include "adapters.cuh"
 
 namespace ct {
